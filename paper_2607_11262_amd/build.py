@@ -28,7 +28,10 @@ KERNELS = (("gts_sim.hip", (), "gts_sim.o"),
            ("gts_window.hip", ("-DGTS_WINDOW_PART=1",), "gts_window1.o"),
            ("gts_window.hip", ("-DGTS_WINDOW_PART=2",), "gts_window2.o"),
            ("gts_team.hip", (), "gts_team.o"),
-           ("gts_noalloc.hip", (), "gts_noalloc.o"))
+           ("gts_noalloc.hip", (), "gts_noalloc.o"),
+           ("gts_rotary.hip", (), "gts_rotary.o"),
+           ("gts_attention.hip", (), "gts_attention.o"))
+HOST = ("gts_host.cpp", "gts_ops_host.cpp")
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include"]
 
 
@@ -45,8 +48,10 @@ def build(verbose: bool = True) -> str:
         o = os.path.join(BUILD, obj)
         jobs.append([HIPCC, *DEVICE_FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", o])
         objs.append(o)
-    host_o = os.path.join(BUILD, "gts_host.o")
-    jobs.append([HIPCC, *HOST_FLAGS, "-x", "c++", "-c", os.path.join(CSRC, "gts_host.cpp"), "-o", host_o])
+    for src in HOST:
+        o = os.path.join(BUILD, src.replace(".cpp", ".o"))
+        jobs.append([HIPCC, *HOST_FLAGS, "-x", "c++", "-c", os.path.join(CSRC, src), "-o", o])
+        objs.append(o)
     # the sources compile independently: all at once
     procs = []
     for cmd in jobs:
@@ -56,7 +61,7 @@ def build(verbose: bool = True) -> str:
     if failed:
         raise subprocess.CalledProcessError(1, failed[0])
     tmp = OUT + f".tmp{os.getpid()}"
-    _run([HIPCC, "-shared", f"--offload-arch={ARCH}", "-fPIC", "-o", tmp, *objs, host_o])
+    _run([HIPCC, "-shared", f"--offload-arch={ARCH}", "-fPIC", "-o", tmp, *objs])
     os.replace(tmp, OUT)
     return OUT
 
@@ -68,7 +73,7 @@ def build_host_sanitized(out: str) -> str:
     Load it into a process started with the sanitizer runtimes preloaded."""
     cmd = ["g++", "-O1", "-g", "-std=c++17", "-fPIC", "-shared", "-fsanitize=address,undefined",
            "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer", "-D__HIP_PLATFORM_AMD__",
-           "-I/opt/rocm/include", os.path.join(CSRC, "gts_host.cpp"), os.path.join(CSRC, "gts_host_only.cpp"),
+           "-I/opt/rocm/include", *(os.path.join(CSRC, src) for src in HOST), os.path.join(CSRC, "gts_host_only.cpp"),
            "-L/opt/rocm/lib", "-lamdhip64", "-o", out]
     _run(cmd)
     return out

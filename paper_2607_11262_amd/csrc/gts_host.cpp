@@ -1054,6 +1054,8 @@ int check_fixed_scratch(const gts_graph* g, uint32_t B, uint64_t limit) {
   return GTS_OK;
 }
 int report_hip(hipError_t e, const char* what) { return fail(GTS_E_HIP, "%s: %s", what, hipGetErrorString(e)); }
+int report(int code, const char* message) { return fail(code, "%s", message); }
+void clear_error() { g_last_error.clear(); }
 }  // namespace gts
 
 extern "C" {

@@ -7,11 +7,19 @@
 
 #include "../../include/gts.h"
 #include "gts_dev.h"
+#include "gts_ops.h"
 
 namespace gts {
 hipError_t launch_sim(const Launch&, uint32_t, hipStream_t) { return hipErrorNoDevice; }
 hipError_t launch_window(const Launch&, uint32_t, hipStream_t) { return hipErrorNoDevice; }
 hipError_t launch_team(const Launch&, uint32_t, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_rotary(const gts_rotary_args&, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_rotary_table(float*, uint32_t, uint32_t, const TableFreqs&, double, hipStream_t) {
+  return hipErrorNoDevice;
+}
+hipError_t launch_append(const gts_append_args&, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_attention(const gts_attention_args&, hipStream_t) { return hipErrorNoDevice; }
+uint64_t attention_scratch(uint32_t, uint32_t, uint32_t, uint32_t, uint32_t) { return 0; }
 }  // namespace gts
 
 extern "C" int gts_simulate_hwset_noalloc(const gts_graph*, const gts_hwset*, uint32_t, uint32_t, uint32_t*,

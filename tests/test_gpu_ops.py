@@ -1,0 +1,581 @@
+"""The serving-step operators against their formulas in 64 bits: rotary
+positions with their gradient, the paged append, and attention over the cache
+with and without a shared prefix -- at the sizes, strides, masks and values where
+they can go wrong."""
+import pytest
+import torch
+
+import ops_reference as R
+from paper_2607_11262_amd import api, ops
+
+pytestmark = pytest.mark.gpu
+
+BF, HF, F = torch.bfloat16, torch.float16, torch.float32
+
+
+def randn(gen, *shape, dtype=F, scale=1.0):
+    return (torch.randn(shape, generator=gen) * scale).to(dtype)
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def note(msg):
+    print(f"[gpu] {msg}", flush=True)
+
+
+def close(got, ref, bound, what):
+    got = got.detach().cpu().double()
+    bad = ~((got - ref).abs() <= bound) & ~((got == ref))
+    if bad.any():
+        i = tuple(int(x) for x in bad.nonzero()[0])
+        raise AssertionError(f"{what}: {int(bad.sum())} of {bad.numel()} outside; at {i}: {got[i]} for {ref[i]} +- {bound[i]}")
+
+
+# ---- rotary -----------------------------------------------------------------------
+
+def test_table():
+    for dim, scaling in ((2, None), (6, {"kind": "linear", "factor": 4}), (64, {"kind": "ntk", "factor": 8}),
+                         (128, {"kind": "ramp", "factor": 16, "original": 4096}), (512, None)):
+        note(f"table {dim} {scaling}")
+        f, m = ops.rotary_frequencies(dim, scaling=scaling)
+        t = ops.rotary_table(301, dim, scaling=scaling).cpu().double()
+        angle = torch.arange(301, dtype=torch.float64)[:, None] * torch.tensor(f, dtype=torch.float64)
+        ref = torch.cat((angle.cos(), angle.sin()), 1) * m
+        assert ((t - ref).abs() <= 1.001 * R.E * ref.abs() + 1e-12).all()
+    # far positions keep their angle: it is never rounded to 32 bits
+    t = ops.rotary_table(1_000_003, 16).cpu().double()
+    f, _ = ops.rotary_frequencies(16)
+    angle = 1_000_002 * torch.tensor(f, dtype=torch.float64)
+    assert ((t[-1] - torch.cat((angle.cos(), angle.sin()))).abs() < 1e-7).all()
+
+
+ROTARY = [
+    # type, B, S, H, D, R, interleaved
+    (BF, 2, 5, 3, 128, 128, False), (BF, 2, 5, 3, 128, 128, True), (HF, 1, 1, 1, 2, 2, False),
+    (HF, 3, 7, 5, 80, 40, False), (HF, 3, 7, 5, 80, 40, True), (F, 2, 3, 7, 80, 32, True), (F, 1, 33, 2, 96, 96, False),
+    (BF, 1, 9, 2, 10, 6, False), (F, 2, 2, 3, 14, 10, True), (BF, 4, 1, 32, 128, 64, False), (HF, 1, 3, 2, 512, 512, True),
+    (BF, 1, 129, 40, 64, 64, False), (F, 1, 2, 1, 512, 2, False),
+]
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("dtype,B,S,H,D,rot,inter", ROTARY)
+def test_rotary(dtype, B, S, H, D, rot, inter, backward):
+    note(f"rotary {dtype} {B}x{S}x{H}x{D} rot {rot} interleaved {inter} backward {backward}")
+    g = gen(B * 1000 + S * 10 + H + D)
+    x = randn(g, B, S, H, D, dtype=dtype)
+    pos = torch.randint(0, 5000, (B, S), generator=g)
+    table = ops.rotary_table(5000, rot, scaling={"kind": "linear", "factor": 3})
+    ref, size = R.rotate(x.double(), table.cpu().double()[pos], inter, backward)
+    f = ops.rotary_backward if backward else ops.rotary
+    y = f(x.cuda(), pos.cuda(), table, interleaved=inter)
+    close(y, ref, R.rotation_bound(ref, size, dtype), "y")
+    if rot < D:
+        assert torch.equal(y[..., rot:].cpu(), x[..., rot:])
+    # 32-bit positions, one row for every batch entry
+    y1 = f(x.cuda(), pos[0].int().cuda(), table, interleaved=inter)
+    ref, size = R.rotate(x.double(), table.cpu().double()[pos[:1]], inter, backward)
+    close(y1, ref, R.rotation_bound(ref, size, dtype), "shared positions")
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_rotary_layouts(inter):
+    """Strides, alignments and orders other than a fresh tensor's."""
+    g = gen(3)
+    B, S, H, D = 2, 6, 4, 64
+    table = ops.rotary_table(64, D)
+    pos = torch.randint(0, 64, (B, S), generator=g).cuda()
+    dense = randn(g, B, S, H, D, dtype=BF).cuda()
+    ref = ops.rotary(dense, pos, table, interleaved=inter)
+    heads_first = dense.transpose(1, 2).contiguous().transpose(1, 2)
+    assert torch.equal(ops.rotary(heads_first, pos, table, interleaved=inter), ref)
+    packed = torch.randn(B, S, H + 3, D, device="cuda").to(BF)
+    packed[:, :, 1:H + 1] = dense
+    before = packed.clone()
+    view = packed[:, :, 1:H + 1]
+    assert torch.equal(ops.rotary(view, pos, table, interleaved=inter), ref)
+    # each alignment down to one element
+    for shift in (1, 2, 4):
+        wide = torch.zeros(B, S, H, D + 8, device="cuda", dtype=BF)
+        off = wide[..., shift:shift + D]
+        off.copy_(dense)
+        assert torch.equal(ops.rotary(off, pos, table, interleaved=inter), ref), shift
+    # a table and positions that are views
+    t2 = torch.zeros(64, D + 1, device="cuda")[:, 1:]
+    t2.copy_(table)
+    p2 = torch.zeros(B, S, 2, device="cuda", dtype=torch.int64)[..., 1]
+    p2.copy_(pos)
+    assert torch.equal(ops.rotary(dense, p2, t2, interleaved=inter), ref)
+    # in place, inside the packed tensor: nothing else changes
+    out = ops.rotary(view, pos, table, interleaved=inter, out=view)
+    assert out is view and torch.equal(view, ref)
+    before[:, :, 1:H + 1] = ref
+    assert torch.equal(packed, before)
+    # an expanded input
+    one = dense[:1].expand(B, S, H, D)
+    assert torch.equal(ops.rotary(one, pos, table, interleaved=inter),
+                       ops.rotary(one.contiguous(), pos, table, interleaved=inter))
+    # [tokens, heads, D]
+    flat = ops.rotary(dense.flatten(0, 1), pos.flatten(), table, interleaved=inter)
+    assert torch.equal(flat, ref.flatten(0, 1))
+
+
+def test_rotary_edges():
+    table = ops.rotary_table(10, 8)
+    x = torch.ones(4, 1, 12, device="cuda", dtype=BF)
+    y = ops.rotary(x, torch.tensor([-1, 0, 9, 10], device="cuda"), table)
+    assert y[[0, 3], :, :8].isnan().all() and not y[[1, 2]].isnan().any() and (y[..., 8:] == 1).all()
+    assert torch.equal(y[1], x[1])  # position 0
+    for shape in ((0, 3, 12), (3, 0, 12)):
+        assert ops.rotary(x.new_zeros(shape), torch.zeros(shape[0], device="cuda", dtype=torch.int32), table).shape == shape
+    # infinities and NaN stay in their own pairs
+    x = torch.zeros(1, 2, 8, device="cuda")
+    x[0, 0, 1], x[0, 1, 6] = float("inf"), float("nan")
+    y = ops.rotary(x, torch.tensor([3], device="cuda"), table)
+    hit = torch.zeros(1, 2, 8, dtype=torch.bool)
+    hit[0, 0, [1, 5]] = hit[0, 1, [2, 6]] = True
+    assert torch.equal(~y.isfinite().cpu(), hit)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_rotary_gradient(inter):
+    """Against the formula's transposed rotation and against differences of the
+    64-bit formula, through autograd, with broadcast inputs and gradients."""
+    g = gen(8)
+    B, S, H, D, rot = 3, 4, 5, 24, 16
+    table = ops.rotary_table(100, rot, scaling={"kind": "ramp", "factor": 4, "original": 32})
+    pos = torch.randint(0, 100, (B, S), generator=g)
+    x, dy = randn(g, B, S, H, D), randn(g, B, S, H, D)
+    leaf = x.cuda().requires_grad_()
+    y = ops.rotary(leaf, pos.cuda(), table, interleaved=inter)
+    (dx,) = torch.autograd.grad(y, leaf, dy.cuda())
+    rows = table.cpu().double()[pos]
+    ref, size = R.rotate(dy.double(), rows, inter, True)
+    close(dx, ref, R.rotation_bound(ref, size, F), "dx")
+    assert torch.equal(dx, ops.rotary_backward(dy.cuda(), pos.cuda(), table, interleaved=inter))
+    # differences: the map is linear, so a step of 1 has no error of its own
+    base, _ = R.rotate(x.double(), rows, inter)
+    for _ in range(12):
+        at = tuple(int(torch.randint(0, n, (1,), generator=g)) for n in x.shape)
+        step = x.double().clone()
+        step[at] += 1.0
+        slope = ((R.rotate(step, rows, inter)[0] - base) * dy.double()).sum()
+        assert abs(float(dx[at]) - float(slope)) <= 1e-6 * max(1.0, float(dy.abs().max()) * 2)
+    # the same gradient everywhere (an expanded tensor of ones), one input for
+    # all batch entries
+    leaf = x[:1].cuda().requires_grad_()
+    ops.rotary(leaf.expand(B, S, H, D), pos.cuda(), table, interleaved=inter).sum().backward()
+    ref, size = R.rotate(torch.ones(B, S, H, D, dtype=torch.float64), rows, inter, True)
+    close(leaf.grad, ref.sum(0, keepdim=True), 4 * R.rotation_bound(ref, size, F).sum(0, keepdim=True) + 1e-6, "broadcast")
+    with torch.no_grad():
+        assert not ops.rotary(leaf, pos[:1].cuda(), table).requires_grad
+
+
+# ---- append -----------------------------------------------------------------------
+
+def cache(g, n_pages, page, H, D, dtype, heads_first=False, fill=None):
+    shape = (n_pages, H, page, D) if heads_first else (n_pages, page, H, D)
+    pair = [randn(g, *shape, dtype=dtype) if fill is None else torch.full(shape, fill, dtype=dtype) for _ in range(2)]
+    return [x.transpose(1, 2) if heads_first else x for x in pair]
+
+
+def on_gpu(t):
+    """A copy with the same strides."""
+    out = torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device="cuda")
+    return out.copy_(t)
+
+
+APPEND = [
+    # type, Hq, Hkv, D, rot, page, counts, lens, prefix, interleaved, heads_first
+    (BF, 32, 8, 128, 128, 64, None, [1, 64, 65, 200], 0, False, False),
+    (BF, 4, 4, 64, 32, 16, [0, 3, 1, 20, 0], [5, 3, 17, 40, 0], 1000, True, True),
+    (HF, 9, 3, 80, 40, 16, [2, 2, 5], [2, 33, 5], 77, True, False),
+    (F, 2, 1, 10, 6, 1, [1, 4], [1, 9], 3, False, False),
+    (HF, 6, 2, 256, 256, 256, [300], [300], 0, False, True),
+    (BF, 1, 1, 2, 2, 8, [1] * 70, list(range(1, 71)), 5, False, False),
+    # fewer own keys than new tokens: the first ones have no place
+    (BF, 2, 2, 16, 16, 4, [5, 2], [3, 0], 9, False, False),
+]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,rot,page,counts,lens,prefix,inter,heads_first", APPEND)
+def test_append(dtype, Hq, Hkv, D, rot, page, counts, lens, prefix, inter, heads_first):
+    note(f"append {dtype} {Hq}/{Hkv}x{D} rot {rot} page {page} counts {counts and counts[:6]} lens {lens[:6]}")
+    g = gen(D + len(lens))
+    B = len(lens)
+    n = [1] * B if counts is None else counts
+    T = sum(n)
+    max_pages = max(-(-m // page) for m in lens) + 1
+    n_pages = B * max_pages + 3
+    kc, vc = cache(g, n_pages, page, Hkv, D, dtype, heads_first)
+    table_pages = torch.randperm(n_pages, generator=g)[:B * max_pages].view(B, max_pages).int()
+    k, v, q = (randn(g, T, h, D, dtype=dtype) for h in (Hkv, Hkv, Hq))
+    starts = None if counts is None else torch.tensor([0] + counts).cumsum(0).int()
+    tab = ops.rotary_table(prefix + max(lens) + 1, rot)
+    kg, vg = on_gpu(kc), on_gpu(vc)
+    qo = torch.full((T, Hq, D), 7.0, dtype=dtype, device="cuda")
+    got = ops.append_kv(k.cuda(), v.cuda(), kg, vg, table_pages.cuda(), torch.tensor(lens).int().cuda(),
+                        starts=None if starts is None else starts.cuda(), table=tab, interleaved=inter, prefix_len=prefix,
+                        q=q.cuda(), q_out=qo)
+    assert got is qo
+    rk, rv, rq = kc.double().clone(), vc.clone(), torch.full((T, Hq, D), 7.0, dtype=torch.float64)
+    bk, bq = torch.zeros_like(rk), torch.zeros_like(rq)
+    for b, (first, cnt) in enumerate(R.own_counts(B, T, starts)):
+        for i in range(cnt):
+            j = lens[b] - cnt + i
+            if j < 0:
+                continue
+            row = tab.cpu().double()[prefix + j]
+            p, s = int(table_pages[b, j // page]), j % page
+            y, size = R.rotate(k[first + i].double(), row, inter)
+            rk[p, s], bk[p, s] = y, R.rotation_bound(y, size, dtype)
+            rv[p, s] = v[first + i]
+            y, size = R.rotate(q[first + i].double(), row, inter)
+            rq[first + i], bq[first + i] = y, R.rotation_bound(y, size, dtype)
+    close(kg, rk, bk, "k_cache")
+    assert torch.equal(vg.cpu(), rv)
+    close(qo, rq, bq, "q")
+
+
+def test_append_without_rotation_and_bad_pages():
+    g = gen(1)
+    kc, vc = (x.cuda() for x in cache(g, 4, 4, 2, 8, BF))
+    k0, v0 = kc.clone(), vc.clone()
+    k, v = randn(g, 4, 2, 8, dtype=BF).cuda(), randn(g, 4, 2, 8, dtype=BF).cuda()
+    # page numbers outside the cache, and a key past the table: written nowhere
+    pages = torch.tensor([[2], [-1], [4], [0]], device="cuda", dtype=torch.int32)
+    lens = torch.tensor([3, 1, 1, 5], device="cuda", dtype=torch.int32)
+    assert ops.append_kv(k, v, kc, vc, pages, lens) is None
+    k0[2, 2], v0[2, 2] = k[0], v[0]
+    assert torch.equal(kc, k0) and torch.equal(vc, v0)
+    # a position past the rotary table: NaN, visibly
+    tab = ops.rotary_table(2, 8)
+    q = randn(g, 1, 4, 8, dtype=BF).cuda()
+    r = ops.append_kv(k[:1], v[:1], kc, vc, pages[:1], lens[:1], table=tab, q=q)
+    assert r.isnan().all() and kc[2, 2].isnan().all() and torch.equal(vc[2, 2], v[0])
+    # tokens of no sequence, and no tokens at all
+    starts = torch.tensor([0, 1, 1], device="cuda", dtype=torch.int32)
+    kc.copy_(k0)
+    ops.append_kv(k, v, kc, vc, pages[:2], lens[:2], starts=starts)
+    k0[2, 2] = k[0]
+    assert torch.equal(kc, k0)
+    ops.append_kv(k[:0], v[:0], kc, vc, pages[:2], lens[:2], starts=starts)
+    # queries in place
+    q2 = q.clone()
+    tab = ops.rotary_table(16, 4)
+    assert ops.append_kv(k[:1], v[:1], kc, vc, pages[:1], lens[:1], table=tab, q=q2, q_out=q2) is q2
+    assert torch.equal(q2, ops.rotary(q, lens[:1] - 1, tab))
+
+
+# ---- attention --------------------------------------------------------------------
+
+def attention_case(dtype, Hq, Hkv, D, page, counts, lens, prefix, heads_first=False, seed=0, fill=float("nan"), scale=None,
+                   size=1.0, spare_tokens=0, drop_pages=()):
+    """A batch over a cache whose unused slots hold `fill`, kernels against
+    the formula."""
+    g = gen(seed + D + len(lens))
+    B = len(lens)
+    n = [1] * B if counts is None else counts
+    T = sum(n) + spare_tokens
+    own_pages = [max(-(-m // page), 0) for m in lens]
+    max_pages = max(own_pages + [1])
+    n_prefix = -(-prefix // page)
+    n_pages = n_prefix + sum(own_pages) + 2
+    kc, vc = cache(g, n_pages, page, Hkv, D, dtype, heads_first, fill)
+    order = torch.randperm(n_pages, generator=g).tolist()
+    shared = order[:n_prefix]
+    table = torch.full((B, max_pages), -7, dtype=torch.int32)
+    at = n_prefix
+    for b, c in enumerate(own_pages):
+        table[b, :c] = torch.tensor(order[at:at + c], dtype=torch.int32)
+        at += c
+    for where, m in [(shared, prefix)] + [(table[b].tolist(), lens[b]) for b in range(B)]:
+        for j in range(m):
+            kc[where[j // page], j % page] = randn(g, Hkv, D, dtype=dtype, scale=size)
+            vc[where[j // page], j % page] = randn(g, Hkv, D, dtype=dtype)
+    for b, i in drop_pages:
+        table[b, i] = -1
+    q = randn(g, T, Hq, D, dtype=dtype, scale=size)
+    starts = None if counts is None else torch.tensor([0] + counts).cumsum(0).int()
+    lens_t = torch.tensor(lens).int()
+    shared_t = torch.tensor(shared).int() if n_prefix else None
+    ref = R.attention(q, kc, vc, table, lens_t, starts, shared_t, prefix, scale)
+    lse = torch.full((T, Hq), 3.0, device="cuda")
+    out = ops.shared_prefix_attention(q.cuda(), on_gpu(kc), on_gpu(vc), table.cuda(), lens_t.cuda(),
+                                      starts=None if starts is None else starts.cuda(),
+                                      prefix_pages=None if shared_t is None else shared_t.cuda(), prefix_len=prefix,
+                                      scale=scale, lse=lse, out=torch.full_like(q.cuda(), 5.0))
+    close(out, ref[0], ref[2], "out")
+    close(lse, ref[1], ref[3], "lse")
+    return out
+
+
+ATTENTION = {
+    "one key": (BF, 4, 2, 128, 64, None, [1], 0),
+    "one key of a prefix": (BF, 4, 2, 128, 64, None, [0], 1),
+    "decode": (BF, 32, 8, 128, 64, None, [1, 63, 64, 65, 127, 128, 129, 300], 0),
+    "decode, prefix": (BF, 8, 2, 128, 64, None, [5, 0, 200, 64], 333),
+    "decode, prefix of whole tiles": (BF, 4, 1, 128, 128, None, [128, 256], 256),
+    "decode float16": (HF, 14, 2, 96, 16, None, [7, 99, 200], 70),
+    "drafts": (BF, 14, 2, 96, 16, [1, 6, 3, 0, 5], [1, 6, 150, 9, 131], 100),
+    "drafts, heads first": (HF, 8, 8, 64, 32, [4, 4, 4], [4, 40, 133], 65),
+    "prompts": (BF, 4, 2, 64, 64, [70, 1, 130], [70, 1, 130], 200),
+    "prompts without a prefix": (HF, 5, 1, 128, 16, [33, 129], [40, 260], 0),
+    "chunk of a prompt": (BF, 2, 1, 128, 64, [150], [400], 0),
+    "many heads": (BF, 64, 1, 64, 16, None, [33, 90], 40),
+    "large head": (BF, 8, 2, 256, 32, [3, 1], [70, 200], 130),
+    "small head": (HF, 3, 3, 8, 8, [2, 1], [9, 30], 20),
+    "head of 16": (BF, 6, 2, 16, 4, None, [3, 50, 5], 33),
+    "odd head": (BF, 6, 2, 33, 4, None, [3, 50], 33),
+    "32 bits": (F, 6, 3, 64, 16, [1, 4], [40, 70], 50),
+    "page of one": (BF, 2, 1, 64, 1, None, [70, 3], 9),
+    "many sequences": (BF, 2, 1, 64, 16, None, [1 + (i * 37) % 90 for i in range(300)], 20),
+    "empty rows": (BF, 4, 2, 64, 16, [3, 1, 2, 0], [1, 0, 0, 50], 0),
+    "empty own part behind a prefix": (HF, 4, 2, 128, 16, [3, 1], [1, 0], 17),
+    "nothing anywhere": (BF, 4, 2, 128, 16, None, [0, 0], 0),
+}
+
+
+@pytest.mark.parametrize("name", ATTENTION)
+def test_attention(name):
+    note(f"attention: {name}")
+    attention_case(*ATTENTION[name], heads_first="heads first" in name)
+
+
+def test_attention_masked_values():
+    """What is masked never reaches a result, whatever it holds."""
+    for fill in (float("inf"), float("-inf"), float("nan"), torch.finfo(BF).min):
+        note(f"masked slots hold {fill}")
+        attention_case(BF, 8, 2, 128, 16, [2, 1, 3], [5, 37, 140], 33, fill=fill)
+
+
+def test_attention_later_tokens_hold_nothing_finite():
+    """Keys and values behind a token's own are masked for it even when
+    another row of the same tile sees them."""
+    g = gen(4)
+    for dtype in (BF, HF, F):
+        kc, vc = (x.cuda() for x in cache(g, 4, 16, 1, 64, dtype))
+        q = randn(g, 6, 4, 64, dtype=dtype).cuda()
+        pages = torch.tensor([[1, 3]], device="cuda", dtype=torch.int32)
+        lens = torch.tensor([20], device="cuda", dtype=torch.int32)
+        starts = torch.tensor([0, 6], device="cuda", dtype=torch.int32)
+        ref = ops.shared_prefix_attention(q, kc, vc, pages, lens, starts=starts)
+        for bad in (float("nan"), float("inf"), float("-inf")):
+            k1, v1 = kc.clone(), vc.clone()
+            k1[3, 1], v1[3, 1] = bad, bad  # own key 17: token 3's
+            out = ops.shared_prefix_attention(q, k1, v1, pages, lens, starts=starts)
+            note(f"token 3's key and value hold {bad} {dtype}")
+            assert torch.equal(out[:3], ref[:3]) and out[3:].isnan().all()
+            k1 = kc.clone()
+            out = ops.shared_prefix_attention(q, k1, v1, pages, lens, starts=starts)
+            assert torch.equal(out[:3], ref[:3]) and not out[3:].isfinite().any()
+
+
+def test_attention_values():
+    """Scores that differ by hundreds, one sharp key, scales of either sign."""
+    attention_case(BF, 4, 2, 128, 16, [2, 1], [90, 300], 150, size=8.0)
+    attention_case(HF, 4, 2, 64, 16, None, [90, 300], 150, size=8.0, scale=0.5)
+    attention_case(BF, 4, 2, 64, 16, None, [90, 130], 150, scale=-0.2)
+    attention_case(BF, 4, 2, 64, 16, None, [90, 130], 150, scale=0.0)
+
+
+def test_attention_missing_pages_and_spare_tokens():
+    attention_case(BF, 4, 2, 128, 16, [2, 1], [90, 300], 40, drop_pages=((0, 0), (1, 3), (1, 10), (1, 18)), seed=5)
+    attention_case(BF, 4, 2, 128, 16, None, [16], 0, drop_pages=((0, 0),))  # its only page
+    # tokens of no sequence get zeros
+    attention_case(HF, 4, 2, 64, 16, [2, 3], [90, 30], 40, spare_tokens=5)
+
+
+def test_attention_long_against_rows_of_parts():
+    """70001 own keys behind 40003 shared ones: the join of many parts; checked
+    on the GPU in 64 bits."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    D, H, page, P, L = 128, 2, 64, 40003, 70001
+    n = -(-P // page) + -(-L // page)
+    kc, vc = (torch.randn(n, page, H, D, generator=g, device="cuda", dtype=BF) for _ in range(2))
+    order = torch.randperm(n, generator=g, device="cuda").int()
+    shared, own = order[:-(-P // page)], order[-(-P // page):][None].contiguous()
+    q = torch.randn(2, 4, D, generator=g, device="cuda", dtype=BF) * 3
+    starts = torch.tensor([0, 2], device="cuda", dtype=torch.int32)
+    lens = torch.tensor([L], device="cuda", dtype=torch.int32)
+    out = ops.shared_prefix_attention(q, kc, vc, own, lens, starts=starts, prefix_pages=shared, prefix_len=P)
+    k = torch.cat((kc[shared.long()].flatten(0, 1)[:P], kc[own[0].long()].flatten(0, 1)[:L])).double()
+    v = torch.cat((vc[shared.long()].flatten(0, 1)[:P], vc[own[0].long()].flatten(0, 1)[:L])).double()
+    for i in range(2):
+        for h in range(4):
+            keys = P + L - 1 + i
+            s = k[:keys, h // 2] @ q[i, h].double() * D ** -0.5
+            w = s.softmax(0)
+            ref, spread = w @ v[:keys, h // 2], w @ v[:keys, h // 2].abs()
+            d = (D + 6) * R.E * (k[:keys, h // 2].abs() @ q[i, h].double().abs() * D ** -0.5).max()
+            assert ((out[i, h].double() - ref).abs() <= (2.01 * R.U[BF] + 2 * d + keys / 8 * R.E) * spread).all()
+
+
+def test_offsets_past_32_bits():
+    """Pages whose elements lie past 2^32 bytes and 2^31 elements: append and
+    attention agree with a small cache."""
+    g = gen(9)
+    page, H, D = 16, 2, 64
+    far = (1 << 31) // 2 + 1024  # elements between pages: page 3 starts past 2^31
+    buf = [torch.zeros(3 * far + page * H * D, dtype=BF, device="cuda") for _ in range(2)]
+    kc, vc = (b.as_strided((4, page, H, D), (far, H * D, D, 1)) for b in buf)
+    ks, vs = (torch.zeros(4, page, H, D, dtype=BF, device="cuda") for _ in range(2))
+    pages = torch.tensor([[3, 0, 2, 1]], device="cuda", dtype=torch.int32)
+    lens = torch.tensor([60], device="cuda", dtype=torch.int32)
+    starts = torch.tensor([0, 60], device="cuda", dtype=torch.int32)
+    k, v, q = (randn(g, 60, h, D, dtype=BF).cuda() for h in (H, H, 4))
+    tab = ops.rotary_table(60, D)
+    outs = []
+    for a, b in ((kc, vc), (ks, vs)):
+        qr = ops.append_kv(k, v, a, b, pages, lens, starts=starts, table=tab, q=q)
+        outs.append(ops.shared_prefix_attention(qr, a, b, pages, lens, starts=starts))
+    assert torch.equal(kc, ks) and torch.equal(vc, vs) and torch.equal(outs[0], outs[1])
+    assert outs[0].isfinite().all() and (outs[0] != 0).any()
+
+
+def step(state):
+    q = ops.append_kv(state["k"], state["v"], state["kc"], state["vc"], state["pages"], state["lens"], table=state["tab"],
+                      prefix_len=state["P"], q=state["q"])
+    return ops.shared_prefix_attention(q, state["kc"], state["vc"], state["pages"], state["lens"],
+                                       prefix_pages=state["shared"], prefix_len=state["P"])
+
+
+def decode_state(B=6, P=200, seed=1):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    page, H, D, Hq = 16, 2, 128, 8
+    n_prefix, per = -(-P // page), 8
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=BF)  # noqa: E731
+    return dict(P=P, kc=rnd(n_prefix + B * per, page, H, D), vc=rnd(n_prefix + B * per, page, H, D), k=rnd(B, H, D),
+                v=rnd(B, H, D), q=rnd(B, Hq, D), tab=ops.rotary_table(400, D),
+                shared=torch.arange(n_prefix, device="cuda", dtype=torch.int32),
+                pages=(n_prefix + torch.arange(B * per, device="cuda", dtype=torch.int32)).view(B, per),
+                lens=torch.arange(1, B + 1, device="cuda", dtype=torch.int32) * 15)
+
+
+def test_decode_steps_in_a_graph():
+    """The step captured once and replayed while the lengths grow, with eager
+    work between the replays, against the eager step."""
+    s = decode_state()
+    step(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(s)
+    for i in range(4):
+        s["lens"] += 1
+        for x in ("q", "k", "v"):
+            s[x].copy_(torch.randn_like(s[x]))
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = got.clone()
+        eager = step(s)
+        torch.cuda.synchronize()
+        note(f"replay {i}")
+        assert torch.equal(kept, eager)
+
+
+def test_another_stream():
+    """A step enqueued on a side stream, its inputs made and dropped on the
+    current one; calls of two states interleaved on two streams."""
+    a, b = decode_state(seed=1), decode_state(seed=2, P=0, B=9)
+    ra, rb = step(a), step(b)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = []
+    for _ in range(5):
+        for s, st in ((a, s1), (b, s2)):
+            st.wait_stream(torch.cuda.current_stream())
+            q = ops.append_kv(s["k"].clone(), s["v"].clone(), s["kc"], s["vc"], s["pages"], s["lens"], table=s["tab"],
+                              prefix_len=s["P"], q=s["q"].clone(), stream=st)
+            with torch.cuda.stream(st):
+                outs.append(ops.shared_prefix_attention(q, s["kc"], s["vc"], s["pages"], s["lens"],
+                                                        prefix_pages=s["shared"], prefix_len=s["P"]))
+    torch.cuda.synchronize()
+    for i, o in enumerate(outs):
+        assert torch.equal(o, rb if i % 2 else ra)
+
+
+def test_repeated_calls_agree():
+    """No atomics, no state between calls: the same bits each time, on a
+    scratch that holds another call's."""
+    s, t = decode_state(B=5, P=350), decode_state(B=3, P=30, seed=7)
+    need = ops.attention_scratch_bytes(5, 5, 8, 2, 128)
+    scratch = torch.full((need + 16,), 255, dtype=torch.uint8, device="cuda")
+    first = None
+    for _ in range(3):
+        out = ops.shared_prefix_attention(s["q"], s["kc"], s["vc"], s["pages"], s["lens"], prefix_pages=s["shared"],
+                                          prefix_len=s["P"], scratch=scratch)
+        ops.shared_prefix_attention(t["q"], t["kc"], t["vc"], t["pages"], t["lens"], prefix_pages=t["shared"],
+                                    prefix_len=t["P"], scratch=scratch)
+        first = out if first is None else first
+        assert torch.equal(out, first)
+
+
+# ---- refusals ---------------------------------------------------------------------
+
+def test_refusals():
+    """Every refused call raises and launches nothing."""
+    x = torch.zeros(2, 3, 4, 16, device="cuda", dtype=BF)
+    pos = torch.zeros(3, device="cuda", dtype=torch.int64)
+    tab = ops.rotary_table(8, 16)
+    bad = [
+        (ValueError, lambda: ops.rotary(x.cpu(), pos, tab)),
+        (ValueError, lambda: ops.rotary(x[..., ::2], pos, tab)),
+        (ValueError, lambda: ops.rotary(x[0, 0], pos, tab)),
+        (TypeError, lambda: ops.rotary(x.double(), pos, tab)),
+        (TypeError, lambda: ops.rotary(x, pos.float(), tab)),
+        (ValueError, lambda: ops.rotary(x, pos[:2], tab)),
+        (ValueError, lambda: ops.rotary(x, pos, ops.rotary_table(8, 32))),
+        (TypeError, lambda: ops.rotary(x, pos, tab.half())),
+        (TypeError, lambda: ops.rotary(x, pos, tab, out=x.half())),
+        (ValueError, lambda: ops.rotary(x, pos, tab, out=x[:1].expand_as(x))),
+        (api.GtsError, lambda: ops.rotary(x[..., :15], pos, tab[:, :14])),   # odd head
+        (api.GtsError, lambda: ops.rotary(x, pos, tab[:, :15])),             # odd part
+        (ValueError, lambda: ops.rotary_table(8, 7)),
+        (ValueError, lambda: ops.rotary_table(0, 8)),
+        (api.GtsError, lambda: ops.rotary_table(8, 514)),
+        (ValueError, lambda: ops.rotary_table(8, 8, scaling={"kind": "other"})),
+        (ValueError, lambda: ops.rotary_table(8, 8, scaling={"kind": "linear", "factor": 0.5})),
+        (ValueError, lambda: ops.rotary_table(8, 8, scaling={"kind": "ramp", "factor": 2})),
+        (ValueError, lambda: ops.rotary_table(8, 8, scaling={"kind": "ntk", "factor": 2, "original": 8})),
+    ]
+    kc, vc = (torch.zeros(3, 4, 2, 16, device="cuda", dtype=BF) for _ in range(2))
+    k, q = torch.zeros(2, 2, 16, device="cuda", dtype=BF), torch.zeros(2, 4, 16, device="cuda", dtype=BF)
+    pages, lens = torch.zeros(2, 1, device="cuda", dtype=torch.int32), torch.ones(2, device="cuda", dtype=torch.int32)
+    starts = torch.tensor([0, 1, 2], device="cuda", dtype=torch.int32)
+    odd = torch.zeros(3, 5, 2, 16, device="cuda", dtype=BF)
+    for f in (lambda q, kc, vc, p, n, **kw: ops.append_kv(k, k, kc, vc, p, n, **{**kw, **({} if q is None else {"q": q})}),
+              ops.shared_prefix_attention):
+        bad += [
+            (TypeError, lambda f=f: f(q, kc.half(), vc, pages, lens)),
+            (ValueError, lambda f=f: f(q, kc, vc[:2], pages, lens)),
+            (ValueError, lambda f=f: f(q, kc[..., :8], vc[..., :8], pages, lens)),
+            (TypeError, lambda f=f: f(q, kc, vc, pages.long(), lens)),
+            (TypeError, lambda f=f: f(q, kc, vc, pages, lens.long())),
+            (ValueError, lambda f=f: f(q, kc, vc, pages[:1], lens)),
+            (ValueError, lambda f=f: f(q, kc, vc, pages.cpu(), lens)),
+            (ValueError, lambda f=f: f(q, kc, vc, pages, lens, starts=starts[:2])),
+            (ValueError, lambda f=f: f(q, kc, vc, pages, lens, prefix_len=-1)),
+            (api.GtsError, lambda f=f: f(q, odd, odd, pages, lens)),                       # pages of 5
+            (api.GtsError, lambda f=f: f(q, kc, vc, pages.expand(2, 1)[:0], lens[:0])),    # no sequence
+        ]
+    bad += [
+        (api.GtsError, lambda: ops.append_kv(k, k, kc, vc, torch.cat([pages, pages[:1]]), torch.cat([lens, lens[:1]]))),
+        (ValueError, lambda: ops.append_kv(k, k[:1], kc, vc, pages, lens)),
+        (ValueError, lambda: ops.append_kv(k, k, kc, vc, pages, lens, q_out=q)),
+        (ValueError, lambda: ops.append_kv(k, k, kc[:1].expand_as(kc), vc, pages, lens)),
+        (api.GtsError, lambda: ops.shared_prefix_attention(q[:, :3], kc, vc, pages, lens)),  # 3 heads over 2
+        (api.GtsError, lambda: ops.shared_prefix_attention(q, kc, vc, pages, lens, prefix_len=1)),
+        (api.GtsError, lambda: ops.shared_prefix_attention(q, kc, vc, pages, lens, prefix_pages=lens, prefix_len=9)),
+        (api.GtsError, lambda: ops.shared_prefix_attention(q, kc, vc, pages, lens, scale=float("nan"))),
+        (ValueError, lambda: ops.shared_prefix_attention(q, kc, vc, pages, lens, lse=torch.zeros(2, 3, device="cuda"))),
+        (ValueError, lambda: ops.shared_prefix_attention(q, kc, vc, pages, lens, out=q[:1])),
+    ]
+    for i, (kind, f) in enumerate(bad):
+        with pytest.raises(kind):
+            f()
+            note(f"refusal {i} was not refused")
+    torch.cuda.synchronize()
+    assert (kc == 0).all()
