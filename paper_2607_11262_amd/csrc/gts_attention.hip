@@ -1,6 +1,19 @@
 // gts_attention.hip — attention of new tokens over a paged cache and the
 // prefix that all sequences share.
 //
+// Two kernels and a join.
+//
+// The tile kernel takes 16-bit caches whose rows can be loaded 16 bytes at a
+// time.  All work is cut into tiles of 64 keys of one key-value head against
+// up to 128 query rows (a row: one new token's one query head).  For the
+// prefix the rows are those of all tokens of the batch, so its keys are read
+// once for everybody; for a sequence's own keys they are its tokens'.  The
+// tiles of all (head, rows) segments stand in one line, and each workgroup
+// takes an equal stretch of it, wherever that starts and ends: ragged lengths
+// and few rows fill the chip alike.  A stretch leaves one partial result per
+// segment it touches (unnormalised sum, running maximum and sum of the
+// softmax, 32 bits), and the join adds up the partials of each row.
+//
 // The row kernel: one wavefront per (token, query head) walks the row's keys 64
 // at a time, one key a lane, with the running maximum and sum of the softmax;
 // the weighted values are summed with a lane per group of dims.  Takes every
@@ -12,23 +25,708 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr uint32_t kTile = 64;        // keys of a tile
+constexpr uint32_t kMostRows = 128;   // query rows of a segment
+constexpr uint32_t kGroups = 512;     // most workgroups: two a CU
 
 // What the kernels need beside the arguments.
 struct AttnParams {
   gts_attention_args a;
   uint32_t page_shift;
-  uint32_t group;  // query heads of a key-value head
+  uint32_t group;       // query heads of a key-value head
+  FastDiv by_group;
+  uint32_t workgroups;  // a multiple of 8
+  uint32_t part_rows;   // rows that a cut between workgroups may add to the partials
 };
 
-// Element offset of own or prefix key j in the cache (before the head), -1
-// when no page holds it.
-__device__ __forceinline__ int64_t key_page(const gts_attention_args& a, const int32_t* pages, uint32_t n, uint32_t shift,
+// Scratch: the plan (what the tile kernel's first workgroup leaves for the
+// join), then the partials: maximum and sum of each row, then its sums.
+struct Plan {
+  uint64_t tiles, per;  // all tiles; tiles of a workgroup
+  uint64_t prefix_tiles;
+};
+struct Scratch {
+  uint64_t begin, stats, sums, bytes;  // offsets; begin: [batch] first tile of each sequence
+};
+__host__ __device__ inline uint64_t up256(uint64_t x) { return (x + 255) & ~255ull; }
+__host__ __device__ inline Scratch scratch_layout(uint32_t batch, uint64_t rows, uint32_t part_rows, uint32_t dim) {
+  Scratch s;
+  s.begin = 256;
+  s.stats = s.begin + up256(8ull * batch);
+  const uint64_t n = 2 * rows + (uint64_t)part_rows * kGroups;
+  s.sums = s.stats + up256(8 * n);
+  s.bytes = s.sums + up256(4 * n * dim);
+  return s;
+}
+
+// Page of own or prefix key j, -1 when none holds it.
+__device__ __forceinline__ int32_t key_page(const gts_attention_args& a, const int32_t* pages, uint32_t n, uint32_t shift,
                                             uint32_t j) {
   const uint32_t at = j >> shift;
   if (at >= n) return -1;
   const int32_t p = pages[at];
   return p >= 0 && (uint32_t)p < a.cache.n_pages ? p : -1;
 }
+
+// ---- the tile kernel -------------------------------------------------------------
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+template <typename T>
+using Vec8 = T __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ f32x16 mfma(Vec8<__bf16> a, Vec8<__bf16> b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma(Vec8<_Float16> a, Vec8<_Float16> b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ uint32_t uni(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uni(uint64_t x) {
+  return ((uint64_t)uni((uint32_t)(x >> 32)) << 32) | uni((uint32_t)x);
+}
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+// The lane's number as a value of its own: what is computed from it stays where
+// it is used, instead of being kept in registers across the loops around.
+__device__ __forceinline__ uint32_t fresh_lane() {
+  uint32_t lane = threadIdx.x & 63u;
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+// The value of the lane 32 away joined with this lane's.
+__device__ __forceinline__ float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float add_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Rows of a segment's tile for n query rows: 32, 64 or 128, by how many of
+// the four waves take rows of their own (the others take other keys).
+__host__ __device__ __forceinline__ uint32_t row_groups(uint32_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+
+// New tokens and own keys of sequence b.
+struct Seq {
+  uint32_t first, n;  // first token, tokens
+  int64_t len;        // own keys by lens
+  uint32_t keys;      // of these, those that pages can hold
+};
+__device__ __forceinline__ Seq load_seq(const AttnParams& p, uint32_t b) {
+  const gts_kv_batch& kb = p.a.batch;
+  Seq s;
+  if (kb.starts) {
+    const int32_t s0 = kb.starts[b], s1 = kb.starts[b + 1];
+    const bool ok = s0 >= 0 && s1 > s0 && (uint32_t)s1 <= kb.tokens;
+    s.first = ok ? (uint32_t)s0 : 0;
+    s.n = ok ? (uint32_t)(s1 - s0) : 0;
+  } else {
+    s.n = kb.tokens / kb.batch;
+    s.first = b * s.n;
+  }
+  s.len = kb.lens[b];
+  const uint64_t cap = (uint64_t)kb.max_pages << p.page_shift;
+  const int64_t k = s.len < 0 || p.a.cache.n_pages == 0 ? 0 : s.len;
+  s.keys = (uint32_t)((uint64_t)k < cap ? (uint64_t)k : cap);
+  return s;
+}
+// Own keys that token i of the sequence sees.
+__device__ __forceinline__ uint32_t seen(const Seq& s, uint32_t i) {
+  const int64_t v = s.len - s.n + i + 1;
+  return v < 0 ? 0 : v < (int64_t)s.keys ? (uint32_t)v : s.keys;
+}
+// Tiles of the rt-th row tile of a sequence (rows rt * 32 rg ..): as far as
+// its last row sees.
+__device__ __forceinline__ uint32_t own_tiles(const AttnParams& p, const Seq& s, uint32_t rg, uint32_t rt) {
+  const uint32_t rows = s.n * p.group, end = (rt + 1) * 32 * rg;
+  const uint32_t last = p.by_group.div((rows < end ? rows : end) - 1);
+  return (seen(s, last) + kTile - 1) / kTile;
+}
+__device__ __forceinline__ uint64_t head_tiles(const AttnParams& p, const Seq& s) {
+  const uint32_t rows = s.n * p.group;
+  if (rows == 0 || s.keys == 0) return 0;
+  const uint32_t rg = row_groups(rows), n = (rows + 32 * rg - 1) / (32 * rg);
+  uint64_t t = 0;
+  for (uint32_t rt = 0; rt < n; ++rt) t += own_tiles(p, s, rg, rt);
+  return t;
+}
+
+// One stretch of one segment.
+struct Work {
+  const int32_t* pages;
+  uint32_t n_pages, keys;    // keys: of the segment's last row
+  uint32_t head, rg, rows;   // key-value head, row groups, valid rows
+  uint32_t first_row;        // token * group + query head within the group
+  uint32_t tile, n_tiles;    // first tile and number of tiles of the stretch
+  uint32_t low;              // keys that its first row sees
+  int64_t see;               // row r sees see + token keys; own == false: all
+  bool own;
+  uint64_t part;             // first row of its partial
+};
+
+template <typename T, int DP>
+struct Tiles {
+  static constexpr int C = DP / 8;         // 16-byte chunks of a row
+  static constexpr int RPI = 64 / C;       // rows that one load of a wave covers
+  static constexpr int NL = 16 / RPI;      // loads of a wave for its 16 rows of a tile
+  static constexpr int KK = DP / 16;       // matrix steps over the head
+  static constexpr int MB = DP / 32;       // blocks of 32 output dims
+  static constexpr int N = kTile * DP;     // values of a tile of keys
+  // Chunk c of row r stands at c ^ swizzle(r): the 16-byte reads of 16 rows
+  // at one chunk (keys), and the reads of 4 rows x 64 bytes that are turned
+  // on the way (values), each touch all 64 banks once.
+  static __device__ __forceinline__ uint32_t swizzle_k(uint32_t r) { return C >= 16 ? r & 15 : (r >> 1) & 7; }
+  static __device__ __forceinline__ uint32_t swizzle_v(uint32_t r) {
+    return C >= 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 2) << 1) | ((r >> 2) & 3);
+  }
+};
+
+// What rows of a tile that do not exist are loaded from.
+__device__ __align__(16) const uint32_t g_zeros[4] = {0, 0, 0, 0};
+
+// Loads one tile of keys and values from the cache straight into LDS (no
+// registers in between, so nothing is held while the tile before is worked
+// on).  A wave loads 16 rows; rows past the segment's keys, or without a page,
+// become zeros.  Returns the wave's rows inside the segment that no page
+// holds (one bit each, the same in all lanes).
+template <typename T, int DP>
+struct Loader {
+  using L = Tiles<T, DP>;
+  int32_t page;  // page of the wave's rows of the next tile (pages of 16 or more)
+  uint32_t wave;
+
+  __device__ __forceinline__ void start(const AttnParams& p, const Work& w, uint32_t wave_) {
+    wave = wave_;
+    if (p.page_shift >= 4) page = key_page(p.a, w.pages, w.n_pages, p.page_shift, w.tile * kTile + wave * 16);
+  }
+
+  __device__ __forceinline__ uint32_t load(const AttnParams& p, const Work& w, uint32_t tile, T* sk, T* sv) {
+    typedef const __attribute__((address_space(1))) void* global_t;
+    typedef __attribute__((address_space(3))) void* lds_t;
+    const gts_kv_cache& kc = p.a.cache;
+    const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
+    const uint32_t j0 = tile * kTile + wave * 16;
+    const T* kh = (const T*)kc.k + (int64_t)w.head * kc.k_stride[2];
+    const T* vh = (const T*)kc.v + (int64_t)w.head * kc.v_stride[2];
+    uint32_t missing = 0;
+    const bool whole = p.page_shift >= 4;  // the wave's rows are of one page
+    if (whole) {
+      const uint32_t slot = j0 & (kc.page - 1);
+      const int64_t pg = page < 0 ? 0 : page;
+      kh += pg * kc.k_stride[0] + (int64_t)slot * kc.k_stride[1];
+      vh += pg * kc.v_stride[0] + (int64_t)slot * kc.v_stride[1];
+      if (page < 0) {
+        const uint32_t n = j0 < w.keys ? w.keys - j0 : 0;
+        missing = n < 16 ? (1u << n) - 1 : 0xFFFFu;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < L::NL; ++n) {
+      const uint32_t r = n * L::RPI + r0, j = j0 + r;
+      const uint32_t ck = c ^ L::swizzle_k(r), cv = c ^ L::swizzle_v(r);
+      bool ok = j < w.keys;
+      const T *kp, *vp;
+      if (whole) {
+        ok = ok && page >= 0;
+        kp = kh + (int64_t)r * kc.k_stride[1];
+        vp = vh + (int64_t)r * kc.v_stride[1];
+      } else {
+        const int32_t pg = ok ? key_page(p.a, w.pages, w.n_pages, p.page_shift, j) : 0;
+        const uint64_t lost = __ballot(ok && pg < 0);
+        for (int i = 0; i < L::RPI; ++i) missing |= (uint32_t)(lost >> (i * L::C) & 1) << (n * L::RPI + i);
+        ok = ok && pg >= 0;
+        const int64_t slot = j & (kc.page - 1);
+        kp = kh + (int64_t)pg * kc.k_stride[0] + slot * kc.k_stride[1];
+        vp = vh + (int64_t)pg * kc.v_stride[0] + slot * kc.v_stride[1];
+      }
+      kp = ok && ck * 8 < kc.dim ? kp + ck * 8 : (const T*)g_zeros;
+      vp = ok && cv * 8 < kc.dim ? vp + cv * 8 : (const T*)g_zeros;
+      const uint32_t at = (wave * 16 + n * L::RPI) * DP;
+      __builtin_amdgcn_global_load_lds((global_t)kp, (lds_t)(sk + at), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_t)vp, (lds_t)(sv + at), 16, 0, 0);
+    }
+    if (whole) page = key_page(p.a, w.pages, w.n_pages, p.page_shift, j0 + kTile);
+    return missing;
+  }
+};
+
+// Values of 8 keys at one dim, as the matrix instruction takes them: keys
+// key .. + 3 and key + 8 .. + 11 of this lane's half (the sum over keys may
+// take them in any order as long as the weights come in the same).
+template <typename T, int DP>
+__device__ __forceinline__ Vec8<T> load_v(const T* sv, uint32_t lane, uint32_t key, uint32_t mb) {
+  using L = Tiles<T, DP>;
+  const uint32_t g = lane / 16, r = 4 * (g / 2) + (lane % 16) / 4;  // key is a multiple of 16
+  const uint32_t c = (g % 2) * 2 + (lane % 4) / 2;
+  typedef __attribute__((address_space(3))) i16x4* lds_t;
+  union {
+    i16x4 h[2];
+    Vec8<T> v;
+  } u;
+  const T* at = sv + (key + r) * DP + (lane % 2) * 4;
+  u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(at + ((c ^ L::swizzle_v(r)) ^ (mb * 4)) * 8));
+  u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(at + 8 * DP + ((c ^ L::swizzle_v(r + 8)) ^ (mb * 4)) * 8));
+  return u.v;
+}
+
+// What a wave holds: 32 query rows against its keys.  Scores are computed as
+// keys x rows, so a lane has 16 of 32 keys of one row: maximum and sum need one
+// exchange with the lane 32 away, and the weights are already where the
+// second product (dims x rows) wants them.
+template <typename T, int DP>
+struct Rows {
+  using L = Tiles<T, DP>;
+  Vec8<T> q[L::KK];
+  f32x16 o[L::MB];
+  float m, l;  // reference maximum of q.k (unscaled), sum of this half's weights
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < L::MB; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+  }
+
+  // NS blocks of 32 keys from LDS row `key` on (key number j0 of the segment).
+  template <int NS>
+  __device__ __forceinline__ void step(uint32_t lane, const T* sk, const T* sv, uint32_t key, uint32_t j0, float c, bool mask,
+                                       uint64_t missing, bool odd, uint32_t sees) {
+    const uint32_t half = lane / 32;
+    f32x16 s[NS];
+    const uint32_t kc = half ^ L::swizzle_k(lane % 32);
+#pragma unroll
+    for (int b = 0; b < NS; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+    }
+#pragma unroll
+    for (int kk = 0; kk < L::KK; ++kk)
+#pragma unroll
+      for (int b = 0; b < NS; ++b)
+        s[b] = mfma(*(const Vec8<T>*)(sk + (key + b * 32 + lane % 32) * DP + (kc ^ (2 * kk)) * 8), q[kk], s[b]);
+    if (mask) {
+#pragma unroll
+      for (int b = 0; b < NS; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t r = b * 32 + 8 * (i / 4) + 4 * half + i % 4;
+          const bool ok = j0 + r < sees && !(missing >> (key + r) & 1);
+          s[b][i] = ok ? s[b][i] : -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NS; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+    mx = max_halves(mx);
+    // The reference follows the maximum only when that is 2^8 ahead: weights
+    // up to 256 are as exact, and sums and output are rescaled rarely.
+    if (__any((mx - m) * c > 8.f || (m == -INFINITY && mx > m))) {
+      const float m1 = fmaxf(m, mx);
+      const float alpha = m == -INFINITY ? 0.f : exp2_((m - m1) * c);
+      l *= alpha;
+#pragma unroll
+      for (int b = 0; b < L::MB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
+      m = m1;
+    }
+    const float base = m == -INFINITY ? 0.f : -m * c;
+    Vec8<T> pw[2 * NS];
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < NS; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float e = exp2_(__builtin_fmaf(s[b][i], c, base));
+        sum[i & 1] += e;
+        pw[2 * b + i / 8][i % 8] = (T)e;
+      }
+    l += sum[0] + sum[1];
+    if (NS == 1 && odd) {
+      odd_values<NS>(lane, sv, key, j0, sees, pw);
+      return;
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2 * NS; ++kb)
+#pragma unroll
+      for (int mb = 0; mb < L::MB; ++mb) o[mb] = mfma(load_v<T, DP>(sv, lane, key + kb * 16, mb), pw[kb], o[mb]);
+  }
+
+  // As the end of step(), for a tile in which some rows do not see every key
+  // and a value is not finite: 0 times it would reach the rows that must not
+  // see it.  The finite values are summed as usual; products of ones find
+  // the rows that see an infinity of either sign or a NaN (both).
+  template <int NS>
+  __device__ __forceinline__ void odd_values(uint32_t lane, const T* sv, uint32_t key, uint32_t j0, uint32_t sees,
+                                             const Vec8<T> (&pw)[2 * NS]) {
+#pragma unroll
+    for (int mb = 0; mb < L::MB; ++mb) {
+#pragma unroll
+      for (int kb = 0; kb < 2 * NS; ++kb) {
+        Vec8<T> v = load_v<T, DP>(sv, lane, key + kb * 16, mb);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __builtin_fabsf((float)v[i]) < INFINITY ? v[i] : (T)0.f;
+        o[mb] = mfma(v, pw[kb], o[mb]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int sign = 0; sign < 2; ++sign) {
+        f32x16 hits;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) hits[i] = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 2 * NS; ++kb) {
+          Vec8<T> v = load_v<T, DP>(sv, lane, key + kb * 16, mb), vis;
+          uint32_t first = j0 + kb * 16 + 4 * (lane / 32);
+          asm volatile("" : "+v"(first));
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float x = sign ? -(float)v[i] : (float)v[i];
+            v[i] = (T)(x < INFINITY ? 0.f : 1.f);  // NaN counts for both signs
+            vis[i] = (T)(first + 8 * (i / 4) + i % 4 < sees ? 1.f : 0.f);
+          }
+          hits = mfma(v, vis, hits);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[mb][i] += hits[i] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+};
+
+// Flags that the waves of a workgroup leave each other for a tile.
+struct Flags {
+  uint16_t missing[2][4];  // rows without a page
+  uint32_t odd[4];         // values that are not finite
+};
+
+template <typename T, int DP>
+__device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, T* s_kv, Flags* flags, float* stats,
+                                            float* sums) {
+  using L = Tiles<T, DP>;
+  const gts_attention_args& a = p.a;
+  const uint32_t lane = fresh_lane(), wave = uni(threadIdx.x >> 6), half = lane / 32;
+  const uint32_t rgroup = wave % w.rg, kgroup = wave / w.rg;
+  const uint32_t row = rgroup * 32 + lane % 32;
+  const bool valid = row < w.rows;
+  const uint32_t flat = w.first_row + (valid ? row : 0);
+  const uint32_t token = p.by_group.div(flat), gq = flat - token * p.group;
+  const float scale = a.scale;
+  const float c = scale == 0.f ? 1.f : __builtin_fabsf(scale) * kLog2e;
+
+  Loader<T, DP> ld;
+  ld.start(p, w, wave);
+  __syncthreads();  // LDS of the stretch before is free
+  const uint32_t missing0 = ld.load(p, w, w.tile, s_kv, s_kv + L::N);
+  if (lane == 0) flags->missing[0][wave] = (uint16_t)missing0;
+
+  Rows<T, DP> r;
+  r.clear();
+  {
+    // scale's sign (and 0) go into the queries: the maximum of q.k is then
+    // that of the scaled scores
+    const T* q = (const T*)a.q + (int64_t)token * a.q_stride[0] + (int64_t)(w.head * p.group + gq) * a.q_stride[1];
+#pragma unroll
+    for (int kk = 0; kk < L::KK; ++kk) {
+      const uint32_t d = kk * 16 + half * 8;
+      const bool in = valid && d < a.cache.dim;
+      u32x4 x = *(const u32x4*)(q + (in ? d : 0));
+      const uint32_t keep = in ? ~0u : 0u, flip = scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = (x[i] & keep) ^ flip;
+      if (scale == 0.f) x = u32x4{0, 0, 0, 0};
+      r.q[kk] = __builtin_bit_cast(Vec8<T>, x);
+    }
+  }
+  uint32_t sees = w.keys;
+  if (w.own) {
+    const int64_t v = w.see + token;
+    sees = !valid ? w.keys : v < 0 ? 0 : v < (int64_t)w.keys ? (uint32_t)v : w.keys;
+  }
+
+  // One tile is worked on while the next is on its way to the other half of
+  // the LDS; one barrier a tile.
+  for (uint32_t i = 0; i < w.n_tiles; ++i) {
+    const uint32_t tile = w.tile + i, j0 = tile * kTile;
+    T* sk = s_kv + (i & 1) * 2 * L::N;
+    T* sv = sk + L::N;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const uint64_t missing = uni(*(const uint64_t*)flags->missing[i & 1]);
+    if (i + 1 < w.n_tiles) {
+      T* next = s_kv + ((i + 1) & 1) * 2 * L::N;
+      const uint32_t miss = ld.load(p, w, tile + 1, next, next + L::N);
+      if (lane == 0) flags->missing[(i + 1) & 1][wave] = (uint16_t)miss;
+    }
+    const bool edge = j0 + kTile > w.low;  // some row does not see all of the tile
+    bool odd = false;
+    if (edge && w.low < w.keys) {
+      constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
+      bool found = false;
+      for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) {
+        const u32x4 v = *(const u32x4*)(sv + x * 8);
+        for (int y = 0; y < 4; ++y) found |= (v[y] & kExp) == kExp || (v[y] >> 16 & kExp) == kExp;
+      }
+      if (lane == 0) flags->odd[wave] = 0;
+      if (__any(found) && lane == 0) flags->odd[wave] = 1;
+      __syncthreads();
+      odd = uni(flags->odd[0] | flags->odd[1] | flags->odd[2] | flags->odd[3]);
+      __syncthreads();
+    }
+    const bool mask = edge || missing;
+    if (w.rg == 4 && !odd) {
+      r.template step<2>(fresh_lane(), sk, sv, 0, j0, c, mask, missing, false, sees);
+    } else if (w.rg != 1 || (i & 1) == kgroup / 2) {
+      // 2 or 4 key groups: halves of every tile, or of every second one
+#pragma unroll 1
+      for (uint32_t x = (kgroup & 1) * 32; x < kTile; x += w.rg == 4 ? 32 : kTile)
+        r.template step<1>(fresh_lane(), sk, sv, x, j0 + x, c, mask, missing, odd, sees);
+    }
+  }
+
+  // waves that took other keys of the same rows hand theirs to the first
+  r.l = add_halves(r.l);
+  if (w.rg < 4) {
+    constexpr int N = L::MB * 16 + 2;
+    static_assert(3 * N * 64 * 4 <= 4 * L::N * sizeof(T), "partials of three waves fit the tiles' LDS");
+    float* mine = (float*)s_kv + (wave - w.rg) * N * 64 + lane;
+    __syncthreads();
+    if (kgroup > 0) {
+#pragma unroll
+      for (int i = 0; i < L::MB * 16; ++i) mine[i * 64] = r.o[i / 16][i % 16];
+      mine[(N - 2) * 64] = r.m;
+      mine[(N - 1) * 64] = r.l;
+    }
+    __syncthreads();
+    if (kgroup == 0) {
+      for (uint32_t x = rgroup; x < 4 - w.rg; x += w.rg) {
+        const float* other = (const float*)s_kv + x * N * 64 + lane;
+        const float mo = other[(N - 2) * 64], lo = other[(N - 1) * 64];
+        const float m1 = fmaxf(r.m, mo);
+        const float fa = r.m == -INFINITY ? 1.f : exp2_((r.m - m1) * c);
+        const float fb = mo == -INFINITY ? 1.f : exp2_((mo - m1) * c);
+#pragma unroll
+        for (int i = 0; i < L::MB * 16; ++i) r.o[i / 16][i % 16] = r.o[i / 16][i % 16] * fa + other[i * 64] * fb;
+        r.l = r.l * fa + lo * fb;
+        r.m = m1;
+      }
+    }
+  }
+  if (kgroup == 0 && valid) {
+    const uint64_t at = w.part + row;
+    if (half == 0) {
+      stats[2 * at] = r.m * c;  // base 2 from here on
+      stats[2 * at + 1] = r.l;
+    }
+    float* dst = sums + at * a.cache.dim;
+#pragma unroll
+    for (int mb = 0; mb < L::MB; ++mb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t d = mb * 32 + 8 * i + 4 * half;
+        if (d < a.cache.dim)
+          *(float4*)(dst + d) = make_float4(r.o[mb][4 * i], r.o[mb][4 * i + 1], r.o[mb][4 * i + 2], r.o[mb][4 * i + 3]);
+      }
+  }
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams p) {
+  const gts_attention_args& a = p.a;
+  const uint32_t B = a.batch.batch, hkv = a.cache.heads, P = a.cache.n_pages ? a.batch.prefix_len : 0;
+  __shared__ __align__(16) T s_kv[4 * kTile * DP];
+  __shared__ uint64_t s_sum[256];
+  __shared__ uint64_t s_wave[4];
+  __shared__ __align__(8) Flags s_flags;
+  const uint32_t tid = threadIdx.x, lane = tid & 63u;
+
+  // The plan: tiles of every sequence, summed.  Thread i takes sequences
+  // [i per, (i + 1) per).
+  const uint32_t per_thread = (B + 255) / 256;
+  const uint32_t prows = a.batch.tokens * p.group;
+  const uint32_t prg = row_groups(prows), n_prt = (prows + 32 * prg - 1) / (32 * prg);
+  const uint32_t ptiles = (P + kTile - 1) / kTile;
+  const uint64_t prefix_tiles = (uint64_t)ptiles * n_prt * hkv;
+  uint64_t mine = 0;
+  for (uint32_t i = 0; i < per_thread; ++i) {
+    const uint32_t b = tid * per_thread + i;
+    if (b < B) mine += head_tiles(p, load_seq(p, b)) * hkv;
+  }
+  uint64_t scan = mine;
+  for (int i = 1; i < 64; i <<= 1) {
+    const uint64_t x = __shfl_up(scan, i);
+    if ((int)lane >= i) scan += x;
+  }
+  if (lane == 63) s_wave[tid >> 6] = scan;
+  __syncthreads();
+  uint64_t before = prefix_tiles;
+  for (uint32_t i = 0; i < tid >> 6; ++i) before += s_wave[i];
+  s_sum[tid] = before + scan - mine;  // first tile of this thread's sequences
+  const uint64_t total = uni(prefix_tiles + s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3]);
+  const uint64_t per = (total + p.workgroups - 1) / p.workgroups;
+  const uint64_t rows = (uint64_t)a.batch.tokens * a.q_heads;
+  const Scratch sc = scratch_layout(B, rows, p.part_rows, a.cache.dim);
+  char* scratch = (char*)a.scratch;
+  if (blockIdx.x == 0) {
+    uint64_t t = s_sum[tid];
+    for (uint32_t i = 0; i < per_thread; ++i) {
+      const uint32_t b = tid * per_thread + i;
+      if (b >= B) break;
+      ((uint64_t*)(scratch + sc.begin))[b] = t;
+      t += head_tiles(p, load_seq(p, b)) * hkv;
+    }
+    if (tid == 0) *(Plan*)scratch = Plan{total, per, prefix_tiles};
+  }
+  __syncthreads();
+
+  // neighbours in the line of tiles go to one XCD (workgroups go round the
+  // eight of them), whose L2 then has the keys that they share
+  const uint32_t g = (blockIdx.x & 7u) * (p.workgroups / 8) + (blockIdx.x >> 3);
+  uint64_t t = (uint64_t)g * per, end = t + per;
+  if (end > total) end = total;
+  while (t < end) {
+    Work w;
+    uint64_t seg, seg_tiles;  // first tile of the segment and its tiles
+    if (t < prefix_tiles) {
+      const uint32_t s = (uint32_t)(t / ptiles);
+      w.head = s / n_prt;
+      const uint32_t rt = s - w.head * n_prt;
+      seg = (uint64_t)s * ptiles;
+      seg_tiles = ptiles;
+      w.pages = a.prefix_pages;
+      w.n_pages = a.n_prefix_pages;
+      w.keys = w.low = P;
+      w.rg = prg;
+      w.first_row = rt * 32 * prg;
+      w.rows = prows - w.first_row < 32 * prg ? prows - w.first_row : 32 * prg;
+      w.own = false;
+      w.see = 0;
+      w.part = (uint64_t)w.head * prows + w.first_row;
+    } else {
+      // the last thread whose sequences start at or before t, then its
+      // sequences one by one (one, up to 256 sequences)
+      uint32_t who = 0;
+      for (uint32_t i = 0; i < 4; ++i) who += (uint32_t)__popcll(__ballot(s_sum[i * 64 + lane] <= t));
+      who = uni(who - 1);
+      uint32_t b = who * per_thread;
+      uint64_t first = uni(s_sum[who]);
+      Seq s = load_seq(p, b < B ? b : B - 1);
+      uint64_t ht = head_tiles(p, s);
+      for (uint32_t i = 1; i < per_thread && t >= first + ht * hkv; ++i) {
+        first += ht * hkv;
+        s = load_seq(p, ++b);
+        ht = head_tiles(p, s);
+      }
+      const uint64_t rel = t - first;
+      w.head = uni((uint32_t)(rel / ht));
+      uint32_t in = uni((uint32_t)(rel - w.head * ht));
+      w.rg = row_groups(s.n * p.group);
+      uint32_t rt = 0;
+      seg = first + w.head * ht;
+      seg_tiles = own_tiles(p, s, w.rg, 0);
+      while (in >= seg_tiles) {
+        in -= (uint32_t)seg_tiles;
+        seg += seg_tiles;
+        seg_tiles = own_tiles(p, s, w.rg, ++rt);
+      }
+      const uint32_t srows = s.n * p.group, r0 = rt * 32 * w.rg;
+      w.pages = a.batch.page_table + (int64_t)b * a.batch.table_stride;
+      w.n_pages = a.batch.max_pages;
+      w.rows = srows - r0 < 32 * w.rg ? srows - r0 : 32 * w.rg;
+      w.first_row = s.first * p.group + r0;
+      w.low = seen(s, p.by_group.div(r0));
+      w.keys = seen(s, p.by_group.div(r0 + w.rows - 1));
+      w.own = true;
+      w.see = s.len - s.n + 1 - (int64_t)s.first;
+      w.part = rows + (uint64_t)hkv * s.first * p.group + (uint64_t)w.head * srows + r0;
+    }
+    w.part += (uint64_t)p.part_rows * g;
+    w.tile = (uint32_t)(t - seg);
+    const uint64_t left = seg + seg_tiles - t;
+    w.n_tiles = (uint32_t)(end - t < left ? end - t : left);
+    run_stretch<T, DP>(p, w, s_kv, &s_flags, (float*)(scratch + sc.stats), (float*)(scratch + sc.sums));
+    t += w.n_tiles;
+  }
+}
+
+// The join: one wavefront a row adds up its partials.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
+  const gts_attention_args& a = p.a;
+  const uint32_t lane = threadIdx.x & 63u;
+  const uint64_t rows = (uint64_t)a.batch.tokens * a.q_heads, row = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= rows) return;
+  const uint32_t t = uni((uint32_t)(row / a.q_heads)), hq = uni((uint32_t)(row - (uint64_t)t * a.q_heads));
+  const uint32_t head = p.by_group.div(hq), gq = hq - head * p.group, hkv = a.cache.heads, D = a.cache.dim;
+  const Scratch sc = scratch_layout(a.batch.batch, rows, p.part_rows, D);
+  const char* scratch = (const char*)a.scratch;
+  const Plan plan = *(const Plan*)scratch;
+  const float* stats = (const float*)(scratch + sc.stats);
+  const float* sums = (const float*)(scratch + sc.sums);
+  float m = -INFINITY, l = 0.f;
+  float2 o[GTS_OPS_MAX_ATTN / 128] = {};
+  uint32_t seq, index, count;
+  if (find_sequence(a.batch, t, &seq, &index, &count)) {
+    for (int part = 0; part < 2; ++part) {
+      uint64_t first, n, at;  // tiles of the segment, its row in the partials
+      if (part == 0) {
+        const uint32_t P = a.cache.n_pages ? a.batch.prefix_len : 0;
+        n = (P + kTile - 1) / kTile;
+        const uint32_t prows = a.batch.tokens * p.group, rg = row_groups(prows);
+        const uint32_t r = t * p.group + gq, n_rt = (prows + 32 * rg - 1) / (32 * rg);
+        first = n * ((uint64_t)head * n_rt + r / (32 * rg));
+        at = (uint64_t)head * prows + r;
+      } else {
+        const Seq s = load_seq(p, seq);
+        const uint32_t srows = s.n * p.group, rg = row_groups(srows), r = index * p.group + gq, rt = r / (32 * rg);
+        if (s.keys == 0) continue;
+        first = ((const uint64_t*)(scratch + sc.begin))[seq] + head * head_tiles(p, s);
+        for (uint32_t i = 0; i < rt; ++i) first += own_tiles(p, s, rg, i);
+        n = own_tiles(p, s, rg, rt);
+        at = rows + (uint64_t)hkv * s.first * p.group + (uint64_t)head * srows + r;
+      }
+      if (n == 0) continue;
+      const uint64_t g1 = (first + n - 1) / plan.per;
+      for (uint64_t g = first / plan.per; g <= g1; ++g) {
+        const uint64_t x = at + p.part_rows * g;
+        const float mx = stats[2 * x], lx = stats[2 * x + 1];
+        const float m1 = fmaxf(m, mx);
+        const float fa = m == -INFINITY ? 1.f : exp2_(m - m1), fb = mx == -INFINITY ? 1.f : exp2_(mx - m1);
+        l = l * fa + lx * fb;
+        m = m1;
+#pragma unroll
+        for (uint32_t i = 0; i < GTS_OPS_MAX_ATTN / 128; ++i) {
+          const uint32_t d = i * 128 + lane * 2;
+          if (d < D) {
+            const float2 v = *(const float2*)(sums + x * D + d);
+            o[i].x = o[i].x * fa + v.x * fb;
+            o[i].y = o[i].y * fa + v.y * fb;
+          }
+        }
+      }
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* out = (T*)a.out + (int64_t)t * a.out_stride[0] + (int64_t)hq * a.out_stride[1];
+#pragma unroll
+  for (uint32_t i = 0; i < GTS_OPS_MAX_ATTN / 128; ++i) {
+    const uint32_t d = i * 128 + lane * 2;
+    if (d < D) *(Pack<T, 2>*)(out + d) = Pack<T, 2>{(T)(o[i].x * inv), (T)(o[i].y * inv)};
+  }
+  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// ---- the row kernel --------------------------------------------------------------
 
 template <typename T>
 __global__ __launch_bounds__(256) void row_kernel(AttnParams p) {
@@ -54,11 +752,11 @@ __global__ __launch_bounds__(256) void row_kernel(AttnParams p) {
     const uint32_t n_pages = part ? a.batch.max_pages : a.n_prefix_pages;
     for (uint32_t j0 = 0; j0 < n; j0 += 64) {
       const uint32_t j = j0 + lane;
-      const int64_t page = j < n ? key_page(a, pages, n_pages, p.page_shift, j) : -1;
+      const int32_t page = j < n ? key_page(a, pages, n_pages, p.page_shift, j) : -1;
       const uint32_t slot = j & (a.cache.page - 1);
       float s = -INFINITY;
       if (page >= 0) {
-        const T* k = (const T*)a.cache.k + page * a.cache.k_stride[0] + (int64_t)slot * a.cache.k_stride[1] +
+        const T* k = (const T*)a.cache.k + (int64_t)page * a.cache.k_stride[0] + (int64_t)slot * a.cache.k_stride[1] +
                      (int64_t)h * a.cache.k_stride[2];
         float acc = 0.f;
         for (uint32_t d = 0; d < D; ++d) acc += s_q[wave][d] * (float)k[d];
@@ -77,7 +775,7 @@ __global__ __launch_bounds__(256) void row_kernel(AttnParams p) {
       for (uint64_t todo = there; todo; todo &= todo - 1) {
         const int src = __builtin_ctzll(todo);
         const float wj = __shfl(w, src);
-        const int64_t pj = __shfl((int)page, src);
+        const int64_t pj = __shfl(page, src);
         const T* v = (const T*)a.cache.v + pj * a.cache.v_stride[0] +
                      (int64_t)((j0 + src) & (a.cache.page - 1)) * a.cache.v_stride[1] + (int64_t)h * a.cache.v_stride[2];
 #pragma unroll
@@ -101,22 +799,61 @@ __global__ __launch_bounds__(256) void row_kernel(AttnParams p) {
 
 }  // namespace
 
-uint64_t attention_scratch(uint32_t, uint32_t, uint32_t, uint32_t, uint32_t) { return 0; }
+// Rows that a cut may add: a segment's, at most all rows of a head.
+static uint32_t part_rows(uint32_t tokens, uint32_t group) {
+  const uint64_t rows = (uint64_t)tokens * group;
+  return rows > 64 ? kMostRows : rows > 32 ? 64 : 32;
+}
+
+uint64_t attention_scratch(uint32_t batch, uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t dim) {
+  return scratch_layout(batch, (uint64_t)tokens * q_heads, part_rows(tokens, q_heads / kv_heads), dim).bytes;
+}
+
+// The tile kernel's loads: 16-bit values, every row of q, k and v and every 16
+// bytes of it aligned to 16 bytes.
+static bool tiles_fit(const gts_attention_args& a) {
+  const gts_kv_cache& c = a.cache;
+  if (c.dtype == GTS_F32 || c.dim % 8 != 0) return false;
+  uint64_t bits = ((uint64_t)a.out_stride[0] | (uint64_t)a.out_stride[1]) % 2;
+  for (int i = 0; i < 3; ++i) bits |= (uint64_t)c.k_stride[i] | (uint64_t)c.v_stride[i];
+  for (int i = 0; i < 2; ++i) bits |= (uint64_t)a.q_stride[i];
+  const uint64_t addr = (uint64_t)(uintptr_t)a.q | (uint64_t)(uintptr_t)c.k | (uint64_t)(uintptr_t)c.v |
+                        (uint64_t)(uintptr_t)a.scratch | (uint64_t)(uintptr_t)a.out % 4 * 4;
+  return bits % 8 == 0 && addr % 16 == 0;
+}
+
+template <typename T>
+static hipError_t launch_typed(AttnParams& p, hipStream_t stream) {
+  const gts_attention_args& a = p.a;
+  const uint64_t rows = (uint64_t)a.batch.tokens * a.q_heads;
+  const dim3 grid((uint32_t)((rows + 3) / 4)), block(256);
+  if constexpr (sizeof(T) == 2) {
+    if (tiles_fit(a)) {
+      p.workgroups = a.cache.dim > 128 ? kGroups / 2 : kGroups;
+      if (a.cache.dim <= 64)
+        tile_kernel<T, 64><<<dim3(p.workgroups), block, 0, stream>>>(p);
+      else if (a.cache.dim <= 128)
+        tile_kernel<T, 128><<<dim3(p.workgroups), block, 0, stream>>>(p);
+      else
+        tile_kernel<T, 256><<<dim3(p.workgroups), block, 0, stream>>>(p);
+      join_kernel<T><<<grid, block, 0, stream>>>(p);
+      return hipGetLastError();
+    }
+  }
+  row_kernel<T><<<grid, block, 0, stream>>>(p);
+  return hipGetLastError();
+}
 
 hipError_t launch_attention(const gts_attention_args& a, hipStream_t stream) {
   AttnParams p{};
   p.a = a;
   p.page_shift = (uint32_t)__builtin_ctz(a.cache.page);
   p.group = a.q_heads / a.cache.heads;
-  const uint64_t rows = (uint64_t)a.batch.tokens * a.q_heads;
-  const dim3 grid((uint32_t)((rows + 3) / 4)), block(256);
-  if (a.cache.dtype == GTS_F32)
-    row_kernel<float><<<grid, block, 0, stream>>>(p);
-  else if (a.cache.dtype == GTS_BF16)
-    row_kernel<__bf16><<<grid, block, 0, stream>>>(p);
-  else
-    row_kernel<_Float16><<<grid, block, 0, stream>>>(p);
-  return hipGetLastError();
+  p.by_group = FastDiv(p.group);
+  p.part_rows = part_rows(a.batch.tokens, p.group);
+  if (a.cache.dtype == GTS_F32) return launch_typed<float>(p, stream);
+  if (a.cache.dtype == GTS_BF16) return launch_typed<__bf16>(p, stream);
+  return launch_typed<_Float16>(p, stream);
 }
 
 }  // namespace gts

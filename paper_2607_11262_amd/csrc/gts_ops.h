@@ -84,7 +84,7 @@ __device__ __forceinline__ bool find_sequence(const gts_kv_batch& b, uint32_t t,
   }
   if (lo >= b.batch) return false;
   const int32_t s0 = b.starts[lo], s1 = b.starts[lo + 1];
-  if (s0 < 0 || s0 > (int32_t)t || s1 <= (int32_t)t) return false;
+  if (s0 < 0 || s0 > (int32_t)t || s1 <= (int32_t)t || (uint32_t)s1 > b.tokens) return false;
   *seq = lo;
   *index = t - (uint32_t)s0;
   *count = (uint32_t)(s1 - s0);
