@@ -8,10 +8,11 @@
 // up to 128 query rows (a row: one new token's one query head).  For the
 // prefix the rows are those of all tokens of the batch, so its keys are read
 // once for everybody; for a sequence's own keys they are its tokens'.  The
-// tiles of all (head, rows) segments stand in one line, and each workgroup
-// takes an equal stretch of it, wherever that starts and ends: ragged lengths
-// and few rows fill the chip alike.  A stretch leaves one partial result per
-// segment it touches (unnormalised sum, running maximum and sum of the
+// tiles of all (head, rows) segments stand in one line, each segment's behind
+// a few places for what beginning and ending it costs, and each workgroup takes
+// an equal stretch of that line, wherever it starts and ends: ragged lengths and
+// few rows fill the chip alike.  A stretch leaves one partial result per
+// segment of which it has tiles (unnormalised sum, running maximum and sum of the
 // softmax, 32 bits), and the join adds up the partials of each row.
 //
 // The row kernel: one wavefront per (token, query head) walks the row's keys 64
@@ -29,12 +30,15 @@ constexpr uint32_t kTile = 64;        // keys of a tile
 constexpr uint32_t kMostRows = 128;   // query rows of a segment
 constexpr uint32_t kGroups = 512;     // most workgroups: two a CU
 
+constexpr uint32_t kSegment = 6;     // places in the line for a segment's begin and end
+
 // What the kernels need beside the arguments.
 struct AttnParams {
   gts_attention_args a;
   uint32_t page_shift;
   uint32_t group;       // query heads of a key-value head
   FastDiv by_group;
+  bool near_rows;       // see Loader
   uint32_t workgroups;  // a multiple of 8
   uint32_t part_rows;   // rows that a cut between workgroups may add to the partials
 };
@@ -42,11 +46,10 @@ struct AttnParams {
 // Scratch: the plan (what the tile kernel's first workgroup leaves for the
 // join), then the partials: maximum and sum of each row, then its sums.
 struct Plan {
-  uint64_t tiles, per;  // all tiles; tiles of a workgroup
-  uint64_t prefix_tiles;
+  uint64_t per;  // places of a workgroup
 };
 struct Scratch {
-  uint64_t begin, stats, sums, bytes;  // offsets; begin: [batch] first tile of each sequence
+  uint64_t begin, stats, sums, bytes;  // offsets; begin: [batch] first place of each sequence
 };
 __host__ __device__ inline uint64_t up256(uint64_t x) { return (x + 255) & ~255ull; }
 __host__ __device__ inline Scratch scratch_layout(uint32_t batch, uint64_t rows, uint32_t part_rows, uint32_t dim) {
@@ -67,6 +70,8 @@ __device__ __forceinline__ int32_t key_page(const gts_attention_args& a, const i
   const int32_t p = pages[at];
   return p >= 0 && (uint32_t)p < a.cache.n_pages ? p : -1;
 }
+
+constexpr int kSchedValu = 0x2, kSchedMfma = 0x8, kSchedRead = 0x100, kSchedTrans = 0x400;
 
 // ---- the tile kernel -------------------------------------------------------------
 
@@ -139,19 +144,21 @@ __device__ __forceinline__ uint32_t seen(const Seq& s, uint32_t i) {
   const int64_t v = s.len - s.n + i + 1;
   return v < 0 ? 0 : v < (int64_t)s.keys ? (uint32_t)v : s.keys;
 }
-// Tiles of the rt-th row tile of a sequence (rows rt * 32 rg ..): as far as
-// its last row sees.
+// Tiles of the rt-th segment of a sequence (rows rt * 32 rg ..): as far as its
+// last row sees.
 __device__ __forceinline__ uint32_t own_tiles(const AttnParams& p, const Seq& s, uint32_t rg, uint32_t rt) {
   const uint32_t rows = s.n * p.group, end = (rt + 1) * 32 * rg;
   const uint32_t last = p.by_group.div((rows < end ? rows : end) - 1);
   return (seen(s, last) + kTile - 1) / kTile;
 }
-__device__ __forceinline__ uint64_t head_tiles(const AttnParams& p, const Seq& s) {
+__device__ __forceinline__ uint32_t places(uint32_t tiles) { return tiles ? tiles + kSegment : 0; }
+// Places of a sequence's segments of one head.
+__device__ __forceinline__ uint64_t head_places(const AttnParams& p, const Seq& s) {
   const uint32_t rows = s.n * p.group;
   if (rows == 0 || s.keys == 0) return 0;
   const uint32_t rg = row_groups(rows), n = (rows + 32 * rg - 1) / (32 * rg);
   uint64_t t = 0;
-  for (uint32_t rt = 0; rt < n; ++rt) t += own_tiles(p, s, rg, rt);
+  for (uint32_t rt = 0; rt < n; ++rt) t += places(own_tiles(p, s, rg, rt));
   return t;
 }
 
@@ -188,68 +195,78 @@ struct Tiles {
 // What rows of a tile that do not exist are loaded from.
 __device__ __align__(16) const uint32_t g_zeros[4] = {0, 0, 0, 0};
 
-// Loads one tile of keys and values from the cache straight into LDS (no
+// Loads tiles of keys and values from the cache straight into LDS (no
 // registers in between, so nothing is held while the tile before is worked
-// on).  A wave loads 16 rows; rows past the segment's keys, or without a page,
-// become zeros.  Returns the wave's rows inside the segment that no page
-// holds (one bit each, the same in all lanes).
+// on).  A wave loads 16 rows of a tile; rows past the segment's keys, or without
+// a page, become zeros.
 template <typename T, int DP>
 struct Loader {
   using L = Tiles<T, DP>;
-  int32_t page;  // page of the wave's rows of the next tile (pages of 16 or more)
+  uint32_t k_off[L::NL], v_off[L::NL];  // bytes from the wave's first row to this lane's chunk
+  int32_t page;                         // page of the wave's rows in the next tile (pages of 16 or more)
   uint32_t wave;
+  bool near;  // pages of 16 or more, and 16 rows lie within 2 GiB: k_off and v_off serve
 
   __device__ __forceinline__ void start(const AttnParams& p, const Work& w, uint32_t wave_) {
+    const gts_kv_cache& kc = p.a.cache;
     wave = wave_;
-    if (p.page_shift >= 4) page = key_page(p.a, w.pages, w.n_pages, p.page_shift, w.tile * kTile + wave * 16);
+    near = p.near_rows;
+    const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
+#pragma unroll
+    for (int n = 0; n < L::NL; ++n) {
+      const uint32_t r = n * L::RPI + r0;
+      k_off[n] = 2 * (r * (uint32_t)kc.k_stride[1] + (c ^ L::swizzle_k(r)) * 8);
+      v_off[n] = 2 * (r * (uint32_t)kc.v_stride[1] + (c ^ L::swizzle_v(r)) * 8);
+    }
+    page = p.page_shift >= 4 ? next_page(p, w, w.tile) : 0;
+  }
+  __device__ __forceinline__ int32_t next_page(const AttnParams& p, const Work& w, uint32_t tile) const {
+    return key_page(p.a, w.pages, w.n_pages, p.page_shift, tile * kTile + wave * 16);
   }
 
+  // Returns the wave's rows inside the segment that no page holds (one bit
+  // each, the same in all lanes).
   __device__ __forceinline__ uint32_t load(const AttnParams& p, const Work& w, uint32_t tile, T* sk, T* sv) {
     typedef const __attribute__((address_space(1))) void* global_t;
     typedef __attribute__((address_space(3))) void* lds_t;
     const gts_kv_cache& kc = p.a.cache;
-    const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
     const uint32_t j0 = tile * kTile + wave * 16;
-    const T* kh = (const T*)kc.k + (int64_t)w.head * kc.k_stride[2];
-    const T* vh = (const T*)kc.v + (int64_t)w.head * kc.v_stride[2];
-    uint32_t missing = 0;
-    const bool whole = p.page_shift >= 4;  // the wave's rows are of one page
-    if (whole) {
+    if (near && page >= 0 && j0 + 16 <= w.keys) {
       const uint32_t slot = j0 & (kc.page - 1);
-      const int64_t pg = page < 0 ? 0 : page;
-      kh += pg * kc.k_stride[0] + (int64_t)slot * kc.k_stride[1];
-      vh += pg * kc.v_stride[0] + (int64_t)slot * kc.v_stride[1];
-      if (page < 0) {
-        const uint32_t n = j0 < w.keys ? w.keys - j0 : 0;
-        missing = n < 16 ? (1u << n) - 1 : 0xFFFFu;
-      }
-    }
+      const char* kp = (const char*)((const T*)kc.k + (int64_t)page * kc.k_stride[0] + (int64_t)slot * kc.k_stride[1] +
+                                     (int64_t)w.head * kc.k_stride[2]);
+      const char* vp = (const char*)((const T*)kc.v + (int64_t)page * kc.v_stride[0] + (int64_t)slot * kc.v_stride[1] +
+                                     (int64_t)w.head * kc.v_stride[2]);
 #pragma unroll
+      for (int n = 0; n < L::NL; ++n) {
+        const uint32_t at = (wave * 16 + n * L::RPI) * DP;
+        __builtin_amdgcn_global_load_lds((global_t)(kp + k_off[n]), (lds_t)(sk + at), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_t)(vp + v_off[n]), (lds_t)(sv + at), 16, 0, 0);
+      }
+      page = next_page(p, w, tile + 1);
+      return 0;
+    }
+    // the general way: every row by itself
+    const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
+    uint32_t missing = 0;
+#pragma unroll 1
     for (int n = 0; n < L::NL; ++n) {
       const uint32_t r = n * L::RPI + r0, j = j0 + r;
-      const uint32_t ck = c ^ L::swizzle_k(r), cv = c ^ L::swizzle_v(r);
-      bool ok = j < w.keys;
-      const T *kp, *vp;
-      if (whole) {
-        ok = ok && page >= 0;
-        kp = kh + (int64_t)r * kc.k_stride[1];
-        vp = vh + (int64_t)r * kc.v_stride[1];
-      } else {
-        const int32_t pg = ok ? key_page(p.a, w.pages, w.n_pages, p.page_shift, j) : 0;
-        const uint64_t lost = __ballot(ok && pg < 0);
-        for (int i = 0; i < L::RPI; ++i) missing |= (uint32_t)(lost >> (i * L::C) & 1) << (n * L::RPI + i);
-        ok = ok && pg >= 0;
-        const int64_t slot = j & (kc.page - 1);
-        kp = kh + (int64_t)pg * kc.k_stride[0] + slot * kc.k_stride[1];
-        vp = vh + (int64_t)pg * kc.v_stride[0] + slot * kc.v_stride[1];
-      }
-      kp = ok && ck * 8 < kc.dim ? kp + ck * 8 : (const T*)g_zeros;
-      vp = ok && cv * 8 < kc.dim ? vp + cv * 8 : (const T*)g_zeros;
+      const bool in = j < w.keys;
+      const int32_t pg = in ? key_page(p.a, w.pages, w.n_pages, p.page_shift, j) : -1;
+      const uint64_t lost = __ballot(in && pg < 0);
+      for (int i = 0; i < L::RPI; ++i) missing |= (uint32_t)(lost >> (i * L::C) & 1) << (n * L::RPI + i);
+      const int64_t slot = j & (kc.page - 1);
+      const uint32_t ck = (c ^ L::swizzle_k(r)) * 8, cv = (c ^ L::swizzle_v(r)) * 8;
+      const T* kp = (const T*)kc.k + (int64_t)pg * kc.k_stride[0] + slot * kc.k_stride[1] + (int64_t)w.head * kc.k_stride[2] + ck;
+      const T* vp = (const T*)kc.v + (int64_t)pg * kc.v_stride[0] + slot * kc.v_stride[1] + (int64_t)w.head * kc.v_stride[2] + cv;
+      kp = pg >= 0 && ck < kc.dim ? kp : (const T*)g_zeros;
+      vp = pg >= 0 && cv < kc.dim ? vp : (const T*)g_zeros;
       const uint32_t at = (wave * 16 + n * L::RPI) * DP;
       __builtin_amdgcn_global_load_lds((global_t)kp, (lds_t)(sk + at), 16, 0, 0);
       __builtin_amdgcn_global_load_lds((global_t)vp, (lds_t)(sv + at), 16, 0, 0);
     }
-    if (whole) page = key_page(p.a, w.pages, w.n_pages, p.page_shift, j0 + kTile);
+    if (p.page_shift >= 4) page = next_page(p, w, tile + 1);
     return missing;
   }
 };
@@ -310,6 +327,14 @@ struct Rows {
 #pragma unroll
       for (int b = 0; b < NS; ++b)
         s[b] = mfma(*(const Vec8<T>*)(sk + (key + b * 32 + lane % 32) * DP + (kc ^ (2 * kk)) * 8), q[kk], s[b]);
+    // four fragments of keys ahead of the products
+    __builtin_amdgcn_sched_group_barrier(kSchedRead, 4, 0);
+#pragma unroll
+    for (int i = 0; i < NS * L::KK - 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 0);
     if (mask) {
 #pragma unroll
       for (int b = 0; b < NS; ++b)
@@ -358,6 +383,18 @@ struct Rows {
     for (int kb = 0; kb < 2 * NS; ++kb)
 #pragma unroll
       for (int mb = 0; mb < L::MB; ++mb) o[mb] = mfma(load_v<T, DP>(sv, lane, key + kb * 16, mb), pw[kb], o[mb]);
+    // the weights of 16 keys and the first values, then each product with the
+    // reads of a later one and the exponentials of the next 16 keys
+    __builtin_amdgcn_sched_group_barrier(kSchedRead, 8, 1);
+    __builtin_amdgcn_sched_group_barrier(kSchedValu, 24, 1);
+    __builtin_amdgcn_sched_group_barrier(kSchedTrans, 8, 1);
+#pragma unroll
+    for (int i = 0; i < 2 * NS * L::MB; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 1);
+      __builtin_amdgcn_sched_group_barrier(kSchedRead, 2, 1);
+      __builtin_amdgcn_sched_group_barrier(kSchedTrans, 2, 1);
+      __builtin_amdgcn_sched_group_barrier(kSchedValu, 6, 1);
+    }
   }
 
   // As the end of step(), for a tile in which some rows do not see every key
@@ -550,17 +587,17 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   __shared__ __align__(8) Flags s_flags;
   const uint32_t tid = threadIdx.x, lane = tid & 63u;
 
-  // The plan: tiles of every sequence, summed.  Thread i takes sequences
+  // The plan: places of every sequence, summed.  Thread i takes sequences
   // [i per, (i + 1) per).
   const uint32_t per_thread = (B + 255) / 256;
   const uint32_t prows = a.batch.tokens * p.group;
   const uint32_t prg = row_groups(prows), n_prt = (prows + 32 * prg - 1) / (32 * prg);
   const uint32_t ptiles = (P + kTile - 1) / kTile;
-  const uint64_t prefix_tiles = (uint64_t)ptiles * n_prt * hkv;
+  const uint64_t prefix_places = (uint64_t)places(ptiles) * n_prt * hkv;
   uint64_t mine = 0;
   for (uint32_t i = 0; i < per_thread; ++i) {
     const uint32_t b = tid * per_thread + i;
-    if (b < B) mine += head_tiles(p, load_seq(p, b)) * hkv;
+    if (b < B) mine += head_places(p, load_seq(p, b)) * hkv;
   }
   uint64_t scan = mine;
   for (int i = 1; i < 64; i <<= 1) {
@@ -569,10 +606,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   }
   if (lane == 63) s_wave[tid >> 6] = scan;
   __syncthreads();
-  uint64_t before = prefix_tiles;
+  uint64_t before = prefix_places;
   for (uint32_t i = 0; i < tid >> 6; ++i) before += s_wave[i];
-  s_sum[tid] = before + scan - mine;  // first tile of this thread's sequences
-  const uint64_t total = uni(prefix_tiles + s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3]);
+  s_sum[tid] = before + scan - mine;  // first place of this thread's sequences
+  const uint64_t total = uni(prefix_places + s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3]);
   const uint64_t per = (total + p.workgroups - 1) / p.workgroups;
   const uint64_t rows = (uint64_t)a.batch.tokens * a.q_heads;
   const Scratch sc = scratch_layout(B, rows, p.part_rows, a.cache.dim);
@@ -583,26 +620,27 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       const uint32_t b = tid * per_thread + i;
       if (b >= B) break;
       ((uint64_t*)(scratch + sc.begin))[b] = t;
-      t += head_tiles(p, load_seq(p, b)) * hkv;
+      t += head_places(p, load_seq(p, b)) * hkv;
     }
-    if (tid == 0) *(Plan*)scratch = Plan{total, per, prefix_tiles};
+    if (tid == 0) *(Plan*)scratch = Plan{per};
   }
   __syncthreads();
 
-  // neighbours in the line of tiles go to one XCD (workgroups go round the
-  // eight of them), whose L2 then has the keys that they share
+  // neighbours in the line go to one XCD (workgroups go round the eight of
+  // them), whose L2 then has the keys that they share
   const uint32_t g = (blockIdx.x & 7u) * (p.workgroups / 8) + (blockIdx.x >> 3);
   uint64_t t = (uint64_t)g * per, end = t + per;
   if (end > total) end = total;
   while (t < end) {
     Work w;
-    uint64_t seg, seg_tiles;  // first tile of the segment and its tiles
-    if (t < prefix_tiles) {
-      const uint32_t s = (uint32_t)(t / ptiles);
+    uint64_t seg;    // first place of the segment
+    uint32_t tiles;  // its tiles
+    if (t < prefix_places) {
+      tiles = ptiles;
+      const uint32_t s = (uint32_t)(t / places(tiles));
       w.head = s / n_prt;
       const uint32_t rt = s - w.head * n_prt;
-      seg = (uint64_t)s * ptiles;
-      seg_tiles = ptiles;
+      seg = (uint64_t)s * places(tiles);
       w.pages = a.prefix_pages;
       w.n_pages = a.n_prefix_pages;
       w.keys = w.low = P;
@@ -621,23 +659,21 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       uint32_t b = who * per_thread;
       uint64_t first = uni(s_sum[who]);
       Seq s = load_seq(p, b < B ? b : B - 1);
-      uint64_t ht = head_tiles(p, s);
+      uint64_t ht = head_places(p, s);
       for (uint32_t i = 1; i < per_thread && t >= first + ht * hkv; ++i) {
         first += ht * hkv;
         s = load_seq(p, ++b);
-        ht = head_tiles(p, s);
+        ht = head_places(p, s);
       }
       const uint64_t rel = t - first;
       w.head = uni((uint32_t)(rel / ht));
-      uint32_t in = uni((uint32_t)(rel - w.head * ht));
       w.rg = row_groups(s.n * p.group);
       uint32_t rt = 0;
       seg = first + w.head * ht;
-      seg_tiles = own_tiles(p, s, w.rg, 0);
-      while (in >= seg_tiles) {
-        in -= (uint32_t)seg_tiles;
-        seg += seg_tiles;
-        seg_tiles = own_tiles(p, s, w.rg, ++rt);
+      tiles = own_tiles(p, s, w.rg, 0);
+      while (t >= seg + places(tiles)) {
+        seg += places(tiles);
+        tiles = own_tiles(p, s, w.rg, ++rt);
       }
       const uint32_t srows = s.n * p.group, r0 = rt * 32 * w.rg;
       w.pages = a.batch.page_table + (int64_t)b * a.batch.table_stride;
@@ -650,12 +686,16 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       w.see = s.len - s.n + 1 - (int64_t)s.first;
       w.part = rows + (uint64_t)hkv * s.first * p.group + (uint64_t)w.head * srows + r0;
     }
-    w.part += (uint64_t)p.part_rows * g;
-    w.tile = (uint32_t)(t - seg);
-    const uint64_t left = seg + seg_tiles - t;
-    w.n_tiles = (uint32_t)(end - t < left ? end - t : left);
-    run_stretch<T, DP>(p, w, s_kv, &s_flags, (float*)(scratch + sc.stats), (float*)(scratch + sc.sums));
-    t += w.n_tiles;
+    // tile i stands at place seg + kSegment + i
+    const uint64_t zero = seg + kSegment, stop = end < zero + tiles ? end : zero + tiles;
+    if (stop > zero) {
+      const uint64_t from = t > zero ? t : zero;
+      w.part += (uint64_t)p.part_rows * g;
+      w.tile = (uint32_t)(from - zero);
+      w.n_tiles = (uint32_t)(stop - from);
+      run_stretch<T, DP>(p, w, s_kv, &s_flags, (float*)(scratch + sc.stats), (float*)(scratch + sc.sums));
+    }
+    t = stop;
   }
 }
 
@@ -678,24 +718,25 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
   uint32_t seq, index, count;
   if (find_sequence(a.batch, t, &seq, &index, &count)) {
     for (int part = 0; part < 2; ++part) {
-      uint64_t first, n, at;  // tiles of the segment, its row in the partials
+      uint64_t first, n, at;  // place and tiles of the segment, the row among the partials
       if (part == 0) {
         const uint32_t P = a.cache.n_pages ? a.batch.prefix_len : 0;
         n = (P + kTile - 1) / kTile;
         const uint32_t prows = a.batch.tokens * p.group, rg = row_groups(prows);
         const uint32_t r = t * p.group + gq, n_rt = (prows + 32 * rg - 1) / (32 * rg);
-        first = n * ((uint64_t)head * n_rt + r / (32 * rg));
+        first = places((uint32_t)n) * ((uint64_t)head * n_rt + r / (32 * rg));
         at = (uint64_t)head * prows + r;
       } else {
         const Seq s = load_seq(p, seq);
         const uint32_t srows = s.n * p.group, rg = row_groups(srows), r = index * p.group + gq, rt = r / (32 * rg);
         if (s.keys == 0) continue;
-        first = ((const uint64_t*)(scratch + sc.begin))[seq] + head * head_tiles(p, s);
-        for (uint32_t i = 0; i < rt; ++i) first += own_tiles(p, s, rg, i);
+        first = ((const uint64_t*)(scratch + sc.begin))[seq] + head * head_places(p, s);
+        for (uint32_t i = 0; i < rt; ++i) first += places(own_tiles(p, s, rg, i));
         n = own_tiles(p, s, rg, rt);
         at = rows + (uint64_t)hkv * s.first * p.group + (uint64_t)head * srows + r;
       }
       if (n == 0) continue;
+      first += kSegment;
       const uint64_t g1 = (first + n - 1) / plan.per;
       for (uint64_t g = first / plan.per; g <= g1; ++g) {
         const uint64_t x = at + p.part_rows * g;
@@ -851,6 +892,11 @@ hipError_t launch_attention(const gts_attention_args& a, hipStream_t stream) {
   p.group = a.q_heads / a.cache.heads;
   p.by_group = FastDiv(p.group);
   p.part_rows = part_rows(a.batch.tokens, p.group);
+  // chunks beyond the head must come out as zeros: the general way alone
+  const int64_t far = 1 << 26;  // elements: 16 rows and a chunk stay below 2^31 bytes
+  p.near_rows = p.page_shift >= 4 && (a.cache.dim == 64 || a.cache.dim == 128 || a.cache.dim == 256) &&
+                a.cache.k_stride[1] >= 0 && a.cache.k_stride[1] < far && a.cache.v_stride[1] >= 0 &&
+                a.cache.v_stride[1] < far;
   if (a.cache.dtype == GTS_F32) return launch_typed<float>(p, stream);
   if (a.cache.dtype == GTS_BF16) return launch_typed<__bf16>(p, stream);
   return launch_typed<_Float16>(p, stream);
