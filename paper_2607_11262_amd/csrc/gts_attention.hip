@@ -71,8 +71,6 @@ __device__ __forceinline__ int32_t key_page(const gts_attention_args& a, const i
   return p >= 0 && (uint32_t)p < a.cache.n_pages ? p : -1;
 }
 
-constexpr int kSchedValu = 0x2, kSchedMfma = 0x8, kSchedRead = 0x100, kSchedTrans = 0x400;
-
 // ---- the tile kernel -------------------------------------------------------------
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -220,8 +218,13 @@ struct Loader {
     }
     page = p.page_shift >= 4 ? next_page(p, w, w.tile) : 0;
   }
+  // By a vector load, though it is the same for all lanes: LDS reads wait for
+  // every scalar load before them (one counter), and this one may be long.
   __device__ __forceinline__ int32_t next_page(const AttnParams& p, const Work& w, uint32_t tile) const {
-    return key_page(p.a, w.pages, w.n_pages, p.page_shift, tile * kTile + wave * 16);
+    const uint32_t at = (tile * kTile + wave * 16) >> p.page_shift;
+    uint32_t zero = 0;
+    asm volatile("" : "+v"(zero));
+    return at < w.n_pages ? (w.pages + at)[zero] : -1;
   }
 
   // Returns the wave's rows inside the segment that no page holds (one bit
@@ -231,11 +234,12 @@ struct Loader {
     typedef __attribute__((address_space(3))) void* lds_t;
     const gts_kv_cache& kc = p.a.cache;
     const uint32_t j0 = tile * kTile + wave * 16;
-    if (near && page >= 0 && j0 + 16 <= w.keys) {
+    const uint32_t pg0 = uni((uint32_t)page);
+    if (near && pg0 < kc.n_pages && j0 + 16 <= w.keys) {
       const uint32_t slot = j0 & (kc.page - 1);
-      const char* kp = (const char*)((const T*)kc.k + (int64_t)page * kc.k_stride[0] + (int64_t)slot * kc.k_stride[1] +
+      const char* kp = (const char*)((const T*)kc.k + (int64_t)pg0 * kc.k_stride[0] + (int64_t)slot * kc.k_stride[1] +
                                      (int64_t)w.head * kc.k_stride[2]);
-      const char* vp = (const char*)((const T*)kc.v + (int64_t)page * kc.v_stride[0] + (int64_t)slot * kc.v_stride[1] +
+      const char* vp = (const char*)((const T*)kc.v + (int64_t)pg0 * kc.v_stride[0] + (int64_t)slot * kc.v_stride[1] +
                                      (int64_t)w.head * kc.v_stride[2]);
 #pragma unroll
       for (int n = 0; n < L::NL; ++n) {
@@ -316,25 +320,33 @@ struct Rows {
                                        uint64_t missing, bool odd, uint32_t sees) {
     const uint32_t half = lane / 32;
     f32x16 s[NS];
+    const T* ka = sk + (key + lane % 32) * DP;
     const uint32_t kc = half ^ L::swizzle_k(lane % 32);
 #pragma unroll
-    for (int b = 0; b < NS; ++b) {
+    for (int b = 0; b < NS; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+    // The fragments of two matrix steps are read while the two before are
+    // multiplied; the fences keep that order.
+    Vec8<T> kf[2][2][NS];
+    const auto read = [&](int at, int kk) {
+#pragma unroll
+      for (int b = 0; b < NS; ++b) {
+        kf[at][0][b] = *(const Vec8<T>*)(ka + b * 32 * DP + (kc ^ (2 * kk)) * 8);
+        kf[at][1][b] = *(const Vec8<T>*)(ka + b * 32 * DP + (kc ^ (2 * kk + 2)) * 8);
+      }
+    };
+    read(0, 0);
+#pragma unroll
+    for (int kk = 0; kk < L::KK; kk += 2) {
+      if (kk + 2 < L::KK) read(kk / 2 + 1 & 1, kk + 2);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int b = 0; b < NS; ++b) s[b] = mfma(kf[kk / 2 & 1][x][b], q[kk + x], s[b]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int kk = 0; kk < L::KK; ++kk)
-#pragma unroll
-      for (int b = 0; b < NS; ++b)
-        s[b] = mfma(*(const Vec8<T>*)(sk + (key + b * 32 + lane % 32) * DP + (kc ^ (2 * kk)) * 8), q[kk], s[b]);
-    // four fragments of keys ahead of the products
-    __builtin_amdgcn_sched_group_barrier(kSchedRead, 4, 0);
-#pragma unroll
-    for (int i = 0; i < NS * L::KK - 4; ++i) {
-      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(kSchedRead, 1, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 0);
     if (mask) {
 #pragma unroll
       for (int b = 0; b < NS; ++b)
@@ -364,37 +376,47 @@ struct Rows {
       m = m1;
     }
     const float base = m == -INFINITY ? 0.f : -m * c;
-    Vec8<T> pw[2 * NS];
     float sum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int b = 0; b < NS; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = exp2_(__builtin_fmaf(s[b][i], c, base));
-        sum[i & 1] += e;
-        pw[2 * b + i / 8][i % 8] = (T)e;
-      }
-    l += sum[0] + sum[1];
+    Vec8<T> pw[2 * NS];
+    const auto weigh = [&](int kb, int i) {
+      const float e = exp2_(__builtin_fmaf(s[kb / 2][kb % 2 * 8 + i], c, base));
+      sum[i & 1] += e;
+      pw[kb][i] = (T)e;
+    };
     if (NS == 1 && odd) {
+#pragma unroll
+      for (int kb = 0; kb < 2 * NS; ++kb)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) weigh(kb, i);
+      l += sum[0] + sum[1];
       odd_values<NS>(lane, sv, key, j0, sees, pw);
       return;
     }
+    // The weights of 16 keys are computed, and the values of 16 keys read,
+    // between the products of the 16 keys before.
+    Vec8<T> vf[2][L::MB];
 #pragma unroll
-    for (int kb = 0; kb < 2 * NS; ++kb)
+    for (int mb = 0; mb < L::MB; ++mb) vf[0][mb] = load_v<T, DP>(sv, lane, key, mb);
 #pragma unroll
-      for (int mb = 0; mb < L::MB; ++mb) o[mb] = mfma(load_v<T, DP>(sv, lane, key + kb * 16, mb), pw[kb], o[mb]);
-    // the weights of 16 keys and the first values, then each product with the
-    // reads of a later one and the exponentials of the next 16 keys
-    __builtin_amdgcn_sched_group_barrier(kSchedRead, 8, 1);
-    __builtin_amdgcn_sched_group_barrier(kSchedValu, 24, 1);
-    __builtin_amdgcn_sched_group_barrier(kSchedTrans, 8, 1);
+    for (int i = 0; i < 8; ++i) weigh(0, i);
 #pragma unroll
-    for (int i = 0; i < 2 * NS * L::MB; ++i) {
-      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 1);
-      __builtin_amdgcn_sched_group_barrier(kSchedRead, 2, 1);
-      __builtin_amdgcn_sched_group_barrier(kSchedTrans, 2, 1);
-      __builtin_amdgcn_sched_group_barrier(kSchedValu, 6, 1);
+    for (int kb = 0; kb < 2 * NS; ++kb) {
+      if (kb + 1 < 2 * NS) {
+#pragma unroll
+        for (int mb = 0; mb < L::MB; ++mb) vf[kb + 1 & 1][mb] = load_v<T, DP>(sv, lane, key + kb * 16 + 16, mb);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int mb = 0; mb < L::MB; ++mb) {
+        o[mb] = mfma(vf[kb & 1][mb], pw[kb], o[mb]);
+        if (kb + 1 < 2 * NS) {
+#pragma unroll
+          for (int i = mb * 8 / L::MB; i < (mb + 1) * 8 / L::MB; ++i) weigh(kb + 1, i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
+    l += sum[0] + sum[1];
   }
 
   // As the end of step(), for a tile in which some rows do not see every key
@@ -447,6 +469,56 @@ struct Flags {
   uint32_t odd[4];         // values that are not finite
 };
 
+// Tiles i0 .. i1 of a stretch, the first of them already on its way.  One tile is
+// worked on while the next is on its way to the other half of the LDS; one
+// barrier a tile.
+template <int NS, typename T, int DP>
+__device__ __forceinline__ void run_tiles(const AttnParams& p, const Work& w, Loader<T, DP>& ld, Rows<T, DP>& r,
+                                          uint32_t i0, uint32_t i1, uint32_t wave, uint32_t kgroup, T* s_kv,
+                                          Flags* flags, float c, uint32_t sees) {
+  using L = Tiles<T, DP>;
+  for (uint32_t i = i0; i < i1; ++i) {
+    const uint32_t tile = w.tile + i, j0 = tile * kTile;
+    T* sk = s_kv + (i & 1) * 2 * L::N;
+    T* sv = sk + L::N;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const uint64_t missing = uni(*(const uint64_t*)flags->missing[i & 1]);
+    if (i + 1 < w.n_tiles) {
+      T* next = s_kv + ((i + 1) & 1) * 2 * L::N;
+      const uint32_t miss = ld.load(p, w, tile + 1, next, next + L::N);
+      if ((threadIdx.x & 63u) == 0) flags->missing[(i + 1) & 1][wave] = (uint16_t)miss;
+    }
+    const bool edge = j0 + kTile > w.low;  // some row does not see all of the tile
+    const bool mask = edge || missing;
+    if constexpr (NS == 2) {
+      r.template step<2>(fresh_lane(), sk, sv, 0, j0, c, mask, missing, false, sees);
+    } else {
+      bool odd = false;
+      if (edge && w.low < w.keys) {
+        constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
+        bool found = false;
+        for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) {
+          const u32x4 v = *(const u32x4*)(sv + x * 8);
+          for (int y = 0; y < 4; ++y) found |= (v[y] & kExp) == kExp || (v[y] >> 16 & kExp) == kExp;
+        }
+        const bool any = __any(found);
+        if ((threadIdx.x & 63u) == 0) flags->odd[wave] = any;
+        __syncthreads();
+        odd = uni(flags->odd[0] | flags->odd[1] | flags->odd[2] | flags->odd[3]);
+        __syncthreads();
+      }
+      // one key group takes all of a tile, two take a half each, four a half
+      // of every second tile
+      if (w.rg != 1 || (i & 1) == kgroup / 2) {
+#pragma unroll 1
+        for (uint32_t x = (kgroup & 1) * 32; x < kTile; x += w.rg == 4 ? 32 : kTile)
+          r.template step<1>(fresh_lane(), sk, sv, x, j0 + x, c, mask, missing, odd, sees);
+      }
+    }
+  }
+}
+
 template <typename T, int DP>
 __device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, T* s_kv, Flags* flags, float* stats,
                                             float* sums) {
@@ -491,45 +563,18 @@ __device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, 
     sees = !valid ? w.keys : v < 0 ? 0 : v < (int64_t)w.keys ? (uint32_t)v : w.keys;
   }
 
-  // One tile is worked on while the next is on its way to the other half of
-  // the LDS; one barrier a tile.
-  for (uint32_t i = 0; i < w.n_tiles; ++i) {
-    const uint32_t tile = w.tile + i, j0 = tile * kTile;
-    T* sk = s_kv + (i & 1) * 2 * L::N;
-    T* sv = sk + L::N;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const uint64_t missing = uni(*(const uint64_t*)flags->missing[i & 1]);
-    if (i + 1 < w.n_tiles) {
-      T* next = s_kv + ((i + 1) & 1) * 2 * L::N;
-      const uint32_t miss = ld.load(p, w, tile + 1, next, next + L::N);
-      if (lane == 0) flags->missing[(i + 1) & 1][wave] = (uint16_t)miss;
+  // Tiles of which every row sees all keys, or a segment whose rows all see
+  // the same: with rows for all four waves, 64 keys a step.
+  uint32_t plain = 0;
+  if (w.rg == 4) {
+    plain = w.n_tiles;
+    if (w.low < w.keys) {
+      const uint32_t full = w.low / kTile;  // tiles before the first that a row does not see to its end
+      plain = full <= w.tile ? 0 : full - w.tile < w.n_tiles ? full - w.tile : w.n_tiles;
     }
-    const bool edge = j0 + kTile > w.low;  // some row does not see all of the tile
-    bool odd = false;
-    if (edge && w.low < w.keys) {
-      constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
-      bool found = false;
-      for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) {
-        const u32x4 v = *(const u32x4*)(sv + x * 8);
-        for (int y = 0; y < 4; ++y) found |= (v[y] & kExp) == kExp || (v[y] >> 16 & kExp) == kExp;
-      }
-      if (lane == 0) flags->odd[wave] = 0;
-      if (__any(found) && lane == 0) flags->odd[wave] = 1;
-      __syncthreads();
-      odd = uni(flags->odd[0] | flags->odd[1] | flags->odd[2] | flags->odd[3]);
-      __syncthreads();
-    }
-    const bool mask = edge || missing;
-    if (w.rg == 4 && !odd) {
-      r.template step<2>(fresh_lane(), sk, sv, 0, j0, c, mask, missing, false, sees);
-    } else if (w.rg != 1 || (i & 1) == kgroup / 2) {
-      // 2 or 4 key groups: halves of every tile, or of every second one
-#pragma unroll 1
-      for (uint32_t x = (kgroup & 1) * 32; x < kTile; x += w.rg == 4 ? 32 : kTile)
-        r.template step<1>(fresh_lane(), sk, sv, x, j0 + x, c, mask, missing, odd, sees);
-    }
+    run_tiles<2>(p, w, ld, r, 0, plain, wave, kgroup, s_kv, flags, c, sees);
   }
+  if (plain < w.n_tiles) run_tiles<1>(p, w, ld, r, plain, w.n_tiles, wave, kgroup, s_kv, flags, c, sees);
 
   // waves that took other keys of the same rows hand theirs to the first
   r.l = add_halves(r.l);
@@ -690,12 +735,22 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
     const uint64_t zero = seg + kSegment, stop = end < zero + tiles ? end : zero + tiles;
     if (stop > zero) {
       const uint64_t from = t > zero ? t : zero;
-      w.part += (uint64_t)p.part_rows * g;
-      w.tile = (uint32_t)(from - zero);
-      w.n_tiles = (uint32_t)(stop - from);
+      // the same in all lanes: kept in scalar registers
+      w.pages = (const int32_t*)uni((uint64_t)w.pages);
+      w.n_pages = uni(w.n_pages);
+      w.keys = uni(w.keys);
+      w.low = uni(w.low);
+      w.head = uni(w.head);
+      w.rg = uni(w.rg);
+      w.rows = uni(w.rows);
+      w.first_row = uni(w.first_row);
+      w.see = (int64_t)uni((uint64_t)w.see);
+      w.part = uni(w.part + (uint64_t)p.part_rows * g);
+      w.tile = uni((uint32_t)(from - zero));
+      w.n_tiles = uni((uint32_t)(stop - from));
       run_stretch<T, DP>(p, w, s_kv, &s_flags, (float*)(scratch + sc.stats), (float*)(scratch + sc.sums));
     }
-    t = stop;
+    t = uni(stop);
   }
 }
 
