@@ -109,8 +109,9 @@ __device__ __forceinline__ float add_halves(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Rows of a segment's tile for n query rows: 32, 64 or 128, by how many of
-// the four waves take rows of their own (the others take other keys).
+// Rows of a segment for n query rows: 32 rg.  rg = 1: the stream below; 2 and 4:
+// so many of the four waves take rows of their own (with 2, the others take the
+// other half of the keys).
 __host__ __device__ __forceinline__ uint32_t row_groups(uint32_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
 
 // New tokens and own keys of sequence b.
@@ -294,6 +295,38 @@ __device__ __forceinline__ Vec8<T> load_v(const T* sv, uint32_t lane, uint32_t k
   return u.v;
 }
 
+// Values that are not finite, in a block of keys that some rows do not see to
+// its end: 0 times one of them would reach rows that must not see it.  So they
+// are cleared in the copy that is multiplied, and added here, from the cache,
+// to the rows that see them.  `add(key, d, x)` gets four values x from dim d on.
+__device__ __forceinline__ bool not_finite(float x) { return !(__builtin_fabsf(x) < INFINITY); }
+template <typename T>
+__device__ __forceinline__ bool any_not_finite(u32x4 v) {
+  constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) found |= (v[i] & kExp) == kExp || (v[i] >> 16 & kExp) == kExp;
+  return found;
+}
+template <typename T>
+__device__ __forceinline__ u32x4 finite_only(u32x4 v) {
+  constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((v[i] & kExp) == kExp) v[i] &= 0xFFFF0000u;
+    if ((v[i] >> 16 & kExp) == kExp) v[i] &= 0xFFFFu;
+  }
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ const T* value_row(const AttnParams& p, const Work& w, uint32_t j) {
+  const gts_kv_cache& kc = p.a.cache;
+  const int32_t page = j < w.keys ? key_page(p.a, w.pages, w.n_pages, p.page_shift, j) : -1;
+  if (page < 0) return nullptr;
+  return (const T*)kc.v + (int64_t)page * kc.v_stride[0] + (int64_t)(j & (kc.page - 1)) * kc.v_stride[1] +
+         (int64_t)w.head * kc.v_stride[2];
+}
+
 // What a wave holds: 32 query rows against its keys.  Scores are computed as
 // keys x rows, so a lane has 16 of 32 keys of one row: maximum and sum need one
 // exchange with the lane 32 away, and the weights are already where the
@@ -317,7 +350,7 @@ struct Rows {
   // NS blocks of 32 keys from LDS row `key` on (key number j0 of the segment).
   template <int NS>
   __device__ __forceinline__ void step(uint32_t lane, const T* sk, const T* sv, uint32_t key, uint32_t j0, float c, bool mask,
-                                       uint64_t missing, bool odd, uint32_t sees) {
+                                       uint64_t missing, uint32_t sees) {
     const uint32_t half = lane / 32;
     f32x16 s[NS];
     const T* ka = sk + (key + lane % 32) * DP;
@@ -383,15 +416,6 @@ struct Rows {
       sum[i & 1] += e;
       pw[kb][i] = (T)e;
     };
-    if (NS == 1 && odd) {
-#pragma unroll
-      for (int kb = 0; kb < 2 * NS; ++kb)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) weigh(kb, i);
-      l += sum[0] + sum[1];
-      odd_values<NS>(lane, sv, key, j0, sees, pw);
-      return;
-    }
     // The weights of 16 keys are computed, and the values of 16 keys read,
     // between the products of the 16 keys before.
     Vec8<T> vf[2][L::MB];
@@ -419,44 +443,20 @@ struct Rows {
     l += sum[0] + sum[1];
   }
 
-  // As the end of step(), for a tile in which some rows do not see every key
-  // and a value is not finite: 0 times it would reach the rows that must not
-  // see it.  The finite values are summed as usual; products of ones find
-  // the rows that see an infinity of either sign or a NaN (both).
-  template <int NS>
-  __device__ __forceinline__ void odd_values(uint32_t lane, const T* sv, uint32_t key, uint32_t j0, uint32_t sees,
-                                             const Vec8<T> (&pw)[2 * NS]) {
+  // See not_finite: keys j0 .. j0 + 31.
+  __device__ __forceinline__ void add_odd(const AttnParams& p, const Work& w, uint32_t lane, uint32_t j0, uint32_t sees) {
+#pragma unroll 1
+    for (uint32_t j = j0; j < j0 + 32; ++j) {
+      const T* v = value_row<T>(p, w, j);
+      if (!v) continue;
 #pragma unroll
-    for (int mb = 0; mb < L::MB; ++mb) {
+      for (int x = 0; x < L::MB * 4; ++x) {
+        const uint32_t d = x / 4 * 32 + 8 * (x % 4) + 4 * (lane / 32);
+        if (d >= p.a.cache.dim) continue;
+        const Pack<T, 4> y = *(const Pack<T, 4>*)(v + d);
 #pragma unroll
-      for (int kb = 0; kb < 2 * NS; ++kb) {
-        Vec8<T> v = load_v<T, DP>(sv, lane, key + kb * 16, mb);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __builtin_fabsf((float)v[i]) < INFINITY ? v[i] : (T)0.f;
-        o[mb] = mfma(v, pw[kb], o[mb]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int sign = 0; sign < 2; ++sign) {
-        f32x16 hits;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) hits[i] = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < 2 * NS; ++kb) {
-          Vec8<T> v = load_v<T, DP>(sv, lane, key + kb * 16, mb), vis;
-          uint32_t first = j0 + kb * 16 + 4 * (lane / 32);
-          asm volatile("" : "+v"(first));
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float x = sign ? -(float)v[i] : (float)v[i];
-            v[i] = (T)(x < INFINITY ? 0.f : 1.f);  // NaN counts for both signs
-            vis[i] = (T)(first + 8 * (i / 4) + i % 4 < sees ? 1.f : 0.f);
-          }
-          hits = mfma(v, vis, hits);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[mb][i] += hits[i] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+        for (int i = 0; i < 4; ++i)
+          if (not_finite((float)y.v[i]) && j < sees) o[x / 4][x % 4 * 4 + i] += (float)y.v[i];
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -492,28 +492,26 @@ __device__ __forceinline__ void run_tiles(const AttnParams& p, const Work& w, Lo
     const bool edge = j0 + kTile > w.low;  // some row does not see all of the tile
     const bool mask = edge || missing;
     if constexpr (NS == 2) {
-      r.template step<2>(fresh_lane(), sk, sv, 0, j0, c, mask, missing, false, sees);
+      r.template step<2>(fresh_lane(), sk, sv, 0, j0, c, mask, missing, sees);
     } else {
       bool odd = false;
       if (edge && w.low < w.keys) {
-        constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
         bool found = false;
-        for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) {
-          const u32x4 v = *(const u32x4*)(sv + x * 8);
-          for (int y = 0; y < 4; ++y) found |= (v[y] & kExp) == kExp || (v[y] >> 16 & kExp) == kExp;
-        }
+        for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) found |= any_not_finite<T>(*(const u32x4*)(sv + x * 8));
         const bool any = __any(found);
         if ((threadIdx.x & 63u) == 0) flags->odd[wave] = any;
         __syncthreads();
         odd = uni(flags->odd[0] | flags->odd[1] | flags->odd[2] | flags->odd[3]);
+        if (odd)
+          for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256)
+            *(u32x4*)(sv + x * 8) = finite_only<T>(*(const u32x4*)(sv + x * 8));
         __syncthreads();
       }
-      // one key group takes all of a tile, two take a half each, four a half
-      // of every second tile
-      if (w.rg != 1 || (i & 1) == kgroup / 2) {
+      // one key group takes all of a tile, two take a half each
 #pragma unroll 1
-        for (uint32_t x = (kgroup & 1) * 32; x < kTile; x += w.rg == 4 ? 32 : kTile)
-          r.template step<1>(fresh_lane(), sk, sv, x, j0 + x, c, mask, missing, odd, sees);
+      for (uint32_t x = kgroup * 32; x < kTile; x += w.rg == 4 ? 32 : kTile) {
+        r.template step<1>(fresh_lane(), sk, sv, x, j0 + x, c, mask, missing, sees);
+        if (odd) r.add_odd(p, w, fresh_lane(), j0 + x, sees);
       }
     }
   }
@@ -576,32 +574,30 @@ __device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, 
   }
   if (plain < w.n_tiles) run_tiles<1>(p, w, ld, r, plain, w.n_tiles, wave, kgroup, s_kv, flags, c, sees);
 
-  // waves that took other keys of the same rows hand theirs to the first
+  // two waves that took other keys of the same rows: the second hands its to
+  // the first
   r.l = add_halves(r.l);
-  if (w.rg < 4) {
+  if (w.rg == 2) {
     constexpr int N = L::MB * 16 + 2;
-    static_assert(3 * N * 64 * 4 <= 4 * L::N * sizeof(T), "partials of three waves fit the tiles' LDS");
-    float* mine = (float*)s_kv + (wave - w.rg) * N * 64 + lane;
+    static_assert(2 * N * 64 * 4 <= 4 * L::N * sizeof(T), "partials of two waves fit the tiles' LDS");
+    float* other = (float*)s_kv + rgroup * N * 64 + lane;
     __syncthreads();
-    if (kgroup > 0) {
+    if (kgroup == 1) {
 #pragma unroll
-      for (int i = 0; i < L::MB * 16; ++i) mine[i * 64] = r.o[i / 16][i % 16];
-      mine[(N - 2) * 64] = r.m;
-      mine[(N - 1) * 64] = r.l;
+      for (int i = 0; i < L::MB * 16; ++i) other[i * 64] = r.o[i / 16][i % 16];
+      other[(N - 2) * 64] = r.m;
+      other[(N - 1) * 64] = r.l;
     }
     __syncthreads();
     if (kgroup == 0) {
-      for (uint32_t x = rgroup; x < 4 - w.rg; x += w.rg) {
-        const float* other = (const float*)s_kv + x * N * 64 + lane;
-        const float mo = other[(N - 2) * 64], lo = other[(N - 1) * 64];
-        const float m1 = fmaxf(r.m, mo);
-        const float fa = r.m == -INFINITY ? 1.f : exp2_((r.m - m1) * c);
-        const float fb = mo == -INFINITY ? 1.f : exp2_((mo - m1) * c);
+      const float mo = other[(N - 2) * 64], lo = other[(N - 1) * 64];
+      const float m1 = fmaxf(r.m, mo);
+      const float fa = r.m == -INFINITY ? 1.f : exp2_((r.m - m1) * c);
+      const float fb = mo == -INFINITY ? 1.f : exp2_((mo - m1) * c);
 #pragma unroll
-        for (int i = 0; i < L::MB * 16; ++i) r.o[i / 16][i % 16] = r.o[i / 16][i % 16] * fa + other[i * 64] * fb;
-        r.l = r.l * fa + lo * fb;
-        r.m = m1;
-      }
+      for (int i = 0; i < L::MB * 16; ++i) r.o[i / 16][i % 16] = r.o[i / 16][i % 16] * fa + other[i * 64] * fb;
+      r.l = r.l * fa + lo * fb;
+      r.m = m1;
     }
   }
   if (kgroup == 0 && valid) {
@@ -622,6 +618,325 @@ __device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, 
   }
 }
 
+// ---- few rows: a stream of keys per wave -------------------------------------------
+//
+// With at most 32 rows the products are small beside the bytes: every wave
+// takes blocks of 32 keys of its own and waits for nobody.  Keys go from the
+// cache to registers just as the matrix instruction takes them (16 keys x 32
+// dims); values are held in registers until the block before is done with the
+// wave's part of the LDS, where they are turned.  So 16 KiB a wave (head dim
+// 128) are on their way while it computes.  16 x 16 tiles, because decode has
+// few rows (query heads of a key-value head).
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f32x4 mfma16(Vec8<__bf16> a, Vec8<__bf16> b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(Vec8<_Float16> a, Vec8<_Float16> b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+// Joins the values of the four lanes with the same number modulo 16.
+__device__ __forceinline__ float max_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float add_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return add_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+constexpr uint32_t kBlock = 32;  // keys of a block
+
+template <typename T, int DP>
+struct Stream {
+  static constexpr int C = DP / 8;           // 16-byte chunks of a row
+  static constexpr int RPI = 64 / C;         // rows that one load of values covers
+  static constexpr int NV = kBlock / RPI;    // loads of values for a block (16 keys are a whole number)
+  static constexpr int KK = DP / 32;         // matrix steps over the head
+  static constexpr int DB = DP / 16;         // blocks of 16 output dims
+  static __device__ __forceinline__ uint32_t swizzle(uint32_t r) { return C >= 16 ? (r & 7) << 1 : (r & 6); }
+
+  u32x4 k[2][KK], v[NV];
+
+  // Lane i (and i + 32): page of key i of the block at j0 (-1: past the end, or
+  // no page).
+  static __device__ __forceinline__ int32_t load_pages(const AttnParams& p, const Work& w, uint32_t lane, uint32_t end, uint32_t j0) {
+    const uint32_t j = j0 + (lane & 31u), at = j >> p.page_shift;
+    const bool in = j < end && at < w.n_pages;
+    const int32_t x = *(in ? w.pages + at : (const int32_t*)g_zeros);
+    return in && (uint32_t)x < p.a.cache.n_pages ? x : -1;
+  }
+
+  // The block at j0, whose keys' pages are in `pages` and `there` (a bit for
+  // each key that has one).
+  __device__ __forceinline__ void load_k(const AttnParams& p, const Work& w, uint32_t j0, int32_t pages, uint32_t there) {
+    const gts_kv_cache& kc = p.a.cache;
+    const uint32_t lane = fresh_lane();
+    if (p.near_rows && there == ~0u) {  // all there, 16 keys on one page, nothing to clear
+      const uint32_t off = 2 * (lane % 16 * (uint32_t)kc.k_stride[1]) + lane / 16 * 16;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const char* x = (const char*)page_row(p, w, kc.k, kc.k_stride, j0, t * 16, pages);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) k[t][kk] = *(const u32x4*)(x + kk * 64 + off);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const T* x = any_row(p, w, kc.k, kc.k_stride, j0, t * 16 + lane % 16, pages);
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          const uint32_t d = kk * 32 + lane / 16 * 8;
+          k[t][kk] = *(const u32x4*)(x && d < kc.dim ? x + d : (const T*)g_zeros);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void load_v(const AttnParams& p, const Work& w, uint32_t j0, int32_t pages, uint32_t there) {
+    const gts_kv_cache& kc = p.a.cache;
+    const uint32_t lane = fresh_lane();
+    if (p.near_rows && there == ~0u) {
+      const uint32_t off = 2 * (lane / C * (uint32_t)kc.v_stride[1]) + lane % C * 16;
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        const T* x = page_row(p, w, kc.v, kc.v_stride, j0, n * RPI / 16 * 16, pages) + n * RPI % 16 * kc.v_stride[1];
+        v[n] = *(const u32x4*)((const char*)x + off);
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        const T* x = any_row(p, w, kc.v, kc.v_stride, j0, n * RPI + lane / C, pages);
+        const uint32_t d = lane % C * 8;
+        v[n] = *(const u32x4*)(x && d < kc.dim ? x + d : (const T*)g_zeros);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  // First value of row r0 (the same in all lanes), or of a row of each lane's
+  // own (NULL: it has no page).
+  static __device__ __forceinline__ const T* page_row(const AttnParams& p, const Work& w, const void* base,
+                                                      const int64_t* stride, uint32_t j0, uint32_t r0, int32_t pages) {
+    return (const T*)base + (int64_t)__builtin_amdgcn_readlane(pages, r0) * stride[0] +
+           (int64_t)((j0 + r0) & (p.a.cache.page - 1)) * stride[1] + (int64_t)w.head * stride[2];
+  }
+  static __device__ __forceinline__ const T* any_row(const AttnParams& p, const Work& w, const void* base,
+                                                     const int64_t* stride, uint32_t j0, uint32_t r, int32_t pages) {
+    const int32_t page = __shfl(pages, (int)r);
+    return page < 0 ? nullptr
+                    : (const T*)base + (int64_t)page * stride[0] + (int64_t)((j0 + r) & (p.a.cache.page - 1)) * stride[1] +
+                          (int64_t)w.head * stride[2];
+  }
+};
+
+template <int NR, typename T, int DP>
+__device__ __forceinline__ void run_stream(const AttnParams& p, const Work& w, T* s_kv, float* s_ml, float* stats,
+                                           float* sums) {
+  using S = Stream<T, DP>;
+  const gts_attention_args& a = p.a;
+  const uint32_t lane = fresh_lane(), wave = uni(threadIdx.x >> 6), quarter = lane / 16;
+  const float scale = a.scale;
+  const float c = scale == 0.f ? 1.f : __builtin_fabsf(scale) * kLog2e;
+  const uint32_t begin = w.tile * kTile;
+  const uint32_t end = begin + w.n_tiles * kTile < w.keys ? begin + w.n_tiles * kTile : w.keys;
+  T* sv = s_kv + wave * kBlock * DP;  // this wave's block of values
+
+  S st;
+  uint32_t j0 = begin + wave * kBlock;
+  int32_t pages = S::load_pages(p, w, lane, end, j0);  // of the block to load next
+  int32_t later = S::load_pages(p, w, lane, end, j0 + 4 * kBlock);
+  uint32_t there = (uint32_t)__ballot(pages >= 0);  // keys of the block in k and v
+  st.load_k(p, w, j0, pages, there);
+  st.load_v(p, w, j0, pages, there);
+  pages = later;
+
+  Vec8<T> q[S::KK][NR];
+  f32x4 o[S::DB][NR];
+  float m[NR], l[NR];
+  uint32_t sees[NR];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    const uint32_t row = r * 16 + lane % 16;
+    const bool valid = row < w.rows;
+    const uint32_t flat = w.first_row + (valid ? row : 0);
+    const uint32_t token = p.by_group.div(flat), gq = flat - token * p.group;
+    // scale's sign (and 0) go into the queries: the maximum of q.k is then
+    // that of the scaled scores
+    const T* x = (const T*)a.q + (int64_t)token * a.q_stride[0] + (int64_t)(w.head * p.group + gq) * a.q_stride[1];
+#pragma unroll
+    for (int kk = 0; kk < S::KK; ++kk) {
+      const uint32_t d = kk * 32 + quarter * 8;
+      const bool in = valid && d < a.cache.dim && scale != 0.f;
+      u32x4 y = *(const u32x4*)(in ? x + d : (const T*)g_zeros);
+      if (scale < 0.f) y ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+      q[kk][r] = __builtin_bit_cast(Vec8<T>, y);
+    }
+    sees[r] = w.keys;
+    if (w.own && valid) {
+      const int64_t n = w.see + token;
+      sees[r] = n < 0 ? 0 : n < (int64_t)w.keys ? (uint32_t)n : w.keys;
+    }
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+#pragma unroll
+    for (int d = 0; d < S::DB; ++d) o[d][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  __syncthreads();  // LDS of the stretch before is free
+
+  for (; j0 < end; j0 += 4 * kBlock) {
+    // the page numbers of the block after next are asked for first: waiting for
+    // them later leaves the loads behind them on their way
+    const uint32_t lane = fresh_lane(), quarter = lane / 16;
+    later = S::load_pages(p, w, lane, end, j0 + 8 * kBlock);
+    const uint32_t here = there;
+    there = (uint32_t)__ballot(pages >= 0);
+    f32x4 s[2][NR];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < NR; ++r) {
+        s[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < S::KK; ++kk) s[t][r] = mfma16(__builtin_bit_cast(Vec8<T>, st.k[t][kk]), q[kk][r], s[t][r]);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    st.load_k(p, w, j0 + 4 * kBlock, pages, there);
+    // values to LDS; one that is not finite matters where some rows do not see
+    // every key
+    const bool edge = j0 + kBlock > w.low, mask = edge || here != ~0u;
+    bool odd = false;
+    if (edge && w.low < w.keys) {
+#pragma unroll
+      for (int n = 0; n < S::NV; ++n) odd |= any_not_finite<T>(st.v[n]);
+      odd = __any(odd);
+      if (odd) {
+#pragma unroll
+        for (int n = 0; n < S::NV; ++n) st.v[n] = finite_only<T>(st.v[n]);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < S::NV; ++n) {
+      const uint32_t row = n * S::RPI + lane / S::C;
+      *(u32x4*)(sv + row * DP + ((lane % S::C) ^ S::swizzle(row)) * 8) = st.v[n];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    st.load_v(p, w, j0 + 4 * kBlock, pages, there);
+    pages = later;
+    __builtin_amdgcn_sched_barrier(0);
+
+    Vec8<T> pw[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      if (mask) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t key = i / 4 * 16 + 4 * quarter + i % 4;
+          s[i / 4][r][i % 4] = j0 + key < sees[r] && (here >> key & 1) ? s[i / 4][r][i % 4] : -INFINITY;
+        }
+      }
+      float mx = s[0][r][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i / 4][r][i % 4]);
+      mx = max_quarters(mx);
+      // as in Rows::step
+      if (__any((mx - m[r]) * c > 8.f || (m[r] == -INFINITY && mx > m[r]))) {
+        const float m1 = fmaxf(m[r], mx);
+        const float alpha = m[r] == -INFINITY ? 0.f : exp2_((m[r] - m1) * c);
+        l[r] *= alpha;
+#pragma unroll
+        for (int d = 0; d < S::DB; ++d) o[d][r] *= alpha;
+        m[r] = m1;
+      }
+      const float base = m[r] == -INFINITY ? 0.f : -m[r] * c;
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float e = exp2_(__builtin_fmaf(s[i / 4][r][i % 4], c, base));
+        sum += e;
+        pw[r][i] = (T)e;
+      }
+      l[r] += sum;
+    }
+    // Values of 8 keys at one dim: keys 4 quarter .. + 3 and 16 further.
+    const uint32_t vr = 4 * quarter + lane % 16 / 4;
+    const T* va = sv + vr * DP + lane % 2 * 4;
+    const uint32_t vc = lane % 4 / 2 ^ S::swizzle(vr);
+    typedef __attribute__((address_space(3))) i16x4* lds_t;
+    const auto turned = [&](int d) {
+      union {
+        i16x4 h[2];
+        Vec8<T> v;
+      } u;
+      const T* x = va + (vc ^ (2 * d)) * 8;
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)x);
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(x + 16 * DP));
+      return u.v;
+    };
+#pragma unroll
+    for (int d = 0; d < S::DB; ++d) {
+      const Vec8<T> x = turned(d);
+#pragma unroll
+      for (int r = 0; r < NR; ++r) o[d][r] = mfma16(x, pw[r], o[d][r]);
+    }
+    if (odd) {
+#pragma unroll 1
+      for (uint32_t j = j0; j < j0 + kBlock; ++j) {
+        const T* x = value_row<T>(p, w, j);
+        if (!x) continue;
+#pragma unroll
+        for (int d = 0; d < S::DB; ++d) {
+          const uint32_t at = d * 16 + 4 * quarter;
+          if (at >= a.cache.dim) continue;
+          const Pack<T, 4> y = *(const Pack<T, 4>*)(x + at);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+              if (not_finite((float)y.v[i]) && j < sees[r]) o[d][r][i] += (float)y.v[i];
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+  }
+
+  // the four waves' sums, rows in order, joined by all threads
+  __syncthreads();
+  float* mine = (float*)s_kv + wave * (NR * 16) * DP;
+  static_assert(4 * NR * 16 * DP * 4 <= 4 * kTile * DP * sizeof(T), "the sums fit the tiles' LDS");
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    const uint32_t row = r * 16 + lane % 16;
+    const float sum = add_quarters(l[r]);
+    if (row < w.rows) {
+      if (quarter == 0) {
+        s_ml[(wave * 32 + row) * 2] = m[r];
+        s_ml[(wave * 32 + row) * 2 + 1] = sum;
+      }
+#pragma unroll
+      for (int d = 0; d < S::DB; ++d) *(f32x4*)(mine + row * DP + ((d * 4 + quarter) ^ (row & 15)) * 4) = o[d][r];
+    }
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < w.rows * (DP / 4); i += 256) {
+    const uint32_t row = i / (DP / 4), d = i % (DP / 4);
+    if (d * 4 >= a.cache.dim) continue;
+    float mw[4], top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      mw[x] = s_ml[(x * 32 + row) * 2];
+      top = fmaxf(top, mw[x]);
+    }
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float f = mw[x] == -INFINITY ? 1.f : exp2_((mw[x] - top) * c);
+      sum += s_ml[(x * 32 + row) * 2 + 1] * f;
+      acc += *(const f32x4*)((float*)s_kv + (x * NR * 16 + row) * DP + (d ^ (row & 15)) * 4) * f;
+    }
+    const uint64_t at = w.part + row;
+    *(f32x4*)(sums + at * a.cache.dim + d * 4) = acc;
+    if (d == 0) *(float2*)(stats + 2 * at) = make_float2(top * c, sum);  // base 2 from here on
+  }
+}
+
 template <typename T, int DP>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams p) {
   const gts_attention_args& a = p.a;
@@ -630,6 +945,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   __shared__ uint64_t s_sum[256];
   __shared__ uint64_t s_wave[4];
   __shared__ __align__(8) Flags s_flags;
+  __shared__ __align__(8) float s_ml[4 * 32 * 2];
   const uint32_t tid = threadIdx.x, lane = tid & 63u;
 
   // The plan: places of every sequence, summed.  Thread i takes sequences
@@ -748,7 +1064,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       w.part = uni(w.part + (uint64_t)p.part_rows * g);
       w.tile = uni((uint32_t)(from - zero));
       w.n_tiles = uni((uint32_t)(stop - from));
-      run_stretch<T, DP>(p, w, s_kv, &s_flags, (float*)(scratch + sc.stats), (float*)(scratch + sc.sums));
+      float *stats = (float*)(scratch + sc.stats), *sums = (float*)(scratch + sc.sums);
+      if (w.rg > 1)
+        run_stretch<T, DP>(p, w, s_kv, &s_flags, stats, sums);
+      else if (w.rows <= 16)
+        run_stream<1, T, DP>(p, w, s_kv, s_ml, stats, sums);
+      else
+        run_stream<2, T, DP>(p, w, s_kv, s_ml, stats, sums);
     }
     t = uni(stop);
   }
