@@ -192,7 +192,9 @@ struct Tiles {
 };
 
 // What rows of a tile that do not exist are loaded from.
-__device__ __align__(16) const uint32_t g_zeros[4] = {0, 0, 0, 0};
+__device__ __align__(16) const uint32_t g_zeros[GTS_OPS_MAX_ATTN / 2] = {};  // a row
+// What the page of a key that does not exist is loaded from.
+__device__ const int32_t g_no_page = -1;
 
 // Loads tiles of keys and values from the cache straight into LDS (no
 // registers in between, so nothing is held while the tile before is worked
@@ -657,73 +659,76 @@ struct Stream {
 
   u32x4 k[2][KK], v[NV];
 
-  // Lane i (and i + 32): page of key i of the block at j0 (-1: past the end, or
-  // no page).
-  static __device__ __forceinline__ int32_t load_pages(const AttnParams& p, const Work& w, uint32_t lane, uint32_t end, uint32_t j0) {
+  // Lane i (and i + 32): what the page table says for key i of the block at j0,
+  // or -1 past the end.  One load whatever the lanes need, and nothing here
+  // looks at its result: it is on its way until known_pages.
+  static __device__ __forceinline__ int32_t load_pages(const AttnParams& p, const Work& w, uint32_t lane, uint32_t end,
+                                                       uint32_t j0) {
     const uint32_t j = j0 + (lane & 31u), at = j >> p.page_shift;
-    const bool in = j < end && at < w.n_pages;
-    const int32_t x = *(in ? w.pages + at : (const int32_t*)g_zeros);
-    return in && (uint32_t)x < p.a.cache.n_pages ? x : -1;
+    uint64_t x = (uint64_t)(j < end && at < w.n_pages ? w.pages + at : &g_no_page);
+    asm volatile("" : "+v"(x));
+    return *(const __attribute__((address_space(1))) int32_t*)x;
+  }
+  static __device__ __forceinline__ int32_t known_pages(const AttnParams& p, int32_t pages) {
+    return (uint32_t)pages < p.a.cache.n_pages ? pages : -1;
   }
 
   // The block at j0, whose keys' pages are in `pages` and `there` (a bit for
-  // each key that has one).
+  // each key that has one).  Addresses come from one branch or the other, the
+  // loads from neither: the compiler then knows how many are on their way.
   __device__ __forceinline__ void load_k(const AttnParams& p, const Work& w, uint32_t j0, int32_t pages, uint32_t there) {
     const gts_kv_cache& kc = p.a.cache;
     const uint32_t lane = fresh_lane();
-    if (p.near_rows && there == ~0u) {  // all there, 16 keys on one page, nothing to clear
-      const uint32_t off = 2 * (lane % 16 * (uint32_t)kc.k_stride[1]) + lane / 16 * 16;
+    const char* x[2];
+    if (p.near_rows && there == ~0u) {  // all there, 16 keys on one page
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const char* x = (const char*)page_row(p, w, kc.k, kc.k_stride, j0, t * 16, pages);
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) k[t][kk] = *(const u32x4*)(x + kk * 64 + off);
-      }
+      for (int t = 0; t < 2; ++t)
+        x[t] = page_row(p, w, kc.k, kc.k_stride, j0, t * 16, pages) + 2 * (lane % 16 * (uint32_t)kc.k_stride[1]);
     } else {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const T* x = any_row(p, w, kc.k, kc.k_stride, j0, t * 16 + lane % 16, pages);
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          const uint32_t d = kk * 32 + lane / 16 * 8;
-          k[t][kk] = *(const u32x4*)(x && d < kc.dim ? x + d : (const T*)g_zeros);
-        }
-      }
+      for (int t = 0; t < 2; ++t) x[t] = any_row(p, w, kc.k, kc.k_stride, j0, t * 16 + lane % 16, pages);
     }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const uint32_t d = kk * 32 + lane / 16 * 8;
+        k[t][kk] = load16((d < kc.dim ? x[t] : (const char*)g_zeros) + d * 2);
+      }
   }
   __device__ __forceinline__ void load_v(const AttnParams& p, const Work& w, uint32_t j0, int32_t pages, uint32_t there) {
     const gts_kv_cache& kc = p.a.cache;
     const uint32_t lane = fresh_lane();
+    const char* x[NV];
     if (p.near_rows && there == ~0u) {
-      const uint32_t off = 2 * (lane / C * (uint32_t)kc.v_stride[1]) + lane % C * 16;
+      const uint32_t off = 2 * (lane / C * (uint32_t)kc.v_stride[1]);
 #pragma unroll
-      for (int n = 0; n < NV; ++n) {
-        const T* x = page_row(p, w, kc.v, kc.v_stride, j0, n * RPI / 16 * 16, pages) + n * RPI % 16 * kc.v_stride[1];
-        v[n] = *(const u32x4*)((const char*)x + off);
-      }
+      for (int n = 0; n < NV; ++n)
+        x[n] = page_row(p, w, kc.v, kc.v_stride, j0, n * RPI / 16 * 16, pages) + n * RPI % 16 * kc.v_stride[1] * 2 + off;
     } else {
 #pragma unroll
-      for (int n = 0; n < NV; ++n) {
-        const T* x = any_row(p, w, kc.v, kc.v_stride, j0, n * RPI + lane / C, pages);
-        const uint32_t d = lane % C * 8;
-        v[n] = *(const u32x4*)(x && d < kc.dim ? x + d : (const T*)g_zeros);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      for (int n = 0; n < NV; ++n) x[n] = any_row(p, w, kc.v, kc.v_stride, j0, n * RPI + lane / C, pages);
     }
+    const uint32_t d = lane % C * 8;
+#pragma unroll
+    for (int n = 0; n < NV; ++n) v[n] = load16((d < kc.dim ? x[n] : (const char*)g_zeros) + d * 2);
   }
-  // First value of row r0 (the same in all lanes), or of a row of each lane's
-  // own (NULL: it has no page).
-  static __device__ __forceinline__ const T* page_row(const AttnParams& p, const Work& w, const void* base,
-                                                      const int64_t* stride, uint32_t j0, uint32_t r0, int32_t pages) {
-    return (const T*)base + (int64_t)__builtin_amdgcn_readlane(pages, r0) * stride[0] +
-           (int64_t)((j0 + r0) & (p.a.cache.page - 1)) * stride[1] + (int64_t)w.head * stride[2];
+  static __device__ __forceinline__ u32x4 load16(const char* x) {
+    return *(const __attribute__((address_space(1))) u32x4*)(uint64_t)x;
   }
-  static __device__ __forceinline__ const T* any_row(const AttnParams& p, const Work& w, const void* base,
-                                                     const int64_t* stride, uint32_t j0, uint32_t r, int32_t pages) {
+  // Row r0 of the block (the same in all lanes), or a row of each lane's own
+  // (the zeros, when it has no page).
+  static __device__ __forceinline__ const char* page_row(const AttnParams& p, const Work& w, const void* base,
+                                                         const int64_t* stride, uint32_t j0, uint32_t r0, int32_t pages) {
+    return (const char*)((const T*)base + (int64_t)__builtin_amdgcn_readlane(pages, r0) * stride[0] +
+                         (int64_t)((j0 + r0) & (p.a.cache.page - 1)) * stride[1] + (int64_t)w.head * stride[2]);
+  }
+  static __device__ __forceinline__ const char* any_row(const AttnParams& p, const Work& w, const void* base,
+                                                        const int64_t* stride, uint32_t j0, uint32_t r, int32_t pages) {
     const int32_t page = __shfl(pages, (int)r);
-    return page < 0 ? nullptr
-                    : (const T*)base + (int64_t)page * stride[0] + (int64_t)((j0 + r) & (p.a.cache.page - 1)) * stride[1] +
-                          (int64_t)w.head * stride[2];
+    const T* x = (const T*)base + (int64_t)page * stride[0] + (int64_t)((j0 + r) & (p.a.cache.page - 1)) * stride[1] +
+                 (int64_t)w.head * stride[2];
+    return page < 0 ? (const char*)g_zeros : (const char*)x;
   }
 };
 
@@ -743,6 +748,7 @@ __device__ __forceinline__ void run_stream(const AttnParams& p, const Work& w, T
   uint32_t j0 = begin + wave * kBlock;
   int32_t pages = S::load_pages(p, w, lane, end, j0);  // of the block to load next
   int32_t later = S::load_pages(p, w, lane, end, j0 + 4 * kBlock);
+  pages = S::known_pages(p, pages);
   uint32_t there = (uint32_t)__ballot(pages >= 0);  // keys of the block in k and v
   st.load_k(p, w, j0, pages, there);
   st.load_v(p, w, j0, pages, there);
@@ -787,6 +793,7 @@ __device__ __forceinline__ void run_stream(const AttnParams& p, const Work& w, T
     const uint32_t lane = fresh_lane(), quarter = lane / 16;
     later = S::load_pages(p, w, lane, end, j0 + 8 * kBlock);
     const uint32_t here = there;
+    pages = S::known_pages(p, pages);
     there = (uint32_t)__ballot(pages >= 0);
     f32x4 s[2][NR];
 #pragma unroll
