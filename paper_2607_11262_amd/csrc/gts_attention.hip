@@ -8,11 +8,13 @@
 // up to 128 query rows (a row: one new token's one query head).  For the
 // prefix the rows are those of all tokens of the batch, so its keys are read
 // once for everybody; for a sequence's own keys they are its tokens'.  The
-// tiles of all (head, rows) segments stand in one line, each segment's behind
-// a few places for what beginning and ending it costs, and each workgroup takes
-// an equal stretch of that line, wherever it starts and ends: ragged lengths and
-// few rows fill the chip alike.  A stretch leaves one partial result per
-// segment of which it has tiles (unnormalised sum, running maximum and sum of the
+// tiles of all segments (rows with the keys that they see) stand in one line,
+// each segment's behind a few places for what beginning and ending it costs.
+// The line is the same for every key-value head; it is cut into equal stretches,
+// wherever they start and end, one for each workgroup of the head: ragged
+// lengths and few rows fill the chip alike, and the workgroups of all heads walk
+// the same pages at the same time, where the heads of a token lie side by side.
+// A stretch leaves one partial result per segment of which it has tiles (unnormalised sum, running maximum and sum of the
 // softmax, 32 bits), and the join adds up the partials of each row.
 //
 // The row kernel: one wavefront per (token, query head) walks the row's keys 64
@@ -39,7 +41,7 @@ struct AttnParams {
   uint32_t group;       // query heads of a key-value head
   FastDiv by_group;
   bool near_rows;       // see Loader
-  uint32_t workgroups;  // a multiple of 8
+  uint32_t cuts;        // stretches of a head's line: so many workgroups for each head
   uint32_t part_rows;   // rows that a cut between workgroups may add to the partials
 };
 
@@ -52,11 +54,11 @@ struct Scratch {
   uint64_t begin, stats, sums, bytes;  // offsets; begin: [batch] first place of each sequence
 };
 __host__ __device__ inline uint64_t up256(uint64_t x) { return (x + 255) & ~255ull; }
-__host__ __device__ inline Scratch scratch_layout(uint32_t batch, uint64_t rows, uint32_t part_rows, uint32_t dim) {
+__host__ __device__ inline Scratch scratch_layout(uint32_t batch, uint64_t rows, uint64_t cut_rows, uint32_t dim) {
   Scratch s;
   s.begin = 256;
   s.stats = s.begin + up256(8ull * batch);
-  const uint64_t n = 2 * rows + (uint64_t)part_rows * kGroups;
+  const uint64_t n = 2 * rows + cut_rows;
   s.sums = s.stats + up256(8 * n);
   s.bytes = s.sums + up256(4 * n * dim);
   return s;
@@ -151,8 +153,8 @@ __device__ __forceinline__ uint32_t own_tiles(const AttnParams& p, const Seq& s,
   return (seen(s, last) + kTile - 1) / kTile;
 }
 __device__ __forceinline__ uint32_t places(uint32_t tiles) { return tiles ? tiles + kSegment : 0; }
-// Places of a sequence's segments of one head.
-__device__ __forceinline__ uint64_t head_places(const AttnParams& p, const Seq& s) {
+// Places of a sequence's segments.
+__device__ __forceinline__ uint64_t seq_places(const AttnParams& p, const Seq& s) {
   const uint32_t rows = s.n * p.group;
   if (rows == 0 || s.keys == 0) return 0;
   const uint32_t rg = row_groups(rows), n = (rows + 32 * rg - 1) / (32 * rg);
@@ -961,11 +963,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   const uint32_t prows = a.batch.tokens * p.group;
   const uint32_t prg = row_groups(prows), n_prt = (prows + 32 * prg - 1) / (32 * prg);
   const uint32_t ptiles = (P + kTile - 1) / kTile;
-  const uint64_t prefix_places = (uint64_t)places(ptiles) * n_prt * hkv;
+  const uint64_t prefix_places = (uint64_t)places(ptiles) * n_prt;
   uint64_t mine = 0;
   for (uint32_t i = 0; i < per_thread; ++i) {
     const uint32_t b = tid * per_thread + i;
-    if (b < B) mine += head_places(p, load_seq(p, b)) * hkv;
+    if (b < B) mine += seq_places(p, load_seq(p, b));
   }
   uint64_t scan = mine;
   for (int i = 1; i < 64; i <<= 1) {
@@ -978,9 +980,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   for (uint32_t i = 0; i < tid >> 6; ++i) before += s_wave[i];
   s_sum[tid] = before + scan - mine;  // first place of this thread's sequences
   const uint64_t total = uni(prefix_places + s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3]);
-  const uint64_t per = (total + p.workgroups - 1) / p.workgroups;
+  const uint64_t per = (total + p.cuts - 1) / p.cuts;
   const uint64_t rows = (uint64_t)a.batch.tokens * a.q_heads;
-  const Scratch sc = scratch_layout(B, rows, p.part_rows, a.cache.dim);
+  const uint64_t cut_rows = (uint64_t)p.part_rows * p.cuts;  // of a head
+  const Scratch sc = scratch_layout(B, rows, cut_rows * hkv, a.cache.dim);
   char* scratch = (char*)a.scratch;
   if (blockIdx.x == 0) {
     uint64_t t = s_sum[tid];
@@ -988,15 +991,17 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       const uint32_t b = tid * per_thread + i;
       if (b >= B) break;
       ((uint64_t*)(scratch + sc.begin))[b] = t;
-      t += head_places(p, load_seq(p, b)) * hkv;
+      t += seq_places(p, load_seq(p, b));
     }
     if (tid == 0) *(Plan*)scratch = Plan{per};
   }
   __syncthreads();
 
-  // neighbours in the line go to one XCD (workgroups go round the eight of
-  // them), whose L2 then has the keys that they share
-  const uint32_t g = (blockIdx.x & 7u) * (p.workgroups / 8) + (blockIdx.x >> 3);
+  // Workgroups go round the eight XCDs: give each a run of the (head, stretch)
+  // pairs, so that rows which share keys also share an L2.
+  const uint32_t xcd = blockIdx.x & 7u, share = gridDim.x / 8, extra = gridDim.x % 8;
+  const uint32_t id = xcd * share + (xcd < extra ? xcd : extra) + (blockIdx.x >> 3);
+  const uint32_t head = id / p.cuts, g = id - head * p.cuts;
   uint64_t t = (uint64_t)g * per, end = t + per;
   if (end > total) end = total;
   while (t < end) {
@@ -1005,10 +1010,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
     uint32_t tiles;  // its tiles
     if (t < prefix_places) {
       tiles = ptiles;
-      const uint32_t s = (uint32_t)(t / places(tiles));
-      w.head = s / n_prt;
-      const uint32_t rt = s - w.head * n_prt;
-      seg = (uint64_t)s * places(tiles);
+      const uint32_t rt = (uint32_t)(t / places(tiles));
+      seg = (uint64_t)rt * places(tiles);
       w.pages = a.prefix_pages;
       w.n_pages = a.n_prefix_pages;
       w.keys = w.low = P;
@@ -1017,7 +1020,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       w.rows = prows - w.first_row < 32 * prg ? prows - w.first_row : 32 * prg;
       w.own = false;
       w.see = 0;
-      w.part = (uint64_t)w.head * prows + w.first_row;
+      w.part = w.first_row;
     } else {
       // the last thread whose sequences start at or before t, then its
       // sequences one by one (one, up to 256 sequences)
@@ -1027,17 +1030,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       uint32_t b = who * per_thread;
       uint64_t first = uni(s_sum[who]);
       Seq s = load_seq(p, b < B ? b : B - 1);
-      uint64_t ht = head_places(p, s);
-      for (uint32_t i = 1; i < per_thread && t >= first + ht * hkv; ++i) {
-        first += ht * hkv;
+      for (uint32_t i = 1; i < per_thread && t >= first + seq_places(p, s); ++i) {
+        first += seq_places(p, s);
         s = load_seq(p, ++b);
-        ht = head_places(p, s);
       }
-      const uint64_t rel = t - first;
-      w.head = uni((uint32_t)(rel / ht));
       w.rg = row_groups(s.n * p.group);
       uint32_t rt = 0;
-      seg = first + w.head * ht;
+      seg = first;
       tiles = own_tiles(p, s, w.rg, 0);
       while (t >= seg + places(tiles)) {
         seg += places(tiles);
@@ -1052,8 +1051,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       w.keys = seen(s, p.by_group.div(r0 + w.rows - 1));
       w.own = true;
       w.see = s.len - s.n + 1 - (int64_t)s.first;
-      w.part = rows + (uint64_t)hkv * s.first * p.group + (uint64_t)w.head * srows + r0;
+      w.part = (uint64_t)prows + s.first * p.group + r0;
     }
+    w.head = head;
     // tile i stands at place seg + kSegment + i
     const uint64_t zero = seg + kSegment, stop = end < zero + tiles ? end : zero + tiles;
     if (stop > zero) {
@@ -1068,7 +1068,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       w.rows = uni(w.rows);
       w.first_row = uni(w.first_row);
       w.see = (int64_t)uni((uint64_t)w.see);
-      w.part = uni(w.part + (uint64_t)p.part_rows * g);
+      w.part = uni((uint64_t)(w.part + ((uint64_t)2 * prows + cut_rows) * head + (uint64_t)p.part_rows * g));
       w.tile = uni((uint32_t)(from - zero));
       w.n_tiles = uni((uint32_t)(stop - from));
       float *stats = (float*)(scratch + sc.stats), *sums = (float*)(scratch + sc.sums);
@@ -1092,7 +1092,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
   if (row >= rows) return;
   const uint32_t t = uni((uint32_t)(row / a.q_heads)), hq = uni((uint32_t)(row - (uint64_t)t * a.q_heads));
   const uint32_t head = p.by_group.div(hq), gq = hq - head * p.group, hkv = a.cache.heads, D = a.cache.dim;
-  const Scratch sc = scratch_layout(a.batch.batch, rows, p.part_rows, D);
+  const uint64_t cut_rows = (uint64_t)p.part_rows * p.cuts;
+  const Scratch sc = scratch_layout(a.batch.batch, rows, cut_rows * hkv, D);
   const char* scratch = (const char*)a.scratch;
   const Plan plan = *(const Plan*)scratch;
   const float* stats = (const float*)(scratch + sc.stats);
@@ -1107,20 +1108,21 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
         const uint32_t P = a.cache.n_pages ? a.batch.prefix_len : 0;
         n = (P + kTile - 1) / kTile;
         const uint32_t prows = a.batch.tokens * p.group, rg = row_groups(prows);
-        const uint32_t r = t * p.group + gq, n_rt = (prows + 32 * rg - 1) / (32 * rg);
-        first = places((uint32_t)n) * ((uint64_t)head * n_rt + r / (32 * rg));
-        at = (uint64_t)head * prows + r;
+        const uint32_t r = t * p.group + gq;
+        first = places((uint32_t)n) * (uint64_t)(r / (32 * rg));
+        at = r;
       } else {
         const Seq s = load_seq(p, seq);
         const uint32_t srows = s.n * p.group, rg = row_groups(srows), r = index * p.group + gq, rt = r / (32 * rg);
         if (s.keys == 0) continue;
-        first = ((const uint64_t*)(scratch + sc.begin))[seq] + head * head_places(p, s);
+        first = ((const uint64_t*)(scratch + sc.begin))[seq];
         for (uint32_t i = 0; i < rt; ++i) first += places(own_tiles(p, s, rg, i));
         n = own_tiles(p, s, rg, rt);
-        at = rows + (uint64_t)hkv * s.first * p.group + (uint64_t)head * srows + r;
+        at = (uint64_t)a.batch.tokens * p.group + s.first * p.group + r;
       }
       if (n == 0) continue;
       first += kSegment;
+      at += (2ull * a.batch.tokens * p.group + cut_rows) * head;
       const uint64_t g1 = (first + n - 1) / plan.per;
       for (uint64_t g = first / plan.per; g <= g1; ++g) {
         const uint64_t x = at + p.part_rows * g;
@@ -1230,8 +1232,17 @@ static uint32_t part_rows(uint32_t tokens, uint32_t group) {
   return rows > 64 ? kMostRows : rows > 32 ? 64 : 32;
 }
 
+// Stretches of a head: two workgroups a CU (one with the largest heads, which
+// take all of its LDS) over all heads, at least one each.
+static uint32_t cuts(uint32_t kv_heads, uint32_t dim) {
+  const uint32_t n = (dim > 128 ? kGroups / 2 : kGroups) / kv_heads;
+  return n ? n : 1;
+}
+
 uint64_t attention_scratch(uint32_t batch, uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t dim) {
-  return scratch_layout(batch, (uint64_t)tokens * q_heads, part_rows(tokens, q_heads / kv_heads), dim).bytes;
+  return scratch_layout(batch, (uint64_t)tokens * q_heads,
+                        (uint64_t)part_rows(tokens, q_heads / kv_heads) * cuts(kv_heads, dim) * kv_heads, dim)
+      .bytes;
 }
 
 // The tile kernel's loads: 16-bit values, every row of q, k and v and every 16
@@ -1254,13 +1265,14 @@ static hipError_t launch_typed(AttnParams& p, hipStream_t stream) {
   const dim3 grid((uint32_t)((rows + 3) / 4)), block(256);
   if constexpr (sizeof(T) == 2) {
     if (tiles_fit(a)) {
-      p.workgroups = a.cache.dim > 128 ? kGroups / 2 : kGroups;
+      p.cuts = cuts(a.cache.heads, a.cache.dim);
+      const dim3 wgs(p.cuts * a.cache.heads);
       if (a.cache.dim <= 64)
-        tile_kernel<T, 64><<<dim3(p.workgroups), block, 0, stream>>>(p);
+        tile_kernel<T, 64><<<wgs, block, 0, stream>>>(p);
       else if (a.cache.dim <= 128)
-        tile_kernel<T, 128><<<dim3(p.workgroups), block, 0, stream>>>(p);
+        tile_kernel<T, 128><<<wgs, block, 0, stream>>>(p);
       else
-        tile_kernel<T, 256><<<dim3(p.workgroups), block, 0, stream>>>(p);
+        tile_kernel<T, 256><<<wgs, block, 0, stream>>>(p);
       join_kernel<T><<<grid, block, 0, stream>>>(p);
       return hipGetLastError();
     }
