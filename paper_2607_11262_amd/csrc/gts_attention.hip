@@ -9,7 +9,7 @@
 // prefix the rows are those of all tokens of the batch, so its keys are read
 // once for everybody; for a sequence's own keys they are its tokens'.  The
 // tiles of all segments (rows with the keys that they see) stand in one line,
-// each segment's behind a few places for what beginning and ending it costs.
+// with as many places as they cost, behind some for a segment's begin and end.
 // The line is the same for every key-value head; it is cut into equal stretches,
 // wherever they start and end, one for each workgroup of the head: ragged
 // lengths and few rows fill the chip alike, and the workgroups of all heads walk
@@ -32,7 +32,14 @@ constexpr uint32_t kTile = 64;        // keys of a tile
 constexpr uint32_t kMostRows = 128;   // query rows of a segment
 constexpr uint32_t kGroups = 512;     // most workgroups: two a CU
 
-constexpr uint32_t kSegment = 6;     // places in the line for a segment's begin and end
+// Places in the line (of about half a microsecond): a segment's begin and end,
+// and a tile, by the segment's row groups.  Measured with few rows 5 us and 1 us
+// (nothing else running), with 128 rows 12 us and 2.6 us (two workgroups a CU).
+constexpr uint32_t kMostPlaces = 5;
+__host__ __device__ __forceinline__ uint32_t segment_places(uint32_t row_groups) { return row_groups == 1 ? 10 : 24; }
+__host__ __device__ __forceinline__ uint32_t tile_places(uint32_t row_groups) {
+  return row_groups == 1 ? 2 : row_groups == 2 ? 3 : kMostPlaces;
+}
 
 // What the kernels need beside the arguments.
 struct AttnParams {
@@ -152,14 +159,16 @@ __device__ __forceinline__ uint32_t own_tiles(const AttnParams& p, const Seq& s,
   const uint32_t last = p.by_group.div((rows < end ? rows : end) - 1);
   return (seen(s, last) + kTile - 1) / kTile;
 }
-__device__ __forceinline__ uint32_t places(uint32_t tiles) { return tiles ? tiles + kSegment : 0; }
+__device__ __forceinline__ uint64_t places(uint32_t tiles, uint32_t rg) {
+  return tiles ? (uint64_t)tiles * tile_places(rg) + segment_places(rg) : 0;
+}
 // Places of a sequence's segments.
 __device__ __forceinline__ uint64_t seq_places(const AttnParams& p, const Seq& s) {
   const uint32_t rows = s.n * p.group;
   if (rows == 0 || s.keys == 0) return 0;
   const uint32_t rg = row_groups(rows), n = (rows + 32 * rg - 1) / (32 * rg);
   uint64_t t = 0;
-  for (uint32_t rt = 0; rt < n; ++rt) t += places(own_tiles(p, s, rg, rt));
+  for (uint32_t rt = 0; rt < n; ++rt) t += places(own_tiles(p, s, rg, rt), rg);
   return t;
 }
 
@@ -625,12 +634,12 @@ __device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, 
 // ---- few rows: a stream of keys per wave -------------------------------------------
 //
 // With at most 32 rows the products are small beside the bytes: every wave
-// takes blocks of 32 keys of its own and waits for nobody.  Keys go from the
-// cache to registers just as the matrix instruction takes them (16 keys x 32
-// dims); values are held in registers until the block before is done with the
-// wave's part of the LDS, where they are turned.  So 16 KiB a wave (head dim
-// 128) are on their way while it computes.  16 x 16 tiles, because decode has
-// few rows (query heads of a key-value head).
+// takes blocks of 32 keys of its own and waits for nobody.  Whole rows of keys and
+// values go to registers, and from there to the wave's part of the LDS when the
+// block before is done with it: 16 KiB a wave (head dim 128) are on their way
+// while it computes.  (Keys loaded as the matrix instruction takes them, 64
+// bytes of each of 16 rows, without LDS: 7 % slower on 64 ragged sequences.)
+// 16 x 16 tiles, because decode has few rows (query heads of a key-value head).
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ f32x4 mfma16(Vec8<__bf16> a, Vec8<__bf16> b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -657,9 +666,12 @@ struct Stream {
   static constexpr int NV = kBlock / RPI;    // loads of values for a block (16 keys are a whole number)
   static constexpr int KK = DP / 32;         // matrix steps over the head
   static constexpr int DB = DP / 16;         // blocks of 16 output dims
-  static __device__ __forceinline__ uint32_t swizzle(uint32_t r) { return C >= 16 ? (r & 7) << 1 : (r & 6); }
+  // Chunk c of row r stands at c ^ swizzle(r), for the reads of 16 rows at one
+  // chunk (keys) and of 16 rows x 32 bytes (values).
+  static __device__ __forceinline__ uint32_t swizzle_k(uint32_t r) { return C >= 16 ? r & 15 : (r >> 1) & 7; }
+  static __device__ __forceinline__ uint32_t swizzle_v(uint32_t r) { return C >= 16 ? (r & 7) << 1 : r & 6; }
 
-  u32x4 k[2][KK], v[NV];
+  u32x4 k[NV], v[NV];
 
   // Lane i (and i + 32): what the page table says for key i of the block at j0,
   // or -1 past the end.  One load whatever the lanes need, and nothing here
@@ -678,42 +690,23 @@ struct Stream {
   // The block at j0, whose keys' pages are in `pages` and `there` (a bit for
   // each key that has one).  Addresses come from one branch or the other, the
   // loads from neither: the compiler then knows how many are on their way.
-  __device__ __forceinline__ void load_k(const AttnParams& p, const Work& w, uint32_t j0, int32_t pages, uint32_t there) {
-    const gts_kv_cache& kc = p.a.cache;
-    const uint32_t lane = fresh_lane();
-    const char* x[2];
-    if (p.near_rows && there == ~0u) {  // all there, 16 keys on one page
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        x[t] = page_row(p, w, kc.k, kc.k_stride, j0, t * 16, pages) + 2 * (lane % 16 * (uint32_t)kc.k_stride[1]);
-    } else {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) x[t] = any_row(p, w, kc.k, kc.k_stride, j0, t * 16 + lane % 16, pages);
-    }
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        const uint32_t d = kk * 32 + lane / 16 * 8;
-        k[t][kk] = load16((d < kc.dim ? x[t] : (const char*)g_zeros) + d * 2);
-      }
-  }
-  __device__ __forceinline__ void load_v(const AttnParams& p, const Work& w, uint32_t j0, int32_t pages, uint32_t there) {
-    const gts_kv_cache& kc = p.a.cache;
+  static __device__ __forceinline__ void load(const AttnParams& p, const Work& w, const void* base,
+                                              const int64_t* stride, uint32_t j0, int32_t pages, uint32_t there,
+                                              u32x4 (&to)[NV]) {
     const uint32_t lane = fresh_lane();
     const char* x[NV];
-    if (p.near_rows && there == ~0u) {
-      const uint32_t off = 2 * (lane / C * (uint32_t)kc.v_stride[1]);
+    if (p.near_rows && there == ~0u) {  // all there, 16 keys on one page
+      const uint32_t off = 2 * (lane / C * (uint32_t)stride[1]);
 #pragma unroll
       for (int n = 0; n < NV; ++n)
-        x[n] = page_row(p, w, kc.v, kc.v_stride, j0, n * RPI / 16 * 16, pages) + n * RPI % 16 * kc.v_stride[1] * 2 + off;
+        x[n] = page_row(p, w, base, stride, j0, n * RPI / 16 * 16, pages) + n * RPI % 16 * stride[1] * 2 + off;
     } else {
 #pragma unroll
-      for (int n = 0; n < NV; ++n) x[n] = any_row(p, w, kc.v, kc.v_stride, j0, n * RPI + lane / C, pages);
+      for (int n = 0; n < NV; ++n) x[n] = any_row(p, w, base, stride, j0, n * RPI + lane / C, pages);
     }
     const uint32_t d = lane % C * 8;
 #pragma unroll
-    for (int n = 0; n < NV; ++n) v[n] = load16((d < kc.dim ? x[n] : (const char*)g_zeros) + d * 2);
+    for (int n = 0; n < NV; ++n) to[n] = load16((d < p.a.cache.dim ? x[n] : (const char*)g_zeros) + d * 2);
   }
   static __device__ __forceinline__ u32x4 load16(const char* x) {
     return *(const __attribute__((address_space(1))) u32x4*)(uint64_t)x;
@@ -744,7 +737,8 @@ __device__ __forceinline__ void run_stream(const AttnParams& p, const Work& w, T
   const float c = scale == 0.f ? 1.f : __builtin_fabsf(scale) * kLog2e;
   const uint32_t begin = w.tile * kTile;
   const uint32_t end = begin + w.n_tiles * kTile < w.keys ? begin + w.n_tiles * kTile : w.keys;
-  T* sv = s_kv + wave * kBlock * DP;  // this wave's block of values
+  T* sk = s_kv + wave * 2 * kBlock * DP;  // this wave's block of keys, then of values
+  T* sv = sk + kBlock * DP;
 
   S st;
   uint32_t j0 = begin + wave * kBlock;
@@ -752,8 +746,8 @@ __device__ __forceinline__ void run_stream(const AttnParams& p, const Work& w, T
   int32_t later = S::load_pages(p, w, lane, end, j0 + 4 * kBlock);
   pages = S::known_pages(p, pages);
   uint32_t there = (uint32_t)__ballot(pages >= 0);  // keys of the block in k and v
-  st.load_k(p, w, j0, pages, there);
-  st.load_v(p, w, j0, pages, there);
+  S::load(p, w, a.cache.k, a.cache.k_stride, j0, pages, there, st.k);
+  S::load(p, w, a.cache.v, a.cache.v_stride, j0, pages, there, st.v);
   pages = later;
 
   Vec8<T> q[S::KK][NR];
@@ -797,17 +791,29 @@ __device__ __forceinline__ void run_stream(const AttnParams& p, const Work& w, T
     const uint32_t here = there;
     pages = S::known_pages(p, pages);
     there = (uint32_t)__ballot(pages >= 0);
+    const uint32_t next = j0 + 4 * kBlock;
+#pragma unroll
+    for (int n = 0; n < S::NV; ++n) {
+      const uint32_t row = n * S::RPI + lane / S::C;
+      *(u32x4*)(sk + row * DP + ((lane % S::C) ^ S::swizzle_k(row)) * 8) = st.k[n];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    S::load(p, w, a.cache.k, a.cache.k_stride, next, pages, there, st.k);
+    __builtin_amdgcn_sched_barrier(0);
     f32x4 s[2][NR];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 2; ++t) {
 #pragma unroll
-      for (int r = 0; r < NR; ++r) {
-        s[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int r = 0; r < NR; ++r) s[t][r] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int kk = 0; kk < S::KK; ++kk) s[t][r] = mfma16(__builtin_bit_cast(Vec8<T>, st.k[t][kk]), q[kk][r], s[t][r]);
+      for (int kk = 0; kk < S::KK; ++kk) {
+        const uint32_t row = lane % 16;
+        const Vec8<T> x =
+            *(const Vec8<T>*)(sk + (t * 16 + row) * DP + (quarter ^ S::swizzle_k(row) ^ (4 * kk)) * 8);
+#pragma unroll
+        for (int r = 0; r < NR; ++r) s[t][r] = mfma16(x, q[kk][r], s[t][r]);
       }
-    __builtin_amdgcn_sched_barrier(0);
-    st.load_k(p, w, j0 + 4 * kBlock, pages, there);
+    }
     // values to LDS; one that is not finite matters where some rows do not see
     // every key
     const bool edge = j0 + kBlock > w.low, mask = edge || here != ~0u;
@@ -824,10 +830,10 @@ __device__ __forceinline__ void run_stream(const AttnParams& p, const Work& w, T
 #pragma unroll
     for (int n = 0; n < S::NV; ++n) {
       const uint32_t row = n * S::RPI + lane / S::C;
-      *(u32x4*)(sv + row * DP + ((lane % S::C) ^ S::swizzle(row)) * 8) = st.v[n];
+      *(u32x4*)(sv + row * DP + ((lane % S::C) ^ S::swizzle_v(row)) * 8) = st.v[n];
     }
     __builtin_amdgcn_sched_barrier(0);
-    st.load_v(p, w, j0 + 4 * kBlock, pages, there);
+    S::load(p, w, a.cache.v, a.cache.v_stride, next, pages, there, st.v);
     pages = later;
     __builtin_amdgcn_sched_barrier(0);
 
@@ -867,7 +873,7 @@ __device__ __forceinline__ void run_stream(const AttnParams& p, const Work& w, T
     // Values of 8 keys at one dim: keys 4 quarter .. + 3 and 16 further.
     const uint32_t vr = 4 * quarter + lane % 16 / 4;
     const T* va = sv + vr * DP + lane % 2 * 4;
-    const uint32_t vc = lane % 4 / 2 ^ S::swizzle(vr);
+    const uint32_t vc = lane % 4 / 2 ^ S::swizzle_v(vr);
     typedef __attribute__((address_space(3))) i16x4* lds_t;
     const auto turned = [&](int d) {
       union {
@@ -963,7 +969,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   const uint32_t prows = a.batch.tokens * p.group;
   const uint32_t prg = row_groups(prows), n_prt = (prows + 32 * prg - 1) / (32 * prg);
   const uint32_t ptiles = (P + kTile - 1) / kTile;
-  const uint64_t prefix_places = (uint64_t)places(ptiles) * n_prt;
+  const uint64_t prefix_places = places(ptiles, prg) * n_prt;
   uint64_t mine = 0;
   for (uint32_t i = 0; i < per_thread; ++i) {
     const uint32_t b = tid * per_thread + i;
@@ -980,7 +986,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   for (uint32_t i = 0; i < tid >> 6; ++i) before += s_wave[i];
   s_sum[tid] = before + scan - mine;  // first place of this thread's sequences
   const uint64_t total = uni(prefix_places + s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3]);
-  const uint64_t per = (total + p.cuts - 1) / p.cuts;
+  // at least a tile's: then every stretch between a segment's first and last
+  // tile begins one
+  uint64_t per = (total + p.cuts - 1) / p.cuts;
+  if (per < kMostPlaces) per = kMostPlaces;
   const uint64_t rows = (uint64_t)a.batch.tokens * a.q_heads;
   const uint64_t cut_rows = (uint64_t)p.part_rows * p.cuts;  // of a head
   const Scratch sc = scratch_layout(B, rows, cut_rows * hkv, a.cache.dim);
@@ -997,11 +1006,21 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   }
   __syncthreads();
 
-  // Workgroups go round the eight XCDs: give each a run of the (head, stretch)
-  // pairs, so that rows which share keys also share an L2.
-  const uint32_t xcd = blockIdx.x & 7u, share = gridDim.x / 8, extra = gridDim.x % 8;
-  const uint32_t id = xcd * share + (xcd < extra ? xcd : extra) + (blockIdx.x >> 3);
-  const uint32_t head = id / p.cuts, g = id - head * p.cuts;
+  // Workgroups go round the eight XCDs.  Where the prefix has several segments
+  // its keys are read several times: an XCD then takes a run of (head,
+  // stretch) pairs and finds them in its L2.  Else every XCD takes all heads in
+  // turn: a head's rows alone lie on some of the memory channels, which are
+  // nearer to some XCDs.
+  uint32_t head, g;
+  if (n_prt > 1 && P) {
+    const uint32_t xcd = blockIdx.x & 7u, share = gridDim.x / 8, extra = gridDim.x % 8;
+    const uint32_t id = xcd * share + (xcd < extra ? xcd : extra) + (blockIdx.x >> 3);
+    head = id / p.cuts;
+    g = id - head * p.cuts;
+  } else {
+    g = blockIdx.x / hkv;
+    head = (blockIdx.x + g) % hkv;
+  }
   uint64_t t = (uint64_t)g * per, end = t + per;
   if (end > total) end = total;
   while (t < end) {
@@ -1010,8 +1029,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
     uint32_t tiles;  // its tiles
     if (t < prefix_places) {
       tiles = ptiles;
-      const uint32_t rt = (uint32_t)(t / places(tiles));
-      seg = (uint64_t)rt * places(tiles);
+      const uint32_t rt = (uint32_t)(t / places(tiles, prg));
+      seg = (uint64_t)rt * places(tiles, prg);
       w.pages = a.prefix_pages;
       w.n_pages = a.n_prefix_pages;
       w.keys = w.low = P;
@@ -1038,8 +1057,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       uint32_t rt = 0;
       seg = first;
       tiles = own_tiles(p, s, w.rg, 0);
-      while (t >= seg + places(tiles)) {
-        seg += places(tiles);
+      while (t >= seg + places(tiles, w.rg)) {
+        seg += places(tiles, w.rg);
         tiles = own_tiles(p, s, w.rg, ++rt);
       }
       const uint32_t srows = s.n * p.group, r0 = rt * 32 * w.rg;
@@ -1054,10 +1073,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       w.part = (uint64_t)prows + s.first * p.group + r0;
     }
     w.head = head;
-    // tile i stands at place seg + kSegment + i
-    const uint64_t zero = seg + kSegment, stop = end < zero + tiles ? end : zero + tiles;
-    if (stop > zero) {
-      const uint64_t from = t > zero ? t : zero;
+    // tile i begins at place zero + i * each; its first place says
+    // whose it is
+    const uint32_t each = tile_places(w.rg);
+    const uint64_t zero = seg + segment_places(w.rg), last = zero + (uint64_t)tiles * each, stop = end < last ? end : last;
+    const uint32_t from = t > zero ? (uint32_t)((t - zero + each - 1) / each) : 0;
+    const uint32_t to = stop > zero ? (uint32_t)((stop - zero + each - 1) / each) : 0;
+    if (to > from) {
       // the same in all lanes: kept in scalar registers
       w.pages = (const int32_t*)uni((uint64_t)w.pages);
       w.n_pages = uni(w.n_pages);
@@ -1069,8 +1091,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       w.first_row = uni(w.first_row);
       w.see = (int64_t)uni((uint64_t)w.see);
       w.part = uni((uint64_t)(w.part + ((uint64_t)2 * prows + cut_rows) * head + (uint64_t)p.part_rows * g));
-      w.tile = uni((uint32_t)(from - zero));
-      w.n_tiles = uni((uint32_t)(stop - from));
+      w.tile = uni(from);
+      w.n_tiles = uni(to - from);
       float *stats = (float*)(scratch + sc.stats), *sums = (float*)(scratch + sc.sums);
       if (w.rg > 1)
         run_stretch<T, DP>(p, w, s_kv, &s_flags, stats, sums);
@@ -1103,27 +1125,31 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
   uint32_t seq, index, count;
   if (find_sequence(a.batch, t, &seq, &index, &count)) {
     for (int part = 0; part < 2; ++part) {
-      uint64_t first, n, at;  // place and tiles of the segment, the row among the partials
+      uint64_t first, at;  // place of the segment, the row among the partials
+      uint32_t n, rg;      // its tiles and row groups
       if (part == 0) {
         const uint32_t P = a.cache.n_pages ? a.batch.prefix_len : 0;
         n = (P + kTile - 1) / kTile;
-        const uint32_t prows = a.batch.tokens * p.group, rg = row_groups(prows);
+        const uint32_t prows = a.batch.tokens * p.group;
+        rg = row_groups(prows);
         const uint32_t r = t * p.group + gq;
-        first = places((uint32_t)n) * (uint64_t)(r / (32 * rg));
+        first = places(n, rg) * (r / (32 * rg));
         at = r;
       } else {
         const Seq s = load_seq(p, seq);
-        const uint32_t srows = s.n * p.group, rg = row_groups(srows), r = index * p.group + gq, rt = r / (32 * rg);
+        const uint32_t srows = s.n * p.group;
+        rg = row_groups(srows);
+        const uint32_t r = index * p.group + gq, rt = r / (32 * rg);
         if (s.keys == 0) continue;
         first = ((const uint64_t*)(scratch + sc.begin))[seq];
-        for (uint32_t i = 0; i < rt; ++i) first += places(own_tiles(p, s, rg, i));
+        for (uint32_t i = 0; i < rt; ++i) first += places(own_tiles(p, s, rg, i), rg);
         n = own_tiles(p, s, rg, rt);
         at = (uint64_t)a.batch.tokens * p.group + s.first * p.group + r;
       }
       if (n == 0) continue;
-      first += kSegment;
+      first += segment_places(rg);
       at += (2ull * a.batch.tokens * p.group + cut_rows) * head;
-      const uint64_t g1 = (first + n - 1) / plan.per;
+      const uint64_t g1 = (first + (uint64_t)(n - 1) * tile_places(rg)) / plan.per;
       for (uint64_t g = first / plan.per; g <= g1; ++g) {
         const uint64_t x = at + p.part_rows * g;
         const float mx = stats[2 * x], lx = stats[2 * x + 1];
