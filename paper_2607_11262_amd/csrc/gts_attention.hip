@@ -708,8 +708,10 @@ struct Stream {
 #pragma unroll
     for (int n = 0; n < NV; ++n) to[n] = load16((d < p.a.cache.dim ? x[n] : (const char*)g_zeros) + d * 2);
   }
+  // Read once: without the hint that says so, 6.1 instead of 6.8 TB/s for the
+  // loads alone.
   static __device__ __forceinline__ u32x4 load16(const char* x) {
-    return *(const __attribute__((address_space(1))) u32x4*)(uint64_t)x;
+    return __builtin_nontemporal_load((const __attribute__((address_space(1))) u32x4*)(uint64_t)x);
   }
   // Row r0 of the block (the same in all lanes), or a row of each lane's own
   // (the zeros, when it has no page).
@@ -1006,21 +1008,12 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   }
   __syncthreads();
 
-  // Workgroups go round the eight XCDs.  Where the prefix has several segments
-  // its keys are read several times: an XCD then takes a run of (head,
-  // stretch) pairs and finds them in its L2.  Else every XCD takes all heads in
-  // turn: a head's rows alone lie on some of the memory channels, which are
-  // nearer to some XCDs.
-  uint32_t head, g;
-  if (n_prt > 1 && P) {
-    const uint32_t xcd = blockIdx.x & 7u, share = gridDim.x / 8, extra = gridDim.x % 8;
-    const uint32_t id = xcd * share + (xcd < extra ? xcd : extra) + (blockIdx.x >> 3);
-    head = id / p.cuts;
-    g = id - head * p.cuts;
-  } else {
-    g = blockIdx.x / hkv;
-    head = (blockIdx.x + g) % hkv;
-  }
+  // Workgroups go round the eight XCDs: each takes a run of the (head, stretch)
+  // pairs, so that rows which share keys also share an L2, and the heads of a
+  // token are read at the same time (taking the heads in turn reads 4 % slower).
+  const uint32_t xcd = blockIdx.x & 7u, share = gridDim.x / 8, extra = gridDim.x % 8;
+  const uint32_t id = xcd * share + (xcd < extra ? xcd : extra) + (blockIdx.x >> 3);
+  const uint32_t head = id / p.cuts, g = id - head * p.cuts;
   uint64_t t = (uint64_t)g * per, end = t + per;
   if (end > total) end = total;
   while (t < end) {
