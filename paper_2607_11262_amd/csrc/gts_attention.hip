@@ -35,7 +35,7 @@ constexpr uint32_t kGroups = 512;     // most workgroups: two a CU
 // Places in the line (of about half a microsecond): a segment's begin and end,
 // and a tile, by the segment's row groups.  Measured with few rows 5 us and 1 us
 // (nothing else running), with 128 rows 12 us and 2.6 us (two workgroups a CU).
-constexpr uint32_t kMostPlaces = 5;
+constexpr uint32_t kMostPlaces = 5, kLeastStretch = 5;
 __host__ __device__ __forceinline__ uint32_t segment_places(uint32_t row_groups) { return row_groups == 1 ? 10 : 24; }
 __host__ __device__ __forceinline__ uint32_t tile_places(uint32_t row_groups) {
   return row_groups == 1 ? 2 : row_groups == 2 ? 3 : kMostPlaces;
@@ -46,7 +46,7 @@ struct AttnParams {
   gts_attention_args a;
   uint32_t page_shift;
   uint32_t group;       // query heads of a key-value head
-  FastDiv by_group;
+  FastDiv by_group, by_q_heads;
   bool near_rows;       // see Loader
   uint32_t cuts;        // stretches of a head's line: so many workgroups for each head
   uint32_t part_rows;   // rows that a cut between workgroups may add to the partials
@@ -55,7 +55,15 @@ struct AttnParams {
 // Scratch: the plan (what the tile kernel's first workgroup leaves for the
 // join), then the partials: maximum and sum of each row, then its sums.
 struct Plan {
-  uint64_t per;  // places of a workgroup
+  uint64_t per;    // places of a workgroup
+  double per_inv;  // 1 / per
+  // Which workgroup has place x (below 2^53), without a 64-bit division.
+  __device__ __forceinline__ uint32_t group_of(uint64_t x) const {
+    uint64_t g = (uint64_t)((double)x * per_inv);
+    if (g * per > x) --g;
+    if ((g + 1) * per <= x) ++g;
+    return (uint32_t)g;
+  }
 };
 struct Scratch {
   uint64_t begin, stats, sums, bytes;  // offsets; begin: [batch] first place of each sequence
@@ -991,7 +999,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   // at least a tile's: then every stretch between a segment's first and last
   // tile begins one
   uint64_t per = (total + p.cuts - 1) / p.cuts;
-  if (per < kMostPlaces) per = kMostPlaces;
+  if (per < kLeastStretch) per = kLeastStretch;
   const uint64_t rows = (uint64_t)a.batch.tokens * a.q_heads;
   const uint64_t cut_rows = (uint64_t)p.part_rows * p.cuts;  // of a head
   const Scratch sc = scratch_layout(B, rows, cut_rows * hkv, a.cache.dim);
@@ -1004,7 +1012,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       ((uint64_t*)(scratch + sc.begin))[b] = t;
       t += seq_places(p, load_seq(p, b));
     }
-    if (tid == 0) *(Plan*)scratch = Plan{per};
+    if (tid == 0) *(Plan*)scratch = Plan{per, 1.0 / (double)per};
   }
   __syncthreads();
 
@@ -1098,76 +1106,111 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   }
 }
 
-// The join: one wavefront a row adds up its partials.
+// The join: one wavefront a row.  Lane i takes the maximum and sum of partial i,
+// then all lanes add up the partials, two dims each.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
   const gts_attention_args& a = p.a;
   const uint32_t lane = threadIdx.x & 63u;
-  const uint64_t rows = (uint64_t)a.batch.tokens * a.q_heads, row = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const uint32_t rows = a.batch.tokens * a.q_heads, row = uni(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (row >= rows) return;
-  const uint32_t t = uni((uint32_t)(row / a.q_heads)), hq = uni((uint32_t)(row - (uint64_t)t * a.q_heads));
-  const uint32_t head = p.by_group.div(hq), gq = hq - head * p.group, hkv = a.cache.heads, D = a.cache.dim;
+  const uint32_t t = p.by_q_heads.div(row), hq = row - t * a.q_heads;
+  const uint32_t head = p.by_group.div(hq), gq = hq - head * p.group, D = a.cache.dim;
+  const uint32_t prows = a.batch.tokens * p.group;  // of a head
   const uint64_t cut_rows = (uint64_t)p.part_rows * p.cuts;
-  const Scratch sc = scratch_layout(a.batch.batch, rows, cut_rows * hkv, D);
+  const Scratch sc = scratch_layout(a.batch.batch, rows, cut_rows * a.cache.heads, D);
   const char* scratch = (const char*)a.scratch;
   const Plan plan = *(const Plan*)scratch;
   const float* stats = (const float*)(scratch + sc.stats);
   const float* sums = (const float*)(scratch + sc.sums);
-  float m = -INFINITY, l = 0.f;
-  float2 o[GTS_OPS_MAX_ATTN / 128] = {};
-  uint32_t seq, index, count;
-  if (find_sequence(a.batch, t, &seq, &index, &count)) {
-    for (int part = 0; part < 2; ++part) {
-      uint64_t first, at;  // place of the segment, the row among the partials
-      uint32_t n, rg;      // its tiles and row groups
-      if (part == 0) {
-        const uint32_t P = a.cache.n_pages ? a.batch.prefix_len : 0;
-        n = (P + kTile - 1) / kTile;
-        const uint32_t prows = a.batch.tokens * p.group;
-        rg = row_groups(prows);
-        const uint32_t r = t * p.group + gq;
-        first = places(n, rg) * (r / (32 * rg));
-        at = r;
-      } else {
-        const Seq s = load_seq(p, seq);
-        const uint32_t srows = s.n * p.group;
-        rg = row_groups(srows);
-        const uint32_t r = index * p.group + gq, rt = r / (32 * rg);
-        if (s.keys == 0) continue;
-        first = ((const uint64_t*)(scratch + sc.begin))[seq];
-        for (uint32_t i = 0; i < rt; ++i) first += places(own_tiles(p, s, rg, i), rg);
-        n = own_tiles(p, s, rg, rt);
-        at = (uint64_t)a.batch.tokens * p.group + s.first * p.group + r;
-      }
-      if (n == 0) continue;
-      first += segment_places(rg);
-      at += (2ull * a.batch.tokens * p.group + cut_rows) * head;
-      const uint64_t g1 = (first + (uint64_t)(n - 1) * tile_places(rg)) / plan.per;
-      for (uint64_t g = first / plan.per; g <= g1; ++g) {
-        const uint64_t x = at + p.part_rows * g;
-        const float mx = stats[2 * x], lx = stats[2 * x + 1];
-        const float m1 = fmaxf(m, mx);
-        const float fa = m == -INFINITY ? 1.f : exp2_(m - m1), fb = mx == -INFINITY ? 1.f : exp2_(mx - m1);
-        l = l * fa + lx * fb;
-        m = m1;
-#pragma unroll
-        for (uint32_t i = 0; i < GTS_OPS_MAX_ATTN / 128; ++i) {
-          const uint32_t d = i * 128 + lane * 2;
-          if (d < D) {
-            const float2 v = *(const float2*)(sums + x * D + d);
-            o[i].x = o[i].x * fa + v.x * fb;
-            o[i].y = o[i].y * fa + v.y * fb;
-          }
-        }
-      }
+
+  // partials of the prefix: workgroups first[0] .. + count[0], rows at[0] +
+  // part_rows * workgroup; of the own keys likewise
+  uint32_t first[2] = {0, 0}, count[2] = {0, 0};
+  uint64_t at[2] = {0, 0};
+  uint32_t seq, index, n_new;
+  if (find_sequence(a.batch, t, &seq, &index, &n_new)) {
+    const uint64_t base = ((uint64_t)2 * prows + cut_rows) * head;
+    const auto locate = [&](int part, uint64_t place, uint32_t tiles, uint32_t rg, uint64_t x) {
+      if (tiles == 0) return;
+      place += segment_places(rg);
+      first[part] = plan.group_of(place);
+      count[part] = plan.group_of(place + (uint64_t)(tiles - 1) * tile_places(rg)) - first[part] + 1;
+      at[part] = base + x;
+    };
+    if (a.cache.n_pages) {
+      const uint32_t tiles = (a.batch.prefix_len + kTile - 1) / kTile, rg = row_groups(prows), r = t * p.group + gq;
+      locate(0, places(tiles, rg) * (r / (32 * rg)), tiles, rg, r);
+    }
+    const Seq s = load_seq(p, seq);
+    if (s.keys) {
+      const uint32_t rg = row_groups(s.n * p.group), r = index * p.group + gq, rt = r / (32 * rg);
+      uint64_t place = ((const uint64_t*)(scratch + sc.begin))[seq];
+      for (uint32_t i = 0; i < rt; ++i) place += places(own_tiles(p, s, rg, i), rg);
+      locate(1, place, own_tiles(p, s, rg, rt), rg, (uint64_t)prows + s.first * p.group + r);
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+
+  float m = -INFINITY, l = 0.f;
+  float2 o[GTS_OPS_MAX_ATTN / 128] = {};
+  const uint32_t n = count[0] + count[1];
+  for (uint32_t i0 = 0; i0 < n; i0 += 64) {
+    const uint32_t i = i0 + lane;
+    const bool own = i >= count[0];
+    const uint64_t x = at[own] + (uint64_t)p.part_rows * (own ? first[1] + i - count[0] : first[0] + i);
+    float mi = -INFINITY, li = 0.f;
+    if (i < n) {
+      const float2 v = *(const float2*)(stats + 2 * x);
+      mi = v.x;
+      li = v.y;
+    }
+    float m1 = mi;
+    for (int k = 32; k; k >>= 1) m1 = fmaxf(m1, __shfl_xor(m1, k));
+    m1 = fmaxf(m1, m);
+    const float f = mi == -INFINITY ? 1.f : exp2_(mi - m1), old = m == -INFINITY ? 1.f : exp2_(m - m1);
+    float sum = li * f;
+    for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
+    l = l * old + sum;
+    m = m1;
+#pragma unroll
+    for (uint32_t d = 0; d < GTS_OPS_MAX_ATTN / 128; ++d) {
+      o[d].x *= old;
+      o[d].y *= old;
+    }
+    const uint32_t here = n - i0 < 64 ? n - i0 : 64;
+    constexpr int kAhead = 8;  // loads on their way
+    for (uint32_t k0 = 0; k0 < here; k0 += kAhead) {
+      float2 v[kAhead][GTS_OPS_MAX_ATTN / 128];
+      float w[kAhead];
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y) {
+        const uint32_t k = k0 + y < here ? k0 + y : here - 1;  // past the end: the last again, weight 0
+        w[y] = k0 + y < here ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), k)) : 0.f;
+        const uint64_t xk = ((uint64_t)__builtin_amdgcn_readlane((uint32_t)(x >> 32), k) << 32) |
+                            __builtin_amdgcn_readlane((uint32_t)x, k);
+        const float* src = sums + xk * D;
+#pragma unroll
+        for (uint32_t d = 0; d < GTS_OPS_MAX_ATTN / 128; ++d) {
+          const uint32_t c = d * 128 + lane * 2;
+          v[y][d] = c < D ? *(const float2*)(src + c) : make_float2(0.f, 0.f);
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y)
+#pragma unroll
+        for (uint32_t d = 0; d < GTS_OPS_MAX_ATTN / 128; ++d)
+          if (k0 + y < here) {
+            o[d].x += v[y][d].x * w[y];
+            o[d].y += v[y][d].y * w[y];
+          }
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;  // no key: zeros
   T* out = (T*)a.out + (int64_t)t * a.out_stride[0] + (int64_t)hq * a.out_stride[1];
 #pragma unroll
-  for (uint32_t i = 0; i < GTS_OPS_MAX_ATTN / 128; ++i) {
-    const uint32_t d = i * 128 + lane * 2;
-    if (d < D) *(Pack<T, 2>*)(out + d) = Pack<T, 2>{(T)(o[i].x * inv), (T)(o[i].y * inv)};
+  for (uint32_t d = 0; d < GTS_OPS_MAX_ATTN / 128; ++d) {
+    const uint32_t c = d * 128 + lane * 2;
+    if (c < D) *(Pack<T, 2>*)(out + c) = Pack<T, 2>{(T)(o[d].x * inv), (T)(o[d].y * inv)};
   }
   if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
@@ -1306,6 +1349,7 @@ hipError_t launch_attention(const gts_attention_args& a, hipStream_t stream) {
   p.page_shift = (uint32_t)__builtin_ctz(a.cache.page);
   p.group = a.q_heads / a.cache.heads;
   p.by_group = FastDiv(p.group);
+  p.by_q_heads = FastDiv(a.q_heads);
   p.part_rows = part_rows(a.batch.tokens, p.group);
   // chunks beyond the head must come out as zeros: the general way alone
   const int64_t far = 1 << 26;  // elements: 16 rows and a chunk stay below 2^31 bytes
