@@ -79,8 +79,12 @@ __host__ __device__ inline Scratch scratch_layout(uint32_t batch, uint64_t rows,
   return s;
 }
 
+// A page table: global memory, said in the type, because a load that might be from
+// LDS makes every LDS read wait for it.
+typedef const __attribute__((address_space(1))) int32_t* pages_t;
+
 // Page of own or prefix key j, -1 when none holds it.
-__device__ __forceinline__ int32_t key_page(const gts_attention_args& a, const int32_t* pages, uint32_t n, uint32_t shift,
+__device__ __forceinline__ int32_t key_page(const gts_attention_args& a, pages_t pages, uint32_t n, uint32_t shift,
                                             uint32_t j) {
   const uint32_t at = j >> shift;
   if (at >= n) return -1;
@@ -182,7 +186,7 @@ __device__ __forceinline__ uint64_t seq_places(const AttnParams& p, const Seq& s
 
 // One stretch of one segment.
 struct Work {
-  const int32_t* pages;
+  pages_t pages;
   uint32_t n_pages, keys;    // keys: of the segment's last row
   uint32_t head, rg, rows;   // key-value head, row groups, valid rows
   uint32_t first_row;        // token * group + query head within the group
@@ -214,6 +218,16 @@ struct Tiles {
 __device__ __align__(16) const uint32_t g_zeros[GTS_OPS_MAX_ATTN / 2] = {};  // a row
 // What the page of a key that does not exist is loaded from.
 __device__ const int32_t g_no_page = -1;
+
+// 16 bytes a lane from memory to LDS, lane after lane from `to` on (the same in
+// all lanes).  Nothing waits for it but the wait for all loads before the barrier
+// that hands the tile over: written as the compiler's builtin, it waits for every
+// such load before the next LDS read, whatever that reads, and no tile is on its
+// way while another is worked on.  (M0, the LDS address, has no other use here.)
+__device__ __forceinline__ void load_to_lds(const void* from, void* to) {
+  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)to;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
+}
 
 // Loads tiles of keys and values from the cache straight into LDS (no
 // registers in between, so nothing is held while the tile before is worked
@@ -252,8 +266,6 @@ struct Loader {
   // Returns the wave's rows inside the segment that no page holds (one bit
   // each, the same in all lanes).
   __device__ __forceinline__ uint32_t load(const AttnParams& p, const Work& w, uint32_t tile, T* sk, T* sv) {
-    typedef const __attribute__((address_space(1))) void* global_t;
-    typedef __attribute__((address_space(3))) void* lds_t;
     const gts_kv_cache& kc = p.a.cache;
     const uint32_t j0 = tile * kTile + wave * 16;
     const uint32_t pg0 = uni((uint32_t)page);
@@ -266,8 +278,8 @@ struct Loader {
 #pragma unroll
       for (int n = 0; n < L::NL; ++n) {
         const uint32_t at = (wave * 16 + n * L::RPI) * DP;
-        __builtin_amdgcn_global_load_lds((global_t)(kp + k_off[n]), (lds_t)(sk + at), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((global_t)(vp + v_off[n]), (lds_t)(sv + at), 16, 0, 0);
+        load_to_lds(kp + k_off[n], sk + at);
+        load_to_lds(vp + v_off[n], sv + at);
       }
       page = next_page(p, w, tile + 1);
       return 0;
@@ -289,8 +301,8 @@ struct Loader {
       kp = pg >= 0 && ck < kc.dim ? kp : (const T*)g_zeros;
       vp = pg >= 0 && cv < kc.dim ? vp : (const T*)g_zeros;
       const uint32_t at = (wave * 16 + n * L::RPI) * DP;
-      __builtin_amdgcn_global_load_lds((global_t)kp, (lds_t)(sk + at), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((global_t)vp, (lds_t)(sv + at), 16, 0, 0);
+      load_to_lds(kp, sk + at);
+      load_to_lds(vp, sv + at);
     }
     if (p.page_shift >= 4) page = next_page(p, w, tile + 1);
     return missing;
@@ -687,9 +699,9 @@ struct Stream {
   static __device__ __forceinline__ int32_t load_pages(const AttnParams& p, const Work& w, uint32_t lane, uint32_t end,
                                                        uint32_t j0) {
     const uint32_t j = j0 + (lane & 31u), at = j >> p.page_shift;
-    uint64_t x = (uint64_t)(j < end && at < w.n_pages ? w.pages + at : &g_no_page);
+    uint64_t x = (uint64_t)(j < end && at < w.n_pages ? w.pages + at : (pages_t)&g_no_page);
     asm volatile("" : "+v"(x));
-    return *(const __attribute__((address_space(1))) int32_t*)x;
+    return *(pages_t)x;
   }
   static __device__ __forceinline__ int32_t known_pages(const AttnParams& p, int32_t pages) {
     return (uint32_t)pages < p.a.cache.n_pages ? pages : -1;
@@ -1032,7 +1044,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       tiles = ptiles;
       const uint32_t rt = (uint32_t)(t / places(tiles, prg));
       seg = (uint64_t)rt * places(tiles, prg);
-      w.pages = a.prefix_pages;
+      w.pages = (pages_t)a.prefix_pages;
       w.n_pages = a.n_prefix_pages;
       w.keys = w.low = P;
       w.rg = prg;
@@ -1063,7 +1075,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
         tiles = own_tiles(p, s, w.rg, ++rt);
       }
       const uint32_t srows = s.n * p.group, r0 = rt * 32 * w.rg;
-      w.pages = a.batch.page_table + (int64_t)b * a.batch.table_stride;
+      w.pages = (pages_t)(a.batch.page_table + (int64_t)b * a.batch.table_stride);
       w.n_pages = a.batch.max_pages;
       w.rows = srows - r0 < 32 * w.rg ? srows - r0 : 32 * w.rg;
       w.first_row = s.first * p.group + r0;
@@ -1082,7 +1094,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
     const uint32_t to = stop > zero ? (uint32_t)((stop - zero + each - 1) / each) : 0;
     if (to > from) {
       // the same in all lanes: kept in scalar registers
-      w.pages = (const int32_t*)uni((uint64_t)w.pages);
+      w.pages = (pages_t)uni((uint64_t)w.pages);
       w.n_pages = uni(w.n_pages);
       w.keys = uni(w.keys);
       w.low = uni(w.low);
@@ -1237,7 +1249,7 @@ __global__ __launch_bounds__(256) void row_kernel(AttnParams p) {
   const float scale = a.scale * kLog2e;
   for (int part = 0; part < 2; ++part) {
     const uint32_t n = part ? (uint32_t)own : n_prefix;
-    const int32_t* pages = part ? a.batch.page_table + (int64_t)seq * a.batch.table_stride : a.prefix_pages;
+    const pages_t pages = (pages_t)(part ? a.batch.page_table + (int64_t)seq * a.batch.table_stride : a.prefix_pages);
     const uint32_t n_pages = part ? a.batch.max_pages : a.n_prefix_pages;
     for (uint32_t j0 = 0; j0 < n; j0 += 64) {
       const uint32_t j = j0 + lane;
