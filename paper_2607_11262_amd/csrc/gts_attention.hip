@@ -14,6 +14,10 @@
 // wherever they start and end, one for each workgroup of the head: ragged
 // lengths and few rows fill the chip alike, and the workgroups of all heads walk
 // the same pages at the same time, where the heads of a token lie side by side.
+// Where the prefix has many rows, its segments are first dealt out whole, or in
+// equal pieces, one for each workgroup: they then walk the same keys at the same
+// time, and all but the first of an XCD find them in its L2.  (All of it in the
+// line: 8 TB/s from behind the L2s, twice the time.)
 // A stretch leaves one partial result per segment of which it has tiles (unnormalised sum, running maximum and sum of the
 // softmax, 32 bits), and the join adds up the partials of each row.
 //
@@ -50,6 +54,8 @@ struct AttnParams {
   bool near_rows;       // see Loader
   uint32_t cuts;        // stretches of a head's line: so many workgroups for each head
   uint32_t part_rows;   // rows that a cut between workgroups may add to the partials
+  uint32_t pieces;      // of each segment of the prefix
+  uint32_t whole;       // pieces that each workgroup takes before its stretch of the line
 };
 
 // Scratch: the plan (what the tile kernel's first workgroup leaves for the
@@ -69,11 +75,14 @@ struct Scratch {
   uint64_t begin, stats, sums, bytes;  // offsets; begin: [batch] first place of each sequence
 };
 __host__ __device__ inline uint64_t up256(uint64_t x) { return (x + 255) & ~255ull; }
+// Rows of partials: every row's of the prefix and of its own keys, and what the
+// cuts between workgroups add: a segment's rows each, once more for pieces.
+__host__ __device__ inline uint64_t head_partials(uint64_t rows, uint64_t cut_rows) { return 2 * rows + 2 * cut_rows; }
 __host__ __device__ inline Scratch scratch_layout(uint32_t batch, uint64_t rows, uint64_t cut_rows, uint32_t dim) {
   Scratch s;
   s.begin = 256;
   s.stats = s.begin + up256(8ull * batch);
-  const uint64_t n = 2 * rows + cut_rows;
+  const uint64_t n = head_partials(rows, cut_rows);
   s.sums = s.stats + up256(8 * n);
   s.bytes = s.sums + up256(4 * n * dim);
   return s;
@@ -232,19 +241,18 @@ __device__ __forceinline__ void load_to_lds(const void* from, void* to) {
 // Loads tiles of keys and values from the cache straight into LDS (no
 // registers in between, so nothing is held while the tile before is worked
 // on).  A wave loads 16 rows of a tile; rows past the segment's keys, or without
-// a page, become zeros.
+// a page, become zeros.  Chunks past the head are not loaded where whole rows
+// are: the LDS holds zeros there from the stretch's beginning on.
 template <typename T, int DP>
 struct Loader {
   using L = Tiles<T, DP>;
   uint32_t k_off[L::NL], v_off[L::NL];  // bytes from the wave's first row to this lane's chunk
-  int32_t page;                         // page of the wave's rows in the next tile (pages of 16 or more)
+  int32_t next, last;  // page of the wave's rows in the next tile of keys, and in the last loaded (pages of 16 or more)
   uint32_t wave;
-  bool near;  // pages of 16 or more, and 16 rows lie within 2 GiB: k_off and v_off serve
 
   __device__ __forceinline__ void start(const AttnParams& p, const Work& w, uint32_t wave_) {
     const gts_kv_cache& kc = p.a.cache;
     wave = wave_;
-    near = p.near_rows;
     const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
 #pragma unroll
     for (int n = 0; n < L::NL; ++n) {
@@ -252,39 +260,55 @@ struct Loader {
       k_off[n] = 2 * (r * (uint32_t)kc.k_stride[1] + (c ^ L::swizzle_k(r)) * 8);
       v_off[n] = 2 * (r * (uint32_t)kc.v_stride[1] + (c ^ L::swizzle_v(r)) * 8);
     }
-    page = p.page_shift >= 4 ? next_page(p, w, w.tile) : 0;
+    next = page_of(p, w, w.tile);
+    last = -1;
   }
   // By a vector load, though it is the same for all lanes: LDS reads wait for
   // every scalar load before them (one counter), and this one may be long.
-  __device__ __forceinline__ int32_t next_page(const AttnParams& p, const Work& w, uint32_t tile) const {
+  __device__ __forceinline__ int32_t page_of(const AttnParams& p, const Work& w, uint32_t tile) const {
     const uint32_t at = (tile * kTile + wave * 16) >> p.page_shift;
     uint32_t zero = 0;
     asm volatile("" : "+v"(zero));
-    return at < w.n_pages ? (w.pages + at)[zero] : -1;
+    return p.page_shift >= 4 && at < w.n_pages ? (w.pages + at)[zero] : -1;
   }
 
-  // Returns the wave's rows inside the segment that no page holds (one bit
-  // each, the same in all lanes).
-  __device__ __forceinline__ uint32_t load(const AttnParams& p, const Work& w, uint32_t tile, T* sk, T* sv) {
+  // The keys of a tile, then the values of the last tile of keys.  Returns the
+  // wave's rows inside the segment that no page holds (one bit each, the same in
+  // all lanes).
+  __device__ __forceinline__ uint32_t keys(const AttnParams& p, const Work& w, uint32_t tile, T* to) {
+    last = uni((uint32_t)next);
+    const uint32_t missing = half<false>(p, w, tile, p.a.cache.k, p.a.cache.k_stride, k_off, to);
+    next = page_of(p, w, tile + 1);
+    return missing;
+  }
+  __device__ __forceinline__ void values(const AttnParams& p, const Work& w, uint32_t tile, T* to) {
+    half<true>(p, w, tile, p.a.cache.v, p.a.cache.v_stride, v_off, to);
+  }
+
+  template <bool V>
+  __device__ __forceinline__ uint32_t half(const AttnParams& p, const Work& w, uint32_t tile, const void* base,
+                                           const int64_t* stride, const uint32_t (&off)[L::NL], T* to) {
     const gts_kv_cache& kc = p.a.cache;
     const uint32_t j0 = tile * kTile + wave * 16;
-    const uint32_t pg0 = uni((uint32_t)page);
-    if (near && pg0 < kc.n_pages && j0 + 16 <= w.keys) {
+    if (p.near_rows && (uint32_t)last < kc.n_pages && j0 + 16 <= w.keys) {
       const uint32_t slot = j0 & (kc.page - 1);
-      const char* kp = (const char*)((const T*)kc.k + (int64_t)pg0 * kc.k_stride[0] + (int64_t)slot * kc.k_stride[1] +
-                                     (int64_t)w.head * kc.k_stride[2]);
-      const char* vp = (const char*)((const T*)kc.v + (int64_t)pg0 * kc.v_stride[0] + (int64_t)slot * kc.v_stride[1] +
-                                     (int64_t)w.head * kc.v_stride[2]);
+      const char* row = (const char*)((const T*)base + (int64_t)last * stride[0] + (int64_t)slot * stride[1] +
+                                      (int64_t)w.head * stride[2]);
+      if (kc.dim == DP) {
 #pragma unroll
-      for (int n = 0; n < L::NL; ++n) {
-        const uint32_t at = (wave * 16 + n * L::RPI) * DP;
-        load_to_lds(kp + k_off[n], sk + at);
-        load_to_lds(vp + v_off[n], sv + at);
+        for (int n = 0; n < L::NL; ++n) load_to_lds(row + off[n], to + (wave * 16 + n * L::RPI) * DP);
+      } else {
+        const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
+#pragma unroll
+        for (int n = 0; n < L::NL; ++n) {
+          const uint32_t r = n * L::RPI + r0;
+          if ((c ^ (V ? L::swizzle_v(r) : L::swizzle_k(r))) * 8 < kc.dim)
+            load_to_lds(row + off[n], to + (wave * 16 + n * L::RPI) * DP);
+        }
       }
-      page = next_page(p, w, tile + 1);
       return 0;
     }
-    // the general way: every row by itself
+    // every row by itself
     const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
     uint32_t missing = 0;
 #pragma unroll 1
@@ -294,17 +318,11 @@ struct Loader {
       const int32_t pg = in ? key_page(p.a, w.pages, w.n_pages, p.page_shift, j) : -1;
       const uint64_t lost = __ballot(in && pg < 0);
       for (int i = 0; i < L::RPI; ++i) missing |= (uint32_t)(lost >> (i * L::C) & 1) << (n * L::RPI + i);
-      const int64_t slot = j & (kc.page - 1);
-      const uint32_t ck = (c ^ L::swizzle_k(r)) * 8, cv = (c ^ L::swizzle_v(r)) * 8;
-      const T* kp = (const T*)kc.k + (int64_t)pg * kc.k_stride[0] + slot * kc.k_stride[1] + (int64_t)w.head * kc.k_stride[2] + ck;
-      const T* vp = (const T*)kc.v + (int64_t)pg * kc.v_stride[0] + slot * kc.v_stride[1] + (int64_t)w.head * kc.v_stride[2] + cv;
-      kp = pg >= 0 && ck < kc.dim ? kp : (const T*)g_zeros;
-      vp = pg >= 0 && cv < kc.dim ? vp : (const T*)g_zeros;
-      const uint32_t at = (wave * 16 + n * L::RPI) * DP;
-      load_to_lds(kp, sk + at);
-      load_to_lds(vp, sv + at);
+      const uint32_t d = (c ^ (V ? L::swizzle_v(r) : L::swizzle_k(r))) * 8;
+      const T* x = (const T*)base + (int64_t)pg * stride[0] + (int64_t)(j & (kc.page - 1)) * stride[1] +
+                   (int64_t)w.head * stride[2] + d;
+      load_to_lds(pg >= 0 && d < kc.dim ? x : (const T*)g_zeros, to + (wave * 16 + n * L::RPI) * DP);
     }
-    if (p.page_shift >= 4) page = next_page(p, w, tile + 1);
     return missing;
   }
 };
@@ -380,57 +398,111 @@ struct Rows {
     l = 0.f;
   }
 
-  // NS blocks of 32 keys from LDS row `key` on (key number j0 of the segment).
-  template <int NS>
-  __device__ __forceinline__ void step(uint32_t lane, const T* sk, const T* sv, uint32_t key, uint32_t j0, float c, bool mask,
-                                       uint64_t missing, uint32_t sees) {
-    const uint32_t half = lane / 32;
-    f32x16 s[NS];
+  // 32 keys from LDS row `key` on (key number j0 of the segment).
+  __device__ __forceinline__ void step(uint32_t lane, const T* sk, const T* sv, uint32_t key, uint32_t j0, float c,
+                                       bool mask, uint64_t missing, uint32_t sees) {
+    f32x16 s[1];
     const T* ka = sk + (key + lane % 32) * DP;
-    const uint32_t kc = half ^ L::swizzle_k(lane % 32);
+    const uint32_t kc = lane / 32 ^ L::swizzle_k(lane % 32);
 #pragma unroll
-    for (int b = 0; b < NS; ++b)
+    for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < L::KK; ++kk) s[0] = mfma(*(const Vec8<T>*)(ka + (kc ^ (2 * kk)) * 8), q[kk], s[0]);
+    if (mask) hide(s, lane, j0, sees, missing >> key);
+    follow(s, c);
+    const float base = m == -INFINITY ? 0.f : -m * c;
+    float sum[2] = {0.f, 0.f};
+    Vec8<T> pw[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float e = exp2_(__builtin_fmaf(s[0][i], c, base));
+      sum[i & 1] += e;
+      pw[i / 8][i % 8] = (T)e;
+    }
+    l += sum[0] + sum[1];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int mb = 0; mb < L::MB; ++mb) o[mb] = mfma(load_v<T, DP>(sv, lane, key + kb * 16, mb), pw[kb], o[mb]);
+  }
+
+  // The scores of 64 keys: dims in `L::KK` steps, the fragments of one step read
+  // while the one before is multiplied; `between(x)` after each of the 2 KK
+  // products.
+  template <typename F>
+  __device__ __forceinline__ void scores(uint32_t lane, const T* sk, f32x16 (&s)[2], F between) const {
+    const T* ka = sk + lane % 32 * DP;
+    const uint32_t kc = lane / 32 ^ L::swizzle_k(lane % 32);
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-    // The fragments of two matrix steps are read while the two before are
-    // multiplied; the fences keep that order.
-    Vec8<T> kf[2][2][NS];
-    const auto read = [&](int at, int kk) {
+    Vec8<T> kf[2][2];
 #pragma unroll
-      for (int b = 0; b < NS; ++b) {
-        kf[at][0][b] = *(const Vec8<T>*)(ka + b * 32 * DP + (kc ^ (2 * kk)) * 8);
-        kf[at][1][b] = *(const Vec8<T>*)(ka + b * 32 * DP + (kc ^ (2 * kk + 2)) * 8);
+    for (int b = 0; b < 2; ++b) kf[0][b] = *(const Vec8<T>*)(ka + b * 32 * DP + kc * 8);
+#pragma unroll
+    for (int kk = 0; kk < L::KK; ++kk) {
+      if (kk + 1 < L::KK) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+          kf[kk + 1 & 1][b] = *(const Vec8<T>*)(ka + b * 32 * DP + (kc ^ (2 * kk + 2)) * 8);
       }
-    };
-    read(0, 0);
-#pragma unroll
-    for (int kk = 0; kk < L::KK; kk += 2) {
-      if (kk + 2 < L::KK) read(kk / 2 + 1 & 1, kk + 2);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+      for (int b = 0; b < 2; ++b) {
+        s[b] = mfma(kf[kk & 1][b], q[kk], s[b]);
+        between(2 * kk + b);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+
+  // The softmax and the second product of 64 keys whose scores are s, and the
+  // first product of the next 64 into `next`: the exponentials stand between the
+  // products, so that a wave keeps both units busy by itself.
+  __device__ __forceinline__ void overlapped(uint32_t lane, f32x16 (&s)[2], f32x16 (&next)[2], const T* sk, const T* sv,
+                                             float c) {
+    follow(s, c);
+    const float base = m == -INFINITY ? 0.f : -m * c;
+    float sum[2] = {0.f, 0.f};
+    Vec8<T> pw[4];
+    scores(lane, sk, next, [&](int x) {
+      constexpr int N = 16 / L::KK;  // weights a product
 #pragma unroll
-        for (int b = 0; b < NS; ++b) s[b] = mfma(kf[kk / 2 & 1][x][b], q[kk + x], s[b]);
+      for (int y = 0; y < N; ++y) {
+        const int i = x * N + y;
+        const float e = exp2_(__builtin_fmaf(s[i / 16][i % 16], c, base));
+        sum[i & 1] += e;
+        pw[i / 8][i % 8] = (T)e;
+      }
+    });
+    l += sum[0] + sum[1];
+    Vec8<T> vf[2][L::MB];
+#pragma unroll
+    for (int mb = 0; mb < L::MB; ++mb) vf[0][mb] = load_v<T, DP>(sv, lane, 0, mb);
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      if (kb + 1 < 4) {
+#pragma unroll
+        for (int mb = 0; mb < L::MB; ++mb) vf[kb + 1 & 1][mb] = load_v<T, DP>(sv, lane, kb * 16 + 16, mb);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int mb = 0; mb < L::MB; ++mb) o[mb] = mfma(vf[kb & 1][mb], pw[kb], o[mb]);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (mask) {
-#pragma unroll
-      for (int b = 0; b < NS; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint32_t r = b * 32 + 8 * (i / 4) + 4 * half + i % 4;
-          const bool ok = j0 + r < sees && !(missing >> (key + r) & 1);
-          s[b][i] = ok ? s[b][i] : -INFINITY;
-        }
-    }
+  }
+
+  // Moves the reference maximum when some row's scores are 2^8 ahead of it:
+  // weights up to 256 are as exact, and sums and output are rescaled rarely.
+  template <int NS>
+  __device__ __forceinline__ void follow(const f32x16 (&s)[NS], float c) {
     float mx = s[0][0];
 #pragma unroll
     for (int b = 0; b < NS; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
     mx = max_halves(mx);
-    // The reference follows the maximum only when that is 2^8 ahead: weights
-    // up to 256 are as exact, and sums and output are rescaled rarely.
     if (__any((mx - m) * c > 8.f || (m == -INFINITY && mx > m))) {
       const float m1 = fmaxf(m, mx);
       const float alpha = m == -INFINITY ? 0.f : exp2_((m - m1) * c);
@@ -441,39 +513,19 @@ struct Rows {
         for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
       m = m1;
     }
-    const float base = m == -INFINITY ? 0.f : -m * c;
-    float sum[2] = {0.f, 0.f};
-    Vec8<T> pw[2 * NS];
-    const auto weigh = [&](int kb, int i) {
-      const float e = exp2_(__builtin_fmaf(s[kb / 2][kb % 2 * 8 + i], c, base));
-      sum[i & 1] += e;
-      pw[kb][i] = (T)e;
-    };
-    // The weights of 16 keys are computed, and the values of 16 keys read,
-    // between the products of the 16 keys before.
-    Vec8<T> vf[2][L::MB];
+  }
+
+  // Scores of keys that a row does not see, or that no page holds.
+  template <int NS>
+  static __device__ __forceinline__ void hide(f32x16 (&s)[NS], uint32_t lane, uint32_t j0, uint32_t sees,
+                                              uint64_t missing) {
 #pragma unroll
-    for (int mb = 0; mb < L::MB; ++mb) vf[0][mb] = load_v<T, DP>(sv, lane, key, mb);
+    for (int b = 0; b < NS; ++b)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) weigh(0, i);
-#pragma unroll
-    for (int kb = 0; kb < 2 * NS; ++kb) {
-      if (kb + 1 < 2 * NS) {
-#pragma unroll
-        for (int mb = 0; mb < L::MB; ++mb) vf[kb + 1 & 1][mb] = load_v<T, DP>(sv, lane, key + kb * 16 + 16, mb);
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t r = b * 32 + 8 * (i / 4) + 4 * (lane / 32) + i % 4;
+        s[b][i] = j0 + r < sees && !(missing >> r & 1) ? s[b][i] : -INFINITY;
       }
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int mb = 0; mb < L::MB; ++mb) {
-        o[mb] = mfma(vf[kb & 1][mb], pw[kb], o[mb]);
-        if (kb + 1 < 2 * NS) {
-#pragma unroll
-          for (int i = mb * 8 / L::MB; i < (mb + 1) * 8 / L::MB; ++i) weigh(kb + 1, i);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    l += sum[0] + sum[1];
   }
 
   // See not_finite: keys j0 .. j0 + 31.
@@ -498,54 +550,91 @@ struct Rows {
 
 // Flags that the waves of a workgroup leave each other for a tile.
 struct Flags {
-  uint16_t missing[2][4];  // rows without a page
+  uint16_t missing[4][4];  // rows without a page, of a tile and three after it
   uint32_t odd[4];         // values that are not finite
 };
 
-// Tiles i0 .. i1 of a stretch, the first of them already on its way.  One tile is
-// worked on while the next is on its way to the other half of the LDS; one
-// barrier a tile.
-template <int NS, typename T, int DP>
-__device__ __forceinline__ void run_tiles(const AttnParams& p, const Work& w, Loader<T, DP>& ld, Rows<T, DP>& r,
-                                          uint32_t i0, uint32_t i1, uint32_t wave, uint32_t kgroup, T* s_kv,
-                                          Flags* flags, float c, uint32_t sees) {
+// Everything that this wave has asked for is there, and everybody's after it.
+__device__ __forceinline__ void arrived() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// Tiles 0 .. n of a stretch whose rows all see the same, or see all of these
+// tiles; the keys of the first are on their way.  While the softmax and the
+// second product of a tile are computed, so is the first product of the next; its
+// values, and the keys of the tile after, are on their way.  Leaves the keys
+// and values of tile n on their way if the stretch has it.
+template <typename T, int DP>
+__device__ __forceinline__ void run_plain(const AttnParams& p, const Work& w, Loader<T, DP>& ld, Rows<T, DP>& r,
+                                          uint32_t n, uint32_t wave, T* s_kv, Flags* flags, float c, uint32_t sees) {
   using L = Tiles<T, DP>;
-  for (uint32_t i = i0; i < i1; ++i) {
+  const uint32_t loads = n < w.n_tiles ? n + 1 : n;
+  const auto load_keys = [&](uint32_t i) {
+    const uint32_t miss = ld.keys(p, w, w.tile + i, s_kv + (i & 1) * 2 * L::N);
+    if ((threadIdx.x & 63u) == 0) flags->missing[i & 3][wave] = (uint16_t)miss;
+  };
+  const auto load_values = [&](uint32_t i) { ld.values(p, w, w.tile + i, s_kv + (i & 1) * 2 * L::N + L::N); };
+  f32x16 s[2][2];
+  arrived();
+  load_values(0);
+  if (1 < loads) load_keys(1);
+  r.scores(fresh_lane(), s_kv, s[0], [](int) {});
+  const auto tile = [&](uint32_t i, f32x16 (&now)[2], f32x16 (&next)[2]) {
+    const uint32_t j0 = (w.tile + i) * kTile;
+    arrived();
+    const uint64_t missing = uni(*(const uint64_t*)flags->missing[i & 3]);
+    if (i + 1 < loads) load_values(i + 1);
+    if (i + 2 < loads) load_keys(i + 2);
+    const uint32_t lane = fresh_lane();
+    if (j0 + kTile > w.low || missing) r.template hide<2>(now, lane, j0, sees, missing);
+    r.overlapped(lane, now, next, s_kv + ((i + 1) & 1) * 2 * L::N, s_kv + (i & 1) * 2 * L::N + L::N, c);
+  };
+  for (uint32_t i = 0; i < n; i += 2) {
+    tile(i, s[0], s[1]);
+    if (i + 1 < n) tile(i + 1, s[1], s[0]);
+  }
+}
+
+// Tiles i0 .. of a stretch in steps of 32 keys, the first of them on its way.  One
+// tile is worked on while the next is on its way to the other half of the LDS.
+template <typename T, int DP>
+__device__ __forceinline__ void run_edges(const AttnParams& p, const Work& w, Loader<T, DP>& ld, Rows<T, DP>& r,
+                                          uint32_t i0, uint32_t wave, uint32_t kgroup, T* s_kv, Flags* flags, float c,
+                                          uint32_t sees) {
+  using L = Tiles<T, DP>;
+  for (uint32_t i = i0; i < w.n_tiles; ++i) {
     const uint32_t tile = w.tile + i, j0 = tile * kTile;
     T* sk = s_kv + (i & 1) * 2 * L::N;
     T* sv = sk + L::N;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    const uint64_t missing = uni(*(const uint64_t*)flags->missing[i & 1]);
+    arrived();
+    const uint64_t missing = uni(*(const uint64_t*)flags->missing[i & 3]);
     if (i + 1 < w.n_tiles) {
       T* next = s_kv + ((i + 1) & 1) * 2 * L::N;
-      const uint32_t miss = ld.load(p, w, tile + 1, next, next + L::N);
-      if ((threadIdx.x & 63u) == 0) flags->missing[(i + 1) & 1][wave] = (uint16_t)miss;
+      const uint32_t miss = ld.keys(p, w, tile + 1, next);
+      ld.values(p, w, tile + 1, next + L::N);
+      if ((threadIdx.x & 63u) == 0) flags->missing[(i + 1) & 3][wave] = (uint16_t)miss;
     }
     const bool edge = j0 + kTile > w.low;  // some row does not see all of the tile
     const bool mask = edge || missing;
-    if constexpr (NS == 2) {
-      r.template step<2>(fresh_lane(), sk, sv, 0, j0, c, mask, missing, sees);
-    } else {
-      bool odd = false;
-      if (edge && w.low < w.keys) {
-        bool found = false;
-        for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) found |= any_not_finite<T>(*(const u32x4*)(sv + x * 8));
-        const bool any = __any(found);
-        if ((threadIdx.x & 63u) == 0) flags->odd[wave] = any;
-        __syncthreads();
-        odd = uni(flags->odd[0] | flags->odd[1] | flags->odd[2] | flags->odd[3]);
-        if (odd)
-          for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256)
-            *(u32x4*)(sv + x * 8) = finite_only<T>(*(const u32x4*)(sv + x * 8));
-        __syncthreads();
-      }
-      // one key group takes all of a tile, two take a half each
+    bool odd = false;
+    if (edge && w.low < w.keys) {
+      bool found = false;
+      for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) found |= any_not_finite<T>(*(const u32x4*)(sv + x * 8));
+      const bool any = __any(found);
+      if ((threadIdx.x & 63u) == 0) flags->odd[wave] = any;
+      __syncthreads();
+      odd = uni(flags->odd[0] | flags->odd[1] | flags->odd[2] | flags->odd[3]);
+      if (odd)
+        for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256)
+          *(u32x4*)(sv + x * 8) = finite_only<T>(*(const u32x4*)(sv + x * 8));
+      __syncthreads();
+    }
+    // one key group takes all of a tile, two take a half each
 #pragma unroll 1
-      for (uint32_t x = kgroup * 32; x < kTile; x += w.rg == 4 ? 32 : kTile) {
-        r.template step<1>(fresh_lane(), sk, sv, x, j0 + x, c, mask, missing, sees);
-        if (odd) r.add_odd(p, w, fresh_lane(), j0 + x, sees);
-      }
+    for (uint32_t x = kgroup * 32; x < kTile; x += w.rg == 4 ? 32 : kTile) {
+      r.step(fresh_lane(), sk, sv, x, j0 + x, c, mask, missing, sees);
+      if (odd) r.add_odd(p, w, fresh_lane(), j0 + x, sees);
     }
   }
 }
@@ -567,7 +656,23 @@ __device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, 
   Loader<T, DP> ld;
   ld.start(p, w, wave);
   __syncthreads();  // LDS of the stretch before is free
-  const uint32_t missing0 = ld.load(p, w, w.tile, s_kv, s_kv + L::N);
+  if (a.cache.dim < DP) {
+    for (uint32_t x = threadIdx.x; x < 4 * L::N / 8; x += 256) *(u32x4*)(s_kv + x * 8) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+  }
+  // Tiles of which every row sees all keys, or a segment whose rows all see
+  // the same, with rows for all four waves: two heads wide (256) would leave no
+  // registers for two tiles' scores.
+  uint32_t plain = 0;
+  if (w.rg == 4 && DP <= 128) {
+    plain = w.n_tiles;
+    if (w.low < w.keys) {
+      const uint32_t full = w.low / kTile;  // tiles before the first that a row does not see to its end
+      plain = full <= w.tile ? 0 : full - w.tile < w.n_tiles ? full - w.tile : w.n_tiles;
+    }
+  }
+  const uint32_t missing0 = ld.keys(p, w, w.tile, s_kv);
+  if (!plain) ld.values(p, w, w.tile, s_kv + L::N);
   if (lane == 0) flags->missing[0][wave] = (uint16_t)missing0;
 
   Rows<T, DP> r;
@@ -594,18 +699,10 @@ __device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, 
     sees = !valid ? w.keys : v < 0 ? 0 : v < (int64_t)w.keys ? (uint32_t)v : w.keys;
   }
 
-  // Tiles of which every row sees all keys, or a segment whose rows all see
-  // the same: with rows for all four waves, 64 keys a step.
-  uint32_t plain = 0;
-  if (w.rg == 4) {
-    plain = w.n_tiles;
-    if (w.low < w.keys) {
-      const uint32_t full = w.low / kTile;  // tiles before the first that a row does not see to its end
-      plain = full <= w.tile ? 0 : full - w.tile < w.n_tiles ? full - w.tile : w.n_tiles;
-    }
-    run_tiles<2>(p, w, ld, r, 0, plain, wave, kgroup, s_kv, flags, c, sees);
+  if constexpr (DP <= 128) {
+    if (plain) run_plain(p, w, ld, r, plain, wave, s_kv, flags, c, sees);
   }
-  if (plain < w.n_tiles) run_tiles<1>(p, w, ld, r, plain, w.n_tiles, wave, kgroup, s_kv, flags, c, sees);
+  if (plain < w.n_tiles) run_edges(p, w, ld, r, plain, wave, kgroup, s_kv, flags, c, sees);
 
   // two waves that took other keys of the same rows: the second hands its to
   // the first
@@ -974,6 +1071,20 @@ __device__ __forceinline__ void run_stream(const AttnParams& p, const Work& w, T
   }
 }
 
+// Of a segment's tiles [from, to), whose places begin at seg, those that a
+// stretch from place t to place stop has: tile i begins at seg +
+// segment_places + (i - from) * tile_places, and is the stretch's in which it
+// begins.
+__device__ __forceinline__ void cut_tiles(uint64_t t, uint64_t stop, uint64_t seg, uint32_t rg, uint32_t& from,
+                                          uint32_t& to) {
+  const uint32_t each = tile_places(rg);
+  const uint64_t zero = seg + segment_places(rg);
+  const uint64_t a = t > zero ? (t - zero + each - 1) / each : 0, b = stop > zero ? (stop - zero + each - 1) / each : 0;
+  const uint32_t n = to - from;
+  to = from + (uint32_t)(b < n ? b : n);
+  from += (uint32_t)(a < n ? a : n);
+}
+
 template <typename T, int DP>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams p) {
   const gts_attention_args& a = p.a;
@@ -991,7 +1102,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   const uint32_t prows = a.batch.tokens * p.group;
   const uint32_t prg = row_groups(prows), n_prt = (prows + 32 * prg - 1) / (32 * prg);
   const uint32_t ptiles = (P + kTile - 1) / kTile;
-  const uint64_t prefix_places = places(ptiles, prg) * n_prt;
+  // pieces of the prefix: piece i is part i / n_prt of segment i % n_prt
+  const uint32_t whole = P ? p.whole : 0, line_piece = whole * p.cuts;  // the first in the line
+  const uint64_t piece_places = places((ptiles + p.pieces - 1) / p.pieces, prg);
+  const uint64_t prefix_places = P ? piece_places * (n_prt * p.pieces - line_piece) : 0;
   uint64_t mine = 0;
   for (uint32_t i = 0; i < per_thread; ++i) {
     const uint32_t b = tid * per_thread + i;
@@ -1036,14 +1150,14 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   const uint32_t head = id / p.cuts, g = id - head * p.cuts;
   uint64_t t = (uint64_t)g * per, end = t + per;
   if (end > total) end = total;
-  while (t < end) {
+  uint32_t dealt = 0;
+  while (dealt < whole || t < end) {
     Work w;
-    uint64_t seg;    // first place of the segment
-    uint32_t tiles;  // its tiles
-    if (t < prefix_places) {
-      tiles = ptiles;
-      const uint32_t rt = (uint32_t)(t / places(tiles, prg));
-      seg = (uint64_t)rt * places(tiles, prg);
+    uint64_t stop = t;   // place behind what is done of the line
+    uint32_t from, to;   // tiles of the segment
+    if (dealt < whole || t < prefix_places) {
+      const uint32_t piece = dealt < whole ? dealt * p.cuts + g : line_piece + (uint32_t)(t / piece_places);
+      const uint32_t j = piece / n_prt, rt = piece - j * n_prt;
       w.pages = (pages_t)a.prefix_pages;
       w.n_pages = a.n_prefix_pages;
       w.keys = w.low = P;
@@ -1052,7 +1166,17 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       w.rows = prows - w.first_row < 32 * prg ? prows - w.first_row : 32 * prg;
       w.own = false;
       w.see = 0;
-      w.part = w.first_row;
+      w.part = (uint64_t)j * prows + w.first_row;
+      from = (uint32_t)((uint64_t)ptiles * j / p.pieces);
+      to = (uint32_t)((uint64_t)ptiles * (j + 1) / p.pieces);
+      if (dealt < whole) {
+        ++dealt;
+      } else {
+        const uint64_t seg = (uint64_t)(piece - line_piece) * piece_places;
+        stop = seg + piece_places < end ? seg + piece_places : end;
+        cut_tiles(t, stop, seg, w.rg, from, to);
+        w.part += (uint64_t)p.part_rows * g;
+      }
     } else {
       // the last thread whose sequences start at or before t, then its
       // sequences one by one (one, up to 256 sequences)
@@ -1067,9 +1191,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
         s = load_seq(p, ++b);
       }
       w.rg = row_groups(s.n * p.group);
-      uint32_t rt = 0;
-      seg = first;
-      tiles = own_tiles(p, s, w.rg, 0);
+      uint32_t rt = 0, tiles = own_tiles(p, s, w.rg, 0);
+      uint64_t seg = first;
       while (t >= seg + places(tiles, w.rg)) {
         seg += places(tiles, w.rg);
         tiles = own_tiles(p, s, w.rg, ++rt);
@@ -1083,15 +1206,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       w.keys = seen(s, p.by_group.div(r0 + w.rows - 1));
       w.own = true;
       w.see = s.len - s.n + 1 - (int64_t)s.first;
-      w.part = (uint64_t)prows + s.first * p.group + r0;
+      w.part = (uint64_t)p.pieces * prows + s.first * p.group + r0 + (uint64_t)p.part_rows * g;
+      stop = seg + places(tiles, w.rg) < end ? seg + places(tiles, w.rg) : end;
+      from = 0;
+      to = tiles;
+      cut_tiles(t, stop, seg, w.rg, from, to);
     }
     w.head = head;
-    // tile i begins at place zero + i * each; its first place says
-    // whose it is
-    const uint32_t each = tile_places(w.rg);
-    const uint64_t zero = seg + segment_places(w.rg), last = zero + (uint64_t)tiles * each, stop = end < last ? end : last;
-    const uint32_t from = t > zero ? (uint32_t)((t - zero + each - 1) / each) : 0;
-    const uint32_t to = stop > zero ? (uint32_t)((stop - zero + each - 1) / each) : 0;
     if (to > from) {
       // the same in all lanes: kept in scalar registers
       w.pages = (pages_t)uni((uint64_t)w.pages);
@@ -1103,7 +1224,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       w.rows = uni(w.rows);
       w.first_row = uni(w.first_row);
       w.see = (int64_t)uni((uint64_t)w.see);
-      w.part = uni((uint64_t)(w.part + ((uint64_t)2 * prows + cut_rows) * head + (uint64_t)p.part_rows * g));
+      w.part = uni((uint64_t)(w.part + head_partials(prows, cut_rows) * head));
       w.tile = uni(from);
       w.n_tiles = uni(to - from);
       float *stats = (float*)(scratch + sc.stats), *sums = (float*)(scratch + sc.sums);
@@ -1136,40 +1257,53 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
   const float* stats = (const float*)(scratch + sc.stats);
   const float* sums = (const float*)(scratch + sc.sums);
 
-  // partials of the prefix: workgroups first[0] .. + count[0], rows at[0] +
-  // part_rows * workgroup; of the own keys likewise
-  uint32_t first[2] = {0, 0}, count[2] = {0, 0};
-  uint64_t at[2] = {0, 0};
+  // Three runs of partials, each count[] rows from at[] on, step[] apart: the
+  // pieces of the prefix that were dealt out, one in the line (of a row's pieces
+  // at most one is, when any are dealt out), and the own keys.
+  uint32_t count[3] = {0, 0, 0};
+  uint64_t at[3] = {0, 0, 0}, step[3] = {prows, p.part_rows, p.part_rows};
   uint32_t seq, index, n_new;
   if (find_sequence(a.batch, t, &seq, &index, &n_new)) {
-    const uint64_t base = ((uint64_t)2 * prows + cut_rows) * head;
-    const auto locate = [&](int part, uint64_t place, uint32_t tiles, uint32_t rg, uint64_t x) {
+    const uint64_t base = head_partials(prows, cut_rows) * head;
+    const uint32_t P = a.cache.n_pages ? a.batch.prefix_len : 0;
+    const auto locate = [&](int run, uint64_t place, uint32_t tiles, uint32_t rg, uint64_t x) {
       if (tiles == 0) return;
       place += segment_places(rg);
-      first[part] = plan.group_of(place);
-      count[part] = plan.group_of(place + (uint64_t)(tiles - 1) * tile_places(rg)) - first[part] + 1;
-      at[part] = base + x;
+      const uint32_t first = plan.group_of(place);
+      count[run] = plan.group_of(place + (uint64_t)(tiles - 1) * tile_places(rg)) - first + 1;
+      at[run] = base + x + (uint64_t)p.part_rows * first;
     };
-    if (a.cache.n_pages) {
-      const uint32_t tiles = (a.batch.prefix_len + kTile - 1) / kTile, rg = row_groups(prows), r = t * p.group + gq;
-      locate(0, places(tiles, rg) * (r / (32 * rg)), tiles, rg, r);
+    if (P) {
+      const uint32_t ptiles = (P + kTile - 1) / kTile, rg = row_groups(prows), n_rt = (prows + 32 * rg - 1) / (32 * rg);
+      const uint32_t r = t * p.group + gq, rt = r / (32 * rg), line = p.whole * p.cuts;
+      // piece j of this row has number j n_rt + rt; those below `line` were dealt out
+      const uint32_t dealt = line > rt ? (line - rt + n_rt - 1) / n_rt : 0;
+      count[0] = dealt < p.pieces ? dealt : p.pieces;
+      at[0] = base + r;
+      if (count[0] < p.pieces) {
+        const uint32_t j = count[0];
+        const uint32_t tiles = (uint32_t)((uint64_t)ptiles * (j + 1) / p.pieces - (uint64_t)ptiles * j / p.pieces);
+        locate(1, places((ptiles + p.pieces - 1) / p.pieces, rg) * (j * n_rt + rt - line), tiles, rg,
+               (uint64_t)j * prows + r);
+      }
     }
     const Seq s = load_seq(p, seq);
     if (s.keys) {
       const uint32_t rg = row_groups(s.n * p.group), r = index * p.group + gq, rt = r / (32 * rg);
       uint64_t place = ((const uint64_t*)(scratch + sc.begin))[seq];
       for (uint32_t i = 0; i < rt; ++i) place += places(own_tiles(p, s, rg, i), rg);
-      locate(1, place, own_tiles(p, s, rg, rt), rg, (uint64_t)prows + s.first * p.group + r);
+      locate(2, place, own_tiles(p, s, rg, rt), rg, (uint64_t)p.pieces * prows + s.first * p.group + r);
     }
   }
 
   float m = -INFINITY, l = 0.f;
   float2 o[GTS_OPS_MAX_ATTN / 128] = {};
-  const uint32_t n = count[0] + count[1];
+  const uint32_t n01 = count[0] + count[1], n = n01 + count[2];
   for (uint32_t i0 = 0; i0 < n; i0 += 64) {
     const uint32_t i = i0 + lane;
-    const bool own = i >= count[0];
-    const uint64_t x = at[own] + (uint64_t)p.part_rows * (own ? first[1] + i - count[0] : first[0] + i);
+    const uint64_t x = i < count[0] ? at[0] + step[0] * i
+                       : i < n01    ? at[1] + step[1] * (i - count[0])
+                                    : at[2] + step[2] * (i - n01);
     float mi = -INFINITY, li = 0.f;
     if (i < n) {
       const float2 v = *(const float2*)(stats + 2 * x);
@@ -1319,6 +1453,19 @@ uint64_t attention_scratch(uint32_t batch, uint32_t tokens, uint32_t q_heads, ui
       .bytes;
 }
 
+// How the prefix is dealt out: segments whole where there are more than
+// workgroups, else in the fewest equal pieces that give each workgroup one, if
+// those are 8 tiles or more (shorter ones cost more to begin than they save).
+// pieces * segments is below workgroups + segments, so that what is left over
+// for the line is less than a piece of each segment.
+static void deal_prefix(AttnParams& p) {
+  const uint32_t rows = p.a.batch.tokens * p.group, rg = row_groups(rows), n = (rows + 32 * rg - 1) / (32 * rg);
+  const uint32_t tiles = (p.a.batch.prefix_len + kTile - 1) / kTile;
+  p.pieces = 1;
+  if (n > 1 && n < p.cuts && tiles / ((p.cuts + n - 1) / n) >= 8) p.pieces = (p.cuts + n - 1) / n;
+  p.whole = n > 1 && tiles ? n * p.pieces / p.cuts : 0;
+}
+
 // The tile kernel's loads: 16-bit values, every row of q, k and v and every 16
 // bytes of it aligned to 16 bytes.
 static bool tiles_fit(const gts_attention_args& a) {
@@ -1340,6 +1487,7 @@ static hipError_t launch_typed(AttnParams& p, hipStream_t stream) {
   if constexpr (sizeof(T) == 2) {
     if (tiles_fit(a)) {
       p.cuts = cuts(a.cache.heads, a.cache.dim);
+      deal_prefix(p);
       const dim3 wgs(p.cuts * a.cache.heads);
       if (a.cache.dim <= 64)
         tile_kernel<T, 64><<<wgs, block, 0, stream>>>(p);
@@ -1363,10 +1511,8 @@ hipError_t launch_attention(const gts_attention_args& a, hipStream_t stream) {
   p.by_group = FastDiv(p.group);
   p.by_q_heads = FastDiv(a.q_heads);
   p.part_rows = part_rows(a.batch.tokens, p.group);
-  // chunks beyond the head must come out as zeros: the general way alone
   const int64_t far = 1 << 26;  // elements: 16 rows and a chunk stay below 2^31 bytes
-  p.near_rows = p.page_shift >= 4 && (a.cache.dim == 64 || a.cache.dim == 128 || a.cache.dim == 256) &&
-                a.cache.k_stride[1] >= 0 && a.cache.k_stride[1] < far && a.cache.v_stride[1] >= 0 &&
+  p.near_rows = p.page_shift >= 4 && a.cache.k_stride[1] >= 0 && a.cache.k_stride[1] < far && a.cache.v_stride[1] >= 0 &&
                 a.cache.v_stride[1] < far;
   if (a.cache.dtype == GTS_F32) return launch_typed<float>(p, stream);
   if (a.cache.dtype == GTS_BF16) return launch_typed<__bf16>(p, stream);

@@ -330,6 +330,10 @@ ATTENTION = {
     "head of 16": (BF, 6, 2, 16, 4, None, [3, 50, 5], 33),
     "odd head": (BF, 6, 2, 33, 4, None, [3, 50], 33),
     "32 bits": (F, 6, 3, 64, 16, [1, 4], [40, 70], 50),
+    # the prefix dealt out: in pieces (8 workgroups a head, 3 segments), and whole
+    # (2 workgroups a head, 3 segments), a piece of each left for the line
+    "prefix in pieces": (BF, 64, 64, 64, 64, [150, 1, 149], [150, 20, 160], 1601),
+    "prefix dealt out whole": (HF, 1024, 256, 8, 16, [50, 46], [50, 60], 100),
     "page of one": (BF, 2, 1, 64, 1, None, [70, 3], 9),
     "many sequences": (BF, 2, 1, 64, 16, None, [1 + (i * 37) % 90 for i in range(300)], 20),
     "empty rows": (BF, 4, 2, 64, 16, [3, 1, 2, 0], [1, 0, 0, 50], 0),
