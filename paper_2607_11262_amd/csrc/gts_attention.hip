@@ -247,12 +247,14 @@ template <typename T, int DP>
 struct Loader {
   using L = Tiles<T, DP>;
   uint32_t k_off[L::NL], v_off[L::NL];  // bytes from the wave's first row to this lane's chunk
-  int32_t next, last;  // page of the wave's rows in the next tile of keys, and in the last loaded (pages of 16 or more)
+  int32_t page;                         // page of the wave's rows in the next tile (pages of 16 or more)
   uint32_t wave;
+  bool near;  // pages of 16 or more, and 16 rows lie within 2 GiB: k_off and v_off serve
 
   __device__ __forceinline__ void start(const AttnParams& p, const Work& w, uint32_t wave_) {
     const gts_kv_cache& kc = p.a.cache;
     wave = wave_;
+    near = p.near_rows;
     const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
 #pragma unroll
     for (int n = 0; n < L::NL; ++n) {
@@ -260,55 +262,49 @@ struct Loader {
       k_off[n] = 2 * (r * (uint32_t)kc.k_stride[1] + (c ^ L::swizzle_k(r)) * 8);
       v_off[n] = 2 * (r * (uint32_t)kc.v_stride[1] + (c ^ L::swizzle_v(r)) * 8);
     }
-    next = page_of(p, w, w.tile);
-    last = -1;
+    page = p.page_shift >= 4 ? next_page(p, w, w.tile) : 0;
   }
   // By a vector load, though it is the same for all lanes: LDS reads wait for
   // every scalar load before them (one counter), and this one may be long.
-  __device__ __forceinline__ int32_t page_of(const AttnParams& p, const Work& w, uint32_t tile) const {
+  __device__ __forceinline__ int32_t next_page(const AttnParams& p, const Work& w, uint32_t tile) const {
     const uint32_t at = (tile * kTile + wave * 16) >> p.page_shift;
     uint32_t zero = 0;
     asm volatile("" : "+v"(zero));
-    return p.page_shift >= 4 && at < w.n_pages ? (w.pages + at)[zero] : -1;
+    return at < w.n_pages ? (w.pages + at)[zero] : -1;
   }
 
-  // The keys of a tile, then the values of the last tile of keys.  Returns the
-  // wave's rows inside the segment that no page holds (one bit each, the same in
-  // all lanes).
-  __device__ __forceinline__ uint32_t keys(const AttnParams& p, const Work& w, uint32_t tile, T* to) {
-    last = uni((uint32_t)next);
-    const uint32_t missing = half<false>(p, w, tile, p.a.cache.k, p.a.cache.k_stride, k_off, to);
-    next = page_of(p, w, tile + 1);
-    return missing;
-  }
-  __device__ __forceinline__ void values(const AttnParams& p, const Work& w, uint32_t tile, T* to) {
-    half<true>(p, w, tile, p.a.cache.v, p.a.cache.v_stride, v_off, to);
-  }
-
-  template <bool V>
-  __device__ __forceinline__ uint32_t half(const AttnParams& p, const Work& w, uint32_t tile, const void* base,
-                                           const int64_t* stride, const uint32_t (&off)[L::NL], T* to) {
+  // Returns the wave's rows inside the segment that no page holds (one bit
+  // each, the same in all lanes).
+  __device__ __forceinline__ uint32_t load(const AttnParams& p, const Work& w, uint32_t tile, T* sk, T* sv) {
     const gts_kv_cache& kc = p.a.cache;
     const uint32_t j0 = tile * kTile + wave * 16;
-    if (p.near_rows && (uint32_t)last < kc.n_pages && j0 + 16 <= w.keys) {
+    const uint32_t pg0 = uni((uint32_t)page);
+    if (near && pg0 < kc.n_pages && j0 + 16 <= w.keys) {
       const uint32_t slot = j0 & (kc.page - 1);
-      const char* row = (const char*)((const T*)base + (int64_t)last * stride[0] + (int64_t)slot * stride[1] +
-                                      (int64_t)w.head * stride[2]);
+      const char* kp = (const char*)((const T*)kc.k + (int64_t)pg0 * kc.k_stride[0] + (int64_t)slot * kc.k_stride[1] +
+                                     (int64_t)w.head * kc.k_stride[2]);
+      const char* vp = (const char*)((const T*)kc.v + (int64_t)pg0 * kc.v_stride[0] + (int64_t)slot * kc.v_stride[1] +
+                                     (int64_t)w.head * kc.v_stride[2]);
       if (kc.dim == DP) {
 #pragma unroll
-        for (int n = 0; n < L::NL; ++n) load_to_lds(row + off[n], to + (wave * 16 + n * L::RPI) * DP);
+        for (int n = 0; n < L::NL; ++n) {
+          const uint32_t at = (wave * 16 + n * L::RPI) * DP;
+          load_to_lds(kp + k_off[n], sk + at);
+          load_to_lds(vp + v_off[n], sv + at);
+        }
       } else {
         const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
 #pragma unroll
         for (int n = 0; n < L::NL; ++n) {
-          const uint32_t r = n * L::RPI + r0;
-          if ((c ^ (V ? L::swizzle_v(r) : L::swizzle_k(r))) * 8 < kc.dim)
-            load_to_lds(row + off[n], to + (wave * 16 + n * L::RPI) * DP);
+          const uint32_t at = (wave * 16 + n * L::RPI) * DP, r = n * L::RPI + r0;
+          if ((c ^ L::swizzle_k(r)) * 8 < kc.dim) load_to_lds(kp + k_off[n], sk + at);
+          if ((c ^ L::swizzle_v(r)) * 8 < kc.dim) load_to_lds(vp + v_off[n], sv + at);
         }
       }
+      page = next_page(p, w, tile + 1);
       return 0;
     }
-    // every row by itself
+    // the general way: every row by itself
     const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
     uint32_t missing = 0;
 #pragma unroll 1
@@ -318,11 +314,17 @@ struct Loader {
       const int32_t pg = in ? key_page(p.a, w.pages, w.n_pages, p.page_shift, j) : -1;
       const uint64_t lost = __ballot(in && pg < 0);
       for (int i = 0; i < L::RPI; ++i) missing |= (uint32_t)(lost >> (i * L::C) & 1) << (n * L::RPI + i);
-      const uint32_t d = (c ^ (V ? L::swizzle_v(r) : L::swizzle_k(r))) * 8;
-      const T* x = (const T*)base + (int64_t)pg * stride[0] + (int64_t)(j & (kc.page - 1)) * stride[1] +
-                   (int64_t)w.head * stride[2] + d;
-      load_to_lds(pg >= 0 && d < kc.dim ? x : (const T*)g_zeros, to + (wave * 16 + n * L::RPI) * DP);
+      const int64_t slot = j & (kc.page - 1);
+      const uint32_t ck = (c ^ L::swizzle_k(r)) * 8, cv = (c ^ L::swizzle_v(r)) * 8;
+      const T* kp = (const T*)kc.k + (int64_t)pg * kc.k_stride[0] + slot * kc.k_stride[1] + (int64_t)w.head * kc.k_stride[2] + ck;
+      const T* vp = (const T*)kc.v + (int64_t)pg * kc.v_stride[0] + slot * kc.v_stride[1] + (int64_t)w.head * kc.v_stride[2] + cv;
+      kp = pg >= 0 && ck < kc.dim ? kp : (const T*)g_zeros;
+      vp = pg >= 0 && cv < kc.dim ? vp : (const T*)g_zeros;
+      const uint32_t at = (wave * 16 + n * L::RPI) * DP;
+      load_to_lds(kp, sk + at);
+      load_to_lds(vp, sv + at);
     }
+    if (p.page_shift >= 4) page = next_page(p, w, tile + 1);
     return missing;
   }
 };
@@ -398,111 +400,57 @@ struct Rows {
     l = 0.f;
   }
 
-  // 32 keys from LDS row `key` on (key number j0 of the segment).
-  __device__ __forceinline__ void step(uint32_t lane, const T* sk, const T* sv, uint32_t key, uint32_t j0, float c,
-                                       bool mask, uint64_t missing, uint32_t sees) {
-    f32x16 s[1];
+  // NS blocks of 32 keys from LDS row `key` on (key number j0 of the segment).
+  template <int NS>
+  __device__ __forceinline__ void step(uint32_t lane, const T* sk, const T* sv, uint32_t key, uint32_t j0, float c, bool mask,
+                                       uint64_t missing, uint32_t sees) {
+    const uint32_t half = lane / 32;
+    f32x16 s[NS];
     const T* ka = sk + (key + lane % 32) * DP;
-    const uint32_t kc = lane / 32 ^ L::swizzle_k(lane % 32);
+    const uint32_t kc = half ^ L::swizzle_k(lane % 32);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
-#pragma unroll
-    for (int kk = 0; kk < L::KK; ++kk) s[0] = mfma(*(const Vec8<T>*)(ka + (kc ^ (2 * kk)) * 8), q[kk], s[0]);
-    if (mask) hide(s, lane, j0, sees, missing >> key);
-    follow(s, c);
-    const float base = m == -INFINITY ? 0.f : -m * c;
-    float sum[2] = {0.f, 0.f};
-    Vec8<T> pw[2];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float e = exp2_(__builtin_fmaf(s[0][i], c, base));
-      sum[i & 1] += e;
-      pw[i / 8][i % 8] = (T)e;
-    }
-    l += sum[0] + sum[1];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int mb = 0; mb < L::MB; ++mb) o[mb] = mfma(load_v<T, DP>(sv, lane, key + kb * 16, mb), pw[kb], o[mb]);
-  }
-
-  // The scores of 64 keys: dims in `L::KK` steps, the fragments of one step read
-  // while the one before is multiplied; `between(x)` after each of the 2 KK
-  // products.
-  template <typename F>
-  __device__ __forceinline__ void scores(uint32_t lane, const T* sk, f32x16 (&s)[2], F between) const {
-    const T* ka = sk + lane % 32 * DP;
-    const uint32_t kc = lane / 32 ^ L::swizzle_k(lane % 32);
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < NS; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-    Vec8<T> kf[2][2];
+    // The fragments of two matrix steps are read while the two before are
+    // multiplied; the fences keep that order.
+    Vec8<T> kf[2][2][NS];
+    const auto read = [&](int at, int kk) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) kf[0][b] = *(const Vec8<T>*)(ka + b * 32 * DP + kc * 8);
-#pragma unroll
-    for (int kk = 0; kk < L::KK; ++kk) {
-      if (kk + 1 < L::KK) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-          kf[kk + 1 & 1][b] = *(const Vec8<T>*)(ka + b * 32 * DP + (kc ^ (2 * kk + 2)) * 8);
+      for (int b = 0; b < NS; ++b) {
+        kf[at][0][b] = *(const Vec8<T>*)(ka + b * 32 * DP + (kc ^ (2 * kk)) * 8);
+        kf[at][1][b] = *(const Vec8<T>*)(ka + b * 32 * DP + (kc ^ (2 * kk + 2)) * 8);
       }
+    };
+    read(0, 0);
+#pragma unroll
+    for (int kk = 0; kk < L::KK; kk += 2) {
+      if (kk + 2 < L::KK) read(kk / 2 + 1 & 1, kk + 2);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        s[b] = mfma(kf[kk & 1][b], q[kk], s[b]);
-        between(2 * kk + b);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-  }
-
-  // The softmax and the second product of 64 keys whose scores are s, and the
-  // first product of the next 64 into `next`: the exponentials stand between the
-  // products, so that a wave keeps both units busy by itself.
-  __device__ __forceinline__ void overlapped(uint32_t lane, f32x16 (&s)[2], f32x16 (&next)[2], const T* sk, const T* sv,
-                                             float c) {
-    follow(s, c);
-    const float base = m == -INFINITY ? 0.f : -m * c;
-    float sum[2] = {0.f, 0.f};
-    Vec8<T> pw[4];
-    scores(lane, sk, next, [&](int x) {
-      constexpr int N = 16 / L::KK;  // weights a product
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
-      for (int y = 0; y < N; ++y) {
-        const int i = x * N + y;
-        const float e = exp2_(__builtin_fmaf(s[i / 16][i % 16], c, base));
-        sum[i & 1] += e;
-        pw[i / 8][i % 8] = (T)e;
-      }
-    });
-    l += sum[0] + sum[1];
-    Vec8<T> vf[2][L::MB];
-#pragma unroll
-    for (int mb = 0; mb < L::MB; ++mb) vf[0][mb] = load_v<T, DP>(sv, lane, 0, mb);
-#pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-      if (kb + 1 < 4) {
-#pragma unroll
-        for (int mb = 0; mb < L::MB; ++mb) vf[kb + 1 & 1][mb] = load_v<T, DP>(sv, lane, kb * 16 + 16, mb);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int mb = 0; mb < L::MB; ++mb) o[mb] = mfma(vf[kb & 1][mb], pw[kb], o[mb]);
+        for (int b = 0; b < NS; ++b) s[b] = mfma(kf[kk / 2 & 1][x][b], q[kk + x], s[b]);
       __builtin_amdgcn_sched_barrier(0);
     }
-  }
-
-  // Moves the reference maximum when some row's scores are 2^8 ahead of it:
-  // weights up to 256 are as exact, and sums and output are rescaled rarely.
-  template <int NS>
-  __device__ __forceinline__ void follow(const f32x16 (&s)[NS], float c) {
+    if (mask) {
+#pragma unroll
+      for (int b = 0; b < NS; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t r = b * 32 + 8 * (i / 4) + 4 * half + i % 4;
+          const bool ok = j0 + r < sees && !(missing >> (key + r) & 1);
+          s[b][i] = ok ? s[b][i] : -INFINITY;
+        }
+    }
     float mx = s[0][0];
 #pragma unroll
     for (int b = 0; b < NS; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
     mx = max_halves(mx);
+    // The reference follows the maximum only when that is 2^8 ahead: weights
+    // up to 256 are as exact, and sums and output are rescaled rarely.
     if (__any((mx - m) * c > 8.f || (m == -INFINITY && mx > m))) {
       const float m1 = fmaxf(m, mx);
       const float alpha = m == -INFINITY ? 0.f : exp2_((m - m1) * c);
@@ -513,19 +461,39 @@ struct Rows {
         for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
       m = m1;
     }
-  }
-
-  // Scores of keys that a row does not see, or that no page holds.
-  template <int NS>
-  static __device__ __forceinline__ void hide(f32x16 (&s)[NS], uint32_t lane, uint32_t j0, uint32_t sees,
-                                              uint64_t missing) {
+    const float base = m == -INFINITY ? 0.f : -m * c;
+    float sum[2] = {0.f, 0.f};
+    Vec8<T> pw[2 * NS];
+    const auto weigh = [&](int kb, int i) {
+      const float e = exp2_(__builtin_fmaf(s[kb / 2][kb % 2 * 8 + i], c, base));
+      sum[i & 1] += e;
+      pw[kb][i] = (T)e;
+    };
+    // The weights of 16 keys are computed, and the values of 16 keys read,
+    // between the products of the 16 keys before.
+    Vec8<T> vf[2][L::MB];
 #pragma unroll
-    for (int b = 0; b < NS; ++b)
+    for (int mb = 0; mb < L::MB; ++mb) vf[0][mb] = load_v<T, DP>(sv, lane, key, mb);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t r = b * 32 + 8 * (i / 4) + 4 * (lane / 32) + i % 4;
-        s[b][i] = j0 + r < sees && !(missing >> r & 1) ? s[b][i] : -INFINITY;
+    for (int i = 0; i < 8; ++i) weigh(0, i);
+#pragma unroll
+    for (int kb = 0; kb < 2 * NS; ++kb) {
+      if (kb + 1 < 2 * NS) {
+#pragma unroll
+        for (int mb = 0; mb < L::MB; ++mb) vf[kb + 1 & 1][mb] = load_v<T, DP>(sv, lane, key + kb * 16 + 16, mb);
       }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int mb = 0; mb < L::MB; ++mb) {
+        o[mb] = mfma(vf[kb & 1][mb], pw[kb], o[mb]);
+        if (kb + 1 < 2 * NS) {
+#pragma unroll
+          for (int i = mb * 8 / L::MB; i < (mb + 1) * 8 / L::MB; ++i) weigh(kb + 1, i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    l += sum[0] + sum[1];
   }
 
   // See not_finite: keys j0 .. j0 + 31.
@@ -550,91 +518,54 @@ struct Rows {
 
 // Flags that the waves of a workgroup leave each other for a tile.
 struct Flags {
-  uint16_t missing[4][4];  // rows without a page, of a tile and three after it
+  uint16_t missing[2][4];  // rows without a page
   uint32_t odd[4];         // values that are not finite
 };
 
-// Everything that this wave has asked for is there, and everybody's after it.
-__device__ __forceinline__ void arrived() {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-}
-
-// Tiles 0 .. n of a stretch whose rows all see the same, or see all of these
-// tiles; the keys of the first are on their way.  While the softmax and the
-// second product of a tile are computed, so is the first product of the next; its
-// values, and the keys of the tile after, are on their way.  Leaves the keys
-// and values of tile n on their way if the stretch has it.
-template <typename T, int DP>
-__device__ __forceinline__ void run_plain(const AttnParams& p, const Work& w, Loader<T, DP>& ld, Rows<T, DP>& r,
-                                          uint32_t n, uint32_t wave, T* s_kv, Flags* flags, float c, uint32_t sees) {
+// Tiles i0 .. i1 of a stretch, the first of them already on its way.  One tile is
+// worked on while the next is on its way to the other half of the LDS; one
+// barrier a tile.
+template <int NS, typename T, int DP>
+__device__ __forceinline__ void run_tiles(const AttnParams& p, const Work& w, Loader<T, DP>& ld, Rows<T, DP>& r,
+                                          uint32_t i0, uint32_t i1, uint32_t wave, uint32_t kgroup, T* s_kv,
+                                          Flags* flags, float c, uint32_t sees) {
   using L = Tiles<T, DP>;
-  const uint32_t loads = n < w.n_tiles ? n + 1 : n;
-  const auto load_keys = [&](uint32_t i) {
-    const uint32_t miss = ld.keys(p, w, w.tile + i, s_kv + (i & 1) * 2 * L::N);
-    if ((threadIdx.x & 63u) == 0) flags->missing[i & 3][wave] = (uint16_t)miss;
-  };
-  const auto load_values = [&](uint32_t i) { ld.values(p, w, w.tile + i, s_kv + (i & 1) * 2 * L::N + L::N); };
-  f32x16 s[2][2];
-  arrived();
-  load_values(0);
-  if (1 < loads) load_keys(1);
-  r.scores(fresh_lane(), s_kv, s[0], [](int) {});
-  const auto tile = [&](uint32_t i, f32x16 (&now)[2], f32x16 (&next)[2]) {
-    const uint32_t j0 = (w.tile + i) * kTile;
-    arrived();
-    const uint64_t missing = uni(*(const uint64_t*)flags->missing[i & 3]);
-    if (i + 1 < loads) load_values(i + 1);
-    if (i + 2 < loads) load_keys(i + 2);
-    const uint32_t lane = fresh_lane();
-    if (j0 + kTile > w.low || missing) r.template hide<2>(now, lane, j0, sees, missing);
-    r.overlapped(lane, now, next, s_kv + ((i + 1) & 1) * 2 * L::N, s_kv + (i & 1) * 2 * L::N + L::N, c);
-  };
-  for (uint32_t i = 0; i < n; i += 2) {
-    tile(i, s[0], s[1]);
-    if (i + 1 < n) tile(i + 1, s[1], s[0]);
-  }
-}
-
-// Tiles i0 .. of a stretch in steps of 32 keys, the first of them on its way.  One
-// tile is worked on while the next is on its way to the other half of the LDS.
-template <typename T, int DP>
-__device__ __forceinline__ void run_edges(const AttnParams& p, const Work& w, Loader<T, DP>& ld, Rows<T, DP>& r,
-                                          uint32_t i0, uint32_t wave, uint32_t kgroup, T* s_kv, Flags* flags, float c,
-                                          uint32_t sees) {
-  using L = Tiles<T, DP>;
-  for (uint32_t i = i0; i < w.n_tiles; ++i) {
+  for (uint32_t i = i0; i < i1; ++i) {
     const uint32_t tile = w.tile + i, j0 = tile * kTile;
     T* sk = s_kv + (i & 1) * 2 * L::N;
     T* sv = sk + L::N;
-    arrived();
-    const uint64_t missing = uni(*(const uint64_t*)flags->missing[i & 3]);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const uint64_t missing = uni(*(const uint64_t*)flags->missing[i & 1]);
     if (i + 1 < w.n_tiles) {
       T* next = s_kv + ((i + 1) & 1) * 2 * L::N;
-      const uint32_t miss = ld.keys(p, w, tile + 1, next);
-      ld.values(p, w, tile + 1, next + L::N);
-      if ((threadIdx.x & 63u) == 0) flags->missing[(i + 1) & 3][wave] = (uint16_t)miss;
+      const uint32_t miss = ld.load(p, w, tile + 1, next, next + L::N);
+      if ((threadIdx.x & 63u) == 0) flags->missing[(i + 1) & 1][wave] = (uint16_t)miss;
     }
     const bool edge = j0 + kTile > w.low;  // some row does not see all of the tile
     const bool mask = edge || missing;
-    bool odd = false;
-    if (edge && w.low < w.keys) {
-      bool found = false;
-      for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) found |= any_not_finite<T>(*(const u32x4*)(sv + x * 8));
-      const bool any = __any(found);
-      if ((threadIdx.x & 63u) == 0) flags->odd[wave] = any;
-      __syncthreads();
-      odd = uni(flags->odd[0] | flags->odd[1] | flags->odd[2] | flags->odd[3]);
-      if (odd)
-        for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256)
-          *(u32x4*)(sv + x * 8) = finite_only<T>(*(const u32x4*)(sv + x * 8));
-      __syncthreads();
-    }
-    // one key group takes all of a tile, two take a half each
+    if constexpr (NS == 2) {
+      r.template step<2>(fresh_lane(), sk, sv, 0, j0, c, mask, missing, sees);
+    } else {
+      bool odd = false;
+      if (edge && w.low < w.keys) {
+        bool found = false;
+        for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) found |= any_not_finite<T>(*(const u32x4*)(sv + x * 8));
+        const bool any = __any(found);
+        if ((threadIdx.x & 63u) == 0) flags->odd[wave] = any;
+        __syncthreads();
+        odd = uni(flags->odd[0] | flags->odd[1] | flags->odd[2] | flags->odd[3]);
+        if (odd)
+          for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256)
+            *(u32x4*)(sv + x * 8) = finite_only<T>(*(const u32x4*)(sv + x * 8));
+        __syncthreads();
+      }
+      // one key group takes all of a tile, two take a half each
 #pragma unroll 1
-    for (uint32_t x = kgroup * 32; x < kTile; x += w.rg == 4 ? 32 : kTile) {
-      r.step(fresh_lane(), sk, sv, x, j0 + x, c, mask, missing, sees);
-      if (odd) r.add_odd(p, w, fresh_lane(), j0 + x, sees);
+      for (uint32_t x = kgroup * 32; x < kTile; x += w.rg == 4 ? 32 : kTile) {
+        r.template step<1>(fresh_lane(), sk, sv, x, j0 + x, c, mask, missing, sees);
+        if (odd) r.add_odd(p, w, fresh_lane(), j0 + x, sees);
+      }
     }
   }
 }
@@ -660,19 +591,7 @@ __device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, 
     for (uint32_t x = threadIdx.x; x < 4 * L::N / 8; x += 256) *(u32x4*)(s_kv + x * 8) = u32x4{0, 0, 0, 0};
     __syncthreads();
   }
-  // Tiles of which every row sees all keys, or a segment whose rows all see
-  // the same, with rows for all four waves: two heads wide (256) would leave no
-  // registers for two tiles' scores.
-  uint32_t plain = 0;
-  if (w.rg == 4 && DP <= 128) {
-    plain = w.n_tiles;
-    if (w.low < w.keys) {
-      const uint32_t full = w.low / kTile;  // tiles before the first that a row does not see to its end
-      plain = full <= w.tile ? 0 : full - w.tile < w.n_tiles ? full - w.tile : w.n_tiles;
-    }
-  }
-  const uint32_t missing0 = ld.keys(p, w, w.tile, s_kv);
-  if (!plain) ld.values(p, w, w.tile, s_kv + L::N);
+  const uint32_t missing0 = ld.load(p, w, w.tile, s_kv, s_kv + L::N);
   if (lane == 0) flags->missing[0][wave] = (uint16_t)missing0;
 
   Rows<T, DP> r;
@@ -699,10 +618,18 @@ __device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, 
     sees = !valid ? w.keys : v < 0 ? 0 : v < (int64_t)w.keys ? (uint32_t)v : w.keys;
   }
 
-  if constexpr (DP <= 128) {
-    if (plain) run_plain(p, w, ld, r, plain, wave, s_kv, flags, c, sees);
+  // Tiles of which every row sees all keys, or a segment whose rows all see
+  // the same: with rows for all four waves, 64 keys a step.
+  uint32_t plain = 0;
+  if (w.rg == 4) {
+    plain = w.n_tiles;
+    if (w.low < w.keys) {
+      const uint32_t full = w.low / kTile;  // tiles before the first that a row does not see to its end
+      plain = full <= w.tile ? 0 : full - w.tile < w.n_tiles ? full - w.tile : w.n_tiles;
+    }
+    run_tiles<2>(p, w, ld, r, 0, plain, wave, kgroup, s_kv, flags, c, sees);
   }
-  if (plain < w.n_tiles) run_edges(p, w, ld, r, plain, wave, kgroup, s_kv, flags, c, sees);
+  if (plain < w.n_tiles) run_tiles<1>(p, w, ld, r, plain, w.n_tiles, wave, kgroup, s_kv, flags, c, sees);
 
   // two waves that took other keys of the same rows: the second hands its to
   // the first
