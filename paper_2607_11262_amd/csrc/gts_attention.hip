@@ -620,14 +620,15 @@ __device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, 
 
   // Tiles of which every row sees all keys, or a segment whose rows all see
   // the same: with rows for all four waves, 64 keys a step.
+  // (Heads of 256 leave no registers for it.)
   uint32_t plain = 0;
-  if (w.rg == 4) {
+  if (DP <= 128 && w.rg == 4) {
     plain = w.n_tiles;
     if (w.low < w.keys) {
       const uint32_t full = w.low / kTile;  // tiles before the first that a row does not see to its end
       plain = full <= w.tile ? 0 : full - w.tile < w.n_tiles ? full - w.tile : w.n_tiles;
     }
-    run_tiles<2>(p, w, ld, r, 0, plain, wave, kgroup, s_kv, flags, c, sees);
+    if constexpr (DP <= 128) run_tiles<2>(p, w, ld, r, 0, plain, wave, kgroup, s_kv, flags, c, sees);
   }
   if (plain < w.n_tiles) run_tiles<1>(p, w, ld, r, plain, w.n_tiles, wave, kgroup, s_kv, flags, c, sees);
 
@@ -1155,12 +1156,16 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
       w.tile = uni(from);
       w.n_tiles = uni(to - from);
       float *stats = (float*)(scratch + sc.stats), *sums = (float*)(scratch + sc.sums);
-      if (w.rg > 1)
+      // 32 rows of 256 values do not fit the stream's registers: half the tile
+      // path's rows stay empty
+      if (DP > 128 && w.rows > 16 && w.rg == 1) w.rg = 2;
+      if (w.rg > 1) {
         run_stretch<T, DP>(p, w, s_kv, &s_flags, stats, sums);
-      else if (w.rows <= 16)
+      } else if (w.rows <= 16) {
         run_stream<1, T, DP>(p, w, s_kv, s_ml, stats, sums);
-      else
-        run_stream<2, T, DP>(p, w, s_kv, s_ml, stats, sums);
+      } else {
+        if constexpr (DP <= 128) run_stream<2, T, DP>(p, w, s_kv, s_ml, stats, sums);
+      }
     }
     t = uni(stop);
   }

@@ -33,6 +33,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import math
+import struct
 
 import torch
 
@@ -79,7 +80,14 @@ class _AttentionArgs(ctypes.Structure):
                 ("scale", _f32), ("reserved", _u32), ("scratch", _vp), ("scratch_bytes", ctypes.c_uint64)]
 
 
-_bound = None
+# The structures' values in one call each, as the C side lays them out: a call of
+# a small batch is bound by the host.
+_pack_rotary = struct.Struct("=4Q3q3q2qq10I").pack
+_pack_cache_batch = "2Q3q3q6I3Qq4I"
+_pack_append = struct.Struct("=" + _pack_cache_batch + "4Q2q2q2q2qQq4I").pack
+_pack_attention = struct.Struct("=" + _pack_cache_batch + "3Q2q2qQ2IfIQQ").pack
+
+_bound, _calls = None, {}  # the library the calls are bound to
 
 
 def lib():
@@ -93,7 +101,9 @@ def lib():
         L.gts_rotary_table.argtypes = [_vp, _u32, _u32, _vp, ctypes.c_double, _vp]
         for name in ("gts_rotary", "gts_append_kv", "gts_shared_prefix_attention"):
             getattr(L, name).argtypes = [_vp, _vp]
+            _calls[name] = getattr(L, name)
         L.gts_shared_prefix_attention_scratch.argtypes = [_u32] * 5 + [ctypes.POINTER(ctypes.c_uint64)]
+        _scratch_bytes.cache_clear()
         _bound = L
     return L
 
@@ -107,34 +117,49 @@ def _refuse(ok, why):
 
 def _data(t, name, dims, like=None):
     """t is a tensor on the GPU with `dims` dimensions and a contiguous last
-    one, of the type and on the device of `like`."""
+    one, of the type and on the device of `like`; returns its strides."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} is a tensor: got {type(t).__name__}")
-    _refuse(t.dim() == dims, f"{name} has {t.dim()} dimensions, not {dims}")
-    _refuse(t.is_cuda, f"{name} is not on the GPU")
-    _refuse(t.stride(-1) == 1 or t.shape[-1] <= 1, f"{name}: the last dimension is not contiguous")
+    if t.dim() != dims:
+        raise ValueError(f"{name} has {t.dim()} dimensions, not {dims}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} is not on the GPU")
+    strides = t.stride()
+    if strides[-1] != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name}: the last dimension is not contiguous")
     if like is None:
         if t.dtype not in _TYPES:
             raise TypeError(f"{name} is {t.dtype}: bfloat16, float16 or float32")
-    else:
-        if t.dtype != like.dtype:
-            raise TypeError(f"{name} is {t.dtype}, not {like.dtype}")
-        _refuse(t.device == like.device, f"{name} is on {t.device}, not {like.device}")
+    elif t.dtype != like.dtype:
+        raise TypeError(f"{name} is {t.dtype}, not {like.dtype}")
+    elif t.get_device() != like.get_device():
+        raise ValueError(f"{name} is on {t.device}, not {like.device}")
+    return strides
 
 
 def _index(t, name, dims, like, types=(torch.int32,)):
+    """t is a tensor of whole numbers beside `like`; returns its strides."""
     if not isinstance(t, torch.Tensor) or t.dtype not in types:
         raise TypeError(f"{name} is a tensor of {' or '.join(str(x) for x in types)}")
-    _refuse(t.dim() == dims, f"{name} has {t.dim()} dimensions, not {dims}")
-    _refuse(t.device == like.device, f"{name} is on {t.device}, not {like.device}")
+    if t.dim() != dims:
+        raise ValueError(f"{name} has {t.dim()} dimensions, not {dims}")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not {like.device}")
+    return t.stride()
 
 
 def _table(table, like, D):
+    """Positions, rotated values and row stride of a rotary table."""
     if not isinstance(table, torch.Tensor) or table.dtype != torch.float32:
         raise TypeError("table is a float32 tensor (rotary_table)")
-    _refuse(table.dim() == 2 and table.device == like.device and (table.stride(1) == 1 or table.shape[1] <= 1),
-            f"table is [positions, rotated values] on {like.device}, its rows contiguous")
-    _refuse(0 < table.shape[1] <= D, f"table turns {table.shape[1]} values of a head of {D}")
+    if table.dim() != 2 or table.device != like.device:
+        raise ValueError(f"table is [positions, rotated values] on {like.device}")
+    (n, rot), (row, one) = table.shape, table.stride()
+    if one != 1 and rot > 1:
+        raise ValueError("table: its rows are not contiguous")
+    if not 0 < rot <= D:
+        raise ValueError(f"table turns {rot} values of a head of {D}")
+    return n, rot, row
 
 
 class _On:
@@ -142,45 +167,59 @@ class _On:
     is enqueued, with the device of the tensors current."""
 
     def __init__(self, stream, like, tensors):
-        self.guard = None
-        device = like.device
-        if stream is None:
-            self.stream = torch.cuda.current_stream(device)
-            if device.index != torch.cuda.current_device():
-                self.guard = torch.cuda.device(device)
-        else:
-            _refuse(stream.device == device, f"stream is on {stream.device}, the tensors on {device}")
-            self.stream = stream
-            self.guard = torch.cuda.stream(stream)  # also makes its device current
-            if stream != torch.cuda.current_stream(device):
-                for t in tensors:
-                    if t is not None:
-                        t.record_stream(stream)
+        _refuse(stream is None or stream.device == like.device, f"stream is not on {like.device}")
+        self.like, self.stream, self.tensors = like, stream, tensors
+        self.guard = torch.cuda.device(like.device) if stream is None else torch.cuda.stream(stream)
 
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream.cuda_stream
+        if self.stream is not None and self.stream != torch.cuda.current_stream(self.like.device):
+            for t in self.tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+        self.guard.__enter__()
+        return torch.cuda.current_stream(self.like.device).cuda_stream
 
     def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        self.guard.__exit__(*exc)
+
+
+class _Here:
+    """The same for a call on the current stream of the current device."""
+
+    def __init__(self, device):
+        self.device = device
+
+    def __enter__(self):
+        return torch._C._cuda_getCurrentRawStream(self.device)
+
+    def __exit__(self, *exc):
+        pass
+
+
+def _on(stream, like, *tensors):
+    device = like.get_device()
+    if stream is None and device == torch._C._cuda_getDevice():
+        return _Here(device)
+    return _On(stream, like, tensors)
 
 
 def _call(name, args, stream):
-    rc = getattr(lib(), name)(ctypes.byref(args), stream)
+    if _bound is None or _bound is not api._lib:
+        lib()
+    rc = _calls[name](args, stream)
     if rc != api.GTS_OK:
         raise api.GtsError(rc, name, api.lib().gts_last_error().decode())
 
 
 def _ptr(t):
-    return None if t is None else t.data_ptr()
+    return 0 if t is None else t.data_ptr()
 
 
-def _disjoint(t, name):
+def _disjoint(strides, shape, name):
     """An output whose elements overlap (an expanded view) would be written
     from several places."""
-    _refuse(all(s != 0 or n <= 1 for s, n in zip(t.stride(), t.shape)), f"{name} is an expanded view")
+    if 0 in strides and any(s == 0 and n > 1 for s, n in zip(strides, shape)):
+        raise ValueError(f"{name} is an expanded view")
 
 
 # ---- rotary ---------------------------------------------------------------------
@@ -236,7 +275,7 @@ def rotary_table(n_positions, dim, *, base=10000.0, scaling=None, device="cuda",
     _refuse(n_positions > 0, f"table of {n_positions} positions")
     like = torch.empty(0, device=device)
     _refuse(like.is_cuda, "the table lives on the GPU")
-    with _On(stream, like, ()) as s:
+    with _on(stream, like) as s:
         table = torch.empty((n_positions, dim), dtype=torch.float32, device=like.device)
         rc = lib().gts_rotary_table(table.data_ptr(), n_positions, dim, (ctypes.c_double * len(f))(*f), mscale, s)
     if rc != api.GTS_OK:
@@ -245,29 +284,30 @@ def rotary_table(n_positions, dim, *, base=10000.0, scaling=None, device="cuda",
 
 
 def _rotary(x, positions, table, flags, out, stream):
-    _refuse(isinstance(x, torch.Tensor) and x.dim() in (3, 4), "x is [tokens, heads, dim] or [batch, tokens, heads, dim]")
-    _data(x, "x", x.dim())
-    B, S, H, D = (1, *x.shape) if x.dim() == 3 else x.shape
-    _table(table, x, D)
-    _index(positions, "positions", positions.dim() if isinstance(positions, torch.Tensor) else 0, x,
-           (torch.int64, torch.int32))
-    shared = positions.dim() == 1
-    _refuse(positions.shape == ((S,) if shared else (B, S)) and (shared or x.dim() == 4),
-            f"positions {tuple(positions.shape)} for {B} x {S} tokens: [tokens] or [batch, tokens]")
+    dims = x.dim() if isinstance(x, torch.Tensor) else 0
+    if dims != 3 and dims != 4:
+        raise ValueError("x is a tensor [tokens, heads, dim] or [batch, tokens, heads, dim]")
+    xs = _data(x, "x", dims)
+    shape = x.shape
+    B, S, H, D = (1, *shape) if dims == 3 else shape
+    n_pos, rot, row = _table(table, x, D)
+    pdims = positions.dim() if isinstance(positions, torch.Tensor) else 0
+    ps = _index(positions, "positions", pdims, x, (torch.int64, torch.int32))
+    if not (pdims == 1 and positions.shape[0] == S or pdims == 2 and dims == 4 and positions.shape == (B, S)):
+        raise ValueError(f"positions {tuple(positions.shape)} for {B} x {S} tokens: [tokens] or [batch, tokens]")
     if out is not None:
-        _data(out, "out", x.dim(), x)
-        _refuse(out.shape == x.shape, f"out is {tuple(out.shape)}, not {tuple(x.shape)}")
-        _disjoint(out, "out")
-    with _On(stream, x, (x, positions, table, out)) as s:
+        _disjoint(_data(out, "out", dims, x), out.shape, "out")
+        _refuse(out.shape == shape, f"out is {tuple(out.shape)}, not {tuple(shape)}")
+    with _on(stream, x, x, positions, table, out) as s:
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        xs, os, ps = x.stride(), out.stride(), positions.stride()
-        if x.dim() == 3:
+            out = x.new_empty(shape)
+        os = out.stride()
+        if dims == 3:
             xs, os = (0, *xs), (0, *os)
-        args = _RotaryArgs(x.data_ptr(), out.data_ptr(), positions.data_ptr(), table.data_ptr(), xs[:3], os[:3],
-                           (0, ps[0]) if shared else ps, table.stride(0), B, S, H, D, table.shape[1], table.shape[0],
-                           _TYPES[x.dtype], positions.element_size(), flags, 0)
-        _call("gts_rotary", args, s)
+        _call("gts_rotary", _pack_rotary(
+            x.data_ptr(), out.data_ptr(), positions.data_ptr(), table.data_ptr(), xs[0], xs[1], xs[2], os[0], os[1], os[2],
+            0 if pdims == 1 else ps[0], ps[-1], row, B, S, H, D, rot, n_pos, _TYPES[x.dtype],
+            8 if positions.dtype == torch.int64 else 4, flags, 0), s)
     return out
 
 
@@ -307,29 +347,33 @@ def rotary_backward(dy, positions, table, *, interleaved=False, out=None, stream
 
 # ---- paged cache ------------------------------------------------------------------
 
-def _cache(k_cache, v_cache, like):
-    _data(k_cache, "k_cache", 4, like)
-    _data(v_cache, "v_cache", 4, like)
-    _refuse(k_cache.shape == v_cache.shape,
-            f"k_cache {tuple(k_cache.shape)} and v_cache {tuple(v_cache.shape)} differ in shape")
-    pages, page, heads, dim = k_cache.shape
-    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), k_cache.stride()[:3], v_cache.stride()[:3], pages, page,
-                  heads, dim, _TYPES[k_cache.dtype], 0)
-
-
-def _batch(T, page_table, lens, starts, prefix_len, like):
-    _index(page_table, "page_table", 2, like)
-    _index(lens, "lens", 1, like)
-    B = lens.shape[0]
-    _refuse(page_table.shape[0] == B and (page_table.stride(1) == 1 or page_table.shape[1] <= 1),
-            f"page_table is [{B}, pages], its rows contiguous: got {tuple(page_table.shape)}")
-    _refuse(lens.stride(0) == 1 or B <= 1, "lens is not contiguous")
+def _cache_batch(k_cache, v_cache, T, page_table, lens, starts, prefix_len, like, written):
+    """The packed values of gts_kv_cache and gts_kv_batch; the cache's heads and
+    dim, and the number of sequences."""
+    ks, vs = _data(k_cache, "k_cache", 4, like), _data(v_cache, "v_cache", 4, like)
+    shape = k_cache.shape
+    if v_cache.shape != shape:
+        raise ValueError(f"k_cache {tuple(shape)} and v_cache {tuple(v_cache.shape)} differ in shape")
+    if written:
+        _disjoint(ks, shape, "k_cache")
+        _disjoint(vs, shape, "v_cache")
+    pages, page, heads, dim = shape
+    ps = _index(page_table, "page_table", 2, like)
+    ls = _index(lens, "lens", 1, like)
+    B, max_pages = lens.shape[0], page_table.shape[1]
+    if page_table.shape[0] != B or (ps[1] != 1 and max_pages > 1):
+        raise ValueError(f"page_table is [{B}, pages], its rows contiguous: got {tuple(page_table.shape)}")
+    if ls[0] != 1 and B > 1:
+        raise ValueError("lens is not contiguous")
     if starts is not None:
-        _index(starts, "starts", 1, like)
-        _refuse(starts.shape[0] == B + 1 and starts.stride(0) == 1, f"starts is [{B + 1}] and contiguous")
-    _refuse(0 <= prefix_len < 1 << 31, f"prefix of {prefix_len} keys")
-    return _Batch(_ptr(starts), lens.data_ptr(), page_table.data_ptr(), page_table.stride(0), B, T,
-                  page_table.shape[1], prefix_len)
+        ss = _index(starts, "starts", 1, like)
+        if starts.shape[0] != B + 1 or ss[0] != 1:
+            raise ValueError(f"starts is [{B + 1}] and contiguous")
+    if not 0 <= prefix_len < 1 << 31:
+        raise ValueError(f"prefix of {prefix_len} keys")
+    return (k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], pages, page, heads, dim,
+            _TYPES[like.dtype], 0, _ptr(starts), lens.data_ptr(), page_table.data_ptr(), ps[0], B, T, max_pages,
+            prefix_len), heads, dim, B
 
 
 def append_kv(k, v, k_cache, v_cache, page_table, lens, *, starts=None, table=None, interleaved=False, prefix_len=0,
@@ -340,36 +384,32 @@ def append_kv(k, v, k_cache, v_cache, page_table, lens, *, starts=None, table=No
     sequence b becomes its own key lens[b] - n + i, in page
     page_table[b, key // page], at position prefix_len + key.  A page number
     outside the cache writes nothing.  Two tokens must not share a slot."""
-    _data(k, "k", 3)
-    _data(v, "v", 3, k)
+    ks, vs = _data(k, "k", 3), _data(v, "v", 3, k)
     T, Hkv, D = k.shape
-    _refuse(v.shape == k.shape, f"k {tuple(k.shape)} and v {tuple(v.shape)} differ in shape")
-    cache = _cache(k_cache, v_cache, k)
-    _refuse(k_cache.shape[2:] == k.shape[1:],
-            f"caches of {tuple(k_cache.shape[2:])} (heads, dim) for keys of {tuple(k.shape[1:])}")
-    _disjoint(k_cache, "k_cache")
-    _disjoint(v_cache, "v_cache")
-    batch = _batch(T, page_table, lens, starts, prefix_len, k)
-    if table is not None:
-        _table(table, k, D)
+    if v.shape != k.shape:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} differ in shape")
+    packed, heads, dim, _ = _cache_batch(k_cache, v_cache, T, page_table, lens, starts, prefix_len, k, True)
+    if heads != Hkv or dim != D:
+        raise ValueError(f"caches of {heads} heads of {dim} for keys of {Hkv} heads of {D}")
+    n_pos, rot, row = (0, 0, 0) if table is None else _table(table, k, D)
+    Hq, qs, os = 0, (0, 0), (0, 0)
     if q is not None:
-        _data(q, "q", 3, k)
-        _refuse(q.shape[0] == T and q.shape[2] == D, f"q is {tuple(q.shape)}: [{T}, heads, {D}]")
+        qs = _data(q, "q", 3, k)
+        Hq = q.shape[1]
+        if q.shape[0] != T or q.shape[2] != D:
+            raise ValueError(f"q is {tuple(q.shape)}: [{T}, heads, {D}]")
     if q_out is not None:
         _refuse(q is not None, "q_out without q")
-        _data(q_out, "q_out", 3, k)
+        _disjoint(_data(q_out, "q_out", 3, k), q_out.shape, "q_out")
         _refuse(q_out.shape == q.shape, f"q_out is {tuple(q_out.shape)}, not {tuple(q.shape)}")
-        _disjoint(q_out, "q_out")
-    with _On(stream, k, (k, v, k_cache, v_cache, page_table, lens, starts, table, q, q_out)) as s:
-        if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        args = _AppendArgs(cache, batch, k.data_ptr(), v.data_ptr(), _ptr(q), _ptr(q_out), k.stride()[:2],
-                           v.stride()[:2], (0, 0) if q is None else q.stride()[:2],
-                           (0, 0) if q is None else q_out.stride()[:2], _ptr(table),
-                           0 if table is None else table.stride(0), 0 if q is None else q.shape[1],
-                           0 if table is None else table.shape[1], 0 if table is None else table.shape[0],
-                           INTERLEAVED if interleaved else 0)
-        _call("gts_append_kv", args, s)
+    with _on(stream, k, k, v, k_cache, v_cache, page_table, lens, starts, table, q, q_out) as s:
+        if q is not None:
+            if q_out is None:
+                q_out = q.new_empty(q.shape)
+            os = q_out.stride()
+        _call("gts_append_kv", _pack_append(
+            *packed, k.data_ptr(), v.data_ptr(), _ptr(q), _ptr(q_out), ks[0], ks[1], vs[0], vs[1], qs[0], qs[1], os[0], os[1],
+            _ptr(table), row, Hq, rot, n_pos, INTERLEAVED if interleaved else 0), s)
     return q_out
 
 
@@ -401,21 +441,19 @@ def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=Non
     out [T, Hq, D] and lse (float32 [T, Hq], natural logarithm) receive the
     results if given; scratch (uint8, attention_scratch_bytes) is allocated if
     not.  Returns out."""
-    _data(q, "q", 3)
+    qs = _data(q, "q", 3)
     T, Hq, D = q.shape
-    cache = _cache(k_cache, v_cache, q)
-    Hkv = k_cache.shape[2]
-    _refuse(k_cache.shape[3] == D, f"caches of head dim {k_cache.shape[3]} for queries of {D}")
-    batch = _batch(T, page_table, lens, starts, prefix_len, q)
+    packed, heads, dim, B = _cache_batch(k_cache, v_cache, T, page_table, lens, starts, prefix_len, q, False)
+    if dim != D:
+        raise ValueError(f"caches of head dim {dim} for queries of {D}")
     n_prefix = 0
     if prefix_pages is not None:
-        _index(prefix_pages, "prefix_pages", 1, q)
-        _refuse(prefix_pages.stride(0) == 1 or prefix_pages.shape[0] <= 1, "prefix_pages is not contiguous")
+        pps = _index(prefix_pages, "prefix_pages", 1, q)
         n_prefix = prefix_pages.shape[0]
+        _refuse(pps[0] == 1 or n_prefix <= 1, "prefix_pages is not contiguous")
     if out is not None:
-        _data(out, "out", 3, q)
+        _disjoint(_data(out, "out", 3, q), out.shape, "out")
         _refuse(out.shape == q.shape, f"out is {tuple(out.shape)}, not {tuple(q.shape)}")
-        _disjoint(out, "out")
     if lse is not None:
         _refuse(isinstance(lse, torch.Tensor) and lse.dtype == torch.float32 and lse.shape == (T, Hq)
                 and lse.is_contiguous() and lse.device == q.device, f"lse is a contiguous float32 [{T}, {Hq}]")
@@ -423,14 +461,14 @@ def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=Non
         _refuse(isinstance(scratch, torch.Tensor) and scratch.dtype == torch.uint8 and scratch.is_contiguous()
                 and scratch.device == q.device, "scratch is a contiguous uint8 tensor")
         _refuse(scratch.data_ptr() % 16 == 0, "scratch is not aligned to 16 bytes")
-    need = _scratch_bytes(batch.batch, T, Hq, Hkv, D)
-    with _On(stream, q, (q, k_cache, v_cache, page_table, lens, starts, prefix_pages, out, lse, scratch)) as s:
+    need = _scratch_bytes(B, T, Hq, heads, D)
+    with _on(stream, q, q, k_cache, v_cache, page_table, lens, starts, prefix_pages, out, lse, scratch) as s:
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if scratch is None and need:
-            scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
-        args = _AttentionArgs(cache, batch, q.data_ptr(), out.data_ptr(), _ptr(lse), q.stride()[:2], out.stride()[:2],
-                              _ptr(prefix_pages), n_prefix, Hq, D ** -0.5 if scale is None else scale, 0, _ptr(scratch),
-                              0 if scratch is None else scratch.numel())
-        _call("gts_shared_prefix_attention", args, s)
+            out = q.new_empty(q.shape)
+        if scratch is None:
+            scratch = q.new_empty(need, dtype=torch.uint8)
+        os = out.stride()
+        _call("gts_shared_prefix_attention", _pack_attention(
+            *packed, q.data_ptr(), out.data_ptr(), _ptr(lse), qs[0], qs[1], os[0], os[1], _ptr(prefix_pages), n_prefix, Hq,
+            D ** -0.5 if scale is None else scale, 0, scratch.data_ptr(), scratch.numel()), s)
     return out

@@ -239,6 +239,38 @@ def test_append(dtype, Hq, Hkv, D, rot, page, counts, lens, prefix, inter, heads
     close(qo, rq, bq, "q")
 
 
+def test_large_calls_agree_with_small_ones():
+    """From 2^19 units (rotary) and 64 MB (append) on a thread takes two units:
+    the same bits as calls of a part each, tokens that end inside a workgroup."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=BF)  # noqa: E731
+    x, tab = rnd(70001, 1, 128), ops.rotary_table(70001, 96)
+    pos = torch.randperm(70001, generator=g, device="cuda")
+    for inter in (False, True):
+        big = ops.rotary(x, pos, tab, interleaved=inter)
+        parts = [ops.rotary(x[i:i + 30000], pos[i:i + 30000], tab, interleaved=inter) for i in range(0, 70001, 30000)]
+        note(f"large rotary, interleaved {inter}")
+        assert torch.equal(big, torch.cat(parts))
+    T, H, D, page = 17003, 5, 128, 64
+    k, v, q = rnd(T, H, D), rnd(T, H, D), rnd(T, 9, D)
+    counts = [5000, 1, 12002]
+    starts = torch.tensor([0] + counts).cumsum(0).int().cuda()
+    lens = torch.tensor(counts).int().cuda()
+    pages = torch.randperm(3 * 190, generator=g, device="cuda").int().view(3, 190)
+    caches = [[torch.zeros(3 * 190, page, H, D, device="cuda", dtype=BF) for _ in range(2)] for _ in range(2)]
+    a = ops.append_kv(k, v, *caches[0], pages, lens, starts=starts, table=tab, q=q)
+    out = []
+    for b in range(3):
+        i, j = int(starts[b]), int(starts[b + 1])
+        for m in range(i, j, 4000):
+            n = min(m + 4000, j)
+            out.append(ops.append_kv(k[m:n], v[m:n], *caches[1], pages[b:b + 1],
+                                     torch.tensor([n - i], device="cuda", dtype=torch.int32), table=tab, q=q[m:n]))
+    note("large append")
+    assert torch.equal(a, torch.cat(out))
+    assert torch.equal(caches[0][0], caches[1][0]) and torch.equal(caches[0][1], caches[1][1])
+
+
 def test_append_without_rotation_and_bad_pages():
     g = gen(1)
     kc, vc = (x.cuda() for x in cache(g, 4, 4, 2, 8, BF))
@@ -326,6 +358,10 @@ ATTENTION = {
     "chunk of a prompt": (BF, 2, 1, 128, 64, [150], [400], 0),
     "many heads": (BF, 64, 1, 64, 16, None, [33, 90], 40),
     "large head": (BF, 8, 2, 256, 32, [3, 1], [70, 200], 130),
+    "24 rows of a large head": (BF, 8, 1, 256, 32, [3, 1], [70, 200], 130),
+    "prompts of a large head": (HF, 4, 1, 256, 16, [40, 33], [60, 40], 70),
+    "32 rows": (BF, 8, 1, 128, 16, [4, 3], [90, 75], 300),
+    "64 rows": (HF, 16, 2, 128, 16, [3, 2, 4], [90, 75, 64], 100),
     "small head": (HF, 3, 3, 8, 8, [2, 1], [9, 30], 20),
     "head of 16": (BF, 6, 2, 16, 4, None, [3, 50, 5], 33),
     "odd head": (BF, 6, 2, 33, 4, None, [3, 50], 33),

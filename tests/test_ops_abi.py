@@ -47,6 +47,49 @@ def test_structures_match_header(tmp_path):
     assert got == want
 
 
+def test_packed_values_match_structures():
+    """The calls pack the structures' values themselves: the same bytes as the
+    ctypes structures, whose layout is the header's."""
+    import struct
+
+    def same(packer, cls, fields):
+        flat = []
+        for v in fields.values():
+            flat += list(v) if isinstance(v, tuple) else [v]
+        n = 0
+
+        def fill(c):
+            out = {}
+            for f in c._fields_:
+                if issubclass(f[1], ctypes.Structure):
+                    out[f[0]] = f[1](**fill(f[1]))
+                else:
+                    out[f[0]] = fields[(c.__name__, f[0])]
+            return out
+
+        assert packer(*flat) == bytes(cls(**fill(cls))), cls.__name__
+        assert struct.calcsize("=Q") == 8 and n == 0
+
+    def values(*classes):
+        """Distinct values, in the order of the members."""
+        out, k = {}, 1
+        for c in classes:
+            for name, kind in c._fields_:
+                if issubclass(kind, ctypes.Structure):
+                    continue
+                if issubclass(kind, ctypes.Array):
+                    out[(c.__name__, name)] = tuple(range(k, k + kind._length_))
+                    k += kind._length_
+                else:
+                    out[(c.__name__, name)] = 0.5 if kind is ctypes.c_float else k
+                    k += 1
+        return out
+
+    same(ops._pack_rotary, ops._RotaryArgs, values(ops._RotaryArgs))
+    same(ops._pack_append, ops._AppendArgs, values(ops._Cache, ops._Batch, ops._AppendArgs))
+    same(ops._pack_attention, ops._AttentionArgs, values(ops._Cache, ops._Batch, ops._AttentionArgs))
+
+
 def rotary_args(**kw):
     d = dict(x=FAKE, out=FAKE, positions=FAKE, table=FAKE, x_stride=(0, 64, 16), out_stride=(0, 64, 16), pos_stride=(0, 1),
              table_stride=16, batch=1, tokens=2, heads=4, dim=16, rot_dim=16, n_positions=8, dtype=ops.BF16, pos_bytes=8,
