@@ -619,3 +619,28 @@ def test_refusals():
             note(f"refusal {i} was not refused")
     torch.cuda.synchronize()
     assert (kc == 0).all()
+
+
+def test_decode_step_example():
+    """The example's step against the formula, with and without a prefix, and
+    its two times."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import decode_step
+    for prefix in (0, 70):
+        d = decode_step.Decode([90, 130, 201], prefix, q_heads=8, kv_heads=2)
+        us, out = decode_step.measure(d, 3)
+        note(f"example, prefix {prefix}: {us:.1f} us a step")
+        ref = d.step()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref) and us > 0
+        rows = d.table.cpu().double()[prefix + d.lens.cpu().long() - 1]
+        q, _ = R.rotate(d.q.cpu().double(), rows)
+        q16 = ops.rotary(d.q, (prefix + d.lens - 1), d.table).cpu()
+        assert ((q16.double() - q).abs() <= 2 ** -8 * q.abs() + 1e-6).all()
+        want = R.attention(q16, d.k_cache.cpu(), d.v_cache.cpu(), d.pages.cpu(), d.lens.cpu(), None,
+                           None if not prefix else d.prefix_pages.cpu(), prefix)
+        close(out, want[0], want[2], "out")
+    r = decode_step.main(["--batch", "3", "--kv-max", "1024", "--prefix", "128", "--steps", "2"])
+    assert r["simulated"] > 0 and r["out"].isfinite().all()
