@@ -1223,7 +1223,12 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
     if (s.keys) {
       const uint32_t rg = row_groups(s.n * p.group), r = index * p.group + gq, rt = r / (32 * rg);
       uint64_t place = ((const uint64_t*)(scratch + sc.begin))[seq];
-      for (uint32_t i = 0; i < rt; ++i) place += places(own_tiles(p, s, rg, i), rg);
+      if (rt) {  // behind rt segments: 64 at a time (8 x 4096 tokens have 128 a sequence)
+        uint64_t before = 0;
+        for (uint32_t i = lane; i < rt; i += 64) before += places(own_tiles(p, s, rg, i), rg);
+        for (int k = 32; k; k >>= 1) before += __shfl_xor(before, k);
+        place += uni(before);
+      }
       locate(2, place, own_tiles(p, s, rg, rt), rg, (uint64_t)p.pieces * prows + s.first * p.group + r);
     }
   }
@@ -1306,15 +1311,14 @@ __global__ __launch_bounds__(256) void row_kernel(AttnParams p) {
   const uint32_t D = a.cache.dim;
   uint32_t seq = 0, index = 0, count = 0;
   const bool has = find_sequence(a.batch, t, &seq, &index, &count);
-  int64_t own = has ? (int64_t)a.batch.lens[seq] - count + index + 1 : 0;
-  if (own < 0) own = 0;
-  const uint32_t n_prefix = has ? a.batch.prefix_len : 0;
+  const uint32_t own = has ? seen(load_seq(p, seq), index) : 0;
+  const uint32_t n_prefix = has && a.cache.n_pages ? a.batch.prefix_len : 0;
   const T* q = (const T*)a.q + (int64_t)t * a.q_stride[0] + (int64_t)hq * a.q_stride[1];
   for (uint32_t d = lane; d < D; d += 64) s_q[wave][d] = (float)q[d];
   float m = -INFINITY, l = 0.f, o[GTS_OPS_MAX_ATTN / 64] = {};
   const float scale = a.scale * kLog2e;
   for (int part = 0; part < 2; ++part) {
-    const uint32_t n = part ? (uint32_t)own : n_prefix;
+    const uint32_t n = part ? own : n_prefix;
     const pages_t pages = (pages_t)(part ? a.batch.page_table + (int64_t)seq * a.batch.table_stride : a.prefix_pages);
     const uint32_t n_pages = part ? a.batch.max_pages : a.n_prefix_pages;
     for (uint32_t j0 = 0; j0 < n; j0 += 64) {

@@ -313,18 +313,25 @@ def _rotary(x, positions, table, flags, out, stream):
 
 class _Rotary(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, positions, table, interleaved, stream):
+    def forward(ctx, x, positions, table, flags, stream):
         ctx.save_for_backward(positions, table)
-        ctx.interleaved, ctx.stream = interleaved, stream
-        return _rotary(x, positions, table, INTERLEAVED if interleaved else 0, None, stream)
+        ctx.flags = flags
+        return _rotary(x, positions, table, flags, None, stream)
 
     @staticmethod
     def backward(ctx, dy):
         positions, table = ctx.saved_tensors
         if dy.stride(-1) != 1:
             dy = dy.contiguous()
-        dx = _rotary(dy, positions, table, (INTERLEAVED if ctx.interleaved else 0) | BACKWARD, None, None)
-        return dx, None, None, None, None
+        # a linear map: its gradient has one of its own, the map again
+        return _Rotary.apply(dy, positions, table, ctx.flags ^ BACKWARD, None), None, None, None, None
+
+
+def _turn(x, positions, table, flags, out, stream):
+    if isinstance(x, torch.Tensor) and x.requires_grad and torch.is_grad_enabled():
+        _refuse(out is None, "out: x requires a gradient")
+        return _Rotary.apply(x, positions, table, flags, stream)
+    return _rotary(x, positions, table, flags, out, stream)
 
 
 def rotary(x, positions, table, *, interleaved=False, out=None, stream=None):
@@ -332,20 +339,28 @@ def rotary(x, positions, table, *, interleaved=False, out=None, stream=None):
     table.shape[1] values of every head turned by the table's row of the
     token's position (int32 or int64 [tokens] or [batch, tokens]); the values
     behind them copied.  Pairs are (i, i + R / 2), or (2 i, 2 i + 1) when
-    interleaved.  out=x rotates in place.  Differentiable in x (without out).
+    interleaved.  out=x rotates in place.  Differentiable in x, to any order
+    (out is then refused).
     A position outside the table gives NaN."""
-    if out is None and torch.is_grad_enabled() and isinstance(x, torch.Tensor) and x.requires_grad:
-        return _Rotary.apply(x, positions, table, interleaved, stream)
-    return _rotary(x, positions, table, INTERLEAVED if interleaved else 0, out, stream)
+    return _turn(x, positions, table, INTERLEAVED if interleaved else 0, out, stream)
 
 
 def rotary_backward(dy, positions, table, *, interleaved=False, out=None, stream=None):
     """The gradient of rotary's x from that of its result: the transposed
     rotation (scaled as the table is)."""
-    return _rotary(dy, positions, table, (INTERLEAVED if interleaved else 0) | BACKWARD, out, stream)
+    return _turn(dy, positions, table, (INTERLEAVED if interleaved else 0) | BACKWARD, out, stream)
 
 
 # ---- paged cache ------------------------------------------------------------------
+
+def _no_gradient(*tensors):
+    """The cache's operators serve and do not train: an input that wants a
+    gradient would silently get none."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("an input requires a gradient, which this operator has not: use torch.no_grad()")
+
 
 def _cache_batch(k_cache, v_cache, T, page_table, lens, starts, prefix_len, like, written):
     """The packed values of gts_kv_cache and gts_kv_batch; the cache's heads and
@@ -383,7 +398,8 @@ def append_kv(k, v, k_cache, v_cache, page_table, lens, *, starts=None, table=No
     (default: a new tensor), which is returned.  New token i of the n of
     sequence b becomes its own key lens[b] - n + i, in page
     page_table[b, key // page], at position prefix_len + key.  A page number
-    outside the cache writes nothing.  Two tokens must not share a slot."""
+    outside the cache writes nothing.  Two tokens must not share a slot.  Has no
+    gradient."""
     ks, vs = _data(k, "k", 3), _data(v, "v", 3, k)
     T, Hkv, D = k.shape
     if v.shape != k.shape:
@@ -402,6 +418,7 @@ def append_kv(k, v, k_cache, v_cache, page_table, lens, *, starts=None, table=No
         _refuse(q is not None, "q_out without q")
         _disjoint(_data(q_out, "q_out", 3, k), q_out.shape, "q_out")
         _refuse(q_out.shape == q.shape, f"q_out is {tuple(q_out.shape)}, not {tuple(q.shape)}")
+    _no_gradient(k, v, q, k_cache, v_cache)
     with _on(stream, k, k, v, k_cache, v_cache, page_table, lens, starts, table, q, q_out) as s:
         if q is not None:
             if q_out is None:
@@ -440,7 +457,7 @@ def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=Non
 
     out [T, Hq, D] and lse (float32 [T, Hq], natural logarithm) receive the
     results if given; scratch (uint8, attention_scratch_bytes) is allocated if
-    not.  Returns out."""
+    not.  Returns out.  Has no gradient."""
     qs = _data(q, "q", 3)
     T, Hq, D = q.shape
     packed, heads, dim, B = _cache_batch(k_cache, v_cache, T, page_table, lens, starts, prefix_len, q, False)
@@ -461,6 +478,7 @@ def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=Non
         _refuse(isinstance(scratch, torch.Tensor) and scratch.dtype == torch.uint8 and scratch.is_contiguous()
                 and scratch.device == q.device, "scratch is a contiguous uint8 tensor")
         _refuse(scratch.data_ptr() % 16 == 0, "scratch is not aligned to 16 bytes")
+    _no_gradient(q, k_cache, v_cache)
     need = _scratch_bytes(B, T, Hq, heads, D)
     with _on(stream, q, q, k_cache, v_cache, page_table, lens, starts, prefix_pages, out, lse, scratch) as s:
         if out is None:

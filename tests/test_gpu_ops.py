@@ -173,6 +173,43 @@ def test_rotary_gradient(inter):
         assert not ops.rotary(leaf, pos[:1].cuda(), table).requires_grad
 
 
+def test_gradient_of_the_gradient():
+    """d/d(dy) of the gradient is the rotation; out has no gradient."""
+    g = gen(18)
+    table = ops.rotary_table(50, 12)
+    pos = torch.arange(4, device="cuda")
+    x, dy, z = (randn(g, 4, 3, 16).cuda() for _ in range(3))
+    leaf, dleaf = x.clone().requires_grad_(), dy.clone().requires_grad_()
+    (dx,) = torch.autograd.grad(ops.rotary(leaf, pos, table, interleaved=True), leaf, dleaf, create_graph=True)
+    (ddy,) = torch.autograd.grad(dx, dleaf, z)
+    assert torch.equal(ddy, ops.rotary(z, pos, table, interleaved=True))
+    (dx,) = torch.autograd.grad(ops.rotary_backward(dleaf, pos, table), dleaf, z)
+    assert torch.equal(dx, ops.rotary(z, pos, table))
+    for f in (ops.rotary, ops.rotary_backward):
+        with pytest.raises(ValueError, match="gradient"):
+            f(leaf, pos, table, out=torch.empty_like(x))
+        with torch.no_grad():
+            assert torch.equal(f(leaf, pos, table, out=torch.empty_like(x)), f(x, pos, table))
+
+
+def test_serving_operators_refuse_gradients():
+    g = gen(19)
+    kc, vc = (x.cuda() for x in cache(g, 2, 16, 2, 64, BF))
+    q, k, v = (randn(g, 1, h, 64, dtype=BF).cuda() for h in (4, 2, 2))
+    pages, lens = torch.tensor([[1]], device="cuda", dtype=torch.int32), torch.tensor([3], device="cuda", dtype=torch.int32)
+    before = kc.clone(), vc.clone()
+    for at in range(3):
+        x = [t.clone().requires_grad_(i == at) for i, t in enumerate((q, k, v))]
+        with pytest.raises(ValueError, match="gradient"):
+            ops.append_kv(x[1], x[2], kc, vc, pages, lens, q=x[0])
+    with pytest.raises(ValueError, match="gradient"):
+        ops.shared_prefix_attention(q.clone().requires_grad_(), kc, vc, pages, lens)
+    assert torch.equal(kc, before[0]) and torch.equal(vc, before[1])
+    with torch.no_grad():
+        out = ops.shared_prefix_attention(q.clone().requires_grad_(), kc, vc, pages, lens)
+    assert torch.equal(out, ops.shared_prefix_attention(q, kc, vc, pages, lens))
+
+
 # ---- append -----------------------------------------------------------------------
 
 def cache(g, n_pages, page, H, D, dtype, heads_first=False, fill=None):
@@ -426,6 +463,27 @@ def test_attention_missing_pages_and_spare_tokens():
     attention_case(BF, 4, 2, 128, 16, None, [16], 0, drop_pages=((0, 0),))  # its only page
     # tokens of no sequence get zeros
     attention_case(HF, 4, 2, 64, 16, [2, 3], [90, 30], 40, spare_tokens=5)
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (F, 64), (HF, 33)])
+def test_lengths_past_the_pages(dtype, D):
+    """Keys that lens counts but no page can hold do not exist, however many."""
+    g = gen(14)
+    kc, vc = (x.cuda() for x in cache(g, 4, 16, 2, D, dtype))
+    q = randn(g, 3, 4, D, dtype=dtype).cuda()
+    pages = torch.tensor([[1, 3], [2, 0]], device="cuda", dtype=torch.int32)
+    starts = torch.tensor([0, 2, 3], device="cuda", dtype=torch.int32)
+    lens = torch.tensor([34, 32], device="cuda", dtype=torch.int32)  # all see 32 keys
+    ref = ops.shared_prefix_attention(q, kc, vc, pages, lens, starts=starts)
+    far = torch.tensor([2 ** 31 - 1, 1 << 30], device="cuda", dtype=torch.int32)
+    note(f"{far.tolist()} keys in two pages of 16 {dtype} {D}")
+    assert torch.equal(ops.shared_prefix_attention(q, kc, vc, pages, far, starts=starts), ref)
+
+
+def test_attention_one_long_prompt():
+    """2100 tokens of one sequence (33 segments of 128 rows for the first of
+    two heads' groups): the places of segments far down the line."""
+    attention_case(BF, 2, 1, 16, 64, [2100, 1], [2100, 5], 70)
 
 
 def test_attention_long_against_rows_of_parts():
