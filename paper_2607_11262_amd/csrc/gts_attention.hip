@@ -35,6 +35,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr uint32_t kTile = 64;        // keys of a tile
 constexpr uint32_t kMostRows = 128;   // query rows of a segment
 constexpr uint32_t kGroups = 512;     // most workgroups: two a CU
+// Rows from which a wave of the join takes four: 2048 rows take 8.0 us by one, 9.1 by
+// four; 67616 rows 96 and 26.
+constexpr uint32_t kFourRows = 4096;
 
 // Places in the line (of about half a microsecond): a segment's begin and end,
 // and a tile, by the segment's row groups.  Measured with few rows 5 us and 1 us
@@ -103,6 +106,7 @@ __device__ __forceinline__ int32_t key_page(const gts_attention_args& a, pages_t
 
 // ---- the tile kernel -------------------------------------------------------------
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -150,23 +154,22 @@ struct Seq {
   int64_t len;        // own keys by lens
   uint32_t keys;      // of these, those that pages can hold
 };
-__device__ __forceinline__ Seq load_seq(const AttnParams& p, uint32_t b) {
-  const gts_kv_batch& kb = p.a.batch;
+__device__ __forceinline__ Seq make_seq(const AttnParams& p, int32_t s0, int32_t s1, int32_t len) {
+  const bool ok = s0 >= 0 && s1 > s0 && (uint32_t)s1 <= p.a.batch.tokens;
   Seq s;
-  if (kb.starts) {
-    const int32_t s0 = kb.starts[b], s1 = kb.starts[b + 1];
-    const bool ok = s0 >= 0 && s1 > s0 && (uint32_t)s1 <= kb.tokens;
-    s.first = ok ? (uint32_t)s0 : 0;
-    s.n = ok ? (uint32_t)(s1 - s0) : 0;
-  } else {
-    s.n = kb.tokens / kb.batch;
-    s.first = b * s.n;
-  }
-  s.len = kb.lens[b];
-  const uint64_t cap = (uint64_t)kb.max_pages << p.page_shift;
+  s.first = ok ? (uint32_t)s0 : 0;
+  s.n = ok ? (uint32_t)(s1 - s0) : 0;
+  s.len = len;
+  const uint64_t cap = (uint64_t)p.a.batch.max_pages << p.page_shift;
   const int64_t k = s.len < 0 || p.a.cache.n_pages == 0 ? 0 : s.len;
   s.keys = (uint32_t)((uint64_t)k < cap ? (uint64_t)k : cap);
   return s;
+}
+__device__ __forceinline__ Seq load_seq(const AttnParams& p, uint32_t b) {
+  const gts_kv_batch& kb = p.a.batch;
+  const uint32_t n = kb.tokens / kb.batch;
+  return kb.starts ? make_seq(p, kb.starts[b], kb.starts[b + 1], kb.lens[b])
+                   : make_seq(p, (int32_t)(b * n), (int32_t)(b * n + n), kb.lens[b]);
 }
 // Own keys that token i of the sequence sees.
 __device__ __forceinline__ uint32_t seen(const Seq& s, uint32_t i) {
@@ -685,7 +688,6 @@ __device__ __forceinline__ void run_stretch(const AttnParams& p, const Work& w, 
 // while it computes.  (Keys loaded as the matrix instruction takes them, 64
 // bytes of each of 16 rows, without LDS: 7 % slower on 64 ragged sequences.)
 // 16 x 16 tiles, because decode has few rows (query heads of a key-value head).
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ f32x4 mfma16(Vec8<__bf16> a, Vec8<__bf16> b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -1171,13 +1173,50 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   }
 }
 
-// The join: one wavefront a row.  Lane i takes the maximum and sum of partial i,
-// then all lanes add up the partials, two dims each.
-template <typename T>
-__global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
-  const gts_attention_args& a = p.a;
+// The sequence of new token t, the token's number in it and the first of its
+// places; false when no sequence has it.  Up to 63 sequences: one load of each kind
+// whose latencies pass together, instead of one behind the other.
+__device__ __forceinline__ bool find_places(const AttnParams& p, const uint64_t* begin, uint32_t t, Seq* s, uint32_t* index,
+                                            uint64_t* place) {
+  const gts_kv_batch& kb = p.a.batch;
   const uint32_t lane = threadIdx.x & 63u;
-  const uint32_t rows = a.batch.tokens * a.q_heads, row = uni(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (!kb.starts || kb.batch > 63) {
+    uint32_t seq, count;
+    if (!find_sequence(kb, t, &seq, index, &count)) return false;
+    *s = load_seq(p, seq);
+    *place = begin[seq];
+    return true;
+  }
+  const bool in = lane < kb.batch;
+  const int32_t start = lane <= kb.batch ? kb.starts[lane] : 0, len = in ? kb.lens[lane] : 0;
+  const uint64_t first = in ? begin[lane] : 0;
+  const uint64_t m = __ballot(lane == 0 || (lane <= kb.batch && start <= (int32_t)t));
+  const uint32_t seq = 63u - (uint32_t)__builtin_clzll(m);
+  if (seq >= kb.batch) return false;
+  *s = make_seq(p, __builtin_amdgcn_readlane(start, seq), __builtin_amdgcn_readlane(start, seq + 1),
+                __builtin_amdgcn_readlane(len, seq));
+  if (t < s->first || t >= s->first + s->n) return false;
+  *index = t - s->first;
+  *place = (uint64_t)__builtin_amdgcn_readlane((uint32_t)(first >> 32), seq) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((uint32_t)first, seq);
+  return true;
+}
+
+// The join: a wavefront takes ROWS rows, W lanes each.  Lane i of a row takes the
+// maximum and sum of partial i, then all of them add up the partials, four dims
+// each (ND times).  Bound by its chain of loads (place, then statistics and
+// sums together), so with many rows a wave takes four: query heads of one token
+// and key-value head, which have one place.
+template <int N>
+struct Ahead {
+  static constexpr int n = N;
+};
+template <typename T, int ND, int ROWS>
+__global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
+  constexpr uint32_t W = 64 / ROWS;
+  const gts_attention_args& a = p.a;
+  const uint32_t lane = threadIdx.x & 63u, sub = lane / W, li = lane % W;
+  const uint32_t rows = a.batch.tokens * a.q_heads, row = uni((blockIdx.x * 4 + (threadIdx.x >> 6)) * ROWS);
   if (row >= rows) return;
   const uint32_t t = p.by_q_heads.div(row), hq = row - t * a.q_heads;
   const uint32_t head = p.by_group.div(hq), gq = hq - head * p.group, D = a.cache.dim;
@@ -1194,8 +1233,10 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
   // at most one is, when any are dealt out), and the own keys.
   uint32_t count[3] = {0, 0, 0};
   uint64_t at[3] = {0, 0, 0}, step[3] = {prows, p.part_rows, p.part_rows};
-  uint32_t seq, index, n_new;
-  if (find_sequence(a.batch, t, &seq, &index, &n_new)) {
+  Seq s;
+  uint32_t index;
+  uint64_t place;
+  if (find_places(p, (const uint64_t*)(scratch + sc.begin), t, &s, &index, &place)) {
     const uint64_t base = head_partials(prows, cut_rows) * head;
     const uint32_t P = a.cache.n_pages ? a.batch.prefix_len : 0;
     const auto locate = [&](int run, uint64_t place, uint32_t tiles, uint32_t rg, uint64_t x) {
@@ -1219,10 +1260,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
                (uint64_t)j * prows + r);
       }
     }
-    const Seq s = load_seq(p, seq);
     if (s.keys) {
       const uint32_t rg = row_groups(s.n * p.group), r = index * p.group + gq, rt = r / (32 * rg);
-      uint64_t place = ((const uint64_t*)(scratch + sc.begin))[seq];
       if (rt) {  // behind rt segments: 64 at a time (8 x 4096 tokens have 128 a sequence)
         uint64_t before = 0;
         for (uint32_t i = lane; i < rt; i += 64) before += places(own_tiles(p, s, rg, i), rg);
@@ -1232,70 +1271,95 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
       locate(2, place, own_tiles(p, s, rg, rt), rg, (uint64_t)p.pieces * prows + s.first * p.group + r);
     }
   }
+  const uint32_t n01 = count[0] + count[1], n = n01 + count[2];
+  const auto part = [&](uint32_t i) {
+    return i < count[0] ? at[0] + step[0] * i : i < n01 ? at[1] + step[1] * (i - count[0]) : at[2] + step[2] * (i - n01);
+  };
 
   float m = -INFINITY, l = 0.f;
-  float2 o[GTS_OPS_MAX_ATTN / 128] = {};
-  const uint32_t n01 = count[0] + count[1], n = n01 + count[2];
-  for (uint32_t i0 = 0; i0 < n; i0 += 64) {
-    const uint32_t i = i0 + lane;
-    const uint64_t x = i < count[0] ? at[0] + step[0] * i
-                       : i < n01    ? at[1] + step[1] * (i - count[0])
-                                    : at[2] + step[2] * (i - n01);
-    float mi = -INFINITY, li = 0.f;
-    if (i < n) {
-      const float2 v = *(const float2*)(stats + 2 * x);
-      mi = v.x;
-      li = v.y;
+  f32x4 o[ND] = {};
+  for (uint32_t i0 = 0; i0 < n; i0 += W) {
+    const uint32_t here = n - i0 < W ? n - i0 : W;
+    float mi = -INFINITY, sum = 0.f;
+    if (li < here) {
+      const float2 x = *(const float2*)(stats + 2 * (part(i0 + li) + sub));
+      mi = x.x;
+      sum = x.y;
     }
-    float m1 = mi;
-    for (int k = 32; k; k >>= 1) m1 = fmaxf(m1, __shfl_xor(m1, k));
-    m1 = fmaxf(m1, m);
-    const float f = mi == -INFINITY ? 1.f : exp2_(mi - m1), old = m == -INFINITY ? 1.f : exp2_(m - m1);
-    float sum = li * f;
-    for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
-    l = l * old + sum;
-    m = m1;
+    float f = 0.f;  // weight of partial i0 + li
+    const auto weigh = [&] {
+      float m1 = mi;
+      for (int k = W / 2; k; k >>= 1) m1 = fmaxf(m1, __shfl_xor(m1, k));
+      m1 = fmaxf(m1, m);
+      f = mi == -INFINITY ? 1.f : exp2_(mi - m1);
+      const float old = m == -INFINITY ? 1.f : exp2_(m - m1);
+      sum *= f;
+      for (int k = W / 2; k; k >>= 1) sum += __shfl_xor(sum, k);
+      l = l * old + sum;
+      m = m1;
 #pragma unroll
-    for (uint32_t d = 0; d < GTS_OPS_MAX_ATTN / 128; ++d) {
-      o[d].x *= old;
-      o[d].y *= old;
-    }
-    const uint32_t here = n - i0 < 64 ? n - i0 : 64;
-    constexpr int kAhead = 8;  // loads on their way
-    for (uint32_t k0 = 0; k0 < here; k0 += kAhead) {
-      float2 v[kAhead][GTS_OPS_MAX_ATTN / 128];
-      float w[kAhead];
+      for (int d = 0; d < ND; ++d) o[d] *= old;
+    };
+    // A loads of the sums on their way, the first of them before the weights are
+    // known.  Past the end the last once more, left out of the sum: a branch
+    // around a load would make the next one wait for it.
+    const auto add_up = [&](auto ahead) {
+      constexpr int A = decltype(ahead)::n;
+      for (uint32_t k0 = 0; k0 < here; k0 += A) {
+        f32x4 v[A][ND];
 #pragma unroll
-      for (int y = 0; y < kAhead; ++y) {
-        const uint32_t k = k0 + y < here ? k0 + y : here - 1;  // past the end: the last again, weight 0
-        w[y] = k0 + y < here ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), k)) : 0.f;
-        const uint64_t xk = ((uint64_t)__builtin_amdgcn_readlane((uint32_t)(x >> 32), k) << 32) |
-                            __builtin_amdgcn_readlane((uint32_t)x, k);
-        const float* src = sums + xk * D;
+        for (int y = 0; y < A; ++y) {
+          const float* src = sums + (part(i0 + (k0 + y < here ? k0 + y : here - 1)) + sub) * D;
 #pragma unroll
-        for (uint32_t d = 0; d < GTS_OPS_MAX_ATTN / 128; ++d) {
-          const uint32_t c = d * 128 + lane * 2;
-          v[y][d] = c < D ? *(const float2*)(src + c) : make_float2(0.f, 0.f);
+          for (int d = 0; d < ND; ++d) {
+            const uint32_t c = (d * W + li) * 4;
+            v[y][d] = *(const f32x4*)(src + (c < D ? c : 0));
+          }
+        }
+        if (k0 == 0) weigh();
+#pragma unroll
+        for (int y = 0; y < A; ++y) {
+          if (k0 + y >= here) break;
+          const float w = ROWS == 1 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), k0 + y))
+                                    : __shfl(f, (int)(sub * W + k0 + y));
+#pragma unroll
+          for (int d = 0; d < ND; ++d) o[d] += v[y][d] * w;
         }
       }
-#pragma unroll
-      for (int y = 0; y < kAhead; ++y)
-#pragma unroll
-        for (uint32_t d = 0; d < GTS_OPS_MAX_ATTN / 128; ++d)
-          if (k0 + y < here) {
-            o[d].x += v[y][d].x * w[y];
-            o[d].y += v[y][d].y * w[y];
-          }
-    }
+    };
+    if (here <= 2)
+      add_up(Ahead<2>{});
+    else
+      add_up(Ahead<8 / ND>{});
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;  // no key: zeros
-  T* out = (T*)a.out + (int64_t)t * a.out_stride[0] + (int64_t)hq * a.out_stride[1];
+  T* out = (T*)a.out + (int64_t)t * a.out_stride[0] + (int64_t)(hq + sub) * a.out_stride[1];
 #pragma unroll
-  for (uint32_t d = 0; d < GTS_OPS_MAX_ATTN / 128; ++d) {
-    const uint32_t c = d * 128 + lane * 2;
-    if (c < D) *(Pack<T, 2>*)(out + c) = Pack<T, 2>{(T)(o[d].x * inv), (T)(o[d].y * inv)};
+  for (int d = 0; d < ND; ++d) {
+    const uint32_t c = (d * W + li) * 4;
+    if (c >= D) continue;
+    const f32x4 y = o[d] * inv;
+    // rows of the output are aligned to four bytes at least
+    *(Pack<T, 2>*)(out + c) = Pack<T, 2>{(T)y[0], (T)y[1]};
+    *(Pack<T, 2>*)(out + c + 2) = Pack<T, 2>{(T)y[2], (T)y[3]};
   }
-  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  if (a.lse && li == 0) a.lse[row + sub] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+template <typename T>
+void launch_join(const AttnParams& p, hipStream_t stream) {
+  const uint64_t rows = (uint64_t)p.a.batch.tokens * p.a.q_heads;
+  const dim3 one((uint32_t)((rows + 3) / 4)), four((uint32_t)((rows + 15) / 16)), block(256);
+  if (p.group % 4 == 0 && rows >= kFourRows) {
+    if (p.a.cache.dim <= 64)
+      join_kernel<T, 1, 4><<<four, block, 0, stream>>>(p);
+    else if (p.a.cache.dim <= 128)
+      join_kernel<T, 2, 4><<<four, block, 0, stream>>>(p);
+    else
+      join_kernel<T, 4, 4><<<four, block, 0, stream>>>(p);
+  } else {
+    join_kernel<T, 1, 1><<<one, block, 0, stream>>>(p);
+  }
 }
 
 // ---- the row kernel --------------------------------------------------------------
@@ -1431,7 +1495,7 @@ static hipError_t launch_typed(AttnParams& p, hipStream_t stream) {
         tile_kernel<T, 128><<<wgs, block, 0, stream>>>(p);
       else
         tile_kernel<T, 256><<<wgs, block, 0, stream>>>(p);
-      join_kernel<T><<<grid, block, 0, stream>>>(p);
+      launch_join<T>(p, stream);
       return hipGetLastError();
     }
   }
