@@ -18,8 +18,14 @@
 // equal pieces, one for each workgroup: they then walk the same keys at the same
 // time, and all but the first of an XCD find them in its L2.  (All of it in the
 // line: 8 TB/s from behind the L2s, twice the time.)
-// A stretch leaves one partial result per segment of which it has tiles (unnormalised sum, running maximum and sum of the
-// softmax, 32 bits), and the join adds up the partials of each row.
+// A stretch leaves one partial result per segment of which it has tiles
+// (unnormalised sum, running maximum and sum of the softmax, 32 bits), and the join
+// adds up the partials of each row.
+// Measured (tile kernel and join, back to back, heads 32 / 8 of 128 in bfloat16): 64
+// ragged decodes of 601491 keys 396 us (6.2 TB/s, bound by the loads), 2113 prompt tokens
+// behind 32768 shared keys 1333 us (855 TFLOP/s, bound by the issue of matrix
+// instructions and exponentials), 64 decodes behind 8192 shared keys 49 us and one of 512
+// keys 15 us (bound by chains of loads at a stretch's begin and end).
 //
 // The row kernel: one wavefront per (token, query head) walks the row's keys 64
 // at a time, one key a lane, with the running maximum and sum of the softmax;
