@@ -421,6 +421,27 @@ def test_attention(name):
     attention_case(*ATTENTION[name], heads_first="heads first" in name)
 
 
+FOUR_ROWS = [(HF, 64, 1100), (BF, 128, 2600), (HF, 256, 1300), (BF, 24, 700)]
+
+
+@pytest.mark.parametrize("dtype,D,prefix", FOUR_ROWS)
+def test_attention_of_4096_rows(dtype, D, prefix):
+    """The join by four rows a wave: every width of head, more partial results of a
+    row than lanes, rows without a key."""
+    note(f"4096 rows of {D}, prefix {prefix}")
+    attention_case(dtype, 64, 1, D, 16, None, [(i * 13) % 70 for i in range(64)], prefix)
+    attention_case(dtype, 64, 16, D, 16, [30, 0, 4, 30], [20, 0, 9, 45], 0, seed=1)
+
+
+@pytest.mark.parametrize("B", [1, 62, 63, 64, 65])
+def test_attention_numbers_of_sequences(B):
+    """Up to 63 sequences' bounds are looked up in one load; some are empty, and
+    the last tokens are no one's."""
+    counts = [(i * 7 + 1) % 4 for i in range(B)]
+    note(f"{B} sequences")
+    attention_case(BF, 4, 2, 64, 16, counts, [c + (i * 5) % 40 for i, c in enumerate(counts)], 20, spare_tokens=2)
+
+
 def test_attention_masked_values():
     """What is masked never reaches a result, whatever it holds."""
     for fill in (float("inf"), float("-inf"), float("nan"), torch.finfo(BF).min):
