@@ -260,7 +260,7 @@ def rotary_frequencies(dim, *, base=10000.0, scaling=None):
         _refuse(fast > slow > 0, "scaling 'ramp': fast > slow > 0")
         # the (fractional) number of the pair that turns `turns` times in n positions
         pair = lambda turns: dim * math.log(n / (turns * 2 * math.pi)) / (2 * math.log(base))  # noqa: E731
-        lo, hi = max(math.floor(pair(fast)), 0), min(math.ceil(pair(slow)), half - 1)
+        lo, hi = max(math.floor(pair(fast)), 0), min(math.ceil(pair(slow)), dim - 1)  # hi may lie behind the last pair
         keep = [1.0 - min(max((i - lo) / max(hi - lo, 1e-3), 0.0), 1.0) for i in range(half)]
         f = [x * k + x / factor * (1.0 - k) for x, k in zip(f, keep)]
         mscale = 0.1 * math.log(factor) + 1.0

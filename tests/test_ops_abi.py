@@ -205,3 +205,22 @@ def test_frequencies():
         if t < 0.9:
             assert math.isclose(y, x / 8)
     assert sorted(g, reverse=True) == g
+
+
+@pytest.mark.parametrize("dim,original,factor", [(128, 4096, 8), (128, 32768, 4), (128, 65536, 4), (128, 131072, 4),
+                                                 (64, 131072, 4), (16, 1 << 20, 2)])
+def test_ramp_frequencies(dim, original, factor):
+    """Every pair of the ramp, its end behind the last pair where that still
+    turns more than once in the original positions."""
+    base = 10000.0
+    f, _ = ops.rotary_frequencies(dim)
+    g, _ = ops.rotary_frequencies(dim, scaling={"kind": "ramp", "factor": factor, "original": original})
+    # the number of the pair whose angle turns n times: original base^(-2 i / dim) = 2 pi n
+    number = lambda n: dim / 2 * math.log(original / (2 * math.pi * n), base)  # noqa: E731
+    lo, hi = max(math.floor(number(32)), 0), math.ceil(number(1))
+    assert hi < dim
+    for i, (x, y) in enumerate(zip(f, g)):
+        t = min(max((i - lo) / (hi - lo), 0.0), 1.0)
+        assert math.isclose(y, x * (1 - t) + x / factor * t, rel_tol=1e-12), i
+        if original * x / (2 * math.pi) > 1.001 and i < hi:
+            assert y > x / factor * (1 + 1e-9), i  # turns more than once: not divided in full
