@@ -33,6 +33,8 @@ extern "C" {
 /* ---- rotation flags ------------------------------------------------------ */
 #define GTS_ROTARY_INTERLEAVED 1u /* pairs (2i, 2i + 1); else (i, i + rot_dim / 2) */
 #define GTS_ROTARY_BACKWARD    2u /* the gradient: the transposed rotation         */
+/* ---- append flags (beside GTS_ROTARY_INTERLEAVED) ------------------------ */
+#define GTS_APPEND_ZERO_REST   4u /* q_out of tokens without a place: zeros        */
 
 /* ---- limits -------------------------------------------------------------- */
 #define GTS_OPS_MAX_DIM  512u     /* head dim of a rotation or an append     */
@@ -94,8 +96,9 @@ typedef struct gts_kv_batch {
 
 /* Writes the new tokens' keys (rotated, with a table) and values into the
  * cache; with q, also writes q rotated to q_out (which may be q).  A
- * token outside every sequence, or whose own index is negative, writes
- * nothing.  Two tokens of one call must not name the same slot. */
+ * token outside every sequence, or whose own index is negative, has no place:
+ * it writes nothing, or with GTS_APPEND_ZERO_REST zeros to its rows of q_out.
+ * Two tokens of one call must not name the same slot. */
 typedef struct gts_append_args {
   gts_kv_cache cache;
   gts_kv_batch batch;

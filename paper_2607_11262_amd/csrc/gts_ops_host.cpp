@@ -113,9 +113,10 @@ int gts_append_kv(const gts_append_args* a, void* hip_stream) {
   if (int rc = check_cache(a->cache)) return rc;
   if (int rc = check_dim(a->cache.dim)) return rc;
   if (int rc = check_batch(a->batch)) return rc;
-  if (a->flags & ~GTS_ROTARY_INTERLEAVED) return refuse(GTS_E_ARG, "unknown flag bits 0x%x", a->flags);
+  constexpr uint32_t known = GTS_ROTARY_INTERLEAVED | GTS_APPEND_ZERO_REST;
+  if (a->flags & ~known) return refuse(GTS_E_ARG, "unknown flag bits 0x%x", a->flags & ~known);
   if (a->table)
-    if (int rc = check_rotation(a->rot_dim, a->cache.dim, a->n_positions, a->flags, GTS_ROTARY_INTERLEAVED)) return rc;
+    if (int rc = check_rotation(a->rot_dim, a->cache.dim, a->n_positions, a->flags, known)) return rc;
   if (a->q && (a->q_heads == 0 || a->q_heads > kMaxHeads)) return refuse(GTS_E_RANGE, "%u query heads", a->q_heads);
   if (a->batch.tokens == 0) return GTS_OK;
   if (!a->k || !a->v) return refuse(GTS_E_ARG, "k or v is NULL");

@@ -207,10 +207,15 @@ __global__ __launch_bounds__(256) void append_kernel(AppendParams p) {
       x = (const T*)(isv ? a.v : a.k) + (int64_t)t * xs[0] + (int64_t)h * xs[1];
       o[k] = (T*)(isv ? a.cache.v : a.cache.k) + page * os[0] + (int64_t)s_slot[tl] * os[1] + (int64_t)h * os[2];
     } else {
-      if (pos[k] < 0) continue;
+      if (pos[k] < 0 && !(a.flags & GTS_APPEND_ZERO_REST)) continue;
       const uint32_t h = head - 2 * hkv;
       x = (const T*)a.q + (int64_t)t * a.q_stride[0] + (int64_t)h * a.q_stride[1];
       o[k] = (T*)a.q_out + (int64_t)t * a.q_out_stride[0] + (int64_t)h * a.q_out_stride[1];
+      if (pos[k] < 0) {
+        rotated[k] = false;
+        v[k] = U{};
+        continue;
+      }
     }
 #pragma unroll
     for (int y = 0; y < U::N; ++y) v[k].x[y] = load<BIG, T, U::W>(x + U::at(y, u, rotated[k], a.rot_dim));

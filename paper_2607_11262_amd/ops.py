@@ -40,7 +40,7 @@ import torch
 from . import api
 
 F32, BF16, F16 = 0, 1, 2
-INTERLEAVED, BACKWARD = 1, 2
+INTERLEAVED, BACKWARD, ZERO_REST = 1, 2, 4
 MAX_ATTENTION_DIM = 256  # GTS_OPS_MAX_ATTN
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
@@ -398,7 +398,9 @@ def append_kv(k, v, k_cache, v_cache, page_table, lens, *, starts=None, table=No
     (default: a new tensor), which is returned.  New token i of the n of
     sequence b becomes its own key lens[b] - n + i, in page
     page_table[b, key // page], at position prefix_len + key.  A page number
-    outside the cache writes nothing.  Two tokens must not share a slot.  Has no
+    outside the cache writes nothing.  A token outside every sequence, or with
+    a negative key, writes nothing either; its rows of a new q_out are zeros, of
+    a given one as they were.  Two tokens must not share a slot.  Has no
     gradient."""
     ks, vs = _data(k, "k", 3), _data(v, "v", 3, k)
     T, Hkv, D = k.shape
@@ -408,7 +410,7 @@ def append_kv(k, v, k_cache, v_cache, page_table, lens, *, starts=None, table=No
     if heads != Hkv or dim != D:
         raise ValueError(f"caches of {heads} heads of {dim} for keys of {Hkv} heads of {D}")
     n_pos, rot, row = (0, 0, 0) if table is None else _table(table, k, D)
-    Hq, qs, os = 0, (0, 0), (0, 0)
+    Hq, qs, os, flags = 0, (0, 0), (0, 0), INTERLEAVED if interleaved else 0
     if q is not None:
         qs = _data(q, "q", 3, k)
         Hq = q.shape[1]
@@ -423,10 +425,11 @@ def append_kv(k, v, k_cache, v_cache, page_table, lens, *, starts=None, table=No
         if q is not None:
             if q_out is None:
                 q_out = q.new_empty(q.shape)
+                flags |= ZERO_REST
             os = q_out.stride()
         _call("gts_append_kv", _pack_append(
             *packed, k.data_ptr(), v.data_ptr(), _ptr(q), _ptr(q_out), ks[0], ks[1], vs[0], vs[1], qs[0], qs[1], os[0], os[1],
-            _ptr(table), row, Hq, rot, n_pos, INTERLEAVED if interleaved else 0), s)
+            _ptr(table), row, Hq, rot, n_pos, flags), s)
     return q_out
 
 

@@ -723,3 +723,36 @@ def test_decode_step_example():
         close(out, want[0], want[2], "out")
     r = decode_step.main(["--batch", "3", "--kv-max", "1024", "--prefix", "128", "--steps", "2"])
     assert r["simulated"] > 0 and r["out"].isfinite().all()
+
+
+def test_append_returns_zeros_for_tokens_without_a_place():
+    """Queries of tokens outside every sequence, or with fewer own keys than new
+    tokens, in a result that the call allocates: zeros, whatever the memory
+    held, and so the same attention behind a prefix each time."""
+    g = gen(23)
+    D, page, P, counts, lens, spare = 64, 16, 20, [5, 0, 3], [2, 0, 9], 4
+    kc, vc = (x.cuda() for x in cache(g, 6, page, 2, D, BF))
+    T = sum(counts) + spare
+    k, v, q = (randn(g, T, h, D, dtype=BF).cuda() for h in (2, 2, 4))
+    pages = torch.tensor([[0], [1], [2]], device="cuda", dtype=torch.int32)
+    shared = torch.tensor([3, 4], device="cuda", dtype=torch.int32)
+    starts = torch.tensor([0, 5, 5, 8], device="cuda", dtype=torch.int32)
+    lens_t = torch.tensor(lens, device="cuda", dtype=torch.int32)
+    placed = torch.tensor([False] * 3 + [True] * 5 + [False] * spare, device="cuda")
+    tab = ops.rotary_table(64, D)
+    for inter in (False, True):
+        for table in (tab, None):
+            given = torch.full_like(q, 7.0)
+            ops.append_kv(k, v, kc, vc, pages, lens_t, starts=starts, table=table, interleaved=inter, prefix_len=P, q=q,
+                          q_out=given)
+            outs = []
+            for fill in (float("nan"), 3.0):
+                for _ in range(4):  # blocks of the size of q, to be taken again
+                    torch.full_like(q, fill)
+                got = ops.append_kv(k, v, kc, vc, pages, lens_t, starts=starts, table=table, interleaved=inter,
+                                    prefix_len=P, q=q)
+                assert (got[~placed] == 0).all() and torch.equal(got[placed], given[placed])
+                outs.append(ops.shared_prefix_attention(got, kc, vc, pages, lens_t, starts=starts, prefix_pages=shared,
+                                                        prefix_len=P))
+            assert torch.equal(outs[0], outs[1]) and outs[0].isfinite().all()
+            assert (given[~placed] == 7).all()  # what the caller hands in keeps its rows

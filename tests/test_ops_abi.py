@@ -224,3 +224,14 @@ def test_ramp_frequencies(dim, original, factor):
         assert math.isclose(y, x * (1 - t) + x / factor * t, rel_tol=1e-12), i
         if original * x / (2 * math.pi) > 1.001 and i < hi:
             assert y > x / factor * (1 + 1e-9), i  # turns more than once: not divided in full
+
+
+def test_append_flags():
+    defined = dict(re.findall(r"#define\s+GTS_(\w+)\s+(\d+)u", header()))
+    assert (ops.INTERLEAVED, ops.BACKWARD, ops.ZERO_REST) == tuple(
+        int(defined[x]) for x in ("ROTARY_INTERLEAVED", "ROTARY_BACKWARD", "APPEND_ZERO_REST"))
+    for flags in (0, 1, 4, 5):
+        refused("gts_append_kv", append_args(b=batch(tokens=0), flags=flags), 0)  # nothing to do
+        refused("gts_append_kv", append_args(flags=flags, q=FAKE, q_heads=4), ARG, "q_out")
+    for flags in (2, 8, 6, 1 << 31):
+        refused("gts_append_kv", append_args(flags=flags), ARG, "flag bits")
