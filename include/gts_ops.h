@@ -120,7 +120,9 @@ int gts_append_kv(const gts_append_args *a, void *hip_stream);
  *   out = sum_j w_j v_j,  w = softmax_j(scale * q . k_j),
  *   lse = log sum_j exp(scale * q . k_j).
  * A token without a key, or outside every sequence, has out = 0 and
- * lse = -inf.  lse may be NULL.  The scratch needs no initialisation. */
+ * lse = -inf.  One that has keys, but none whose score is above -inf, is 0 / 0:
+ * out = NaN and lse = -inf.  A score of +inf or NaN makes both NaN.  lse may be
+ * NULL.  The scratch needs no initialisation. */
 typedef struct gts_attention_args {
   gts_kv_cache cache;
   gts_kv_batch batch;

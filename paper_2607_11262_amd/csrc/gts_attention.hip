@@ -1179,6 +1179,26 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void tile_kernel(AttnParams
   }
 }
 
+// Whether a page holds one of keys 0 .. keys - 1.  All 64 lanes, 64 pages a load.
+__device__ __forceinline__ bool any_page(const AttnParams& p, pages_t pages, uint32_t n, uint32_t keys) {
+  for (uint32_t first = 0; (uint64_t)first << p.page_shift < keys; first += 64) {
+    const uint32_t at = first + (threadIdx.x & 63u);
+    const bool in = at < n && (uint64_t)at << p.page_shift < keys;
+    if (__any(in && (uint32_t)pages[at] < p.a.cache.n_pages)) return true;
+  }
+  return false;
+}
+// Whether new token t sees a key: what a row whose weights are all zero is asked.
+// With a key (their scores are all -inf) it is 0 / 0; without one it is zeros.
+__device__ __forceinline__ bool sees_key(const AttnParams& p, uint32_t t) {
+  const gts_kv_batch& kb = p.a.batch;
+  uint32_t seq, index, count;
+  if (!find_sequence(kb, t, &seq, &index, &count)) return false;
+  return any_page(p, (pages_t)p.a.prefix_pages, p.a.n_prefix_pages, kb.prefix_len) ||
+         any_page(p, (pages_t)(kb.page_table + (int64_t)seq * kb.table_stride), kb.max_pages,
+                  seen(load_seq(p, seq), index));
+}
+
 // The sequence of new token t, the token's number in it and the first of its
 // places; false when no sequence has it.  Up to 63 sequences: one load of each kind
 // whose latencies pass together, instead of one behind the other.
@@ -1338,7 +1358,11 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
     else
       add_up(Ahead<8 / ND>{});
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;  // no key: zeros
+  float inv = 1.f / l;
+  if (__any(l == 0.f)) {
+    const float none = sees_key(p, t) ? __builtin_nanf("") : 0.f;
+    if (l == 0.f) inv = none;
+  }
   T* out = (T*)a.out + (int64_t)t * a.out_stride[0] + (int64_t)(hq + sub) * a.out_stride[1];
 #pragma unroll
   for (int d = 0; d < ND; ++d) {
@@ -1428,7 +1452,8 @@ __global__ __launch_bounds__(256) void row_kernel(AttnParams p) {
     }
   }
   for (int i = 32; i; i >>= 1) l += __shfl_xor(l, i);
-  const float inv = l == 0.f ? 0.f : 1.f / l;  // no key: zeros
+  float inv = 1.f / l;
+  if (l == 0.f) inv = sees_key(p, t) ? __builtin_nanf("") : 0.f;  // the same in all lanes
   T* out = (T*)a.out + (int64_t)t * a.out_stride[0] + (int64_t)hq * a.out_stride[1];
 #pragma unroll
   for (uint32_t i = 0; i < GTS_OPS_MAX_ATTN / 64; ++i) {

@@ -456,7 +456,7 @@ def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=Non
     with the new ones).  Query head h reads key-value head h // (Hq / Hkv).
     scale defaults to D ** -0.5.  Without a prefix this is attention over a
     paged cache, one token a sequence or many.  A token without a key gives
-    zeros and a log-sum of -inf.
+    zeros and a log-sum of -inf; one whose keys all score -inf is 0 / 0, NaN.
 
     out [T, Hq, D] and lse (float32 [T, Hq], natural logarithm) receive the
     results if given; scratch (uint8, attention_scratch_bytes) is allocated if

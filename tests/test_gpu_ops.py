@@ -756,3 +756,55 @@ def test_append_returns_zeros_for_tokens_without_a_place():
                                                         prefix_len=P))
             assert torch.equal(outs[0], outs[1]) and outs[0].isfinite().all()
             assert (given[~placed] == 7).all()  # what the caller hands in keeps its rows
+
+
+@pytest.mark.parametrize("dtype,D,group,counts", [
+    (BF, 64, 4, None), (HF, 128, 4, None), (BF, 256, 8, None), (BF, 128, 8, [3, 4, 2, 3]), (BF, 128, 4, [13, 12, 9, 10]),
+    (HF, 256, 4, [13, 12, 9, 10]), (BF, 64, 4, [40, 33, 35, 37]), (HF, 128, 4, [40, 33, 35, 37]), (F, 64, 4, [3, 4, 2, 3]),
+    (HF, 33, 4, None)])
+@pytest.mark.parametrize("prefix", [0, 33, 150])
+def test_attention_scores_of_minus_infinity(dtype, D, group, counts, prefix):
+    """Keys whose score is -inf weigh nothing beside others; a row that has no
+    other keys is 0 / 0, unlike a row without a key, which is zeros."""
+    note(f"-inf scores {dtype} {D} group {group} counts {counts} prefix {prefix}")
+    g = gen(31)
+    page, H = 16, 2
+    lens = [70, 50, 150, 0]
+    n = [1] * 4 if counts is None else counts
+    T = sum(n)
+    n_prefix, n_pages = -(-prefix // page), 40
+    kc, vc = cache(g, n_pages, page, H, D, dtype)
+    q = randn(g, T, group * H, D, dtype=dtype).abs() + 0.1
+    order = torch.randperm(n_pages, generator=g).int()
+    shared = order[:n_prefix]
+    table = torch.full((4, 10), -1, dtype=torch.int32)
+    at = n_prefix
+    for b, m in enumerate(lens):
+        c = -(-m // page)
+        table[b, :c] = order[at:at + c]
+        at += c
+    starts = None if counts is None else torch.tensor([0] + counts).cumsum(0).int()
+    # sequence 0: every key; 1: its first two pages (rows of its first tokens may see
+    # no other); 2: a page in the middle; the prefix: all of it
+    finite = table.clone()
+    finite[0], finite[1, :2], finite[2, 4] = -1, -1, -1
+    for b in range(4):
+        for x in table[b][(finite[b] < 0) & (table[b] >= 0)].tolist():
+            kc[x, :, :, 1] = -float("inf")
+    for x in shared.tolist():
+        kc[x, :, :, 0] = -float("inf")
+    lens_t = torch.tensor(lens).int()
+    # the same without those keys; the rows that have keys
+    want = R.attention(q, kc, vc, finite, lens_t, starts, None, 0)
+    ones = torch.zeros_like(kc), torch.ones_like(vc)
+    has = R.attention(q, *ones, table, lens_t, starts, shared if prefix else None, prefix)[1] > -float("inf")
+    lse = torch.full((T, group * H), 3.0, device="cuda")
+    out = ops.shared_prefix_attention(q.cuda(), kc.cuda(), vc.cuda(), table.cuda(), lens_t.cuda(),
+                                      starts=None if starts is None else starts.cuda(),
+                                      prefix_pages=shared.cuda() if prefix else None, prefix_len=prefix, lse=lse)
+    none = want[1] == -float("inf")
+    assert (none & has).any() and (~none).any() and (has.all() if prefix else not has.all())
+    close(lse, want[1], want[3], "lse")
+    got = out.cpu()
+    assert got[none & has].isnan().all() and (got[none & ~has] == 0).all()
+    close(out[~none.cuda()], want[0][~none], want[2][~none], "out")
