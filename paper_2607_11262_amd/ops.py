@@ -36,6 +36,7 @@ import math
 import struct
 
 import torch
+from torch.autograd import forward_ad
 
 from . import api
 
@@ -215,6 +216,23 @@ def _ptr(t):
     return 0 if t is None else t.data_ptr()
 
 
+def _no_gradient(what, *tensors):
+    """Refuses a tensor that wants a derivative which the operator does not have
+    and would drop without a word: by reverse mode, or a tangent."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{what} requires a gradient, which it does not get here: use torch.no_grad()")
+    _no_tangent(what, *tensors)
+
+
+def _no_tangent(what, *tensors):
+    if forward_ad._current_level >= 0:  # inside forward_ad.dual_level()
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError(f"{what} has a tangent: the operators have no forward-mode derivative")
+
+
 def _disjoint(strides, shape, name):
     """An output whose elements overlap (an expanded view) would be written
     from several places."""
@@ -328,9 +346,15 @@ class _Rotary(torch.autograd.Function):
 
 
 def _turn(x, positions, table, flags, out, stream):
-    if isinstance(x, torch.Tensor) and x.requires_grad and torch.is_grad_enabled():
-        _refuse(out is None, "out: x requires a gradient")
-        return _Rotary.apply(x, positions, table, flags, stream)
+    if isinstance(table, torch.Tensor):
+        _no_gradient("table", table)
+    if isinstance(x, torch.Tensor):
+        _no_tangent("x", x)
+        if x.requires_grad and torch.is_grad_enabled():
+            _refuse(out is None, "out: x requires a gradient")
+            return _Rotary.apply(x, positions, table, flags, stream)
+    if isinstance(out, torch.Tensor):
+        _no_gradient("out", out)
     return _rotary(x, positions, table, flags, out, stream)
 
 
@@ -339,8 +363,10 @@ def rotary(x, positions, table, *, interleaved=False, out=None, stream=None):
     table.shape[1] values of every head turned by the table's row of the
     token's position (int32 or int64 [tokens] or [batch, tokens]); the values
     behind them copied.  Pairs are (i, i + R / 2), or (2 i, 2 i + 1) when
-    interleaved.  out=x rotates in place.  Differentiable in x, to any order
-    (out is then refused).
+    interleaved.  out=x rotates in place (any other overlap of the two mixes
+    rotated values with others).  Differentiable in x by reverse mode, to any
+    order (out is then refused); a table that requires a gradient, an out that
+    does and tangents of forward mode are refused.
     A position outside the table gives NaN."""
     return _turn(x, positions, table, INTERLEAVED if interleaved else 0, out, stream)
 
@@ -352,15 +378,6 @@ def rotary_backward(dy, positions, table, *, interleaved=False, out=None, stream
 
 
 # ---- paged cache ------------------------------------------------------------------
-
-def _no_gradient(*tensors):
-    """The cache's operators serve and do not train: an input that wants a
-    gradient would silently get none."""
-    if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise ValueError("an input requires a gradient, which this operator has not: use torch.no_grad()")
-
 
 def _cache_batch(k_cache, v_cache, T, page_table, lens, starts, prefix_len, like, written):
     """The packed values of gts_kv_cache and gts_kv_batch; the cache's heads and
@@ -420,7 +437,7 @@ def append_kv(k, v, k_cache, v_cache, page_table, lens, *, starts=None, table=No
         _refuse(q is not None, "q_out without q")
         _disjoint(_data(q_out, "q_out", 3, k), q_out.shape, "q_out")
         _refuse(q_out.shape == q.shape, f"q_out is {tuple(q_out.shape)}, not {tuple(q.shape)}")
-    _no_gradient(k, v, q, k_cache, v_cache)
+    _no_gradient("a tensor of the append", k, v, q, k_cache, v_cache, table, q_out)
     with _on(stream, k, k, v, k_cache, v_cache, page_table, lens, starts, table, q, q_out) as s:
         if q is not None:
             if q_out is None:
@@ -481,7 +498,7 @@ def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=Non
         _refuse(isinstance(scratch, torch.Tensor) and scratch.dtype == torch.uint8 and scratch.is_contiguous()
                 and scratch.device == q.device, "scratch is a contiguous uint8 tensor")
         _refuse(scratch.data_ptr() % 16 == 0, "scratch is not aligned to 16 bytes")
-    _no_gradient(q, k_cache, v_cache)
+    _no_gradient("a tensor of the attention", q, k_cache, v_cache, out, lse)
     need = _scratch_bytes(B, T, Hq, heads, D)
     with _on(stream, q, q, k_cache, v_cache, page_table, lens, starts, prefix_pages, out, lse, scratch) as s:
         if out is None:

@@ -808,3 +808,53 @@ def test_attention_scores_of_minus_infinity(dtype, D, group, counts, prefix):
     got = out.cpu()
     assert got[none & has].isnan().all() and (got[none & ~has] == 0).all()
     close(out[~none.cuda()], want[0][~none], want[2][~none], "out")
+
+
+def test_tangents_are_refused():
+    """Forward-mode derivatives, which no operator has, are refused and not
+    dropped."""
+    import torch.autograd.forward_ad as fw
+    g = gen(41)
+    table, pos = ops.rotary_table(50, 64), torch.arange(2, device="cuda")
+    kc, vc = (x.cuda() for x in cache(g, 2, 16, 2, 64, F))
+    q, k, v = (randn(g, 2, h, 64).cuda() for h in (4, 2, 2))
+    pages, lens = torch.tensor([[1]], device="cuda", dtype=torch.int32), torch.tensor([3], device="cuda", dtype=torch.int32)
+    before = kc.clone(), vc.clone()
+    calls = [lambda t: ops.rotary(t(q), pos, table), lambda t: ops.rotary(q, pos, t(table)),
+             lambda t: ops.rotary_backward(t(q), pos, table), lambda t: ops.rotary(q, pos, table, out=t(q.clone())),
+             lambda t: ops.append_kv(t(k), v, kc, vc, pages, lens), lambda t: ops.append_kv(k, t(v), kc, vc, pages, lens),
+             lambda t: ops.append_kv(k, v, t(kc), vc, pages, lens), lambda t: ops.append_kv(k, v, kc, vc, pages, lens, q=t(q)),
+             lambda t: ops.append_kv(k, v, kc, vc, pages, lens, table=t(table)),
+             lambda t: ops.shared_prefix_attention(t(q), kc, vc, pages, lens),
+             lambda t: ops.shared_prefix_attention(q, kc, t(vc), pages, lens),
+             lambda t: ops.shared_prefix_attention(q, kc, vc, pages, lens, out=t(q.clone()))]
+    with fw.dual_level():
+        for i, f in enumerate(calls):
+            with pytest.raises(ValueError, match="tangent"):
+                f(lambda x: fw.make_dual(x, torch.ones_like(x)))
+                note(f"tangent {i} was not refused")
+    assert torch.equal(kc, before[0]) and torch.equal(vc, before[1])
+    with fw.dual_level():  # a level alone is no reason
+        assert torch.equal(ops.rotary(q, pos, table), ops.rotary(q.clone(), pos, table))
+
+
+def test_gradients_that_would_be_lost_are_refused():
+    """A table has no gradient, and neither has what an operator writes to."""
+    g = gen(42)
+    table, pos = ops.rotary_table(50, 64), torch.arange(2, device="cuda")
+    kc, vc = (x.cuda() for x in cache(g, 2, 16, 2, 64, F))
+    q, k, v = (randn(g, 2, h, 64).cuda() for h in (4, 2, 2))
+    pages, lens = torch.tensor([[1]], device="cuda", dtype=torch.int32), torch.tensor([3], device="cuda", dtype=torch.int32)
+    leaf = lambda x: x.clone().requires_grad_()  # noqa: E731
+    calls = [lambda: ops.rotary(q, pos, leaf(table)), lambda: ops.rotary(leaf(q), pos, leaf(table)),
+             lambda: ops.rotary_backward(q, pos, leaf(table)), lambda: ops.rotary(q, pos, table, out=leaf(q)),
+             lambda: ops.append_kv(k, v, kc, vc, pages, lens, table=leaf(table)),
+             lambda: ops.append_kv(k, v, kc, vc, pages, lens, q=q, q_out=leaf(q)),
+             lambda: ops.shared_prefix_attention(q, kc, vc, pages, lens, out=leaf(q)),
+             lambda: ops.shared_prefix_attention(q, kc, vc, pages, lens, lse=leaf(q[..., 0].contiguous()))]
+    for i, f in enumerate(calls):
+        with pytest.raises(ValueError, match="gradient"):
+            f()
+            note(f"gradient {i} was not refused")
+        with torch.no_grad():
+            f()
