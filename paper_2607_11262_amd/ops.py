@@ -26,7 +26,9 @@ api.GtsError for what the library refuses.  Work is enqueued on `stream`
 (default: the current one) and not waited for; outputs and scratch are
 allocated on it, and tensors handed to another stream than the current one are
 kept from reuse until it has run (record_stream).  The caller orders the
-streams.  Every call may be captured into a graph.
+streams.  Every call may be captured into a graph.  For autograd the caller's
+tensors that a call writes (out, q_out, lse, scratch, the caches) are modified in
+place.
 """
 from __future__ import annotations
 
@@ -233,6 +235,14 @@ def _no_tangent(what, *tensors):
                 raise ValueError(f"{what} has a tangent: the operators have no forward-mode derivative")
 
 
+def _wrote(*tensors):
+    """Tells autograd of the caller's tensors that a call has written, so that
+    the backward of an operation that saved one of them earlier raises."""
+    tensors = [t for t in tensors if t is not None]
+    if tensors:
+        torch.autograd.graph.increment_version(tensors)
+
+
 def _disjoint(strides, shape, name):
     """An output whose elements overlap (an expanded view) would be written
     from several places."""
@@ -317,16 +327,16 @@ def _rotary(x, positions, table, flags, out, stream):
         _disjoint(_data(out, "out", dims, x), out.shape, "out")
         _refuse(out.shape == shape, f"out is {tuple(out.shape)}, not {tuple(shape)}")
     with _on(stream, x, x, positions, table, out) as s:
-        if out is None:
-            out = x.new_empty(shape)
-        os = out.stride()
+        y = x.new_empty(shape) if out is None else out
+        ys = y.stride()
         if dims == 3:
-            xs, os = (0, *xs), (0, *os)
+            xs, ys = (0, *xs), (0, *ys)
         _call("gts_rotary", _pack_rotary(
-            x.data_ptr(), out.data_ptr(), positions.data_ptr(), table.data_ptr(), xs[0], xs[1], xs[2], os[0], os[1], os[2],
+            x.data_ptr(), y.data_ptr(), positions.data_ptr(), table.data_ptr(), xs[0], xs[1], xs[2], ys[0], ys[1], ys[2],
             0 if pdims == 1 else ps[0], ps[-1], row, B, S, H, D, rot, n_pos, _TYPES[x.dtype],
             8 if positions.dtype == torch.int64 else 4, flags, 0), s)
-    return out
+    _wrote(out)
+    return y
 
 
 class _Rotary(torch.autograd.Function):
@@ -447,6 +457,7 @@ def append_kv(k, v, k_cache, v_cache, page_table, lens, *, starts=None, table=No
         _call("gts_append_kv", _pack_append(
             *packed, k.data_ptr(), v.data_ptr(), _ptr(q), _ptr(q_out), ks[0], ks[1], vs[0], vs[1], qs[0], qs[1], os[0], os[1],
             _ptr(table), row, Hq, rot, n_pos, flags), s)
+    _wrote(k_cache, v_cache, q_out)
     return q_out
 
 
@@ -500,6 +511,7 @@ def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=Non
         _refuse(scratch.data_ptr() % 16 == 0, "scratch is not aligned to 16 bytes")
     _no_gradient("a tensor of the attention", q, k_cache, v_cache, out, lse)
     need = _scratch_bytes(B, T, Hq, heads, D)
+    written = out, lse, scratch
     with _on(stream, q, q, k_cache, v_cache, page_table, lens, starts, prefix_pages, out, lse, scratch) as s:
         if out is None:
             out = q.new_empty(q.shape)
@@ -509,4 +521,5 @@ def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=Non
         _call("gts_shared_prefix_attention", _pack_attention(
             *packed, q.data_ptr(), out.data_ptr(), _ptr(lse), qs[0], qs[1], os[0], os[1], _ptr(prefix_pages), n_prefix, Hq,
             D ** -0.5 if scale is None else scale, 0, scratch.data_ptr(), scratch.numel()), s)
+    _wrote(*written)
     return out

@@ -858,3 +858,39 @@ def test_gradients_that_would_be_lost_are_refused():
             note(f"gradient {i} was not refused")
         with torch.no_grad():
             f()
+
+
+def test_writes_are_known_to_autograd():
+    """A tensor that an earlier operation saved and one of the operators has
+    since written to is an error in that operation's backward, as with torch's
+    own in-place operations."""
+    g = gen(43)
+    table, pos = ops.rotary_table(50, 64), torch.arange(2, device="cuda")
+    q, k, v = (randn(g, 2, h, 64).cuda() for h in (4, 2, 2))
+    pages, lens = torch.tensor([[1]], device="cuda", dtype=torch.int32), torch.tensor([3], device="cuda", dtype=torch.int32)
+    kc, vc = (x.cuda() for x in cache(g, 2, 16, 2, 64, F))
+    lse, q_out, out = torch.zeros(2, 4, device="cuda"), torch.zeros_like(q), torch.zeros_like(q)
+    scratch = torch.zeros(ops.attention_scratch_bytes(1, 2, 4, 2, 64), device="cuda", dtype=torch.uint8)
+    writes = [(lambda: ops.rotary(q, pos, table, out=q), (q,)),
+              (lambda: ops.rotary_backward(q, pos, table, out=out), (out,)),
+              (lambda: ops.append_kv(k, v, kc, vc, pages, lens, q=q, q_out=q_out), (kc, vc, q_out)),
+              (lambda: ops.shared_prefix_attention(q, kc, vc, pages, lens, out=out, lse=lse), (out, lse)),
+              (lambda: ops.shared_prefix_attention(q, kc, vc, pages, lens, scratch=scratch), (scratch,))]
+    for i, (write, written) in enumerate(writes):
+        note(f"write {i}")
+        others = [x for x in (q, k, v, kc, vc, lse, q_out, out, table, scratch) if not any(x is y for y in written)]
+        versions = [x._version for x in others]
+        for x in written:
+            w = torch.ones((), device="cuda", requires_grad=True)
+            y = w * x.float() if x.dtype == torch.uint8 else w * x
+            before = x._version
+            write()
+            assert x._version > before
+            if x.dtype != torch.uint8:
+                with pytest.raises(RuntimeError, match="inplace"):
+                    y.sum().backward()
+        assert [x._version for x in others] == versions
+    with torch.inference_mode():
+        c = torch.zeros_like(kc), torch.zeros_like(vc)
+        ops.append_kv(k, v, *c, pages, lens)
+        assert ops.rotary(q, pos, table, out=q) is q
