@@ -35,6 +35,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import math
+import operator
 import struct
 
 import torch
@@ -411,6 +412,7 @@ def _cache_batch(k_cache, v_cache, T, page_table, lens, starts, prefix_len, like
         ss = _index(starts, "starts", 1, like)
         if starts.shape[0] != B + 1 or ss[0] != 1:
             raise ValueError(f"starts is [{B + 1}] and contiguous")
+    prefix_len = operator.index(prefix_len)
     if not 0 <= prefix_len < 1 << 31:
         raise ValueError(f"prefix of {prefix_len} keys")
     return (k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], pages, page, heads, dim,
@@ -520,6 +522,6 @@ def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=Non
         os = out.stride()
         _call("gts_shared_prefix_attention", _pack_attention(
             *packed, q.data_ptr(), out.data_ptr(), _ptr(lse), qs[0], qs[1], os[0], os[1], _ptr(prefix_pages), n_prefix, Hq,
-            D ** -0.5 if scale is None else scale, 0, scratch.data_ptr(), scratch.numel()), s)
+            D ** -0.5 if scale is None else _f32(scale).value, 0, scratch.data_ptr(), scratch.numel()), s)
     _wrote(*written)
     return out

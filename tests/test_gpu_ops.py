@@ -894,3 +894,19 @@ def test_writes_are_known_to_autograd():
         c = torch.zeros_like(kc), torch.zeros_like(vc)
         ops.append_kv(k, v, *c, pages, lens)
         assert ops.rotary(q, pos, table, out=q) is q
+
+
+def test_scales_and_prefix_lengths_of_no_call():
+    """Refused with the documented errors, whatever their kind."""
+    kc, vc = (torch.zeros(3, 4, 2, 16, device="cuda", dtype=BF) for _ in range(2))
+    k, q = torch.zeros(2, 2, 16, device="cuda", dtype=BF), torch.zeros(2, 4, 16, device="cuda", dtype=BF)
+    pages, lens = torch.zeros(2, 1, device="cuda", dtype=torch.int32), torch.ones(2, device="cuda", dtype=torch.int32)
+    attend_ = lambda **kw: ops.shared_prefix_attention(q, kc, vc, pages, lens, **kw)  # noqa: E731
+    for kind, f in ((api.GtsError, lambda: attend_(scale=1e39)), (api.GtsError, lambda: attend_(scale=-float("inf"))),
+                    (TypeError, lambda: attend_(scale="1")), (TypeError, lambda: attend_(prefix_len=0.5)),
+                    (ValueError, lambda: attend_(prefix_len=1 << 31)), (ValueError, lambda: attend_(prefix_len=-1 << 40)),
+                    (TypeError, lambda: ops.append_kv(k, k, kc, vc, pages, lens, prefix_len=1.5))):
+        with pytest.raises(kind):
+            f()
+    torch.cuda.synchronize()
+    assert torch.equal(attend_(scale=1), attend_(scale=1.0))
