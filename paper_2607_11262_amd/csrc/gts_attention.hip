@@ -1242,7 +1242,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
   constexpr uint32_t W = 64 / ROWS;
   const gts_attention_args& a = p.a;
   const uint32_t lane = threadIdx.x & 63u, sub = lane / W, li = lane % W;
-  const uint32_t rows = a.batch.tokens * a.q_heads, row = uni((blockIdx.x * 4 + (threadIdx.x >> 6)) * ROWS);
+  const uint32_t rows = a.batch.tokens * a.q_heads, row = uni(((uint32_t)block_number() * 4 + (threadIdx.x >> 6)) * ROWS);
   if (row >= rows) return;
   const uint32_t t = p.by_q_heads.div(row), hq = row - t * a.q_heads;
   const uint32_t head = p.by_group.div(hq), gq = hq - head * p.group, D = a.cache.dim;
@@ -1379,7 +1379,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnParams p) {
 template <typename T>
 void launch_join(const AttnParams& p, hipStream_t stream) {
   const uint64_t rows = (uint64_t)p.a.batch.tokens * p.a.q_heads;
-  const dim3 one((uint32_t)((rows + 3) / 4)), four((uint32_t)((rows + 15) / 16)), block(256);
+  const dim3 one = grid_of((rows + 3) / 4), four = grid_of((rows + 15) / 16), block(256);
   if (p.group % 4 == 0 && rows >= kFourRows) {
     if (p.a.cache.dim <= 64)
       join_kernel<T, 1, 4><<<four, block, 0, stream>>>(p);
@@ -1399,7 +1399,7 @@ __global__ __launch_bounds__(256) void row_kernel(AttnParams p) {
   const gts_attention_args& a = p.a;
   __shared__ float s_q[4][GTS_OPS_MAX_ATTN];
   const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
-  const uint64_t row = (uint64_t)blockIdx.x * 4 + wave;
+  const uint64_t row = block_number() * 4 + wave;
   if (row >= (uint64_t)a.batch.tokens * a.q_heads) return;
   const uint32_t t = (uint32_t)(row / a.q_heads), hq = (uint32_t)(row % a.q_heads), h = hq / p.group;
   const uint32_t D = a.cache.dim;
@@ -1514,7 +1514,7 @@ template <typename T>
 static hipError_t launch_typed(AttnParams& p, hipStream_t stream) {
   const gts_attention_args& a = p.a;
   const uint64_t rows = (uint64_t)a.batch.tokens * a.q_heads;
-  const dim3 grid((uint32_t)((rows + 3) / 4)), block(256);
+  const dim3 grid = grid_of((rows + 3) / 4), block(256);
   if constexpr (sizeof(T) == 2) {
     if (tiles_fit(a)) {
       p.cuts = cuts(a.cache.heads, a.cache.dim);

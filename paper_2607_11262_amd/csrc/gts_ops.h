@@ -22,6 +22,15 @@ hipError_t launch_attention(const gts_attention_args& a, hipStream_t stream);
 uint64_t attention_scratch(uint32_t batch, uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t dim);
 
 #ifdef __HIPCC__
+// A launch has less than 2^32 threads in each dimension: workgroups of 256 past
+// 2^23 go on in further rows of the grid (the last row may pass their number).
+constexpr uint32_t kGridRow = 1u << 23;
+constexpr uint64_t kMostBlocks = (uint64_t)kGridRow * 65535;
+inline dim3 grid_of(uint64_t blocks) {
+  return blocks <= kGridRow ? dim3((uint32_t)blocks) : dim3(kGridRow, (uint32_t)((blocks + kGridRow - 1) / kGridRow));
+}
+__device__ __forceinline__ uint64_t block_number() { return (uint64_t)blockIdx.y * kGridRow + blockIdx.x; }
+
 // n / d for n < 2^31 and 1 <= d < 2^31: one multiplication high and a shift
 // (m = ceil(2^(32 + s) / d) - 2^32 with 2^s >= d; the sum with n keeps the
 // 33rd bit of the multiplier).

@@ -76,13 +76,11 @@ __device__ __forceinline__ void store(T* p, const Pack<T, V>& x) {
     *reinterpret_cast<Pack<T, V>*>(p) = x;
 }
 
-// Units of a call: per token and head, and where a workgroup's 256 R begin.
+// Units of a call: per token and head, and the token and unit of unit `first`.
 struct Units {
   FastDiv per_token, per_head;
   uint64_t all;
-  template <int R>
-  __device__ __forceinline__ void begin(uint32_t* token, uint32_t* unit) const {
-    const uint64_t first = (uint64_t)blockIdx.x * (256 * R);
+  __device__ __forceinline__ void begin(uint64_t first, uint32_t* token, uint32_t* unit) const {
     *token = all < (1ull << 31) ? per_token.div((uint32_t)first) : (uint32_t)(first / per_token.d);
     *unit = (uint32_t)(first - (uint64_t)*token * per_token.d);
   }
@@ -98,9 +96,11 @@ template <typename T, int V, bool INTER, int R>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   typedef Unit<T, V, INTER> U;
   const gts_rotary_args& a = p.a;
-  const uint64_t left = p.units.all - (uint64_t)blockIdx.x * (256 * R);
+  const uint64_t first = block_number() * (256 * R);
+  if (first >= p.units.all) return;
+  const uint64_t left = p.units.all - first;
   uint32_t t0, i0;
-  p.units.begin<R>(&t0, &i0);
+  p.units.begin(first, &t0, &i0);
   U v[R];
   T* o[R] = {};  // NULL: nothing to write
   int64_t pos[R];
@@ -154,9 +154,11 @@ __global__ __launch_bounds__(256) void append_kernel(AppendParams p) {
   __shared__ int64_t s_pos[kTokens];   // position; -1: the token is in no sequence
   __shared__ int32_t s_page[kTokens];  // page; -1: none
   __shared__ uint32_t s_slot[kTokens];
+  const uint64_t first = block_number() * (256 * R);
+  if (first >= p.units.all) return;
+  const uint64_t left = p.units.all - first;
   uint32_t t0, i0;
-  p.units.begin<R>(&t0, &i0);
-  const uint64_t left = p.units.all - (uint64_t)blockIdx.x * (256 * R);
+  p.units.begin(first, &t0, &i0);
   const uint32_t nt = p.units.per_token.div(i0 + (left < 256 * R ? (uint32_t)left : 256 * R) - 1) + 1;
   for (uint32_t k = threadIdx.x >> 6; k < nt; k += 4) {
     uint32_t seq, index, count;
@@ -294,21 +296,21 @@ hipError_t launch_dtype(uint32_t dtype, uint32_t v, uint32_t flags, const P& p, 
 }
 
 // 0: more workgroups than a launch can have.
-uint32_t blocks_of(const Units& u, int r) {
+uint64_t blocks_of(const Units& u, int r) {
   const uint64_t n = (u.all + 256 * r - 1) / (256 * r);
-  return n < (1ull << 31) ? (uint32_t)n : 0;
+  return n <= kMostBlocks ? n : 0;
 }
 
 template <typename T, int V, bool INTER>
 struct RotaryKernel {
   static hipError_t go(const RotaryParams& p, hipStream_t s) {
     const bool two = p.units.all >= (1u << 19);
-    const uint32_t blocks = blocks_of(p.units, two ? 2 : 1);
+    const uint64_t blocks = blocks_of(p.units, two ? 2 : 1);
     if (!blocks) return hipErrorInvalidValue;
     if (two)
-      rotary_kernel<T, V, INTER, 2><<<dim3(blocks), dim3(256), 0, s>>>(p);
+      rotary_kernel<T, V, INTER, 2><<<grid_of(blocks), dim3(256), 0, s>>>(p);
     else
-      rotary_kernel<T, V, INTER, 1><<<dim3(blocks), dim3(256), 0, s>>>(p);
+      rotary_kernel<T, V, INTER, 1><<<grid_of(blocks), dim3(256), 0, s>>>(p);
     return hipGetLastError();
   }
 };
@@ -316,12 +318,12 @@ template <typename T, int V, bool INTER>
 struct AppendKernel {
   static hipError_t go(const AppendParams& p, hipStream_t s) {
     const bool big = p.units.all * (2 * V * sizeof(T)) >= (64ull << 20);
-    const uint32_t blocks = blocks_of(p.units, big ? 2 : 1);
+    const uint64_t blocks = blocks_of(p.units, big ? 2 : 1);
     if (!blocks) return hipErrorInvalidValue;
     if (big)
-      append_kernel<T, V, INTER, true><<<dim3(blocks), dim3(256), 0, s>>>(p);
+      append_kernel<T, V, INTER, true><<<grid_of(blocks), dim3(256), 0, s>>>(p);
     else
-      append_kernel<T, V, INTER, false><<<dim3(blocks), dim3(256), 0, s>>>(p);
+      append_kernel<T, V, INTER, false><<<grid_of(blocks), dim3(256), 0, s>>>(p);
     return hipGetLastError();
   }
 };

@@ -910,3 +910,42 @@ def test_scales_and_prefix_lengths_of_no_call():
             f()
     torch.cuda.synchronize()
     assert torch.equal(attend_(scale=1), attend_(scale=1.0))
+
+
+# ---- launches of 2^32 threads and more -----------------------------------------------
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D", [(F, 64, 8, 2), (HF, 24, 8, 8)])
+def test_attention_of_more_rows_than_a_grid_is_wide(dtype, Hq, Hkv, D):
+    """2^26 rows and a few of 64 threads each: the row kernel, and the join by one
+    row a wave.  All see one key, so that the result is its value."""
+    T = (1 << 26) // Hq + 3
+    note(f"{T} x {Hq} rows {dtype}")
+    g = torch.Generator(device="cuda").manual_seed(71)
+    kc, vc = (torch.randn(2, 4, Hkv, D, generator=g, device="cuda").to(dtype) for _ in range(2))
+    q = torch.randn(T, Hq, D, generator=g, device="cuda", dtype=dtype)
+    pages = torch.full((1, 1), -1, device="cuda", dtype=torch.int32)
+    lens, shared = torch.zeros(1, device="cuda", dtype=torch.int32), torch.ones(1, device="cuda", dtype=torch.int32)
+    lse = torch.full((T, Hq), 7.0, device="cuda")
+    out = ops.shared_prefix_attention(q, kc, vc, pages, lens, prefix_pages=shared, prefix_len=1, lse=lse)
+    v, k = (c[1, 0].repeat_interleave(Hq // Hkv, 0) for c in (vc, kc))
+    assert (out == v).all()
+    for t in range(0, T, 1 << 18):
+        s = (q[t:t + (1 << 18)].float() * k.float()).sum(-1) * D ** -0.5
+        size = (q[t:t + (1 << 18)].float() * k.float()).abs().sum(-1)
+        assert ((lse[t:t + (1 << 18)] - s).abs() <= (D + 10) * R.E * size + 4 * R.E).all()
+
+
+def test_rotary_of_more_units_than_a_grid_is_wide():
+    """2^33 units and a few (34 GB of heads of 2), two a thread: every token as in a
+    small call."""
+    n, H, times = 4096, 8192, 257
+    g = torch.Generator(device="cuda").manual_seed(72)
+    x = torch.randn(1, H, 2, generator=g, device="cuda", dtype=BF)
+    tab = ops.rotary_table(n, 2)
+    pos = torch.randperm(n, generator=g, device="cuda")
+    ref = ops.rotary(x.expand(n, H, 2), pos, tab)
+    note(f"{n * times} tokens of {H} heads of 2")
+    out = torch.empty(times, n, H, 2, device="cuda", dtype=BF)
+    ops.rotary(x.expand(n * times, H, 2), pos.repeat(times), tab, out=out.flatten(0, 1))
+    for i in range(times):
+        assert torch.equal(out[i], ref), i
