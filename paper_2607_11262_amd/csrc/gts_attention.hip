@@ -241,10 +241,15 @@ __device__ const int32_t g_no_page = -1;
 // all lanes).  Nothing waits for it but the wait for all loads before the barrier
 // that hands the tile over: written as the compiler's builtin, it waits for every
 // such load before the next LDS read, whatever that reads, and no tile is on its
-// way while another is worked on.  (M0, the LDS address, has no other use here.)
+// way while another is worked on.  M0, the LDS address, is the compiler's: it gets
+// its value back.
 __device__ __forceinline__ void load_to_lds(const void* from, void* to) {
   const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)to;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
+               : "s"(at), "v"(from)
+               : "memory");
 }
 
 // Loads tiles of keys and values from the cache straight into LDS (no
