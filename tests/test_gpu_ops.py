@@ -949,3 +949,288 @@ def test_rotary_of_more_units_than_a_grid_is_wide():
     ops.rotary(x.expand(n * times, H, 2), pos.repeat(times), tab, out=out.flatten(0, 1))
     for i in range(times):
         assert torch.equal(out[i], ref), i
+
+
+# ---- segments of many rows: the tiles' masks -------------------------------------------
+
+# New tokens of a sequence and query heads of a group: 48 rows (two of the four waves
+# take rows of their own), 80 and 160 (all four, the second in two segments).
+MANY_ROWS = [(12, 4), (20, 4), (20, 8)]
+
+
+@pytest.mark.parametrize("fill", [float("inf"), float("-inf"), float("nan"), torch.finfo(BF).min])
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (HF, 128), (BF, 256), (BF, 96)])
+def test_masked_values_of_many_rows(dtype, D, fill):
+    note(f"masked slots hold {fill}, many rows {dtype} {D}")
+    fill = fill if dtype == BF or fill != torch.finfo(BF).min else torch.finfo(HF).min
+    attention_case(dtype, 8, 2, D, 16, [12, 20, 40], [25, 37, 140], 33, fill=fill)
+    attention_case(dtype, 4, 1, D, 64, [12, 20, 9], [12, 90, 4], 0, fill=fill)
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (HF, 128), (BF, 256), (BF, 96)])
+def test_missing_pages_of_many_rows(dtype, D):
+    note(f"missing pages, many rows {dtype} {D}")
+    drop = ((0, 0), (0, 4), (1, 2), (1, 3), (2, 0))
+    attention_case(dtype, 8, 2, D, 16, [12, 40, 20], [90, 300, 16], 40, drop_pages=drop, seed=5)
+    attention_case(dtype, 8, 2, D, 8, [12, 40, 20], [90, 300, 16], 0, drop_pages=drop, seed=6)
+    attention_case(dtype, 8, 2, D, 64, [12, 40, 20], [90, 300, 20], 0, drop_pages=((0, 1), (1, 0), (1, 4)), seed=7)
+
+
+@pytest.mark.parametrize("rows", [(1, 4), (3, 8)] + MANY_ROWS)
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (HF, 128), (BF, 256), (F, 64)])
+def test_missing_pages_of_the_prefix(dtype, D, rows):
+    """Pages of the prefix outside the cache: the same as a prefix without their
+    keys."""
+    n, G = rows
+    g, page, H, P = gen(51), 16, 2, 300
+    note(f"prefix without pages 0, 7 and 18 {dtype} {D} rows {rows}")
+    kc, vc = (x.cuda() for x in cache(g, 24, page, H, D, dtype))
+    q = randn(g, 2 * n, G * H, D, dtype=dtype)
+    order = torch.randperm(24, generator=g)[:19].int()
+    shared = order.clone()
+    shared[[0, 7, 18]] = torch.tensor([-1, 24, 1 << 30], dtype=torch.int32)
+    own = torch.tensor([[23, 22], [21, 20]], dtype=torch.int32)
+    lens = torch.tensor([0, 20]).int()
+    want = R.attention(q, kc.cpu(), vc.cpu(), own, lens, None, shared, P)
+    lse = torch.zeros(2 * n, G * H, device="cuda")
+    out = ops.shared_prefix_attention(q.cuda(), kc, vc, own.cuda(), lens.cuda(), prefix_pages=shared.cuda(), prefix_len=P,
+                                      lse=lse)
+    close(out, want[0], want[2], "out")
+    close(lse, want[1], want[3], "lse")
+
+
+@pytest.mark.parametrize("at", [0, 37, 70, 75, 79])
+@pytest.mark.parametrize("n,G", [(2, 4), (5, 5)] + MANY_ROWS)
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (HF, 128), (BF, 256), (BF, 96), (F, 64)])
+def test_values_not_finite_behind_some_rows(dtype, D, n, G, at):
+    """One value of one key is not finite: it is in that dim of the rows that see
+    the key, and nowhere else."""
+    g, H, L = gen(52), 2, 80
+    note(f"a value of key {at} of {L}, {n} tokens x {G} heads {dtype} {D}")
+    kc, vc = cache(g, 6, 16, H, D, dtype)
+    q = randn(g, n, G * H, D, dtype=dtype)
+    pages, lens = torch.tensor([[4, 1, 5, 0, 2]], dtype=torch.int32), torch.tensor([L]).int()
+    want = R.attention(q, kc, vc, pages, lens, None)
+    seen = torch.arange(L - n, L) >= at
+    for bad, d in ((float("inf"), 3), (float("-inf"), D - 1), (float("nan"), 8)):
+        v1 = vc.clone()
+        v1[pages[0, at // 16], at % 16, 1, d] = bad  # key-value head 1
+        lse = torch.zeros(n, G * H, device="cuda")
+        out = ops.shared_prefix_attention(q.cuda(), kc.cuda(), v1.cuda(), pages.cuda(), lens.cuda(), lse=lse)
+        close(lse, want[1], want[3], "lse")
+        out = out.cpu()
+        hit = out[seen][:, G:, d]
+        assert (hit.isnan() if bad != bad else hit == bad).all(), f"{bad} in dim {d}"
+        out[:, G:, d][seen] = 0
+        ref = want[0].clone()
+        ref[:, G:, d][seen] = 0
+        close(out, ref, want[2], f"without {bad} in dim {d}")
+
+
+@pytest.mark.parametrize("n,G", MANY_ROWS)
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (HF, 128), (BF, 256)])
+def test_keys_not_finite_behind_some_rows(dtype, D, n, G):
+    g, H, L, at = gen(53), 2, 80, 72
+    note(f"key {at} of {L} holds nothing finite, {n} tokens x {G} heads {dtype} {D}")
+    kc, vc = cache(g, 6, 16, H, D, dtype)
+    q = randn(g, n, G * H, D, dtype=dtype)
+    pages, lens = torch.tensor([[4, 1, 5, 0, 2]], dtype=torch.int32), torch.tensor([L]).int()
+    want = R.attention(q, kc, vc, pages, lens, None)
+    first = at - (L - n)  # the first token that sees it
+    for bad in (float("inf"), float("-inf"), float("nan")):
+        k1, v1 = kc.clone(), vc.clone()
+        k1[pages[0, at // 16], at % 16] = bad
+        v1[pages[0, at // 16], at % 16] = bad
+        out = ops.shared_prefix_attention(q.cuda(), k1.cuda(), v1.cuda(), pages.cuda(), lens.cuda())
+        assert out[first:].isnan().all()
+        close(out[:first], want[0][:first], want[2][:first], f"before {bad}")
+
+
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (HF, 128), (BF, 256)])
+def test_lengths_past_the_pages_of_many_rows(dtype, D):
+    g = gen(54)
+    kc, vc = (x.cuda() for x in cache(g, 8, 16, 2, D, dtype))
+    q = randn(g, 60, 8, D, dtype=dtype).cuda()
+    pages = torch.tensor([[1, 3, 5, 7], [2, 0, 4, 6]], device="cuda", dtype=torch.int32)
+    starts = torch.tensor([0, 40, 60], device="cuda", dtype=torch.int32)
+    lens = torch.tensor([64 + 40, 64 + 20], device="cuda", dtype=torch.int32)  # all see 64 keys
+    ref = ops.shared_prefix_attention(q, kc, vc, pages, lens, starts=starts)
+    far = torch.tensor([2 ** 31 - 1, 1 << 30], device="cuda", dtype=torch.int32)
+    note(f"{far.tolist()} keys in four pages of 16, many rows {dtype} {D}")
+    assert torch.equal(ops.shared_prefix_attention(q, kc, vc, pages, far, starts=starts), ref)
+    want = R.attention(q.cpu(), kc.cpu(), vc.cpu(), pages.cpu(), lens.cpu(), starts.cpu())
+    close(ref, want[0], want[2], "out")
+
+
+@pytest.mark.parametrize("dtype,D,n,G", [(BF, 64, 5, 2), (HF, 128, 30, 4), (F, 64, 4, 2)])
+def test_the_same_number_of_tokens_each(dtype, D, n, G):
+    """starts=None with several tokens a sequence: the same bits as with starts."""
+    g, H, B = gen(55), 2, 3
+    kc, vc = (x.cuda() for x in cache(g, 16, 16, H, D, dtype))
+    k, v, q = (randn(g, B * n, h, D, dtype=dtype).cuda() for h in (H, H, G * H))
+    pages = torch.randperm(16, generator=g)[:15].view(3, 5).int().cuda()
+    lens = torch.tensor([n, n + 40, 77], device="cuda", dtype=torch.int32)
+    starts = torch.arange(B + 1, device="cuda", dtype=torch.int32) * n
+    tab = ops.rotary_table(80, D)
+    got = []
+    for s in (None, starts):
+        k1, v1 = kc.clone(), vc.clone()
+        q1 = ops.append_kv(k, v, k1, v1, pages, lens, starts=s, table=tab, q=q)
+        got.append((k1, v1, q1, ops.shared_prefix_attention(q1, k1, v1, pages, lens, starts=s)))
+    note(f"{B} x {n} tokens {dtype} {D}")
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and not torch.equal(got[0][0], kc)
+    want = R.attention(got[0][2].cpu(), got[0][0].cpu(), got[0][1].cpu(), pages.cpu(), lens.cpu())
+    close(got[0][3], want[0], want[2], "out")
+
+
+# ---- layouts of the paged operators ------------------------------------------------------
+
+def shifted(t, by):
+    """The same values, `by` elements behind a 16-byte boundary, rows `by` further apart."""
+    wide = torch.zeros(*t.shape[:-1], t.shape[-1] + 8, dtype=t.dtype, device="cuda")
+    off = wide[..., by:by + t.shape[-1]]
+    off.copy_(t)
+    return off
+
+
+def odd_rows(t):
+    """The same values in rows an odd number of elements apart."""
+    off = torch.zeros(*t.shape[:-1], t.shape[-1] + 1, dtype=t.dtype, device="cuda")[..., :t.shape[-1]]
+    return off.copy_(t)
+
+
+def paged(g, dtype, D, H, G, page=16, prefix=40, counts=(5, 1, 14), lens=(9, 70, 33)):
+    """Inputs of both operators on the GPU: a packed projection's q, k and v."""
+    T, B = sum(counts), len(counts)
+    n = -(-max(lens) // page)
+    n_prefix = -(-prefix // page)
+    order = torch.randperm(B * n + n_prefix, generator=g).int()
+    packed = randn(g, T, (G + 2) * H, D, dtype=dtype).cuda()
+    q, k, v = packed[:, :G * H], packed[:, G * H:(G + 1) * H], packed[:, (G + 1) * H:]
+    kc, vc = (x.cuda() for x in cache(g, B * n + n_prefix, page, H, D, dtype))
+    return dict(q=q, k=k, v=v, kc=kc, vc=vc, pages=order[n_prefix:].view(B, n).cuda(), shared=order[:n_prefix].cuda(),
+                P=prefix, lens=torch.tensor(lens).int().cuda(),
+                starts=torch.tensor([0, *counts]).cumsum(0).int().cuda(), tab=ops.rotary_table(200, D // 2 * 2))
+
+
+def attend(s, **kw):
+    s = {**s, **kw}
+    return ops.shared_prefix_attention(s["q"], s["kc"], s["vc"], s["pages"], s["lens"], starts=s["starts"],
+                                       prefix_pages=s["shared"], prefix_len=s["P"], out=s.get("out"), lse=s.get("lse"))
+
+
+def append(s, inter=False, **kw):
+    s = {**s, **kw}
+    return ops.append_kv(s["k"], s["v"], s["kc"], s["vc"], s["pages"], s["lens"], starts=s["starts"], table=s["tab"],
+                         interleaved=inter, prefix_len=s["P"], q=s["q"], q_out=s.get("q_out"))
+
+
+@pytest.mark.parametrize("dtype,D,inter", [(BF, 64, False), (HF, 128, True), (BF, 40, False), (F, 64, False), (F, 64, True),
+                                           (F, 512, False)])
+def test_append_layouts(dtype, D, inter):
+    """Every layout of k, v, q, the result and the caches gives the bits of
+    contiguous ones, whose values are those of the formula."""
+    g = gen(61)
+    s = paged(g, dtype, D, 2, 3)
+    dense = {x: s[x].contiguous() for x in "qkv"}
+    kc, vc = s["kc"].clone(), s["vc"].clone()
+    ref = append(s, inter, **dense, kc=kc, vc=vc)
+    rows = s["tab"].cpu().double()
+    at = [(b, j) for b, (n, m) in enumerate(zip((5, 1, 14), (9, 70, 33))) for j in range(m - n, m)]
+    row = rows[[s["P"] + j for _, j in at]]
+    slots = torch.stack([s["pages"].cpu()[b, j // 16] for b, j in at]).long(), torch.tensor([j % 16 for _, j in at])
+    for got, x in ((ref, "q"), (kc.cpu()[slots], "k")):
+        y, size = R.rotate(s[x].cpu().double(), row, inter)
+        close(got, y, R.rotation_bound(y, size, dtype), x)
+    assert torch.equal(vc.cpu()[slots], s["v"].cpu())
+
+    def same(what, **kw):
+        note(f"append {dtype} {D} interleaved {inter}: {what}")
+        k1, v1 = kw.pop("kc", s["kc"].clone()), kw.pop("vc", s["vc"].clone())
+        got = append(s, inter, kc=k1, vc=v1, **kw)
+        assert torch.equal(got, ref) and torch.equal(k1, kc) and torch.equal(v1, vc), what
+
+    same("views of a packed projection")
+    heads_first = lambda x: x.transpose(1, 2).contiguous().transpose(1, 2)  # noqa: E731
+    same("keys head by head", kc=heads_first(s["kc"]))
+    same("values head by head", vc=heads_first(s["vc"]))
+    for by in (1, 2, 4):
+        for x in "qkv":
+            same(f"{x} shifted by {by}", **{x: shifted(s[x], by)})
+        same(f"result shifted by {by}", q_out=shifted(torch.zeros_like(dense["q"]), by))
+        same(f"keys' cache shifted by {by}", kc=shifted(s["kc"], by))
+        same(f"values' cache shifted by {by}", vc=shifted(s["vc"], by))
+    for x in "qkv":
+        same(f"{x} in odd rows", **{x: odd_rows(s[x])})
+    same("result in odd rows", q_out=odd_rows(torch.zeros_like(dense["q"])))
+    same("caches in odd rows", kc=odd_rows(s["kc"]), vc=odd_rows(s["vc"]))
+    # into the packed projection itself: nothing else in it changes
+    whole = torch.cat((s["q"], s["k"], s["v"]), 1)
+    G = s["q"].shape[1]
+    same("in place", q=whole[:, :G], q_out=whole[:, :G], k=whole[:, G:G + 2], v=whole[:, G + 2:])
+    assert torch.equal(whole[:, :G], ref) and torch.equal(whole[:, G:], torch.cat((s["k"], s["v"]), 1))
+
+
+@pytest.mark.parametrize("dtype,D,G", [(BF, 64, 3), (HF, 128, 4), (BF, 256, 4), (HF, 80, 4), (F, 64, 2), (HF, 33, 2)])
+def test_attention_layouts(dtype, D, G):
+    g = gen(62)
+    s = paged(g, dtype, D, 2, G)
+    dense = s["q"].contiguous()
+    want = R.attention(dense.cpu(), s["kc"].cpu(), s["vc"].cpu(), s["pages"].cpu(), s["lens"].cpu(), s["starts"].cpu(),
+                       s["shared"].cpu(), s["P"])
+    ref = attend(s, q=dense)
+    close(ref, want[0], want[2], "out")
+    bits = ref.clone()
+
+    def check(what, same, **kw):
+        """`same`: the kernel that contiguous tensors take, so its bits."""
+        note(f"attention {dtype} {D}: {what}")
+        lse = torch.zeros(dense.shape[:2], device="cuda")
+        got = attend(s, lse=lse, **kw)
+        close(got, want[0], want[2], what)
+        close(lse, want[1], want[3], what)
+        if same:
+            assert torch.equal(got, bits), what
+
+    check("queries of a packed projection", D % 8 == 0)
+    heads_first = lambda x: x.transpose(1, 2).contiguous().transpose(1, 2)  # noqa: E731
+    check("keys head by head", True, kc=heads_first(s["kc"]))
+    check("values head by head", True, vc=heads_first(s["vc"]))
+    check("a result inside a packed tensor", True, out=torch.zeros_like(torch.cat((s["q"], s["k"]), 1))[:, :dense.shape[1]])
+    check("a result two elements off", True, out=shifted(torch.zeros_like(dense), 2))
+    # rows that cannot be loaded 16 bytes at a time, or stored four
+    for by in (1, 2, 4):
+        check(f"queries shifted by {by}", False, q=shifted(s["q"], by))
+        check(f"keys shifted by {by}", False, kc=shifted(s["kc"], by))
+        check(f"values shifted by {by}", False, vc=shifted(s["vc"], by))
+    check("a result one element off", False, out=shifted(torch.zeros_like(dense), 1))
+    check("a result in odd rows", False, out=odd_rows(torch.zeros_like(dense)))
+    check("queries in odd rows", False, q=odd_rows(s["q"]))
+    check("caches in odd rows", False, kc=odd_rows(s["kc"]), vc=odd_rows(s["vc"]))
+    check("caches in rows of 8 more", False, kc=shifted(s["kc"], 0), vc=shifted(s["vc"], 0))
+    buf = torch.zeros(dense.numel() + 8, dtype=dtype, device="cuda")
+    check("the result's neighbours", True, out=buf[4:4 + dense.numel()].view(dense.shape))
+    assert (buf[:4] == 0).all() and (buf[4 + dense.numel():] == 0).all()
+
+
+@pytest.mark.parametrize("counts,lens", [((1, 1, 1), (9, 70, 33)), ((30, 1, 14), (40, 70, 33))])
+def test_slots_far_apart(counts, lens):
+    """Slots of a page 2^26 elements and more apart, so that 16 rows pass 2 GiB:
+    the general way of loading, with pages of 16."""
+    g = gen(63)
+    s = paged(g, BF, 64, 2, 4, counts=counts, lens=lens)
+    ref = attend(s)
+    n, page, H, D = s["kc"].shape
+    slot = (1 << 26) + 8
+    buf = torch.empty((page - 1) * slot + n * H * D, dtype=BF, device="cuda")
+    far = buf.as_strided((n, page, H, D), (H * D, slot, D, 1))
+    for x in ("kc", "vc"):
+        far.copy_(s[x])
+        note(f"{x} with slots {slot} elements apart, {counts} tokens")
+        assert torch.equal(attend(s, **{x: far}), ref)
+    far.zero_()
+    kc, vc = s["kc"].clone(), s["vc"].clone()
+    zero = torch.zeros_like(kc)
+    append(s, kc=far, vc=vc)
+    append(s, kc=zero, vc=s["vc"].clone())
+    assert torch.equal(far, zero) and torch.equal(kc, s["kc"])
