@@ -115,7 +115,6 @@ __device__ __forceinline__ int32_t key_page(const gts_attention_args& a, pages_t
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 template <typename T>
 using Vec8 = T __attribute__((ext_vector_type(8)));

@@ -1,6 +1,6 @@
 // gts_ops.h — what the operators' host checks and kernels share: the launch
-// functions, and the device helpers for 16-byte loads, element types and
-// division by a number known at launch.
+// functions, and the device helpers for 16-byte loads, grids and division by a
+// number known at launch.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -43,21 +43,6 @@ struct FastDiv {
     m = (uint32_t)(((1ull << 32) * ((1ull << s) - div)) / div + 1);
   }
   __device__ __forceinline__ uint32_t div(uint32_t n) const { return (uint32_t)(((uint64_t)__umulhi(n, m) + n) >> s); }
-};
-
-template <uint32_t DT>
-struct Elem;
-template <>
-struct Elem<GTS_F32> {
-  using type = float;
-};
-template <>
-struct Elem<GTS_BF16> {
-  using type = __bf16;
-};
-template <>
-struct Elem<GTS_F16> {
-  using type = _Float16;
 };
 
 // N values of T that are loaded and stored as one access (N * sizeof(T) <= 16

@@ -45,7 +45,6 @@ from . import api
 
 F32, BF16, F16 = 0, 1, 2
 INTERLEAVED, BACKWARD, ZERO_REST = 1, 2, 4
-MAX_ATTENTION_DIM = 256  # GTS_OPS_MAX_ATTN
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 EXPORTS = ("gts_rotary_table", "gts_rotary", "gts_append_kv", "gts_shared_prefix_attention",
