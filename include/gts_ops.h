@@ -14,7 +14,10 @@
  * captured into a graph.  Pointers are device pointers unless a comment says
  * host.  Strides count elements; the last dimension of every tensor is
  * contiguous.  All sums, softmax statistics and rotations are in 32 bits; a
- * result is rounded once, to the type it is stored in.
+ * result is rounded once, to the type it is stored in.  One value more is
+ * rounded: attention over a 16-bit cache whose rows are aligned to 16 bytes
+ * multiplies the values by softmax weights in the cache's type (their sum, and so
+ * lse, keeps them in 32 bits).
  */
 #ifndef GTS_OPS_H
 #define GTS_OPS_H
@@ -115,14 +118,16 @@ int gts_append_kv(const gts_append_args *a, void *hip_stream);
 /* Attention of the new tokens over the cache.  Query head h reads key-value
  * head h / (q_heads / heads).  Token i of a sequence sees every key of the
  * prefix (key j in slot j % page of page prefix_pages[j / page], j <
- * prefix_len, the same for all sequences and read once for all of them) and
- * its own keys 0 .. lens[b] - n + i:
+ * prefix_len, the same for all sequences) and its own keys 0 .. lens[b] - n + i:
  *   out = sum_j w_j v_j,  w = softmax_j(scale * q . k_j),
  *   lse = log sum_j exp(scale * q . k_j).
  * A token without a key, or outside every sequence, has out = 0 and
  * lse = -inf.  One that has keys, but none whose score is above -inf, is 0 / 0:
  * out = NaN and lse = -inf.  A score of +inf or NaN makes both NaN.  lse may be
- * NULL.  The scratch needs no initialisation. */
+ * NULL.  The scratch needs no initialisation.
+ * 16-bit caches whose rows of q, k and v are aligned to 16 bytes, with a dim of
+ * whole 16 bytes and an even out, read the prefix once for all sequences; any
+ * other call reads each key for every query head that sees it. */
 typedef struct gts_attention_args {
   gts_kv_cache cache;
   gts_kv_batch batch;

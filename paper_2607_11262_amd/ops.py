@@ -376,7 +376,7 @@ def rotary(x, positions, table, *, interleaved=False, out=None, stream=None):
     interleaved.  out=x rotates in place (any other overlap of the two mixes
     rotated values with others).  Differentiable in x by reverse mode, to any
     order (out is then refused); a table that requires a gradient, an out that
-    does and tangents of forward mode are refused.
+    does and tangents of forward mode are refused, torch.func's transforms raise.
     A position outside the table gives NaN."""
     return _turn(x, positions, table, INTERLEAVED if interleaved else 0, out, stream)
 
@@ -480,12 +480,16 @@ def attention_scratch_bytes(sequences, tokens, q_heads, kv_heads, dim):
 def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=None, prefix_pages=None, prefix_len=0,
                             scale=None, out=None, lse=None, scratch=None, stream=None):
     """Attention of the new tokens' q [T, Hq, D] over the cache: every token
-    sees the prefix_len keys in prefix_pages (int32 [n], read once for the
-    whole batch) and its sequence's own keys up to its own (lens counts them
-    with the new ones).  Query head h reads key-value head h // (Hq / Hkv).
+    sees the prefix_len keys in prefix_pages (int32 [n]) and its sequence's own
+    keys up to its own (lens counts them with the new ones).  Query head h reads key-value head h // (Hq / Hkv).
     scale defaults to D ** -0.5.  Without a prefix this is attention over a
     paged cache, one token a sequence or many.  A token without a key gives
     zeros and a log-sum of -inf; one whose keys all score -inf is 0 / 0, NaN.
+
+    16-bit caches with rows aligned to 16 bytes have softmax weights rounded to
+    their type for the product with the values, and read the prefix once for the
+    whole batch; 32 bits, odd head dims and unaligned rows take a kernel that
+    reads each key for every query head.
 
     out [T, Hq, D] and lse (float32 [T, Hq], natural logarithm) receive the
     results if given; scratch (uint8, attention_scratch_bytes) is allocated if

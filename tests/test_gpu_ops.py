@@ -1234,3 +1234,16 @@ def test_slots_far_apart(counts, lens):
     append(s, kc=far, vc=vc)
     append(s, kc=zero, vc=s["vc"].clone())
     assert torch.equal(far, zero) and torch.equal(kc, s["kc"])
+
+
+def test_function_transforms_raise():
+    """torch.func's transforms hand over tensors without memory: an error, not a
+    lost derivative."""
+    g = gen(44)
+    table, pos = ops.rotary_table(50, 64), torch.arange(2, device="cuda")
+    q = randn(g, 2, 4, 64).cuda()
+    turn = lambda x: ops.rotary(x, pos, table)  # noqa: E731
+    for f in (lambda: torch.func.grad(lambda x: turn(x).sum())(q), lambda: torch.func.jvp(turn, (q,), (q,)),
+              lambda: torch.func.vmap(turn)(q[None]), lambda: torch.func.jvp(lambda t: ops.rotary(q, pos, t), (table,), (table,))):
+        with pytest.raises((RuntimeError, ValueError)):
+            f()
