@@ -30,7 +30,10 @@ KERNELS = (("gts_sim.hip", (), "gts_sim.o"),
            ("gts_team.hip", (), "gts_team.o"),
            ("gts_noalloc.hip", (), "gts_noalloc.o"),
            ("gts_rotary.hip", (), "gts_rotary.o"),
-           ("gts_attention.hip", (), "gts_attention.o"))
+           ("gts_attention.hip", (), "gts_attention.o"),
+           ("gts_norm.hip", (), "gts_norm.o"),
+           ("gts_linear.hip", (), "gts_linear.o"),
+           ("gts_prompt.hip", (), "gts_prompt.o"))
 HOST = ("gts_host.cpp", "gts_ops_host.cpp")
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include"]
 

@@ -33,12 +33,11 @@
 // the weighted values are summed with a lane per group of dims.  Takes every
 // type, head dim, stride and alignment; every row reads its keys by itself.
 #include "gts_ops.h"
+#include "gts_tile.h"
 
 namespace gts {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr uint32_t kTile = 64;        // keys of a tile
 constexpr uint32_t kMostRows = 128;   // query rows of a segment
 constexpr uint32_t kGroups = 512;     // most workgroups: two a CU
@@ -112,42 +111,6 @@ __device__ __forceinline__ int32_t key_page(const gts_attention_args& a, pages_t
 }
 
 // ---- the tile kernel -------------------------------------------------------------
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-template <typename T>
-using Vec8 = T __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ f32x16 mfma(Vec8<__bf16> a, Vec8<__bf16> b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x16 mfma(Vec8<_Float16> a, Vec8<_Float16> b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-}
-
-__device__ __forceinline__ uint32_t uni(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ uint64_t uni(uint64_t x) {
-  return ((uint64_t)uni((uint32_t)(x >> 32)) << 32) | uni((uint32_t)x);
-}
-__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-// The lane's number as a value of its own: what is computed from it stays where
-// it is used, instead of being kept in registers across the loops around.
-__device__ __forceinline__ uint32_t fresh_lane() {
-  uint32_t lane = threadIdx.x & 63u;
-  asm volatile("" : "+v"(lane));
-  return lane;
-}
-// The value of the lane 32 away joined with this lane's.
-__device__ __forceinline__ float max_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float add_halves(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 
 // Rows of a segment for n query rows: 32 rg.  rg = 1: the stream below; 2 and 4:
 // so many of the four waves take rows of their own (with 2, the others take the
@@ -236,21 +199,6 @@ struct Tiles {
 __device__ __align__(16) const uint32_t g_zeros[GTS_OPS_MAX_ATTN / 2] = {};  // a row
 // What the page of a key that does not exist is loaded from.
 __device__ const int32_t g_no_page = -1;
-
-// 16 bytes a lane from memory to LDS, lane after lane from `to` on (the same in
-// all lanes).  Nothing waits for it but the wait for all loads before the barrier
-// that hands the tile over: written as the compiler's builtin, it waits for every
-// such load before the next LDS read, whatever that reads, and no tile is on its
-// way while another is worked on.  M0, the LDS address, is the compiler's: it gets
-// its value back.
-__device__ __forceinline__ void load_to_lds(const void* from, void* to) {
-  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)to;
-  uint32_t m0;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
-               : "=&s"(m0)
-               : "s"(at), "v"(from)
-               : "memory");
-}
 
 // Loads tiles of keys and values from the cache straight into LDS (no
 // registers in between, so nothing is held while the tile before is worked
@@ -366,25 +314,6 @@ __device__ __forceinline__ Vec8<T> load_v(const T* sv, uint32_t lane, uint32_t k
 // its end: 0 times one of them would reach rows that must not see it.  So they
 // are cleared in the copy that is multiplied, and added here, from the cache,
 // to the rows that see them.  `add(key, d, x)` gets four values x from dim d on.
-__device__ __forceinline__ bool not_finite(float x) { return !(__builtin_fabsf(x) < INFINITY); }
-template <typename T>
-__device__ __forceinline__ bool any_not_finite(u32x4 v) {
-  constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
-  bool found = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) found |= (v[i] & kExp) == kExp || (v[i] >> 16 & kExp) == kExp;
-  return found;
-}
-template <typename T>
-__device__ __forceinline__ u32x4 finite_only(u32x4 v) {
-  constexpr uint32_t kExp = __is_same(T, __bf16) ? 0x7F80u : 0x7C00u;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if ((v[i] & kExp) == kExp) v[i] &= 0xFFFF0000u;
-    if ((v[i] >> 16 & kExp) == kExp) v[i] &= 0xFFFFu;
-  }
-  return v;
-}
 template <typename T>
 __device__ __forceinline__ const T* value_row(const AttnParams& p, const Work& w, uint32_t j) {
   const gts_kv_cache& kc = p.a.cache;

@@ -20,6 +20,17 @@ hipError_t launch_rotary_table(float*, uint32_t, uint32_t, const TableFreqs&, do
 hipError_t launch_append(const gts_append_args&, hipStream_t) { return hipErrorNoDevice; }
 hipError_t launch_attention(const gts_attention_args&, hipStream_t) { return hipErrorNoDevice; }
 uint64_t attention_scratch(uint32_t, uint32_t, uint32_t, uint32_t, uint32_t) { return 0; }
+hipError_t launch_norm(const gts_norm_args&, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_norm_grad(const gts_norm_grad_args&, hipStream_t) { return hipErrorNoDevice; }
+uint64_t norm_grad_scratch(uint32_t, uint32_t) { return 0; }
+hipError_t launch_matmul(const gts_matmul_args&, hipStream_t) { return hipErrorNoDevice; }
+uint64_t matmul_scratch(uint32_t, uint32_t, uint32_t) { return 0; }
+hipError_t launch_linear_grad(const gts_linear_grad_args&, hipStream_t) { return hipErrorNoDevice; }
+uint64_t linear_grad_scratch(uint32_t, uint32_t) { return 0; }
+hipError_t launch_prompt(const gts_prompt_args&, hipStream_t) { return hipErrorNoDevice; }
+uint64_t prompt_groups(uint32_t, uint32_t, uint32_t) { return 0; }
+hipError_t launch_prompt_grad(const gts_prompt_grad_args&, hipStream_t) { return hipErrorNoDevice; }
+uint64_t prompt_grad_scratch(uint32_t, uint32_t, uint32_t, uint32_t, uint32_t) { return 0; }
 }  // namespace gts
 
 extern "C" int gts_simulate_hwset_noalloc(const gts_graph*, const gts_hwset*, uint32_t, uint32_t, uint32_t*,

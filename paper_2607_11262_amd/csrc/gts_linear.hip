@@ -1,0 +1,335 @@
+// gts_linear.hip — matrix products with bias, activation, gate and residual in the
+// epilogue, and the elementwise part of their gradient.
+//
+//   z = sum_k a[m][k] b[n][k] + bias[n],  out = act(z) gate[m][n] + residual[m][n]
+//   dz = dy gate act'(z),  dgate = dy act(z),  dbias[n] = sum_m dz[m][n]
+//
+// Either operand may be stored with the sum's index as its rows (the products of a
+// backward pass), so nothing is transposed in memory.
+#include "gts_ops.h"
+#include "gts_tile.h"
+
+namespace gts {
+namespace {
+
+// ---- activations ---------------------------------------------------------------------
+
+constexpr float kRootHalf = 0.70710678118654752f;   // 1 / sqrt(2)
+constexpr float kNormal = 0.39894228040143268f;     // 1 / sqrt(2 pi)
+constexpr float kTanhA = 0.79788456080286536f;      // sqrt(2 / pi)
+constexpr float kTanhB = 0.044715f;
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+// Twice the argument of the tanh form; past 30 its sigmoid is 0 or 1 in 32 bits.
+__device__ __forceinline__ float clamp30(float z) { return fminf(fmaxf(z, -30.f), 30.f); }
+__device__ __forceinline__ float tanh_arg(float z) { return 2.f * kTanhA * (z + kTanhB * z * z * z); }
+
+__device__ __forceinline__ float activate(uint32_t act, float z) {
+  switch (act) {
+    case GTS_ACT_RELU: return z > 0.f || z != z ? z : 0.f;
+    case GTS_ACT_GELU: return 0.5f * z * erfcf(-z * kRootHalf);  // no difference of near numbers for z < 0
+    case GTS_ACT_GELU_TANH: return z != z ? z : z * sigmoid(tanh_arg(clamp30(z)));
+    case GTS_ACT_SILU: return z * sigmoid(z);
+    default: return z;
+  }
+}
+__device__ __forceinline__ float slope(uint32_t act, float z) {
+  switch (act) {
+    case GTS_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
+    case GTS_ACT_GELU: return 0.5f * erfcf(-z * kRootHalf) + z * kNormal * expf(-0.5f * z * z);
+    case GTS_ACT_GELU_TANH: {
+      const float c = clamp30(z), s = sigmoid(tanh_arg(c));
+      return z != z ? z : s + c * s * (1.f - s) * 2.f * kTanhA * (1.f + 3.f * kTanhB * c * c);
+    }
+    case GTS_ACT_SILU: {
+      const float s = sigmoid(z);
+      return s * (1.f + z * (1.f - s));
+    }
+    default: return 1.f;
+  }
+}
+
+struct MatmulParams {
+  gts_matmul_args a;
+  bool a_vec, b_vec;   // rows aligned to 16 bytes
+  uint32_t splits;     // of the sum; more than one: the parts go to the scratch
+  uint32_t k_split;    // places of a split
+};
+
+// What becomes of z = the whole sum of (m, n).
+template <typename T>
+__device__ __forceinline__ void finish(const gts_matmul_args& a, uint32_t m, uint32_t n, float z) {
+  if (a.bias) z += (float)((const T*)a.bias)[n];
+  if (a.preact) ((T*)a.preact)[(int64_t)m * a.preact_stride + n] = (T)z;
+  z = activate(a.activation, z);
+  if (a.gate) z *= (float)((const T*)a.gate)[(int64_t)m * a.gate_stride + n];
+  if (a.residual) z += (float)((const T*)a.residual)[(int64_t)m * a.residual_stride + n];
+  ((T*)a.out)[(int64_t)m * a.out_stride + n] = (T)z;
+}
+
+// ---- the general kernel ----------------------------------------------------------------
+// Any type, size, stride and alignment.  Four waves take 64 x 64 each of a 128 x 128
+// tile; 32 places of the sum at a time go through registers to LDS, the next while
+// these are multiplied.
+constexpr uint32_t kTileM = 128, kTileN = 128, kTileK = 32;
+
+// LDS of an operand's 128 rows (or columns) and 32 places: rows of 16 values more than
+// they hold, so that reads of neighbouring rows meet other banks.
+template <bool COLUMNS>
+constexpr uint32_t kPitch = COLUMNS ? kTileM + 8 : kTileK + 8;
+constexpr uint32_t kTileSize = kTileM * (kTileK + 8);  // the larger of both
+
+template <typename T, bool COLUMNS>
+struct Staged {
+  Vec8<T> x[2];
+  // Rows r0 .. + 127 of `rows`, places k0 .. + 31 of those below `k_end`.
+  __device__ __forceinline__ void load(const T* p, int64_t stride, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t k_end,
+                                       bool vec) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t id = threadIdx.x + 256 * i;
+      uint32_t row, column;
+      int64_t valid;
+      if (COLUMNS) {
+        row = k0 + id / 16;
+        column = r0 + id % 16 * 8;
+        valid = row < k_end ? (int64_t)rows - column : 0;
+      } else {
+        row = r0 + id / 4;
+        column = k0 + id % 4 * 8;
+        valid = row < rows ? (int64_t)k_end - column : 0;
+      }
+      x[i] = load8(p + (int64_t)row * stride + column, valid, vec);
+    }
+  }
+  __device__ __forceinline__ void store(T* s) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t id = threadIdx.x + 256 * i;
+      write8(s + (COLUMNS ? id / 16 * kPitch<true> + id % 16 * 8 : id / 4 * kPitch<false> + id % 4 * 8), x[i]);
+    }
+  }
+};
+template <typename T, bool COLUMNS>
+__device__ __forceinline__ Vec8<T> staged_frag(const T* s, uint32_t row, uint32_t k, uint32_t lane) {
+  if constexpr (COLUMNS)
+    return frag_columns<false>(s, kPitch<true>, k, row, lane);
+  else
+    return frag_rows(s, kPitch<false>, row, k, lane);
+}
+
+template <typename T, bool AC, bool BC>
+__global__ __launch_bounds__(256) void matmul_kernel(MatmulParams p) {
+  const gts_matmul_args& a = p.a;
+  __shared__ __align__(16) T s_a[2][kTileSize], s_b[2][kTileSize];
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+  const uint32_t tiles_n = (a.n + kTileN - 1) / kTileN;
+  const uint32_t tile = blockIdx.x / p.splits, split = blockIdx.x - tile * p.splits;
+  const uint32_t m0 = tile / tiles_n * kTileM, n0 = tile % tiles_n * kTileN;
+  const uint32_t wm = wave / 2 * 64, wn = wave % 2 * 64;
+  const uint64_t k_first = (uint64_t)split * p.k_split, k_last = k_first + p.k_split;
+  const uint32_t k0 = (uint32_t)k_first, k1 = k_last < a.k ? (uint32_t)k_last : a.k;
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) acc[i / 2][i % 2][j] = 0.f;
+  Staged<T, AC> sa;
+  Staged<T, BC> sb;
+  if (k0 < k1) {
+    sa.load((const T*)a.a, a.a_stride, m0, a.m, k0, k1, p.a_vec);
+    sb.load((const T*)a.b, a.b_stride, n0, a.n, k0, k1, p.b_vec);
+    sa.store(s_a[0]);
+    sb.store(s_b[0]);
+  }
+  __syncthreads();
+  uint32_t at = 0;
+  for (uint64_t k = k0; k < k1; k += kTileK, at ^= 1) {
+    const bool more = k + kTileK < k1;
+    if (more) {
+      sa.load((const T*)a.a, a.a_stride, m0, a.m, (uint32_t)k + kTileK, k1, p.a_vec);
+      sb.load((const T*)a.b, a.b_stride, n0, a.n, (uint32_t)k + kTileK, k1, p.b_vec);
+    }
+#pragma unroll
+    for (uint32_t kk = 0; kk < kTileK; kk += 16) {
+      Vec8<T> fa[2], fb[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fa[i] = staged_frag<T, AC>(s_a[at], wm + i * 32, kk, lane);
+        fb[i] = staged_frag<T, BC>(s_b[at], wn + i * 32, kk, lane);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = mfma(fa[i], fb[j], acc[i][j]);
+    }
+    if (more) {
+      sa.store(s_a[at ^ 1]);
+      sb.store(s_b[at ^ 1]);
+    }
+    __syncthreads();
+  }
+  float* part = (float*)a.scratch + (uint64_t)split * a.m * a.n;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t n = n0 + wn + j * 32 + lane % 32;
+    if (n >= a.n) continue;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const uint32_t m = m0 + wm + i * 32 + frag_row(e, lane / 32);
+        if (m >= a.m) continue;
+        if (p.splits > 1)
+          part[(uint64_t)m * a.n + n] = acc[i][j][e];
+        else
+          finish<T>(a, m, n, acc[i][j][e]);
+      }
+  }
+}
+
+// The sums of the splits, in order.
+template <typename T>
+__global__ __launch_bounds__(256) void join_splits_kernel(MatmulParams p, FastDiv by_n) {
+  const gts_matmul_args& a = p.a;
+  const uint64_t i = block_number() * 256 + threadIdx.x, all = (uint64_t)a.m * a.n;
+  if (i >= all) return;
+  const float* part = (const float*)a.scratch + i;
+  float z = part[0];
+  for (uint32_t s = 1; s < p.splits; ++s) z += part[s * all];
+  const uint32_t m = all < (1ull << 31) ? by_n.div((uint32_t)i) : (uint32_t)(i / a.n);
+  finish<T>(a, m, (uint32_t)(i - (uint64_t)m * a.n), z);
+}
+
+uint64_t size(int64_t x) { return (uint64_t)(x < 0 ? -x : x); }
+bool rows_aligned(const void* p, int64_t stride, uint32_t e) {
+  return (uintptr_t)p % 16 == 0 && size(stride) * e % 16 == 0;
+}
+
+// Splits of the sum: where the tiles do not fill the chip twice, as many as do, of at
+// least 128 places.  By sizes alone: the scratch is asked for before the layout is known.
+uint32_t splits_of(uint32_t m, uint32_t n, uint32_t k) {
+  const uint64_t tiles = (((uint64_t)m + kTileM - 1) / kTileM) * (((uint64_t)n + kTileN - 1) / kTileN);
+  if (tiles == 0 || tiles >= 256) return 1;
+  const uint32_t most = (k + 127) / 128, want = (uint32_t)(512 / tiles);
+  return most <= 1 ? 1 : want < most ? want : most;
+}
+
+template <typename T, bool AC, bool BC>
+hipError_t launch_general(MatmulParams& p, hipStream_t s) {
+  const gts_matmul_args& a = p.a;
+  p.splits = splits_of(a.m, a.n, a.k);
+  p.k_split = ((a.k + p.splits - 1) / p.splits + kTileK - 1) / kTileK * kTileK;
+  const uint64_t tiles = (((uint64_t)a.m + kTileM - 1) / kTileM) * (((uint64_t)a.n + kTileN - 1) / kTileN);
+  if (tiles * p.splits > 0x7FFFFFull) return hipErrorInvalidValue;  // x 256 threads stay below 2^31
+  matmul_kernel<T, AC, BC><<<dim3((uint32_t)(tiles * p.splits)), dim3(256), 0, s>>>(p);
+  if (p.splits > 1)
+    join_splits_kernel<T><<<grid_of(((uint64_t)a.m * a.n + 255) / 256), dim3(256), 0, s>>>(p, FastDiv(a.n));
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_matmul_t(const gts_matmul_args& a, hipStream_t s) {
+  MatmulParams p{};
+  p.a = a;
+  p.a_vec = rows_aligned(a.a, a.a_stride, sizeof(T));
+  p.b_vec = rows_aligned(a.b, a.b_stride, sizeof(T));
+  const bool ac = a.flags & GTS_MATMUL_A_COLUMNS, bc = a.flags & GTS_MATMUL_B_COLUMNS;
+  if (ac) return bc ? launch_general<T, true, true>(p, s) : launch_general<T, true, false>(p, s);
+  return bc ? launch_general<T, false, true>(p, s) : launch_general<T, false, false>(p, s);
+}
+
+// ---- the elementwise part of the gradient ------------------------------------------------
+// A wave takes 64 V columns of a strip of rows, and keeps its part of dbias in registers.
+struct LinearGradParams {
+  gts_linear_grad_args a;
+  float* db;  // [strips][n], NULL if not wanted
+  uint32_t strips;
+};
+
+template <typename T, int V>
+__global__ __launch_bounds__(256) void linear_grad_kernel(LinearGradParams p) {
+  const gts_linear_grad_args& a = p.a;
+  const uint32_t strip = blockIdx.y * 4 + (threadIdx.x >> 6);
+  const uint64_t at = ((uint64_t)blockIdx.x * 64 + (threadIdx.x & 63u)) * V;
+  if (strip >= p.strips || at >= a.n) return;
+  float db[V] = {};
+  for (uint64_t m = strip; m < a.m; m += p.strips) {
+    const Pack<T, V> dy = *(const Pack<T, V>*)((const T*)a.dy + (int64_t)m * a.dy_stride + at);
+    Pack<T, V> z = {}, g = {}, dg, dz;
+    if (a.preact) z = *(const Pack<T, V>*)((const T*)a.preact + (int64_t)m * a.preact_stride + at);
+    if (a.gate) g = *(const Pack<T, V>*)((const T*)a.gate + (int64_t)m * a.gate_stride + at);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      float d = (float)dy.v[i];
+      if (a.dgate) dg.v[i] = (T)(d * activate(a.activation, (float)z.v[i]));
+      if (a.gate) d *= (float)g.v[i];
+      if (a.activation != GTS_ACT_NONE) d *= slope(a.activation, (float)z.v[i]);
+      dz.v[i] = (T)d;
+      db[i] += d;
+    }
+    if (a.dz) *(Pack<T, V>*)((T*)a.dz + (int64_t)m * a.dz_stride + at) = dz;
+    if (a.dgate) *(Pack<T, V>*)((T*)a.dgate + (int64_t)m * a.dgate_stride + at) = dg;
+  }
+  if (p.db) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) p.db[(uint64_t)strip * a.n + at + i] = db[i];
+  }
+}
+
+// Strips of rows: 16 rows each, but no more than keep the chip busy, so that the parts
+// of dbias stay small beside the rows.
+uint32_t strips_of(uint32_t m, uint32_t n) {
+  const uint64_t waves = ((uint64_t)n + 511) / 512;
+  uint64_t most = 16384 / (waves ? waves : 1);
+  if (most < 16) most = 16;
+  const uint64_t want = ((uint64_t)m + 15) / 16;
+  return (uint32_t)(want < 1 ? 1 : want < most ? want : most);
+}
+
+template <typename T>
+void launch_linear_grad_t(const LinearGradParams& p, hipStream_t s) {
+  constexpr uint32_t V = 16 / sizeof(T);
+  const gts_linear_grad_args& a = p.a;
+  const bool wide = a.n % V == 0 && rows_aligned(a.dy, a.dy_stride, sizeof(T)) &&
+                    rows_aligned(a.preact, a.preact ? a.preact_stride : 0, sizeof(T)) &&
+                    rows_aligned(a.gate, a.gate ? a.gate_stride : 0, sizeof(T)) &&
+                    rows_aligned(a.dz, a.dz ? a.dz_stride : 0, sizeof(T)) &&
+                    rows_aligned(a.dgate, a.dgate ? a.dgate_stride : 0, sizeof(T));
+  const uint32_t v = wide ? V : 1;
+  const dim3 grid((uint32_t)(((uint64_t)a.n + 64 * v - 1) / (64 * v)), (p.strips + 3) / 4);
+  if (wide)
+    linear_grad_kernel<T, V><<<grid, dim3(256), 0, s>>>(p);
+  else
+    linear_grad_kernel<T, 1><<<grid, dim3(256), 0, s>>>(p);
+}
+
+}  // namespace
+
+uint64_t matmul_scratch(uint32_t m, uint32_t n, uint32_t k) {
+  const uint32_t s = splits_of(m, n, k);
+  return s > 1 ? 4ull * s * m * n : 0;
+}
+
+hipError_t launch_matmul(const gts_matmul_args& a, hipStream_t s) {
+  if (a.dtype == GTS_F32) return launch_matmul_t<float>(a, s);
+  if (a.dtype == GTS_BF16) return launch_matmul_t<__bf16>(a, s);
+  return launch_matmul_t<_Float16>(a, s);
+}
+
+uint64_t linear_grad_scratch(uint32_t m, uint32_t n) { return 4ull * strips_of(m, n) * n; }
+
+hipError_t launch_linear_grad(const gts_linear_grad_args& a, hipStream_t s) {
+  LinearGradParams p{a, a.dbias ? (float*)a.scratch : nullptr, strips_of(a.m, a.n)};
+  if (a.dtype == GTS_F32)
+    launch_linear_grad_t<float>(p, s);
+  else if (a.dtype == GTS_BF16)
+    launch_linear_grad_t<__bf16>(p, s);
+  else
+    launch_linear_grad_t<_Float16>(p, s);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_column_sums(p.db, a.dbias, nullptr, nullptr, p.strips, a.n, a.dtype, s);
+}
+
+}  // namespace gts

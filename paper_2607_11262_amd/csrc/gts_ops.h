@@ -20,6 +20,20 @@ hipError_t launch_rotary_table(float* table, uint32_t n_positions, uint32_t rot_
 hipError_t launch_append(const gts_append_args& a, hipStream_t stream);
 hipError_t launch_attention(const gts_attention_args& a, hipStream_t stream);
 uint64_t attention_scratch(uint32_t batch, uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t dim);
+hipError_t launch_norm(const gts_norm_args& a, hipStream_t stream);
+hipError_t launch_norm_grad(const gts_norm_grad_args& a, hipStream_t stream);
+uint64_t norm_grad_scratch(uint32_t rows, uint32_t dim);
+hipError_t launch_matmul(const gts_matmul_args& a, hipStream_t stream);
+uint64_t matmul_scratch(uint32_t m, uint32_t n, uint32_t k);
+hipError_t launch_linear_grad(const gts_linear_grad_args& a, hipStream_t stream);
+uint64_t linear_grad_scratch(uint32_t m, uint32_t n);
+hipError_t launch_prompt(const gts_prompt_args& a, hipStream_t stream);
+uint64_t prompt_groups(uint32_t batch, uint32_t tokens, uint32_t heads);  // workgroups of a launch
+hipError_t launch_prompt_grad(const gts_prompt_grad_args& a, hipStream_t stream);
+uint64_t prompt_grad_scratch(uint32_t batch, uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t dim);
+// out[c] = sum over parts p of in[p][c], for one or two pairs (NULL: none).
+hipError_t launch_column_sums(const float* in0, void* out0, const float* in1, void* out1, uint32_t parts, uint32_t n,
+                              uint32_t dtype, hipStream_t stream);
 
 #ifdef __HIPCC__
 // A launch has less than 2^32 threads in each dimension: workgroups of 256 past

@@ -1,0 +1,463 @@
+// gts_prompt.hip — attention over whole prompts packed one behind the other, and its
+// gradient.
+//
+//   forward   s_ij = scale q_i . k_j over the keys of i's sequence (up to its own: causal),
+//             lse_i = log sum_j exp(s_ij),  out_i = sum_j exp(s_ij - lse_i) v_j
+//   backward  p_ij = exp(s_ij - lse_i),  delta_i = dout_i . out_i,  dp_ij = dout_i . v_j,
+//             ds_ij = p_ij (dp_ij - delta_i),
+//             dv_j = sum_i p_ij dout_i,  dk_j = scale sum_i ds_ij q_i,  dq_i = scale sum_j ds_ij k_j
+//
+// Scores are computed so that a lane has one row (forward and dq: keys x rows) or one key
+// (dk, dv: rows x keys): what leaves the first product is an operand of the second as it
+// stands.  The gradient takes two kernels, one by rows for dq and one by keys for dk and
+// dv, which compute scores twice (seven products instead of five): sums stay in registers,
+// without atomics, the same bits on every run; the query heads that share a key-value head
+// are summed there too.
+#include "gts_ops.h"
+#include "gts_tile.h"
+
+namespace gts {
+namespace {
+
+// ---- which rows a workgroup takes -------------------------------------------------------
+// The tokens before the first sequence, the sequences, and the tokens behind the last are
+// batch + 2 spans.  Span e has the places floor(first(e) / tile) + e on: as many as its
+// tiles or one more, because ceil(n / tile) is at most floor(end / tile) - floor(first / tile) + 1.
+// So a place's span is found without a plan of the lengths.
+struct Span {
+  uint32_t first, n;  // of the span
+  uint32_t tile;      // its tile
+  bool in;            // a sequence
+};
+__device__ __forceinline__ uint32_t bound_of(const int32_t* starts, uint32_t batch, uint32_t tokens, uint32_t e) {
+  if (e == 0) return 0;
+  if (e == batch + 2) return tokens;
+  if (!starts) return e == 1 ? 0 : tokens;
+  const int32_t s = starts[e - 1];
+  return s < 0 ? 0 : (uint32_t)s < tokens ? (uint32_t)s : tokens;
+}
+__host__ __device__ inline uint32_t places_of(uint32_t batch, uint32_t tokens, uint32_t tile) {
+  return tokens / tile + batch + 2;
+}
+// All 64 lanes with the same place; false: nothing is there.
+__device__ __forceinline__ bool find_span(const int32_t* starts, uint32_t batch, uint32_t tokens, uint32_t tile,
+                                          uint32_t place, Span* s) {
+  const uint32_t lane = threadIdx.x & 63u;
+  uint32_t lo = 0, n = batch + 2;  // the span is one of lo .. lo + n - 1
+  while (n > 1) {
+    const uint32_t step = (n + 63u) / 64u, e = lane * step;
+    const bool le = e < n && (lane == 0 || bound_of(starts, batch, tokens, lo + e) / tile + lo + e <= place);
+    const uint32_t last = 63u - (uint32_t)__builtin_clzll(__ballot(le));
+    lo += last * step;
+    n = n - last * step < step ? n - last * step : step;
+  }
+  const uint32_t b0 = uni(bound_of(starts, batch, tokens, lo)), b1 = uni(bound_of(starts, batch, tokens, lo + 1));
+  s->first = b0;
+  s->n = b1 > b0 ? b1 - b0 : 0;
+  s->tile = place - (b0 / tile + lo);
+  s->in = lo > 0 && lo <= batch;
+  return (uint64_t)s->tile * tile < s->n;
+}
+
+// ---- the general kernels ----------------------------------------------------------------
+// Any type, head, stride and alignment.  128 rows (or keys) a workgroup, 32 a wave, which
+// holds their operands in registers; 32 keys (or rows) at a time go through registers to
+// LDS.
+constexpr uint32_t kRows = 128, kStep = 32;
+
+template <typename T, int DP>
+struct Held {  // 32 rows of a wave
+  Vec8<T> x[DP / 16];
+  __device__ __forceinline__ void load(const T* p, bool valid, uint32_t dim, bool vec, uint32_t half) {
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i)
+      x[i] = load8(p + i * 16 + 8 * half, valid ? (int64_t)dim - (i * 16 + 8 * half) : 0, vec);
+  }
+};
+template <typename T, int DP>
+constexpr uint32_t kRowPitch = DP + 8;
+
+// Rows j0 .. j0 + 31 of n to LDS, zeros where there is none.  Returns whether a value was
+// not finite; with `clear`, those are zeros in LDS.
+template <typename T, int DP>
+__device__ __forceinline__ bool stage_rows(const T* p, int64_t stride, uint32_t j0, uint32_t n, uint32_t dim, bool vec,
+                                           bool clear, T* s) {
+  bool found = false;
+#pragma unroll
+  for (uint32_t id = threadIdx.x; id < kStep * (DP / 8); id += 256) {
+    const uint32_t r = id / (DP / 8), c = id % (DP / 8) * 8;
+    Vec8<T> x = load8(p + (int64_t)(j0 + r) * stride + c, j0 + r < n ? (int64_t)dim - c : 0, vec);
+    if (clear) found |= clear_not_finite(x);
+    write8(s + r * kRowPitch<T, DP> + c, x);
+  }
+  return found;
+}
+// Clears them in LDS afterwards (where the product before wanted them).
+template <typename T, int DP>
+__device__ __forceinline__ void clear_rows(T* s) {
+  for (uint32_t id = threadIdx.x; id < kStep * (DP / 8); id += 256) {
+    T* at = s + id / (DP / 8) * kRowPitch<T, DP> + id % (DP / 8) * 8;
+    Vec8<T> x = read8(at);
+    if (clear_not_finite(x)) write8(at, x);
+  }
+}
+
+// sum += rows of LDS x held rows: a 32 x 32 product over the head.
+template <typename T, int DP>
+__device__ __forceinline__ f32x16 times_held(const T* s, const Held<T, DP>& h, uint32_t lane) {
+  f32x16 r;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) r[i] = 0.f;
+#pragma unroll
+  for (int i = 0; i < DP / 16; ++i) r = mfma(frag_rows(s, kRowPitch<T, DP>, 0, i * 16, lane), h.x[i], r);
+  return r;
+}
+// o (dims x the lane's row or key) += turned rows of LDS x weights w of 32 rows, rounded to T.
+template <typename T, int DP>
+__device__ __forceinline__ void add_weighted(f32x16* o, const T* s, const f32x16& w, uint32_t lane) {
+  Vec8<T> u[2];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) u[i / 8][i % 8] = (T)w[i];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) o[d] = mfma(frag_columns<true>(s, kRowPitch<T, DP>, k * 16, d * 32, lane), u[k], o[d]);
+}
+template <int N>
+__device__ __forceinline__ void clear(f32x16 (&o)[N]) {
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+}
+// Values that are not finite in a block whose rows some lanes do not see to its end: 0
+// times one of them would reach lanes that must not see it.  They are cleared in the copy
+// that is multiplied, and added here, from memory, where `sees(j)`: themselves, or NaN, as
+// which they reach a gradient's sum whatever their weight.
+template <typename T, int DP, typename F>
+__device__ __forceinline__ void add_odd(f32x16* o, const T* p, int64_t stride, uint32_t j0, uint32_t n, uint32_t dim,
+                                        uint32_t half, bool as_nan, F sees) {
+#pragma unroll 1
+  for (uint32_t j = j0; j < n && j < j0 + kStep; ++j) {
+    const T* row = p + (int64_t)j * stride;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t c = d * 32 + frag_row(i, half);
+        if (c >= dim) continue;
+        const float x = (float)row[c];
+        if (not_finite(x) && sees(j)) o[d][i] += as_nan ? __builtin_nanf("") : x;
+      }
+  }
+}
+// The lane's row of a result.
+template <typename T, int DP>
+__device__ __forceinline__ void write_row(T* out, const f32x16* o, float f, uint32_t dim, uint32_t half) {
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t c = d * 32 + frag_row(i, half);
+      if (c < dim) out[c] = (T)(o[d][i] * f);
+    }
+}
+
+struct PromptParams {
+  gts_prompt_args a;
+  uint32_t group;
+  bool vec;  // rows of q, k and v are aligned to 16 bytes
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void prompt_kernel(PromptParams p) {
+  const gts_prompt_args& a = p.a;
+  __shared__ __align__(16) T s_k[kStep * kRowPitch<T, DP>], s_v[kStep * kRowPitch<T, DP>];
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, half = lane / 32;
+  const uint32_t hq = blockIdx.x % a.q_heads, h = hq / p.group;
+  Span sp;
+  if (!find_span(a.starts, a.batch, a.tokens, kRows, blockIdx.x / a.q_heads, &sp)) return;
+  const uint32_t r0 = sp.tile * kRows, row = r0 + wave * 32 + lane % 32, token = sp.first + row;
+  const bool valid = row < sp.n, causal = a.flags & GTS_PROMPT_CAUSAL;
+  T* out = (T*)a.out + (int64_t)token * a.out_stride[0] + (int64_t)hq * a.out_stride[1];
+  f32x16 o[DP / 32];
+  clear(o);
+  if (!sp.in) {
+    if (valid) {
+      write_row<T, DP>(out, o, 0.f, a.dim, half);
+      if (a.lse && half == 0) a.lse[(uint64_t)token * a.q_heads + hq] = -INFINITY;
+    }
+    return;
+  }
+  Held<T, DP> q;
+  q.load((const T*)a.q + (int64_t)token * a.q_stride[0] + (int64_t)hq * a.q_stride[1], valid, a.dim, p.vec, half);
+  const T* k = (const T*)a.k + (int64_t)sp.first * a.k_stride[0] + (int64_t)h * a.k_stride[1];
+  const T* v = (const T*)a.v + (int64_t)sp.first * a.v_stride[0] + (int64_t)h * a.v_stride[1];
+  const uint32_t keys = causal && r0 + kRows < sp.n ? r0 + kRows : sp.n;
+  const uint32_t sees = causal ? row + 1 : sp.n;
+  const float c = a.scale * kLog2e;
+  float m = -INFINITY, l = 0.f;
+  for (uint32_t j0 = 0; j0 < keys; j0 += kStep) {
+    const bool edge = causal && j0 + kStep > r0 + 1;  // some row does not see all of the block
+    __syncthreads();
+    stage_rows<T, DP>(k, a.k_stride[0], j0, sp.n, a.dim, p.vec, false, s_k);
+    const bool found = stage_rows<T, DP>(v, a.v_stride[0], j0, sp.n, a.dim, p.vec, edge, s_v);
+    const bool odd = __syncthreads_or(found);
+    f32x16 s = times_held<T, DP>(s_k, q, lane);
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t j = j0 + frag_row(i, half);
+      s[i] = j < sees && j < sp.n ? s[i] * c : -INFINITY;
+      mx = fmaxf(mx, s[i]);
+    }
+    const float m1 = fmaxf(m, max_halves(mx));
+    const float base = m1 == -INFINITY ? 0.f : m1, alpha = exp2_(m - base);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = exp2_(s[i] - base);
+      sum += s[i];
+    }
+    l = l * alpha + add_halves(sum);
+    m = m1;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
+    add_weighted<T, DP>(o, s_v, s, lane);
+    if (odd) add_odd<T, DP>(o, v, a.v_stride[0], j0, sp.n, a.dim, half, false, [&](uint32_t j) { return j < sees; });
+  }
+  if (!valid) return;
+  write_row<T, DP>(out, o, 1.f / l, a.dim, half);
+  if (a.lse && half == 0) a.lse[(uint64_t)token * a.q_heads + hq] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+struct PromptGradParams {
+  gts_prompt_grad_args a;
+  uint32_t group;
+  bool vec;      // rows of dout, q, k and v are aligned to 16 bytes
+  float* delta;  // [tokens][q_heads]
+};
+
+// delta: a wave per row.
+template <typename T>
+__global__ __launch_bounds__(256) void delta_kernel(PromptGradParams p) {
+  const gts_prompt_grad_args& a = p.a;
+  const uint64_t row = block_number() * 4 + (threadIdx.x >> 6);
+  if (row >= (uint64_t)a.tokens * a.q_heads) return;
+  const uint32_t t = (uint32_t)(row / a.q_heads), h = (uint32_t)(row % a.q_heads), lane = threadIdx.x & 63u;
+  const T* x = (const T*)a.dout + (int64_t)t * a.dout_stride[0] + (int64_t)h * a.dout_stride[1];
+  const T* y = (const T*)a.out + (int64_t)t * a.out_stride[0] + (int64_t)h * a.out_stride[1];
+  float sum = 0.f;
+  for (uint32_t d = lane; d < a.dim; d += 64) sum += (float)x[d] * (float)y[d];
+#pragma unroll
+  for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i);
+  if (lane == 0) p.delta[row] = sum;
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void dq_kernel(PromptGradParams p) {
+  const gts_prompt_grad_args& a = p.a;
+  __shared__ __align__(16) T s_k[kStep * kRowPitch<T, DP>], s_v[kStep * kRowPitch<T, DP>];
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, half = lane / 32;
+  const uint32_t hq = blockIdx.x % a.q_heads, h = hq / p.group;
+  Span sp;
+  if (!find_span(a.starts, a.batch, a.tokens, kRows, blockIdx.x / a.q_heads, &sp)) return;
+  const uint32_t r0 = sp.tile * kRows, row = r0 + wave * 32 + lane % 32, token = sp.first + row;
+  const bool valid = row < sp.n, causal = a.flags & GTS_PROMPT_CAUSAL;
+  T* dq = (T*)a.dq + (int64_t)token * a.dq_stride[0] + (int64_t)hq * a.dq_stride[1];
+  f32x16 o[DP / 32];
+  clear(o);
+  if (!sp.in) {
+    if (valid) write_row<T, DP>(dq, o, 0.f, a.dim, half);
+    return;
+  }
+  Held<T, DP> q, dout;
+  q.load((const T*)a.q + (int64_t)token * a.q_stride[0] + (int64_t)hq * a.q_stride[1], valid, a.dim, p.vec, half);
+  dout.load((const T*)a.dout + (int64_t)token * a.dout_stride[0] + (int64_t)hq * a.dout_stride[1], valid, a.dim, p.vec, half);
+  const T* k = (const T*)a.k + (int64_t)sp.first * a.k_stride[0] + (int64_t)h * a.k_stride[1];
+  const T* v = (const T*)a.v + (int64_t)sp.first * a.v_stride[0] + (int64_t)h * a.v_stride[1];
+  const uint32_t keys = causal && r0 + kRows < sp.n ? r0 + kRows : sp.n;
+  const uint32_t sees = !valid ? 0 : causal ? row + 1 : sp.n;
+  const float c = a.scale * kLog2e;
+  const float lse = valid ? a.lse[(uint64_t)token * a.q_heads + hq] * kLog2e : 0.f;
+  const float delta = valid ? p.delta[(uint64_t)token * a.q_heads + hq] : 0.f;
+  for (uint32_t j0 = 0; j0 < keys; j0 += kStep) {
+    const bool edge = causal && j0 + kStep > r0 + 1;
+    __syncthreads();
+    stage_rows<T, DP>(k, a.k_stride[0], j0, sp.n, a.dim, p.vec, false, s_k);
+    stage_rows<T, DP>(v, a.v_stride[0], j0, sp.n, a.dim, p.vec, false, s_v);
+    __syncthreads();
+    f32x16 s = times_held<T, DP>(s_k, q, lane);
+    const f32x16 dp = times_held<T, DP>(s_v, dout, lane);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t j = j0 + frag_row(i, half);
+      s[i] = j < sees && j < sp.n ? exp2_(s[i] * c - lse) * (dp[i] - delta) : 0.f;
+    }
+    bool odd = false;
+    if (edge) {
+      bool found = false;
+      for (uint32_t id = threadIdx.x; id < kStep * (DP / 8); id += 256) {
+        Vec8<T> x = read8(s_k + id / (DP / 8) * kRowPitch<T, DP> + id % (DP / 8) * 8);
+        found |= clear_not_finite(x);
+      }
+      odd = __syncthreads_or(found);
+      if (odd) {
+        clear_rows<T, DP>(s_k);
+        __syncthreads();
+      }
+    }
+    add_weighted<T, DP>(o, s_k, s, lane);
+    if (odd) add_odd<T, DP>(o, k, a.k_stride[0], j0, sp.n, a.dim, half, true, [&](uint32_t j) { return j < sees; });
+  }
+  if (valid) write_row<T, DP>(dq, o, a.scale, a.dim, half);
+}
+
+// WHAT: 1 dv, 2 dk, 3 both (32 bits with heads of 256 have no registers for both).
+template <typename T, int DP, int WHAT>
+__global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
+  const gts_prompt_grad_args& a = p.a;
+  constexpr bool kV = WHAT & 1, kK = WHAT & 2;
+  __shared__ __align__(16) T s_q[kStep * kRowPitch<T, DP>], s_o[kStep * kRowPitch<T, DP>];
+  __shared__ float s_lse[kStep], s_delta[kStep];
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, half = lane / 32;
+  const uint32_t h = blockIdx.x % a.kv_heads;
+  Span sp;
+  if (!find_span(a.starts, a.batch, a.tokens, kRows, blockIdx.x / a.kv_heads, &sp)) return;
+  const uint32_t k0 = sp.tile * kRows, key = k0 + wave * 32 + lane % 32, token = sp.first + key;
+  const bool valid = key < sp.n, causal = a.flags & GTS_PROMPT_CAUSAL;
+  T* dk = (T*)a.dk + (int64_t)token * a.dk_stride[0] + (int64_t)h * a.dk_stride[1];
+  T* dv = (T*)a.dv + (int64_t)token * a.dv_stride[0] + (int64_t)h * a.dv_stride[1];
+  f32x16 ok[kK ? DP / 32 : 1], ov[kV ? DP / 32 : 1];
+  clear(ok);
+  clear(ov);
+  if (sp.in) {
+    Held<T, DP> k, v;
+    k.load((const T*)a.k + (int64_t)token * a.k_stride[0] + (int64_t)h * a.k_stride[1], valid, a.dim, p.vec, half);
+    if constexpr (kK)
+      v.load((const T*)a.v + (int64_t)token * a.v_stride[0] + (int64_t)h * a.v_stride[1], valid, a.dim, p.vec, half);
+    const float c = a.scale * kLog2e;
+    const uint32_t first = causal ? k0 : 0;
+    for (uint32_t g = 0; g < p.group; ++g) {
+      const uint32_t hq = h * p.group + g;
+      const T* q = (const T*)a.q + (int64_t)sp.first * a.q_stride[0] + (int64_t)hq * a.q_stride[1];
+      const T* dout = (const T*)a.dout + (int64_t)sp.first * a.dout_stride[0] + (int64_t)hq * a.dout_stride[1];
+      for (uint32_t i0 = first; i0 < sp.n; i0 += kStep) {
+        const bool edge = causal && i0 + 1 < k0 + kRows;  // some key is not seen by all of the rows
+        __syncthreads();
+        stage_rows<T, DP>(q, a.q_stride[0], i0, sp.n, a.dim, p.vec, false, s_q);
+        stage_rows<T, DP>(dout, a.dout_stride[0], i0, sp.n, a.dim, p.vec, false, s_o);
+        if (threadIdx.x < kStep) {
+          const bool in = i0 + threadIdx.x < sp.n;
+          const uint64_t at = (uint64_t)(sp.first + i0 + threadIdx.x) * a.q_heads + hq;
+          s_lse[threadIdx.x] = in ? a.lse[at] * kLog2e : 0.f;
+          s_delta[threadIdx.x] = in ? p.delta[at] : 0.f;
+        }
+        __syncthreads();
+        f32x16 s = times_held<T, DP>(s_q, k, lane), ds;
+        if constexpr (kK) ds = times_held<T, DP>(s_o, v, lane);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t r = frag_row(i, half), row = i0 + r;
+          const bool seen = row < sp.n && (!causal || key <= row);
+          s[i] = seen ? exp2_(s[i] * c - s_lse[r]) : 0.f;
+          if constexpr (kK) ds[i] = seen ? s[i] * (ds[i] - s_delta[r]) : 0.f;
+        }
+        bool odd = false;
+        if (edge) {
+          bool found = false;
+          for (uint32_t id = threadIdx.x; id < kStep * (DP / 8); id += 256) {
+            const uint32_t at = id / (DP / 8) * kRowPitch<T, DP> + id % (DP / 8) * 8;
+            Vec8<T> x = read8(s_q + at), y = read8(s_o + at);
+            found |= clear_not_finite(x);
+            found |= clear_not_finite(y);
+          }
+          odd = __syncthreads_or(found);
+          if (odd) {
+            clear_rows<T, DP>(s_q);
+            clear_rows<T, DP>(s_o);
+            __syncthreads();
+          }
+        }
+        if constexpr (kV) add_weighted<T, DP>(ov, s_o, s, lane);
+        if constexpr (kK) add_weighted<T, DP>(ok, s_q, ds, lane);
+        if (odd) {
+          const auto sees = [&](uint32_t row) { return key <= row; };
+          if constexpr (kV) add_odd<T, DP>(ov, dout, a.dout_stride[0], i0, sp.n, a.dim, half, false, sees);
+          if constexpr (kK) add_odd<T, DP>(ok, q, a.q_stride[0], i0, sp.n, a.dim, half, true, sees);
+        }
+      }
+    }
+  }
+  if (!valid) return;
+  if constexpr (kV) write_row<T, DP>(dv, ov, 1.f, a.dim, half);
+  if constexpr (kK) write_row<T, DP>(dk, ok, a.scale, a.dim, half);
+}
+
+bool rows_aligned(const void* p, const int64_t* stride, uint32_t e) {
+  return (uintptr_t)p % 16 == 0 && (uint64_t)stride[0] * e % 16 == 0 && (uint64_t)stride[1] * e % 16 == 0;
+}
+
+template <typename T, int DP>
+hipError_t launch_prompt_d(const PromptParams& p, hipStream_t s) {
+  const uint64_t groups = (uint64_t)places_of(p.a.batch, p.a.tokens, kRows) * p.a.q_heads;
+  prompt_kernel<T, DP><<<dim3((uint32_t)groups), dim3(256), 0, s>>>(p);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_prompt_t(const gts_prompt_args& a, hipStream_t s) {
+  PromptParams p{a, a.q_heads / a.kv_heads, false};
+  p.vec = rows_aligned(a.q, a.q_stride, sizeof(T)) && rows_aligned(a.k, a.k_stride, sizeof(T)) &&
+          rows_aligned(a.v, a.v_stride, sizeof(T));
+  if (a.dim <= 64) return launch_prompt_d<T, 64>(p, s);
+  if (a.dim <= 128) return launch_prompt_d<T, 128>(p, s);
+  return launch_prompt_d<T, 256>(p, s);
+}
+
+template <typename T, int DP>
+hipError_t launch_prompt_grad_d(const PromptGradParams& p, hipStream_t s) {
+  const gts_prompt_grad_args& a = p.a;
+  const uint32_t places = places_of(a.batch, a.tokens, kRows);
+  delta_kernel<T><<<grid_of(((uint64_t)a.tokens * a.q_heads + 3) / 4), dim3(256), 0, s>>>(p);
+  dq_kernel<T, DP><<<dim3(places * a.q_heads), dim3(256), 0, s>>>(p);
+  if constexpr (sizeof(T) == 4 && DP == 256) {
+    dkv_kernel<T, DP, 1><<<dim3(places * a.kv_heads), dim3(256), 0, s>>>(p);
+    dkv_kernel<T, DP, 2><<<dim3(places * a.kv_heads), dim3(256), 0, s>>>(p);
+  } else {
+    dkv_kernel<T, DP, 3><<<dim3(places * a.kv_heads), dim3(256), 0, s>>>(p);
+  }
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_prompt_grad_t(const gts_prompt_grad_args& a, hipStream_t s) {
+  PromptGradParams p{a, a.q_heads / a.kv_heads, false, (float*)a.scratch};
+  p.vec = rows_aligned(a.q, a.q_stride, sizeof(T)) && rows_aligned(a.k, a.k_stride, sizeof(T)) &&
+          rows_aligned(a.v, a.v_stride, sizeof(T)) && rows_aligned(a.dout, a.dout_stride, sizeof(T));
+  if (a.dim <= 64) return launch_prompt_grad_d<T, 64>(p, s);
+  if (a.dim <= 128) return launch_prompt_grad_d<T, 128>(p, s);
+  return launch_prompt_grad_d<T, 256>(p, s);
+}
+
+}  // namespace
+
+uint64_t prompt_groups(uint32_t batch, uint32_t tokens, uint32_t heads) {
+  return (uint64_t)places_of(batch, tokens, kRows) * heads;
+}
+
+hipError_t launch_prompt(const gts_prompt_args& a, hipStream_t s) {
+  if (a.dtype == GTS_F32) return launch_prompt_t<float>(a, s);
+  if (a.dtype == GTS_BF16) return launch_prompt_t<__bf16>(a, s);
+  return launch_prompt_t<_Float16>(a, s);
+}
+
+uint64_t prompt_grad_scratch(uint32_t batch, uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t dim) {
+  return 4ull * tokens * q_heads;
+}
+
+hipError_t launch_prompt_grad(const gts_prompt_grad_args& a, hipStream_t s) {
+  if (a.dtype == GTS_F32) return launch_prompt_grad_t<float>(a, s);
+  if (a.dtype == GTS_BF16) return launch_prompt_grad_t<__bf16>(a, s);
+  return launch_prompt_grad_t<_Float16>(a, s);
+}
+
+}  // namespace gts

@@ -1,7 +1,8 @@
-"""Operators of the serving step whose tile graphs this package simulates, as
-hand-written kernels on the card (C ABI: include/gts_ops.h): rotary positions,
-appending keys and values to a paged cache, and attention over that cache for a
-batch whose sequences share a prefix.
+"""Operators of the steps whose tile graphs this package simulates, as
+hand-written kernels on the card (C ABI: include/gts_ops.h).
+
+The serving step: rotary positions, appending keys and values to a paged cache, and
+attention over that cache for a batch whose sequences share a prefix.
 
     from paper_2607_11262_amd import ops
     table = ops.rotary_table(65536, 128)                   # once
@@ -13,9 +14,20 @@ batch whose sequences share a prefix.
     y = ops.rotary(x, positions, table)                    # a training step
     dx = ops.rotary_backward(dy, positions, table)         # (autograd calls it too)
 
+The rest of a decoder layer, at prefill and in training: norms, matrix products
+with their epilogue, attention over whole prompts.
+
+    h = ops.layer_norm(x, w_norm, center=False)
+    q, k, v = ops.linear(h, w_qkv).view(T, -1, D).split((Hq, Hkv, Hkv), 1)
+    o = ops.prompt_attention(ops.rotary(q, positions, table), ops.rotary(k, positions, table), v, starts)
+    x = ops.linear(o.flatten(1), w_o, residual=x)
+    h = ops.layer_norm(x, w_norm2, center=False)
+    x = ops.linear(ops.linear(h, w_gate, activation="silu", gate=ops.linear(h, w_up)), w_down, residual=x)
+    x.backward(dx)                                         # or the *_backward calls
+
 Shapes.  q [T, Hq, D], k and v [T, Hkv, D]: the new tokens of all sequences one
 behind the other, sequence b's at starts[b] .. starts[b + 1] (starts=None: the
-same number each).  Caches [pages, page, Hkv, D] in any memory order whose last
+same number each; for prompts one sequence).  Caches [pages, page, Hkv, D] in any memory order whose last
 dimension is contiguous (pages kept head by head are a transposed view), page a
 power of two.  page_table [B, max_pages] int32; lens [B] int32 counts a
 sequence's own keys with its new ones, the shared prefix apart.  Types: bfloat16,
@@ -27,8 +39,8 @@ api.GtsError for what the library refuses.  Work is enqueued on `stream`
 allocated on it, and tensors handed to another stream than the current one are
 kept from reuse until it has run (record_stream).  The caller orders the
 streams.  Every call may be captured into a graph.  For autograd the caller's
-tensors that a call writes (out, q_out, lse, scratch, the caches) are modified in
-place.
+tensors that a call writes (out, q_out, lse, scratch, preact, mean, rstd, the
+caches) are modified in place.
 """
 from __future__ import annotations
 
@@ -47,8 +59,14 @@ F32, BF16, F16 = 0, 1, 2
 INTERLEAVED, BACKWARD, ZERO_REST = 1, 2, 4
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
+A_COLUMNS, B_COLUMNS, CENTER, CAUSAL = 1, 2, 1, 1
+ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
 EXPORTS = ("gts_rotary_table", "gts_rotary", "gts_append_kv", "gts_shared_prefix_attention",
-           "gts_shared_prefix_attention_scratch")
+           "gts_shared_prefix_attention_scratch", "gts_layer_norm", "gts_layer_norm_backward",
+           "gts_layer_norm_backward_scratch", "gts_matmul", "gts_matmul_scratch", "gts_linear_backward",
+           "gts_linear_backward_scratch", "gts_prompt_attention", "gts_prompt_attention_backward",
+           "gts_prompt_attention_backward_scratch")
 
 _u32, _i64, _vp, _f32 = ctypes.c_uint32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float
 
@@ -83,12 +101,60 @@ class _AttentionArgs(ctypes.Structure):
                 ("scale", _f32), ("reserved", _u32), ("scratch", _vp), ("scratch_bytes", ctypes.c_uint64)]
 
 
+class _NormArgs(ctypes.Structure):
+    _fields_ = [("x", _vp), ("out", _vp), ("weight", _vp), ("bias", _vp), ("mean", _vp), ("rstd", _vp), ("x_stride", _i64),
+                ("out_stride", _i64), ("rows", _u32), ("dim", _u32), ("eps", _f32), ("dtype", _u32), ("flags", _u32),
+                ("reserved", _u32)]
+
+
+class _NormGradArgs(ctypes.Structure):
+    _fields_ = [("dy", _vp), ("x", _vp), ("weight", _vp), ("mean", _vp), ("rstd", _vp), ("dx", _vp), ("dweight", _vp),
+                ("dbias", _vp), ("dy_stride", _i64), ("x_stride", _i64), ("dx_stride", _i64), ("rows", _u32),
+                ("dim", _u32), ("dtype", _u32), ("flags", _u32), ("scratch", _vp), ("scratch_bytes", ctypes.c_uint64)]
+
+
+class _MatmulArgs(ctypes.Structure):
+    _fields_ = [("a", _vp), ("b", _vp), ("out", _vp), ("preact", _vp), ("bias", _vp), ("gate", _vp), ("residual", _vp),
+                ("a_stride", _i64), ("b_stride", _i64), ("out_stride", _i64), ("preact_stride", _i64),
+                ("gate_stride", _i64), ("residual_stride", _i64), ("m", _u32), ("n", _u32), ("k", _u32), ("dtype", _u32),
+                ("activation", _u32), ("flags", _u32), ("scratch", _vp), ("scratch_bytes", ctypes.c_uint64)]
+
+
+class _LinearGradArgs(ctypes.Structure):
+    _fields_ = [("dy", _vp), ("preact", _vp), ("gate", _vp), ("dz", _vp), ("dgate", _vp), ("dbias", _vp),
+                ("dy_stride", _i64), ("preact_stride", _i64), ("gate_stride", _i64), ("dz_stride", _i64),
+                ("dgate_stride", _i64), ("m", _u32), ("n", _u32), ("dtype", _u32), ("activation", _u32), ("scratch", _vp),
+                ("scratch_bytes", ctypes.c_uint64)]
+
+
+class _PromptArgs(ctypes.Structure):
+    _fields_ = [("q", _vp), ("k", _vp), ("v", _vp), ("out", _vp), ("lse", _vp), ("starts", _vp), ("q_stride", _i64 * 2),
+                ("k_stride", _i64 * 2), ("v_stride", _i64 * 2), ("out_stride", _i64 * 2), ("batch", _u32),
+                ("tokens", _u32), ("q_heads", _u32), ("kv_heads", _u32), ("dim", _u32), ("dtype", _u32), ("scale", _f32),
+                ("flags", _u32)]
+
+
+class _PromptGradArgs(ctypes.Structure):
+    _fields_ = [("dout", _vp), ("q", _vp), ("k", _vp), ("v", _vp), ("out", _vp), ("lse", _vp), ("starts", _vp),
+                ("dq", _vp), ("dk", _vp), ("dv", _vp)] + [
+        (x + "_stride", _i64 * 2) for x in ("dout", "q", "k", "v", "out", "dq", "dk", "dv")] + [
+        ("batch", _u32), ("tokens", _u32), ("q_heads", _u32), ("kv_heads", _u32), ("dim", _u32), ("dtype", _u32),
+        ("scale", _f32), ("flags", _u32), ("scratch", _vp), ("scratch_bytes", ctypes.c_uint64)]
+
+
 # The structures' values in one call each, as the C side lays them out: a call of
 # a small batch is bound by the host.
 _pack_rotary = struct.Struct("=4Q3q3q2qq10I").pack
 _pack_cache_batch = "2Q3q3q6I3Qq4I"
 _pack_append = struct.Struct("=" + _pack_cache_batch + "4Q2q2q2q2qQq4I").pack
 _pack_attention = struct.Struct("=" + _pack_cache_batch + "3Q2q2qQ2IfIQQ").pack
+
+_pack_norm = struct.Struct("=6Q2q2If3I").pack
+_pack_norm_grad = struct.Struct("=8Q3q4IQQ").pack
+_pack_matmul = struct.Struct("=7Q6q6IQQ").pack
+_pack_linear_grad = struct.Struct("=6Q5q4IQQ").pack
+_pack_prompt = struct.Struct("=6Q8q6IfI").pack
+_pack_prompt_grad = struct.Struct("=10Q16q6IfIQQ").pack
 
 _bound, _calls = None, {}  # the library the calls are bound to
 
@@ -102,11 +168,17 @@ def lib():
         for name in EXPORTS:
             getattr(L, name).restype = ctypes.c_int
         L.gts_rotary_table.argtypes = [_vp, _u32, _u32, _vp, ctypes.c_double, _vp]
-        for name in ("gts_rotary", "gts_append_kv", "gts_shared_prefix_attention"):
+        for name in ("gts_rotary", "gts_append_kv", "gts_shared_prefix_attention", "gts_layer_norm",
+                     "gts_layer_norm_backward", "gts_matmul", "gts_linear_backward", "gts_prompt_attention",
+                     "gts_prompt_attention_backward"):
             getattr(L, name).argtypes = [_vp, _vp]
             _calls[name] = getattr(L, name)
-        L.gts_shared_prefix_attention_scratch.argtypes = [_u32] * 5 + [ctypes.POINTER(ctypes.c_uint64)]
+        for name, sizes in (("gts_shared_prefix_attention_scratch", 5), ("gts_layer_norm_backward_scratch", 2),
+                            ("gts_matmul_scratch", 3), ("gts_linear_backward_scratch", 2),
+                            ("gts_prompt_attention_backward_scratch", 5)):
+            getattr(L, name).argtypes = [_u32] * sizes + [ctypes.POINTER(ctypes.c_uint64)]
         _scratch_bytes.cache_clear()
+        _scratch_of.cache_clear()
         _bound = L
     return L
 
@@ -528,3 +600,402 @@ def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=Non
             D ** -0.5 if scale is None else _f32(scale).value, 0, scratch.data_ptr(), scratch.numel()), s)
     _wrote(*written)
     return out
+
+
+# ---- norms --------------------------------------------------------------------------
+
+@functools.lru_cache(maxsize=1024)
+def _scratch_of(name, *sizes):
+    n = ctypes.c_uint64(0)
+    rc = getattr(lib(), name)(*sizes, ctypes.byref(n))
+    if rc != api.GTS_OK:
+        raise api.GtsError(rc, name, api.lib().gts_last_error().decode())
+    return int(n.value)
+
+
+def _scratch(like, name, *sizes):
+    """Scratch of a call, allocated on its stream: (tensor or None, bytes)."""
+    n = _scratch_of(name, *sizes)
+    return (like.new_empty(n, dtype=torch.uint8) if n else None), n
+
+
+def _vector(t, name, n, like):
+    """t is None or a contiguous [n] of the type and on the device of `like`."""
+    if t is not None:
+        s = _data(t, name, 1, like)
+        if t.shape[0] != n or (n > 1 and s[0] != 1):
+            raise ValueError(f"{name} is a contiguous [{n}]: got {tuple(t.shape)}")
+
+
+def _matrix(t, name, shape, like, written=False):
+    """t is None or a matrix of that shape; returns its row stride."""
+    if t is None:
+        return 0
+    s = _data(t, name, 2, like)
+    if t.shape != shape:
+        raise ValueError(f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
+    if written:
+        _disjoint(s, shape, name)
+    return s[0]
+
+
+def _stats(t, name, rows, like):
+    if t is not None and not (isinstance(t, torch.Tensor) and t.dtype == torch.float32 and t.shape == (rows,)
+                              and t.is_contiguous() and t.get_device() == like.get_device()):
+        raise ValueError(f"{name} is a contiguous float32 [{rows}] beside x")
+
+
+def _flat(x, name="x"):
+    """x [..., dim] as rows [n, dim] (a view where its layout has one) and its leading shape."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} is a tensor: got {type(x).__name__}")
+    if x.dim() == 2:
+        return x
+    if x.dim() < 1:
+        raise ValueError(f"{name} has no dimensions")
+    return x.reshape(-1, x.shape[-1]) if x.numel() else x.new_empty((math.prod(x.shape[:-1]), x.shape[-1]))
+
+
+def _norm(x, weight, bias, eps, center, out, mean, rstd, stream):
+    xs = _data(x, "x", 2)
+    rows, dim = x.shape
+    _refuse(dim > 0, "x has rows of no values")
+    _vector(weight, "weight", dim, x)
+    _vector(bias, "bias", dim, x)
+    os = _matrix(out, "out", x.shape, x, True)
+    _stats(mean, "mean", rows, x)
+    _stats(rstd, "rstd", rows, x)
+    with _on(stream, x, x, weight, bias, out, mean, rstd) as s:
+        y = x.new_empty((rows, dim)) if out is None else out
+        _call("gts_layer_norm", _pack_norm(
+            x.data_ptr(), y.data_ptr(), _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd), xs[0],
+            dim if out is None else os, rows, dim, eps, _TYPES[x.dtype], CENTER if center else 0, 0), s)
+    _wrote(out, mean, rstd)
+    return y
+
+
+class _Norm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps, center, mean, rstd, stream):
+        # statistics that the caller gave may be written again before the backward pass
+        own_mean = x.new_empty(x.shape[0], dtype=torch.float32) if center else None
+        own_rstd = x.new_empty(x.shape[0], dtype=torch.float32)
+        y = _norm(x, weight, bias, eps, center, None, own_mean, own_rstd, stream)
+        ctx.save_for_backward(x, weight, own_mean, own_rstd)
+        ctx.bias = bias is not None
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx, dw, db = _norm_backward(_rows(dy), x, weight, rstd, mean, need[0], weight is not None and need[1],
+                                    ctx.bias and need[2], None)
+        return dx, dw, db, None, None, None, None, None
+
+
+def _rows(t):
+    return t if t.stride(-1) == 1 or t.shape[-1] <= 1 else t.contiguous()
+
+
+def layer_norm(x, weight=None, bias=None, *, eps=1e-5, center=True, out=None, mean=None, rstd=None, stream=None):
+    """Rows of x [..., dim] with their mean taken off and divided by the root of
+    their mean square plus eps, times weight [dim], plus bias [dim]; without `center`
+    the mean stays (RMS norm).  out=x writes over x.  mean and rstd (float32, one
+    a row) receive what layer_norm_backward takes.  Differentiable once in x, weight and
+    bias by reverse mode (out, mean and rstd are then refused)."""
+    _no_tangent_of("a tensor of the norm", x, weight, bias)
+    shape = x.shape if isinstance(x, torch.Tensor) else None
+    flat = _flat(x)
+    if _wants_gradient(x, weight, bias):
+        _refuse(out is None and mean is None and rstd is None, "out, mean and rstd are refused: an input requires a gradient")
+        y = _Norm.apply(flat, weight, bias, eps, center, None, None, stream)
+    else:
+        _no_gradient("out of the norm", out, mean, rstd)
+        if out is not None:
+            _refuse(isinstance(out, torch.Tensor) and out.shape == shape, f"out is a tensor {tuple(shape)}")
+            flat_out = _flat(out, "out")
+            _refuse(flat_out.data_ptr() == out.data_ptr(), "out: its rows are not evenly apart")
+            _norm(flat, weight, bias, eps, center, flat_out, mean, rstd, stream)
+            return out
+        y = _norm(flat, weight, bias, eps, center, None, mean, rstd, stream)
+    return y if y.shape == shape else y.view(shape)
+
+
+def _norm_backward(dy, x, weight, rstd, mean, want_dx, want_dw, want_db, stream):
+    xs = _data(x, "x", 2)
+    rows, dim = x.shape
+    _refuse(dim > 0, "x has rows of no values")
+    dys = _matrix(dy, "dy", x.shape, x)
+    _vector(weight, "weight", dim, x)
+    _stats(mean, "mean", rows, x)
+    _stats(rstd, "rstd", rows, x)
+    with _on(stream, x, x, dy, weight, mean, rstd) as s:
+        dx = x.new_empty((rows, dim)) if want_dx else None
+        dw = x.new_empty(dim) if want_dw else None
+        db = x.new_empty(dim) if want_db else None
+        scratch, n = _scratch(x, "gts_layer_norm_backward_scratch", rows, dim) if want_dw or want_db else (None, 0)
+        _call("gts_layer_norm_backward", _pack_norm_grad(
+            dy.data_ptr(), x.data_ptr(), _ptr(weight), _ptr(mean), rstd.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db), dys, xs[0],
+            dim, rows, dim, _TYPES[x.dtype], 0 if mean is None else CENTER, _ptr(scratch), n), s)
+    return dx, dw, db
+
+
+def layer_norm_backward(dy, x, weight, rstd, mean=None, *, bias=False, stream=None):
+    """(dx, dweight, dbias) of layer_norm from the gradient of its result, x and the
+    statistics that the forward pass left; mean=None is the norm without `center`.
+    dweight is None without a weight, dbias unless `bias` asks for it."""
+    _no_gradient("a tensor of the norm's gradient", dy, x, weight, rstd, mean)
+    _refuse(isinstance(rstd, torch.Tensor), "rstd is a float32 tensor, one value a row")
+    flat = _flat(x)
+    _refuse(isinstance(dy, torch.Tensor) and dy.shape == x.shape, "dy has the shape of x")
+    dx, dw, db = _norm_backward(_flat(dy, "dy"), flat, weight, rstd, mean, True, weight is not None, bias, stream)
+    return dx.view(x.shape), dw, db
+
+
+# ---- products -------------------------------------------------------------------------
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError(f"activation {name!r}: one of {list(ACTIVATIONS)}")
+    return ACTIVATIONS[name]
+
+
+def _matmul(a, b, out, preact, bias, gate, residual, strides, m, n, k, act, flags, s):
+    """One product on stream s; strides of a, b, out, preact, gate, residual."""
+    scratch, size = _scratch(out, "gts_matmul_scratch", m, n, k)
+    _call("gts_matmul", _pack_matmul(
+        a.data_ptr(), b.data_ptr(), out.data_ptr(), _ptr(preact), _ptr(bias), _ptr(gate), _ptr(residual), *strides, m, n, k,
+        _TYPES[out.dtype], act, flags, _ptr(scratch), size), s)
+
+
+def _linear(x, weight, bias, act, gate, residual, out, preact, stream):
+    xs = _data(x, "x", 2)
+    ws = _data(weight, "weight", 2, x)
+    (M, K), N = x.shape, weight.shape[0]
+    if weight.shape[1] != K:
+        raise ValueError(f"weight is {tuple(weight.shape)} for x of {K} columns: [columns of the result, {K}]")
+    _vector(bias, "bias", N, x)
+    gs, rs = _matrix(gate, "gate", (M, N), x), _matrix(residual, "residual", (M, N), x)
+    os, ps = _matrix(out, "out", (M, N), x, True), _matrix(preact, "preact", (M, N), x, True)
+    with _on(stream, x, x, weight, bias, gate, residual, out, preact) as s:
+        y = x.new_empty((M, N)) if out is None else out
+        _matmul(x, weight, y, preact, bias, gate, residual, (xs[0], ws[0], N if out is None else os, ps, gs, rs), M, N, K, act,
+                0, s)
+    _wrote(out, preact)
+    return y
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, act, gate, residual, stream):
+        preact = None
+        if (act or gate is not None) and any(t is not None and t.requires_grad for t in (x, weight, bias, gate)):
+            preact = x.new_empty((x.shape[0], weight.shape[0]))
+        y = _linear(x, weight, bias, act, gate, residual, None, preact, stream)
+        ctx.save_for_backward(x, weight, preact, gate)
+        ctx.act, ctx.bias, ctx.residual = act, bias is not None, residual is not None
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, preact, gate = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dres = dy if ctx.residual and need[5] else None
+        if not (need[0] or need[1] or need[2] or need[4]):
+            return None, None, None, None, None, dres, None
+        dx, dw, db, dg = _linear_backward(_rows(dy), x, weight, ctx.act, preact, gate, need[0], need[1], ctx.bias and need[2],
+                                          gate is not None and need[4], None)
+        return dx, dw, db, None, dg, dres, None
+
+
+def _wants_gradient(*tensors):
+    return torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors)
+
+
+def _no_tangent_of(what, *tensors):
+    _no_tangent(what, *(t for t in tensors if isinstance(t, torch.Tensor)))
+
+
+def linear(x, weight, bias=None, *, activation=None, gate=None, residual=None, out=None, preact=None, stream=None):
+    """act(x weight^T + bias) * gate + residual, in one pass: x [..., K], weight
+    [N, K], bias [N]; gate and residual have the result's shape [..., N].  `activation` is
+    None, "relu", "gelu" (by the normal distribution), "gelu_tanh" or "silu"; with gate
+    the result is that of a gated layer.  All of it is computed in 32 bits and rounded
+    once.  out may be gate or residual; preact (of the result's shape and type)
+    receives x weight^T + bias for linear_backward.  Differentiable once in x, weight,
+    bias, gate and residual by reverse mode (out and preact are then refused)."""
+    act = _activation(activation)
+    _no_tangent_of("a tensor of the product", x, weight, bias, gate, residual)
+    flat = _flat(x)
+    _refuse(isinstance(weight, torch.Tensor) and weight.dim() == 2, "weight is a matrix [N, K]")
+    shape = (*x.shape[:-1], weight.shape[0])
+    for t, name in ((gate, "gate"), (residual, "residual"), (out, "out"), (preact, "preact")):
+        if t is not None:
+            _refuse(isinstance(t, torch.Tensor) and t.shape == shape, f"{name} is a tensor {shape}")
+    g, r = (None if t is None else _flat(t) for t in (gate, residual))
+    if _wants_gradient(x, weight, bias, gate, residual):
+        _refuse(out is None and preact is None, "out and preact are refused: an input requires a gradient")
+        y = _Linear.apply(flat, weight, bias, act, g, r, stream)
+    else:
+        _no_gradient("out of the product", out, preact)
+        o, z = (None if t is None else _flat(t) for t in (out, preact))
+        for t, f, name in ((out, o, "out"), (preact, z, "preact")):
+            _refuse(t is None or f.data_ptr() == t.data_ptr(), f"{name}: its rows are not evenly apart")
+        y = _linear(flat, weight, bias, act, g, r, o, z, stream)
+        if out is not None:
+            return out
+    return y if y.shape == shape else y.view(shape)
+
+
+def _linear_backward(dy, x, weight, act, preact, gate, want_dx, want_dw, want_db, want_dg, stream):
+    xs, ws = _data(x, "x", 2), _data(weight, "weight", 2, x)
+    (M, K), N = x.shape, weight.shape[0]
+    if weight.shape[1] != K:
+        raise ValueError(f"weight is {tuple(weight.shape)} for x of {K} columns")
+    dys = _matrix(dy, "dy", (M, N), x)
+    ps, gs = _matrix(preact, "preact", (M, N), x), _matrix(gate, "gate", (M, N), x)
+    if preact is None and (act or gate is not None):
+        raise ValueError("preact is missing: linear left it for an activation or a gate")
+    with _on(stream, x, x, weight, dy, preact, gate) as s:
+        dz, zs = dy, dys
+        db = x.new_empty(N) if want_db else None
+        dg = x.new_empty((M, N)) if want_dg else None
+        own = (act or gate is not None) and (want_dx or want_dw)
+        if own:
+            dz, zs = x.new_empty((M, N)), N
+        if own or want_db or want_dg:
+            scratch, n = _scratch(x, "gts_linear_backward_scratch", M, N) if want_db else (None, 0)
+            _call("gts_linear_backward", _pack_linear_grad(
+                dy.data_ptr(), _ptr(preact), _ptr(gate), dz.data_ptr() if own else 0, _ptr(dg), _ptr(db), dys, ps, gs, zs, N,
+                M, N, _TYPES[x.dtype], act, _ptr(scratch), n), s)
+        dx = dw = None
+        if want_dx:
+            dx = x.new_empty((M, K))
+            _matmul(dz, weight, dx, None, None, None, None, (zs, ws[0], K, 0, 0, 0), M, K, N, 0, B_COLUMNS, s)
+        if want_dw:
+            dw = x.new_empty((N, K))
+            _matmul(dz, x, dw, None, None, None, None, (zs, xs[0], K, 0, 0, 0), N, K, M, 0, A_COLUMNS | B_COLUMNS, s)
+    return dx, dw, db, dg
+
+
+def linear_backward(dy, x, weight, *, activation=None, preact=None, gate=None, bias=False, stream=None):
+    """(dx, dweight, dbias, dgate) of linear from the gradient of its result, its
+    operands and, with an activation or a gate, the preact that it left.  dbias is None
+    unless `bias` asks for it, dgate without a gate.  The gradient of residual is dy.
+    What is multiplied (dy times the gate and the activation's slope) is in dy's type."""
+    act = _activation(activation)
+    _no_gradient("a tensor of the product's gradient", dy, x, weight, preact, gate)
+    flat = _flat(x)
+    _refuse(isinstance(weight, torch.Tensor) and weight.dim() == 2, "weight is a matrix [N, K]")
+    shape = (*x.shape[:-1], weight.shape[0])
+    for t, name in ((dy, "dy"), (preact, "preact"), (gate, "gate")):
+        if t is not None or name == "dy":
+            _refuse(isinstance(t, torch.Tensor) and t.shape == shape, f"{name} is a tensor {shape}")
+    z, g = (None if t is None else _flat(t) for t in (preact, gate))
+    dx, dw, db, dg = _linear_backward(_flat(dy), flat, weight, act, z, g, True, True, bias, gate is not None, stream)
+    return dx.view(x.shape), dw, db, None if dg is None else dg.view(shape)
+
+
+# ---- attention over prompts ---------------------------------------------------------------
+
+def _prompt_shapes(q, k, v, starts):
+    qs, ks, vs = _data(q, "q", 3), _data(k, "k", 3, q), _data(v, "v", 3, q)
+    T, Hq, D = q.shape
+    if k.shape != v.shape or k.shape[0] != T or k.shape[2] != D:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}: [{T}, heads, {D}], k and v alike")
+    B = 1
+    if starts is not None:
+        ss = _index(starts, "starts", 1, q)
+        B = starts.shape[0] - 1
+        if B < 1 or ss[0] != 1:
+            raise ValueError("starts is [sequences + 1] and contiguous")
+    return qs, ks, vs, B, T, Hq, k.shape[1], D
+
+
+def _lse_like(lse, T, Hq, q):
+    _refuse(isinstance(lse, torch.Tensor) and lse.dtype == torch.float32 and lse.shape == (T, Hq) and lse.is_contiguous()
+            and lse.device == q.device, f"lse is a contiguous float32 [{T}, {Hq}]")
+
+
+def _scale(scale, D):
+    return D ** -0.5 if scale is None else _f32(scale).value
+
+
+def _prompt(q, k, v, starts, causal, scale, out, lse, stream):
+    qs, ks, vs, B, T, Hq, Hkv, D = _prompt_shapes(q, k, v, starts)
+    if out is not None:
+        _disjoint(_data(out, "out", 3, q), out.shape, "out")
+        _refuse(out.shape == q.shape, f"out is {tuple(out.shape)}, not {tuple(q.shape)}")
+    if lse is not None:
+        _lse_like(lse, T, Hq, q)
+    with _on(stream, q, q, k, v, starts, out, lse) as s:
+        o = q.new_empty(q.shape) if out is None else out
+        os = o.stride()
+        _call("gts_prompt_attention", _pack_prompt(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), _ptr(starts), qs[0], qs[1], ks[0], ks[1], vs[0],
+            vs[1], os[0], os[1], B, T, Hq, Hkv, D, _TYPES[q.dtype], _scale(scale, D), CAUSAL if causal else 0), s)
+    _wrote(out, lse)
+    return o
+
+
+class _Prompt(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, starts, causal, scale, stream):
+        lse = q.new_empty(q.shape[:2], dtype=torch.float32)
+        o = _prompt(q, k, v, starts, causal, scale, None, lse, stream)
+        ctx.save_for_backward(q, k, v, o, lse, starts)
+        ctx.causal, ctx.scale = causal, scale
+        return o
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        q, k, v, o, lse, starts = ctx.saved_tensors
+        dq, dk, dv = _prompt_backward(_rows(dout), q, k, v, o, lse, starts, ctx.causal, ctx.scale, None)
+        return dq, dk, dv, None, None, None, None
+
+
+def prompt_attention(q, k, v, starts=None, *, causal=True, scale=None, out=None, lse=None, stream=None):
+    """Attention over whole prompts: q [T, Hq, D], k and v [T, Hkv, D], the tokens of
+    sequence b at starts[b] .. starts[b + 1] (int32 [B + 1], ascending; None: one
+    sequence).  A token sees the keys of its sequence, with `causal` those up to its own.
+    Query head h reads key-value head h // (Hq / Hkv); scale defaults to D ** -0.5.  A token
+    outside every sequence gives zeros and a log-sum of -inf.  out and lse (float32
+    [T, Hq], natural logarithm) receive the results if given.  Softmax weights are rounded
+    to the tensors' type for the product with the values.  Differentiable once in q, k and
+    v by reverse mode (out and lse are then refused)."""
+    _no_tangent_of("a tensor of the attention", q, k, v)
+    if _wants_gradient(q, k, v):
+        _refuse(out is None and lse is None, "out and lse are refused: an input requires a gradient")
+        return _Prompt.apply(q, k, v, starts, causal, scale, stream)
+    _no_gradient("out of the attention", out, lse)
+    return _prompt(q, k, v, starts, causal, scale, out, lse, stream)
+
+
+def _prompt_backward(dout, q, k, v, out, lse, starts, causal, scale, stream):
+    qs, ks, vs, B, T, Hq, Hkv, D = _prompt_shapes(q, k, v, starts)
+    ds, os = _data(dout, "dout", 3, q), _data(out, "out", 3, q)
+    _refuse(dout.shape == q.shape and out.shape == q.shape, f"dout and out are {tuple(q.shape)}")
+    _lse_like(lse, T, Hq, q)
+    with _on(stream, q, dout, q, k, v, out, lse, starts) as s:
+        dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
+        scratch, n = _scratch(q, "gts_prompt_attention_backward_scratch", B, T, Hq, Hkv, D)
+        _call("gts_prompt_attention_backward", _pack_prompt_grad(
+            dout.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), _ptr(starts),
+            dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ds[0], ds[1], qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os[0], os[1],
+            Hq * D, D, Hkv * D, D, Hkv * D, D, B, T, Hq, Hkv, D, _TYPES[q.dtype], _scale(scale, D), CAUSAL if causal else 0,
+            _ptr(scratch), n), s)
+    return dq, dk, dv
+
+
+def prompt_attention_backward(dout, q, k, v, out, lse, starts=None, *, causal=True, scale=None, stream=None):
+    """(dq, dk, dv) of prompt_attention from the gradient of its result, its inputs,
+    its result and the log-sums that it left; causal and scale as in the forward call.
+    Weights and their gradients are rounded to the tensors' type for the products, and
+    summed over a key-value head's query heads in 32 bits.  Tokens outside every
+    sequence get zeros.  The same bits on every run."""
+    _no_gradient("a tensor of the attention's gradient", dout, q, k, v, out, lse)
+    return _prompt_backward(dout, q, k, v, out, lse, starts, causal, scale, stream)
