@@ -83,7 +83,7 @@ template <typename T, int DP>
 __device__ __forceinline__ bool stage_rows(const T* p, int64_t stride, uint32_t j0, uint32_t n, uint32_t dim, bool vec,
                                            bool clear, T* s) {
   bool found = false;
-#pragma unroll
+#pragma unroll 4
   for (uint32_t id = threadIdx.x; id < kStep * (DP / 8); id += 256) {
     const uint32_t r = id / (DP / 8), c = id % (DP / 8) * 8;
     Vec8<T> x = load8(p + (int64_t)(j0 + r) * stride + c, j0 + r < n ? (int64_t)dim - c : 0, vec);
@@ -166,6 +166,7 @@ __device__ __forceinline__ void write_row(T* out, const f32x16* o, float f, uint
 struct PromptParams {
   gts_prompt_args a;
   uint32_t group;
+  uint32_t places;
   bool vec;  // rows of q, k and v are aligned to 16 bytes
 };
 
@@ -229,6 +230,347 @@ __global__ __launch_bounds__(256) void prompt_kernel(PromptParams p) {
   if (!valid) return;
   write_row<T, DP>(out, o, 1.f / l, a.dim, half);
   if (a.lse && half == 0) a.lse[(uint64_t)token * a.q_heads + hq] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// ---- the tile kernels ---------------------------------------------------------------------
+// 16-bit values whose rows are aligned to 16 bytes, heads of whole 16 bytes.  As the general
+// kernels, with tiles of 64 rows of two matrices (keys and values, or queries and dout) that
+// go straight to LDS while the tile before is worked on: one barrier a tile.
+constexpr uint32_t kTile = 64;
+
+__device__ __align__(16) const uint32_t g_zeros[GTS_OPS_MAX_ATTN / 2] = {};  // a row that is not there
+
+template <typename T, int DP>
+struct Tiles {
+  static constexpr int C = DP / 8;      // 16-byte chunks of a row
+  static constexpr int RPI = 64 / C;    // rows of one load of a wave
+  static constexpr int NL = 16 / RPI;   // loads of a wave for its 16 rows
+  static constexpr int N = kTile * DP;  // values of a tile
+  // Chunk c of row r stands at c ^ swizzle(r): reads of 16 rows at one chunk, and reads of 4
+  // rows x 64 bytes that are turned on the way, each touch all 64 banks once.
+  static __device__ __forceinline__ uint32_t swizzle(uint32_t r) {
+    return C >= 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 2) << 1) | ((r >> 2) & 3);
+  }
+};
+
+// Loads tiles of two matrices to LDS, 16 rows of each a wave.
+template <typename T, int DP>
+struct Loader {
+  using L = Tiles<T, DP>;
+  const T *a, *b;  // of the first row
+  int64_t a_stride, b_stride;
+  uint32_t n, dim;                      // rows that are there, values of a row
+  uint32_t a_off[L::NL], b_off[L::NL];  // bytes from the wave's first row to this lane's chunk
+
+  __device__ __forceinline__ void start() {
+    const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
+#pragma unroll
+    for (int i = 0; i < L::NL; ++i) {
+      const uint32_t r = i * L::RPI + r0;
+      a_off[i] = 2 * (r * (uint32_t)a_stride + (c ^ L::swizzle(r)) * 8);
+      b_off[i] = 2 * (r * (uint32_t)b_stride + (c ^ L::swizzle(r)) * 8);
+    }
+  }
+  __device__ __forceinline__ void load(uint32_t j0, uint32_t wave, T* sa, T* sb) const {
+    const uint32_t j = j0 + wave * 16;
+    const char* pa = (const char*)(a + (int64_t)j * a_stride);
+    const char* pb = (const char*)(b + (int64_t)j * b_stride);
+    if (j + 16 <= n && dim == DP) {
+#pragma unroll
+      for (int i = 0; i < L::NL; ++i) {
+        load_to_lds(pa + a_off[i], sa + (wave * 16 + i * L::RPI) * DP);
+        load_to_lds(pb + b_off[i], sb + (wave * 16 + i * L::RPI) * DP);
+      }
+      return;
+    }
+    const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
+#pragma unroll
+    for (int i = 0; i < L::NL; ++i) {
+      const uint32_t r = i * L::RPI + r0;
+      const bool there = j + r < n && (c ^ L::swizzle(r)) * 8 < dim;
+      load_to_lds(there ? pa + a_off[i] : (const char*)g_zeros, sa + (wave * 16 + i * L::RPI) * DP);
+      load_to_lds(there ? pb + b_off[i] : (const char*)g_zeros, sb + (wave * 16 + i * L::RPI) * DP);
+    }
+  }
+};
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Fragments of a tile: rows row + lane % 32, places 16 kk + 8 half ..; at = the lane's part.
+template <typename T, int DP>
+struct RowFrags {
+  const T* at;
+  uint32_t c;
+  __device__ __forceinline__ RowFrags(const T* s, uint32_t row, uint32_t lane)
+      : at(s + (row + lane % 32) * DP), c(lane / 32 ^ Tiles<T, DP>::swizzle(lane % 32)) {}
+  __device__ __forceinline__ Vec8<T> operator()(int kk) const { return *(const Vec8<T>*)(at + (c ^ (2 * kk)) * 8); }
+};
+// The same of columns 32 d + lane % 32, rows row + 4 half .. + 3 and 8 further (what a lane
+// has of a product's result).
+template <typename T, int DP>
+__device__ __forceinline__ Vec8<T> column_frag(const T* s, uint32_t row, int d, uint32_t lane) {
+  using L = Tiles<T, DP>;
+  const uint32_t g = lane / 16, r = 4 * (g / 2) + lane % 16 / 4, c = g % 2 * 2 + lane % 4 / 2;  // row: whole 16s
+  typedef __attribute__((address_space(3))) i16x4* lds_t;
+  union {
+    i16x4 h[2];
+    Vec8<T> v;
+  } u;
+  const T* at = s + (row + r) * DP + lane % 2 * 4;
+  u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(at + ((c ^ L::swizzle(r)) ^ (d * 4)) * 8));
+  u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(at + 8 * DP + ((c ^ L::swizzle(r + 8)) ^ (d * 4)) * 8));
+  return u.v;
+}
+template <typename T, int N>
+__device__ __forceinline__ void clear_tile(T* s) {
+  for (uint32_t x = threadIdx.x; x < N / 8; x += 256) *(u32x4*)(s + x * 8) = finite_only<T>(*(const u32x4*)(s + x * 8));
+}
+// The wave's 32 rows of a result (dims x rows, a lane its row) to memory, through LDS that the
+// wave has for itself, so that whole rows are written.  lane_ok: the lane's row is there.
+template <typename T, int DP>
+__device__ __forceinline__ void write_rows(T* s, const f32x16* o, float f, T* out, int64_t stride, uint32_t rows, uint32_t dim,
+                                           uint32_t lane) {
+  constexpr uint32_t P = DP + 8;
+  const uint32_t half = lane / 32;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      Pack<T, 4> x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x.v[j] = (T)(o[d][i + j] * f);
+      *(Pack<T, 4>*)(s + lane % 32 * P + d * 32 + frag_row(i, half)) = x;
+    }
+  asm volatile("" ::: "memory");  // a wave's accesses to LDS keep their order
+#pragma unroll
+  for (uint32_t i = 0; i < DP / 16; ++i) {
+    const uint32_t id = i * 64 + lane, r = id / (DP / 8), c = id % (DP / 8) * 8;
+    if (r < rows && c < dim) *(u32x4*)(out + (int64_t)r * stride + c) = *(const u32x4*)(s + r * P + c);
+  }
+}
+
+// Position of a workgroup among the heads of a place: those of a key-value head, and as many
+// key-value heads as divide 8, stand 8 / that many apart, so that they meet in the L2 of one XCD.
+__device__ __forceinline__ uint32_t head_at(uint32_t at, uint32_t kv_heads, uint32_t group, uint32_t* kv) {
+  const uint32_t s = kv_heads % 8 == 0 ? 8 : kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1;
+  *kv = at % s + at / (s * group) * s;
+  return *kv * group + at / s % group;
+}
+
+// What a wave of the forward kernel holds: 32 rows.
+template <typename T, int DP>
+struct Rows {
+  Vec8<T> q[DP / 16];
+  f32x16 o[DP / 32];
+  float m, l;  // reference maximum of q.k (unscaled), sum of this half's weights
+
+  // 32 NS keys from LDS row `key` on; the lane's row sees those before `sees` (from there).
+  template <int NS>
+  __device__ __forceinline__ void step(uint32_t lane, const T* sk, const T* sv, uint32_t key, float c, bool mask, int32_t sees) {
+    f32x16 s[NS];
+#pragma unroll
+    for (int b = 0; b < NS; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+    // The fragments of two matrix steps are read while the two before are multiplied; the
+    // fences keep that order.
+    const RowFrags<T, DP> k(sk, key, lane);
+    Vec8<T> kf[2][2][NS];
+    const auto read = [&](int at, int kk) {
+#pragma unroll
+      for (int b = 0; b < NS; ++b)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) kf[at][x][b] = *(const Vec8<T>*)(k.at + b * 32 * DP + (k.c ^ (2 * (kk + x))) * 8);
+    };
+    read(0, 0);
+#pragma unroll
+    for (int kk = 0; kk < DP / 16; kk += 2) {
+      if (kk + 2 < DP / 16) read(kk / 2 + 1 & 1, kk + 2);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int b = 0; b < NS; ++b) s[b] = mfma(kf[kk / 2 & 1][x][b], q[kk + x], s[b]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (mask) {
+#pragma unroll
+      for (int b = 0; b < NS; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[b][i] = (int32_t)(b * 32 + frag_row(i, lane / 32)) < sees ? s[b][i] : -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NS; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+    mx = max_halves(mx);
+    // The reference follows the maximum only when that is 2^8 ahead: weights up to 256 are as
+    // exact, and sums and output are rescaled rarely.
+    if (__any((mx - m) * c > 8.f || (m == -INFINITY && mx > m))) {
+      const float m1 = fmaxf(m, mx);
+      const float alpha = m == -INFINITY ? 0.f : exp2_((m - m1) * c);
+      l *= alpha;
+#pragma unroll
+      for (int b = 0; b < DP / 32; ++b) o[b] *= alpha;
+      m = m1;
+    }
+    const float base = m == -INFINITY ? 0.f : -m * c;
+    // Weights are multiplied in the tensors' type, as the matrix instruction takes them,
+    // and summed in 32 bits, which lse keeps.
+    float sum[2] = {0.f, 0.f};
+    Vec8<T> pw[2 * NS];
+    const auto weigh = [&](int kb, int i) {
+      const float e = exp2_(__builtin_fmaf(s[kb / 2][kb % 2 * 8 + i], c, base));
+      sum[i & 1] += e;
+      pw[kb][i] = (T)e;
+    };
+    // The weights of 16 keys are computed, and the values of 16 keys read, between the
+    // products of the 16 keys before.
+    Vec8<T> vf[2][DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) vf[0][d] = column_frag<T, DP>(sv, key, d, lane);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) weigh(0, i);
+#pragma unroll
+    for (int kb = 0; kb < 2 * NS; ++kb) {
+      if (kb + 1 < 2 * NS) {
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) vf[kb + 1 & 1][d] = column_frag<T, DP>(sv, key + kb * 16 + 16, d, lane);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        o[d] = mfma(vf[kb & 1][d], pw[kb], o[d]);
+        if (kb + 1 < 2 * NS) {
+#pragma unroll
+          for (int i = d * 8 / (DP / 32); i < (d + 1) * 8 / (DP / 32); ++i) weigh(kb + 1, i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    l += sum[0] + sum[1];
+  }
+};
+
+// 128 rows, 32 a wave.  First without a look at values that are not finite; a workgroup that
+// then finds one among its results computes them again with it (`odd`): 0 times one of them
+// would reach rows that must not see it.
+template <typename T, int DP, bool ODD>
+__device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& sp, uint32_t hq, uint32_t h, T* s_kv) {
+  using L = Tiles<T, DP>;
+  const gts_prompt_args& a = p.a;
+  const uint32_t lane = fresh_lane(), wave = uni(threadIdx.x >> 6), half = lane / 32;
+  const uint32_t r0 = sp.tile * kRows, w0 = r0 + wave * 32, row = w0 + lane % 32;
+  const bool valid = row < sp.n, causal = a.flags & GTS_PROMPT_CAUSAL;
+  const float c = a.scale == 0.f ? 1.f : __builtin_fabsf(a.scale) * kLog2e;
+  Loader<T, DP> ld;
+  ld.a = (const T*)a.k + (int64_t)sp.first * a.k_stride[0] + (int64_t)h * a.k_stride[1];
+  ld.b = (const T*)a.v + (int64_t)sp.first * a.v_stride[0] + (int64_t)h * a.v_stride[1];
+  ld.a_stride = a.k_stride[0];
+  ld.b_stride = a.v_stride[0];
+  ld.n = sp.n;
+  ld.dim = a.dim;
+  ld.start();
+  const uint32_t keys = causal && r0 + kRows < sp.n ? r0 + kRows : sp.n, tiles = (keys + kTile - 1) / kTile;
+  __syncthreads();
+  ld.load(0, wave, s_kv, s_kv + L::N);
+  Rows<T, DP> r;
+  clear(r.o);
+  r.m = -INFINITY;
+  r.l = 0.f;
+  {
+    // scale's sign (and 0) go into the queries: the maximum of q.k is then that of the scores
+    const T sign = (T)(a.scale == 0.f ? 0.f : a.scale < 0.f ? -1.f : 1.f);
+    const T* q = (const T*)a.q + (int64_t)(sp.first + (valid ? row : 0)) * a.q_stride[0] + (int64_t)hq * a.q_stride[1];
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+      const uint32_t at = i * 16 + 8 * half;
+      r.q[i] = *(const Vec8<T>*)(at < a.dim ? q + at : (const T*)g_zeros);
+      if (a.scale <= 0.f) r.q[i] *= sign;
+    }
+  }
+  for (uint32_t t = 0; t < tiles; ++t) {
+    const uint32_t j0 = t * kTile;
+    T *sk = s_kv + (t & 1) * 2 * L::N, *sv = sk + L::N;
+    wait_loads();
+    __syncthreads();
+    if (t + 1 < tiles) {
+      T* next = s_kv + ((t + 1) & 1) * 2 * L::N;
+      ld.load(j0 + kTile, wave, next, next + L::N);
+    }
+    const uint32_t seen = causal && row + 1 < sp.n ? row + 1 : sp.n;  // keys of the lane's row
+    bool odd = false;
+    if constexpr (ODD) {
+      if (causal && j0 + kTile > r0 + 1) {
+        bool found = false;
+        for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) found |= any_not_finite<T>(*(const u32x4*)(sv + x * 8));
+        odd = __syncthreads_or(found);
+        if (odd) {
+          clear_tile<T, L::N>(sv);
+          __syncthreads();
+        }
+      }
+    }
+    // some row of the wave does not see all of the tile; it sees none of it
+    const uint32_t low = causal ? w0 + 1 : sp.n;
+    if (causal && j0 > w0 + 31) continue;
+    const bool mask = j0 + kTile > low || j0 + kTile > sp.n;
+    if constexpr (DP <= 64) {
+      r.template step<2>(lane, sk, sv, 0, c, mask, (int32_t)(seen - j0));
+    } else {
+#pragma unroll 1
+      for (uint32_t x = 0; x < kTile; x += 32) r.template step<1>(fresh_lane(), sk, sv, x, c, mask, (int32_t)(seen - j0 - x));
+    }
+    if constexpr (ODD) {
+      if (odd)
+        for (uint32_t x = 0; x < kTile; x += 32)
+          add_odd<T, DP>(r.o, ld.b, ld.b_stride, j0 + x, sp.n, a.dim, half, false, [&](uint32_t j) { return j < seen; });
+    }
+  }
+  const float l = add_halves(r.l), inv = 1.f / l;
+  bool found = false;
+  if constexpr (!ODD) {
+    if (causal && valid) {
+      float x = 0.f;  // NaN or infinite if one of them is
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x = fmaxf(x, not_finite(r.o[d][i]) ? 1.f : 0.f);
+      found = x > 0.f;
+    }
+    found = __syncthreads_or(found);
+    if (found) return true;
+  } else {
+    __syncthreads();
+  }
+  T* out = (T*)a.out + (int64_t)(sp.first + w0) * a.out_stride[0] + (int64_t)hq * a.out_stride[1];
+  write_rows<T, DP>(s_kv + wave * 32 * (DP + 8), r.o, inv, out, a.out_stride[0], sp.n > w0 ? sp.n - w0 : 0, a.dim, lane);
+  if (a.lse && valid && half == 0)
+    a.lse[(uint64_t)(sp.first + row) * a.q_heads + hq] = l == 0.f ? -INFINITY : (r.m * c + log2f(l)) * kLn2;
+  return false;
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(PromptParams p) {
+  const gts_prompt_args& a = p.a;
+  __shared__ __align__(16) T s_kv[4 * Tiles<T, DP>::N];
+  uint32_t h;
+  const uint32_t hq = head_at(blockIdx.x % a.q_heads, a.kv_heads, p.group, &h);
+  Span sp;
+  // the last tiles of a sequence see the most keys: first
+  const uint32_t place = p.places - 1 - blockIdx.x / a.q_heads;
+  if (!find_span(a.starts, a.batch, a.tokens, kRows, place, &sp)) return;
+  if (!sp.in) {
+    const uint32_t rows = sp.n - sp.tile * kRows < kRows ? sp.n - sp.tile * kRows : kRows, first = sp.first + sp.tile * kRows;
+    for (uint32_t i = threadIdx.x; i < rows * (a.dim / 8); i += 256)
+      *(u32x4*)((T*)a.out + (int64_t)(first + i / (a.dim / 8)) * a.out_stride[0] + (int64_t)hq * a.out_stride[1] +
+                i % (a.dim / 8) * 8) = u32x4{0, 0, 0, 0};
+    if (a.lse)
+      for (uint32_t i = threadIdx.x; i < rows; i += 256) a.lse[(uint64_t)(first + i) * a.q_heads + hq] = -INFINITY;
+    return;
+  }
+  if (prompt_rows<T, DP, false>(p, sp, hq, h, s_kv)) prompt_rows<T, DP, true>(p, sp, hq, h, s_kv);
 }
 
 struct PromptGradParams {
@@ -398,15 +740,25 @@ bool rows_aligned(const void* p, const int64_t* stride, uint32_t e) {
   return (uintptr_t)p % 16 == 0 && (uint64_t)stride[0] * e % 16 == 0 && (uint64_t)stride[1] * e % 16 == 0;
 }
 
+// 16 rows lie within 2 GiB: a tile's offsets have 32 bits.
+bool near(const int64_t* stride) { return stride[0] >= 0 && stride[0] < 1 << 26; }
+
 template <typename T, int DP>
 hipError_t launch_prompt_d(const PromptParams& p, hipStream_t s) {
-  const uint64_t groups = (uint64_t)places_of(p.a.batch, p.a.tokens, kRows) * p.a.q_heads;
-  prompt_kernel<T, DP><<<dim3((uint32_t)groups), dim3(256), 0, s>>>(p);
+  const dim3 grid(p.places * p.a.q_heads), block(256);
+  if constexpr (sizeof(T) == 2) {
+    const gts_prompt_args& a = p.a;
+    if (p.vec && a.dim % 8 == 0 && rows_aligned(a.out, a.out_stride, 2) && near(a.k_stride) && near(a.v_stride)) {
+      prompt_tile_kernel<T, DP><<<grid, block, 0, s>>>(p);
+      return hipGetLastError();
+    }
+  }
+  prompt_kernel<T, DP><<<grid, block, 0, s>>>(p);
   return hipGetLastError();
 }
 template <typename T>
 hipError_t launch_prompt_t(const gts_prompt_args& a, hipStream_t s) {
-  PromptParams p{a, a.q_heads / a.kv_heads, false};
+  PromptParams p{a, a.q_heads / a.kv_heads, places_of(a.batch, a.tokens, kRows), false};
   p.vec = rows_aligned(a.q, a.q_stride, sizeof(T)) && rows_aligned(a.k, a.k_stride, sizeof(T)) &&
           rows_aligned(a.v, a.v_stride, sizeof(T));
   if (a.dim <= 64) return launch_prompt_d<T, 64>(p, s);

@@ -405,11 +405,12 @@ def test_prompt_layouts(dtype, D):
             check_prompt(q, k, v, starts, dout, causal, wrap=wrap)
     # into a given view, the rest as it was
     st = starts.cuda()
-    o = ops.prompt_attention(q.cuda(), k.cuda(), v.cuda(), st)
     wide = torch.full((T, 9, D + 2), 5.0, device="cuda", dtype=dtype)
     view = wide[:, 3:7, :D]
     assert ops.prompt_attention(q.cuda(), k.cuda(), v.cuda(), st, out=view) is view
-    assert torch.equal(view, o)
+    # rows of another alignment may take another kernel: the reference decides
+    ref, _, err, _ = R.prompt(*d64(q, k, v), starts, True, None, dtype)
+    close(view, ref, err, dtype, "a given view")
     wide[:, 3:7, :D] = 5.0
     assert (wide == 5.0).all()
     one = k[:, :1].cuda().expand(T, 2, D)
