@@ -551,6 +551,15 @@ __device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& s
   return false;
 }
 
+// Zeros to the rows of a tile that is in no sequence.
+template <typename T>
+__device__ __forceinline__ void zero_rows(T* out, const int64_t* stride, const Span& sp, uint32_t head, uint32_t dim) {
+  const uint32_t rows = sp.n - sp.tile * kRows < kRows ? sp.n - sp.tile * kRows : kRows, first = sp.first + sp.tile * kRows;
+  for (uint32_t i = threadIdx.x; i < rows * (dim / 8); i += 256)
+    *(u32x4*)(out + (int64_t)(first + i / (dim / 8)) * stride[0] + (int64_t)head * stride[1] + i % (dim / 8) * 8) =
+        u32x4{0, 0, 0, 0};
+}
+
 template <typename T, int DP>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(PromptParams p) {
   const gts_prompt_args& a = p.a;
@@ -562,12 +571,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
   const uint32_t place = p.places - 1 - blockIdx.x / a.q_heads;
   if (!find_span(a.starts, a.batch, a.tokens, kRows, place, &sp)) return;
   if (!sp.in) {
-    const uint32_t rows = sp.n - sp.tile * kRows < kRows ? sp.n - sp.tile * kRows : kRows, first = sp.first + sp.tile * kRows;
-    for (uint32_t i = threadIdx.x; i < rows * (a.dim / 8); i += 256)
-      *(u32x4*)((T*)a.out + (int64_t)(first + i / (a.dim / 8)) * a.out_stride[0] + (int64_t)hq * a.out_stride[1] +
-                i % (a.dim / 8) * 8) = u32x4{0, 0, 0, 0};
+    zero_rows((T*)a.out, a.out_stride, sp, hq, a.dim);
+    const uint32_t first = sp.tile * kRows;
     if (a.lse)
-      for (uint32_t i = threadIdx.x; i < rows; i += 256) a.lse[(uint64_t)(first + i) * a.q_heads + hq] = -INFINITY;
+      for (uint32_t i = first + threadIdx.x; i < sp.n && i < first + kRows; i += 256)
+        a.lse[(uint64_t)(sp.first + i) * a.q_heads + hq] = -INFINITY;
     return;
   }
   if (prompt_rows<T, DP, false>(p, sp, hq, h, s_kv)) prompt_rows<T, DP, true>(p, sp, hq, h, s_kv);
@@ -576,24 +584,39 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
 struct PromptGradParams {
   gts_prompt_grad_args a;
   uint32_t group;
+  uint32_t places;
   bool vec;      // rows of dout, q, k and v are aligned to 16 bytes
-  float* delta;  // [tokens][q_heads]
+  // [q_heads][tokens]: a head's values side by side; lse in base 2
+  float *lse, *delta;
+  __device__ __forceinline__ uint64_t stat(uint32_t head, uint32_t token) const { return (uint64_t)head * a.tokens + token; }
 };
 
-// delta: a wave per row.
+// delta, and lse in base 2: 64 tokens of a head a workgroup, 16 lanes a row.
 template <typename T>
-__global__ __launch_bounds__(256) void delta_kernel(PromptGradParams p) {
+__global__ __launch_bounds__(256) void stats_kernel(PromptGradParams p, bool vec) {
   const gts_prompt_grad_args& a = p.a;
-  const uint64_t row = block_number() * 4 + (threadIdx.x >> 6);
-  if (row >= (uint64_t)a.tokens * a.q_heads) return;
-  const uint32_t t = (uint32_t)(row / a.q_heads), h = (uint32_t)(row % a.q_heads), lane = threadIdx.x & 63u;
-  const T* x = (const T*)a.dout + (int64_t)t * a.dout_stride[0] + (int64_t)h * a.dout_stride[1];
-  const T* y = (const T*)a.out + (int64_t)t * a.out_stride[0] + (int64_t)h * a.out_stride[1];
-  float sum = 0.f;
-  for (uint32_t d = lane; d < a.dim; d += 64) sum += (float)x[d] * (float)y[d];
+  const uint32_t h = blockIdx.x % a.q_heads, t0 = blockIdx.x / a.q_heads * 64, lane = threadIdx.x & 63u;
+  const uint32_t sub = lane / 16, li = lane % 16;
 #pragma unroll
-  for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i);
-  if (lane == 0) p.delta[row] = sum;
+  for (uint32_t i = 0; i < 4; ++i) {
+    const uint32_t t = t0 + (threadIdx.x >> 6) * 16 + i * 4 + sub;
+    float sum = 0.f;
+    if (t < a.tokens) {
+      const T* x = (const T*)a.dout + (int64_t)t * a.dout_stride[0] + (int64_t)h * a.dout_stride[1];
+      const T* y = (const T*)a.out + (int64_t)t * a.out_stride[0] + (int64_t)h * a.out_stride[1];
+      for (uint32_t d = li * 8; d < a.dim; d += 128) {
+        const Vec8<T> u = load8(x + d, (int64_t)a.dim - d, vec), v = load8(y + d, (int64_t)a.dim - d, vec);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += (float)u[j] * (float)v[j];
+      }
+    }
+#pragma unroll
+    for (int k = 8; k; k >>= 1) sum += __shfl_xor(sum, k);
+    if (li == 0 && t < a.tokens) {
+      p.delta[p.stat(h, t)] = sum;
+      p.lse[p.stat(h, t)] = a.lse[(uint64_t)t * a.q_heads + h] * kLog2e;
+    }
+  }
 }
 
 template <typename T, int DP>
@@ -621,8 +644,8 @@ __global__ __launch_bounds__(256) void dq_kernel(PromptGradParams p) {
   const uint32_t keys = causal && r0 + kRows < sp.n ? r0 + kRows : sp.n;
   const uint32_t sees = !valid ? 0 : causal ? row + 1 : sp.n;
   const float c = a.scale * kLog2e;
-  const float lse = valid ? a.lse[(uint64_t)token * a.q_heads + hq] * kLog2e : 0.f;
-  const float delta = valid ? p.delta[(uint64_t)token * a.q_heads + hq] : 0.f;
+  const float lse = valid ? p.lse[p.stat(hq, token)] : 0.f;
+  const float delta = valid ? p.delta[p.stat(hq, token)] : 0.f;
   for (uint32_t j0 = 0; j0 < keys; j0 += kStep) {
     const bool edge = causal && j0 + kStep > r0 + 1;
     __syncthreads();
@@ -655,7 +678,7 @@ __global__ __launch_bounds__(256) void dq_kernel(PromptGradParams p) {
   if (valid) write_row<T, DP>(dq, o, a.scale, a.dim, half);
 }
 
-// WHAT: 1 dv, 2 dk, 3 both (32 bits with heads of 256 have no registers for both).
+// WHAT: 1 dv, 2 dk, 3 both.
 template <typename T, int DP, int WHAT>
 __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
   const gts_prompt_grad_args& a = p.a;
@@ -691,8 +714,8 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
         stage_rows<T, DP>(dout, a.dout_stride[0], i0, sp.n, a.dim, p.vec, false, s_o);
         if (threadIdx.x < kStep) {
           const bool in = i0 + threadIdx.x < sp.n;
-          const uint64_t at = (uint64_t)(sp.first + i0 + threadIdx.x) * a.q_heads + hq;
-          s_lse[threadIdx.x] = in ? a.lse[at] * kLog2e : 0.f;
+          const uint64_t at = p.stat(hq, sp.first + i0 + threadIdx.x);
+          s_lse[threadIdx.x] = in ? p.lse[at] : 0.f;
           s_delta[threadIdx.x] = in ? p.delta[at] : 0.f;
         }
         __syncthreads();
@@ -736,6 +759,356 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
   if constexpr (kK) write_row<T, DP>(dk, ok, a.scale, a.dim, half);
 }
 
+// ---- the gradient's tile kernels -------------------------------------------------------------
+// As prompt_tile_kernel: values that are not finite are looked for only where a result has one.
+// Masked scores are -inf then; with `odd` masked weights and their gradients are 0 whatever the
+// row's statistics are.
+template <int N>
+__device__ __forceinline__ bool any_odd(const f32x16 (&o)[N]) {
+  bool found = false;
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) found |= not_finite(o[d][i]);
+  return found;
+}
+
+template <typename T, int DP, bool ODD>
+__device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& sp, uint32_t hq, uint32_t h, T* s_kv) {
+  using L = Tiles<T, DP>;
+  const gts_prompt_grad_args& a = p.a;
+  const uint32_t lane = fresh_lane(), wave = uni(threadIdx.x >> 6), half = lane / 32;
+  const uint32_t r0 = sp.tile * kRows, w0 = r0 + wave * 32, row = w0 + lane % 32, there = row < sp.n ? row : 0;
+  const bool valid = row < sp.n, causal = a.flags & GTS_PROMPT_CAUSAL;
+  const float c = a.scale * kLog2e;
+  Loader<T, DP> ld;
+  ld.a = (const T*)a.k + (int64_t)sp.first * a.k_stride[0] + (int64_t)h * a.k_stride[1];
+  ld.b = (const T*)a.v + (int64_t)sp.first * a.v_stride[0] + (int64_t)h * a.v_stride[1];
+  ld.a_stride = a.k_stride[0];
+  ld.b_stride = a.v_stride[0];
+  ld.n = sp.n;
+  ld.dim = a.dim;
+  ld.start();
+  const uint32_t keys = causal && r0 + kRows < sp.n ? r0 + kRows : sp.n, tiles = (keys + kTile - 1) / kTile;
+  __syncthreads();
+  ld.load(0, wave, s_kv, s_kv + L::N);
+  Vec8<T> q[DP / 16], dout[DP / 16];
+  const T* qp = (const T*)a.q + (int64_t)(sp.first + there) * a.q_stride[0] + (int64_t)hq * a.q_stride[1];
+  const T* op = (const T*)a.dout + (int64_t)(sp.first + there) * a.dout_stride[0] + (int64_t)hq * a.dout_stride[1];
+#pragma unroll
+  for (int i = 0; i < DP / 16; ++i) {
+    const uint32_t at = i * 16 + 8 * half;
+    q[i] = *(const Vec8<T>*)(at < a.dim ? qp + at : (const T*)g_zeros);
+    dout[i] = *(const Vec8<T>*)(at < a.dim ? op + at : (const T*)g_zeros);
+  }
+  const float lse = p.lse[p.stat(hq, sp.first + there)], delta = p.delta[p.stat(hq, sp.first + there)];
+  f32x16 o[DP / 32];
+  clear(o);
+  for (uint32_t t = 0; t < tiles; ++t) {
+    const uint32_t j0 = t * kTile;
+    T *sk = s_kv + (t & 1) * 2 * L::N, *sv = sk + L::N;
+    wait_loads();
+    __syncthreads();
+    if (t + 1 < tiles) {
+      T* next = s_kv + ((t + 1) & 1) * 2 * L::N;
+      ld.load(j0 + kTile, wave, next, next + L::N);
+    }
+    const uint32_t seen = causal && row + 1 < sp.n ? row + 1 : sp.n;
+    const bool edge = causal && j0 + kTile > r0 + 1;
+    if (!ODD && causal && j0 > w0 + 31) continue;  // the wave sees none of it
+    const bool mask = j0 + kTile > (causal ? w0 + 1 : sp.n) || j0 + kTile > sp.n;
+    const auto weigh = [&](uint32_t x, f32x16& s, const f32x16& dp) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const bool hidden = mask && j0 + x + frag_row(i, half) >= seen;
+        if (!ODD && hidden) s[i] = -INFINITY;
+        s[i] = exp2_(__builtin_fmaf(s[i], c, -lse)) * (dp[i] - delta);
+        if (ODD && hidden) s[i] = 0.f;
+      }
+    };
+    const auto scores = [&](uint32_t x, f32x16& s, f32x16& dp) {
+      const RowFrags<T, DP> k(sk, x, fresh_lane()), v(sv, x, fresh_lane());
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
+      Vec8<T> f[2][2];
+      f[0][0] = k(0);
+      f[0][1] = v(0);
+#pragma unroll
+      for (int kk = 0; kk < DP / 16; ++kk) {
+        if (kk + 1 < DP / 16) {
+          f[kk + 1 & 1][0] = k(kk + 1);
+          f[kk + 1 & 1][1] = v(kk + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        s = mfma(f[kk & 1][0], q[kk], s);
+        dp = mfma(f[kk & 1][1], dout[kk], dp);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    const auto add = [&](uint32_t x, const f32x16& ds) {
+      Vec8<T> u[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) u[i / 8][i % 8] = (T)ds[i];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) o[d] = mfma(column_frag<T, DP>(sk, x + k * 16, d, lane), u[k], o[d]);
+    };
+    if constexpr (!ODD) {
+#pragma unroll 1
+      for (uint32_t x = 0; x < kTile; x += 32) {
+        f32x16 s, dp;
+        scores(x, s, dp);
+        if (mask) {
+          weigh(x, s, dp);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = exp2_(__builtin_fmaf(s[i], c, -lse)) * (dp[i] - delta);
+        }
+        add(x, s);
+      }
+    } else {
+      f32x16 s[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        f32x16 dp;
+        scores(x * 32, s[x], dp);
+        weigh(x * 32, s[x], dp);
+      }
+      bool odd = false;
+      if (edge) {
+        bool found = false;
+        for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) found |= any_not_finite<T>(*(const u32x4*)(sk + x * 8));
+        odd = __syncthreads_or(found);
+        if (odd) {
+          clear_tile<T, L::N>(sk);
+          __syncthreads();
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        add(x * 32, s[x]);
+        if (odd)
+          add_odd<T, DP>(o, ld.a, ld.a_stride, j0 + x * 32, sp.n, a.dim, half, true, [&](uint32_t j) { return j < seen; });
+      }
+    }
+  }
+  if constexpr (!ODD) {
+    if (__syncthreads_or(causal && valid && any_odd(o))) return true;
+  } else {
+    __syncthreads();
+  }
+  T* out = (T*)a.dq + (int64_t)(sp.first + w0) * a.dq_stride[0] + (int64_t)hq * a.dq_stride[1];
+  write_rows<T, DP>(s_kv + wave * 32 * (DP + 8), o, a.scale, out, a.dq_stride[0], sp.n > w0 ? sp.n - w0 : 0, a.dim, lane);
+  return false;
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dq_tile_kernel(PromptGradParams p) {
+  const gts_prompt_grad_args& a = p.a;
+  __shared__ __align__(16) T s_kv[4 * Tiles<T, DP>::N];
+  uint32_t h;
+  const uint32_t hq = head_at(blockIdx.x % a.q_heads, a.kv_heads, p.group, &h);
+  Span sp;
+  if (!find_span(a.starts, a.batch, a.tokens, kRows, p.places - 1 - blockIdx.x / a.q_heads, &sp)) return;
+  if (!sp.in) {
+    zero_rows((T*)a.dq, a.dq_stride, sp, hq, a.dim);
+    return;
+  }
+  if (dq_rows<T, DP, false>(p, sp, hq, h, s_kv)) dq_rows<T, DP, true>(p, sp, hq, h, s_kv);
+}
+
+// 4 bytes a lane from memory to LDS, as load_to_lds.
+__device__ __forceinline__ void load_to_lds4(const void* from, void* to) {
+  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)to;
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, off\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
+               : "s"(at), "v"(from)
+               : "memory");
+}
+
+// 128 keys, 32 a wave; all rows that see them, of all query heads of the key-value head, 64 at
+// a time in two blocks: the first block's weights are computed between the products of the
+// second's scores, and the second's between the products of the first's sums.  So a wave by
+// itself keeps the matrix unit busy, and may take all registers of its SIMD: keys, values and both
+// sums stay in them.
+template <typename T, int DP, int WHAT, bool ODD>
+__device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& sp, uint32_t h, T* s_qo,
+                                         float (*s_stat)[2][kTile]) {
+  using L = Tiles<T, DP>;
+  constexpr bool kV = WHAT & 1, kK = WHAT & 2;
+  constexpr int KK = DP / 16, MB = DP / 32;
+  const gts_prompt_grad_args& a = p.a;
+  const uint32_t lane = fresh_lane(), wave = uni(threadIdx.x >> 6), half = lane / 32;
+  const uint32_t k0 = sp.tile * kRows, w0 = k0 + wave * 32, key = w0 + lane % 32, there = key < sp.n ? key : 0;
+  const bool valid = key < sp.n, causal = a.flags & GTS_PROMPT_CAUSAL;
+  const float c = a.scale * kLog2e;
+  Loader<T, DP> ld;
+  ld.a_stride = a.q_stride[0];
+  ld.b_stride = a.dout_stride[0];
+  ld.n = sp.n;
+  ld.dim = a.dim;
+  ld.start();
+  const uint32_t first = causal ? k0 / kTile : 0, tiles = (sp.n + kTile - 1) / kTile;
+  const auto load = [&](uint32_t g, uint32_t t, uint32_t buffer) {
+    const uint32_t hq = h * p.group + g;
+    ld.a = (const T*)a.q + (int64_t)sp.first * a.q_stride[0] + (int64_t)hq * a.q_stride[1];
+    ld.b = (const T*)a.dout + (int64_t)sp.first * a.dout_stride[0] + (int64_t)hq * a.dout_stride[1];
+    T* to = s_qo + buffer * 2 * L::N;
+    ld.load(t * kTile, wave, to, to + L::N);
+    if (wave < 2) {  // statistics: a wave each
+      const uint32_t i = t * kTile + fresh_lane();
+      const float* from = (wave ? p.delta : p.lse) + p.stat(hq, sp.first + i);
+      load_to_lds4(i < sp.n ? from : (const float*)g_zeros, s_stat[buffer][wave]);
+    }
+  };
+  __syncthreads();
+  load(0, first, 0);
+  Vec8<T> k[KK], v[kK ? KK : 1];
+  const T* kp = (const T*)a.k + (int64_t)(sp.first + there) * a.k_stride[0] + (int64_t)h * a.k_stride[1];
+  const T* vp = (const T*)a.v + (int64_t)(sp.first + there) * a.v_stride[0] + (int64_t)h * a.v_stride[1];
+#pragma unroll
+  for (int i = 0; i < KK; ++i) {
+    const uint32_t at = i * 16 + 8 * half;
+    k[i] = *(const Vec8<T>*)(at < a.dim ? kp + at : (const T*)g_zeros);
+    if constexpr (kK) v[i] = *(const Vec8<T>*)(at < a.dim ? vp + at : (const T*)g_zeros);
+  }
+  f32x16 ok[kK ? MB : 1], ov[kV ? MB : 1];
+  clear(ok);
+  clear(ov);
+  uint32_t buffer = 0;
+  for (uint32_t g = 0; g < p.group; ++g)
+    for (uint32_t t = first; t < tiles; ++t, buffer ^= 1) {
+      const uint32_t i0 = t * kTile;
+      T *sq = s_qo + buffer * 2 * L::N, *so = sq + L::N;
+      wait_loads();
+      __syncthreads();
+      if (t + 1 < tiles)
+        load(g, t + 1, buffer ^ 1);
+      else if (g + 1 < p.group)
+        load(g + 1, first, buffer ^ 1);
+      if (!ODD && causal && i0 + kTile <= w0) continue;  // no row of it sees a key of the wave
+      const bool mask = (causal && i0 < w0 + 31) || i0 + kTile > sp.n;
+      f32x16 s[2], ds[2];
+      Vec8<T> pu[2][2], du[2][2];
+      // two products of block b: the fragments of a step are read while the one before is multiplied
+      Vec8<T> f[2][2];
+      const auto read = [&](int b, int kk) {
+        const uint32_t fl = fresh_lane();
+        f[kk & 1][0] = RowFrags<T, DP>(sq, b * 32, fl)(kk);
+        if constexpr (kK) f[kk & 1][1] = RowFrags<T, DP>(so, b * 32, fl)(kk);
+      };
+      const auto product = [&](int b, int kk) {
+        s[b] = mfma(f[kk & 1][0], k[kk], s[b]);
+        if constexpr (kK) ds[b] = mfma(f[kk & 1][1], v[kk], ds[b]);
+      };
+      const auto weigh = [&](int b, int i) {
+        const uint32_t r = b * 32 + frag_row(i, half);
+        float x = s[b][i];
+        const bool hidden = (causal && i0 + r < key) || i0 + r >= sp.n;
+        if (!ODD && mask) x = hidden ? -INFINITY : x;
+        x = exp2_(__builtin_fmaf(x, c, -s_stat[buffer][0][r]));
+        if (ODD) x = hidden ? 0.f : x;
+        pu[b][i / 8][i % 8] = (T)x;
+        if constexpr (kK) {
+          x *= ds[b][i] - s_stat[buffer][1][r];
+          if (ODD) x = hidden ? 0.f : x;
+          du[b][i / 8][i % 8] = (T)x;
+        }
+      };
+      const auto sum = [&](int b, int d, int x) {
+        if constexpr (kV) ov[d] = mfma(column_frag<T, DP>(so, b * 32 + x * 16, d, lane), pu[b][x], ov[d]);
+        if constexpr (kK) ok[d] = mfma(column_frag<T, DP>(sq, b * 32 + x * 16, d, lane), du[b][x], ok[d]);
+      };
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] = ds[b][i] = 0.f;
+      read(0, 0);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        if (kk + 1 < KK) read(0, kk + 1);
+        product(0, kk);
+      }
+      read(1, 0);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        if (kk + 1 < KK) read(1, kk + 1);
+        product(1, kk);
+#pragma unroll
+        for (int i = kk * 16 / KK; i < (kk + 1) * 16 / KK; ++i) weigh(0, i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      bool odd = false;
+      if constexpr (ODD) {
+        if (causal && i0 + 1 < k0 + kRows) {
+          bool found = false;
+          for (uint32_t x = threadIdx.x; x < L::N / 4; x += 256) found |= any_not_finite<T>(*(const u32x4*)(sq + x * 8));
+          odd = __syncthreads_or(found);  // and every wave has its scores
+          if (odd) {
+            clear_tile<T, 2 * L::N>(sq);
+            __syncthreads();
+          }
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < MB; ++d)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          sum(0, d, x);
+#pragma unroll
+          for (int i = (d * 2 + x) * 16 / (2 * MB); i < (d * 2 + x + 1) * 16 / (2 * MB); ++i) weigh(1, i);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+      for (int d = 0; d < MB; ++d)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) sum(1, d, x);
+      if constexpr (ODD) {
+        if (odd) {
+          const uint32_t hq = h * p.group + g;
+          const T* qp = (const T*)a.q + (int64_t)sp.first * a.q_stride[0] + (int64_t)hq * a.q_stride[1];
+          const T* op = (const T*)a.dout + (int64_t)sp.first * a.dout_stride[0] + (int64_t)hq * a.dout_stride[1];
+          const auto sees = [&](uint32_t row) { return key <= row; };
+          for (uint32_t x = 0; x < kTile; x += 32) {
+            if constexpr (kV) add_odd<T, DP>(ov, op, a.dout_stride[0], i0 + x, sp.n, a.dim, half, false, sees);
+            if constexpr (kK) add_odd<T, DP>(ok, qp, a.q_stride[0], i0 + x, sp.n, a.dim, half, true, sees);
+          }
+        }
+      }
+    }
+  if constexpr (!ODD) {
+    if (__syncthreads_or(causal && valid && (any_odd(ok) || any_odd(ov)))) return true;
+  } else {
+    __syncthreads();
+  }
+  T* s = s_qo + wave * 32 * (DP + 8);
+  const uint32_t rows = sp.n > w0 ? sp.n - w0 : 0;
+  T* dk = (T*)a.dk + (int64_t)(sp.first + w0) * a.dk_stride[0] + (int64_t)h * a.dk_stride[1];
+  T* dv = (T*)a.dv + (int64_t)(sp.first + w0) * a.dv_stride[0] + (int64_t)h * a.dv_stride[1];
+  if constexpr (kV) write_rows<T, DP>(s, ov, 1.f, dv, a.dv_stride[0], rows, a.dim, lane);
+  asm volatile("" ::: "memory");
+  if constexpr (kK) write_rows<T, DP>(s, ok, a.scale, dk, a.dk_stride[0], rows, a.dim, lane);
+  return false;
+}
+
+template <typename T, int DP, int WHAT>
+__global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void dkv_tile_kernel(PromptGradParams p) {
+  const gts_prompt_grad_args& a = p.a;
+  __shared__ __align__(16) T s_qo[4 * Tiles<T, DP>::N];
+  __shared__ __align__(16) float s_stat[2][2][kTile];
+  const uint32_t h = blockIdx.x % a.kv_heads;
+  Span sp;
+  if (!find_span(a.starts, a.batch, a.tokens, kRows, blockIdx.x / a.kv_heads, &sp)) return;
+  if (!sp.in) {
+    if (WHAT & 1) zero_rows((T*)a.dv, a.dv_stride, sp, h, a.dim);
+    if (WHAT & 2) zero_rows((T*)a.dk, a.dk_stride, sp, h, a.dim);
+    return;
+  }
+  if (dkv_keys<T, DP, WHAT, false>(p, sp, h, s_qo, s_stat)) dkv_keys<T, DP, WHAT, true>(p, sp, h, s_qo, s_stat);
+}
+
 bool rows_aligned(const void* p, const int64_t* stride, uint32_t e) {
   return (uintptr_t)p % 16 == 0 && (uint64_t)stride[0] * e % 16 == 0 && (uint64_t)stride[1] * e % 16 == 0;
 }
@@ -769,20 +1142,35 @@ hipError_t launch_prompt_t(const gts_prompt_args& a, hipStream_t s) {
 template <typename T, int DP>
 hipError_t launch_prompt_grad_d(const PromptGradParams& p, hipStream_t s) {
   const gts_prompt_grad_args& a = p.a;
-  const uint32_t places = places_of(a.batch, a.tokens, kRows);
-  delta_kernel<T><<<grid_of(((uint64_t)a.tokens * a.q_heads + 3) / 4), dim3(256), 0, s>>>(p);
-  dq_kernel<T, DP><<<dim3(places * a.q_heads), dim3(256), 0, s>>>(p);
-  if constexpr (sizeof(T) == 4 && DP == 256) {
-    dkv_kernel<T, DP, 1><<<dim3(places * a.kv_heads), dim3(256), 0, s>>>(p);
-    dkv_kernel<T, DP, 2><<<dim3(places * a.kv_heads), dim3(256), 0, s>>>(p);
+  const dim3 rows(p.places * a.q_heads), keys(p.places * a.kv_heads), block(256);
+  const bool out_vec = p.vec && rows_aligned(a.out, a.out_stride, sizeof(T));
+  stats_kernel<T><<<dim3((a.tokens + 63) / 64 * a.q_heads), block, 0, s>>>(p, out_vec);
+  if constexpr (sizeof(T) == 2) {
+    if (p.vec && a.dim % 8 == 0 && rows_aligned(a.dq, a.dq_stride, 2) && rows_aligned(a.dk, a.dk_stride, 2) &&
+        rows_aligned(a.dv, a.dv_stride, 2) && near(a.k_stride) && near(a.v_stride) && near(a.q_stride) && near(a.dout_stride)) {
+      dq_tile_kernel<T, DP><<<rows, block, 0, s>>>(p);
+      if constexpr (DP == 256) {
+        dkv_tile_kernel<T, DP, 1><<<keys, block, 0, s>>>(p);
+        dkv_tile_kernel<T, DP, 2><<<keys, block, 0, s>>>(p);
+      } else {
+        dkv_tile_kernel<T, DP, 3><<<keys, block, 0, s>>>(p);
+      }
+      return hipGetLastError();
+    }
+  }
+  dq_kernel<T, DP><<<rows, block, 0, s>>>(p);
+  if constexpr (DP == 256) {  // no registers for both
+    dkv_kernel<T, DP, 1><<<keys, block, 0, s>>>(p);
+    dkv_kernel<T, DP, 2><<<keys, block, 0, s>>>(p);
   } else {
-    dkv_kernel<T, DP, 3><<<dim3(places * a.kv_heads), dim3(256), 0, s>>>(p);
+    dkv_kernel<T, DP, 3><<<keys, block, 0, s>>>(p);
   }
   return hipGetLastError();
 }
 template <typename T>
 hipError_t launch_prompt_grad_t(const gts_prompt_grad_args& a, hipStream_t s) {
-  PromptGradParams p{a, a.q_heads / a.kv_heads, false, (float*)a.scratch};
+  PromptGradParams p{a, a.q_heads / a.kv_heads, places_of(a.batch, a.tokens, kRows), false, (float*)a.scratch,
+                     (float*)a.scratch + (uint64_t)a.tokens * a.q_heads};
   p.vec = rows_aligned(a.q, a.q_stride, sizeof(T)) && rows_aligned(a.k, a.k_stride, sizeof(T)) &&
           rows_aligned(a.v, a.v_stride, sizeof(T)) && rows_aligned(a.dout, a.dout_stride, sizeof(T));
   if (a.dim <= 64) return launch_prompt_grad_d<T, 64>(p, s);
@@ -803,7 +1191,7 @@ hipError_t launch_prompt(const gts_prompt_args& a, hipStream_t s) {
 }
 
 uint64_t prompt_grad_scratch(uint32_t batch, uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t dim) {
-  return 4ull * tokens * q_heads;
+  return 8ull * tokens * q_heads;
 }
 
 hipError_t launch_prompt_grad(const gts_prompt_grad_args& a, hipStream_t s) {
