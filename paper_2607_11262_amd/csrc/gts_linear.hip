@@ -54,6 +54,7 @@ struct MatmulParams {
   bool a_vec, b_vec;   // rows aligned to 16 bytes
   uint32_t splits;     // of the sum; more than one: the parts go to the scratch
   uint32_t k_split;    // places of a split
+  bool wide;           // eight values of a result, its bias, gate and residual are 16 bytes
 };
 
 // What becomes of z = the whole sum of (m, n).
@@ -201,6 +202,235 @@ __global__ __launch_bounds__(256) void join_splits_kernel(MatmulParams p, FastDi
   finish<T>(a, m, (uint32_t)(i - (uint64_t)m * a.n), z);
 }
 
+// ---- the tile kernel ---------------------------------------------------------------------
+// 16-bit operands whose rows are aligned to 16 bytes.  Stages of 32 places of the sum go
+// straight to LDS, four of them in turn: while one is multiplied, the fragments of the next are
+// read and those behind it are on their way, so that matrix instructions wait for neither;
+// one barrier a stage.
+constexpr uint32_t kStage = 32;
+constexpr int kStages = 4;
+
+__device__ __align__(16) const uint32_t g_nothing[4] = {};  // 16 bytes of zeros
+
+// An operand's ROWS rows, 32 places a stage, loaded by W waves.  In LDS chunk c (16 bytes) of
+// a row stands at c ^ swizzle, so that the reads of a fragment touch all 64 banks once.
+template <typename T, bool COLUMNS, int ROWS, int W>
+struct Operand {
+  static constexpr int C = COLUMNS ? ROWS / 8 : 4;          // chunks of a row of LDS
+  static constexpr int N = ROWS * kStage / 8 / (64 * W);    // loads of a wave
+  static constexpr int SIZE = ROWS * kStage;                // values of a stage
+  static_assert(ROWS * kStage / 8 % (64 * W) == 0 && (!COLUMNS || C >= 16), "whole loads");
+  static __device__ __forceinline__ uint32_t swizzle(uint32_t r) {
+    return COLUMNS ? ((r & 3) << 2) | ((r >> 2) & 3) : (r >> 2) & 3;
+  }
+  const char* base;   // of the tile's first value, the stage's first place
+  int64_t step;       // bytes from a stage to the next
+  uint32_t off[N];    // bytes to this lane's chunk
+  uint32_t chunk[N];  // its place in the stage (rows: the first of 8)
+
+  // Rows past the operand's end are its last ones again (whole chunks of them, if it is stored
+  // by columns): what they give is not stored.
+  __device__ __forceinline__ void start(const void* p, int64_t stride, uint32_t r0, uint32_t rows, uint32_t k0,
+                                        uint32_t wave) {
+    const uint32_t lane = threadIdx.x & 63u;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t id = (wave * N + i) * 64 + lane, r = id / C, c = id % C ^ swizzle(r);
+      if constexpr (COLUMNS) {
+        const uint32_t m = r0 + c * 8 + 8 <= rows ? c * 8 : rows - 8 - r0;
+        off[i] = 2 * (r * (uint32_t)stride + m);
+        chunk[i] = r;
+      } else {
+        const uint32_t m = r0 + r < rows ? r : rows - 1 - r0;
+        off[i] = 2 * (m * (uint32_t)stride + c * 8);
+        chunk[i] = c * 8;
+      }
+    }
+    base = (const char*)((const T*)p + (COLUMNS ? (int64_t)k0 * stride + r0 : (int64_t)r0 * stride + k0));
+    step = COLUMNS ? 2 * kStage * stride : 2 * kStage;
+  }
+  // left: places from the stage's first on; those past it are zeros.
+  __device__ __forceinline__ void load(T* s, uint32_t wave, uint32_t left) {
+    if (left >= kStage) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) load_to_lds(base, off[i], s + (wave * N + i) * 512);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        load_to_lds(chunk[i] < left ? (const void*)(base + off[i]) : (const void*)g_nothing, s + (wave * N + i) * 512);
+    }
+    base += step;
+  }
+  // Rows row + lane % 32, places 16 kk + 8 half ..
+  static __device__ __forceinline__ Vec8<T> frag(const T* s, uint32_t row, int kk, uint32_t lane) {
+    if constexpr (COLUMNS) {
+      typedef __attribute__((address_space(3))) i16x4* lds_t;
+      const uint32_t k = kk * 16 + lane / 32 * 8 + lane % 16 / 4, c = row / 8 + lane / 16 % 2 * 2 + lane % 4 / 2;
+      union {
+        i16x4 h[2];
+        Vec8<T> v;
+      } u;
+      const T* at = s + k * ROWS + lane % 2 * 4;
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(at + (c ^ swizzle(k)) * 8));
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(at + 4 * ROWS + (c ^ swizzle(k + 4)) * 8));
+      return u.v;
+    } else {
+      const uint32_t r = row + lane % 32;
+      return *(const Vec8<T>*)(s + r * kStage + ((2 * kk + lane / 32) ^ swizzle(r)) * 8);
+    }
+  }
+};
+
+// Eight values of a row at once; `wide`: everything is aligned to that.
+template <typename T>
+__device__ __forceinline__ void finish8(const gts_matmul_args& a, uint32_t m, uint32_t n, const float* zs, bool wide) {
+  if (!wide) {
+    for (uint32_t i = 0; i < 8 && n + i < a.n; ++i) finish<T>(a, m, n + i, zs[i]);
+    return;
+  }
+  float z[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) z[i] = zs[i];
+  if (a.bias) {
+    const Pack<T, 8> b = *(const Pack<T, 8>*)((const T*)a.bias + n);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] += (float)b.v[i];
+  }
+  Pack<T, 8> y;
+  if (a.preact) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y.v[i] = (T)z[i];
+    *(Pack<T, 8>*)((T*)a.preact + (int64_t)m * a.preact_stride + n) = y;
+  }
+  if (a.activation != GTS_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = activate(a.activation, z[i]);
+  }
+  if (a.gate) {
+    const Pack<T, 8> g = *(const Pack<T, 8>*)((const T*)a.gate + (int64_t)m * a.gate_stride + n);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] *= (float)g.v[i];
+  }
+  if (a.residual) {
+    const Pack<T, 8> r = *(const Pack<T, 8>*)((const T*)a.residual + (int64_t)m * a.residual_stride + n);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] += (float)r.v[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y.v[i] = (T)z[i];
+  *(Pack<T, 8>*)((T*)a.out + (int64_t)m * a.out_stride + n) = y;
+}
+
+// WR x WC waves, MB x NB blocks of 32 x 32 each.
+template <typename T, bool AC, bool BC, int WR, int WC, int MB, int NB>
+__global__ __launch_bounds__(WR * WC * 64, WR * WC == 8 ? 2 : 2) void tile_kernel(MatmulParams p) {
+  constexpr int W = WR * WC;
+  constexpr uint32_t TM = WR * MB * 32, TN = WC * NB * 32;
+  typedef Operand<T, AC, TM, W> OA;
+  typedef Operand<T, BC, TN, W> OB;
+  constexpr int kLoads = OA::N + OB::N;
+  const gts_matmul_args& a = p.a;
+  __shared__ __align__(16) T s_ab[kStages * (OA::SIZE + OB::SIZE)];
+  const uint32_t lane = threadIdx.x & 63u, wave = uni(threadIdx.x >> 6);
+  // Workgroups go round the eight XCDs: each takes a run of the tiles, in columns of eight, so
+  // that those at work at one time share rows of both operands in its L2.
+  const uint32_t tiles_m = (a.m + TM - 1) / TM, tiles_n = (a.n + TN - 1) / TN;
+  const uint32_t xcd = blockIdx.x & 7u, share = gridDim.x / 8, extra = gridDim.x % 8;
+  const uint32_t id = xcd * share + (xcd < extra ? xcd : extra) + (blockIdx.x >> 3);
+  const uint32_t split = id / (tiles_m * tiles_n), tile = id - split * (tiles_m * tiles_n);
+  const uint32_t band = tile / (8 * tiles_n), in = tile - band * 8 * tiles_n;
+  const uint32_t height = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
+  const uint32_t m0 = (band * 8 + in % height) * TM, n0 = in / height * TN;
+  const uint32_t wm = wave / WC * MB * 32, wn = wave % WC * NB * 32;
+  const uint64_t k_first = (uint64_t)split * p.k_split;
+  const uint32_t places = k_first >= a.k ? 0 : a.k - k_first < p.k_split ? (uint32_t)(a.k - k_first) : p.k_split;
+  const uint32_t stages = (places + kStage - 1) / kStage;
+  OA oa;
+  OB ob;
+  oa.start(a.a, a.a_stride, m0, a.m, (uint32_t)k_first, wave);
+  ob.start(a.b, a.b_stride, n0, a.n, (uint32_t)k_first, wave);
+  const auto sa = [&](uint32_t t) { return s_ab + t % kStages * (OA::SIZE + OB::SIZE); };
+  const auto load = [&](uint32_t t) {
+    const uint32_t left = places - t * kStage;
+    oa.load(sa(t), wave, left);
+    ob.load(sa(t) + OA::SIZE, wave, left);
+  };
+  f32x16 acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  Vec8<T> fa[2][MB], fb[2][NB];
+  const auto read = [&](uint32_t t, int kk) {
+    const T* s = sa(t);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) fb[kk][j] = OB::frag(s + OA::SIZE, wn + j * 32, kk, lane);
+#pragma unroll
+    for (int i = 0; i < MB; ++i) fa[kk][i] = OA::frag(s, wm + i * 32, kk, lane);
+  };
+  const auto multiply = [&](int kk) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[i][j] = mfma(fa[kk][i], fb[kk][j], acc[i][j]);
+  };
+  for (uint32_t t = 0; t < 3 && t < stages; ++t) load(t);
+  // stage 0 is there when at most the loads of the stages behind it are on their way
+  if (stages > 2)
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+  else
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (stages) read(0, 0);
+  for (uint32_t t = 0; t < stages; ++t) {
+    // stage t + 1 is there; what the stage before t was read into is free
+    if (t + 2 < stages)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");  // no read of LDS moves before the barrier
+    if (t + 3 < stages) load(t + 3);
+    read(t, 1);
+    multiply(0);
+    if (t + 1 < stages) read(t + 1, 0);
+    multiply(1);
+  }
+  // Results: through LDS, a block of 32 rows of the wave at a time, so that whole rows are
+  // written (and gate and residual read).
+  constexpr uint32_t P = NB * 32 + 4;
+  static_assert(W * 32 * P * 4 <= sizeof(s_ab), "the results fit the stages' LDS");
+  __syncthreads();
+  float* s = (float*)s_ab + wave * 32 * P;
+  float* part = (float*)a.scratch + (uint64_t)split * a.m * a.n;
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    asm volatile("" ::: "memory");  // a wave's accesses to LDS keep their order
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[frag_row(e, lane / 32) * P + j * 32 + lane % 32] = acc[i][j][e];
+    asm volatile("" ::: "memory");
+#pragma unroll 1
+    for (int x = 0; x < NB * 2; ++x) {
+      const uint32_t at = x * 64 + lane, r = at / (NB * 4), c = at % (NB * 4) * 8;
+      const uint32_t m = m0 + wm + i * 32 + r, n = n0 + wn + c;
+      if (m >= a.m || n >= a.n) continue;
+      float z[8];
+      *(f32x4*)z = *(const f32x4*)(s + r * P + c);
+      *(f32x4*)(z + 4) = *(const f32x4*)(s + r * P + c + 4);
+      if (p.splits > 1) {
+        float* to = part + (uint64_t)m * a.n + n;
+        for (uint32_t y = 0; y < 8 && n + y < a.n; ++y) to[y] = z[y];
+      } else {
+        finish8<T>(a, m, n, z, p.wide);
+      }
+    }
+  }
+}
+
 uint64_t size(int64_t x) { return (uint64_t)(x < 0 ? -x : x); }
 bool rows_aligned(const void* p, int64_t stride, uint32_t e) {
   return (uintptr_t)p % 16 == 0 && size(stride) * e % 16 == 0;
@@ -215,9 +445,34 @@ uint32_t splits_of(uint32_t m, uint32_t n, uint32_t k) {
   return most <= 1 ? 1 : want < most ? want : most;
 }
 
+// An operand's stages as the tile kernel loads them: 16 bytes at a time, whole chunks, a tile's
+// offsets in 32 bits.
+bool fits_tiles(const void* p, int64_t stride, uint32_t rows, uint32_t k, bool columns) {
+  return rows_aligned(p, stride, 2) && stride >= 0 && stride < 1 << 22 && (columns ? rows : k) % 8 == 0;
+}
+
+template <typename T, bool AC, bool BC, int WR, int WC, int MB, int NB>
+hipError_t launch_tiles(MatmulParams& p, hipStream_t s) {
+  const gts_matmul_args& a = p.a;
+  constexpr uint32_t TM = WR * MB * 32, TN = WC * NB * 32;
+  p.splits = 1;
+  p.k_split = a.k;
+  const uint64_t tiles = (uint64_t)((a.m + TM - 1) / TM) * ((a.n + TN - 1) / TN);
+  tile_kernel<T, AC, BC, WR, WC, MB, NB><<<dim3((uint32_t)(tiles * p.splits)), dim3(WR * WC * 64), 0, s>>>(p);
+  return hipGetLastError();
+}
+
 template <typename T, bool AC, bool BC>
 hipError_t launch_general(MatmulParams& p, hipStream_t s) {
   const gts_matmul_args& a = p.a;
+  if constexpr (sizeof(T) == 2) {
+    if (fits_tiles(a.a, a.a_stride, a.m, a.k, AC) && fits_tiles(a.b, a.b_stride, a.n, a.k, BC)) {
+      const uint64_t t256 = (uint64_t)((a.m + 255) / 256) * ((a.n + 255) / 256);
+      const uint64_t t128 = (uint64_t)((a.m + 255) / 256) * ((a.n + 127) / 128);
+      if (t256 >= 192) return launch_tiles<T, AC, BC, 2, 4, 4, 2>(p, s);
+      if (t128 >= 192) return launch_tiles<T, AC, BC, 4, 2, 2, 2>(p, s);
+    }
+  }
   p.splits = splits_of(a.m, a.n, a.k);
   p.k_split = ((a.k + p.splits - 1) / p.splits + kTileK - 1) / kTileK * kTileK;
   const uint64_t tiles = (((uint64_t)a.m + kTileM - 1) / kTileM) * (((uint64_t)a.n + kTileN - 1) / kTileN);
@@ -234,6 +489,10 @@ hipError_t launch_matmul_t(const gts_matmul_args& a, hipStream_t s) {
   p.a = a;
   p.a_vec = rows_aligned(a.a, a.a_stride, sizeof(T));
   p.b_vec = rows_aligned(a.b, a.b_stride, sizeof(T));
+  p.wide = a.n % 8 == 0 && rows_aligned(a.out, a.out_stride, sizeof(T)) &&
+           rows_aligned(a.preact, a.preact ? a.preact_stride : 0, sizeof(T)) &&
+           rows_aligned(a.gate, a.gate ? a.gate_stride : 0, sizeof(T)) &&
+           rows_aligned(a.residual, a.residual ? a.residual_stride : 0, sizeof(T)) && (uintptr_t)a.bias % 16 == 0;
   const bool ac = a.flags & GTS_MATMUL_A_COLUMNS, bc = a.flags & GTS_MATMUL_B_COLUMNS;
   if (ac) return bc ? launch_general<T, true, true>(p, s) : launch_general<T, true, false>(p, s);
   return bc ? launch_general<T, false, true>(p, s) : launch_general<T, false, false>(p, s);

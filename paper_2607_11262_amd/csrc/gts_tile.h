@@ -60,6 +60,16 @@ __device__ __forceinline__ void load_to_lds(const void* from, void* to) {
                : "memory");
 }
 
+// The same from a base that all lanes share and an offset in bytes below 2^32.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, void* to) {
+  const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)to;
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
+               : "s"(at), "v"(offset), "s"(base)
+               : "memory");
+}
+
 __device__ __forceinline__ bool not_finite(float x) { return !(__builtin_fabsf(x) < INFINITY); }
 template <typename T>
 __device__ __forceinline__ bool any_not_finite(u32x4 v) {

@@ -228,6 +228,45 @@ def test_linear_layouts(M, N, K, dtype):
     assert torch.equal(ops.linear(one, w, b), ops.linear(one.contiguous(), w, b))
 
 
+# Results of many tiles, whose edges and ends of the sum fall inside tiles and stages.
+LARGE = [(2048, 2048, 64), (2040, 3000, 104), (4096, 1032, 40), (3500, 1999, 96), (1, 40000, 64), (20000, 8, 32),
+         (2056, 3080, 8), (2048, 4096, 200)]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("M,N,K", LARGE)
+def test_linear_large(M, N, K, dtype):
+    """Against 64-bit products on the card: each tile kernel, each layout of the operands."""
+    g = torch.Generator(device="cuda").manual_seed(M + N + K)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=dtype)  # noqa: E731
+    x, w, b, gate, res, dy = rand(M, K), rand(N, K), rand(N), rand(M, N), rand(M, N), rand(M, N)
+
+    def check(got, a, c, scale=1.0, plus=0.0, err=0.0, what=""):
+        """got is a c^T * scale + plus, for a [m, k] and c [n, k] of 64 bits."""
+        ref = (a @ c.T.contiguous()) * scale + plus
+        size = 2 * (a.shape[1] + 4) * R.E * (a.abs() @ c.abs().T.contiguous()) * abs(scale) + 4 * R.E * ref.abs() + err
+        bad = (got.double() - ref).abs() > R.rounded(ref, size, dtype)
+        assert not bad.any(), (what, int(bad.sum()), bad.nonzero()[0].tolist())
+
+    xd, wd, gd = x.double(), w.double(), gate.double()
+    z = torch.empty(M, N, dtype=dtype, device="cuda")
+    y = ops.linear(x, w, b, gate=gate, residual=res, preact=z)
+    check(z, xd, wd, plus=b.double(), err=R.E * b.double().abs(), what="preact")
+    ref = (xd @ wd.T.contiguous() + b.double()) * gd + res.double()
+    size = 2 * (K + 6) * R.E * ((xd.abs() @ wd.abs().T.contiguous() + b.double().abs()) * gd.abs() + res.double().abs())
+    assert ((y.double() - ref).abs() <= R.rounded(ref, size, dtype)).all()
+    dx, dw, db, _ = ops.linear_backward(dy, x, w, bias=True)
+    dyd = dy.double()
+    check(dx, dyd, wd.T.contiguous(), what="dx")
+    check(dw, dyd.T.contiguous(), xd.T.contiguous(), what="dw")
+    assert ((db.double() - dyd.sum(0)).abs() <= R.rounded(dyd.sum(0), (M / 4 + 40) * R.E * dyd.abs().sum(0), dtype)).all()
+    # rows behind the operands' ends are not finite and reach nothing
+    pad = lambda t: torch.nn.functional.pad(t, (0, 8, 0, 9), value=float("nan"))[:t.shape[0], :t.shape[1]]  # noqa: E731
+    assert torch.equal(ops.linear(pad(x), pad(w), b, gate=gate, residual=res), y)
+    again = ops.linear_backward(pad(dy), pad(x), pad(w), bias=True)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
+
+
 def test_linear_of_nothing():
     x, w, b = (t.cuda() for t in (torch.ones(4, 8), torch.ones(6, 8), torch.arange(6.0)))
     assert ops.linear(x[:0], w, b).shape == (0, 6)
