@@ -189,39 +189,27 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulParams p) {
   }
 }
 
-// The sums of the splits, in order.
-template <typename T>
-__global__ __launch_bounds__(256) void join_splits_kernel(MatmulParams p, FastDiv by_n) {
-  const gts_matmul_args& a = p.a;
-  const uint64_t i = block_number() * 256 + threadIdx.x, all = (uint64_t)a.m * a.n;
-  if (i >= all) return;
-  const float* part = (const float*)a.scratch + i;
-  float z = part[0];
-  for (uint32_t s = 1; s < p.splits; ++s) z += part[s * all];
-  const uint32_t m = all < (1ull << 31) ? by_n.div((uint32_t)i) : (uint32_t)(i / a.n);
-  finish<T>(a, m, (uint32_t)(i - (uint64_t)m * a.n), z);
-}
-
 // ---- the tile kernel ---------------------------------------------------------------------
-// 16-bit operands whose rows are aligned to 16 bytes.  Stages of 32 places of the sum go
-// straight to LDS, four of them in turn: while one is multiplied, the fragments of the next are
-// read and those behind it are on their way, so that matrix instructions wait for neither;
-// one barrier a stage.
-constexpr uint32_t kStage = 32;
-constexpr int kStages = 4;
+// 16-bit operands whose rows are aligned to 16 bytes.  Stages of 64 places of the sum (whole
+// lines of 128 bytes) go straight to LDS, two in turn.  A stage is four matrix steps; the
+// fragments of a step are read while the one before is multiplied, also across stages, and the
+// one barrier of a stage stands where its last fragments have been read: there the next
+// stage has arrived, and the one behind it may be loaded over this one.
+constexpr uint32_t kStage = 64;
+constexpr int kSteps = kStage / 16;
 
 __device__ __align__(16) const uint32_t g_nothing[4] = {};  // 16 bytes of zeros
 
-// An operand's ROWS rows, 32 places a stage, loaded by W waves.  In LDS chunk c (16 bytes) of
+// An operand's ROWS rows, 64 places a stage, loaded by W waves.  In LDS chunk c (16 bytes) of
 // a row stands at c ^ swizzle, so that the reads of a fragment touch all 64 banks once.
 template <typename T, bool COLUMNS, int ROWS, int W>
 struct Operand {
-  static constexpr int C = COLUMNS ? ROWS / 8 : 4;          // chunks of a row of LDS
+  static constexpr int C = COLUMNS ? ROWS / 8 : 8;          // chunks of a row of LDS
   static constexpr int N = ROWS * kStage / 8 / (64 * W);    // loads of a wave
   static constexpr int SIZE = ROWS * kStage;                // values of a stage
   static_assert(ROWS * kStage / 8 % (64 * W) == 0 && (!COLUMNS || C >= 16), "whole loads");
   static __device__ __forceinline__ uint32_t swizzle(uint32_t r) {
-    return COLUMNS ? ((r & 3) << 2) | ((r >> 2) & 3) : (r >> 2) & 3;
+    return COLUMNS ? ((r & 3) << 2) | ((r >> 2) & 3) : (r >> 1) & 7;
   }
   const char* base;   // of the tile's first value, the stage's first place
   int64_t step;       // bytes from a stage to the next
@@ -330,7 +318,7 @@ __global__ __launch_bounds__(WR * WC * 64, WR * WC == 8 ? 2 : 2) void tile_kerne
   typedef Operand<T, BC, TN, W> OB;
   constexpr int kLoads = OA::N + OB::N;
   const gts_matmul_args& a = p.a;
-  __shared__ __align__(16) T s_ab[kStages * (OA::SIZE + OB::SIZE)];
+  __shared__ __align__(16) T s_ab[2 * (OA::SIZE + OB::SIZE)];
   const uint32_t lane = threadIdx.x & 63u, wave = uni(threadIdx.x >> 6);
   // Workgroups go round the eight XCDs: each takes a run of the tiles, in columns of eight, so
   // that those at work at one time share rows of both operands in its L2.
@@ -349,7 +337,7 @@ __global__ __launch_bounds__(WR * WC * 64, WR * WC == 8 ? 2 : 2) void tile_kerne
   OB ob;
   oa.start(a.a, a.a_stride, m0, a.m, (uint32_t)k_first, wave);
   ob.start(a.b, a.b_stride, n0, a.n, (uint32_t)k_first, wave);
-  const auto sa = [&](uint32_t t) { return s_ab + t % kStages * (OA::SIZE + OB::SIZE); };
+  const auto sa = [&](uint32_t t) { return s_ab + (t & 1) * (OA::SIZE + OB::SIZE); };
   const auto load = [&](uint32_t t) {
     const uint32_t left = places - t * kStage;
     oa.load(sa(t), wave, left);
@@ -366,37 +354,40 @@ __global__ __launch_bounds__(WR * WC * 64, WR * WC == 8 ? 2 : 2) void tile_kerne
   const auto read = [&](uint32_t t, int kk) {
     const T* s = sa(t);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) fb[kk][j] = OB::frag(s + OA::SIZE, wn + j * 32, kk, lane);
+    for (int j = 0; j < NB; ++j) fb[kk & 1][j] = OB::frag(s + OA::SIZE, wn + j * 32, kk, lane);
 #pragma unroll
-    for (int i = 0; i < MB; ++i) fa[kk][i] = OA::frag(s, wm + i * 32, kk, lane);
+    for (int i = 0; i < MB; ++i) fa[kk & 1][i] = OA::frag(s, wm + i * 32, kk, lane);
   };
   const auto multiply = [&](int kk) {
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
-      for (int j = 0; j < NB; ++j) acc[i][j] = mfma(fa[kk][i], fb[kk][j], acc[i][j]);
+      for (int j = 0; j < NB; ++j) acc[i][j] = mfma(fa[kk & 1][i], fb[kk & 1][j], acc[i][j]);
   };
-  for (uint32_t t = 0; t < 3 && t < stages; ++t) load(t);
-  // stage 0 is there when at most the loads of the stages behind it are on their way
-  if (stages > 2)
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
-  else
+  if (stages) load(0);
+  if (stages > 1) {
+    load(1);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+  } else {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
+  }
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");  // no read of LDS moves before the barrier
   if (stages) read(0, 0);
   for (uint32_t t = 0; t < stages; ++t) {
-    // stage t + 1 is there; what the stage before t was read into is free
-    if (t + 2 < stages)
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads) : "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");  // no read of LDS moves before the barrier
-    if (t + 3 < stages) load(t + 3);
-    read(t, 1);
-    multiply(0);
-    if (t + 1 < stages) read(t + 1, 0);
-    multiply(1);
+#pragma unroll
+    for (int kk = 0; kk < kSteps; ++kk) {
+      if (kk + 1 < kSteps) {
+        read(t, kk + 1);
+      } else {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (t + 2 < stages) load(t + 2);
+        if (t + 1 < stages) read(t + 1, 0);
+      }
+      multiply(kk);
+    }
   }
   // Results: through LDS, a block of 32 rows of the wave at a time, so that whole rows are
   // written (and gate and residual read).
@@ -431,19 +422,164 @@ __global__ __launch_bounds__(WR * WC * 64, WR * WC == 8 ? 2 : 2) void tile_kerne
   }
 }
 
+// The sums of the splits, in order; eight values of a row a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void join_splits_kernel(MatmulParams p) {
+  const gts_matmul_args& a = p.a;
+  const uint32_t per = (a.n + 7) / 8;
+  const uint64_t i = block_number() * 256 + threadIdx.x, all = (uint64_t)a.m * a.n;
+  if (i >= (uint64_t)a.m * per) return;
+  const uint32_t m = (uint32_t)(i / per), n = (uint32_t)(i - (uint64_t)m * per) * 8;
+  const float* part = (const float*)a.scratch + (uint64_t)m * a.n + n;
+  float z[8] = {};
+  if (a.n % 8 == 0) {
+    for (uint32_t s = 0; s < p.splits; ++s)
+#pragma unroll
+      for (int x = 0; x < 8; x += 4) {
+        const f32x4 y = *(const f32x4*)(part + s * all + x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[x + e] += y[e];
+      }
+  } else {
+    for (uint32_t s = 0; s < p.splits; ++s)
+      for (uint32_t x = 0; x < 8 && n + x < a.n; ++x) z[x] += part[s * all + x];
+  }
+  finish8<T>(a, m, n, z, p.wide);
+}
+
+// ---- few rows ----------------------------------------------------------------------------
+// Up to 64 rows of a: the rows of b are streamed through registers, each read once, 16 RB of
+// them a workgroup; its eight waves take 64 places of the sum in turn and join their sums in
+// LDS.  Bound by the loads of b; a comes from the L2s.
+constexpr uint32_t kFew = 64;
+constexpr int kAhead = 4;  // steps of 64 places whose loads of b are on their way together
+
+__device__ __forceinline__ f32x4 mfma16(Vec8<__bf16> a, Vec8<__bf16> b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(Vec8<_Float16> a, Vec8<_Float16> b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+template <typename T, int MB, int RB>
+__global__ __launch_bounds__(512) void few_kernel(MatmulParams p) {
+  const gts_matmul_args& a = p.a;
+  constexpr uint32_t W = 8, TN = RB * 16, P = TN + 4;
+  __shared__ __align__(16) float s_sum[W][MB * 16][P];
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane % 16, quarter = lane / 16;
+  const uint32_t n0 = blockIdx.x * TN;
+  // rows past the end are the last again: what they give is not stored
+  const T *pa[MB], *pb[RB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    const uint32_t m = i * 16 + r;
+    pa[i] = (const T*)a.a + (int64_t)(m < a.m ? m : a.m - 1) * a.a_stride;
+  }
+#pragma unroll
+  for (int i = 0; i < RB; ++i) {
+    const uint32_t n = n0 + i * 16 + r;
+    pb[i] = (const T*)a.b + (int64_t)(n < a.n ? n : a.n - 1) * a.b_stride;
+  }
+  f32x4 acc[RB][MB];
+#pragma unroll
+  for (int i = 0; i < RB; ++i)
+#pragma unroll
+    for (int j = 0; j < MB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint32_t steps = (a.k + 63) / 64;
+  // 16 bytes of a row at step s, half x of its places; zeros behind the end
+  const auto at = [&](const T* row, uint32_t s, int x) {
+    const uint64_t k = (uint64_t)s * 64 + x * 32 + quarter * 8;
+    return (const Vec8<T>*)(k < a.k ? row + k : (const T*)g_nothing);
+  };
+  Vec8<T> fb[kAhead][2][RB];
+  const auto load = [&](uint32_t s) {
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y)
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < RB; ++i) fb[y][x][i] = __builtin_nontemporal_load(at(pb[i], s + y * W, x));
+  };
+  for (uint32_t s = wave; s < steps; s += kAhead * W) {
+    load(s);
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y) {
+      Vec8<T> fa[2][MB];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int j = 0; j < MB; ++j) fa[x][j] = *at(pa[j], s + y * W, x);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int j = 0; j < MB; ++j) acc[i][j] = mfma16(fb[y][x][i], fa[x][j], acc[i][j]);
+    }
+  }
+  // a lane has column r of a block of rows of a, and four rows of b side by side
+#pragma unroll
+  for (int i = 0; i < RB; ++i)
+#pragma unroll
+    for (int j = 0; j < MB; ++j) *(f32x4*)&s_sum[wave][j * 16 + r][i * 16 + quarter * 4] = acc[i][j];
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < MB * 16 * (TN / 8); i += 512) {
+    const uint32_t m = i / (TN / 8), c = i % (TN / 8) * 8;
+    if (m >= a.m || n0 + c >= a.n) continue;
+    float z[8] = {};
+#pragma unroll
+    for (uint32_t w = 0; w < W; ++w)
+#pragma unroll
+      for (int x = 0; x < 8; ++x) z[x] += s_sum[w][m][c + x];
+    finish8<T>(a, m, n0 + c, z, p.wide);
+  }
+}
+
 uint64_t size(int64_t x) { return (uint64_t)(x < 0 ? -x : x); }
 bool rows_aligned(const void* p, int64_t stride, uint32_t e) {
   return (uintptr_t)p % 16 == 0 && size(stride) * e % 16 == 0;
 }
 
-// Splits of the sum: where the tiles do not fill the chip twice, as many as do, of at
-// least 128 places.  By sizes alone: the scratch is asked for before the layout is known.
-uint32_t splits_of(uint32_t m, uint32_t n, uint32_t k) {
-  const uint64_t tiles = (((uint64_t)m + kTileM - 1) / kTileM) * (((uint64_t)n + kTileN - 1) / kTileN);
-  if (tiles == 0 || tiles >= 256) return 1;
-  const uint32_t most = (k + 127) / 128, want = (uint32_t)(512 / tiles);
-  return most <= 1 ? 1 : want < most ? want : most;
+// How a product is cut: its tile, and the splits of its sum.  By sizes alone: the scratch is
+// asked for before the layout is known.
+struct Cut {
+  uint32_t tile;  // of kCuts; 0: the general kernel's
+  uint32_t splits;
+};
+// Microseconds that a stage of 64 places takes a workgroup, and workgroups at work at one time.
+// Measured: 8192 x 8192 x 8192 in tiles of 256 x 256, 2048 x 4096 x 14336 in 256 x 128, 2048 x
+// 2048 x 2048 in 128 x 128; the general kernel at 1000 x 1000 x 4000.
+struct TileCost {
+  uint32_t m, n;
+  float stage;
+  uint32_t at_once;
+};
+constexpr TileCost kCuts[] = {{kTileM, kTileN, 2.2f, 768}, {256, 256, 1.8f, 256}, {256, 128, 0.95f, 256}, {128, 128, 1.05f, 512}};
+// A workgroup's begin and end, a further launch, a byte of the parts written and read.
+constexpr float kBegin = 3.f, kJoin = 5.f, kPartBytes = 2.f / 4e6f;
+
+float cost_of(const TileCost& c, uint32_t m, uint32_t n, uint32_t k, uint32_t splits) {
+  const uint64_t tiles = (uint64_t)((m + c.m - 1) / c.m) * ((n + c.n - 1) / c.n);
+  const uint64_t rounds = (tiles * splits + c.at_once - 1) / c.at_once;
+  const uint32_t stages = ((k + 63) / 64 + splits - 1) / splits;
+  const float join = splits > 1 ? kJoin + kPartBytes * 4.f * splits * (float)m * (float)n : 0.f;
+  return (float)rounds * ((float)stages * c.stage + kBegin) + join;
 }
+Cut cut_of(uint32_t m, uint32_t n, uint32_t k, bool tiled) {
+  Cut best{0, 1};
+  float least = INFINITY;
+  for (uint32_t t = tiled ? 1 : 0; t < (tiled ? 4 : 1); ++t)
+    for (const uint32_t splits : {1u, 2u, 3u, 4u, 6u, 8u, 12u, 16u, 24u, 32u}) {
+      if (splits > 1 && splits * 128 > k) break;
+      const float c = cost_of(kCuts[t], m, n, k, splits);
+      if (c < least) {
+        least = c;
+        best = {t, splits};
+      }
+    }
+  return best;
+}
+uint64_t parts_bytes(uint32_t m, uint32_t n, uint32_t splits) { return splits > 1 ? 4ull * splits * m * n : 0; }
 
 // An operand's stages as the tile kernel loads them: 16 bytes at a time, whole chunks, a tile's
 // offsets in 32 bits.
@@ -451,35 +587,65 @@ bool fits_tiles(const void* p, int64_t stride, uint32_t rows, uint32_t k, bool c
   return rows_aligned(p, stride, 2) && stride >= 0 && stride < 1 << 22 && (columns ? rows : k) % 8 == 0;
 }
 
+template <typename T>
+void launch_join(const MatmulParams& p, hipStream_t s) {
+  const uint64_t all = (uint64_t)p.a.m * ((p.a.n + 7) / 8);
+  join_splits_kernel<T><<<grid_of((all + 255) / 256), dim3(256), 0, s>>>(p);
+}
+
 template <typename T, bool AC, bool BC, int WR, int WC, int MB, int NB>
-hipError_t launch_tiles(MatmulParams& p, hipStream_t s) {
+void launch_tiles(const MatmulParams& p, hipStream_t s) {
   const gts_matmul_args& a = p.a;
   constexpr uint32_t TM = WR * MB * 32, TN = WC * NB * 32;
-  p.splits = 1;
-  p.k_split = a.k;
   const uint64_t tiles = (uint64_t)((a.m + TM - 1) / TM) * ((a.n + TN - 1) / TN);
   tile_kernel<T, AC, BC, WR, WC, MB, NB><<<dim3((uint32_t)(tiles * p.splits)), dim3(WR * WC * 64), 0, s>>>(p);
-  return hipGetLastError();
+}
+
+// Few rows: a workgroup takes 16 or 32 rows of b, which is read once; with the larger, a is
+// read from the L2s half as often.
+template <typename T, int MB>
+void launch_few(const MatmulParams& p, hipStream_t s) {
+  if (MB > 1 && p.a.n >= 32 * 128)
+    few_kernel<T, MB, 2><<<dim3((p.a.n + 31) / 32), dim3(512), 0, s>>>(p);
+  else
+    few_kernel<T, MB, 1><<<dim3((p.a.n + 15) / 16), dim3(512), 0, s>>>(p);
 }
 
 template <typename T, bool AC, bool BC>
-hipError_t launch_general(MatmulParams& p, hipStream_t s) {
+hipError_t launch_layout(MatmulParams& p, hipStream_t s) {
   const gts_matmul_args& a = p.a;
   if constexpr (sizeof(T) == 2) {
     if (fits_tiles(a.a, a.a_stride, a.m, a.k, AC) && fits_tiles(a.b, a.b_stride, a.n, a.k, BC)) {
-      const uint64_t t256 = (uint64_t)((a.m + 255) / 256) * ((a.n + 255) / 256);
-      const uint64_t t128 = (uint64_t)((a.m + 255) / 256) * ((a.n + 127) / 128);
-      if (t256 >= 192) return launch_tiles<T, AC, BC, 2, 4, 4, 2>(p, s);
-      if (t128 >= 192) return launch_tiles<T, AC, BC, 4, 2, 2, 2>(p, s);
+      if constexpr (!AC && !BC) {
+        if (a.m <= kFew) {
+          if (a.m <= 16)
+            launch_few<T, 1>(p, s);
+          else if (a.m <= 32)
+            launch_few<T, 2>(p, s);
+          else
+            launch_few<T, 4>(p, s);
+          return hipGetLastError();
+        }
+      }
+      const Cut cut = cut_of(a.m, a.n, a.k, true);
+      p.splits = cut.splits;
+      p.k_split = ((a.k + p.splits - 1) / p.splits + kStage - 1) / kStage * kStage;
+      if (cut.tile == 1)
+        launch_tiles<T, AC, BC, 2, 4, 4, 2>(p, s);
+      else if (cut.tile == 2)
+        launch_tiles<T, AC, BC, 4, 2, 2, 2>(p, s);
+      else
+        launch_tiles<T, AC, BC, 2, 2, 2, 2>(p, s);
+      if (p.splits > 1) launch_join<T>(p, s);
+      return hipGetLastError();
     }
   }
-  p.splits = splits_of(a.m, a.n, a.k);
+  p.splits = cut_of(a.m, a.n, a.k, false).splits;
   p.k_split = ((a.k + p.splits - 1) / p.splits + kTileK - 1) / kTileK * kTileK;
   const uint64_t tiles = (((uint64_t)a.m + kTileM - 1) / kTileM) * (((uint64_t)a.n + kTileN - 1) / kTileN);
   if (tiles * p.splits > 0x7FFFFFull) return hipErrorInvalidValue;  // x 256 threads stay below 2^31
   matmul_kernel<T, AC, BC><<<dim3((uint32_t)(tiles * p.splits)), dim3(256), 0, s>>>(p);
-  if (p.splits > 1)
-    join_splits_kernel<T><<<grid_of(((uint64_t)a.m * a.n + 255) / 256), dim3(256), 0, s>>>(p, FastDiv(a.n));
+  if (p.splits > 1) launch_join<T>(p, s);
   return hipGetLastError();
 }
 
@@ -494,8 +660,8 @@ hipError_t launch_matmul_t(const gts_matmul_args& a, hipStream_t s) {
            rows_aligned(a.gate, a.gate ? a.gate_stride : 0, sizeof(T)) &&
            rows_aligned(a.residual, a.residual ? a.residual_stride : 0, sizeof(T)) && (uintptr_t)a.bias % 16 == 0;
   const bool ac = a.flags & GTS_MATMUL_A_COLUMNS, bc = a.flags & GTS_MATMUL_B_COLUMNS;
-  if (ac) return bc ? launch_general<T, true, true>(p, s) : launch_general<T, true, false>(p, s);
-  return bc ? launch_general<T, false, true>(p, s) : launch_general<T, false, false>(p, s);
+  if (ac) return bc ? launch_layout<T, true, true>(p, s) : launch_layout<T, true, false>(p, s);
+  return bc ? launch_layout<T, false, true>(p, s) : launch_layout<T, false, false>(p, s);
 }
 
 // ---- the elementwise part of the gradient ------------------------------------------------
@@ -566,8 +732,8 @@ void launch_linear_grad_t(const LinearGradParams& p, hipStream_t s) {
 }  // namespace
 
 uint64_t matmul_scratch(uint32_t m, uint32_t n, uint32_t k) {
-  const uint32_t s = splits_of(m, n, k);
-  return s > 1 ? 4ull * s * m * n : 0;
+  const uint64_t x = parts_bytes(m, n, cut_of(m, n, k, true).splits), y = parts_bytes(m, n, cut_of(m, n, k, false).splits);
+  return x > y ? x : y;
 }
 
 hipError_t launch_matmul(const gts_matmul_args& a, hipStream_t s) {
