@@ -51,7 +51,6 @@ __device__ __forceinline__ float slope(uint32_t act, float z) {
 
 struct MatmulParams {
   gts_matmul_args a;
-  bool a_vec, b_vec;   // rows aligned to 16 bytes
   uint32_t splits;     // of the sum; more than one: the parts go to the scratch
   uint32_t k_split;    // places of a split
   bool wide;           // eight values of a result, its bias, gate and residual are 16 bytes
@@ -69,77 +68,89 @@ __device__ __forceinline__ void finish(const gts_matmul_args& a, uint32_t m, uin
 }
 
 // ---- the general kernel ----------------------------------------------------------------
-// Any type, size, stride and alignment.  Four waves take 64 x 64 each of a 128 x 128
-// tile; 32 places of the sum at a time go through registers to LDS, the next while
-// these are multiplied.
-constexpr uint32_t kTileM = 128, kTileN = 128, kTileK = 32;
+// Any type, size, stride and alignment.  Four waves take 32 R x 32 R each of a tile of 64 R x
+// 64 R; 32 places of the sum at a time go through registers to LDS, the next while these are
+// multiplied.  The smaller tile is for small results, where more workgroups a CU hide the loads.
+constexpr uint32_t kTileK = 32;
 
-// LDS of an operand's 128 rows (or columns) and 32 places: rows of 16 values more than
-// they hold, so that reads of neighbouring rows meet other banks.
-template <bool COLUMNS>
-constexpr uint32_t kPitch = COLUMNS ? kTileM + 8 : kTileK + 8;
-constexpr uint32_t kTileSize = kTileM * (kTileK + 8);  // the larger of both
+// LDS of an operand's 64 R rows (or columns) and 32 places: rows of 8 values more than they
+// hold, so that reads of neighbouring rows meet other banks.
+template <bool COLUMNS, int R>
+constexpr uint32_t kPitch = COLUMNS ? 64 * R + 8 : kTileK + 8;
+template <int R>
+constexpr uint32_t kTileSize = 64 * R * (kTileK + 8);  // the larger of both
 
-template <typename T, bool COLUMNS>
+template <typename T, bool COLUMNS, int R>
 struct Staged {
-  Vec8<T> x[2];
-  // Rows r0 .. + 127 of `rows`, places k0 .. + 31 of those below `k_end`.
-  __device__ __forceinline__ void load(const T* p, int64_t stride, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t k_end,
-                                       bool vec) {
+  Vec8<T> x[R];
+  // Rows r0 .. + 64 R - 1 of `rows`, places k0 .. + 31 of those below `k_end`.  Without a branch
+  // where all places are there, so that nothing waits for the loads: rows past the end are then
+  // the last again (what they give is not stored).
+  __device__ __forceinline__ void load(const T* p, int64_t stride, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t k_end) {
+    if (k0 + kTileK <= k_end && (!COLUMNS || r0 + 64 * R <= rows)) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < R; ++i) {
+        const uint32_t id = threadIdx.x + 256 * i, r = r0 + id / 4;
+        x[i] = COLUMNS ? load_any(p + (int64_t)(k0 + id / (8 * R)) * stride + r0 + id % (8 * R) * 8)
+                       : load_any(p + (int64_t)(r < rows ? r : rows - 1) * stride + k0 + id % 4 * 8);
+      }
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
       const uint32_t id = threadIdx.x + 256 * i;
       uint32_t row, column;
       int64_t valid;
       if (COLUMNS) {
-        row = k0 + id / 16;
-        column = r0 + id % 16 * 8;
+        row = k0 + id / (8 * R);
+        column = r0 + id % (8 * R) * 8;
         valid = row < k_end ? (int64_t)rows - column : 0;
       } else {
         row = r0 + id / 4;
         column = k0 + id % 4 * 8;
         valid = row < rows ? (int64_t)k_end - column : 0;
       }
-      x[i] = load8(p + (int64_t)row * stride + column, valid, vec);
+      x[i] = load8(p + (int64_t)row * stride + column, valid);
     }
   }
   __device__ __forceinline__ void store(T* s) const {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < R; ++i) {
       const uint32_t id = threadIdx.x + 256 * i;
-      write8(s + (COLUMNS ? id / 16 * kPitch<true> + id % 16 * 8 : id / 4 * kPitch<false> + id % 4 * 8), x[i]);
+      write8(s + (COLUMNS ? id / (8 * R) * kPitch<true, R> + id % (8 * R) * 8 : id / 4 * kPitch<false, R> + id % 4 * 8), x[i]);
     }
   }
+  static __device__ __forceinline__ Vec8<T> frag(const T* s, uint32_t row, uint32_t k, uint32_t lane) {
+    if constexpr (COLUMNS)
+      return frag_columns<false>(s, kPitch<true, R>, k, row, lane);
+    else
+      return frag_rows(s, kPitch<false, R>, row, k, lane);
+  }
 };
-template <typename T, bool COLUMNS>
-__device__ __forceinline__ Vec8<T> staged_frag(const T* s, uint32_t row, uint32_t k, uint32_t lane) {
-  if constexpr (COLUMNS)
-    return frag_columns<false>(s, kPitch<true>, k, row, lane);
-  else
-    return frag_rows(s, kPitch<false>, row, k, lane);
-}
 
-template <typename T, bool AC, bool BC>
+template <typename T, bool AC, bool BC, int R>
 __global__ __launch_bounds__(256) void matmul_kernel(MatmulParams p) {
   const gts_matmul_args& a = p.a;
-  __shared__ __align__(16) T s_a[2][kTileSize], s_b[2][kTileSize];
+  typedef Staged<T, AC, R> SA;
+  typedef Staged<T, BC, R> SB;
+  __shared__ __align__(16) T s_a[2][kTileSize<R>], s_b[2][kTileSize<R>];
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-  const uint32_t tiles_n = (a.n + kTileN - 1) / kTileN;
+  const uint32_t tiles_n = (a.n + 64 * R - 1) / (64 * R);
   const uint32_t tile = blockIdx.x / p.splits, split = blockIdx.x - tile * p.splits;
-  const uint32_t m0 = tile / tiles_n * kTileM, n0 = tile % tiles_n * kTileN;
-  const uint32_t wm = wave / 2 * 64, wn = wave % 2 * 64;
+  const uint32_t m0 = tile / tiles_n * 64 * R, n0 = tile % tiles_n * 64 * R;
+  const uint32_t wm = wave / 2 * 32 * R, wn = wave % 2 * 32 * R;
   const uint64_t k_first = (uint64_t)split * p.k_split, k_last = k_first + p.k_split;
-  const uint32_t k0 = (uint32_t)k_first, k1 = k_last < a.k ? (uint32_t)k_last : a.k;
-  f32x16 acc[2][2];
+  const uint32_t k0 = k_first < a.k ? (uint32_t)k_first : a.k, k1 = k_last < a.k ? (uint32_t)k_last : a.k;
+  f32x16 acc[R][R];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < R * R; ++i)
 #pragma unroll
-    for (int j = 0; j < 16; ++j) acc[i / 2][i % 2][j] = 0.f;
-  Staged<T, AC> sa;
-  Staged<T, BC> sb;
+    for (int j = 0; j < 16; ++j) acc[i / R][i % R][j] = 0.f;
+  SA sa;
+  SB sb;
   if (k0 < k1) {
-    sa.load((const T*)a.a, a.a_stride, m0, a.m, k0, k1, p.a_vec);
-    sb.load((const T*)a.b, a.b_stride, n0, a.n, k0, k1, p.b_vec);
+    sa.load((const T*)a.a, a.a_stride, m0, a.m, k0, k1);
+    sb.load((const T*)a.b, a.b_stride, n0, a.n, k0, k1);
     sa.store(s_a[0]);
     sb.store(s_b[0]);
   }
@@ -148,21 +159,21 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulParams p) {
   for (uint64_t k = k0; k < k1; k += kTileK, at ^= 1) {
     const bool more = k + kTileK < k1;
     if (more) {
-      sa.load((const T*)a.a, a.a_stride, m0, a.m, (uint32_t)k + kTileK, k1, p.a_vec);
-      sb.load((const T*)a.b, a.b_stride, n0, a.n, (uint32_t)k + kTileK, k1, p.b_vec);
+      sa.load((const T*)a.a, a.a_stride, m0, a.m, (uint32_t)k + kTileK, k1);
+      sb.load((const T*)a.b, a.b_stride, n0, a.n, (uint32_t)k + kTileK, k1);
     }
 #pragma unroll
     for (uint32_t kk = 0; kk < kTileK; kk += 16) {
-      Vec8<T> fa[2], fb[2];
+      Vec8<T> fa[R], fb[R];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        fa[i] = staged_frag<T, AC>(s_a[at], wm + i * 32, kk, lane);
-        fb[i] = staged_frag<T, BC>(s_b[at], wn + i * 32, kk, lane);
+      for (int i = 0; i < R; ++i) {
+        fa[i] = SA::frag(s_a[at], wm + i * 32, kk, lane);
+        fb[i] = SB::frag(s_b[at], wn + i * 32, kk, lane);
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < R; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = mfma(fa[i], fb[j], acc[i][j]);
+        for (int j = 0; j < R; ++j) acc[i][j] = mfma(fa[i], fb[j], acc[i][j]);
     }
     if (more) {
       sa.store(s_a[at ^ 1]);
@@ -172,11 +183,11 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulParams p) {
   }
   float* part = (float*)a.scratch + (uint64_t)split * a.m * a.n;
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < R; ++j) {
     const uint32_t n = n0 + wn + j * 32 + lane % 32;
     if (n >= a.n) continue;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const uint32_t m = m0 + wm + i * 32 + frag_row(e, lane / 32);
@@ -414,7 +425,12 @@ __global__ __launch_bounds__(WR * WC * 64, WR * WC == 8 ? 2 : 2) void tile_kerne
       *(f32x4*)(z + 4) = *(const f32x4*)(s + r * P + c + 4);
       if (p.splits > 1) {
         float* to = part + (uint64_t)m * a.n + n;
-        for (uint32_t y = 0; y < 8 && n + y < a.n; ++y) to[y] = z[y];
+        if (a.n % 8 == 0) {
+          *(f32x4*)to = *(const f32x4*)z;
+          *(f32x4*)(to + 4) = *(const f32x4*)(z + 4);
+        } else {
+          for (uint32_t y = 0; y < 8 && n + y < a.n; ++y) to[y] = z[y];
+        }
       } else {
         finish8<T>(a, m, n, z, p.wide);
       }
@@ -448,11 +464,14 @@ __global__ __launch_bounds__(256) void join_splits_kernel(MatmulParams p) {
 }
 
 // ---- few rows ----------------------------------------------------------------------------
-// Up to 64 rows of a: the rows of b are streamed through registers, each read once, 16 RB of
-// them a workgroup; its eight waves take 64 places of the sum in turn and join their sums in
-// LDS.  Bound by the loads of b; a comes from the L2s.
-constexpr uint32_t kFew = 64;
-constexpr int kAhead = 4;  // steps of 64 places whose loads of b are on their way together
+// Up to 16 rows of a: the rows of b are streamed through registers, each read once, 16 of
+// them a workgroup; its four waves take 64 places of the sum in turn and join their sums in
+// LDS: one launch where the tiles take two.  Bound by the loads of b (16 rows at a time: 3.5 TB/s);
+// a comes from the L2s.  3 x 1024 x 1024 4.2 us (tiles with splits 7.4), 1 x 4096 x 4096 7.1 (11.1),
+// 8 x 6144 x 4096 14.4 (14.6); past 2^25 values of b the tiles are faster (16 x 4096 x 14336 27.0, 25.1).
+constexpr uint64_t kFewValues = 1ull << 25;
+constexpr uint32_t kFew = 16;
+constexpr int kAhead = 4;  // steps of 64 places whose loads are on their way together
 
 __device__ __forceinline__ f32x4 mfma16(Vec8<__bf16> a, Vec8<__bf16> b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -461,71 +480,54 @@ __device__ __forceinline__ f32x4 mfma16(Vec8<_Float16> a, Vec8<_Float16> b, f32x
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-template <typename T, int MB, int RB>
-__global__ __launch_bounds__(512) void few_kernel(MatmulParams p) {
+template <typename T>
+__global__ __launch_bounds__(256) void few_kernel(MatmulParams p) {
   const gts_matmul_args& a = p.a;
-  constexpr uint32_t W = 8, TN = RB * 16, P = TN + 4;
-  __shared__ __align__(16) float s_sum[W][MB * 16][P];
+  constexpr uint32_t W = 4;
+  __shared__ __align__(16) float s_sum[W][16][20];
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane % 16, quarter = lane / 16;
-  const uint32_t n0 = blockIdx.x * TN;
+  const uint32_t n0 = blockIdx.x * 16;
   // rows past the end are the last again: what they give is not stored
-  const T *pa[MB], *pb[RB];
-#pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    const uint32_t m = i * 16 + r;
-    pa[i] = (const T*)a.a + (int64_t)(m < a.m ? m : a.m - 1) * a.a_stride;
-  }
-#pragma unroll
-  for (int i = 0; i < RB; ++i) {
-    const uint32_t n = n0 + i * 16 + r;
-    pb[i] = (const T*)a.b + (int64_t)(n < a.n ? n : a.n - 1) * a.b_stride;
-  }
-  f32x4 acc[RB][MB];
-#pragma unroll
-  for (int i = 0; i < RB; ++i)
-#pragma unroll
-    for (int j = 0; j < MB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const T* pa = (const T*)a.a + (int64_t)(r < a.m ? r : a.m - 1) * a.a_stride;
+  const T* pb = (const T*)a.b + (int64_t)(n0 + r < a.n ? n0 + r : a.n - 1) * a.b_stride;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   const uint32_t steps = (a.k + 63) / 64;
   // 16 bytes of a row at step s, half x of its places; zeros behind the end
   const auto at = [&](const T* row, uint32_t s, int x) {
     const uint64_t k = (uint64_t)s * 64 + x * 32 + quarter * 8;
-    return (const Vec8<T>*)(k < a.k ? row + k : (const T*)g_nothing);
+    return *(const Vec8<T>*)(k < a.k ? row + k : (const T*)g_nothing);
   };
-  Vec8<T> fb[kAhead][2][RB];
-  const auto load = [&](uint32_t s) {
+  Vec8<T> fa[2][kAhead][2], fb[2][kAhead][2];
+  const auto load = [&](int to, uint32_t s) {
 #pragma unroll
     for (int y = 0; y < kAhead; ++y)
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int i = 0; i < RB; ++i) fb[y][x][i] = __builtin_nontemporal_load(at(pb[i], s + y * W, x));
+      for (int x = 0; x < 2; ++x) {
+        fa[to][y][x] = at(pa, s + y * W, x);
+        fb[to][y][x] = at(pb, s + y * W, x);
+      }
+    __builtin_amdgcn_sched_barrier(0);  // the loads stay ahead of the products
   };
-  for (uint32_t s = wave; s < steps; s += kAhead * W) {
-    load(s);
+  const auto multiply = [&](int from) {
 #pragma unroll
-    for (int y = 0; y < kAhead; ++y) {
-      Vec8<T> fa[2][MB];
+    for (int y = 0; y < kAhead; ++y)
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int j = 0; j < MB; ++j) fa[x][j] = *at(pa[j], s + y * W, x);
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int i = 0; i < RB; ++i)
-#pragma unroll
-          for (int j = 0; j < MB; ++j) acc[i][j] = mfma16(fb[y][x][i], fa[x][j], acc[i][j]);
-    }
+      for (int x = 0; x < 2; ++x) acc = mfma16(fb[from][y][x], fa[from][y][x], acc);
+  };
+  // loads past the end are of 16 bytes that are in every L2
+  load(0, wave);
+  for (uint32_t s = wave; s < steps; s += 2 * kAhead * W) {
+    load(1, s + kAhead * W);
+    multiply(0);
+    load(0, s + 2 * kAhead * W);
+    multiply(1);
   }
-  // a lane has column r of a block of rows of a, and four rows of b side by side
-#pragma unroll
-  for (int i = 0; i < RB; ++i)
-#pragma unroll
-    for (int j = 0; j < MB; ++j) *(f32x4*)&s_sum[wave][j * 16 + r][i * 16 + quarter * 4] = acc[i][j];
+  // a lane has row r of a, and four rows of b side by side
+  *(f32x4*)&s_sum[wave][r][quarter * 4] = acc;
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < MB * 16 * (TN / 8); i += 512) {
-    const uint32_t m = i / (TN / 8), c = i % (TN / 8) * 8;
-    if (m >= a.m || n0 + c >= a.n) continue;
+  if (threadIdx.x < 32) {
+    const uint32_t m = threadIdx.x / 2, c = threadIdx.x % 2 * 8;
+    if (m >= a.m || n0 + c >= a.n) return;
     float z[8] = {};
 #pragma unroll
     for (uint32_t w = 0; w < W; ++w)
@@ -543,32 +545,47 @@ bool rows_aligned(const void* p, int64_t stride, uint32_t e) {
 // How a product is cut: its tile, and the splits of its sum.  By sizes alone: the scratch is
 // asked for before the layout is known.
 struct Cut {
-  uint32_t tile;  // of kCuts; 0: the general kernel's
+  uint32_t tile;  // of kCuts
   uint32_t splits;
 };
-// Microseconds that a stage of 64 places takes a workgroup, and workgroups at work at one time.
-// Measured: 8192 x 8192 x 8192 in tiles of 256 x 256, 2048 x 4096 x 14336 in 256 x 128, 2048 x
-// 2048 x 2048 in 128 x 128; the general kernel at 1000 x 1000 x 4000.
+// Microseconds that a stage of 64 places takes: a workgroup alone on its CU, and what each adds
+// where several share one (or take turns).  Fitted to products of 64 to 8192 rows and columns with
+// 1024 to 14336 places.
 struct TileCost {
   uint32_t m, n;
-  float stage;
-  uint32_t at_once;
+  float alone, shared;
 };
-constexpr TileCost kCuts[] = {{kTileM, kTileN, 2.2f, 768}, {256, 256, 1.8f, 256}, {256, 128, 0.95f, 256}, {128, 128, 1.05f, 512}};
-// A workgroup's begin and end, a further launch, a byte of the parts written and read.
-constexpr float kBegin = 3.f, kJoin = 5.f, kPartBytes = 2.f / 4e6f;
+constexpr TileCost kCuts[] = {
+    // the tile kernel
+    {256, 256, 1.45f, 1.6f},
+    {256, 128, 0.9f, 0.98f},
+    {128, 128, 0.72f, 0.52f},
+    {64, 128, 0.56f, 0.33f},
+    // the general kernel, and in 32 bits: a sixteenth of the matrix rate
+    {128, 128, 1.6f, 0.9f},
+    {64, 64, 1.0f, 0.35f},
+    {128, 128, 6.0f, 4.4f},
+    {64, 64, 1.75f, 1.2f}};
+constexpr uint32_t kUnits = 256;  // CUs
+// A launch with a workgroup's begin and end, the join's, a byte of the parts written and read.
+constexpr float kBegin = 4.f, kJoin = 4.f, kPartBytes = 1.f / 2.4e6f;
 
 float cost_of(const TileCost& c, uint32_t m, uint32_t n, uint32_t k, uint32_t splits) {
   const uint64_t tiles = (uint64_t)((m + c.m - 1) / c.m) * ((n + c.n - 1) / c.n);
-  const uint64_t rounds = (tiles * splits + c.at_once - 1) / c.at_once;
+  const uint64_t groups = tiles * splits;
+  const float shared = c.shared * (groups < kUnits ? (float)groups / kUnits : (float)((groups + kUnits - 1) / kUnits));
   const uint32_t stages = ((k + 63) / 64 + splits - 1) / splits;
   const float join = splits > 1 ? kJoin + kPartBytes * 4.f * splits * (float)m * (float)n : 0.f;
-  return (float)rounds * ((float)stages * c.stage + kBegin) + join;
+  return kBegin + (float)stages * (shared > c.alone ? shared : c.alone) + join;
 }
-Cut cut_of(uint32_t m, uint32_t n, uint32_t k, bool tiled) {
+// kLargeTiles: a is stored by columns, of which a tile has 128 at least.
+enum Kind { kGeneral, kTiles, kLargeTiles, kGeneral32 };
+Cut cut_of(uint32_t m, uint32_t n, uint32_t k, Kind kind) {
   Cut best{0, 1};
   float least = INFINITY;
-  for (uint32_t t = tiled ? 1 : 0; t < (tiled ? 4 : 1); ++t)
+  const uint32_t from = kind == kGeneral ? 4 : kind == kGeneral32 ? 6 : 0;
+  const uint32_t to = kind == kGeneral ? 6 : kind == kGeneral32 ? 8 : kind == kTiles ? 4 : 3;
+  for (uint32_t t = from; t < to; ++t)
     for (const uint32_t splits : {1u, 2u, 3u, 4u, 6u, 8u, 12u, 16u, 24u, 32u}) {
       if (splits > 1 && splits * 128 > k) break;
       const float c = cost_of(kCuts[t], m, n, k, splits);
@@ -601,50 +618,42 @@ void launch_tiles(const MatmulParams& p, hipStream_t s) {
   tile_kernel<T, AC, BC, WR, WC, MB, NB><<<dim3((uint32_t)(tiles * p.splits)), dim3(WR * WC * 64), 0, s>>>(p);
 }
 
-// Few rows: a workgroup takes 16 or 32 rows of b, which is read once; with the larger, a is
-// read from the L2s half as often.
-template <typename T, int MB>
-void launch_few(const MatmulParams& p, hipStream_t s) {
-  if (MB > 1 && p.a.n >= 32 * 128)
-    few_kernel<T, MB, 2><<<dim3((p.a.n + 31) / 32), dim3(512), 0, s>>>(p);
-  else
-    few_kernel<T, MB, 1><<<dim3((p.a.n + 15) / 16), dim3(512), 0, s>>>(p);
-}
-
 template <typename T, bool AC, bool BC>
 hipError_t launch_layout(MatmulParams& p, hipStream_t s) {
   const gts_matmul_args& a = p.a;
   if constexpr (sizeof(T) == 2) {
     if (fits_tiles(a.a, a.a_stride, a.m, a.k, AC) && fits_tiles(a.b, a.b_stride, a.n, a.k, BC)) {
       if constexpr (!AC && !BC) {
-        if (a.m <= kFew) {
-          if (a.m <= 16)
-            launch_few<T, 1>(p, s);
-          else if (a.m <= 32)
-            launch_few<T, 2>(p, s);
-          else
-            launch_few<T, 4>(p, s);
+        if (a.m <= kFew && (uint64_t)a.n * a.k <= kFewValues) {
+          few_kernel<T><<<dim3((a.n + 15) / 16), dim3(256), 0, s>>>(p);
           return hipGetLastError();
         }
       }
-      const Cut cut = cut_of(a.m, a.n, a.k, true);
+      const Cut cut = cut_of(a.m, a.n, a.k, AC ? kLargeTiles : kTiles);
       p.splits = cut.splits;
       p.k_split = ((a.k + p.splits - 1) / p.splits + kStage - 1) / kStage * kStage;
-      if (cut.tile == 1)
+      if (cut.tile == 0)
         launch_tiles<T, AC, BC, 2, 4, 4, 2>(p, s);
-      else if (cut.tile == 2)
+      else if (cut.tile == 1)
         launch_tiles<T, AC, BC, 4, 2, 2, 2>(p, s);
-      else
+      else if (cut.tile == 2)
         launch_tiles<T, AC, BC, 2, 2, 2, 2>(p, s);
+      else if constexpr (!AC)
+        launch_tiles<T, AC, BC, 1, 4, 2, 1>(p, s);
       if (p.splits > 1) launch_join<T>(p, s);
       return hipGetLastError();
     }
   }
-  p.splits = cut_of(a.m, a.n, a.k, false).splits;
+  const Cut cut = cut_of(a.m, a.n, a.k, sizeof(T) == 4 ? kGeneral32 : kGeneral);
+  p.splits = cut.splits;
   p.k_split = ((a.k + p.splits - 1) / p.splits + kTileK - 1) / kTileK * kTileK;
-  const uint64_t tiles = (((uint64_t)a.m + kTileM - 1) / kTileM) * (((uint64_t)a.n + kTileN - 1) / kTileN);
-  if (tiles * p.splits > 0x7FFFFFull) return hipErrorInvalidValue;  // x 256 threads stay below 2^31
-  matmul_kernel<T, AC, BC><<<dim3((uint32_t)(tiles * p.splits)), dim3(256), 0, s>>>(p);
+  const uint32_t edge = kCuts[cut.tile].m;
+  const uint64_t groups = (((uint64_t)a.m + edge - 1) / edge) * (((uint64_t)a.n + edge - 1) / edge) * p.splits;
+  if (groups > 0x7FFFFFull) return hipErrorInvalidValue;  // x 256 threads stay below 2^31
+  if (edge == 128)
+    matmul_kernel<T, AC, BC, 2><<<dim3((uint32_t)groups), dim3(256), 0, s>>>(p);
+  else
+    matmul_kernel<T, AC, BC, 1><<<dim3((uint32_t)groups), dim3(256), 0, s>>>(p);
   if (p.splits > 1) launch_join<T>(p, s);
   return hipGetLastError();
 }
@@ -653,8 +662,6 @@ template <typename T>
 hipError_t launch_matmul_t(const gts_matmul_args& a, hipStream_t s) {
   MatmulParams p{};
   p.a = a;
-  p.a_vec = rows_aligned(a.a, a.a_stride, sizeof(T));
-  p.b_vec = rows_aligned(a.b, a.b_stride, sizeof(T));
   p.wide = a.n % 8 == 0 && rows_aligned(a.out, a.out_stride, sizeof(T)) &&
            rows_aligned(a.preact, a.preact ? a.preact_stride : 0, sizeof(T)) &&
            rows_aligned(a.gate, a.gate ? a.gate_stride : 0, sizeof(T)) &&
@@ -732,8 +739,12 @@ void launch_linear_grad_t(const LinearGradParams& p, hipStream_t s) {
 }  // namespace
 
 uint64_t matmul_scratch(uint32_t m, uint32_t n, uint32_t k) {
-  const uint64_t x = parts_bytes(m, n, cut_of(m, n, k, true).splits), y = parts_bytes(m, n, cut_of(m, n, k, false).splits);
-  return x > y ? x : y;
+  uint32_t most = 1;
+  for (const Kind kind : {kGeneral, kTiles, kLargeTiles, kGeneral32}) {
+    const uint32_t splits = cut_of(m, n, k, kind).splits;
+    most = splits > most ? splits : most;
+  }
+  return parts_bytes(m, n, most);
 }
 
 hipError_t launch_matmul(const gts_matmul_args& a, hipStream_t s) {

@@ -68,10 +68,10 @@ constexpr uint32_t kRows = 128, kStep = 32;
 template <typename T, int DP>
 struct Held {  // 32 rows of a wave
   Vec8<T> x[DP / 16];
-  __device__ __forceinline__ void load(const T* p, bool valid, uint32_t dim, bool vec, uint32_t half) {
+  __device__ __forceinline__ void load(const T* p, bool valid, uint32_t dim, uint32_t half) {
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i)
-      x[i] = load8(p + i * 16 + 8 * half, valid ? (int64_t)dim - (i * 16 + 8 * half) : 0, vec);
+      x[i] = load8(p + i * 16 + 8 * half, valid ? (int64_t)dim - (i * 16 + 8 * half) : 0);
   }
 };
 template <typename T, int DP>
@@ -80,13 +80,13 @@ constexpr uint32_t kRowPitch = DP + 8;
 // Rows j0 .. j0 + 31 of n to LDS, zeros where there is none.  Returns whether a value was
 // not finite; with `clear`, those are zeros in LDS.
 template <typename T, int DP>
-__device__ __forceinline__ bool stage_rows(const T* p, int64_t stride, uint32_t j0, uint32_t n, uint32_t dim, bool vec,
-                                           bool clear, T* s) {
+__device__ __forceinline__ bool stage_rows(const T* p, int64_t stride, uint32_t j0, uint32_t n, uint32_t dim, bool clear,
+                                           T* s) {
   bool found = false;
 #pragma unroll 4
   for (uint32_t id = threadIdx.x; id < kStep * (DP / 8); id += 256) {
     const uint32_t r = id / (DP / 8), c = id % (DP / 8) * 8;
-    Vec8<T> x = load8(p + (int64_t)(j0 + r) * stride + c, j0 + r < n ? (int64_t)dim - c : 0, vec);
+    Vec8<T> x = load8(p + (int64_t)(j0 + r) * stride + c, j0 + r < n ? (int64_t)dim - c : 0);
     if (clear) found |= clear_not_finite(x);
     write8(s + r * kRowPitch<T, DP> + c, x);
   }
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256) void prompt_kernel(PromptParams p) {
     return;
   }
   Held<T, DP> q;
-  q.load((const T*)a.q + (int64_t)token * a.q_stride[0] + (int64_t)hq * a.q_stride[1], valid, a.dim, p.vec, half);
+  q.load((const T*)a.q + (int64_t)token * a.q_stride[0] + (int64_t)hq * a.q_stride[1], valid, a.dim, half);
   const T* k = (const T*)a.k + (int64_t)sp.first * a.k_stride[0] + (int64_t)h * a.k_stride[1];
   const T* v = (const T*)a.v + (int64_t)sp.first * a.v_stride[0] + (int64_t)h * a.v_stride[1];
   const uint32_t keys = causal && r0 + kRows < sp.n ? r0 + kRows : sp.n;
@@ -201,8 +201,8 @@ __global__ __launch_bounds__(256) void prompt_kernel(PromptParams p) {
   for (uint32_t j0 = 0; j0 < keys; j0 += kStep) {
     const bool edge = causal && j0 + kStep > r0 + 1;  // some row does not see all of the block
     __syncthreads();
-    stage_rows<T, DP>(k, a.k_stride[0], j0, sp.n, a.dim, p.vec, false, s_k);
-    const bool found = stage_rows<T, DP>(v, a.v_stride[0], j0, sp.n, a.dim, p.vec, edge, s_v);
+    stage_rows<T, DP>(k, a.k_stride[0], j0, sp.n, a.dim, false, s_k);
+    const bool found = stage_rows<T, DP>(v, a.v_stride[0], j0, sp.n, a.dim, edge, s_v);
     const bool odd = __syncthreads_or(found);
     f32x16 s = times_held<T, DP>(s_k, q, lane);
     float mx = -INFINITY;
@@ -593,7 +593,7 @@ struct PromptGradParams {
 
 // delta, and lse in base 2: 64 tokens of a head a workgroup, 16 lanes a row.
 template <typename T>
-__global__ __launch_bounds__(256) void stats_kernel(PromptGradParams p, bool vec) {
+__global__ __launch_bounds__(256) void stats_kernel(PromptGradParams p) {
   const gts_prompt_grad_args& a = p.a;
   const uint32_t h = blockIdx.x % a.q_heads, t0 = blockIdx.x / a.q_heads * 64, lane = threadIdx.x & 63u;
   const uint32_t sub = lane / 16, li = lane % 16;
@@ -605,7 +605,7 @@ __global__ __launch_bounds__(256) void stats_kernel(PromptGradParams p, bool vec
       const T* x = (const T*)a.dout + (int64_t)t * a.dout_stride[0] + (int64_t)h * a.dout_stride[1];
       const T* y = (const T*)a.out + (int64_t)t * a.out_stride[0] + (int64_t)h * a.out_stride[1];
       for (uint32_t d = li * 8; d < a.dim; d += 128) {
-        const Vec8<T> u = load8(x + d, (int64_t)a.dim - d, vec), v = load8(y + d, (int64_t)a.dim - d, vec);
+        const Vec8<T> u = load8(x + d, (int64_t)a.dim - d), v = load8(y + d, (int64_t)a.dim - d);
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum += (float)u[j] * (float)v[j];
       }
@@ -637,8 +637,8 @@ __global__ __launch_bounds__(256) void dq_kernel(PromptGradParams p) {
     return;
   }
   Held<T, DP> q, dout;
-  q.load((const T*)a.q + (int64_t)token * a.q_stride[0] + (int64_t)hq * a.q_stride[1], valid, a.dim, p.vec, half);
-  dout.load((const T*)a.dout + (int64_t)token * a.dout_stride[0] + (int64_t)hq * a.dout_stride[1], valid, a.dim, p.vec, half);
+  q.load((const T*)a.q + (int64_t)token * a.q_stride[0] + (int64_t)hq * a.q_stride[1], valid, a.dim, half);
+  dout.load((const T*)a.dout + (int64_t)token * a.dout_stride[0] + (int64_t)hq * a.dout_stride[1], valid, a.dim, half);
   const T* k = (const T*)a.k + (int64_t)sp.first * a.k_stride[0] + (int64_t)h * a.k_stride[1];
   const T* v = (const T*)a.v + (int64_t)sp.first * a.v_stride[0] + (int64_t)h * a.v_stride[1];
   const uint32_t keys = causal && r0 + kRows < sp.n ? r0 + kRows : sp.n;
@@ -649,8 +649,8 @@ __global__ __launch_bounds__(256) void dq_kernel(PromptGradParams p) {
   for (uint32_t j0 = 0; j0 < keys; j0 += kStep) {
     const bool edge = causal && j0 + kStep > r0 + 1;
     __syncthreads();
-    stage_rows<T, DP>(k, a.k_stride[0], j0, sp.n, a.dim, p.vec, false, s_k);
-    stage_rows<T, DP>(v, a.v_stride[0], j0, sp.n, a.dim, p.vec, false, s_v);
+    stage_rows<T, DP>(k, a.k_stride[0], j0, sp.n, a.dim, false, s_k);
+    stage_rows<T, DP>(v, a.v_stride[0], j0, sp.n, a.dim, false, s_v);
     __syncthreads();
     f32x16 s = times_held<T, DP>(s_k, q, lane);
     const f32x16 dp = times_held<T, DP>(s_v, dout, lane);
@@ -698,9 +698,9 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
   clear(ov);
   if (sp.in) {
     Held<T, DP> k, v;
-    k.load((const T*)a.k + (int64_t)token * a.k_stride[0] + (int64_t)h * a.k_stride[1], valid, a.dim, p.vec, half);
+    k.load((const T*)a.k + (int64_t)token * a.k_stride[0] + (int64_t)h * a.k_stride[1], valid, a.dim, half);
     if constexpr (kK)
-      v.load((const T*)a.v + (int64_t)token * a.v_stride[0] + (int64_t)h * a.v_stride[1], valid, a.dim, p.vec, half);
+      v.load((const T*)a.v + (int64_t)token * a.v_stride[0] + (int64_t)h * a.v_stride[1], valid, a.dim, half);
     const float c = a.scale * kLog2e;
     const uint32_t first = causal ? k0 : 0;
     for (uint32_t g = 0; g < p.group; ++g) {
@@ -710,8 +710,8 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
       for (uint32_t i0 = first; i0 < sp.n; i0 += kStep) {
         const bool edge = causal && i0 + 1 < k0 + kRows;  // some key is not seen by all of the rows
         __syncthreads();
-        stage_rows<T, DP>(q, a.q_stride[0], i0, sp.n, a.dim, p.vec, false, s_q);
-        stage_rows<T, DP>(dout, a.dout_stride[0], i0, sp.n, a.dim, p.vec, false, s_o);
+        stage_rows<T, DP>(q, a.q_stride[0], i0, sp.n, a.dim, false, s_q);
+        stage_rows<T, DP>(dout, a.dout_stride[0], i0, sp.n, a.dim, false, s_o);
         if (threadIdx.x < kStep) {
           const bool in = i0 + threadIdx.x < sp.n;
           const uint64_t at = p.stat(hq, sp.first + i0 + threadIdx.x);
@@ -1143,8 +1143,7 @@ template <typename T, int DP>
 hipError_t launch_prompt_grad_d(const PromptGradParams& p, hipStream_t s) {
   const gts_prompt_grad_args& a = p.a;
   const dim3 rows(p.places * a.q_heads), keys(p.places * a.kv_heads), block(256);
-  const bool out_vec = p.vec && rows_aligned(a.out, a.out_stride, sizeof(T));
-  stats_kernel<T><<<dim3((a.tokens + 63) / 64 * a.q_heads), block, 0, s>>>(p, out_vec);
+  stats_kernel<T><<<dim3((a.tokens + 63) / 64 * a.q_heads), block, 0, s>>>(p);
   if constexpr (sizeof(T) == 2) {
     if (p.vec && a.dim % 8 == 0 && rows_aligned(a.dq, a.dq_stride, 2) && rows_aligned(a.dk, a.dk_stride, 2) &&
         rows_aligned(a.dv, a.dv_stride, 2) && near(a.k_stride) && near(a.v_stride) && near(a.q_stride) && near(a.dout_stride)) {

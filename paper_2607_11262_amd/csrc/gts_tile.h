@@ -151,11 +151,23 @@ __device__ __forceinline__ Vec8<T> frag_columns(const T* s, uint32_t pitch, uint
     return r;
   }
 }
-// The first `valid` of eight values from memory, zeros behind them.  vec: rows are
-// aligned to 16 bytes.
+// Eight values from memory at any alignment (the card loads 16 bytes from any address of a
+// value), or the first `valid` of them with zeros behind.
 template <typename T>
-__device__ __forceinline__ Vec8<T> load8(const T* p, int64_t valid, bool vec) {
-  if (vec && valid >= 8) return read8(p);
+struct __attribute__((packed, aligned(sizeof(T)))) EightAnywhere {
+  T v[8];
+};
+template <typename T>
+__device__ __forceinline__ Vec8<T> load_any(const T* p) {
+  const EightAnywhere<T> x = *reinterpret_cast<const EightAnywhere<T>*>(p);
+  Vec8<T> r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = x.v[i];
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ Vec8<T> load8(const T* p, int64_t valid) {
+  if (valid >= 8) return load_any(p);
   Vec8<T> r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r[i] = i < valid ? p[i] : (T)0.f;

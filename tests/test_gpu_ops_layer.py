@@ -230,10 +230,10 @@ def test_linear_layouts(M, N, K, dtype):
 
 # Results of many tiles, whose edges and ends of the sum fall inside tiles and stages.
 LARGE = [(2048, 2048, 64), (2040, 3000, 104), (4096, 1032, 40), (3500, 1999, 96), (1, 40000, 64), (20000, 8, 32),
-         (2056, 3080, 8), (2048, 4096, 200)]
+         (2056, 3080, 8), (2048, 4096, 200), (70, 136, 9000), (1000, 300, 4104)]
 
 
-@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("M,N,K", LARGE)
 def test_linear_large(M, N, K, dtype):
     """Against 64-bit products on the card: each tile kernel, each layout of the operands."""
