@@ -5,32 +5,35 @@
 //   backward  g = dy w,  dx = r (g - mean(g) - h mean(g h)) (no mean(g) without
 //             centering),  dw = sum_rows(dy h),  db = sum_rows(dy)
 //
-// A row belongs to a team: one wave, four or sixteen, the fewest whose registers
-// hold it (32 values a thread), so x is read once and the variance is of the
-// differences, not a difference of sums.  Longer rows are read again from memory for
-// each pass over them.  Bound by HBM when large and by the launch when small.
+// A row belongs to a team: 16 lanes, a wave, four or eight, the fewest whose registers hold it
+// (16 values a lane, or 32), so x is read once and the variance is of the differences, not a
+// difference of sums.  Longer rows are read again from memory for each pass over them.
+// Bound by HBM when large (32768 rows of 4096 in bfloat16: 4.9 TB/s forward, 4.8 backward) and by
+// the launch when small.
 #include "gts_ops.h"
 #include "gts_tile.h"
 
 namespace gts {
 namespace {
 
-constexpr int kHeld = 32;  // values of a row that a thread holds
+constexpr int kHeld = 32;                   // values of a row that a lane holds
+constexpr uint32_t kLongest = 512 * kHeld;  // longest row that a team holds
 
-// Sums over a team of W waves; every lane gets them.  s: one slot a wave and sum,
-// twice, used in turn so that one barrier a call is enough.
-template <int W>
+// Sums over a team of L lanes; every lane gets them.  s: one slot a wave and sum, twice, used in
+// turn so that one barrier a call is enough.
+template <int L>
 struct Team {
+  static constexpr int W = L / 64;
   float (*s)[2][16];
   uint32_t turn = 0;
-  __device__ __forceinline__ static float wave_sum(float x) {
+  __device__ __forceinline__ static float lanes_sum(float x) {
 #pragma unroll
-    for (int k = 32; k; k >>= 1) x += __shfl_xor(x, k);
+    for (int k = L < 64 ? L / 2 : 32; k; k >>= 1) x += __shfl_xor(x, k);
     return x;
   }
   __device__ __forceinline__ void sum2(float& a, float& b) {
-    a = wave_sum(a);
-    b = wave_sum(b);
+    a = lanes_sum(a);
+    b = lanes_sum(b);
     if constexpr (W > 1) {
       float(*t)[16] = s[turn & 1];
       ++turn;
@@ -55,52 +58,75 @@ struct Team {
   }
 };
 
-// Threads of a workgroup: teams of one wave share one of four.
-template <int W>
-constexpr int kThreads = W == 1 ? 256 : W * 64;
-template <int W>
-constexpr int kTeams = W == 1 ? 4 : 1;
+template <int L>
+constexpr int kThreads = L < 256 ? 256 : L;
+template <int L>
+constexpr int kTeams = kThreads<L> / L;
 
-// V values at column at of a row, zeros behind its end (V divides the row's length, so
-// an access is inside or outside as a whole).
+// V values of a row, loaded and stored at any alignment.
 template <typename T, int V>
-__device__ __forceinline__ Pack<T, V> columns(const T* row, uint32_t at, uint32_t dim) {
-  Pack<T, V> x = {};
-  if (at < dim) x = *reinterpret_cast<const Pack<T, V>*>(row + at);
-  return x;
-}
+struct __attribute__((packed, aligned(sizeof(T)))) Anywhere {
+  T v[V];
+};
+// A lane's c-th access to a row: V values from column `at` on.  WHOLE: V divides the row.  Else
+// the last access of a row reaches back over `skip` values that are another lane's: they are left
+// out of sums, and stored by both.
+template <typename T, int V, int L, bool WHOLE>
+struct Access {
+  uint32_t at, skip;
+  bool in;
+  __device__ __forceinline__ Access(int c, uint32_t lane, uint32_t dim) : at((c * L + lane) * V), skip(0), in(at < dim) {
+    if (!WHOLE && in && at + V > dim) {
+      skip = at + V - dim;
+      at -= skip;
+    }
+  }
+  __device__ __forceinline__ Anywhere<T, V> load(const T* row) const {
+    Anywhere<T, V> x = {};
+    if (in) x = *reinterpret_cast<const Anywhere<T, V>*>(row + at);
+    return x;
+  }
+  __device__ __forceinline__ void store(T* row, const Anywhere<T, V>& x) const {
+    if (in) *reinterpret_cast<Anywhere<T, V>*>(row + at) = x;
+  }
+  // Whether value i is the lane's own (one outside the row is zero).
+  __device__ __forceinline__ bool own(int i) const { return WHOLE || i >= (int)skip; }
+};
 
-template <typename T, int V, int W, int C>
-__global__ __launch_bounds__(kThreads<W>) void norm_kernel(gts_norm_args a) {
+template <typename T, int V, int L, int C, bool WHOLE>
+__global__ __launch_bounds__(kThreads<L>) void norm_kernel(gts_norm_args a) {
   __shared__ float s_sum[2][2][16];
-  Team<W> team{s_sum};
-  const uint32_t lane = W == 1 ? threadIdx.x & 63u : threadIdx.x;
-  const uint64_t row = block_number() * kTeams<W> + (W == 1 ? threadIdx.x >> 6 : 0);
+  Team<L> team{s_sum};
+  const uint32_t lane = threadIdx.x % L;
+  const uint64_t row = block_number() * kTeams<L> + threadIdx.x / L;
   if (row >= a.rows) return;
   const bool center = a.flags & GTS_NORM_CENTER;
   const T* x = (const T*)a.x + (int64_t)row * a.x_stride;
   const float n = 1.f / (float)a.dim;
-  Pack<T, V> v[C];
+  Anywhere<T, V> v[C];
 #pragma unroll
-  for (int c = 0; c < C; ++c) v[c] = columns<T, V>(x, (c * W * 64 + lane) * V, a.dim);
+  for (int c = 0; c < C; ++c) v[c] = Access<T, V, L, WHOLE>(c, lane, a.dim).load(x);
   float mu = 0.f;
   if (center) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c) {
+      const Access<T, V, L, WHOLE> at(c, lane, a.dim);
 #pragma unroll
-      for (int i = 0; i < V; ++i) mu += (float)v[c].v[i];
+      for (int i = 0; i < V; ++i) mu += at.own(i) ? (float)v[c].v[i] : 0.f;
+    }
     mu = team.sum(mu) * n;
   }
   float q = 0.f;
 #pragma unroll
-  for (int c = 0; c < C; ++c)
-    if ((c * W * 64 + lane) * V < a.dim) {
+  for (int c = 0; c < C; ++c) {
+    const Access<T, V, L, WHOLE> at(c, lane, a.dim);
+    if (!at.in) continue;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float d = (float)v[c].v[i] - mu;
-        q += d * d;
-      }
+    for (int i = 0; i < V; ++i) {
+      const float d = at.own(i) ? (float)v[c].v[i] - mu : 0.f;
+      q += d * d;
     }
+  }
   const float r = 1.f / sqrtf(team.sum(q) * n + a.eps);
   if (lane == 0) {
     if (a.mean) a.mean[row] = mu;
@@ -109,11 +135,11 @@ __global__ __launch_bounds__(kThreads<W>) void norm_kernel(gts_norm_args a) {
   T* y = (T*)a.out + (int64_t)row * a.out_stride;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const uint32_t at = (c * W * 64 + lane) * V;
-    if (at >= a.dim) continue;
-    const Pack<T, V> w = a.weight ? *reinterpret_cast<const Pack<T, V>*>((const T*)a.weight + at) : Pack<T, V>{};
-    const Pack<T, V> b = a.bias ? *reinterpret_cast<const Pack<T, V>*>((const T*)a.bias + at) : Pack<T, V>{};
-    Pack<T, V> o;
+    const Access<T, V, L, WHOLE> at(c, lane, a.dim);
+    if (!at.in) continue;
+    Anywhere<T, V> w = {}, b = {}, o;
+    if (a.weight) w = at.load((const T*)a.weight);
+    if (a.bias) b = at.load((const T*)a.bias);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       float h = ((float)v[c].v[i] - mu) * r;
@@ -121,15 +147,15 @@ __global__ __launch_bounds__(kThreads<W>) void norm_kernel(gts_norm_args a) {
       if (a.bias) h += (float)b.v[i];
       o.v[i] = (T)h;
     }
-    *reinterpret_cast<Pack<T, V>*>(y + at) = o;
+    at.store(y, o);
   }
 }
 
-// Rows of any length: three passes over memory, sums of a thread in order.
+// Rows of any other length: three passes over memory, sums of a thread in order.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_long_kernel(gts_norm_args a) {
   __shared__ float s_sum[2][2][16];
-  Team<16> team{s_sum};
+  Team<1024> team{s_sum};
   const uint64_t row = block_number();
   if (row >= a.rows) return;
   const T* x = (const T*)a.x + (int64_t)row * a.x_stride;
@@ -156,83 +182,121 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(gts_norm_args a) {
   }
 }
 
-// The gradient.  A workgroup takes every gridDim.x-th group of rows and keeps its part
-// of dw and db in registers: columns of a thread are the same in every row.  The
-// parts, one row of scratch a workgroup, are added up in order by sum_kernel.
+// The gradient.  A team takes every (gridDim.x x teams)-th row and keeps its part of dw and db in
+// registers: columns of a lane are the same in every row.  The teams of a workgroup join theirs in
+// LDS; the parts, one row of scratch a workgroup, are added up in order by column_sums_kernel.
 struct NormGradParams {
   gts_norm_grad_args a;
   float *dw, *db;  // [groups][dim], NULL if not wanted
 };
 
-template <typename T, int V, int W, int C>
-__global__ __launch_bounds__(kThreads<W>) void norm_grad_kernel(NormGradParams p) {
+template <typename T, int V, int L, int C, bool WHOLE>
+__global__ __launch_bounds__(kThreads<L>) void norm_grad_kernel(NormGradParams p) {
   __shared__ float s_sum[2][2][16];
   const gts_norm_grad_args& a = p.a;
-  Team<W> team{s_sum};
-  const uint32_t lane = W == 1 ? threadIdx.x & 63u : threadIdx.x, mine = W == 1 ? threadIdx.x >> 6 : 0;
+  Team<L> team{s_sum};
+  const uint32_t lane = threadIdx.x % L, mine = threadIdx.x / L;
   const float n = 1.f / (float)a.dim;
   const bool center = a.flags & GTS_NORM_CENTER;
   float dw[C][V] = {}, db[C][V] = {};
-  Pack<T, V> w[C];
+  Anywhere<T, V> w[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const uint32_t at = (c * W * 64 + lane) * V;
     if (a.weight) {
-      w[c] = columns<T, V>((const T*)a.weight, at, a.dim);
+      w[c] = Access<T, V, L, WHOLE>(c, lane, a.dim).load((const T*)a.weight);
     } else {
 #pragma unroll
       for (int i = 0; i < V; ++i) w[c].v[i] = (T)1.f;
     }
   }
-  for (uint64_t row = (uint64_t)blockIdx.x * kTeams<W> + mine; row < a.rows; row += (uint64_t)gridDim.x * kTeams<W>) {
+  // The next row is on its way while a row's sums are taken (32768 rows of 4096 in bfloat16: 252
+  // us without, 168 with).
+  Anywhere<T, V> xv[C], dv[C];
+  float mu = 0.f, r = 0.f;
+  const uint64_t step = (uint64_t)gridDim.x * kTeams<L>;
+  const auto load = [&](uint64_t row) {
     const T* x = (const T*)a.x + (int64_t)row * a.x_stride;
     const T* dy = (const T*)a.dy + (int64_t)row * a.dy_stride;
-    Pack<T, V> xv[C], dv[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const uint32_t at = (c * W * 64 + lane) * V;
-      xv[c] = columns<T, V>(x, at, a.dim);
-      dv[c] = columns<T, V>(dy, at, a.dim);
+      const Access<T, V, L, WHOLE> at(c, lane, a.dim);
+      xv[c] = at.load(x);
+      dv[c] = at.load(dy);
     }
-    const float mu = center ? a.mean[row] : 0.f, r = a.rstd[row];
-    float sg = 0.f, sgh = 0.f;
+    mu = center ? a.mean[row] : 0.f;
+    r = a.rstd[row];
+  };
+  uint64_t row = (uint64_t)blockIdx.x * kTeams<L> + mine;
+  if (row < a.rows) load(row);
+  for (; row < a.rows; row += step) {
+    float h[C][V], g[C][V], sg = 0.f, sgh = 0.f;
+    const float rs = r;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-      if ((c * W * 64 + lane) * V < a.dim) {
+    for (int c = 0; c < C; ++c) {
+      const Access<T, V, L, WHOLE> at(c, lane, a.dim);
+      if (!at.in) continue;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float h = ((float)xv[c].v[i] - mu) * r, d = (float)dv[c].v[i], g = d * (float)w[c].v[i];
-          sg += g;
-          sgh += g * h;
-          dw[c][i] += d * h;
-          db[c][i] += d;
+      for (int i = 0; i < V; ++i) {
+        const float d = (float)dv[c].v[i];
+        h[c][i] = ((float)xv[c].v[i] - mu) * r;
+        g[c][i] = d * (float)w[c].v[i];
+        if (at.own(i)) {
+          sg += g[c][i];
+          sgh += g[c][i] * h[c][i];
         }
+        dw[c][i] += d * h[c][i];
+        db[c][i] += d;
       }
+    }
+    if (row + step < a.rows) load(row + step);
     team.sum2(sg, sgh);
     const float mg = center ? sg * n : 0.f, mgh = sgh * n;
+    if (!a.dx) continue;
     T* dx = (T*)a.dx + (int64_t)row * a.dx_stride;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const uint32_t at = (c * W * 64 + lane) * V;
-      if (at >= a.dim) continue;
-      Pack<T, V> o;
+      const Access<T, V, L, WHOLE> at(c, lane, a.dim);
+      if (!at.in) continue;
+      Anywhere<T, V> o;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float h = ((float)xv[c].v[i] - mu) * r;
-        o.v[i] = (T)(((float)dv[c].v[i] * (float)w[c].v[i] - mg - h * mgh) * r);
-      }
-      if (a.dx) *reinterpret_cast<Pack<T, V>*>(dx + at) = o;
+      for (int i = 0; i < V; ++i) o.v[i] = (T)((g[c][i] - mg - h[c][i] * mgh) * rs);
+      at.store(dx, o);
     }
   }
-  const uint64_t part = ((uint64_t)blockIdx.x * kTeams<W> + mine) * a.dim;
+  const uint64_t part = (uint64_t)blockIdx.x * a.dim;
+  if constexpr (kTeams<L> == 1) {
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const uint32_t at = (c * W * 64 + lane) * V;
-    if (at >= a.dim) continue;
+    for (int c = 0; c < C; ++c) {
+      const Access<T, V, L, WHOLE> at(c, lane, a.dim);
+      if (!at.in) continue;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (p.dw) p.dw[part + at + i] = dw[c][i];
-      if (p.db) p.db[part + at + i] = db[c][i];
+      for (int i = 0; i < V; ++i) {
+        if (!at.own(i)) continue;
+        if (p.dw) p.dw[part + at.at + i] = dw[c][i];
+        if (p.db) p.db[part + at.at + i] = db[c][i];
+      }
+    }
+  } else {
+    __shared__ float s_part[kTeams<L>][C * L * V];
+    for (int which = 0; which < 2; ++which) {
+      float* to = which ? p.db : p.dw;
+      if (!to) continue;
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const Access<T, V, L, WHOLE> at(c, lane, a.dim);
+        if (!at.in) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (at.own(i)) s_part[mine][at.at + i] = which ? db[c][i] : dw[c][i];
+      }
+      __syncthreads();
+      for (uint32_t at = threadIdx.x; at < a.dim; at += kThreads<L>) {
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < kTeams<L>; ++t) sum += s_part[t][at];
+        to[part + at] = sum;
+      }
     }
   }
 }
@@ -241,7 +305,7 @@ __global__ __launch_bounds__(kThreads<W>) void norm_grad_kernel(NormGradParams p
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(gts_norm_grad_args a) {
   __shared__ float s_sum[2][2][16];
-  Team<16> team{s_sum};
+  Team<1024> team{s_sum};
   const uint64_t row = block_number();
   if (row >= a.rows) return;
   const T* x = (const T*)a.x + (int64_t)row * a.x_stride;
@@ -279,94 +343,82 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormGradParams p) {
   if (p.db) p.db[(uint64_t)blockIdx.y * a.dim + at] = db;
 }
 
-bool wide(uint64_t bytes, uint64_t elements, uint32_t v, uint32_t e) { return bytes % (v * e) == 0 && elements % v == 0; }
-uint64_t size(int64_t x) { return (uint64_t)(x < 0 ? -x : x); }
-
-template <typename T, int V, int W>
-void launch_norm_w(const gts_norm_args& a, hipStream_t s) {
-  const uint32_t per = W * 64 * V;
-  const dim3 grid = grid_of(((uint64_t)a.rows + kTeams<W> - 1) / kTeams<W>), block(kThreads<W>);
-  constexpr int C = kHeld / V;
-  if (C >= 4 && a.dim <= per * (C / 4))
-    norm_kernel<T, V, W, C / 4 ? C / 4 : 1><<<grid, block, 0, s>>>(a);
-  else if (C >= 2 && a.dim <= per * (C / 2))
-    norm_kernel<T, V, W, C / 2 ? C / 2 : 1><<<grid, block, 0, s>>>(a);
+// The team of a row: lanes, and the accesses of 16 bytes that each makes.
+template <template <typename, int, int, int> class K, typename T, int L, typename P>
+void launch_lanes(const P& p, uint32_t dim, uint32_t groups, hipStream_t s) {
+  constexpr int V = 16 / sizeof(T), C = kHeld / V;
+  if (dim <= L * V * (C / 4))
+    K<T, V, L, C / 4>::go(p, groups, s);
+  else if (dim <= L * V * (C / 2))
+    K<T, V, L, C / 2>::go(p, groups, s);
   else
-    norm_kernel<T, V, W, C><<<grid, block, 0, s>>>(a);
+    K<T, V, L, C>::go(p, groups, s);
 }
-
-template <typename T, int V>
-void launch_norm_v(const gts_norm_args& a, hipStream_t s) {
-  if (a.dim <= 64 * kHeld / 2)
-    launch_norm_w<T, V, 1>(a, s);
-  else if (a.dim <= 256 * kHeld)
-    launch_norm_w<T, V, 4>(a, s);
-  else
-    launch_norm_w<T, V, 16>(a, s);
+// Rows that teams take: neither longer than they hold nor shorter than an access.
+template <typename T>
+bool held(uint32_t dim) {
+  return dim <= kLongest && dim >= 16 / sizeof(T);
 }
+uint32_t lanes_of(uint32_t dim) {
+  return dim <= 16 * kHeld / 2 ? 16 : dim <= 64 * kHeld / 2 ? 64 : dim <= 256 * kHeld ? 256 : 512;
+}
+template <template <typename, int, int, int> class K, typename T, typename P>
+void launch_team(const P& p, uint32_t dim, uint32_t groups, hipStream_t s) {
+  switch (lanes_of(dim)) {
+    case 16: return launch_lanes<K, T, 16>(p, dim, groups, s);
+    case 64: return launch_lanes<K, T, 64>(p, dim, groups, s);
+    case 256: return launch_lanes<K, T, 256>(p, dim, groups, s);
+    default: return launch_lanes<K, T, 512>(p, dim, groups, s);
+  }
+}
+template <typename T, int V, int L, int C>
+struct Forward {
+  static void go(const gts_norm_args& a, uint32_t, hipStream_t s) {
+    const dim3 grid = grid_of(((uint64_t)a.rows + kTeams<L> - 1) / kTeams<L>);
+    if (a.dim % V == 0)
+      norm_kernel<T, V, L, C, true><<<grid, dim3(kThreads<L>), 0, s>>>(a);
+    else
+      norm_kernel<T, V, L, C, false><<<grid, dim3(kThreads<L>), 0, s>>>(a);
+  }
+};
+template <typename T, int V, int L, int C>
+struct Gradient {
+  static void go(const NormGradParams& p, uint32_t groups, hipStream_t s) {
+    if (p.a.dim % V == 0)
+      norm_grad_kernel<T, V, L, C, true><<<dim3(groups), dim3(kThreads<L>), 0, s>>>(p);
+    else
+      norm_grad_kernel<T, V, L, C, false><<<dim3(groups), dim3(kThreads<L>), 0, s>>>(p);
+  }
+};
 
 template <typename T>
 void launch_norm_t(const gts_norm_args& a, hipStream_t s) {
-  constexpr int V = 16 / sizeof(T);
-  if (a.dim > 1024 * kHeld) {
+  if (!held<T>(a.dim))
     norm_long_kernel<T><<<grid_of(a.rows), dim3(1024), 0, s>>>(a);
-    return;
-  }
-  const uint64_t bytes = (uint64_t)(uintptr_t)a.x | (uint64_t)(uintptr_t)a.out | (uint64_t)(uintptr_t)a.weight |
-                         (uint64_t)(uintptr_t)a.bias;
-  if (wide(bytes, size(a.x_stride) | size(a.out_stride) | a.dim, V, sizeof(T)))
-    launch_norm_v<T, V>(a, s);
   else
-    launch_norm_v<T, 1>(a, s);
+    launch_team<Forward, T>(a, a.dim, 0, s);
 }
 
-// Workgroups of the gradient: rows enough for each, and two a CU at most, so that
-// the parts stay small beside the rows.
-constexpr uint32_t kGradGroups = 512;
-uint32_t grad_groups(uint32_t rows) {
-  const uint64_t n = ((uint64_t)rows + 3) / 4;
-  return n < 1 ? 1 : n < kGradGroups ? (uint32_t)n : kGradGroups;  // no rows: sums of nothing
+// Workgroups of the gradient, and so rows of parts: eight rows a team, so that the parts stay small
+// beside the rows, but 128 of them where there are two rows for each team, and 512 at most (no
+// rows: sums of nothing).
+uint32_t grad_groups(uint32_t rows, uint32_t dim) {
+  const uint32_t lanes = lanes_of(dim), teams = lanes < 256 ? 256 / lanes : 1;
+  const auto groups = [&](uint32_t each) { return (uint32_t)(((uint64_t)rows + each * teams - 1) / (each * teams)); };
+  const uint32_t few = groups(2) < 128 ? groups(2) : 128, n = groups(8) > few ? groups(8) : few;
+  return n < 1 ? 1 : n < 512 ? n : 512;
 }
-// Rows of parts: four a workgroup where a team is one wave.
-uint32_t grad_parts(uint32_t rows, uint32_t dim) { return grad_groups(rows) * (dim <= 64 * kHeld / 2 ? 4 : 1); }
 
-template <typename T, int V, int W>
-void launch_grad_w(const NormGradParams& p, hipStream_t s) {
-  const uint32_t per = W * 64 * V;
-  const dim3 grid(grad_groups(p.a.rows)), block(kThreads<W>);
-  constexpr int C = kHeld / V;
-  if (C >= 4 && p.a.dim <= per * (C / 4))
-    norm_grad_kernel<T, V, W, C / 4 ? C / 4 : 1><<<grid, block, 0, s>>>(p);
-  else if (C >= 2 && p.a.dim <= per * (C / 2))
-    norm_grad_kernel<T, V, W, C / 2 ? C / 2 : 1><<<grid, block, 0, s>>>(p);
-  else
-    norm_grad_kernel<T, V, W, C><<<grid, block, 0, s>>>(p);
-}
-template <typename T, int V>
-void launch_grad_v(const NormGradParams& p, hipStream_t s) {
-  if (p.a.dim <= 64 * kHeld / 2)
-    launch_grad_w<T, V, 1>(p, s);
-  else if (p.a.dim <= 256 * kHeld)
-    launch_grad_w<T, V, 4>(p, s);
-  else
-    launch_grad_w<T, V, 16>(p, s);
-}
 template <typename T>
 void launch_grad_t(const NormGradParams& p, hipStream_t s) {
   const gts_norm_grad_args& a = p.a;
-  constexpr int V = 16 / sizeof(T);
-  if (a.dim > 1024 * kHeld) {
+  const uint32_t groups = grad_groups(a.rows, a.dim);
+  if (!held<T>(a.dim)) {
     if (a.dx && a.rows) norm_grad_long_kernel<T><<<grid_of(a.rows), dim3(1024), 0, s>>>(a);
-    if (p.dw || p.db)
-      norm_columns_kernel<T><<<dim3((a.dim + 255) / 256, grad_parts(a.rows, a.dim)), dim3(256), 0, s>>>(p);
+    if (p.dw || p.db) norm_columns_kernel<T><<<dim3((a.dim + 255) / 256, groups), dim3(256), 0, s>>>(p);
     return;
   }
-  const uint64_t bytes = (uint64_t)(uintptr_t)a.x | (uint64_t)(uintptr_t)a.dy | (uint64_t)(uintptr_t)a.weight |
-                         (uint64_t)(uintptr_t)a.dx;
-  if (wide(bytes, size(a.x_stride) | size(a.dy_stride) | size(a.dx_stride) | a.dim, V, sizeof(T)))
-    launch_grad_v<T, V>(p, s);
-  else
-    launch_grad_v<T, 1>(p, s);
+  launch_team<Gradient, T>(p, a.dim, groups, s);
 }
 
 }  // namespace
@@ -381,11 +433,11 @@ hipError_t launch_norm(const gts_norm_args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-uint64_t norm_grad_scratch(uint32_t rows, uint32_t dim) { return 8ull * grad_parts(rows, dim) * dim; }
+uint64_t norm_grad_scratch(uint32_t rows, uint32_t dim) { return 8ull * grad_groups(rows, dim) * dim; }
 
 hipError_t launch_norm_grad(const gts_norm_grad_args& a, hipStream_t s) {
   NormGradParams p{a, nullptr, nullptr};
-  const uint32_t parts = grad_parts(a.rows, a.dim);
+  const uint32_t parts = grad_groups(a.rows, a.dim);
   if (a.dweight) p.dw = (float*)a.scratch;
   if (a.dbias) p.db = (float*)a.scratch + (uint64_t)parts * a.dim;
   if (a.dtype == GTS_F32)
@@ -401,38 +453,42 @@ hipError_t launch_norm_grad(const gts_norm_grad_args& a, hipStream_t s) {
 
 // ---- sums of parts ------------------------------------------------------------------
 
-// out[c] = the sum over parts p of in[p][c], p in the same order on every run: a
-// workgroup takes 64 columns, a wave every fourth part.
+// out[c] = the sum over parts p of in[p][c], p in the same order on every run: a workgroup takes
+// 64 columns, a wave every 16th part, eight loads on their way.
 template <typename T>
-__global__ __launch_bounds__(256) void column_sums_kernel(const float* in0, void* out0, const float* in1, void* out1,
-                                                          uint32_t parts, uint32_t n) {
-  __shared__ float s[4][64];
+__global__ __launch_bounds__(1024) void column_sums_kernel(const float* in0, void* out0, const float* in1, void* out1,
+                                                           uint32_t parts, uint32_t n) {
+  __shared__ float s[16][64];
   const float* in = blockIdx.y ? in1 : in0;
   T* out = (T*)(blockIdx.y ? out1 : out0);
   if (!in) return;
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   float sum = 0.f;
   if (c < n) {
-    // eight loads on their way
     uint32_t i = wave;
-    for (; i + 28 < parts; i += 32) {
+    for (; i + 112 < parts; i += 128) {
       float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = in[(uint64_t)(i + 4 * k) * n + c];
+      for (int k = 0; k < 8; ++k) v[k] = in[(uint64_t)(i + 16 * k) * n + c];
 #pragma unroll
       for (int k = 0; k < 8; ++k) sum += v[k];
     }
-    for (; i < parts; i += 4) sum += in[(uint64_t)i * n + c];
+    for (; i < parts; i += 16) sum += in[(uint64_t)i * n + c];
   }
   s[wave][lane] = sum;
   __syncthreads();
-  if (wave == 0 && c < n) out[c] = (T)((s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]));
+  if (wave == 0 && c < n) {
+    sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sum += s[k][lane];
+    out[c] = (T)sum;
+  }
 }
 
 hipError_t launch_column_sums(const float* in0, void* out0, const float* in1, void* out1, uint32_t parts, uint32_t n,
                               uint32_t dtype, hipStream_t s) {
   if (!in0 && !in1) return hipSuccess;
-  const dim3 grid((n + 63) / 64, in1 ? 2 : 1), block(256);
+  const dim3 grid((n + 63) / 64, in1 ? 2 : 1), block(1024);
   if (dtype == GTS_F32)
     column_sums_kernel<float><<<grid, block, 0, s>>>(in0, out0, in1, out1, parts, n);
   else if (dtype == GTS_BF16)

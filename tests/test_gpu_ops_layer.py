@@ -479,3 +479,341 @@ def test_prompt_long_against_blocks():
     refs, errs = R.prompt_gradient(*d64(dout, q, k, v, o, lse), None, True, None, BF)
     for a, r, e, name in zip(got, refs, errs, ("dq", "dk", "dv")):
         close(a, r, e, BF, name)
+
+
+# ---- autograd, streams, graphs, refusals ------------------------------------------------------
+
+def directional(f, tensors, dirs, eps=1e-6):
+    """Central difference of the 64-bit function f along dirs."""
+    up = f(*[t + eps * d for t, d in zip(tensors, dirs)])
+    down = f(*[t - eps * d for t, d in zip(tensors, dirs)])
+    return (up - down) / (2 * eps)
+
+
+def check_autograd(op, reference, tensors, seed):
+    """Gradients of a weighted sum of op's result against differences of the 64-bit reference:
+    the bound is that of 32-bit sums of the terms' size."""
+    g = gen(seed)
+    leaves = [t.cuda().requires_grad_() for t in tensors]
+    y = op(*leaves)
+    c = randn(g, *y.shape)
+    (y * c.cuda()).sum().backward()
+    dirs = [torch.randn(t.shape, generator=g, dtype=torch.float64) for t in tensors]
+    got = sum((leaf.grad.cpu().double() * d).sum() for leaf, d in zip(leaves, dirs))
+    size = sum((leaf.grad.cpu().double().abs() * d.abs()).sum() for leaf, d in zip(leaves, dirs))
+    ref = directional(lambda *a: (reference(*a) * c.double()).sum(), d64(*tensors), dirs)
+    # each gradient is off by a few thousand roundings at most (sums of up to 300 products, twice);
+    # the difference itself is off by eps^2 and 1e-16 / eps of the sum
+    assert abs(got - ref) <= 4096 * R.E * size + 1e-6 * (1 + abs(ref)), (got, ref)
+
+
+def test_norm_autograd():
+    g = gen(1)
+    x, w, b = randn(g, 7, 130), randn(g, 130), randn(g, 130)
+    check_autograd(lambda x, w, b: ops.layer_norm(x, w, b), lambda x, w, b: R.norm(x, w, b, 1e-5, True)[0], (x, w, b), 2)
+    check_autograd(lambda x, w: ops.layer_norm(x.view(7, 10, 13).transpose(0, 1), w, center=False).transpose(0, 1).reshape(7, 130),
+                   lambda x, w: R.norm(x.view(70, 13), w, None, 1e-5, False)[0].view(7, 130), (x, w[:13].clone()), 3)
+    # only what is asked for
+    x1 = x.cuda()
+    w1 = w.cuda().requires_grad_()
+    ops.layer_norm(x1, w1).sum().backward()
+    assert w1.grad is not None and x1.grad is None
+    # a gradient that is an expanded view, one that is not contiguous
+    x2 = x.cuda().requires_grad_()
+    ops.layer_norm(x2, w.cuda()).sum().backward()
+    x3 = x.cuda().requires_grad_()
+    ops.layer_norm(x3, w.cuda()).t().contiguous().sum().backward()
+    assert torch.equal(x2.grad, x3.grad)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_linear_autograd(act):
+    g = gen(4)
+    t = randn(g, 9, 40), randn(g, 24, 40, scale=0.2), randn(g, 24), randn(g, 9, 24), randn(g, 9, 24)
+    z = t[0] @ t[1].T + t[2]
+    if act == "relu":  # differences do not cross its corner
+        t[2].add_(0)
+        assert (z.abs() > 1e-4).all()
+    check_autograd(lambda x, w, b, gt, r: ops.linear(x, w, b, activation=act, gate=gt, residual=r),
+                   lambda x, w, b, gt, r: R.linear(x, w, b, act, gt, r)[0], t, 5)
+    check_autograd(lambda x, w: ops.linear(x.view(3, 3, 40), w, activation=act).view(9, 24),
+                   lambda x, w: R.linear(x, w, None, act, None, None)[0], t[:2], 6)
+    # only what is asked for; the same tensor twice
+    w = t[1].cuda().requires_grad_()
+    ops.linear(t[0].cuda(), w, activation=act).sum().backward()
+    assert w.grad.shape == w.shape
+    r = t[3].cuda().requires_grad_()
+    y = ops.linear(t[0].cuda(), t[1].cuda(), activation=act, gate=r, residual=r)
+    y.sum().backward()
+    zd = t[0].double() @ t[1].double().T
+    close(r.grad, R.activation(act, zd) + 1, 1e-4 * (1 + zd.abs()), F, "gate and residual")
+
+
+def test_prompt_autograd():
+    g = gen(7)
+    starts = torch.tensor([0, 37, 37, 140], dtype=torch.int32)
+    q, k, v = randn(g, 140, 4, 32), randn(g, 140, 2, 32), randn(g, 140, 2, 32)
+    for causal in (True, False):
+        check_autograd(lambda q, k, v: ops.prompt_attention(q, k, v, starts.cuda(), causal=causal),
+                       lambda q, k, v: R.prompt(q, k, v, starts, causal, None, F)[0], (q, k, v), 8)
+    # one leaf that is queries, keys and values (views of one projection)
+    qkv = randn(g, 60, 6, 32)
+    check_autograd(lambda x: ops.prompt_attention(*x.split((2, 2, 2), 1)),
+                   lambda x: R.prompt(*x.split((2, 2, 2), 1), None, True, None, F)[0], (qkv,), 9)
+
+
+def test_once_differentiable_and_refused_derivatives():
+    from torch.autograd import forward_ad
+    x = torch.randn(4, 64, device="cuda", requires_grad=True)
+    w = torch.randn(64, 64, device="cuda")
+    q = torch.randn(5, 2, 32, device="cuda", requires_grad=True)
+    calls = {"norm": lambda t: ops.layer_norm(t), "linear": lambda t: ops.linear(t, w, activation="silu")}
+    for name, f in calls.items():
+        gx, = torch.autograd.grad(f(x).square().sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError):
+            gx.sum().backward()
+        with forward_ad.dual_level(), torch.no_grad():
+            with pytest.raises(ValueError, match="tangent"):
+                f(forward_ad.make_dual(x.detach(), torch.ones_like(x)))
+    gq, = torch.autograd.grad(ops.prompt_attention(q, q, q).square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError):
+        gq.sum().backward()
+    out = torch.empty(4, 64, device="cuda")
+    for f in (lambda: ops.layer_norm(x, out=out), lambda: ops.linear(x, w, out=out), lambda: ops.linear(x, w, preact=out),
+              lambda: ops.layer_norm(x, rstd=out[:, 0].contiguous()), lambda: ops.prompt_attention(q, q, q, out=torch.empty_like(q))):
+        with pytest.raises(ValueError, match="requires a gradient"):
+            f()
+    for f in (lambda: ops.layer_norm_backward(out, x, None, out[:, 0].contiguous()), lambda: ops.linear_backward(out, x, w),
+              lambda: ops.layer_norm(out, out=x), lambda: ops.linear(out, w, out=x)):
+        with pytest.raises(ValueError, match="requires a gradient"):
+            f()
+
+
+def test_writes_are_known_to_autograd():
+    x = torch.randn(4, 64, device="cuda")
+    w = torch.randn(64, 64, device="cuda")
+    leaf = torch.randn(4, 64, device="cuda", requires_grad=True)
+    q = torch.randn(4, 2, 32, device="cuda")
+    lse, rstd = torch.empty(4, 2, device="cuda"), torch.empty(4, device="cuda")
+    for t, f in ((x, lambda: ops.layer_norm(x, out=x)), (x, lambda: ops.linear(x, w, out=x, residual=x)),
+                 (x, lambda: ops.linear(leaf.detach(), w, preact=x)), (q, lambda: ops.prompt_attention(q.clone(), q.clone(), q.clone(), out=q)),
+                 (lse, lambda: ops.prompt_attention(q, q, q, lse=lse)), (rstd, lambda: ops.layer_norm(x, rstd=rstd))):
+        before = t._version
+        f()
+        assert t._version > before
+    # an operand changed between forward and backward is noticed
+    y = ops.linear(leaf * 1.0, w.clone().requires_grad_())
+    wide = (leaf * 2.0)
+    y = ops.layer_norm(wide)
+    wide.add_(1.0)
+    with pytest.raises(RuntimeError, match="modified"):
+        y.sum().backward()
+
+
+def layer_state(dtype=BF, T=300, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    hidden, heads, kv, D, ffn = 256, 4, 2, 64, 512
+    rand = lambda *s, scale=1.0: (torch.randn(s, generator=g, device="cuda") * scale).to(dtype)  # noqa: E731
+    p = dict(n1=1 + rand(hidden, scale=0.1), wqkv=rand((heads + 2 * kv) * D, hidden, scale=hidden ** -0.5),
+             wo=rand(hidden, heads * D, scale=0.06), n2=1 + rand(hidden, scale=0.1), wg=rand(ffn, hidden, scale=hidden ** -0.5),
+             wu=rand(ffn, hidden, scale=hidden ** -0.5), wd=rand(hidden, ffn, scale=ffn ** -0.5))
+    starts = torch.tensor([0, 1, 130, T], dtype=torch.int32, device="cuda")
+    positions = torch.cat([torch.arange(n) for n in (1, 129, T - 130)]).cuda()
+    return dict(p=p, x=rand(T, hidden), dy=rand(T, hidden), starts=starts, positions=positions,
+                table=ops.rotary_table(T, D), heads=heads, kv=kv, D=D)
+
+
+def layer(s, x, p):
+    """A decoder layer as a user writes it."""
+    h = ops.layer_norm(x, p["n1"], center=False)
+    q, k, v = ops.linear(h, p["wqkv"]).view(x.shape[0], -1, s["D"]).split((s["heads"], s["kv"], s["kv"]), 1)
+    q, k = ops.rotary(q, s["positions"], s["table"]), ops.rotary(k, s["positions"], s["table"])
+    x = ops.linear(ops.prompt_attention(q, k, v, s["starts"]).flatten(1), p["wo"], residual=x)
+    h = ops.layer_norm(x, p["n2"], center=False)
+    return ops.linear(ops.linear(h, p["wg"], activation="silu", gate=ops.linear(h, p["wu"])), p["wd"], residual=x)
+
+
+def layer64(s, x, p):
+    """The same from the formulas in 64 bits, on the CPU."""
+    norm = lambda x, w: x / (x.square().mean(1, keepdim=True) + 1e-5).sqrt() * w  # noqa: E731
+    rows = s["table"].cpu().double()[s["positions"].cpu()][:, None]
+
+    def turn(t):
+        a, b = t.chunk(2, -1)
+        c, d = rows.chunk(2, -1)
+        return torch.cat((a * c - b * d, b * c + a * d), -1)
+
+    T, G = x.shape[0], s["heads"] // s["kv"]
+    q, k, v = (norm(x, p["n1"]) @ p["wqkv"].T).view(T, -1, s["D"]).split((s["heads"], s["kv"], s["kv"]), 1)
+    q, k = turn(q), turn(k)
+    parts = []
+    for a, b in R.spans(T, s["starts"].cpu()):
+        w = torch.einsum("ihd,jhd->hij", q[a:b], k[a:b].repeat_interleave(G, 1)) * s["D"] ** -0.5
+        w = w.masked_fill(torch.ones(b - a, b - a, dtype=torch.bool).triu(1), -math.inf).softmax(-1)
+        parts.append(torch.einsum("hij,jhd->ihd", w, v[a:b].repeat_interleave(G, 1)))
+    x = x + torch.cat(parts).flatten(1) @ p["wo"].T
+    h = norm(x, p["n2"])
+    z = h @ p["wg"].T
+    return x + (z * torch.sigmoid(z) * (h @ p["wu"].T)) @ p["wd"].T
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_decoder_layer(dtype):
+    """All of them together, forward and backward: the error beside that of the formulas whose
+    results of each operator are rounded to the type (about a dozen roundings in a row, each of
+    at most u of the values' size, and their sums' worst case is not the root of their number)."""
+    s = layer_state(dtype)
+    p = {k: v.clone().requires_grad_() for k, v in s["p"].items()}
+    x = s["x"].clone().requires_grad_()
+    y = layer(s, x, p)
+    y.backward(s["dy"])
+    p64 = {k: v.detach().cpu().double().requires_grad_() for k, v in s["p"].items()}
+    x64 = s["x"].cpu().double().requires_grad_()
+    y64 = layer64(s, x64, p64)
+    y64.backward(s["dy"].cpu().double())
+    for name, a, b in [("y", y, y64), ("x", x.grad, x64.grad)] + [(k, p[k].grad, p64[k].grad) for k in p]:
+        a, b = a.detach().cpu().double(), b.detach()
+        assert (a - b).norm() <= (24 * R.U[dtype] + 1e-5) * b.norm(), (name, float((a - b).norm() / b.norm()))
+
+
+def test_decoder_layer_in_a_graph():
+    """A training step captured once: replays with other inputs give the eager bits, with eager work
+    and synchronizations between them."""
+    s = layer_state()
+    names = list(s["p"])
+
+    def step(x, dy):
+        # leaves of the call's own: no eager graph of them lives while another is captured
+        leaf = x.detach().requires_grad_()
+        p = {k: v.detach().requires_grad_() for k, v in s["p"].items()}
+        y = layer(s, leaf, p)
+        return [y.detach(), *torch.autograd.grad(y, [leaf] + [p[k] for k in names], dy)]
+
+    static = s["x"].clone(), s["dy"].clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*static)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step(*static)
+    for seed in range(4):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        x, dy = (torch.randn(t.shape, generator=g, device="cuda").to(BF) for t in static)
+        static[0].copy_(x)
+        static[1].copy_(dy)
+        graph.replay()
+        eager = step(x, dy)
+        torch.cuda.synchronize()
+        for a, b in zip(captured, eager):
+            assert torch.equal(a, b)
+
+
+def test_calls_in_two_graphs():
+    """Scratch of two captured graphs, replayed in turn and on two streams, is their own."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda *t: torch.randn(t, generator=g, device="cuda", dtype=BF)  # noqa: E731
+    cases = []
+    for M, N, K in ((40, 256, 4096), (24, 384, 8192)):
+        x, w, dy, q = rand(M, K), rand(N, K), rand(M, N), rand(M, 4, 64)
+        lse = torch.empty(M, 4, device="cuda")
+
+        def calls(x=x, w=w, dy=dy, q=q, lse=lse):
+            o = ops.prompt_attention(q, q, q, lse=lse)
+            return [ops.linear(x, w), *ops.linear_backward(dy, x, w, bias=True)[:3],
+                    *ops.prompt_attention_backward(q, q, q, q, o, lse), *ops.layer_norm_backward(x, x, w[0].contiguous(), lse[:, 0].contiguous())[:2]]
+
+        want = [t.clone() for t in calls()]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = calls()
+        cases.append((graph, got, want, calls))  # calls keeps the inputs that the graph reads
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for turn in range(6):
+        for (graph, got, *_), stream in zip(cases, streams):
+            for t in got:
+                t.zero_()
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream if turn % 2 else torch.cuda.current_stream()):
+                graph.replay()
+        torch.cuda.synchronize()
+        for _, got, want, _ in cases:
+            for a, b in zip(got, want):
+                assert torch.equal(a, b), turn
+
+
+def test_layer_on_another_stream():
+    """Calls on a side stream, their inputs made on the current one and dropped at once."""
+    s = layer_state()
+    x, w = s["x"], s["p"]["wqkv"]
+    rstd = torch.empty(x.shape[0], device="cuda")
+    want_n, want_y = ops.layer_norm(x, rstd=rstd), ops.linear(x, w)
+    want_b = ops.linear_backward(want_y, x, w, bias=True)
+    want_g = ops.layer_norm_backward(x, x, None, rstd)
+    q = want_y.view(-1, 8, 64)
+    lse = torch.empty(x.shape[0], 8, device="cuda")
+    want_o = ops.prompt_attention(q, q, q, s["starts"], lse=lse)
+    want_d = ops.prompt_attention_backward(q, q, q, q, want_o, lse, s["starts"])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(4):
+        copies = [t.clone() for t in (x, w, rstd, want_y, q, want_o, lse, s["starts"])]
+        side.wait_stream(torch.cuda.current_stream())
+        cx, cw, cr, cy, cq, co, cl, cs = copies
+        n, y = ops.layer_norm(cx, stream=side), ops.linear(cx, cw, stream=side)
+        b = ops.linear_backward(cy, cx, cw, bias=True, stream=side)
+        gr = ops.layer_norm_backward(cx, cx, None, cr, stream=side)
+        o = ops.prompt_attention(cq, cq, cq, cs, stream=side)
+        d = ops.prompt_attention_backward(cq, cq, cq, cq, co, cl, cs, stream=side)
+        del copies, cx, cw, cr, cy, cq, co, cl, cs
+        trash = [torch.full((x.numel(),), 7.0, device="cuda", dtype=BF) for _ in range(8)]
+        torch.cuda.synchronize()
+        del trash
+        for a, c in zip((n, y, *b[:3], gr[0], o, *d), (want_n, want_y, *want_b[:3], want_g[0], want_o, *want_d)):
+            assert torch.equal(a, c)
+
+
+def test_layer_refusals():
+    """Every refused call raises and launches nothing."""
+    x, w = torch.zeros(4, 16, device="cuda", dtype=BF), torch.zeros(8, 16, device="cuda", dtype=BF)
+    y, v16, v8 = torch.zeros(4, 8, device="cuda", dtype=BF), torch.zeros(16, device="cuda", dtype=BF), torch.zeros(8, device="cuda", dtype=BF)
+    f4 = torch.zeros(4, device="cuda")
+    q = torch.zeros(4, 2, 16, device="cuda", dtype=BF)
+    st, lse = torch.tensor([0, 4], dtype=torch.int32, device="cuda"), torch.zeros(4, 2, device="cuda")
+    wide = torch.zeros(4, 32, device="cuda", dtype=BF)
+    bad = [
+        (ValueError, lambda: ops.layer_norm(x.cpu())), (TypeError, lambda: ops.layer_norm(x.int())), (TypeError, lambda: ops.layer_norm(None)),
+        (ValueError, lambda: ops.layer_norm(x, v8)), (TypeError, lambda: ops.layer_norm(x, v16.float())),
+        (ValueError, lambda: ops.layer_norm(x, v16, v8)), (ValueError, lambda: ops.layer_norm(wide[:, ::2])),
+        (ValueError, lambda: ops.layer_norm(x, out=y)), (ValueError, lambda: ops.layer_norm(x, out=x[:1].expand(4, 16))),
+        (ValueError, lambda: ops.layer_norm(x, mean=f4[:3])), (ValueError, lambda: ops.layer_norm(x, rstd=f4.double())),
+        (ValueError, lambda: ops.layer_norm(x[:, :0])), (api.GtsError, lambda: ops.layer_norm(x, eps=-1.0)),
+        (api.GtsError, lambda: ops.layer_norm(x, eps=math.nan)), (ValueError, lambda: ops.layer_norm(torch.zeros((), device="cuda"))),
+        (ValueError, lambda: ops.layer_norm_backward(y, x, v16, f4)), (ValueError, lambda: ops.layer_norm_backward(x, x, v16, None)),
+        (ValueError, lambda: ops.layer_norm_backward(x, x, v16, f4[:2])), (TypeError, lambda: ops.layer_norm_backward(x.float(), x, v16, f4)),
+        (ValueError, lambda: ops.linear(x, w, activation="tanh")), (ValueError, lambda: ops.linear(x, v16)),
+        (ValueError, lambda: ops.linear(y, w)), (TypeError, lambda: ops.linear(x, w.float())), (ValueError, lambda: ops.linear(x, w, v16)),
+        (ValueError, lambda: ops.linear(x, w, gate=x)), (ValueError, lambda: ops.linear(x, w, residual=y[:3])),
+        (TypeError, lambda: ops.linear(x, w, residual=y.float())), (ValueError, lambda: ops.linear(x, w, out=y[:1].expand(4, 8))),
+        (ValueError, lambda: ops.linear(wide[:, ::2], w)), (ValueError, lambda: ops.linear(x, w.cpu())),
+        (ValueError, lambda: ops.linear_backward(y, x, w, activation="silu")), (ValueError, lambda: ops.linear_backward(x, x, w)),
+        (ValueError, lambda: ops.linear_backward(y, x, w, gate=y)), (ValueError, lambda: ops.linear_backward(y, x, w, activation="silu", preact=x)),
+        (ValueError, lambda: ops.prompt_attention(q[0], q, q)), (ValueError, lambda: ops.prompt_attention(q, q[:3], q)),
+        (ValueError, lambda: ops.prompt_attention(q, q, q[..., :8])), (api.GtsError, lambda: ops.prompt_attention(q, torch.zeros(4, 3, 16, device="cuda", dtype=BF), torch.zeros(4, 3, 16, device="cuda", dtype=BF))),
+        (TypeError, lambda: ops.prompt_attention(q, q.half(), q)), (TypeError, lambda: ops.prompt_attention(q, q, q, st.long())),
+        (ValueError, lambda: ops.prompt_attention(q, q, q, st[:1])), (ValueError, lambda: ops.prompt_attention(q, q, q, st.cpu())),
+        (ValueError, lambda: ops.prompt_attention(q, q, q, lse=lse.half())), (ValueError, lambda: ops.prompt_attention(q, q, q, out=q[:, :1].expand(4, 2, 16))),
+        (api.GtsError, lambda: ops.prompt_attention(q, q, q, scale=math.inf)),
+        (ValueError, lambda: ops.prompt_attention_backward(q[:2], q, q, q, q, lse)), (ValueError, lambda: ops.prompt_attention_backward(q, q, q, q, q, f4)),
+    ]
+    for i, (kind, f) in enumerate(bad):
+        with pytest.raises(kind):
+            f()
+            note(f"refusal {i} missing")
+    big = torch.zeros(3, 1, 300, device="cuda", dtype=BF)
+    with pytest.raises(api.GtsError):
+        ops.prompt_attention(big, big, big)
+    torch.cuda.synchronize()
