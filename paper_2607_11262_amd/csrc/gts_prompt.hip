@@ -134,17 +134,18 @@ __device__ __forceinline__ void clear(f32x16 (&o)[N]) {
 // times one of them would reach lanes that must not see it.  They are cleared in the copy
 // that is multiplied, and added here, from memory, where `sees(j)`: themselves, or NaN, as
 // which they reach a gradient's sum whatever their weight.
-template <typename T, int DP, typename F>
-__device__ __forceinline__ void add_odd(f32x16* o, const T* p, int64_t stride, uint32_t j0, uint32_t n, uint32_t dim,
-                                        uint32_t half, bool as_nan, F sees) {
+// N blocks of 32 columns from `column` on.
+template <typename T, int N, typename F>
+__device__ __forceinline__ void add_odd(f32x16* o, const T* p, int64_t stride, uint32_t j0, uint32_t n, uint32_t column,
+                                        uint32_t dim, uint32_t half, bool as_nan, F sees) {
 #pragma unroll 1
   for (uint32_t j = j0; j < n && j < j0 + kStep; ++j) {
     const T* row = p + (int64_t)j * stride;
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
+    for (int d = 0; d < N; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const uint32_t c = d * 32 + frag_row(i, half);
+        const uint32_t c = column + d * 32 + frag_row(i, half);
         if (c >= dim) continue;
         const float x = (float)row[c];
         if (not_finite(x) && sees(j)) o[d][i] += as_nan ? __builtin_nanf("") : x;
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(256) void prompt_kernel(PromptParams p) {
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
     add_weighted<T, DP>(o, s_v, s, lane);
-    if (odd) add_odd<T, DP>(o, v, a.v_stride[0], j0, sp.n, a.dim, half, false, [&](uint32_t j) { return j < sees; });
+    if (odd) add_odd<T, DP / 32>(o, v, a.v_stride[0], j0, sp.n, 0, a.dim, half, false, [&](uint32_t j) { return j < sees; });
   }
   if (!valid) return;
   write_row<T, DP>(out, o, 1.f / l, a.dim, half);
@@ -244,7 +245,6 @@ template <typename T, int DP>
 struct Tiles {
   static constexpr int C = DP / 8;      // 16-byte chunks of a row
   static constexpr int RPI = 64 / C;    // rows of one load of a wave
-  static constexpr int NL = 16 / RPI;   // loads of a wave for its 16 rows
   static constexpr int N = kTile * DP;  // values of a tile
   // Chunk c of row r stands at c ^ swizzle(r): reads of 16 rows at one chunk, and reads of 4
   // rows x 64 bytes that are turned on the way, each touch all 64 banks once.
@@ -253,43 +253,46 @@ struct Tiles {
   }
 };
 
-// Loads tiles of two matrices to LDS, 16 rows of each a wave.
-template <typename T, int DP>
+// Loads tiles of two matrices to LDS: each of W waves 64 / W rows of both.
+template <typename T, int DP, int W = 4>
 struct Loader {
   using L = Tiles<T, DP>;
+  static constexpr uint32_t R = kTile / W;  // rows of a wave
+  static constexpr int NL = R / L::RPI;     // its loads
+  static_assert(NL * L::RPI == R, "whole loads");
   const T *a, *b;  // of the first row
   int64_t a_stride, b_stride;
   uint32_t n, dim;                      // rows that are there, values of a row
-  uint32_t a_off[L::NL], b_off[L::NL];  // bytes from the wave's first row to this lane's chunk
+  uint32_t a_off[NL], b_off[NL];  // bytes from the wave's first row to this lane's chunk
 
-  __device__ __forceinline__ void start() {
+  __device__ __forceinline__ void start(uint32_t wave) {
     const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
 #pragma unroll
-    for (int i = 0; i < L::NL; ++i) {
+    for (int i = 0; i < NL; ++i) {
       const uint32_t r = i * L::RPI + r0;
-      a_off[i] = 2 * (r * (uint32_t)a_stride + (c ^ L::swizzle(r)) * 8);
-      b_off[i] = 2 * (r * (uint32_t)b_stride + (c ^ L::swizzle(r)) * 8);
+      a_off[i] = 2 * (r * (uint32_t)a_stride + (c ^ L::swizzle(wave * R + r)) * 8);
+      b_off[i] = 2 * (r * (uint32_t)b_stride + (c ^ L::swizzle(wave * R + r)) * 8);
     }
   }
   __device__ __forceinline__ void load(uint32_t j0, uint32_t wave, T* sa, T* sb) const {
-    const uint32_t j = j0 + wave * 16;
+    const uint32_t j = j0 + wave * R;
     const char* pa = (const char*)(a + (int64_t)j * a_stride);
     const char* pb = (const char*)(b + (int64_t)j * b_stride);
-    if (j + 16 <= n && dim == DP) {
+    if (j + R <= n && dim == DP) {
 #pragma unroll
-      for (int i = 0; i < L::NL; ++i) {
-        load_to_lds(pa + a_off[i], sa + (wave * 16 + i * L::RPI) * DP);
-        load_to_lds(pb + b_off[i], sb + (wave * 16 + i * L::RPI) * DP);
+      for (int i = 0; i < NL; ++i) {
+        load_to_lds(pa + a_off[i], sa + (wave * R + i * L::RPI) * DP);
+        load_to_lds(pb + b_off[i], sb + (wave * R + i * L::RPI) * DP);
       }
       return;
     }
     const uint32_t lane = fresh_lane(), c = lane % L::C, r0 = lane / L::C;
 #pragma unroll
-    for (int i = 0; i < L::NL; ++i) {
+    for (int i = 0; i < NL; ++i) {
       const uint32_t r = i * L::RPI + r0;
-      const bool there = j + r < n && (c ^ L::swizzle(r)) * 8 < dim;
-      load_to_lds(there ? pa + a_off[i] : (const char*)g_zeros, sa + (wave * 16 + i * L::RPI) * DP);
-      load_to_lds(there ? pb + b_off[i] : (const char*)g_zeros, sb + (wave * 16 + i * L::RPI) * DP);
+      const bool there = j + r < n && (c ^ L::swizzle(wave * R + r)) * 8 < dim;
+      load_to_lds(there ? pa + a_off[i] : (const char*)g_zeros, sa + (wave * R + i * L::RPI) * DP);
+      load_to_lds(there ? pb + b_off[i] : (const char*)g_zeros, sb + (wave * R + i * L::RPI) * DP);
     }
   }
 };
@@ -324,15 +327,16 @@ template <typename T, int N>
 __device__ __forceinline__ void clear_tile(T* s) {
   for (uint32_t x = threadIdx.x; x < N / 8; x += 256) *(u32x4*)(s + x * 8) = finite_only<T>(*(const u32x4*)(s + x * 8));
 }
-// The wave's 32 rows of a result (dims x rows, a lane its row) to memory, through LDS that the
-// wave has for itself, so that whole rows are written.  lane_ok: the lane's row is there.
-template <typename T, int DP>
-__device__ __forceinline__ void write_rows(T* s, const f32x16* o, float f, T* out, int64_t stride, uint32_t rows, uint32_t dim,
-                                           uint32_t lane) {
-  constexpr uint32_t P = DP + 8;
+// The wave's 32 rows of a result (N blocks of 32 columns x rows, a lane its row) to memory, through
+// LDS that the wave has for itself, so that whole rows are written.
+template <typename T, int N>
+__device__ __forceinline__ void write_rows(T* s, const f32x16* o, float f, T* out, int64_t stride, uint32_t rows,
+                                           uint32_t column, uint32_t dim, uint32_t lane) {
+  constexpr uint32_t P = N * 32 + 8;
   const uint32_t half = lane / 32;
+  asm volatile("" ::: "memory");  // a wave's accesses to LDS keep their order
 #pragma unroll
-  for (int d = 0; d < DP / 32; ++d)
+  for (int d = 0; d < N; ++d)
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
       Pack<T, 4> x;
@@ -340,11 +344,11 @@ __device__ __forceinline__ void write_rows(T* s, const f32x16* o, float f, T* ou
       for (int j = 0; j < 4; ++j) x.v[j] = (T)(o[d][i + j] * f);
       *(Pack<T, 4>*)(s + lane % 32 * P + d * 32 + frag_row(i, half)) = x;
     }
-  asm volatile("" ::: "memory");  // a wave's accesses to LDS keep their order
+  asm volatile("" ::: "memory");
 #pragma unroll
-  for (uint32_t i = 0; i < DP / 16; ++i) {
-    const uint32_t id = i * 64 + lane, r = id / (DP / 8), c = id % (DP / 8) * 8;
-    if (r < rows && c < dim) *(u32x4*)(out + (int64_t)r * stride + c) = *(const u32x4*)(s + r * P + c);
+  for (uint32_t i = 0; i < N * 2; ++i) {
+    const uint32_t id = i * 64 + lane, r = id / (N * 4), c = id % (N * 4) * 8;
+    if (r < rows && column + c < dim) *(u32x4*)(out + (int64_t)r * stride + column + c) = *(const u32x4*)(s + r * P + c);
   }
 }
 
@@ -356,11 +360,12 @@ __device__ __forceinline__ uint32_t head_at(uint32_t at, uint32_t kv_heads, uint
   return *kv * group + at / s % group;
 }
 
-// What a wave of the forward kernel holds: 32 rows.
-template <typename T, int DP>
+// What a wave of the forward kernel holds: 32 rows, and N blocks of 32 columns of their results.
+template <typename T, int DP, int N>
 struct Rows {
   Vec8<T> q[DP / 16];
-  f32x16 o[DP / 32];
+  f32x16 o[N];
+  int d0;  // the first of the blocks
   float m, l;  // reference maximum of q.k (unscaled), sum of this half's weights
 
   // 32 NS keys from LDS row `key` on; the lane's row sees those before `sees` (from there).
@@ -412,7 +417,7 @@ struct Rows {
       const float alpha = m == -INFINITY ? 0.f : exp2_((m - m1) * c);
       l *= alpha;
 #pragma unroll
-      for (int b = 0; b < DP / 32; ++b) o[b] *= alpha;
+      for (int b = 0; b < N; ++b) o[b] *= alpha;
       m = m1;
     }
     const float base = m == -INFINITY ? 0.f : -m * c;
@@ -427,24 +432,24 @@ struct Rows {
     };
     // The weights of 16 keys are computed, and the values of 16 keys read, between the
     // products of the 16 keys before.
-    Vec8<T> vf[2][DP / 32];
+    Vec8<T> vf[2][N];
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d) vf[0][d] = column_frag<T, DP>(sv, key, d, lane);
+    for (int d = 0; d < N; ++d) vf[0][d] = column_frag<T, DP>(sv, key, d0 + d, lane);
 #pragma unroll
     for (int i = 0; i < 8; ++i) weigh(0, i);
 #pragma unroll
     for (int kb = 0; kb < 2 * NS; ++kb) {
       if (kb + 1 < 2 * NS) {
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d) vf[kb + 1 & 1][d] = column_frag<T, DP>(sv, key + kb * 16 + 16, d, lane);
+        for (int d = 0; d < N; ++d) vf[kb + 1 & 1][d] = column_frag<T, DP>(sv, key + kb * 16 + 16, d0 + d, lane);
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int d = 0; d < DP / 32; ++d) {
+      for (int d = 0; d < N; ++d) {
         o[d] = mfma(vf[kb & 1][d], pw[kb], o[d]);
         if (kb + 1 < 2 * NS) {
 #pragma unroll
-          for (int i = d * 8 / (DP / 32); i < (d + 1) * 8 / (DP / 32); ++i) weigh(kb + 1, i);
+          for (int i = d * 8 / N; i < (d + 1) * 8 / N; ++i) weigh(kb + 1, i);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -455,9 +460,12 @@ struct Rows {
 
 // 128 rows, 32 a wave.  First without a look at values that are not finite; a workgroup that
 // then finds one among its results computes them again with it (`odd`): 0 times one of them
-// would reach rows that must not see it.
+// would reach rows that must not see it.  That takes 32 columns at a time (block d0), so that
+// it does not need more registers than the usual way.
 template <typename T, int DP, bool ODD>
-__device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& sp, uint32_t hq, uint32_t h, T* s_kv) {
+__device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& sp, uint32_t hq, uint32_t h, T* s_kv,
+                                            int d0 = 0) {
+  constexpr int N = ODD ? 1 : DP / 32;
   using L = Tiles<T, DP>;
   const gts_prompt_args& a = p.a;
   const uint32_t lane = fresh_lane(), wave = uni(threadIdx.x >> 6), half = lane / 32;
@@ -471,12 +479,13 @@ __device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& s
   ld.b_stride = a.v_stride[0];
   ld.n = sp.n;
   ld.dim = a.dim;
-  ld.start();
+  ld.start(wave);
   const uint32_t keys = causal && r0 + kRows < sp.n ? r0 + kRows : sp.n, tiles = (keys + kTile - 1) / kTile;
   __syncthreads();
   ld.load(0, wave, s_kv, s_kv + L::N);
-  Rows<T, DP> r;
+  Rows<T, DP, N> r;
   clear(r.o);
+  r.d0 = d0;
   r.m = -INFINITY;
   r.l = 0.f;
   {
@@ -525,7 +534,8 @@ __device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& s
     if constexpr (ODD) {
       if (odd)
         for (uint32_t x = 0; x < kTile; x += 32)
-          add_odd<T, DP>(r.o, ld.b, ld.b_stride, j0 + x, sp.n, a.dim, half, false, [&](uint32_t j) { return j < seen; });
+          add_odd<T, N>(r.o, ld.b, ld.b_stride, j0 + x, sp.n, d0 * 32, a.dim, half, false,
+                        [&](uint32_t j) { return j < seen; });
     }
   }
   const float l = add_halves(r.l), inv = 1.f / l;
@@ -534,7 +544,7 @@ __device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& s
     if (causal && valid) {
       float x = 0.f;  // NaN or infinite if one of them is
 #pragma unroll
-      for (int d = 0; d < DP / 32; ++d)
+      for (int d = 0; d < N; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) x = fmaxf(x, not_finite(r.o[d][i]) ? 1.f : 0.f);
       found = x > 0.f;
@@ -545,8 +555,8 @@ __device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& s
     __syncthreads();
   }
   T* out = (T*)a.out + (int64_t)(sp.first + w0) * a.out_stride[0] + (int64_t)hq * a.out_stride[1];
-  write_rows<T, DP>(s_kv + wave * 32 * (DP + 8), r.o, inv, out, a.out_stride[0], sp.n > w0 ? sp.n - w0 : 0, a.dim, lane);
-  if (a.lse && valid && half == 0)
+  write_rows<T, N>(s_kv + wave * 32 * (DP + 8), r.o, inv, out, a.out_stride[0], sp.n > w0 ? sp.n - w0 : 0, d0 * 32, a.dim, lane);
+  if (a.lse && valid && half == 0 && d0 == 0)
     a.lse[(uint64_t)(sp.first + row) * a.q_heads + hq] = l == 0.f ? -INFINITY : (r.m * c + log2f(l)) * kLn2;
   return false;
 }
@@ -555,7 +565,7 @@ __device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& s
 template <typename T>
 __device__ __forceinline__ void zero_rows(T* out, const int64_t* stride, const Span& sp, uint32_t head, uint32_t dim) {
   const uint32_t rows = sp.n - sp.tile * kRows < kRows ? sp.n - sp.tile * kRows : kRows, first = sp.first + sp.tile * kRows;
-  for (uint32_t i = threadIdx.x; i < rows * (dim / 8); i += 256)
+  for (uint32_t i = threadIdx.x; i < rows * (dim / 8); i += blockDim.x)
     *(u32x4*)(out + (int64_t)(first + i / (dim / 8)) * stride[0] + (int64_t)head * stride[1] + i % (dim / 8) * 8) =
         u32x4{0, 0, 0, 0};
 }
@@ -578,7 +588,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
         a.lse[(uint64_t)(sp.first + i) * a.q_heads + hq] = -INFINITY;
     return;
   }
-  if (prompt_rows<T, DP, false>(p, sp, hq, h, s_kv)) prompt_rows<T, DP, true>(p, sp, hq, h, s_kv);
+  if (prompt_rows<T, DP, false>(p, sp, hq, h, s_kv))
+    for (int d = 0; d < DP / 32; ++d) prompt_rows<T, DP, true>(p, sp, hq, h, s_kv, d);
 }
 
 struct PromptGradParams {
@@ -673,7 +684,7 @@ __global__ __launch_bounds__(256) void dq_kernel(PromptGradParams p) {
       }
     }
     add_weighted<T, DP>(o, s_k, s, lane);
-    if (odd) add_odd<T, DP>(o, k, a.k_stride[0], j0, sp.n, a.dim, half, true, [&](uint32_t j) { return j < sees; });
+    if (odd) add_odd<T, DP / 32>(o, k, a.k_stride[0], j0, sp.n, 0, a.dim, half, true, [&](uint32_t j) { return j < sees; });
   }
   if (valid) write_row<T, DP>(dq, o, a.scale, a.dim, half);
 }
@@ -748,8 +759,8 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
         if constexpr (kK) add_weighted<T, DP>(ok, s_q, ds, lane);
         if (odd) {
           const auto sees = [&](uint32_t row) { return key <= row; };
-          if constexpr (kV) add_odd<T, DP>(ov, dout, a.dout_stride[0], i0, sp.n, a.dim, half, false, sees);
-          if constexpr (kK) add_odd<T, DP>(ok, q, a.q_stride[0], i0, sp.n, a.dim, half, true, sees);
+          if constexpr (kV) add_odd<T, DP / 32>(ov, dout, a.dout_stride[0], i0, sp.n, 0, a.dim, half, false, sees);
+          if constexpr (kK) add_odd<T, DP / 32>(ok, q, a.q_stride[0], i0, sp.n, 0, a.dim, half, true, sees);
         }
       }
     }
@@ -773,8 +784,68 @@ __device__ __forceinline__ bool any_odd(const f32x16 (&o)[N]) {
   return found;
 }
 
+// 32 rows of one or two tiles times held rows (B): the fragments of two steps are read while the
+// two before are multiplied.
+template <typename T, int DP, bool BOTH>
+__device__ __forceinline__ void two_products(const T* sa, const T* sb, uint32_t row, const Vec8<T>* a, const Vec8<T>* b, f32x16& ra,
+                                             f32x16& rb) {
+  const uint32_t lane = fresh_lane();
+  const RowFrags<T, DP> fa(sa, row, lane), fb(sb, row, lane);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) ra[i] = rb[i] = 0.f;
+  Vec8<T> f[2][2][2];
+  const auto read = [&](int kk) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      f[kk / 2 & 1][x][0] = fa(kk + x);
+      if constexpr (BOTH) f[kk / 2 & 1][x][1] = fb(kk + x);
+    }
+  };
+  read(0);
+#pragma unroll
+  for (int kk = 0; kk < DP / 16; kk += 2) {
+    if (kk + 2 < DP / 16) read(kk + 2);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      ra = mfma(f[kk / 2 & 1][x][0], a[kk + x], ra);
+      if constexpr (BOTH) rb = mfma(f[kk / 2 & 1][x][1], b[kk + x], rb);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+// N blocks of columns, from block d0 on, of 32 rows of a tile times the lane's weights, rounded to T.
+template <typename T, int DP, int N>
+__device__ __forceinline__ void add_columns(f32x16* o, const T* s, uint32_t row, int d0, const f32x16& w, uint32_t lane) {
+  Vec8<T> u[2], f[2][N];
+#pragma unroll
+  for (int d = 0; d < N; ++d) f[0][d] = column_frag<T, DP>(s, row, d0 + d, lane);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) u[i / 8][i % 8] = (T)w[i];
+#pragma unroll
+  for (int d = 0; d < N; ++d) f[1][d] = column_frag<T, DP>(s, row + 16, d0 + d, lane);
+#pragma unroll
+  for (int y = 0; y < 2; ++y)
+#pragma unroll
+    for (int d = 0; d < N; ++d) o[d] = mfma(f[y][d], u[y], o[d]);
+}
+// At an edge, once every wave has its scores: whether the tile has a value that is not finite; those
+// are zeros afterwards.
+template <typename T, int N>
+__device__ __forceinline__ bool clear_if_odd(T* s, bool edge, uint32_t threads) {
+  if (!edge) return false;
+  bool found = false;
+  for (uint32_t x = threadIdx.x; x < N / 8; x += threads) found |= any_not_finite<T>(*(const u32x4*)(s + x * 8));
+  if (!__syncthreads_or(found)) return false;
+  for (uint32_t x = threadIdx.x; x < N / 8; x += threads) *(u32x4*)(s + x * 8) = finite_only<T>(*(const u32x4*)(s + x * 8));
+  __syncthreads();
+  return true;
+}
+
 template <typename T, int DP, bool ODD>
-__device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& sp, uint32_t hq, uint32_t h, T* s_kv) {
+__device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& sp, uint32_t hq, uint32_t h, T* s_kv,
+                                        int d0 = 0) {
+  constexpr int N = ODD ? 1 : DP / 32;
   using L = Tiles<T, DP>;
   const gts_prompt_grad_args& a = p.a;
   const uint32_t lane = fresh_lane(), wave = uni(threadIdx.x >> 6), half = lane / 32;
@@ -788,7 +859,7 @@ __device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& s
   ld.b_stride = a.v_stride[0];
   ld.n = sp.n;
   ld.dim = a.dim;
-  ld.start();
+  ld.start(wave);
   const uint32_t keys = causal && r0 + kRows < sp.n ? r0 + kRows : sp.n, tiles = (keys + kTile - 1) / kTile;
   __syncthreads();
   ld.load(0, wave, s_kv, s_kv + L::N);
@@ -802,7 +873,7 @@ __device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& s
     dout[i] = *(const Vec8<T>*)(at < a.dim ? op + at : (const T*)g_zeros);
   }
   const float lse = p.lse[p.stat(hq, sp.first + there)], delta = p.delta[p.stat(hq, sp.first + there)];
-  f32x16 o[DP / 32];
+  f32x16 o[N];
   clear(o);
   for (uint32_t t = 0; t < tiles; ++t) {
     const uint32_t j0 = t * kTile;
@@ -814,82 +885,43 @@ __device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& s
       ld.load(j0 + kTile, wave, next, next + L::N);
     }
     const uint32_t seen = causal && row + 1 < sp.n ? row + 1 : sp.n;
-    const bool edge = causal && j0 + kTile > r0 + 1;
     if (!ODD && causal && j0 > w0 + 31) continue;  // the wave sees none of it
     const bool mask = j0 + kTile > (causal ? w0 + 1 : sp.n) || j0 + kTile > sp.n;
-    const auto weigh = [&](uint32_t x, f32x16& s, const f32x16& dp) {
+    const auto weigh = [&](uint32_t x, f32x16& s, const f32x16& dp, bool masked) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const bool hidden = mask && j0 + x + frag_row(i, half) >= seen;
+        const bool hidden = masked && j0 + x + frag_row(i, half) >= seen;
         if (!ODD && hidden) s[i] = -INFINITY;
         s[i] = exp2_(__builtin_fmaf(s[i], c, -lse)) * (dp[i] - delta);
         if (ODD && hidden) s[i] = 0.f;
       }
     };
-    const auto scores = [&](uint32_t x, f32x16& s, f32x16& dp) {
-      const RowFrags<T, DP> k(sk, x, fresh_lane()), v(sv, x, fresh_lane());
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
-      Vec8<T> f[2][2];
-      f[0][0] = k(0);
-      f[0][1] = v(0);
-#pragma unroll
-      for (int kk = 0; kk < DP / 16; ++kk) {
-        if (kk + 1 < DP / 16) {
-          f[kk + 1 & 1][0] = k(kk + 1);
-          f[kk + 1 & 1][1] = v(kk + 1);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        s = mfma(f[kk & 1][0], q[kk], s);
-        dp = mfma(f[kk & 1][1], dout[kk], dp);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    };
-    const auto add = [&](uint32_t x, const f32x16& ds) {
-      Vec8<T> u[2];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) u[i / 8][i % 8] = (T)ds[i];
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int d = 0; d < DP / 32; ++d) o[d] = mfma(column_frag<T, DP>(sk, x + k * 16, d, lane), u[k], o[d]);
-    };
     if constexpr (!ODD) {
 #pragma unroll 1
       for (uint32_t x = 0; x < kTile; x += 32) {
         f32x16 s, dp;
-        scores(x, s, dp);
-        if (mask) {
-          weigh(x, s, dp);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = exp2_(__builtin_fmaf(s[i], c, -lse)) * (dp[i] - delta);
-        }
-        add(x, s);
+        two_products<T, DP, true>(sk, sv, x, q, dout, s, dp);
+        if (mask)
+          weigh(x, s, dp, true);
+        else
+          weigh(x, s, dp, false);
+        add_columns<T, DP, N>(o, sk, x, 0, s, lane);
       }
     } else {
       f32x16 s[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         f32x16 dp;
-        scores(x * 32, s[x], dp);
-        weigh(x * 32, s[x], dp);
+        two_products<T, DP, true>(sk, sv, x * 32, q, dout, s[x], dp);
+        weigh(x * 32, s[x], dp, true);
       }
-      bool odd = false;
-      if (edge) {
-        bool found = false;
-        for (uint32_t x = threadIdx.x; x < L::N / 8; x += 256) found |= any_not_finite<T>(*(const u32x4*)(sk + x * 8));
-        odd = __syncthreads_or(found);
-        if (odd) {
-          clear_tile<T, L::N>(sk);
-          __syncthreads();
-        }
-      }
+      const bool odd = clear_if_odd<T, L::N>(sk, causal && j0 + kTile > r0 + 1, 256);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        add(x * 32, s[x]);
+        add_columns<T, DP, N>(o, sk, x * 32, d0, s[x], lane);
         if (odd)
-          add_odd<T, DP>(o, ld.a, ld.a_stride, j0 + x * 32, sp.n, a.dim, half, true, [&](uint32_t j) { return j < seen; });
+          add_odd<T, N>(o, ld.a, ld.a_stride, j0 + x * 32, sp.n, d0 * 32, a.dim, half, true,
+                        [&](uint32_t j) { return j < seen; });
       }
     }
   }
@@ -899,7 +931,7 @@ __device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& s
     __syncthreads();
   }
   T* out = (T*)a.dq + (int64_t)(sp.first + w0) * a.dq_stride[0] + (int64_t)hq * a.dq_stride[1];
-  write_rows<T, DP>(s_kv + wave * 32 * (DP + 8), o, a.scale, out, a.dq_stride[0], sp.n > w0 ? sp.n - w0 : 0, a.dim, lane);
+  write_rows<T, N>(s_kv + wave * 32 * (DP + 8), o, a.scale, out, a.dq_stride[0], sp.n > w0 ? sp.n - w0 : 0, d0 * 32, a.dim, lane);
   return false;
 }
 
@@ -915,7 +947,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dq_tile_kernel(PromptG
     zero_rows((T*)a.dq, a.dq_stride, sp, hq, a.dim);
     return;
   }
-  if (dq_rows<T, DP, false>(p, sp, hq, h, s_kv)) dq_rows<T, DP, true>(p, sp, hq, h, s_kv);
+  if (dq_rows<T, DP, false>(p, sp, hq, h, s_kv))
+    for (int d = 0; d < DP / 32; ++d) dq_rows<T, DP, true>(p, sp, hq, h, s_kv, d);
 }
 
 // 4 bytes a lane from memory to LDS, as load_to_lds.
@@ -928,28 +961,30 @@ __device__ __forceinline__ void load_to_lds4(const void* from, void* to) {
                : "memory");
 }
 
-// 128 keys, 32 a wave; all rows that see them, of all query heads of the key-value head, 64 at
-// a time in two blocks: the first block's weights are computed between the products of the
-// second's scores, and the second's between the products of the first's sums.  So a wave by
-// itself keeps the matrix unit busy, and may take all registers of its SIMD: keys, values and both
-// sums stay in them.
-template <typename T, int DP, int WHAT, bool ODD>
+// 128 keys, four groups of 32; all rows that see them, of all query heads of the key-value head,
+// 64 at a time: eight waves, one for each group of keys and half of the rows, whose sums are joined
+// at the end.  dv and dk take a kernel each (`DV`), which computes the scores once more but leaves
+// registers for two waves a SIMD, one of which computes weights while the other multiplies.
+// Heads of 256 take two passes of 128 columns each, for which there are registers.
+template <int DP>
+constexpr int kBlocks = DP / 32 < 4 ? DP / 32 : 4;
+
+template <typename T, int DP, bool DV, bool ODD>
 __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& sp, uint32_t h, T* s_qo,
-                                         float (*s_stat)[2][kTile]) {
+                                         float (*s_stat)[2][kTile], int d0 = 0) {
   using L = Tiles<T, DP>;
-  constexpr bool kV = WHAT & 1, kK = WHAT & 2;
-  constexpr int KK = DP / 16, MB = DP / 32;
+  constexpr int KK = DP / 16, N = ODD ? 1 : kBlocks<DP>;
   const gts_prompt_grad_args& a = p.a;
-  const uint32_t lane = fresh_lane(), wave = uni(threadIdx.x >> 6), half = lane / 32;
-  const uint32_t k0 = sp.tile * kRows, w0 = k0 + wave * 32, key = w0 + lane % 32, there = key < sp.n ? key : 0;
+  const uint32_t lane = fresh_lane(), wave = uni(threadIdx.x >> 6), half = lane / 32, x0 = wave / 4 * 32;
+  const uint32_t k0 = sp.tile * kRows, w0 = k0 + wave % 4 * 32, key = w0 + lane % 32, there = key < sp.n ? key : 0;
   const bool valid = key < sp.n, causal = a.flags & GTS_PROMPT_CAUSAL;
   const float c = a.scale * kLog2e;
-  Loader<T, DP> ld;
+  Loader<T, DP, 8> ld;
   ld.a_stride = a.q_stride[0];
   ld.b_stride = a.dout_stride[0];
   ld.n = sp.n;
   ld.dim = a.dim;
-  ld.start();
+  ld.start(wave);
   const uint32_t first = causal ? k0 / kTile : 0, tiles = (sp.n + kTile - 1) / kTile;
   const auto load = [&](uint32_t g, uint32_t t, uint32_t buffer) {
     const uint32_t hq = h * p.group + g;
@@ -965,136 +1000,108 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
   };
   __syncthreads();
   load(0, first, 0);
-  Vec8<T> k[KK], v[kK ? KK : 1];
+  Vec8<T> k[KK], v[DV ? 1 : KK];
   const T* kp = (const T*)a.k + (int64_t)(sp.first + there) * a.k_stride[0] + (int64_t)h * a.k_stride[1];
   const T* vp = (const T*)a.v + (int64_t)(sp.first + there) * a.v_stride[0] + (int64_t)h * a.v_stride[1];
 #pragma unroll
   for (int i = 0; i < KK; ++i) {
     const uint32_t at = i * 16 + 8 * half;
     k[i] = *(const Vec8<T>*)(at < a.dim ? kp + at : (const T*)g_zeros);
-    if constexpr (kK) v[i] = *(const Vec8<T>*)(at < a.dim ? vp + at : (const T*)g_zeros);
+    if constexpr (!DV) v[i] = *(const Vec8<T>*)(at < a.dim ? vp + at : (const T*)g_zeros);
   }
-  f32x16 ok[kK ? MB : 1], ov[kV ? MB : 1];
-  clear(ok);
-  clear(ov);
+  f32x16 o[N];
+  clear(o);
   uint32_t buffer = 0;
   for (uint32_t g = 0; g < p.group; ++g)
     for (uint32_t t = first; t < tiles; ++t, buffer ^= 1) {
-      const uint32_t i0 = t * kTile;
-      T *sq = s_qo + buffer * 2 * L::N, *so = sq + L::N;
+      const uint32_t i0 = t * kTile + x0;  // the wave's first row
+      T *sq = s_qo + buffer * 2 * L::N, *so = sq + L::N, *added = DV ? so : sq;
       wait_loads();
       __syncthreads();
       if (t + 1 < tiles)
         load(g, t + 1, buffer ^ 1);
       else if (g + 1 < p.group)
         load(g + 1, first, buffer ^ 1);
-      if (!ODD && causal && i0 + kTile <= w0) continue;  // no row of it sees a key of the wave
-      const bool mask = (causal && i0 < w0 + 31) || i0 + kTile > sp.n;
-      f32x16 s[2], ds[2];
-      Vec8<T> pu[2][2], du[2][2];
-      // two products of block b: the fragments of a step are read while the one before is multiplied
-      Vec8<T> f[2][2];
-      const auto read = [&](int b, int kk) {
-        const uint32_t fl = fresh_lane();
-        f[kk & 1][0] = RowFrags<T, DP>(sq, b * 32, fl)(kk);
-        if constexpr (kK) f[kk & 1][1] = RowFrags<T, DP>(so, b * 32, fl)(kk);
-      };
-      const auto product = [&](int b, int kk) {
-        s[b] = mfma(f[kk & 1][0], k[kk], s[b]);
-        if constexpr (kK) ds[b] = mfma(f[kk & 1][1], v[kk], ds[b]);
-      };
-      const auto weigh = [&](int b, int i) {
-        const uint32_t r = b * 32 + frag_row(i, half);
-        float x = s[b][i];
-        const bool hidden = (causal && i0 + r < key) || i0 + r >= sp.n;
-        if (!ODD && mask) x = hidden ? -INFINITY : x;
-        x = exp2_(__builtin_fmaf(x, c, -s_stat[buffer][0][r]));
-        if (ODD) x = hidden ? 0.f : x;
-        pu[b][i / 8][i % 8] = (T)x;
-        if constexpr (kK) {
-          x *= ds[b][i] - s_stat[buffer][1][r];
-          if (ODD) x = hidden ? 0.f : x;
-          du[b][i / 8][i % 8] = (T)x;
-        }
-      };
-      const auto sum = [&](int b, int d, int x) {
-        if constexpr (kV) ov[d] = mfma(column_frag<T, DP>(so, b * 32 + x * 16, d, lane), pu[b][x], ov[d]);
-        if constexpr (kK) ok[d] = mfma(column_frag<T, DP>(sq, b * 32 + x * 16, d, lane), du[b][x], ok[d]);
-      };
+      if (!ODD && ((causal && i0 + 32 <= w0) || i0 >= sp.n)) continue;  // no row of the wave's sees a key of its
+      const bool mask = (causal && i0 < w0 + 31) || i0 + 32 > sp.n;
+      f32x16 s, dp;
+      two_products<T, DP, !DV>(sq, so, x0, k, v, s, dp);
+      const auto weigh = [&](bool masked) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+        for (int e = 0; e < 16; e += 4) {
+          const uint32_t r = frag_row(e, half);  // four rows side by side
+          const f32x4 lse = *(const f32x4*)&s_stat[buffer][0][x0 + r];
+          f32x4 delta = {};
+          if constexpr (!DV) delta = *(const f32x4*)&s_stat[buffer][1][x0 + r];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[b][i] = ds[b][i] = 0.f;
-      read(0, 0);
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        if (kk + 1 < KK) read(0, kk + 1);
-        product(0, kk);
-      }
-      read(1, 0);
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        if (kk + 1 < KK) read(1, kk + 1);
-        product(1, kk);
-#pragma unroll
-        for (int i = kk * 16 / KK; i < (kk + 1) * 16 / KK; ++i) weigh(0, i);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      bool odd = false;
-      if constexpr (ODD) {
-        if (causal && i0 + 1 < k0 + kRows) {
-          bool found = false;
-          for (uint32_t x = threadIdx.x; x < L::N / 4; x += 256) found |= any_not_finite<T>(*(const u32x4*)(sq + x * 8));
-          odd = __syncthreads_or(found);  // and every wave has its scores
-          if (odd) {
-            clear_tile<T, 2 * L::N>(sq);
-            __syncthreads();
+          for (int i = 0; i < 4; ++i) {
+            const bool hidden = masked && ((causal && i0 + r + i < key) || i0 + r + i >= sp.n);
+            float y = !ODD && hidden ? -INFINITY : s[e + i];
+            y = exp2_(__builtin_fmaf(y, c, -lse[i]));
+            if constexpr (!DV) y *= dp[e + i] - delta[i];
+            s[e + i] = ODD && hidden ? 0.f : y;
           }
         }
-      }
-#pragma unroll
-      for (int d = 0; d < MB; ++d)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          sum(0, d, x);
-#pragma unroll
-          for (int i = (d * 2 + x) * 16 / (2 * MB); i < (d * 2 + x + 1) * 16 / (2 * MB); ++i) weigh(1, i);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-      for (int d = 0; d < MB; ++d)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) sum(1, d, x);
+      };
+      if (ODD || mask)
+        weigh(true);
+      else
+        weigh(false);
+      bool odd = false;
+      if constexpr (ODD) odd = clear_if_odd<T, L::N>(added, causal && t * kTile + 1 < k0 + kRows, 512);
+      add_columns<T, DP, N>(o, added, x0, d0, s, lane);
       if constexpr (ODD) {
         if (odd) {
           const uint32_t hq = h * p.group + g;
-          const T* qp = (const T*)a.q + (int64_t)sp.first * a.q_stride[0] + (int64_t)hq * a.q_stride[1];
-          const T* op = (const T*)a.dout + (int64_t)sp.first * a.dout_stride[0] + (int64_t)hq * a.dout_stride[1];
-          const auto sees = [&](uint32_t row) { return key <= row; };
-          for (uint32_t x = 0; x < kTile; x += 32) {
-            if constexpr (kV) add_odd<T, DP>(ov, op, a.dout_stride[0], i0 + x, sp.n, a.dim, half, false, sees);
-            if constexpr (kK) add_odd<T, DP>(ok, qp, a.q_stride[0], i0 + x, sp.n, a.dim, half, true, sees);
-          }
+          const T* from = DV ? (const T*)a.dout + (int64_t)sp.first * a.dout_stride[0] + (int64_t)hq * a.dout_stride[1]
+                             : (const T*)a.q + (int64_t)sp.first * a.q_stride[0] + (int64_t)hq * a.q_stride[1];
+          add_odd<T, N>(o, from, DV ? a.dout_stride[0] : a.q_stride[0], i0, sp.n, d0 * 32, a.dim, half, !DV,
+                        [&](uint32_t row) { return key <= row; });
         }
       }
     }
+  // the second half's sums, a block of columns at a time, to the first half's waves
+  __syncthreads();
+  float* s_sum = (float*)s_qo + wave % 4 * (N * 1024) + lane * 4;
+  static_assert(4 * N * 1024 * 4 <= 4 * L::N * sizeof(T), "the sums fit the tiles' LDS");
+  if (wave >= 4) {
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = o[d][i * 4 + e];
+        *(f32x4*)(s_sum + d * 1024 + i * 256) = y;
+      }
+  }
+  __syncthreads();
+  if (wave < 4) {
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 y = *(const f32x4*)(s_sum + d * 1024 + i * 256);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[d][i * 4 + e] += y[e];
+      }
+  }
   if constexpr (!ODD) {
-    if (__syncthreads_or(causal && valid && (any_odd(ok) || any_odd(ov)))) return true;
+    if (__syncthreads_or(causal && wave < 4 && valid && any_odd(o))) return true;
   } else {
     __syncthreads();
   }
-  T* s = s_qo + wave * 32 * (DP + 8);
-  const uint32_t rows = sp.n > w0 ? sp.n - w0 : 0;
-  T* dk = (T*)a.dk + (int64_t)(sp.first + w0) * a.dk_stride[0] + (int64_t)h * a.dk_stride[1];
-  T* dv = (T*)a.dv + (int64_t)(sp.first + w0) * a.dv_stride[0] + (int64_t)h * a.dv_stride[1];
-  if constexpr (kV) write_rows<T, DP>(s, ov, 1.f, dv, a.dv_stride[0], rows, a.dim, lane);
-  asm volatile("" ::: "memory");
-  if constexpr (kK) write_rows<T, DP>(s, ok, a.scale, dk, a.dk_stride[0], rows, a.dim, lane);
+  if (wave < 4) {
+    const int64_t* stride = DV ? a.dv_stride : a.dk_stride;
+    T* out = (T*)(DV ? a.dv : a.dk) + (int64_t)(sp.first + w0) * stride[0] + (int64_t)h * stride[1];
+    write_rows<T, N>(s_qo + wave * 32 * (DP + 8), o, DV ? 1.f : a.scale, out, stride[0], sp.n > w0 ? sp.n - w0 : 0, d0 * 32,
+                     a.dim, lane);
+  }
   return false;
 }
 
-template <typename T, int DP, int WHAT>
-__global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void dkv_tile_kernel(PromptGradParams p) {
+template <typename T, int DP, bool DV>
+__global__ __launch_bounds__(512, 2) void dkv_tile_kernel(PromptGradParams p) {
   const gts_prompt_grad_args& a = p.a;
   __shared__ __align__(16) T s_qo[4 * Tiles<T, DP>::N];
   __shared__ __align__(16) float s_stat[2][2][kTile];
@@ -1102,11 +1109,16 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void dkv_tile_kernel(PromptG
   Span sp;
   if (!find_span(a.starts, a.batch, a.tokens, kRows, blockIdx.x / a.kv_heads, &sp)) return;
   if (!sp.in) {
-    if (WHAT & 1) zero_rows((T*)a.dv, a.dv_stride, sp, h, a.dim);
-    if (WHAT & 2) zero_rows((T*)a.dk, a.dk_stride, sp, h, a.dim);
+    if (DV)
+      zero_rows((T*)a.dv, a.dv_stride, sp, h, a.dim);
+    else
+      zero_rows((T*)a.dk, a.dk_stride, sp, h, a.dim);
     return;
   }
-  if (dkv_keys<T, DP, WHAT, false>(p, sp, h, s_qo, s_stat)) dkv_keys<T, DP, WHAT, true>(p, sp, h, s_qo, s_stat);
+  bool odd = false;
+  for (int d = 0; d < DP / 32; d += kBlocks<DP>) odd |= dkv_keys<T, DP, DV, false>(p, sp, h, s_qo, s_stat, d);
+  if (odd)
+    for (int d = 0; d < DP / 32; ++d) dkv_keys<T, DP, DV, true>(p, sp, h, s_qo, s_stat, d);
 }
 
 bool rows_aligned(const void* p, const int64_t* stride, uint32_t e) {
@@ -1148,12 +1160,8 @@ hipError_t launch_prompt_grad_d(const PromptGradParams& p, hipStream_t s) {
     if (p.vec && a.dim % 8 == 0 && rows_aligned(a.dq, a.dq_stride, 2) && rows_aligned(a.dk, a.dk_stride, 2) &&
         rows_aligned(a.dv, a.dv_stride, 2) && near(a.k_stride) && near(a.v_stride) && near(a.q_stride) && near(a.dout_stride)) {
       dq_tile_kernel<T, DP><<<rows, block, 0, s>>>(p);
-      if constexpr (DP == 256) {
-        dkv_tile_kernel<T, DP, 1><<<keys, block, 0, s>>>(p);
-        dkv_tile_kernel<T, DP, 2><<<keys, block, 0, s>>>(p);
-      } else {
-        dkv_tile_kernel<T, DP, 3><<<keys, block, 0, s>>>(p);
-      }
+      dkv_tile_kernel<T, DP, false><<<keys, dim3(512), 0, s>>>(p);
+      dkv_tile_kernel<T, DP, true><<<keys, dim3(512), 0, s>>>(p);
       return hipGetLastError();
     }
   }
