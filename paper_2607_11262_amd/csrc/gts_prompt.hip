@@ -64,6 +64,7 @@ __device__ __forceinline__ bool find_span(const int32_t* starts, uint32_t batch,
 // holds their operands in registers; 32 keys (or rows) at a time go through registers to
 // LDS.
 constexpr uint32_t kRows = 128, kStep = 32;
+constexpr uint32_t kKeys = 64;  // keys of a workgroup of dkv_tile_kernel
 
 template <typename T, int DP>
 struct Held {  // 32 rows of a wave
@@ -562,9 +563,9 @@ __device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& s
 }
 
 // Zeros to the rows of a tile that is in no sequence.
-template <typename T>
+template <uint32_t ROWS, typename T>
 __device__ __forceinline__ void zero_rows(T* out, const int64_t* stride, const Span& sp, uint32_t head, uint32_t dim) {
-  const uint32_t rows = sp.n - sp.tile * kRows < kRows ? sp.n - sp.tile * kRows : kRows, first = sp.first + sp.tile * kRows;
+  const uint32_t rows = sp.n - sp.tile * ROWS < ROWS ? sp.n - sp.tile * ROWS : ROWS, first = sp.first + sp.tile * ROWS;
   for (uint32_t i = threadIdx.x; i < rows * (dim / 8); i += blockDim.x)
     *(u32x4*)(out + (int64_t)(first + i / (dim / 8)) * stride[0] + (int64_t)head * stride[1] + i % (dim / 8) * 8) =
         u32x4{0, 0, 0, 0};
@@ -581,7 +582,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
   const uint32_t place = p.places - 1 - blockIdx.x / a.q_heads;
   if (!find_span(a.starts, a.batch, a.tokens, kRows, place, &sp)) return;
   if (!sp.in) {
-    zero_rows((T*)a.out, a.out_stride, sp, hq, a.dim);
+    zero_rows<kRows>((T*)a.out, a.out_stride, sp, hq, a.dim);
     const uint32_t first = sp.tile * kRows;
     if (a.lse)
       for (uint32_t i = first + threadIdx.x; i < sp.n && i < first + kRows; i += 256)
@@ -599,14 +600,60 @@ struct PromptGradParams {
   bool vec;      // rows of dout, q, k and v are aligned to 16 bytes
   // [q_heads][tokens]: a head's values side by side; lse in base 2
   float *lse, *delta;
+  uint32_t key_places;
+  uint32_t* order;  // [key_places] those with the most rows to a key first
   __device__ __forceinline__ uint64_t stat(uint32_t head, uint32_t token) const { return (uint64_t)head * a.tokens + token; }
 };
 
-// delta, and lse in base 2: 64 tokens of a head a workgroup, 16 lanes a row.
+// The order in which places of keys are taken: a workgroup's work goes with the rows that see its
+// keys, and the longest must not begin last (8 packed texts in the order of their tokens: a fifth
+// more time).  Places are counted by the logarithm of their work; a thread a place.
+__device__ __forceinline__ void sort_places(const PromptGradParams& p) {
+  const gts_prompt_grad_args& a = p.a;
+  __shared__ uint32_t s_count[256];
+  const auto bucket = [&](uint32_t place) {
+    uint32_t lo = 0, n = a.batch + 2;  // as find_span, by one thread
+    while (n > 1) {
+      const uint32_t e = lo + n / 2;
+      if (bound_of(a.starts, a.batch, a.tokens, e) / kKeys + e <= place) {
+        lo = e;
+        n -= n / 2;
+      } else {
+        n /= 2;
+      }
+    }
+    const uint32_t b0 = bound_of(a.starts, a.batch, a.tokens, lo), b1 = bound_of(a.starts, a.batch, a.tokens, lo + 1);
+    const uint64_t n_rows = b1 > b0 ? b1 - b0 : 0, k0 = (uint64_t)(place - (b0 / kKeys + lo)) * kKeys;
+    const uint64_t work = k0 >= n_rows ? 0 : a.flags & GTS_PROMPT_CAUSAL ? n_rows - k0 : n_rows;
+    return 255u - (uint32_t)(log2f((float)(work / kTile + 1)) * 9.f);  // 2^31 rows: 225
+  };
+  s_count[threadIdx.x] = 0;
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < p.key_places; i += 256) atomicAdd(&s_count[bucket(i)], 1u);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t sum = 0;
+    for (int i = 0; i < 256; ++i) {
+      const uint32_t c = s_count[i];
+      s_count[i] = sum;
+      sum += c;
+    }
+  }
+  __syncthreads();
+  // places of one bucket in any order: it says when they are taken, not what they give
+  for (uint32_t i = threadIdx.x; i < p.key_places; i += 256) p.order[atomicAdd(&s_count[bucket(i)], 1u)] = i;
+}
+
+// delta, and lse in base 2: 64 tokens of a head a workgroup, 16 lanes a row.  The first workgroup
+// sorts the places.
 template <typename T>
 __global__ __launch_bounds__(256) void stats_kernel(PromptGradParams p) {
   const gts_prompt_grad_args& a = p.a;
-  const uint32_t h = blockIdx.x % a.q_heads, t0 = blockIdx.x / a.q_heads * 64, lane = threadIdx.x & 63u;
+  if (blockIdx.x == 0) {
+    sort_places(p);
+    return;
+  }
+  const uint32_t h = (blockIdx.x - 1) % a.q_heads, t0 = (blockIdx.x - 1) / a.q_heads * 64, lane = threadIdx.x & 63u;
   const uint32_t sub = lane / 16, li = lane % 16;
 #pragma unroll
   for (uint32_t i = 0; i < 4; ++i) {
@@ -944,7 +991,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dq_tile_kernel(PromptG
   Span sp;
   if (!find_span(a.starts, a.batch, a.tokens, kRows, p.places - 1 - blockIdx.x / a.q_heads, &sp)) return;
   if (!sp.in) {
-    zero_rows((T*)a.dq, a.dq_stride, sp, hq, a.dim);
+    zero_rows<kRows>((T*)a.dq, a.dq_stride, sp, hq, a.dim);
     return;
   }
   if (dq_rows<T, DP, false>(p, sp, hq, h, s_kv))
@@ -961,8 +1008,8 @@ __device__ __forceinline__ void load_to_lds4(const void* from, void* to) {
                : "memory");
 }
 
-// 128 keys, four groups of 32; all rows that see them, of all query heads of the key-value head,
-// 64 at a time: eight waves, one for each group of keys and half of the rows, whose sums are joined
+// 64 keys, two groups of 32; all rows that see them, of all query heads of the key-value head,
+// 64 at a time: four waves, one for each group of keys and half of the rows, whose sums are joined
 // at the end.  dv and dk take a kernel each (`DV`), which computes the scores once more but leaves
 // registers for two waves a SIMD, one of which computes weights while the other multiplies.
 // Heads of 256 take two passes of 128 columns each, for which there are registers.
@@ -975,11 +1022,11 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
   using L = Tiles<T, DP>;
   constexpr int KK = DP / 16, N = ODD ? 1 : kBlocks<DP>;
   const gts_prompt_grad_args& a = p.a;
-  const uint32_t lane = fresh_lane(), wave = uni(threadIdx.x >> 6), half = lane / 32, x0 = wave / 4 * 32;
-  const uint32_t k0 = sp.tile * kRows, w0 = k0 + wave % 4 * 32, key = w0 + lane % 32, there = key < sp.n ? key : 0;
+  const uint32_t lane = fresh_lane(), wave = uni(threadIdx.x >> 6), half = lane / 32, x0 = wave / 2 * 32;
+  const uint32_t k0 = sp.tile * kKeys, w0 = k0 + wave % 2 * 32, key = w0 + lane % 32, there = key < sp.n ? key : 0;
   const bool valid = key < sp.n, causal = a.flags & GTS_PROMPT_CAUSAL;
   const float c = a.scale * kLog2e;
-  Loader<T, DP, 8> ld;
+  Loader<T, DP> ld;
   ld.a_stride = a.q_stride[0];
   ld.b_stride = a.dout_stride[0];
   ld.n = sp.n;
@@ -1048,7 +1095,7 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
       else
         weigh(false);
       bool odd = false;
-      if constexpr (ODD) odd = clear_if_odd<T, L::N>(added, causal && t * kTile + 1 < k0 + kRows, 512);
+      if constexpr (ODD) odd = clear_if_odd<T, L::N>(added, causal && t * kTile + 1 < k0 + kKeys, 256);
       add_columns<T, DP, N>(o, added, x0, d0, s, lane);
       if constexpr (ODD) {
         if (odd) {
@@ -1062,9 +1109,9 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
     }
   // the second half's sums, a block of columns at a time, to the first half's waves
   __syncthreads();
-  float* s_sum = (float*)s_qo + wave % 4 * (N * 1024) + lane * 4;
-  static_assert(4 * N * 1024 * 4 <= 4 * L::N * sizeof(T), "the sums fit the tiles' LDS");
-  if (wave >= 4) {
+  float* s_sum = (float*)s_qo + wave % 2 * (N * 1024) + lane * 4;
+  static_assert(2 * N * 1024 * 4 <= 4 * L::N * sizeof(T), "the sums fit the tiles' LDS");
+  if (wave >= 2) {
 #pragma unroll
     for (int d = 0; d < N; ++d)
 #pragma unroll
@@ -1076,7 +1123,7 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
       }
   }
   __syncthreads();
-  if (wave < 4) {
+  if (wave < 2) {
 #pragma unroll
     for (int d = 0; d < N; ++d)
 #pragma unroll
@@ -1087,11 +1134,11 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
       }
   }
   if constexpr (!ODD) {
-    if (__syncthreads_or(causal && wave < 4 && valid && any_odd(o))) return true;
+    if (__syncthreads_or(causal && wave < 2 && valid && any_odd(o))) return true;
   } else {
     __syncthreads();
   }
-  if (wave < 4) {
+  if (wave < 2) {
     const int64_t* stride = DV ? a.dv_stride : a.dk_stride;
     T* out = (T*)(DV ? a.dv : a.dk) + (int64_t)(sp.first + w0) * stride[0] + (int64_t)h * stride[1];
     write_rows<T, N>(s_qo + wave * 32 * (DP + 8), o, DV ? 1.f : a.scale, out, stride[0], sp.n > w0 ? sp.n - w0 : 0, d0 * 32,
@@ -1101,18 +1148,18 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
 }
 
 template <typename T, int DP, bool DV>
-__global__ __launch_bounds__(512, 2) void dkv_tile_kernel(PromptGradParams p) {
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_tile_kernel(PromptGradParams p) {
   const gts_prompt_grad_args& a = p.a;
   __shared__ __align__(16) T s_qo[4 * Tiles<T, DP>::N];
   __shared__ __align__(16) float s_stat[2][2][kTile];
   const uint32_t h = blockIdx.x % a.kv_heads;
   Span sp;
-  if (!find_span(a.starts, a.batch, a.tokens, kRows, blockIdx.x / a.kv_heads, &sp)) return;
+  if (!find_span(a.starts, a.batch, a.tokens, kKeys, uni(p.order[blockIdx.x / a.kv_heads]), &sp)) return;
   if (!sp.in) {
     if (DV)
-      zero_rows((T*)a.dv, a.dv_stride, sp, h, a.dim);
+      zero_rows<kKeys>((T*)a.dv, a.dv_stride, sp, h, a.dim);
     else
-      zero_rows((T*)a.dk, a.dk_stride, sp, h, a.dim);
+      zero_rows<kKeys>((T*)a.dk, a.dk_stride, sp, h, a.dim);
     return;
   }
   bool odd = false;
@@ -1155,13 +1202,13 @@ template <typename T, int DP>
 hipError_t launch_prompt_grad_d(const PromptGradParams& p, hipStream_t s) {
   const gts_prompt_grad_args& a = p.a;
   const dim3 rows(p.places * a.q_heads), keys(p.places * a.kv_heads), block(256);
-  stats_kernel<T><<<dim3((a.tokens + 63) / 64 * a.q_heads), block, 0, s>>>(p);
+  stats_kernel<T><<<dim3((a.tokens + 63) / 64 * a.q_heads + 1), block, 0, s>>>(p);
   if constexpr (sizeof(T) == 2) {
     if (p.vec && a.dim % 8 == 0 && rows_aligned(a.dq, a.dq_stride, 2) && rows_aligned(a.dk, a.dk_stride, 2) &&
         rows_aligned(a.dv, a.dv_stride, 2) && near(a.k_stride) && near(a.v_stride) && near(a.q_stride) && near(a.dout_stride)) {
       dq_tile_kernel<T, DP><<<rows, block, 0, s>>>(p);
-      dkv_tile_kernel<T, DP, false><<<keys, dim3(512), 0, s>>>(p);
-      dkv_tile_kernel<T, DP, true><<<keys, dim3(512), 0, s>>>(p);
+      dkv_tile_kernel<T, DP, false><<<dim3(p.key_places * a.kv_heads), block, 0, s>>>(p);
+      dkv_tile_kernel<T, DP, true><<<dim3(p.key_places * a.kv_heads), block, 0, s>>>(p);
       return hipGetLastError();
     }
   }
@@ -1177,7 +1224,8 @@ hipError_t launch_prompt_grad_d(const PromptGradParams& p, hipStream_t s) {
 template <typename T>
 hipError_t launch_prompt_grad_t(const gts_prompt_grad_args& a, hipStream_t s) {
   PromptGradParams p{a, a.q_heads / a.kv_heads, places_of(a.batch, a.tokens, kRows), false, (float*)a.scratch,
-                     (float*)a.scratch + (uint64_t)a.tokens * a.q_heads};
+                     (float*)a.scratch + (uint64_t)a.tokens * a.q_heads,
+                     places_of(a.batch, a.tokens, kKeys), (uint32_t*)a.scratch + 2 * (uint64_t)a.tokens * a.q_heads};
   p.vec = rows_aligned(a.q, a.q_stride, sizeof(T)) && rows_aligned(a.k, a.k_stride, sizeof(T)) &&
           rows_aligned(a.v, a.v_stride, sizeof(T)) && rows_aligned(a.dout, a.dout_stride, sizeof(T));
   if (a.dim <= 64) return launch_prompt_grad_d<T, 64>(p, s);
@@ -1188,7 +1236,7 @@ hipError_t launch_prompt_grad_t(const gts_prompt_grad_args& a, hipStream_t s) {
 }  // namespace
 
 uint64_t prompt_groups(uint32_t batch, uint32_t tokens, uint32_t heads) {
-  return (uint64_t)places_of(batch, tokens, kRows) * heads;
+  return (uint64_t)places_of(batch, tokens, kKeys) * heads;  // the most of any kernel
 }
 
 hipError_t launch_prompt(const gts_prompt_args& a, hipStream_t s) {
@@ -1198,7 +1246,7 @@ hipError_t launch_prompt(const gts_prompt_args& a, hipStream_t s) {
 }
 
 uint64_t prompt_grad_scratch(uint32_t batch, uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t dim) {
-  return 8ull * tokens * q_heads;
+  return 8ull * tokens * q_heads + 4ull * places_of(batch, tokens, kKeys);
 }
 
 hipError_t launch_prompt_grad(const gts_prompt_grad_args& a, hipStream_t s) {
