@@ -6,6 +6,8 @@
 //
 // Either operand may be stored with the sum's index as its rows (the products of a
 // backward pass), so nothing is transposed in memory.
+#include <type_traits>
+
 #include "gts_ops.h"
 #include "gts_tile.h"
 
@@ -19,33 +21,47 @@ constexpr float kNormal = 0.39894228040143268f;     // 1 / sqrt(2 pi)
 constexpr float kTanhA = 0.79788456080286536f;      // sqrt(2 / pi)
 constexpr float kTanhB = 0.044715f;
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + expf(-x)); }
+// One exponential and one reciprocal of the card's, off by a step of 32 bits each; the argument's
+// rounding is |x| steps of the exponential.
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + exp2_(-kLog2e * x)); }
 // Twice the argument of the tanh form; past 30 its sigmoid is 0 or 1 in 32 bits.
 __device__ __forceinline__ float clamp30(float z) { return fminf(fmaxf(z, -30.f), 30.f); }
 __device__ __forceinline__ float tanh_arg(float z) { return 2.f * kTanhA * (z + kTanhB * z * z * z); }
 
-__device__ __forceinline__ float activate(uint32_t act, float z) {
-  switch (act) {
-    case GTS_ACT_RELU: return z > 0.f || z != z ? z : 0.f;
-    case GTS_ACT_GELU: return 0.5f * z * erfcf(-z * kRootHalf);  // no difference of near numbers for z < 0
-    case GTS_ACT_GELU_TANH: return z != z ? z : z * sigmoid(tanh_arg(clamp30(z)));
-    case GTS_ACT_SILU: return z * sigmoid(z);
-    default: return z;
+// The activation of z and its slope there; what the caller drops is not computed.
+struct Shape {
+  float y, slope;
+};
+template <uint32_t ACT>
+__device__ __forceinline__ Shape shape_of(float z) {
+  if constexpr (ACT == GTS_ACT_RELU) {
+    return {z > 0.f || z != z ? z : 0.f, z > 0.f ? 1.f : z != z ? z : 0.f};
+  } else if constexpr (ACT == GTS_ACT_GELU) {
+    const float below = 0.5f * erfcf(-z * kRootHalf);  // no difference of near numbers for z < 0
+    return {z * below, below + z * kNormal * exp2_(-0.5f * kLog2e * z * z)};
+  } else if constexpr (ACT == GTS_ACT_GELU_TANH) {
+    const float c = clamp30(z), s = sigmoid(tanh_arg(c));
+    return {z != z ? z : z * s, z != z ? z : s + c * s * (1.f - s) * 2.f * kTanhA * (1.f + 3.f * kTanhB * c * c)};
+  } else if constexpr (ACT == GTS_ACT_SILU) {
+    const float s = sigmoid(z);
+    return {z * s, s * (1.f + z * (1.f - s))};
+  } else {
+    return {z, 1.f};
   }
 }
-__device__ __forceinline__ float slope(uint32_t act, float z) {
+template <uint32_t ACT, int N>
+__device__ __forceinline__ void activate_all(float* z) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) z[i] = shape_of<ACT>(z[i]).y;
+}
+template <int N>
+__device__ __forceinline__ void activate(uint32_t act, float* z) {
   switch (act) {
-    case GTS_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
-    case GTS_ACT_GELU: return 0.5f * erfcf(-z * kRootHalf) + z * kNormal * expf(-0.5f * z * z);
-    case GTS_ACT_GELU_TANH: {
-      const float c = clamp30(z), s = sigmoid(tanh_arg(c));
-      return z != z ? z : s + c * s * (1.f - s) * 2.f * kTanhA * (1.f + 3.f * kTanhB * c * c);
-    }
-    case GTS_ACT_SILU: {
-      const float s = sigmoid(z);
-      return s * (1.f + z * (1.f - s));
-    }
-    default: return 1.f;
+    case GTS_ACT_RELU: return activate_all<GTS_ACT_RELU, N>(z);
+    case GTS_ACT_GELU: return activate_all<GTS_ACT_GELU, N>(z);
+    case GTS_ACT_GELU_TANH: return activate_all<GTS_ACT_GELU_TANH, N>(z);
+    case GTS_ACT_SILU: return activate_all<GTS_ACT_SILU, N>(z);
+    default: return;
   }
 }
 
@@ -61,7 +77,7 @@ template <typename T>
 __device__ __forceinline__ void finish(const gts_matmul_args& a, uint32_t m, uint32_t n, float z) {
   if (a.bias) z += (float)((const T*)a.bias)[n];
   if (a.preact) ((T*)a.preact)[(int64_t)m * a.preact_stride + n] = (T)z;
-  z = activate(a.activation, z);
+  activate<1>(a.activation, &z);
   if (a.gate) z *= (float)((const T*)a.gate)[(int64_t)m * a.gate_stride + n];
   if (a.residual) z += (float)((const T*)a.residual)[(int64_t)m * a.residual_stride + n];
   ((T*)a.out)[(int64_t)m * a.out_stride + n] = (T)z;
@@ -301,10 +317,7 @@ __device__ __forceinline__ void finish8(const gts_matmul_args& a, uint32_t m, ui
     for (int i = 0; i < 8; ++i) y.v[i] = (T)z[i];
     *(Pack<T, 8>*)((T*)a.preact + (int64_t)m * a.preact_stride + n) = y;
   }
-  if (a.activation != GTS_ACT_NONE) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = activate(a.activation, z[i]);
-  }
+  activate<8>(a.activation, z);
   if (a.gate) {
     const Pack<T, 8> g = *(const Pack<T, 8>*)((const T*)a.gate + (int64_t)m * a.gate_stride + n);
 #pragma unroll
@@ -679,29 +692,42 @@ struct LinearGradParams {
   uint32_t strips;
 };
 
-template <typename T, int V>
+template <typename T, int V, uint32_t ACT>
 __global__ __launch_bounds__(256) void linear_grad_kernel(LinearGradParams p) {
   const gts_linear_grad_args& a = p.a;
   const uint32_t strip = blockIdx.y * 4 + (threadIdx.x >> 6);
   const uint64_t at = ((uint64_t)blockIdx.x * 64 + (threadIdx.x & 63u)) * V;
   if (strip >= p.strips || at >= a.n) return;
   float db[V] = {};
-  for (uint64_t m = strip; m < a.m; m += p.strips) {
-    const Pack<T, V> dy = *(const Pack<T, V>*)((const T*)a.dy + (int64_t)m * a.dy_stride + at);
-    Pack<T, V> z = {}, g = {}, dg, dz;
-    if (a.preact) z = *(const Pack<T, V>*)((const T*)a.preact + (int64_t)m * a.preact_stride + at);
-    if (a.gate) g = *(const Pack<T, V>*)((const T*)a.gate + (int64_t)m * a.gate_stride + at);
+  constexpr int R = 2;  // rows whose loads are on their way together
+  for (uint64_t m0 = strip; m0 < a.m; m0 += (uint64_t)R * p.strips) {
+    Pack<T, V> dy[R], z[R] = {}, g[R] = {};
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      float d = (float)dy.v[i];
-      if (a.dgate) dg.v[i] = (T)(d * activate(a.activation, (float)z.v[i]));
-      if (a.gate) d *= (float)g.v[i];
-      if (a.activation != GTS_ACT_NONE) d *= slope(a.activation, (float)z.v[i]);
-      dz.v[i] = (T)d;
-      db[i] += d;
+    for (int k = 0; k < R; ++k) {
+      const uint64_t m = m0 + (uint64_t)k * p.strips;
+      if (m >= a.m) break;
+      dy[k] = *(const Pack<T, V>*)((const T*)a.dy + (int64_t)m * a.dy_stride + at);
+      if (a.preact) z[k] = *(const Pack<T, V>*)((const T*)a.preact + (int64_t)m * a.preact_stride + at);
+      if (a.gate) g[k] = *(const Pack<T, V>*)((const T*)a.gate + (int64_t)m * a.gate_stride + at);
     }
-    if (a.dz) *(Pack<T, V>*)((T*)a.dz + (int64_t)m * a.dz_stride + at) = dz;
-    if (a.dgate) *(Pack<T, V>*)((T*)a.dgate + (int64_t)m * a.dgate_stride + at) = dg;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const uint64_t m = m0 + (uint64_t)k * p.strips;
+      if (m >= a.m) break;
+      Pack<T, V> dg, dz;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float d = (float)dy[k].v[i];
+        const Shape at_z = shape_of<ACT>((float)z[k].v[i]);
+        if (a.dgate) dg.v[i] = (T)(d * at_z.y);
+        if (a.gate) d *= (float)g[k].v[i];
+        if constexpr (ACT != GTS_ACT_NONE) d *= at_z.slope;
+        dz.v[i] = (T)d;
+        db[i] += d;
+      }
+      if (a.dz) *(Pack<T, V>*)((T*)a.dz + (int64_t)m * a.dz_stride + at) = dz;
+      if (a.dgate) *(Pack<T, V>*)((T*)a.dgate + (int64_t)m * a.dgate_stride + at) = dg;
+    }
   }
   if (p.db) {
 #pragma unroll
@@ -730,10 +756,20 @@ void launch_linear_grad_t(const LinearGradParams& p, hipStream_t s) {
                     rows_aligned(a.dgate, a.dgate ? a.dgate_stride : 0, sizeof(T));
   const uint32_t v = wide ? V : 1;
   const dim3 grid((uint32_t)(((uint64_t)a.n + 64 * v - 1) / (64 * v)), (p.strips + 3) / 4);
-  if (wide)
-    linear_grad_kernel<T, V><<<grid, dim3(256), 0, s>>>(p);
-  else
-    linear_grad_kernel<T, 1><<<grid, dim3(256), 0, s>>>(p);
+  const auto launch = [&](auto act) {
+    constexpr uint32_t A = decltype(act)::value;
+    if (wide)
+      linear_grad_kernel<T, V, A><<<grid, dim3(256), 0, s>>>(p);
+    else
+      linear_grad_kernel<T, 1, A><<<grid, dim3(256), 0, s>>>(p);
+  };
+  switch (a.activation) {
+    case GTS_ACT_RELU: return launch(std::integral_constant<uint32_t, GTS_ACT_RELU>{});
+    case GTS_ACT_GELU: return launch(std::integral_constant<uint32_t, GTS_ACT_GELU>{});
+    case GTS_ACT_GELU_TANH: return launch(std::integral_constant<uint32_t, GTS_ACT_GELU_TANH>{});
+    case GTS_ACT_SILU: return launch(std::integral_constant<uint32_t, GTS_ACT_SILU>{});
+    default: return launch(std::integral_constant<uint32_t, GTS_ACT_NONE>{});
+  }
 }
 
 }  // namespace

@@ -361,6 +361,20 @@ __device__ __forceinline__ uint32_t head_at(uint32_t at, uint32_t kv_heads, uint
   return *kv * group + at / s % group;
 }
 
+// Which (place, head) pair a workgroup takes, the last places first: with a causal mask they see
+// the most keys.  Of one sequence whose workgroups are all at work at once, two a CU, the second of
+// a CU should be short if its first is long: the second 256 come in the other order.  Places without
+// tokens are then the last.
+__device__ __forceinline__ uint32_t place_at(uint32_t batch, uint32_t tokens, uint32_t places, uint32_t heads, bool causal,
+                                             uint32_t* at) {
+  uint32_t i = blockIdx.x;
+  const uint32_t n = (tokens + kRows - 1) / kRows;
+  if (batch == 1 && causal && n * heads <= 512 && i >= 256 && i < n * heads) i = 256 + n * heads - 1 - i;
+  *at = i % heads;
+  i /= heads;
+  return batch > 1 ? places - 1 - i : i < n ? n - i : i == n ? 0 : i;
+}
+
 // What a wave of the forward kernel holds: 32 rows, and N blocks of 32 columns of their results.
 template <typename T, int DP, int N>
 struct Rows {
@@ -576,10 +590,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
   const gts_prompt_args& a = p.a;
   __shared__ __align__(16) T s_kv[4 * Tiles<T, DP>::N];
   uint32_t h;
-  const uint32_t hq = head_at(blockIdx.x % a.q_heads, a.kv_heads, p.group, &h);
+  uint32_t at;
+  const uint32_t place = place_at(a.batch, a.tokens, p.places, a.q_heads, a.flags & GTS_PROMPT_CAUSAL, &at);
+  const uint32_t hq = head_at(at, a.kv_heads, p.group, &h);
   Span sp;
-  // the last tiles of a sequence see the most keys: first
-  const uint32_t place = p.places - 1 - blockIdx.x / a.q_heads;
   if (!find_span(a.starts, a.batch, a.tokens, kRows, place, &sp)) return;
   if (!sp.in) {
     zero_rows<kRows>((T*)a.out, a.out_stride, sp, hq, a.dim);
@@ -987,9 +1001,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dq_tile_kernel(PromptG
   const gts_prompt_grad_args& a = p.a;
   __shared__ __align__(16) T s_kv[4 * Tiles<T, DP>::N];
   uint32_t h;
-  const uint32_t hq = head_at(blockIdx.x % a.q_heads, a.kv_heads, p.group, &h);
+  uint32_t at;
+  const uint32_t place = place_at(a.batch, a.tokens, p.places, a.q_heads, a.flags & GTS_PROMPT_CAUSAL, &at);
+  const uint32_t hq = head_at(at, a.kv_heads, p.group, &h);
   Span sp;
-  if (!find_span(a.starts, a.batch, a.tokens, kRows, p.places - 1 - blockIdx.x / a.q_heads, &sp)) return;
+  if (!find_span(a.starts, a.batch, a.tokens, kRows, place, &sp)) return;
   if (!sp.in) {
     zero_rows<kRows>((T*)a.dq, a.dq_stride, sp, hq, a.dim);
     return;
