@@ -817,3 +817,30 @@ def test_layer_refusals():
     with pytest.raises(api.GtsError):
         ops.prompt_attention(big, big, big)
     torch.cuda.synchronize()
+
+
+def test_decoder_layer_example():
+    import importlib.util
+    import os
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    folder = os.path.join(root, "examples")
+    sys.path.insert(0, folder)
+    try:
+        spec = importlib.util.spec_from_file_location("decoder_layer", os.path.join(folder, "decoder_layer.py"))
+        example = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(example)
+    finally:
+        sys.path.remove(folder)
+    args = ["--tokens", "128", "--hidden", "256", "--heads", "2", "--kv-heads", "1", "--ffn", "384", "--steps", "3", "--backward"]
+    r = example.main(args)
+    assert r["measured"] > 0 and r["train"] > 0 and r["simulated"] > 0
+    # the captured pass and its gradients are those of the eager calls
+    lay = example.Layer(128, 256, 2, 1, 384)
+    assert torch.equal(r["out"], lay.step())
+    y, grads = lay.train()
+    assert torch.equal(y, r["out"]) and len(grads) == len(r["grads"])
+    for a, b in zip(grads, r["grads"]):
+        assert torch.equal(a, b)
+    with pytest.raises(SystemExit):
+        example.main(["--hidden", "100"])
