@@ -615,6 +615,10 @@ struct PromptGradParams {
   // [q_heads][tokens]: a head's values side by side; lse in base 2
   float *lse, *delta;
   uint32_t key_places;
+  // The query heads of a key-value head are summed in this many parts; with more than one, the
+  // parts are [splits][tokens][kv_heads][dim] in 32 bits.
+  uint32_t splits;
+  float* parts;
   uint32_t* order;  // [key_places] those with the most rows to a key first
   __device__ __forceinline__ uint64_t stat(uint32_t head, uint32_t token) const { return (uint64_t)head * a.tokens + token; }
 };
@@ -1033,7 +1037,7 @@ template <int DP>
 constexpr int kBlocks = DP / 32 < 4 ? DP / 32 : 4;
 
 template <typename T, int DP, bool DV, bool ODD>
-__device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& sp, uint32_t h, T* s_qo,
+__device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& sp, uint32_t h, uint32_t split, T* s_qo,
                                          float (*s_stat)[2][kTile], int d0 = 0) {
   using L = Tiles<T, DP>;
   constexpr int KK = DP / 16, N = ODD ? 1 : kBlocks<DP>;
@@ -1061,8 +1065,9 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
       load_to_lds4(i < sp.n ? from : (const float*)g_zeros, s_stat[buffer][wave]);
     }
   };
+  const uint32_t g0 = split * (p.group / p.splits), g1 = g0 + p.group / p.splits;  // its query heads
   __syncthreads();
-  load(0, first, 0);
+  load(g0, first, 0);
   Vec8<T> k[KK], v[DV ? 1 : KK];
   const T* kp = (const T*)a.k + (int64_t)(sp.first + there) * a.k_stride[0] + (int64_t)h * a.k_stride[1];
   const T* vp = (const T*)a.v + (int64_t)(sp.first + there) * a.v_stride[0] + (int64_t)h * a.v_stride[1];
@@ -1075,7 +1080,7 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
   f32x16 o[N];
   clear(o);
   uint32_t buffer = 0;
-  for (uint32_t g = 0; g < p.group; ++g)
+  for (uint32_t g = g0; g < g1; ++g)
     for (uint32_t t = first; t < tiles; ++t, buffer ^= 1) {
       const uint32_t i0 = t * kTile + x0;  // the wave's first row
       T *sq = s_qo + buffer * 2 * L::N, *so = sq + L::N, *added = DV ? so : sq;
@@ -1083,7 +1088,7 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
       __syncthreads();
       if (t + 1 < tiles)
         load(g, t + 1, buffer ^ 1);
-      else if (g + 1 < p.group)
+      else if (g + 1 < g1)
         load(g + 1, first, buffer ^ 1);
       if (!ODD && ((causal && i0 + 32 <= w0) || i0 >= sp.n)) continue;  // no row of the wave's sees a key of its
       const bool mask = (causal && i0 < w0 + 31) || i0 + 32 > sp.n;
@@ -1154,11 +1159,24 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
   } else {
     __syncthreads();
   }
-  if (wave < 2) {
+  if (wave >= 2) return false;
+  const uint32_t rows = sp.n > w0 ? sp.n - w0 : 0;
+  if (p.splits == 1) {
     const int64_t* stride = DV ? a.dv_stride : a.dk_stride;
     T* out = (T*)(DV ? a.dv : a.dk) + (int64_t)(sp.first + w0) * stride[0] + (int64_t)h * stride[1];
-    write_rows<T, N>(s_qo + wave * 32 * (DP + 8), o, DV ? 1.f : a.scale, out, stride[0], sp.n > w0 ? sp.n - w0 : 0, d0 * 32,
-                     a.dim, lane);
+    write_rows<T, N>(s_qo + wave * 32 * (DP + 8), o, DV ? 1.f : a.scale, out, stride[0], rows, d0 * 32, a.dim, lane);
+  } else if (valid) {
+    float* out = p.parts + (((uint64_t)split * a.tokens + sp.first + key) * a.kv_heads + h) * a.dim;
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const uint32_t c = (d0 + d) * 32 + frag_row(i, half);
+        f32x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = o[d][i + e] * (DV ? 1.f : a.scale);
+        if (c < a.dim) *(f32x4*)(out + c) = y;
+      }
   }
   return false;
 }
@@ -1168,10 +1186,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_tile_kernel(Prompt
   const gts_prompt_grad_args& a = p.a;
   __shared__ __align__(16) T s_qo[4 * Tiles<T, DP>::N];
   __shared__ __align__(16) float s_stat[2][2][kTile];
-  const uint32_t h = blockIdx.x % a.kv_heads;
+  const uint32_t h = blockIdx.x % a.kv_heads, at = blockIdx.x / a.kv_heads, place = at / p.splits, split = at - place * p.splits;
   Span sp;
-  if (!find_span(a.starts, a.batch, a.tokens, kKeys, uni(p.order[blockIdx.x / a.kv_heads]), &sp)) return;
+  if (!find_span(a.starts, a.batch, a.tokens, kKeys, uni(p.order[place]), &sp)) return;
   if (!sp.in) {
+    if (split) return;
     if (DV)
       zero_rows<kKeys>((T*)a.dv, a.dv_stride, sp, h, a.dim);
     else
@@ -1179,9 +1198,30 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_tile_kernel(Prompt
     return;
   }
   bool odd = false;
-  for (int d = 0; d < DP / 32; d += kBlocks<DP>) odd |= dkv_keys<T, DP, DV, false>(p, sp, h, s_qo, s_stat, d);
+  for (int d = 0; d < DP / 32; d += kBlocks<DP>) odd |= dkv_keys<T, DP, DV, false>(p, sp, h, split, s_qo, s_stat, d);
   if (odd)
-    for (int d = 0; d < DP / 32; ++d) dkv_keys<T, DP, DV, true>(p, sp, h, s_qo, s_stat, d);
+    for (int d = 0; d < DP / 32; ++d) dkv_keys<T, DP, DV, true>(p, sp, h, split, s_qo, s_stat, d);
+}
+
+// The parts' sum, in order, for the tokens of the sequences; four values a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void join_parts_kernel(PromptGradParams p, T* out, int64_t stride0, int64_t stride1) {
+  const gts_prompt_grad_args& a = p.a;
+  const uint64_t i = (block_number() * 256 + threadIdx.x) * 4, all = (uint64_t)a.tokens * a.kv_heads * a.dim;
+  if (i >= all) return;
+  const uint32_t row = (uint32_t)(i / a.dim), c = (uint32_t)(i - (uint64_t)row * a.dim), t = row / a.kv_heads;
+  if (a.starts && (int64_t)t < a.starts[0]) return;
+  if (a.starts && (int64_t)t >= a.starts[a.batch]) return;
+  f32x4 sum = *(const f32x4*)(p.parts + i);
+  for (uint32_t s = 1; s < p.splits; ++s) {
+    const f32x4 x = *(const f32x4*)(p.parts + s * all + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += x[e];
+  }
+  Pack<T, 4> y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y.v[e] = (T)sum[e];
+  *(Pack<T, 4>*)(out + (int64_t)t * stride0 + (int64_t)(row - t * a.kv_heads) * stride1 + c) = y;
 }
 
 bool rows_aligned(const void* p, const int64_t* stride, uint32_t e) {
@@ -1214,6 +1254,21 @@ hipError_t launch_prompt_t(const gts_prompt_args& a, hipStream_t s) {
   return launch_prompt_d<T, 256>(p, s);
 }
 
+// Parts of the sum over a key-value head's query heads: where its workgroups do not fill the chip
+// twice over, the most that divide the group and give no more than that.  By sizes alone.
+uint32_t splits_of(uint32_t tokens, uint32_t q_heads, uint32_t kv_heads) {
+  const uint32_t group = q_heads / kv_heads;
+  const uint64_t groups = (uint64_t)(tokens / kKeys + 1) * kv_heads;
+  uint32_t n = 1;
+  for (uint32_t s = 2; s <= group && groups * s <= 1024; ++s)
+    if (group % s == 0) n = s;
+  return n;
+}
+uint64_t parts_bytes(uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t dim) {
+  const uint32_t s = splits_of(tokens, q_heads, kv_heads);
+  return s > 1 ? ((4ull * s * tokens * kv_heads * dim + 15) & ~15ull) : 0;
+}
+
 template <typename T, int DP>
 hipError_t launch_prompt_grad_d(const PromptGradParams& p, hipStream_t s) {
   const gts_prompt_grad_args& a = p.a;
@@ -1223,8 +1278,12 @@ hipError_t launch_prompt_grad_d(const PromptGradParams& p, hipStream_t s) {
     if (p.vec && a.dim % 8 == 0 && rows_aligned(a.dq, a.dq_stride, 2) && rows_aligned(a.dk, a.dk_stride, 2) &&
         rows_aligned(a.dv, a.dv_stride, 2) && near(a.k_stride) && near(a.v_stride) && near(a.q_stride) && near(a.dout_stride)) {
       dq_tile_kernel<T, DP><<<rows, block, 0, s>>>(p);
-      dkv_tile_kernel<T, DP, false><<<dim3(p.key_places * a.kv_heads), block, 0, s>>>(p);
-      dkv_tile_kernel<T, DP, true><<<dim3(p.key_places * a.kv_heads), block, 0, s>>>(p);
+      const dim3 groups(p.key_places * a.kv_heads * p.splits);
+      const dim3 join = grid_of(((uint64_t)a.tokens * a.kv_heads * a.dim / 4 + 255) / 256);
+      dkv_tile_kernel<T, DP, false><<<groups, block, 0, s>>>(p);
+      if (p.splits > 1) join_parts_kernel<T><<<join, block, 0, s>>>(p, (T*)a.dk, a.dk_stride[0], a.dk_stride[1]);
+      dkv_tile_kernel<T, DP, true><<<groups, block, 0, s>>>(p);
+      if (p.splits > 1) join_parts_kernel<T><<<join, block, 0, s>>>(p, (T*)a.dv, a.dv_stride[0], a.dv_stride[1]);
       return hipGetLastError();
     }
   }
@@ -1239,9 +1298,16 @@ hipError_t launch_prompt_grad_d(const PromptGradParams& p, hipStream_t s) {
 }
 template <typename T>
 hipError_t launch_prompt_grad_t(const gts_prompt_grad_args& a, hipStream_t s) {
-  PromptGradParams p{a, a.q_heads / a.kv_heads, places_of(a.batch, a.tokens, kRows), false, (float*)a.scratch,
-                     (float*)a.scratch + (uint64_t)a.tokens * a.q_heads,
-                     places_of(a.batch, a.tokens, kKeys), (uint32_t*)a.scratch + 2 * (uint64_t)a.tokens * a.q_heads};
+  PromptGradParams p{};
+  p.a = a;
+  p.group = a.q_heads / a.kv_heads;
+  p.places = places_of(a.batch, a.tokens, kRows);
+  p.key_places = places_of(a.batch, a.tokens, kKeys);
+  p.splits = splits_of(a.tokens, a.q_heads, a.kv_heads);
+  p.parts = (float*)a.scratch;
+  p.lse = (float*)((char*)a.scratch + parts_bytes(a.tokens, a.q_heads, a.kv_heads, a.dim));
+  p.delta = p.lse + (uint64_t)a.tokens * a.q_heads;
+  p.order = (uint32_t*)(p.delta + (uint64_t)a.tokens * a.q_heads);
   p.vec = rows_aligned(a.q, a.q_stride, sizeof(T)) && rows_aligned(a.k, a.k_stride, sizeof(T)) &&
           rows_aligned(a.v, a.v_stride, sizeof(T)) && rows_aligned(a.dout, a.dout_stride, sizeof(T));
   if (a.dim <= 64) return launch_prompt_grad_d<T, 64>(p, s);
@@ -1262,7 +1328,7 @@ hipError_t launch_prompt(const gts_prompt_args& a, hipStream_t s) {
 }
 
 uint64_t prompt_grad_scratch(uint32_t batch, uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t dim) {
-  return 8ull * tokens * q_heads + 4ull * places_of(batch, tokens, kKeys);
+  return parts_bytes(tokens, q_heads, kv_heads, dim) + 8ull * tokens * q_heads + 4ull * places_of(batch, tokens, kKeys);
 }
 
 hipError_t launch_prompt_grad(const gts_prompt_grad_args& a, hipStream_t s) {
