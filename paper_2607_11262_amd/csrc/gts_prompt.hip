@@ -299,17 +299,42 @@ struct Loader {
 };
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// Fragments of a tile: rows row + lane % 32, places 16 kk + 8 half ..; at = the lane's part.
+// Where a lane's parts of a tile's fragments stand, in bytes from the row that the fragment begins
+// with (a whole number of 16): kept for all tiles, because computing them took a third of the vector
+// instructions beside the matrix ones.
 template <typename T, int DP>
-struct RowFrags {
-  const T* at;
-  uint32_t c;
-  __device__ __forceinline__ RowFrags(const T* s, uint32_t row, uint32_t lane)
-      : at(s + (row + lane % 32) * DP), c(lane / 32 ^ Tiles<T, DP>::swizzle(lane % 32)) {}
-  __device__ __forceinline__ Vec8<T> operator()(int kk) const { return *(const Vec8<T>*)(at + (c ^ (2 * kk)) * 8); }
+struct Parts {
+  uint32_t row[DP / 16], column[2][DP / 32];
+  __device__ __forceinline__ void start(uint32_t lane) {
+    using L = Tiles<T, DP>;
+    const uint32_t c = lane / 32 ^ L::swizzle(lane % 32);
+#pragma unroll
+    for (int kk = 0; kk < DP / 16; ++kk) row[kk] = 2 * (lane % 32 * DP + (c ^ (2 * kk)) * 8);
+    const uint32_t g = lane / 16, r = 4 * (g / 2) + lane % 16 / 4, cc = g % 2 * 2 + lane % 4 / 2;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+        column[x][d] = 2 * ((r + 8 * x) * DP + lane % 2 * 4 + ((cc ^ L::swizzle(r + 8 * x)) ^ (d * 4)) * 8);
+  }
+  // Rows at + lane % 32 of s, places 16 kk + 8 half ..
+  __device__ __forceinline__ Vec8<T> rows(const T* s, uint32_t at, int kk) const {
+    return *(const Vec8<T>*)((const char*)s + row[kk] + at * DP * 2);
+  }
+  // Columns 32 d + lane % 32, rows at + 4 half .. + 3 and 8 further.
+  __device__ __forceinline__ Vec8<T> columns(const T* s, uint32_t at, int d) const {
+    typedef __attribute__((address_space(3))) i16x4* lds_t;
+    union {
+      i16x4 h[2];
+      Vec8<T> v;
+    } u;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      u.h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)((const char*)s + column[x][d] + at * DP * 2));
+    return u.v;
+  }
 };
-// The same of columns 32 d + lane % 32, rows row + 4 half .. + 3 and 8 further (what a lane
-// has of a product's result).
+// The same columns for a block d that is not known when this is compiled.
 template <typename T, int DP>
 __device__ __forceinline__ Vec8<T> column_frag(const T* s, uint32_t row, int d, uint32_t lane) {
   using L = Tiles<T, DP>;
@@ -380,7 +405,8 @@ template <typename T, int DP, int N>
 struct Rows {
   Vec8<T> q[DP / 16];
   f32x16 o[N];
-  int d0;  // the first of the blocks
+  Parts<T, DP> at;
+  int d0;  // the first of the blocks; 0 where they are all
   float m, l;  // reference maximum of q.k (unscaled), sum of this half's weights
 
   // 32 NS keys from LDS row `key` on; the lane's row sees those before `sees` (from there).
@@ -393,13 +419,12 @@ struct Rows {
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
     // The fragments of two matrix steps are read while the two before are multiplied; the
     // fences keep that order.
-    const RowFrags<T, DP> k(sk, key, lane);
     Vec8<T> kf[2][2][NS];
-    const auto read = [&](int at, int kk) {
+    const auto read = [&](int to, int kk) {
 #pragma unroll
       for (int b = 0; b < NS; ++b)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) kf[at][x][b] = *(const Vec8<T>*)(k.at + b * 32 * DP + (k.c ^ (2 * (kk + x))) * 8);
+        for (int x = 0; x < 2; ++x) kf[to][x][b] = at.rows(sk, key + b * 32, kk + x);
     };
     read(0, 0);
 #pragma unroll
@@ -448,15 +473,21 @@ struct Rows {
     // The weights of 16 keys are computed, and the values of 16 keys read, between the
     // products of the 16 keys before.
     Vec8<T> vf[2][N];
+    const auto values = [&](uint32_t from, int d) {
+      if constexpr (N == DP / 32)
+        return at.columns(sv, from, d);
+      else
+        return column_frag<T, DP>(sv, from, d0 + d, lane);
+    };
 #pragma unroll
-    for (int d = 0; d < N; ++d) vf[0][d] = column_frag<T, DP>(sv, key, d0 + d, lane);
+    for (int d = 0; d < N; ++d) vf[0][d] = values(key, d);
 #pragma unroll
     for (int i = 0; i < 8; ++i) weigh(0, i);
 #pragma unroll
     for (int kb = 0; kb < 2 * NS; ++kb) {
       if (kb + 1 < 2 * NS) {
 #pragma unroll
-        for (int d = 0; d < N; ++d) vf[kb + 1 & 1][d] = column_frag<T, DP>(sv, key + kb * 16 + 16, d0 + d, lane);
+        for (int d = 0; d < N; ++d) vf[kb + 1 & 1][d] = values(key + kb * 16 + 16, d);
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -501,6 +532,7 @@ __device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& s
   Rows<T, DP, N> r;
   clear(r.o);
   r.d0 = d0;
+  r.at.start(lane);
   r.m = -INFINITY;
   r.l = 0.f;
   {
@@ -544,7 +576,7 @@ __device__ __forceinline__ bool prompt_rows(const PromptParams& p, const Span& s
       r.template step<2>(lane, sk, sv, 0, c, mask, (int32_t)(seen - j0));
     } else {
 #pragma unroll 1
-      for (uint32_t x = 0; x < kTile; x += 32) r.template step<1>(fresh_lane(), sk, sv, x, c, mask, (int32_t)(seen - j0 - x));
+      for (uint32_t x = 0; x < kTile; x += 32) r.template step<1>(lane, sk, sv, x, c, mask, (int32_t)(seen - j0 - x));
     }
     if constexpr (ODD) {
       if (odd)
@@ -849,46 +881,51 @@ __device__ __forceinline__ bool any_odd(const f32x16 (&o)[N]) {
   return found;
 }
 
-// 32 rows of one or two tiles times held rows (B): the fragments of two steps are read while the
-// two before are multiplied.
-template <typename T, int DP, bool BOTH>
-__device__ __forceinline__ void two_products(const T* sa, const T* sb, uint32_t row, const Vec8<T>* a, const Vec8<T>* b, f32x16& ra,
-                                             f32x16& rb) {
-  const uint32_t lane = fresh_lane();
-  const RowFrags<T, DP> fa(sa, row, lane), fb(sb, row, lane);
+// 32 rows of one or two tiles times held rows (B): the fragments of AHEAD steps are read while those
+// before are multiplied.
+template <typename T, int DP, bool BOTH, int AHEAD>
+__device__ __forceinline__ void two_products(const Parts<T, DP>& at, const T* sa, const T* sb, uint32_t row, const Vec8<T>* a,
+                                             const Vec8<T>* b, f32x16& ra, f32x16& rb) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) ra[i] = rb[i] = 0.f;
-  Vec8<T> f[2][2][2];
+  Vec8<T> f[2][AHEAD][2];
   const auto read = [&](int kk) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      f[kk / 2 & 1][x][0] = fa(kk + x);
-      if constexpr (BOTH) f[kk / 2 & 1][x][1] = fb(kk + x);
+    for (int x = 0; x < AHEAD; ++x) {
+      f[kk / AHEAD & 1][x][0] = at.rows(sa, row, kk + x);
+      if constexpr (BOTH) f[kk / AHEAD & 1][x][1] = at.rows(sb, row, kk + x);
     }
   };
   read(0);
 #pragma unroll
-  for (int kk = 0; kk < DP / 16; kk += 2) {
-    if (kk + 2 < DP / 16) read(kk + 2);
+  for (int kk = 0; kk < DP / 16; kk += AHEAD) {
+    if (kk + AHEAD < DP / 16) read(kk + AHEAD);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      ra = mfma(f[kk / 2 & 1][x][0], a[kk + x], ra);
-      if constexpr (BOTH) rb = mfma(f[kk / 2 & 1][x][1], b[kk + x], rb);
+    for (int x = 0; x < AHEAD; ++x) {
+      ra = mfma(f[kk / AHEAD & 1][x][0], a[kk + x], ra);
+      if constexpr (BOTH) rb = mfma(f[kk / AHEAD & 1][x][1], b[kk + x], rb);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
 }
 // N blocks of columns, from block d0 on, of 32 rows of a tile times the lane's weights, rounded to T.
 template <typename T, int DP, int N>
-__device__ __forceinline__ void add_columns(f32x16* o, const T* s, uint32_t row, int d0, const f32x16& w, uint32_t lane) {
+__device__ __forceinline__ void add_columns(const Parts<T, DP>& at, f32x16* o, const T* s, uint32_t row, int d0, const f32x16& w,
+                                            uint32_t lane) {
   Vec8<T> u[2], f[2][N];
+  const auto columns = [&](uint32_t from, int d) {
+    if constexpr (N == DP / 32)
+      return at.columns(s, from, d);
+    else
+      return column_frag<T, DP>(s, from, d0 + d, lane);
+  };
 #pragma unroll
-  for (int d = 0; d < N; ++d) f[0][d] = column_frag<T, DP>(s, row, d0 + d, lane);
+  for (int d = 0; d < N; ++d) f[0][d] = columns(row, d);
 #pragma unroll
   for (int i = 0; i < 16; ++i) u[i / 8][i % 8] = (T)w[i];
 #pragma unroll
-  for (int d = 0; d < N; ++d) f[1][d] = column_frag<T, DP>(s, row + 16, d0 + d, lane);
+  for (int d = 0; d < N; ++d) f[1][d] = columns(row + 16, d);
 #pragma unroll
   for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -933,13 +970,15 @@ __device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& s
   const T* op = (const T*)a.dout + (int64_t)(sp.first + there) * a.dout_stride[0] + (int64_t)hq * a.dout_stride[1];
 #pragma unroll
   for (int i = 0; i < DP / 16; ++i) {
-    const uint32_t at = i * 16 + 8 * half;
-    q[i] = *(const Vec8<T>*)(at < a.dim ? qp + at : (const T*)g_zeros);
-    dout[i] = *(const Vec8<T>*)(at < a.dim ? op + at : (const T*)g_zeros);
+    const uint32_t c0 = i * 16 + 8 * half;
+    q[i] = *(const Vec8<T>*)(c0 < a.dim ? qp + c0 : (const T*)g_zeros);
+    dout[i] = *(const Vec8<T>*)(c0 < a.dim ? op + c0 : (const T*)g_zeros);
   }
   const float lse = p.lse[p.stat(hq, sp.first + there)], delta = p.delta[p.stat(hq, sp.first + there)];
   f32x16 o[N];
   clear(o);
+  Parts<T, DP> at;
+  at.start(lane);
   for (uint32_t t = 0; t < tiles; ++t) {
     const uint32_t j0 = t * kTile;
     T *sk = s_kv + (t & 1) * 2 * L::N, *sv = sk + L::N;
@@ -965,25 +1004,25 @@ __device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& s
 #pragma unroll 1
       for (uint32_t x = 0; x < kTile; x += 32) {
         f32x16 s, dp;
-        two_products<T, DP, true>(sk, sv, x, q, dout, s, dp);
+        two_products<T, DP, true, 1>(at, sk, sv, x, q, dout, s, dp);
         if (mask)
           weigh(x, s, dp, true);
         else
           weigh(x, s, dp, false);
-        add_columns<T, DP, N>(o, sk, x, 0, s, lane);
+        add_columns<T, DP, N>(at, o, sk, x, 0, s, lane);
       }
     } else {
       f32x16 s[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         f32x16 dp;
-        two_products<T, DP, true>(sk, sv, x * 32, q, dout, s[x], dp);
+        two_products<T, DP, true, 1>(at, sk, sv, x * 32, q, dout, s[x], dp);
         weigh(x * 32, s[x], dp, true);
       }
       const bool odd = clear_if_odd<T, L::N>(sk, causal && j0 + kTile > r0 + 1, 256);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        add_columns<T, DP, N>(o, sk, x * 32, d0, s[x], lane);
+        add_columns<T, DP, N>(at, o, sk, x * 32, d0, s[x], lane);
         if (odd)
           add_odd<T, N>(o, ld.a, ld.a_stride, j0 + x * 32, sp.n, d0 * 32, a.dim, half, true,
                         [&](uint32_t j) { return j < seen; });
@@ -1079,6 +1118,8 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
   }
   f32x16 o[N];
   clear(o);
+  Parts<T, DP> at;
+  at.start(lane);
   uint32_t buffer = 0;
   for (uint32_t g = g0; g < g1; ++g)
     for (uint32_t t = first; t < tiles; ++t, buffer ^= 1) {
@@ -1093,7 +1134,7 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
       if (!ODD && ((causal && i0 + 32 <= w0) || i0 >= sp.n)) continue;  // no row of the wave's sees a key of its
       const bool mask = (causal && i0 < w0 + 31) || i0 + 32 > sp.n;
       f32x16 s, dp;
-      two_products<T, DP, !DV>(sq, so, x0, k, v, s, dp);
+      two_products<T, DP, !DV, 2>(at, sq, so, x0, k, v, s, dp);
       const auto weigh = [&](bool masked) {
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
@@ -1117,7 +1158,7 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
         weigh(false);
       bool odd = false;
       if constexpr (ODD) odd = clear_if_odd<T, L::N>(added, causal && t * kTile + 1 < k0 + kKeys, 256);
-      add_columns<T, DP, N>(o, added, x0, d0, s, lane);
+      add_columns<T, DP, N>(at, o, added, x0, d0, s, lane);
       if constexpr (ODD) {
         if (odd) {
           const uint32_t hq = h * p.group + g;
