@@ -27,9 +27,9 @@ with their epilogue, attention over whole prompts.
 
 Shapes.  q [T, Hq, D], k and v [T, Hkv, D]: the new tokens of all sequences one
 behind the other, sequence b's at starts[b] .. starts[b + 1] (starts=None: the
-same number each; for prompts one sequence).  Caches [pages, page, Hkv, D] in any memory order whose last
-dimension is contiguous (pages kept head by head are a transposed view), page a
-power of two.  page_table [B, max_pages] int32; lens [B] int32 counts a
+same number each; for prompts one sequence).  Caches [pages, page, Hkv, D] in any
+memory order whose last dimension is contiguous (pages kept head by head are a
+transposed view), page a power of two.  page_table [B, max_pages] int32; lens [B] int32 counts a
 sequence's own keys with its new ones, the shared prefix apart.  Types: bfloat16,
 float16, float32.
 
@@ -38,9 +38,10 @@ api.GtsError for what the library refuses.  Work is enqueued on `stream`
 (default: the current one) and not waited for; outputs and scratch are
 allocated on it, and tensors handed to another stream than the current one are
 kept from reuse until it has run (record_stream).  The caller orders the
-streams.  Every call may be captured into a graph.  For autograd the caller's
-tensors that a call writes (out, q_out, lse, scratch, preact, mean, rstd, the
-caches) are modified in place.
+streams.  Every call may be captured into a graph (a backward pass too, where no
+eager autograd graph of the same leaves lives meanwhile: that is torch's rule).  For
+autograd the caller's tensors that a call writes (out, q_out, lse, scratch, preact,
+mean, rstd, the caches) are modified in place.
 """
 from __future__ import annotations
 
@@ -645,15 +646,21 @@ def _stats(t, name, rows, like):
         raise ValueError(f"{name} is a contiguous float32 [{rows}] beside x")
 
 
-def _flat(x, name="x"):
-    """x [..., dim] as rows [n, dim] (a view where its layout has one) and its leading shape."""
+def _flat(x, name="x", stream=None):
+    """x [..., dim] as rows [n, dim]: a view where its layout has one, else a copy on the
+    current stream, which a call on another one does not wait for and so refuses."""
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{name} is a tensor: got {type(x).__name__}")
     if x.dim() == 2:
         return x
     if x.dim() < 1:
         raise ValueError(f"{name} has no dimensions")
-    return x.reshape(-1, x.shape[-1]) if x.numel() else x.new_empty((math.prod(x.shape[:-1]), x.shape[-1]))
+    if not x.numel():
+        return x.new_empty((math.prod(x.shape[:-1]), x.shape[-1]))
+    flat = x.reshape(-1, x.shape[-1])
+    if stream is not None and flat.data_ptr() != x.data_ptr():
+        raise ValueError(f"{name}: its rows are not evenly apart, so that it would be copied on another stream")
+    return flat
 
 
 def _norm(x, weight, bias, eps, center, out, mean, rstd, stream):
@@ -707,7 +714,7 @@ def layer_norm(x, weight=None, bias=None, *, eps=1e-5, center=True, out=None, me
     bias by reverse mode (out, mean and rstd are then refused)."""
     _no_tangent_of("a tensor of the norm", x, weight, bias)
     shape = x.shape if isinstance(x, torch.Tensor) else None
-    flat = _flat(x)
+    flat = _flat(x, "x", stream)
     if _wants_gradient(x, weight, bias):
         _refuse(out is None and mean is None and rstd is None, "out, mean and rstd are refused: an input requires a gradient")
         y = _Norm.apply(flat, weight, bias, eps, center, None, None, stream)
@@ -748,9 +755,9 @@ def layer_norm_backward(dy, x, weight, rstd, mean=None, *, bias=False, stream=No
     dweight is None without a weight, dbias unless `bias` asks for it."""
     _no_gradient("a tensor of the norm's gradient", dy, x, weight, rstd, mean)
     _refuse(isinstance(rstd, torch.Tensor), "rstd is a float32 tensor, one value a row")
-    flat = _flat(x)
+    flat = _flat(x, "x", stream)
     _refuse(isinstance(dy, torch.Tensor) and dy.shape == x.shape, "dy has the shape of x")
-    dx, dw, db = _norm_backward(_flat(dy, "dy"), flat, weight, rstd, mean, True, weight is not None, bias, stream)
+    dx, dw, db = _norm_backward(_flat(dy, "dy", stream), flat, weight, rstd, mean, True, weight is not None, bias, stream)
     return dx.view(x.shape), dw, db
 
 
@@ -829,13 +836,13 @@ def linear(x, weight, bias=None, *, activation=None, gate=None, residual=None, o
     bias, gate and residual by reverse mode (out and preact are then refused)."""
     act = _activation(activation)
     _no_tangent_of("a tensor of the product", x, weight, bias, gate, residual)
-    flat = _flat(x)
+    flat = _flat(x, "x", stream)
     _refuse(isinstance(weight, torch.Tensor) and weight.dim() == 2, "weight is a matrix [N, K]")
     shape = (*x.shape[:-1], weight.shape[0])
     for t, name in ((gate, "gate"), (residual, "residual"), (out, "out"), (preact, "preact")):
         if t is not None:
             _refuse(isinstance(t, torch.Tensor) and t.shape == shape, f"{name} is a tensor {shape}")
-    g, r = (None if t is None else _flat(t) for t in (gate, residual))
+    g, r = (None if t is None else _flat(t, "gate or residual", stream) for t in (gate, residual))
     if _wants_gradient(x, weight, bias, gate, residual):
         _refuse(out is None and preact is None, "out and preact are refused: an input requires a gradient")
         y = _Linear.apply(flat, weight, bias, act, g, r, stream)
@@ -888,14 +895,14 @@ def linear_backward(dy, x, weight, *, activation=None, preact=None, gate=None, b
     What is multiplied (dy times the gate and the activation's slope) is in dy's type."""
     act = _activation(activation)
     _no_gradient("a tensor of the product's gradient", dy, x, weight, preact, gate)
-    flat = _flat(x)
+    flat = _flat(x, "x", stream)
     _refuse(isinstance(weight, torch.Tensor) and weight.dim() == 2, "weight is a matrix [N, K]")
     shape = (*x.shape[:-1], weight.shape[0])
     for t, name in ((dy, "dy"), (preact, "preact"), (gate, "gate")):
         if t is not None or name == "dy":
             _refuse(isinstance(t, torch.Tensor) and t.shape == shape, f"{name} is a tensor {shape}")
-    z, g = (None if t is None else _flat(t) for t in (preact, gate))
-    dx, dw, db, dg = _linear_backward(_flat(dy), flat, weight, act, z, g, True, True, bias, gate is not None, stream)
+    z, g = (None if t is None else _flat(t, "preact or gate", stream) for t in (preact, gate))
+    dx, dw, db, dg = _linear_backward(_flat(dy, "dy", stream), flat, weight, act, z, g, True, True, bias, gate is not None, stream)
     return dx.view(x.shape), dw, db, None if dg is None else dg.view(shape)
 
 
@@ -963,8 +970,8 @@ def prompt_attention(q, k, v, starts=None, *, causal=True, scale=None, out=None,
     sequence b at starts[b] .. starts[b + 1] (int32 [B + 1], ascending; None: one
     sequence).  A token sees the keys of its sequence, with `causal` those up to its own.
     Query head h reads key-value head h // (Hq / Hkv); scale defaults to D ** -0.5.  A token
-    outside every sequence gives zeros and a log-sum of -inf.  out and lse (float32
-    [T, Hq], natural logarithm) receive the results if given.  Softmax weights are rounded
+    outside every sequence gives zeros and a log-sum of -inf.  out (which shares no memory
+    with the inputs) and lse (float32 [T, Hq], natural logarithm) receive the results if given.  Softmax weights are rounded
     to the tensors' type for the product with the values.  Differentiable once in q, k and
     v by reverse mode (out and lse are then refused)."""
     _no_tangent_of("a tensor of the attention", q, k, v)

@@ -776,6 +776,65 @@ def test_layer_on_another_stream():
             assert torch.equal(a, c)
 
 
+def test_copies_are_not_made_on_another_stream():
+    x = torch.zeros(4, 3, 16, device="cuda").transpose(0, 1)
+    w = torch.zeros(16, 16, device="cuda")
+    side = torch.cuda.Stream()
+    assert ops.layer_norm(x).shape == x.shape and ops.linear(x, w).shape == x.shape
+    rstd = torch.ones(12, device="cuda")
+    for f in (lambda: ops.layer_norm(x, stream=side), lambda: ops.linear(x, w, stream=side),
+              lambda: ops.linear(x.contiguous(), w, gate=x, stream=side), lambda: ops.linear_backward(x, x, w, stream=side),
+              lambda: ops.layer_norm_backward(x, x, None, rstd, stream=side)):
+        with pytest.raises(ValueError, match="copied"):
+            f()
+
+
+def test_layer_offsets_past_32_bits():
+    """Tensors of more than 2^31 values: their last rows are those of a small call."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rows, dim = 530_000, 4096  # 2.17e9 values
+    x = torch.zeros(rows, dim, device="cuda", dtype=BF)
+    last = slice(rows - 300, rows)
+    x[last] = torch.randn(300, dim, generator=g, device="cuda").to(BF)
+    w, v = torch.randn(dim, generator=g, device="cuda").to(BF), torch.randn(64, dim, generator=g, device="cuda").to(BF)
+    small = x[last].clone()
+    rstd, srstd = torch.empty(rows, device="cuda"), torch.empty(300, device="cuda")
+    y = ops.layer_norm(x, w, center=False, rstd=rstd)
+    assert torch.equal(y[last], ops.layer_norm(small, w, center=False, rstd=srstd)) and torch.equal(rstd[last], srstd)
+    assert not y[:100].any()
+    dx, dw, _ = ops.layer_norm_backward(x, x, w, rstd)
+    sdx, sdw, _ = ops.layer_norm_backward(small, small, w, srstd)
+    assert torch.equal(dx[last], sdx) and not dx[:100].any()
+    del y, dx
+    z = ops.linear(x, v)
+    ref, size = small.double() @ v.double().T.contiguous(), small.double().abs() @ v.double().abs().T.contiguous()
+    assert ((z[last].double() - ref).abs() <= R.rounded(ref, 2 * (dim + 4) * R.E * size, BF)).all() and not z[:100].any()
+    dz = torch.zeros(rows, 64, device="cuda", dtype=BF)
+    dz[last] = torch.randn(300, 64, generator=g, device="cuda").to(BF)
+    dx, dv, db, _ = ops.linear_backward(dz, x, v, bias=True)
+    d = dz[last].double()
+    ref, size = d @ v.double(), d.abs() @ v.double().abs()
+    assert ((dx[last].double() - ref).abs() <= R.rounded(ref, 2 * 68 * R.E * size, BF)).all() and not dx[:100].any()
+    ref, size = d.T.contiguous() @ small.double(), d.abs().T.contiguous() @ small.double().abs()
+    assert ((dv.double() - ref).abs() <= R.rounded(ref, 2 * 304 * R.E * size, BF)).all()
+    del x, z, dx, dz
+    T, H, D = 135_000, 125, 128  # 2.16e9 values
+    q = torch.zeros(T, H, D, device="cuda", dtype=BF)
+    k = torch.zeros(T, 1, D, device="cuda", dtype=BF)
+    starts = torch.arange(0, T + 1, 100, device="cuda", dtype=torch.int32)
+    last = slice(T - 100, T)
+    q[last], k[last] = torch.randn(100, H, D, generator=g, device="cuda").to(BF), torch.randn(100, 1, D, generator=g, device="cuda").to(BF)
+    lse, slse = torch.empty(T, H, device="cuda"), torch.empty(100, H, device="cuda")
+    sq, sk = q[last].clone(), k[last].clone()
+    o, so = ops.prompt_attention(q, k, k, starts, lse=lse), ops.prompt_attention(sq, sk, sk, lse=slse)
+    assert torch.equal(o[last], so) and torch.equal(lse[last], slse) and not o[:100].any()
+    got, want = ops.prompt_attention_backward(q, q, k, k, o, lse, starts), ops.prompt_attention_backward(sq, sq, sk, sk, so, slse)
+    assert torch.equal(got[0][last], want[0])
+    ref, errs = R.prompt_gradient(*d64(sq, sq, sk, sk, so, slse), None, True, None, BF)
+    for a, r, e, name in zip(got[1:], ref[1:], errs[1:], ("dk", "dv")):
+        close(a[last], r, e, BF, name)  # the parts of the sum over heads differ with the number of tokens
+
+
 def test_layer_refusals():
     """Every refused call raises and launches nothing."""
     x, w = torch.zeros(4, 16, device="cuda", dtype=BF), torch.zeros(8, 16, device="cuda", dtype=BF)

@@ -105,13 +105,14 @@ def test_norm_refusals():
     name = "gts_layer_norm_backward"
     refused(name, None, ARG)
     for code, kw in ((ARG, dict(dtype=3)), (RANGE, dict(dim=0)), (ARG, dict(flags=2)), (ARG, dict(x=None)), (ARG, dict(dy=None)),
-                     (ARG, dict(rstd=None)), (ARG, dict(mean=None)), (SCRATCH, dict(scratch=None)), (ARG, dict(scratch=FAKE + 4))):
+                     (ARG, dict(rstd=None)), (ARG, dict(mean=None)), (ARG, dict(scratch=FAKE + 4))):
         refused(name, norm_grad(**kw), code)
     refused(name, norm_grad(dx=None, dweight=None), 0)
     refused(name, norm_grad(rows=0, dweight=None), 0)
     need = scratch_of("gts_layer_norm_backward_scratch", 2, 8)
     if need:
         refused(name, norm_grad(scratch_bytes=need - 1), SCRATCH, str(need))
+        refused(name, norm_grad(scratch=None), SCRATCH)
     assert ops.lib().gts_layer_norm_backward_scratch(2, 8, None) == ARG
     assert scratch_of("gts_layer_norm_backward_scratch", 2, 0) == RANGE
 
