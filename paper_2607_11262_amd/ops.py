@@ -681,14 +681,25 @@ def _norm(x, weight, bias, eps, center, out, mean, rstd, stream):
     return y
 
 
+def _keep(stream, like, *tensors):
+    """Tensors that a call on `stream` allocates there, and its backward pass reads on the current one."""
+    if stream is not None:
+        current = torch.cuda.current_stream(like.device)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(current)
+
+
 class _Norm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, eps, center, mean, rstd, stream):
-        # statistics that the caller gave may be written again before the backward pass
-        own_mean = x.new_empty(x.shape[0], dtype=torch.float32) if center else None
-        own_rstd = x.new_empty(x.shape[0], dtype=torch.float32)
-        y = _norm(x, weight, bias, eps, center, None, own_mean, own_rstd, stream)
-        ctx.save_for_backward(x, weight, own_mean, own_rstd)
+    def forward(ctx, x, weight, bias, eps, center, stream):
+        _data(x, "x", 2)
+        with _on(stream, x):
+            mean = x.new_empty(x.shape[0], dtype=torch.float32) if center else None
+            rstd = x.new_empty(x.shape[0], dtype=torch.float32)
+        y = _norm(x, weight, bias, eps, center, None, mean, rstd, stream)
+        _keep(stream, x, mean, rstd)
+        ctx.save_for_backward(x, weight, mean, rstd)
         ctx.bias = bias is not None
         return y
 
@@ -699,7 +710,7 @@ class _Norm(torch.autograd.Function):
         need = ctx.needs_input_grad
         dx, dw, db = _norm_backward(_rows(dy), x, weight, rstd, mean, need[0], weight is not None and need[1],
                                     ctx.bias and need[2], None)
-        return dx, dw, db, None, None, None, None, None
+        return dx, dw, db, None, None, None
 
 
 def _rows(t):
@@ -717,7 +728,7 @@ def layer_norm(x, weight=None, bias=None, *, eps=1e-5, center=True, out=None, me
     flat = _flat(x, "x", stream)
     if _wants_gradient(x, weight, bias):
         _refuse(out is None and mean is None and rstd is None, "out, mean and rstd are refused: an input requires a gradient")
-        y = _Norm.apply(flat, weight, bias, eps, center, None, None, stream)
+        y = _Norm.apply(flat, weight, bias, eps, center, stream)
     else:
         _no_gradient("out of the norm", out, mean, rstd)
         if out is not None:
@@ -799,8 +810,11 @@ class _Linear(torch.autograd.Function):
     def forward(ctx, x, weight, bias, act, gate, residual, stream):
         preact = None
         if (act or gate is not None) and any(t is not None and t.requires_grad for t in (x, weight, bias, gate)):
-            preact = x.new_empty((x.shape[0], weight.shape[0]))
+            _data(x, "x", 2)
+            with _on(stream, x):
+                preact = x.new_empty((x.shape[0], weight.shape[0]))
         y = _linear(x, weight, bias, act, gate, residual, None, preact, stream)
+        _keep(stream, x, preact)
         ctx.save_for_backward(x, weight, preact, gate)
         ctx.act, ctx.bias, ctx.residual = act, bias is not None, residual is not None
         return y
@@ -951,8 +965,11 @@ def _prompt(q, k, v, starts, causal, scale, out, lse, stream):
 class _Prompt(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, starts, causal, scale, stream):
-        lse = q.new_empty(q.shape[:2], dtype=torch.float32)
+        _data(q, "q", 3)
+        with _on(stream, q):
+            lse = q.new_empty(q.shape[:2], dtype=torch.float32)
         o = _prompt(q, k, v, starts, causal, scale, None, lse, stream)
+        _keep(stream, q, o, lse)
         ctx.save_for_backward(q, k, v, o, lse, starts)
         ctx.causal, ctx.scale = causal, scale
         return o

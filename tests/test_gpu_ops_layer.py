@@ -776,6 +776,34 @@ def test_layer_on_another_stream():
             assert torch.equal(a, c)
 
 
+@pytest.mark.parametrize("op", ["norm", "linear", "attention"])
+def test_what_a_backward_pass_needs_is_of_the_calls_stream(op):
+    """What a forward pass on a side stream keeps for its gradient is not in memory that work of the
+    current stream still writes."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rows = 1 << 15
+    x = torch.randn(rows, 64, generator=g, device="cuda").to(BF).requires_grad_()
+    w = torch.randn(64, 64, generator=g, device="cuda").to(BF).requires_grad_()
+    kept = dict(norm=[(rows,), (rows,)], linear=[(rows, 32)], attention=[(rows,)])[op]  # float32 of the same bytes
+    call = dict(norm=lambda **kw: ops.layer_norm(x, **kw), linear=lambda **kw: ops.linear(x, w, activation="silu", **kw),
+                attention=lambda **kw: ops.prompt_attention(x.view(rows, 1, 64), x.view(rows, 1, 64), x.view(rows, 1, 64),
+                                                            starts, **kw))[op]
+    starts = torch.arange(0, rows + 1, 64, dtype=torch.int32, device="cuda")
+    want, = torch.autograd.grad(call().float().square().sum(), x)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    held = [torch.empty(shape, device="cuda") for shape in kept]
+    torch.cuda._sleep(50_000_000)  # some 20 ms
+    for t in held:
+        t.fill_(3.0)
+    del held, t  # their memory is free for the current stream, which has yet to write it
+    y = call(stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    got, = torch.autograd.grad(y.float().square().sum(), x)
+    assert torch.equal(got, want)
+
+
 def test_copies_are_not_made_on_another_stream():
     x = torch.zeros(4, 3, 16, device="cuda").transpose(0, 1)
     w = torch.zeros(16, 16, device="cuda")

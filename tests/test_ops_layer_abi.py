@@ -166,5 +166,14 @@ def test_prompt_refusals(name, args):
         assert scratch_of("gts_prompt_attention_backward_scratch", 1, 4, 4, 3, 16) == RANGE
 
 
+def test_host_tensors_are_refused_with_a_gradient_too():
+    torch = pytest.importorskip("torch")
+    x = torch.zeros(4, 16, requires_grad=True)
+    q = x.view(4, 1, 16)
+    for f in (lambda: ops.layer_norm(x), lambda: ops.linear(x, x, activation="relu"), lambda: ops.prompt_attention(q, q, q)):
+        with pytest.raises(ValueError, match="not on the GPU"):
+            f()
+
+
 def test_offsets_of_packing_are_native():
     assert struct.calcsize("=Q") == 8 and struct.calcsize("=I") == 4
