@@ -8,7 +8,7 @@
 // A row belongs to a team: 16 lanes, a wave, four or eight, the fewest whose registers hold it
 // (16 values a lane, or 32), so x is read once and the variance is of the differences, not a
 // difference of sums.  Longer rows are read again from memory for each pass over them.
-// Bound by HBM when large (32768 rows of 4096 in bfloat16: 4.9 TB/s forward, 4.8 backward) and by
+// Bound by HBM when large (32768 rows of 4096 in bfloat16: 4.9 TB/s forward, 5.1 backward) and by
 // the launch when small.
 #include "gts_ops.h"
 #include "gts_tile.h"
