@@ -85,36 +85,37 @@ __device__ __forceinline__ void finish(const gts_matmul_args& a, uint32_t m, uin
 
 // ---- the general kernel ----------------------------------------------------------------
 // Any type, size, stride and alignment.  Four waves take 32 R x 32 R each of a tile of 64 R x
-// 64 R; 32 places of the sum at a time go through registers to LDS, the next while these are
-// multiplied.  The smaller tile is for small results, where more workgroups a CU hide the loads
-// (1021 x 1000 x 777 in 32 bits: 51 us in the larger, 26 in this).  In 32 bits bound by matrix issue, a
-// sixteenth of the 16-bit rate (4096 x 4096 x 4096 1128 us, 122 TFLOP/s of 139 that a library product
-// reaches); in 16 bits by the way through registers (4095 x 4097 x 4099 375 us, 367 TFLOP/s).
+// 64 R; 32 places of the sum at a time go through registers to LDS, their loads two stages ahead of
+// the products.  The smaller tile is for small results, where more workgroups a CU hide the loads
+// (1021 x 1000 x 777 in 32 bits: 51 us in the larger, 25 in this).  In 32 bits bound by matrix issue, a
+// sixteenth of the 16-bit rate (4096 x 4096 x 4096 1022 us, 134 TFLOP/s; a library product 1033; with
+// loads one stage ahead, in one loop with those of the edges, 1140); in 16 bits by the way through
+// registers (4095 x 4097 x 4099 355 us, 387 TFLOP/s).
 constexpr uint32_t kTileK = 32;
 
-// LDS of an operand's 64 R rows (or columns) and 32 places: rows of 8 values more than they
+// LDS of an operand's 64 R rows (or columns) and 32 places: rows of 8 values (16 bytes) more than they
 // hold, so that reads of neighbouring rows meet other banks.
-template <bool COLUMNS, int R>
-constexpr uint32_t kPitch = COLUMNS ? 64 * R + 8 : kTileK + 8;
+template <typename T, bool COLUMNS, int R>
+constexpr uint32_t kPitch = COLUMNS ? 64 * R + 8 : kTileK + 16 / sizeof(T);
 template <int R>
 constexpr uint32_t kTileSize = 64 * R * (kTileK + 8);  // the larger of both
 
 template <typename T, bool COLUMNS, int R>
 struct Staged {
   Vec8<T> x[R];
-  // Rows r0 .. + 64 R - 1 of `rows`, places k0 .. + 31 of those below `k_end`.  Without a branch
-  // where all places are there, so that nothing waits for the loads: rows past the end are then
-  // the last again (what they give is not stored).
-  __device__ __forceinline__ void load(const T* p, int64_t stride, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t k_end) {
-    if (k0 + kTileK <= k_end && (!COLUMNS || r0 + 64 * R <= rows)) {
+  // Rows r0 .. + 64 R - 1 of `rows`, places k0 .. + 31, which are all there: without a branch, so that
+  // nothing waits for the loads.  Rows past the end are the last again (what they give is not stored).
+  __device__ __forceinline__ void load_whole(const T* p, int64_t stride, uint32_t r0, uint32_t rows, uint32_t k0) {
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const uint32_t id = threadIdx.x + 256 * i, r = r0 + id / 4;
-        x[i] = COLUMNS ? load_any(p + (int64_t)(k0 + id / (8 * R)) * stride + r0 + id % (8 * R) * 8)
-                       : load_any(p + (int64_t)(r < rows ? r : rows - 1) * stride + k0 + id % 4 * 8);
-      }
-      return;
+    for (int i = 0; i < R; ++i) {
+      const uint32_t id = threadIdx.x + 256 * i, r = r0 + id / 4;
+      x[i] = COLUMNS ? load_any(p + (int64_t)(k0 + id / (8 * R)) * stride + r0 + id % (8 * R) * 8)
+                     : load_any(p + (int64_t)(r < rows ? r : rows - 1) * stride + k0 + id % 4 * 8);
     }
+  }
+  // The same of the places below `k_end`, or columns of which some may be missing.
+  __device__ __forceinline__ void load(const T* p, int64_t stride, uint32_t r0, uint32_t rows, uint32_t k0, uint32_t k_end) {
+    if (k0 + kTileK <= k_end && (!COLUMNS || r0 + 64 * R <= rows)) return load_whole(p, stride, r0, rows, k0);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const uint32_t id = threadIdx.x + 256 * i;
@@ -136,14 +137,14 @@ struct Staged {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const uint32_t id = threadIdx.x + 256 * i;
-      write8(s + (COLUMNS ? id / (8 * R) * kPitch<true, R> + id % (8 * R) * 8 : id / 4 * kPitch<false, R> + id % 4 * 8), x[i]);
+      write8(s + (COLUMNS ? id / (8 * R) * kPitch<T, true, R> + id % (8 * R) * 8 : id / 4 * kPitch<T, false, R> + id % 4 * 8), x[i]);
     }
   }
   static __device__ __forceinline__ Vec8<T> frag(const T* s, uint32_t row, uint32_t k, uint32_t lane) {
     if constexpr (COLUMNS)
-      return frag_columns<false>(s, kPitch<true, R>, k, row, lane);
+      return frag_columns<false>(s, kPitch<T, true, R>, k, row, lane);
     else
-      return frag_rows(s, kPitch<false, R>, row, k, lane);
+      return frag_rows(s, kPitch<T, false, R>, row, k, lane);
   }
 };
 
@@ -165,22 +166,18 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulParams p) {
   for (int i = 0; i < R * R; ++i)
 #pragma unroll
     for (int j = 0; j < 16; ++j) acc[i / R][i % R][j] = 0.f;
-  SA sa;
-  SB sb;
-  if (k0 < k1) {
-    sa.load((const T*)a.a, a.a_stride, m0, a.m, k0, k1);
-    sb.load((const T*)a.b, a.b_stride, n0, a.n, k0, k1);
-    sa.store(s_a[0]);
-    sb.store(s_b[0]);
-  }
-  __syncthreads();
-  uint32_t at = 0;
-  for (uint64_t k = k0; k < k1; k += kTileK, at ^= 1) {
-    const bool more = k + kTileK < k1;
-    if (more) {
-      sa.load((const T*)a.a, a.a_stride, m0, a.m, (uint32_t)k + kTileK, k1);
-      sb.load((const T*)a.b, a.b_stride, n0, a.n, (uint32_t)k + kTileK, k1);
-    }
+  SA sa[2];
+  SB sb[2];
+  const uint32_t stages = (k1 - k0 + kTileK - 1) / kTileK;
+  const auto load = [&](int set, uint32_t t) {
+    sa[set].load((const T*)a.a, a.a_stride, m0, a.m, k0 + t * kTileK, k1);
+    sb[set].load((const T*)a.b, a.b_stride, n0, a.n, k0 + t * kTileK, k1);
+  };
+  const auto store = [&](int set) {
+    sa[set].store(s_a[set]);
+    sb[set].store(s_b[set]);
+  };
+  const auto multiply = [&](int at) {
 #pragma unroll
     for (uint32_t kk = 0; kk < kTileK; kk += 16) {
       Vec8<T> fa[R], fb[R];
@@ -194,11 +191,32 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulParams p) {
 #pragma unroll
         for (int j = 0; j < R; ++j) acc[i][j] = mfma(fa[i], fb[j], acc[i][j]);
     }
-    if (more) {
-      sa.store(s_a[at ^ 1]);
-      sb.store(s_b[at ^ 1]);
+  };
+  if (stages > 0) load(0, 0);
+  if (stages > 1) load(1, 1);
+  if (stages > 0) store(0);
+  __syncthreads();
+  uint32_t t = 0;
+  if ((!AC || m0 + 64 * R <= a.m) && (!BC || n0 + 64 * R <= a.n)) {
+    for (; t + 4 < stages; t += 2) {  // whole stages, whose loads are without a branch
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        sa[x].load_whole((const T*)a.a, a.a_stride, m0, a.m, k0 + (t + 2 + x) * kTileK);
+        sb[x].load_whole((const T*)a.b, a.b_stride, n0, a.n, k0 + (t + 2 + x) * kTileK);
+        multiply(x);
+        store(x ^ 1);
+        __syncthreads();
+      }
     }
-    __syncthreads();
+  }
+  for (; t < stages; t += 2) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      if (t + 2 + x < stages) load(x, t + 2 + x);
+      if (t + x < stages) multiply(x);
+      if (t + 1 + x < stages) store(x ^ 1);
+      __syncthreads();
+    }
   }
   float* part = (float*)a.scratch + (uint64_t)split * a.m * a.n;
 #pragma unroll
