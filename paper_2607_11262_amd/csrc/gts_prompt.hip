@@ -67,7 +67,9 @@ __device__ __forceinline__ bool find_span(const int32_t* starts, uint32_t batch,
 // ---- the general kernels ----------------------------------------------------------------
 // Any type, head, stride and alignment.  128 rows (or keys) a workgroup, 32 a wave, which
 // holds their operands in registers; 32 keys (or rows) at a time go through registers to
-// LDS.
+// LDS.  In 32 bits the matrix rate is a sixteenth; what is left is bound by the way to LDS and its
+// barriers (one causal prompt, 32 bits: 4096 tokens, 16 / 4 heads of 64 566 us forward, 2865 backward;
+// 3807 with all query heads of a key-value head in one workgroup).
 constexpr uint32_t kRows = 128, kStep = 32;
 constexpr uint32_t kKeys = 64;  // keys of a workgroup of dkv_tile_kernel
 
@@ -791,7 +793,7 @@ __global__ __launch_bounds__(256) void dq_kernel(PromptGradParams p) {
   if (valid) write_row<T, DP>(dq, o, a.scale, a.dim, half);
 }
 
-// WHAT: 1 dv, 2 dk, 3 both.
+// WHAT: 1 dv, 2 dk, 3 both (with one part only: the parts' memory is for one of them).
 template <typename T, int DP, int WHAT>
 __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
   const gts_prompt_grad_args& a = p.a;
@@ -799,9 +801,10 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
   __shared__ __align__(16) T s_q[kStep * kRowPitch<T, DP>], s_o[kStep * kRowPitch<T, DP>];
   __shared__ float s_lse[kStep], s_delta[kStep];
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, half = lane / 32;
-  const uint32_t h = blockIdx.x % a.kv_heads;
+  const uint32_t h = blockIdx.x % a.kv_heads, at = blockIdx.x / a.kv_heads, place = at / p.splits, split = at - place * p.splits;
   Span sp;
-  if (!find_span(a.starts, a.batch, a.tokens, kRows, blockIdx.x / a.kv_heads, &sp)) return;
+  if (!find_span(a.starts, a.batch, a.tokens, kRows, place, &sp)) return;
+  const uint32_t g0 = split * (p.group / p.splits), g1 = g0 + p.group / p.splits;  // its query heads
   const uint32_t k0 = sp.tile * kRows, key = k0 + wave * 32 + lane % 32, token = sp.first + key;
   const bool valid = key < sp.n, causal = a.flags & GTS_PROMPT_CAUSAL;
   T* dk = (T*)a.dk + (int64_t)token * a.dk_stride[0] + (int64_t)h * a.dk_stride[1];
@@ -816,7 +819,7 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
       v.load((const T*)a.v + (int64_t)token * a.v_stride[0] + (int64_t)h * a.v_stride[1], valid, a.dim, half);
     const float c = a.scale * kLog2e;
     const uint32_t first = causal ? k0 : 0;
-    for (uint32_t g = 0; g < p.group; ++g) {
+    for (uint32_t g = g0; g < g1; ++g) {
       const uint32_t hq = h * p.group + g;
       const T* q = (const T*)a.q + (int64_t)sp.first * a.q_stride[0] + (int64_t)hq * a.q_stride[1];
       const T* dout = (const T*)a.dout + (int64_t)sp.first * a.dout_stride[0] + (int64_t)hq * a.dout_stride[1];
@@ -867,7 +870,15 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
       }
     }
   }
-  if (!valid) return;
+  if (!valid || (!sp.in && split)) return;
+  if (WHAT != 3 && p.splits > 1 && sp.in) {
+    float* out = p.parts + (((uint64_t)split * a.tokens + token) * a.kv_heads + h) * a.dim;
+    if constexpr (kV)
+      write_row<float, DP>(out, ov, 1.f, a.dim, half);
+    else
+      write_row<float, DP>(out, ok, a.scale, a.dim, half);
+    return;
+  }
   if constexpr (kV) write_row<T, DP>(dv, ov, 1.f, a.dim, half);
   if constexpr (kK) write_row<T, DP>(dk, ok, a.scale, a.dim, half);
 }
@@ -1251,25 +1262,26 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_tile_kernel(Prompt
     for (int d = 0; d < DP / 32; ++d) dkv_keys<T, DP, DV, true>(p, sp, h, split, s_qo, s_stat, d);
 }
 
-// The parts' sum, in order, for the tokens of the sequences; four values a thread.
-template <typename T>
+// The parts' sum, in order, for the tokens of the sequences; V values a thread.
+template <typename T, int V>
 __global__ __launch_bounds__(256) void join_parts_kernel(PromptGradParams p, T* out, int64_t stride0, int64_t stride1) {
   const gts_prompt_grad_args& a = p.a;
-  const uint64_t i = (block_number() * 256 + threadIdx.x) * 4, all = (uint64_t)a.tokens * a.kv_heads * a.dim;
+  const uint64_t i = (block_number() * 256 + threadIdx.x) * V, all = (uint64_t)a.tokens * a.kv_heads * a.dim;
   if (i >= all) return;
-  const uint32_t row = (uint32_t)(i / a.dim), c = (uint32_t)(i - (uint64_t)row * a.dim), t = row / a.kv_heads;
+  const uint64_t row = i / a.dim;
+  const uint32_t c = (uint32_t)(i - row * a.dim), t = (uint32_t)(row / a.kv_heads), h = (uint32_t)(row - (uint64_t)t * a.kv_heads);
   if (a.starts && (int64_t)t < a.starts[0]) return;
   if (a.starts && (int64_t)t >= a.starts[a.batch]) return;
-  f32x4 sum = *(const f32x4*)(p.parts + i);
+  Pack<float, V> sum = *(const Pack<float, V>*)(p.parts + i);
   for (uint32_t s = 1; s < p.splits; ++s) {
-    const f32x4 x = *(const f32x4*)(p.parts + s * all + i);
+    const Pack<float, V> x = *(const Pack<float, V>*)(p.parts + s * all + i);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] += x[e];
+    for (int e = 0; e < V; ++e) sum.v[e] += x.v[e];
   }
-  Pack<T, 4> y;
+  Pack<T, V> y;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y.v[e] = (T)sum[e];
-  *(Pack<T, 4>*)(out + (int64_t)t * stride0 + (int64_t)(row - t * a.kv_heads) * stride1 + c) = y;
+  for (int e = 0; e < V; ++e) y.v[e] = (T)sum.v[e];
+  *(Pack<T, V>*)(out + (int64_t)t * stride0 + (int64_t)h * stride1 + c) = y;
 }
 
 bool rows_aligned(const void* p, const int64_t* stride, uint32_t e) {
@@ -1320,7 +1332,7 @@ uint64_t parts_bytes(uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint3
 template <typename T, int DP>
 hipError_t launch_prompt_grad_d(const PromptGradParams& p, hipStream_t s) {
   const gts_prompt_grad_args& a = p.a;
-  const dim3 rows(p.places * a.q_heads), keys(p.places * a.kv_heads), block(256);
+  const dim3 rows(p.places * a.q_heads), keys(p.places * a.kv_heads * p.splits), block(256);
   stats_kernel<T><<<dim3((a.tokens + 63) / 64 * a.q_heads + 1), block, 0, s>>>(p);
   if constexpr (sizeof(T) == 2) {
     if (p.vec && a.dim % 8 == 0 && rows_aligned(a.dq, a.dq_stride, 2) && rows_aligned(a.dk, a.dk_stride, 2) &&
@@ -1329,17 +1341,20 @@ hipError_t launch_prompt_grad_d(const PromptGradParams& p, hipStream_t s) {
       const dim3 groups(p.key_places * a.kv_heads * p.splits);
       const dim3 join = grid_of(((uint64_t)a.tokens * a.kv_heads * a.dim / 4 + 255) / 256);
       dkv_tile_kernel<T, DP, false><<<groups, block, 0, s>>>(p);
-      if (p.splits > 1) join_parts_kernel<T><<<join, block, 0, s>>>(p, (T*)a.dk, a.dk_stride[0], a.dk_stride[1]);
+      if (p.splits > 1) join_parts_kernel<T, 4><<<join, block, 0, s>>>(p, (T*)a.dk, a.dk_stride[0], a.dk_stride[1]);
       dkv_tile_kernel<T, DP, true><<<groups, block, 0, s>>>(p);
-      if (p.splits > 1) join_parts_kernel<T><<<join, block, 0, s>>>(p, (T*)a.dv, a.dv_stride[0], a.dv_stride[1]);
+      if (p.splits > 1) join_parts_kernel<T, 4><<<join, block, 0, s>>>(p, (T*)a.dv, a.dv_stride[0], a.dv_stride[1]);
       return hipGetLastError();
     }
   }
   dq_kernel<T, DP><<<rows, block, 0, s>>>(p);
-  if constexpr (DP == 256) {  // no registers for both
+  if (DP == 256 || p.splits > 1) {  // no registers for both, or no memory for both's parts
+    const dim3 join = grid_of(((uint64_t)a.tokens * a.kv_heads * a.dim + 255) / 256);
     dkv_kernel<T, DP, 1><<<keys, block, 0, s>>>(p);
+    if (p.splits > 1) join_parts_kernel<T, 1><<<join, block, 0, s>>>(p, (T*)a.dv, a.dv_stride[0], a.dv_stride[1]);
     dkv_kernel<T, DP, 2><<<keys, block, 0, s>>>(p);
-  } else {
+    if (p.splits > 1) join_parts_kernel<T, 1><<<join, block, 0, s>>>(p, (T*)a.dk, a.dk_stride[0], a.dk_stride[1]);
+  } else if constexpr (DP < 256) {
     dkv_kernel<T, DP, 3><<<keys, block, 0, s>>>(p);
   }
   return hipGetLastError();

@@ -357,7 +357,7 @@ def test_prompt_scales(dtype, scale):
     check_prompt(q, k, v, None, dout, True, scale)
 
 
-@pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 64), (F, 64), (BF, 40), (BF, 256)])
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 64), (F, 64), (BF, 40), (BF, 256), (BF, 33), (F, 130)])
 def test_prompt_tokens_outside(dtype, D):
     """Tokens before the first sequence and behind the last: zeros, and no part of others."""
     g = gen(4)
