@@ -42,9 +42,6 @@ streams.  Every call may be captured into a graph (a backward pass too, where no
 eager autograd graph of the same leaves lives meanwhile: that is torch's rule).  For
 autograd the caller's tensors that a call writes (out, q_out, lse, scratch, preact,
 mean, rstd, the caches) are modified in place.
-A backward pass captured into a graph needs leaves that no live eager graph holds:
-torch accumulates a leaf's gradient on the stream of its first graph, on which a capture
-must not wait.
 """
 from __future__ import annotations
 
