@@ -885,8 +885,8 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
 
 // ---- the gradient's tile kernels -------------------------------------------------------------
 // As prompt_tile_kernel: values that are not finite are looked for only where a result has one.
-// Masked scores are -inf then; with `odd` masked weights and their gradients are 0 whatever the
-// row's statistics are.
+// Masked exponents are -inf then, whatever scale's sign and the row's log-sum are; with `odd` masked
+// weights and their gradients are 0 whatever else the row has.
 template <int N>
 __device__ __forceinline__ bool any_odd(const f32x16 (&o)[N]) {
   bool found = false;
@@ -1011,9 +1011,10 @@ __device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& s
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const bool hidden = masked && j0 + x + frag_row(i, half) >= seen;
-        if (!ODD && hidden) s[i] = -INFINITY;
-        s[i] = exp2_(__builtin_fmaf(s[i], c, -lse)) * (dp[i] - delta);
-        if (ODD && hidden) s[i] = 0.f;
+        float y = __builtin_fmaf(s[i], c, -lse);  // hidden behind the product: c has scale's sign
+        if (!ODD && hidden) y = -INFINITY;
+        y = exp2_(y) * (dp[i] - delta);
+        s[i] = ODD && hidden ? 0.f : y;
       }
     };
     if constexpr (!ODD) {
@@ -1163,8 +1164,9 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const bool hidden = masked && ((causal && i0 + r + i < key) || i0 + r + i >= sp.n);
-            float y = !ODD && hidden ? -INFINITY : s[e + i];
-            y = exp2_(__builtin_fmaf(y, c, -lse[i]));
+            float y = __builtin_fmaf(s[e + i], c, -lse[i]);  // hidden behind the product: c has scale's sign
+            if (!ODD && hidden) y = -INFINITY;
+            y = exp2_(y);
             if constexpr (!DV) y *= dp[e + i] - delta[i];
             s[e + i] = ODD && hidden ? 0.f : y;
           }

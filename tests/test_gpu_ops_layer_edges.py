@@ -1,0 +1,51 @@
+"""The operators of a decoder layer at the edges of what their calls allow."""
+import math
+
+import pytest
+import torch
+
+import layer_reference as R
+from paper_2607_11262_amd import ops
+from test_gpu_ops_layer import BF, F, HF, close, d64, prompt_case
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- attention over prompts: scales ------------------------------------------------------
+
+def flush_errors(dout, q, k, v, out, starts, causal, scale):
+    """What is lost of dq, dk and dv where an exponential is below 2^-126, the smallest number of 32
+    bits with all of its bits, and may be 0: 2^-126 of each weight, and of its gradient that times
+    |dp - delta|, or 2^-126 where that product is the one below it."""
+    G, tiny = q.shape[1] // k.shape[1], 2.0 ** -126
+    r = [torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)]
+    for a, b in R.spans(q.shape[0], starts):
+        for h in range(q.shape[1]):
+            x, y = (slice(a, b), h), (slice(a, b), h // G)
+            seen = R._scores(q[x], k[y], causal, 1.0) > -math.inf
+            size = (dout[x] @ v[y].T - (dout[x] * out[x]).sum(-1, keepdim=True)).abs()
+            ds = tiny * (1.0 + size) * seen
+            r[0][x] += abs(scale) * (ds @ k[y].abs())
+            r[1][y] += abs(scale) * (ds.T @ q[x].abs())
+            r[2][y] += tiny * (seen.double().T @ dout[x].abs())
+    return r
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("scale", [0.0, -0.0, -0.3, -1e-30, 2.0])
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (BF, 128), (BF, 256), (HF, 96), (HF, 256), (F, 64), (F, 256), (BF, 33)])
+def test_prompt_scales_of_any_sign(dtype, D, scale, causal):
+    """Lengths that no tile divides: what is hidden behind a sequence's end stays so."""
+    for lens in ([1], [33], [150], [64, 70], [31, 0, 97]):
+        q, k, v, starts, dout = prompt_case(2, 1, D, lens, dtype)
+        st, lse = starts.cuda(), torch.empty(q.shape[:2], device="cuda")
+        qc, kc, vc, dc = (t.cuda() for t in (q, k, v, dout))
+        o = ops.prompt_attention(qc, kc, vc, st, causal=causal, scale=scale, lse=lse)
+        ref, lr, err, l_err = R.prompt(*d64(q, k, v), starts, causal, scale, dtype)
+        close(o, ref, err, dtype, "out")
+        close(lse, lr, l_err, F, "lse")
+        got = ops.prompt_attention_backward(dc, qc, kc, vc, o, lse, st, causal=causal, scale=scale)
+        refs, errs = R.prompt_gradient(*d64(dout, q, k, v, o, lse), starts, causal, scale, dtype)
+        flushed = flush_errors(*d64(dout, q, k, v, o), starts, causal, scale)
+        for a, r, e, f, name in zip(got, refs, errs, flushed, ("dq", "dk", "dv")):
+            close(a, r, e + f, dtype, name)
