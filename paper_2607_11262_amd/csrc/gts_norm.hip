@@ -414,8 +414,9 @@ void launch_grad_t(const NormGradParams& p, hipStream_t s) {
   const gts_norm_grad_args& a = p.a;
   const uint32_t groups = grad_groups(a.rows, a.dim);
   if (!held<T>(a.dim)) {
-    if (a.dx && a.rows) norm_grad_long_kernel<T><<<grid_of(a.rows), dim3(1024), 0, s>>>(a);
+    // first what only reads: dx may be dy or x
     if (p.dw || p.db) norm_columns_kernel<T><<<dim3((a.dim + 255) / 256, groups), dim3(256), 0, s>>>(p);
+    if (a.dx && a.rows) norm_grad_long_kernel<T><<<grid_of(a.rows), dim3(1024), 0, s>>>(a);
     return;
   }
   launch_team<Gradient, T>(p, a.dim, groups, s);

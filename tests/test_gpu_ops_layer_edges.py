@@ -6,7 +6,7 @@ import torch
 
 import layer_reference as R
 from paper_2607_11262_amd import ops
-from test_gpu_ops_layer import BF, F, HF, close, d64, prompt_case
+from test_gpu_ops_layer import BF, F, HF, TYPES, close, d64, gen, prompt_case, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,37 @@ def test_prompt_scales_of_any_sign(dtype, D, scale, causal):
         flushed = flush_errors(*d64(dout, q, k, v, o), starts, causal, scale)
         for a, r, e, f, name in zip(got, refs, errs, flushed, ("dq", "dk", "dv")):
             close(a, r, e + f, dtype, name)
+
+
+# ---- norm: gradients in place ------------------------------------------------------------
+
+def norm_gradient_into(dy, x, weight, rstd, mean, dx):
+    """gts_layer_norm_backward with a dx of the caller's: (dweight, dbias)."""
+    rows, dim = x.shape
+    dw, db = torch.empty_like(weight), torch.empty_like(weight)
+    scratch = torch.empty(ops._scratch_of("gts_layer_norm_backward_scratch", rows, dim), device="cuda", dtype=torch.uint8)
+    ops._call("gts_layer_norm_backward", ops._pack_norm_grad(
+        dy.data_ptr(), x.data_ptr(), weight.data_ptr(), ops._ptr(mean), rstd.data_ptr(), dx.data_ptr(), dw.data_ptr(), db.data_ptr(),
+        dy.stride(0), x.stride(0), dx.stride(0), rows, dim, ops._TYPES[x.dtype], 0 if mean is None else ops.CENTER,
+        scratch.data_ptr(), scratch.numel()), torch.cuda.current_stream().cuda_stream)
+    return dw, db
+
+
+@pytest.mark.parametrize("center", [True, False])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,dim", [(50, 3), (300, 136), (9, 2048), (40, 8200), (70, 20000), (5, 16385)])
+def test_norm_gradient_in_place(rows, dim, dtype, center):
+    g = gen(rows + dim)
+    x, dy, w = (t.cuda() for t in (randn(g, rows, dim, dtype=dtype, shift=0.5), randn(g, rows, dim, dtype=dtype), randn(g, dim, dtype=dtype)))
+    mean, rstd = torch.empty(rows, device="cuda") if center else None, torch.empty(rows, device="cuda")
+    ops.layer_norm(x, w, center=center, mean=mean, rstd=rstd)
+    want = ops.layer_norm_backward(dy, x, w, rstd, mean, bias=True)
+    refs = R.norm_gradient(*d64(dy, x, w, mean, rstd))
+    for a, r, e, name in zip(want, refs, refs[3:], ("dx", "dw", "db")):
+        close(a, r, e, dtype, name)
+    for which in ("dy", "x", "neither"):
+        dy1, x1 = dy.clone(), x.clone()
+        dx = dict(dy=dy1, x=x1, neither=torch.empty_like(x))[which]
+        got = (dx, *norm_gradient_into(dy1, x1, w, rstd, mean, dx))
+        for a, b, name in zip(got, want, ("dx", "dw", "db")):
+            assert torch.equal(a, b), (which, name)
