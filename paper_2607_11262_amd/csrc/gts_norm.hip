@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kThreads<L>) void norm_kernel(gts_norm_args a) {
   __shared__ float s_sum[2][2][16];
   Team<L> team{s_sum};
   const uint32_t lane = threadIdx.x % L;
-  const uint64_t row = block_number() * kTeams<L> + threadIdx.x / L;
+  const uint64_t row = block_number<kThreads<L>>() * kTeams<L> + threadIdx.x / L;
   if (row >= a.rows) return;
   const bool center = a.flags & GTS_NORM_CENTER;
   const T* x = (const T*)a.x + (int64_t)row * a.x_stride;
@@ -156,7 +156,7 @@ template <typename T>
 __global__ __launch_bounds__(1024) void norm_long_kernel(gts_norm_args a) {
   __shared__ float s_sum[2][2][16];
   Team<1024> team{s_sum};
-  const uint64_t row = block_number();
+  const uint64_t row = block_number<1024>();
   if (row >= a.rows) return;
   const T* x = (const T*)a.x + (int64_t)row * a.x_stride;
   T* y = (T*)a.out + (int64_t)row * a.out_stride;
@@ -306,7 +306,7 @@ template <typename T>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(gts_norm_grad_args a) {
   __shared__ float s_sum[2][2][16];
   Team<1024> team{s_sum};
-  const uint64_t row = block_number();
+  const uint64_t row = block_number<1024>();
   if (row >= a.rows) return;
   const T* x = (const T*)a.x + (int64_t)row * a.x_stride;
   const T* dy = (const T*)a.dy + (int64_t)row * a.dy_stride;
@@ -374,7 +374,7 @@ void launch_team(const P& p, uint32_t dim, uint32_t groups, hipStream_t s) {
 template <typename T, int V, int L, int C>
 struct Forward {
   static void go(const gts_norm_args& a, uint32_t, hipStream_t s) {
-    const dim3 grid = grid_of(((uint64_t)a.rows + kTeams<L> - 1) / kTeams<L>);
+    const dim3 grid = grid_of<kThreads<L>>(((uint64_t)a.rows + kTeams<L> - 1) / kTeams<L>);
     if (a.dim % V == 0)
       norm_kernel<T, V, L, C, true><<<grid, dim3(kThreads<L>), 0, s>>>(a);
     else
@@ -394,7 +394,7 @@ struct Gradient {
 template <typename T>
 void launch_norm_t(const gts_norm_args& a, hipStream_t s) {
   if (!held<T>(a.dim))
-    norm_long_kernel<T><<<grid_of(a.rows), dim3(1024), 0, s>>>(a);
+    norm_long_kernel<T><<<grid_of<1024>(a.rows), dim3(1024), 0, s>>>(a);
   else
     launch_team<Forward, T>(a, a.dim, 0, s);
 }
@@ -416,7 +416,7 @@ void launch_grad_t(const NormGradParams& p, hipStream_t s) {
   if (!held<T>(a.dim)) {
     // first what only reads: dx may be dy or x
     if (p.dw || p.db) norm_columns_kernel<T><<<dim3((a.dim + 255) / 256, groups), dim3(256), 0, s>>>(p);
-    if (a.dx && a.rows) norm_grad_long_kernel<T><<<grid_of(a.rows), dim3(1024), 0, s>>>(a);
+    if (a.dx && a.rows) norm_grad_long_kernel<T><<<grid_of<1024>(a.rows), dim3(1024), 0, s>>>(a);
     return;
   }
   launch_team<Gradient, T>(p, a.dim, groups, s);

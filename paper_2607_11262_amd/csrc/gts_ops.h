@@ -36,14 +36,20 @@ hipError_t launch_column_sums(const float* in0, void* out0, const float* in1, vo
                               uint32_t dtype, hipStream_t stream);
 
 #ifdef __HIPCC__
-// A launch has less than 2^32 threads in each dimension: workgroups of 256 past
-// 2^23 go on in further rows of the grid (the last row may pass their number).
-constexpr uint32_t kGridRow = 1u << 23;
-constexpr uint64_t kMostBlocks = (uint64_t)kGridRow * 65535;
+// A launch has less than 2^32 threads in each dimension: workgroups past 2^31 threads (2^23 of 256)
+// go on in further rows of the grid (the last row may pass their number).
+template <uint32_t THREADS = 256>
+constexpr uint32_t kGridRow = (1u << 31) / THREADS;
+constexpr uint64_t kMostBlocks = (uint64_t)kGridRow<> * 65535;
+template <uint32_t THREADS = 256>
 inline dim3 grid_of(uint64_t blocks) {
-  return blocks <= kGridRow ? dim3((uint32_t)blocks) : dim3(kGridRow, (uint32_t)((blocks + kGridRow - 1) / kGridRow));
+  constexpr uint32_t row = kGridRow<THREADS>;
+  return blocks <= row ? dim3((uint32_t)blocks) : dim3(row, (uint32_t)((blocks + row - 1) / row));
 }
-__device__ __forceinline__ uint64_t block_number() { return (uint64_t)blockIdx.y * kGridRow + blockIdx.x; }
+template <uint32_t THREADS = 256>
+__device__ __forceinline__ uint64_t block_number() {
+  return (uint64_t)blockIdx.y * kGridRow<THREADS> + blockIdx.x;
+}
 
 // n / d for n < 2^31 and 1 <= d < 2^31: one multiplication high and a shift
 // (m = ceil(2^(32 + s) / d) - 2^32 with 2^s >= d; the sum with n keeps the

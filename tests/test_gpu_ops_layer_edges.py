@@ -83,3 +83,31 @@ def test_norm_gradient_in_place(rows, dim, dtype, center):
         got = (dx, *norm_gradient_into(dy1, x1, w, rstd, mean, dx))
         for a, b, name in zip(got, want, ("dx", "dw", "db")):
             assert torch.equal(a, b), (which, name)
+
+
+# ---- norm: many rows -----------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,dim", [(BF, 3), (HF, 7), (F, 2)])
+def test_norm_of_more_rows_than_a_row_of_the_grid(dtype, dim):
+    """More workgroups of 1024 threads than 2^32 threads hold."""
+    rows = (1 << 22) + 5
+    g = torch.Generator(device="cuda").manual_seed(dim)
+    x, dy = (torch.randn(rows, dim, generator=g, device="cuda").to(dtype) for _ in range(2))
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    y = ops.layer_norm(x, eps=0.1, mean=mean, rstd=rstd)
+    few = torch.cat((torch.arange(40), torch.arange(rows // 2 - 20, rows // 2 + 20), torch.arange(rows - 40, rows))).cuda()
+    ref = R.norm(*d64(x[few], None, None), 0.1, True)
+    close(y[few], ref[0], ref[3], dtype, "y")
+    # every row: what a call of the same rows in parts gives
+    part = 1 << 20
+    for i in range(0, rows, part):
+        assert torch.equal(y[i:i + part], ops.layer_norm(x[i:i + part], eps=0.1))
+    dx, _, db = ops.layer_norm_backward(dy, x, None, rstd, mean, bias=True)
+    refs = R.norm_gradient(*d64(dy[few], x[few], None, mean[few], rstd[few]))
+    close(dx[few], refs[0], refs[3], dtype, "dx")
+    for i in range(0, rows, part):
+        at = slice(i, i + part)
+        assert torch.equal(dx[at], ops.layer_norm_backward(dy[at], x[at], None, rstd[at], mean[at])[0])
+    total = dy.double().sum(0)
+    # 512 strips of rows, each a sum of its own, then their sum
+    assert ((db.double() - total).abs() <= R.rounded(total, (rows / 512 + 600) * R.E * dy.double().abs().sum(0), dtype)).all()
