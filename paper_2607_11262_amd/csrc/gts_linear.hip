@@ -610,6 +610,7 @@ constexpr float kBegin = 4.f, kJoin = 4.f, kPartBytes = 1.f / 2.4e6f;
 float cost_of(const TileCost& c, uint32_t m, uint32_t n, uint32_t k, uint32_t splits) {
   const uint64_t tiles = (uint64_t)((m + c.m - 1) / c.m) * ((n + c.n - 1) / c.n);
   const uint64_t groups = tiles * splits;
+  if (groups > kMostGroups) return INFINITY;  // never tiles of 128 x 128 in one split: the sizes were checked for them
   const float shared = c.shared * (groups < kUnits ? (float)groups / kUnits : (float)((groups + kUnits - 1) / kUnits));
   const uint32_t stages = ((k + 63) / 64 + splits - 1) / splits;
   const float join = splits > 1 ? kJoin + kPartBytes * 4.f * splits * (float)m * (float)n : 0.f;
@@ -686,7 +687,6 @@ hipError_t launch_layout(MatmulParams& p, hipStream_t s) {
   p.k_split = ((a.k + p.splits - 1) / p.splits + kTileK - 1) / kTileK * kTileK;
   const uint32_t edge = kCuts[cut.tile].m;
   const uint64_t groups = (((uint64_t)a.m + edge - 1) / edge) * (((uint64_t)a.n + edge - 1) / edge) * p.splits;
-  if (groups > 0x7FFFFFull) return hipErrorInvalidValue;  // x 256 threads stay below 2^31
   if (edge == 128)
     matmul_kernel<T, AC, BC, 2><<<dim3((uint32_t)groups), dim3(256), 0, s>>>(p);
   else

@@ -9,6 +9,9 @@
 
 namespace gts {
 
+// Workgroups of a launch of one row, of 512 threads at most: their threads stay below 2^32.
+constexpr uint32_t kMostGroups = 0x7FFFFFu;
+
 constexpr uint32_t kTableFreqs = GTS_OPS_MAX_DIM / 2;
 struct TableFreqs {
   double f[kTableFreqs];

@@ -227,8 +227,8 @@ static int check_activation(uint32_t act) {
 }
 static int check_product(uint32_t m, uint32_t n, uint32_t k) {
   if (m > kMaxCount || k > kMaxCount || n > GTS_OPS_MAX_WIDTH) return refuse(GTS_E_RANGE, "product of %u x %u x %u", m, n, k);
-  // tiles of a launch, with room for splits
-  if ((((uint64_t)m + 127) / 128) * (((uint64_t)n + 127) / 128) > 0x7FFFFFu)
+  // tiles of a launch: where smaller ones or splits of the sum would be too many, these are taken
+  if ((((uint64_t)m + 127) / 128) * (((uint64_t)n + 127) / 128) > gts::kMostGroups)
     return refuse(GTS_E_RANGE, "a result of %u x %u is too large", m, n);
   return GTS_OK;
 }
@@ -282,7 +282,7 @@ int gts_linear_backward(const gts_linear_grad_args* a, void* hip_stream) {
 
 static int check_prompt(uint32_t batch, uint32_t tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t dim) {
   if (int rc = check_attention_sizes(batch, tokens, q_heads, kv_heads, dim)) return rc;
-  if (tokens > kMaxCount || gts::prompt_groups(batch, tokens, q_heads) > 0x7FFFFFu)
+  if (tokens > kMaxCount || gts::prompt_groups(batch, tokens, q_heads) > gts::kMostGroups)
     return refuse(GTS_E_RANGE, "%u sequences with %u tokens of %u heads", batch, tokens, q_heads);
   return GTS_OK;
 }

@@ -111,3 +111,14 @@ def test_norm_of_more_rows_than_a_row_of_the_grid(dtype, dim):
     total = dy.double().sum(0)
     # 512 strips of rows, each a sum of its own, then their sum
     assert ((db.double() - total).abs() <= R.rounded(total, (rows / 512 + 600) * R.E * dy.double().abs().sum(0), dtype)).all()
+
+
+# ---- products: tall and narrow ---------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_product_of_more_rows_than_small_tiles_take(dtype):
+    """Results that 2^23 tiles of 128 rows hold, and tiles of 64 rows do not."""
+    rows = 64 * (1 << 23) + 77
+    x = (torch.arange(rows, device="cuda", dtype=torch.int32) % 251).to(dtype).view(rows, 1)
+    y = ops.linear(x, torch.tensor([[2.0]], device="cuda", dtype=dtype))
+    assert torch.equal(y, x * 2)
