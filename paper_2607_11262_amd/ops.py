@@ -201,7 +201,7 @@ def _data(t, name, dims, like=None):
     if not t.is_cuda:
         raise ValueError(f"{name} is not on the GPU")
     strides = t.stride()
-    if strides[-1] != 1 and t.shape[-1] > 1:
+    if strides[-1] != 1 and t.shape[-1] > 1 and t.numel():
         raise ValueError(f"{name}: the last dimension is not contiguous")
     if like is None:
         if t.dtype not in _TYPES:
@@ -655,9 +655,7 @@ def _flat(x, name="x", stream=None):
         return x
     if x.dim() < 1:
         raise ValueError(f"{name} has no dimensions")
-    if not x.numel():
-        return x.new_empty((math.prod(x.shape[:-1]), x.shape[-1]))
-    flat = x.reshape(-1, x.shape[-1])
+    flat = x.reshape(math.prod(x.shape[:-1]), x.shape[-1])  # sizes that an empty x leaves open with -1
     if stream is not None and flat.data_ptr() != x.data_ptr():
         raise ValueError(f"{name}: its rows are not evenly apart, so that it would be copied on another stream")
     return flat

@@ -122,3 +122,43 @@ def test_product_of_more_rows_than_small_tiles_take(dtype):
     x = (torch.arange(rows, device="cuda", dtype=torch.int32) % 251).to(dtype).view(rows, 1)
     y = ops.linear(x, torch.tensor([[2.0]], device="cuda", dtype=dtype))
     assert torch.equal(y, x * 2)
+
+
+# ---- batches of nothing ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("shape", [(0, 16), (3, 0, 16), (0, 5, 16), (2, 0, 3, 16)])
+@pytest.mark.parametrize("params", [False, True])
+def test_batches_of_nothing_have_gradients(shape, params):
+    """A batch without a token is a training step like any other: zeros for the parameters."""
+    leaf = lambda *s: torch.ones(s, device="cuda").requires_grad_()  # noqa: E731
+    x, gate, res = leaf(*shape), leaf(*shape[:-1], 8), leaf(*shape[:-1], 8)
+    w, b, weight, bias = leaf(16), leaf(16), leaf(8, 16), leaf(8)
+    if not params:
+        w, b, weight, bias = (t.detach() for t in (w, b, weight, bias))
+    h = ops.layer_norm(x, w, b)
+    y = ops.linear(h, weight, bias, activation="silu", gate=gate, residual=res)
+    assert h.shape == shape and y.shape == (*shape[:-1], 8) and h.requires_grad and y.requires_grad
+    y.sum().backward()
+    for t in (x, gate, res):
+        assert t.grad is not None and t.grad.shape == t.shape
+    for t in (w, b, weight, bias) if params else ():
+        assert t.grad is not None and (t.grad == 0).all()
+
+
+def test_sums_of_nothing_have_gradients():
+    """Rows of no values: the product is its bias, the operands' gradients are empty."""
+    x, w = torch.ones(2, 3, 0, device="cuda").requires_grad_(), torch.ones(4, 0, device="cuda").requires_grad_()
+    b = torch.arange(4.0, device="cuda").requires_grad_()
+    y = ops.linear(x, w, b)
+    assert torch.equal(y, b.detach().expand(2, 3, 4))
+    y.sum().backward()
+    assert x.grad.shape == x.shape and w.grad.shape == w.shape and (b.grad == 6).all()
+
+
+def test_prompts_of_nothing_have_gradients():
+    q, k, v = (torch.ones(0, h, 32, device="cuda").requires_grad_() for h in (4, 2, 2))
+    for starts in (None, torch.zeros(4, dtype=torch.int32, device="cuda")):
+        o = ops.prompt_attention(q, k, v, starts)
+        assert o.shape == q.shape and o.requires_grad
+        o.sum().backward()
+        assert all(t.grad.shape == t.shape for t in (q, k, v))
