@@ -19,7 +19,8 @@
  * rounded: attention over a 16-bit cache whose rows are aligned to 16 bytes
  * multiplies the values by softmax weights in the cache's type (their sum, and so
  * lse, keeps them in 32 bits).  So do attention over prompts and its gradient with
- * weights and their gradients, and gts_linear_backward's dz is in its tensors' type.
+ * weights and their gradients (in float16 scaled by powers of two that keep them
+ * in its range), and gts_linear_backward's dz is in its tensors' type.
  */
 #ifndef GTS_OPS_H
 #define GTS_OPS_H

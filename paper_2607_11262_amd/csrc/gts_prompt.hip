@@ -646,12 +646,65 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
     for (int d = 0; d < DP / 32; ++d) prompt_rows<T, DP, true>(p, sp, hq, h, s_kv, d);
 }
 
+// ---- float16 in the gradient ------------------------------------------------------------------
+// Weights p and their gradients ds are rounded to the tensors' type for the products.  float16 has all
+// its bits from 2^-14 to 65504 only: p of n equal keys is 1 / n, and ds goes with dout and v, whose
+// size nothing bounds.  So p is lifted by 2^10 (lse is 10 less in base 2), and ds scaled by a power of
+// two of the lane's, whose row (dq) or key (dk) the sums are: the first that is not 0 to 2^8, and less
+// when one has grown past 2^15.  The sums take both back in 32 bits.  bfloat16 has the range of
+// 32 bits.
+template <typename T>
+constexpr float kLift = __is_same(T, _Float16) ? 10.f : 0.f;
+
+template <typename T>
+struct Scaled {
+  template <int N>
+  __device__ __forceinline__ void fit(f32x16*, f32x16&) {}
+  template <int N>
+  __device__ __forceinline__ void back(f32x16*) const {}
+};
+template <>
+struct Scaled<_Float16> {
+  float f = 0x1p100f;  // 2^-120 at least
+  __device__ __forceinline__ static float inverse(float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
+  // w becomes f w; the sums o follow when f changes.
+  template <int N>
+  __device__ __forceinline__ void fit(f32x16* o, f32x16& w) {
+    float mx = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, __builtin_fabsf(w[i]));
+    mx = max_halves(mx);
+    const bool large = mx * f > 0x1p15f;
+    if (__any(large)) {
+      const float f1 = large ? __uint_as_float((262u - (__float_as_uint(mx) >> 23)) << 23) : f, r = f1 * inverse(f);
+#pragma unroll
+      for (int d = 0; d < N; ++d) o[d] *= r;
+      f = f1;
+    }
+    w *= f;
+  }
+  template <int N>
+  __device__ __forceinline__ void back(f32x16* o) const {
+    const float r = 0x1p-10f * inverse(f);
+#pragma unroll
+    for (int d = 0; d < N; ++d) o[d] *= r;
+  }
+};
+// The same for sums of weights.
+template <typename T, int N>
+__device__ __forceinline__ void lower(f32x16* o) {
+  if constexpr (kLift<T> != 0.f) {
+#pragma unroll
+    for (int d = 0; d < N; ++d) o[d] *= 0x1p-10f;
+  }
+}
+
 struct PromptGradParams {
   gts_prompt_grad_args a;
   uint32_t group;
   uint32_t places;
   bool vec;      // rows of dout, q, k and v are aligned to 16 bytes
-  // [q_heads][tokens]: a head's values side by side; lse in base 2
+  // [q_heads][tokens]: a head's values side by side; lse in base 2, less kLift
   float *lse, *delta;
   uint32_t key_places;
   // The query heads of a key-value head are summed in this many parts; with more than one, the
@@ -729,7 +782,7 @@ __global__ __launch_bounds__(256) void stats_kernel(PromptGradParams p) {
     for (int k = 8; k; k >>= 1) sum += __shfl_xor(sum, k);
     if (li == 0 && t < a.tokens) {
       p.delta[p.stat(h, t)] = sum;
-      p.lse[p.stat(h, t)] = a.lse[(uint64_t)t * a.q_heads + h] * kLog2e;
+      p.lse[p.stat(h, t)] = a.lse[(uint64_t)t * a.q_heads + h] * kLog2e - kLift<T>;
     }
   }
 }
@@ -761,6 +814,7 @@ __global__ __launch_bounds__(256) void dq_kernel(PromptGradParams p) {
   const float c = a.scale * kLog2e;
   const float lse = valid ? p.lse[p.stat(hq, token)] : 0.f;
   const float delta = valid ? p.delta[p.stat(hq, token)] : 0.f;
+  Scaled<T> scaled;
   for (uint32_t j0 = 0; j0 < keys; j0 += kStep) {
     const bool edge = causal && j0 + kStep > r0 + 1;
     __syncthreads();
@@ -787,9 +841,11 @@ __global__ __launch_bounds__(256) void dq_kernel(PromptGradParams p) {
         __syncthreads();
       }
     }
+    scaled.template fit<DP / 32>(o, s);
     add_weighted<T, DP>(o, s_k, s, lane);
     if (odd) add_odd<T, DP / 32>(o, k, a.k_stride[0], j0, sp.n, 0, a.dim, half, true, [&](uint32_t j) { return j < sees; });
   }
+  scaled.template back<DP / 32>(o);
   if (valid) write_row<T, DP>(dq, o, a.scale, a.dim, half);
 }
 
@@ -818,6 +874,7 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
     if constexpr (kK)
       v.load((const T*)a.v + (int64_t)token * a.v_stride[0] + (int64_t)h * a.v_stride[1], valid, a.dim, half);
     const float c = a.scale * kLog2e;
+    Scaled<T> scaled;
     const uint32_t first = causal ? k0 : 0;
     for (uint32_t g = g0; g < g1; ++g) {
       const uint32_t hq = h * p.group + g;
@@ -861,7 +918,10 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
           }
         }
         if constexpr (kV) add_weighted<T, DP>(ov, s_o, s, lane);
-        if constexpr (kK) add_weighted<T, DP>(ok, s_q, ds, lane);
+        if constexpr (kK) {
+          scaled.template fit<DP / 32>(ok, ds);
+          add_weighted<T, DP>(ok, s_q, ds, lane);
+        }
         if (odd) {
           const auto sees = [&](uint32_t row) { return key <= row; };
           if constexpr (kV) add_odd<T, DP / 32>(ov, dout, a.dout_stride[0], i0, sp.n, 0, a.dim, half, false, sees);
@@ -869,6 +929,8 @@ __global__ __launch_bounds__(256) void dkv_kernel(PromptGradParams p) {
         }
       }
     }
+    if constexpr (kV) lower<T, DP / 32>(ov);
+    if constexpr (kK) scaled.template back<DP / 32>(ok);
   }
   if (!valid || (!sp.in && split)) return;
   if (WHAT != 3 && p.splits > 1 && sp.in) {
@@ -995,6 +1057,7 @@ __device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& s
   clear(o);
   Parts<T, DP> at;
   at.start(lane);
+  Scaled<T> scaled;
   for (uint32_t t = 0; t < tiles; ++t) {
     const uint32_t j0 = t * kTile;
     T *sk = s_kv + (t & 1) * 2 * L::N, *sv = sk + L::N;
@@ -1026,6 +1089,7 @@ __device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& s
           weigh(x, s, dp, true);
         else
           weigh(x, s, dp, false);
+        scaled.template fit<N>(o, s);
         add_columns<T, DP, N>(at, o, sk, x, 0, s, lane);
       }
     } else {
@@ -1039,6 +1103,7 @@ __device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& s
       const bool odd = clear_if_odd<T, L::N>(sk, causal && j0 + kTile > r0 + 1, 256);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
+        scaled.template fit<N>(o, s[x]);
         add_columns<T, DP, N>(at, o, sk, x * 32, d0, s[x], lane);
         if (odd)
           add_odd<T, N>(o, ld.a, ld.a_stride, j0 + x * 32, sp.n, d0 * 32, a.dim, half, true,
@@ -1046,6 +1111,7 @@ __device__ __forceinline__ bool dq_rows(const PromptGradParams& p, const Span& s
       }
     }
   }
+  scaled.template back<N>(o);
   if constexpr (!ODD) {
     if (__syncthreads_or(causal && valid && any_odd(o))) return true;
   } else {
@@ -1139,6 +1205,7 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
   clear(o);
   Parts<T, DP> at;
   at.start(lane);
+  Scaled<T> scaled;
   uint32_t buffer = 0;
   for (uint32_t g = g0; g < g1; ++g)
     for (uint32_t t = first; t < tiles; ++t, buffer ^= 1) {
@@ -1178,6 +1245,7 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
         weigh(false);
       bool odd = false;
       if constexpr (ODD) odd = clear_if_odd<T, L::N>(added, causal && t * kTile + 1 < k0 + kKeys, 256);
+      if constexpr (!DV) scaled.template fit<N>(o, s);
       add_columns<T, DP, N>(at, o, added, x0, d0, s, lane);
       if constexpr (ODD) {
         if (odd) {
@@ -1189,6 +1257,10 @@ __device__ __forceinline__ bool dkv_keys(const PromptGradParams& p, const Span& 
         }
       }
     }
+  if constexpr (DV)
+    lower<T, N>(o);
+  else
+    scaled.template back<N>(o);
   // the second half's sums, a block of columns at a time, to the first half's waves
   __syncthreads();
   float* s_sum = (float*)s_qo + wave % 2 * (N * 1024) + lane * 4;

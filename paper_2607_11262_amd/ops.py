@@ -1016,7 +1016,8 @@ def _prompt_backward(dout, q, k, v, out, lse, starts, causal, scale, stream):
 def prompt_attention_backward(dout, q, k, v, out, lse, starts=None, *, causal=True, scale=None, stream=None):
     """(dq, dk, dv) of prompt_attention from the gradient of its result, its inputs,
     its result and the log-sums that it left; causal and scale as in the forward call.
-    Weights and their gradients are rounded to the tensors' type for the products, and
+    Weights and their gradients are rounded to the tensors' type for the products (in
+    float16 scaled by powers of two, so that no size of dout or v loses them), and
     summed over a key-value head's query heads in 32 bits.  Tokens outside every
     sequence get zeros.  The same bits on every run."""
     _no_gradient("a tensor of the attention's gradient", dout, q, k, v, out, lse)

@@ -162,3 +162,79 @@ def test_prompts_of_nothing_have_gradients():
         assert o.shape == q.shape and o.requires_grad
         o.sum().backward()
         assert all(t.grad.shape == t.shape for t in (q, k, v))
+
+
+# ---- float16: gradients that are small or large ------------------------------------------------
+
+def half_gradient(dout, q, k, v, out, lse, causal, scale):
+    """dq, dk, dv of one sequence in 64 bits, and their errors before the last rounding, of a
+    gradient that keeps weights and their gradients as float16 of the size that suits them.  A weight
+    is rounded by 2^-11 of itself or, lifted by 2^10, half of the smallest number, 2^-25, below 2^-14.
+    A weight's gradient is rounded by 2^-11 of itself or, scaled so that the largest of its row (for dq) or
+    of its key (for dk) is 2^8 at least, 2^-25: 2^-33 of that largest.  Otherwise as in 32 bits."""
+    exact = R.prompt_gradient(dout, q, k, v, out, lse, None, causal, scale, F)
+    refs, errs = exact
+    G, u = q.shape[1] // k.shape[1], R.U[HF]
+    for h in range(q.shape[1]):
+        x, y = (slice(None), h), (slice(None), h // G)
+        s = R._scores(q[x], k[y], causal, scale)
+        seen = s > -math.inf
+        p = torch.exp(s - lse[x][:, None])
+        ds = p * (dout[x] @ v[y].T - (dout[x] * out[x]).sum(-1, keepdim=True))
+        size = ds.abs()
+        errs[0][x] += abs(scale) * ((u * size + 2.0 ** -33 * size.amax(1, keepdim=True) * seen) @ k[y].abs())
+        errs[1][y] += abs(scale) * ((u * size + 2.0 ** -33 * size.amax(0, keepdim=True) * seen).T @ q[x].abs())
+        errs[2][y] += (u * p + 2.0 ** -35 * seen).T @ dout[x].abs()
+    return refs, errs
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("D,Hq,Hkv", [(64, 2, 1), (128, 4, 2), (256, 2, 2), (33, 2, 1), (200, 1, 1)])
+@pytest.mark.parametrize("powers", [(-14, 0, 0), (-14, -6, 0), (-14, 6, 0), (10, -6, 4), (10, 6, 4), (8, 0, 6), (-12, -8, 8)])
+def test_prompt_gradient_of_any_size_in_float16(powers, D, Hq, Hkv, causal):
+    """dout times 2^powers[0], keys times 2^powers[1] and queries divided by it, values times
+    2^powers[2]: scores stay, their gradients leave the range of float16 where the results do not."""
+    q, k, v, _, dout = prompt_case(Hq, Hkv, D, [150], F)
+    scale = D ** -0.5
+    q, k = (q * 2.0 ** -powers[1]).half(), (k * 2.0 ** powers[1]).half()
+    v, dout = (v * 2.0 ** powers[2]).half(), (dout * 2.0 ** powers[0]).half()
+    qc, kc, vc, dc = (t.cuda() for t in (q, k, v, dout))
+    lse = torch.empty(150, Hq, device="cuda")
+    o = ops.prompt_attention(qc, kc, vc, causal=causal, lse=lse)
+    assert o.isfinite().all()
+    got = ops.prompt_attention_backward(dc, qc, kc, vc, o, lse, causal=causal)
+    refs, errs = half_gradient(*d64(dout, q, k, v, o, lse), causal, scale)
+    for a, r, e, name in zip(got, refs, errs, ("dq", "dk", "dv")):
+        # a result whose bound reaches past the largest number may be infinite
+        reaches = r.abs() + R.rounded(r, e, HF) >= torch.finfo(HF).max
+        a = a.cpu()
+        assert (a.isfinite() | reaches & (a.sign() == r.sign())).all(), name
+        compared = a.isfinite()
+        close(torch.where(compared, a, 0), torch.where(compared, r, 0.0), e, HF, name)
+
+
+@pytest.mark.parametrize("D", [64, 33])
+def test_prompt_gradient_of_equal_weights_of_many_keys(D):
+    """Weights 1 / n of which float16 as it stands has few bits, and would round all to the same side."""
+    n = 332_222 if D == 64 else 166_932  # 2^24 / n is near 50.5 and 100.5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rand = lambda: torch.randn(n, 1, D, generator=g, device="cuda").half()  # noqa: E731
+    q, k, v, dout = torch.zeros(n, 1, D, device="cuda", dtype=HF), rand(), rand(), (rand() + 1).half()
+    lse = torch.empty(n, 1, device="cuda")
+    o = ops.prompt_attention(q, k, v, causal=False, lse=lse)
+    dq, dk, dv = ops.prompt_attention_backward(dout, q, k, v, o, lse, causal=False)
+    do, vd, kd = dout[:, 0].double(), v[:, 0].double(), k[:, 0].double()
+    p = torch.exp(-lse[0, 0].double())  # the same for all
+    # weights of one rounding; sums in 32 bits, 16 terms a matrix instruction, whose order within is not known
+    steps = 2 * (n / 16 + 100) * R.E
+    ref = (do.sum(0) * p).expand(n, D)
+    err = (R.U[HF] + steps) * do.abs().sum(0) * p
+    close(dv[:, 0], ref.cpu(), err.cpu().expand(n, D), HF, "dv")
+    assert not dk.any()
+    few = slice(1000, 1040)  # dq of some rows
+    ds = p * (do[few] @ vd.T.contiguous() - (do[few] * o[few, 0].double()).sum(1, keepdim=True))
+    ref = D ** -0.5 * (ds @ kd)
+    sizes = (ds.abs() @ kd.abs()) * D ** -0.5
+    off = p * 2 * (D + 4) * R.E * (do[few].abs() @ vd.abs().T.contiguous() + (do[few] * o[few, 0].double()).abs().sum(1, keepdim=True))
+    err = (R.U[HF] + steps) * sizes + (off + 2.0 ** -33 * ds.abs().amax(1, keepdim=True)) @ kd.abs() * D ** -0.5
+    close(dq[few, 0], ref.cpu(), err.cpu(), HF, "dq")
