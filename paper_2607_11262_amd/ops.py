@@ -316,6 +316,11 @@ def _wrote(*tensors):
         torch.autograd.graph.increment_version(tensors)
 
 
+def _scale(scale, D):
+    """scale as its field takes it; by default that of heads of D (heads of 0 are refused by the library)."""
+    return max(D, 1) ** -0.5 if scale is None else _f32(scale).value
+
+
 def _disjoint(strides, shape, name):
     """An output whose elements overlap (an expanded view) would be written
     from several places."""
@@ -598,7 +603,7 @@ def shared_prefix_attention(q, k_cache, v_cache, page_table, lens, *, starts=Non
         os = out.stride()
         _call("gts_shared_prefix_attention", _pack_attention(
             *packed, q.data_ptr(), out.data_ptr(), _ptr(lse), qs[0], qs[1], os[0], os[1], _ptr(prefix_pages), n_prefix, Hq,
-            D ** -0.5 if scale is None else _f32(scale).value, 0, scratch.data_ptr(), scratch.numel()), s)
+            _scale(scale, D), 0, scratch.data_ptr(), scratch.numel()), s)
     _wrote(*written)
     return out
 
@@ -674,7 +679,7 @@ def _norm(x, weight, bias, eps, center, out, mean, rstd, stream):
         y = x.new_empty((rows, dim)) if out is None else out
         _call("gts_layer_norm", _pack_norm(
             x.data_ptr(), y.data_ptr(), _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd), xs[0],
-            dim if out is None else os, rows, dim, eps, _TYPES[x.dtype], CENTER if center else 0, 0), s)
+            dim if out is None else os, rows, dim, _f32(eps).value, _TYPES[x.dtype], CENTER if center else 0, 0), s)
     _wrote(out, mean, rstd)
     return y
 
@@ -937,10 +942,6 @@ def _prompt_shapes(q, k, v, starts):
 def _lse_like(lse, T, Hq, q):
     _refuse(isinstance(lse, torch.Tensor) and lse.dtype == torch.float32 and lse.shape == (T, Hq) and lse.is_contiguous()
             and lse.device == q.device, f"lse is a contiguous float32 [{T}, {Hq}]")
-
-
-def _scale(scale, D):
-    return D ** -0.5 if scale is None else _f32(scale).value
 
 
 def _prompt(q, k, v, starts, causal, scale, out, lse, stream):

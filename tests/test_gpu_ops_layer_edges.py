@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import layer_reference as R
-from paper_2607_11262_amd import ops
+from paper_2607_11262_amd import api, ops
 from test_gpu_ops_layer import BF, F, HF, TYPES, close, d64, gen, prompt_case, randn
 
 pytestmark = pytest.mark.gpu
@@ -238,3 +238,19 @@ def test_prompt_gradient_of_equal_weights_of_many_keys(D):
     off = p * 2 * (D + 4) * R.E * (do[few].abs() @ vd.abs().T.contiguous() + (do[few] * o[few, 0].double()).abs().sum(1, keepdim=True))
     err = (R.U[HF] + steps) * sizes + (off + 2.0 ** -33 * ds.abs().amax(1, keepdim=True)) @ kd.abs() * D ** -0.5
     close(dq[few, 0], ref.cpu(), err.cpu(), HF, "dq")
+
+
+# ---- refusals ------------------------------------------------------------------------------------
+
+def test_numbers_that_no_field_takes_are_refused():
+    x, q = torch.zeros(4, 16, device="cuda"), torch.zeros(4, 2, 0, device="cuda")
+    lse = torch.zeros(4, 2, device="cuda")
+    for eps in (1e300, -1e300, math.inf):
+        with pytest.raises(api.GtsError):
+            ops.layer_norm(x, eps=eps)
+    for eps in ("small", None):
+        with pytest.raises(TypeError):
+            ops.layer_norm(x, eps=eps)
+    for f in (lambda: ops.prompt_attention(q, q, q), lambda: ops.prompt_attention_backward(q, q, q, q, q, lse)):
+        with pytest.raises(api.GtsError, match="head dim 0"):
+            f()
