@@ -343,24 +343,27 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(NormGradParams p) {
   if (p.db) p.db[(uint64_t)blockIdx.y * a.dim + at] = db;
 }
 
-// The team of a row: lanes, and the accesses of 16 bytes that each makes.
+// The team of a row: the fewest lanes whose registers hold it, with 16 values a lane (16 or 64 lanes) or 32.
+template <int L>
+constexpr uint32_t kMost = L < 256 ? L * kHeld / 2 : L * kHeld;  // values of a row
+static_assert(kMost<512> == kLongest, "the largest team holds the longest row");
+uint32_t lanes_of(uint32_t dim) { return dim <= kMost<16> ? 16 : dim <= kMost<64> ? 64 : dim <= kMost<256> ? 256 : 512; }
+
+// The accesses of 16 bytes that each lane makes.  Shorter rows (up to `below`) have a smaller team.
 template <template <typename, int, int, int> class K, typename T, int L, typename P>
 void launch_lanes(const P& p, uint32_t dim, uint32_t groups, hipStream_t s) {
   constexpr int V = 16 / sizeof(T), C = kHeld / V;
-  if (dim <= L * V * (C / 4))
-    K<T, V, L, C / 4>::go(p, groups, s);
-  else if (dim <= L * V * (C / 2))
-    K<T, V, L, C / 2>::go(p, groups, s);
-  else
-    K<T, V, L, C>::go(p, groups, s);
+  constexpr uint32_t below = L == 16 ? 0 : L == 64 ? kMost<16> : L == 256 ? kMost<64> : kMost<256>;
+  if constexpr (below < L * kHeld / 4)
+    if (dim <= L * kHeld / 4) return K<T, V, L, C / 4>::go(p, groups, s);
+  if constexpr (below < L * kHeld / 2)
+    if (dim <= L * kHeld / 2) return K<T, V, L, C / 2>::go(p, groups, s);
+  if constexpr (kMost<L> > L * kHeld / 2) K<T, V, L, C>::go(p, groups, s);
 }
 // Rows that teams take: neither longer than they hold nor shorter than an access.
 template <typename T>
 bool held(uint32_t dim) {
   return dim <= kLongest && dim >= 16 / sizeof(T);
-}
-uint32_t lanes_of(uint32_t dim) {
-  return dim <= 16 * kHeld / 2 ? 16 : dim <= 64 * kHeld / 2 ? 64 : dim <= 256 * kHeld ? 256 : 512;
 }
 template <template <typename, int, int, int> class K, typename T, typename P>
 void launch_team(const P& p, uint32_t dim, uint32_t groups, hipStream_t s) {

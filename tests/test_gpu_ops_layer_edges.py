@@ -254,3 +254,22 @@ def test_numbers_that_no_field_takes_are_refused():
     for f in (lambda: ops.prompt_attention(q, q, q), lambda: ops.prompt_attention_backward(q, q, q, q, q, lse)):
         with pytest.raises(api.GtsError, match="head dim 0"):
             f()
+
+
+# ---- norm: widths at the limits of the kernels -----------------------------------------------------
+
+@pytest.mark.parametrize("center", [True, False])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("limit", [4, 8, 128, 256, 512, 1024, 2048, 4096, 8192, 16384])
+def test_norm_widths_about_the_limits(limit, dtype, center):
+    for dim in (limit - 1, limit, limit + 1):
+        g = gen(dim)
+        x, dy, w, b = (randn(g, *s, dtype=dtype) for s in ((5, dim), (5, dim), (dim,), (dim,)))
+        mean, rstd = torch.empty(5, device="cuda") if center else None, torch.empty(5, device="cuda")
+        y = ops.layer_norm(x.cuda(), w.cuda(), b.cuda(), eps=1e-3, center=center, mean=mean, rstd=rstd)
+        ref = R.norm(*d64(x, w, b), 1e-3, center)
+        close(y, ref[0], ref[3], dtype, f"y of {dim}")
+        got = ops.layer_norm_backward(dy.cuda(), x.cuda(), w.cuda(), rstd, mean, bias=True)
+        refs = R.norm_gradient(*d64(dy, x, w, mean, rstd))
+        for a, r, e, name in zip(got, refs, refs[3:], ("dx", "dw", "db")):
+            close(a, r, e, dtype, f"{name} of {dim}")
