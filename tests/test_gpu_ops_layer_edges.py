@@ -67,7 +67,8 @@ def norm_gradient_into(dy, x, weight, rstd, mean, dx):
 
 @pytest.mark.parametrize("center", [True, False])
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows,dim", [(50, 3), (300, 136), (9, 2048), (40, 8200), (70, 20000), (5, 16385)])
+@pytest.mark.parametrize("rows,dim", [(50, 3), (300, 136), (300, 137), (9, 2048), (9, 2045), (40, 8200), (40, 8201),
+                                      (70, 20000), (5, 16385)])
 def test_norm_gradient_in_place(rows, dim, dtype, center):
     g = gen(rows + dim)
     x, dy, w = (t.cuda() for t in (randn(g, rows, dim, dtype=dtype, shift=0.5), randn(g, rows, dim, dtype=dtype), randn(g, dim, dtype=dtype)))
@@ -273,3 +274,28 @@ def test_norm_widths_about_the_limits(limit, dtype, center):
         refs = R.norm_gradient(*d64(dy, x, w, mean, rstd))
         for a, r, e, name in zip(got, refs, refs[3:], ("dx", "dw", "db")):
             close(a, r, e, dtype, f"{name} of {dim}")
+
+
+# ---- products: in place ------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,N,K", [(5, 72, 48), (5, 71, 48), (150, 136, 264), (150, 135, 264), (40, 24, 3000), (700, 512, 64)])
+def test_products_in_place(M, N, K, dtype):
+    """out over gate or residual, and in the C call of the gradient dz over dy: the bits of a result apart."""
+    g = gen(M + N + K)
+    x, w, gate, res, dy, z = (randn(g, *s, dtype=dtype).cuda() for s in ((M, K), (N, K), (M, N), (M, N), (M, N), (M, N)))
+    want = ops.linear(x, w, activation="gelu", gate=gate, residual=res)
+    for which in ("gate", "residual"):
+        t = dict(gate=gate.clone(), residual=res.clone())
+        out = t[which]
+        assert ops.linear(x, w, activation="gelu", out=out, **t) is out and torch.equal(out, want), which
+    scratch = torch.empty(ops._scratch_of("gts_linear_backward_scratch", M, N), device="cuda", dtype=torch.uint8)
+    results = []
+    for dz in (torch.empty_like(dy), dy):
+        dgate, dbias = torch.empty_like(dy), torch.empty(N, device="cuda", dtype=dtype)
+        ops._call("gts_linear_backward", ops._pack_linear_grad(
+            dy.data_ptr(), z.data_ptr(), gate.data_ptr(), dz.data_ptr(), dgate.data_ptr(), dbias.data_ptr(), N, N, N, N, N, M, N,
+            ops._TYPES[dtype], ops.ACTIVATIONS["gelu"], scratch.data_ptr(), scratch.numel()), torch.cuda.current_stream().cuda_stream)
+        results.append((dz, dgate, dbias))
+    for a, b, name in zip(*results, ("dz", "dgate", "dbias")):
+        assert torch.equal(a, b), name
