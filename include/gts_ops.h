@@ -204,7 +204,7 @@ int gts_layer_norm_backward_scratch(uint32_t rows, uint32_t dim, uint64_t *bytes
  *   out = act(z) gate + residual.
  * bias [n], gate and residual [m][n] may be NULL.  preact (NULL or [m][n])
  * receives z for the backward pass.  Everything up to out is in 32 bits.  out may be
- * gate or residual with the same stride. */
+ * gate or residual with the same stride; out and preact share no other memory. */
 typedef struct gts_matmul_args {
   const void *a, *b;
   void *out, *preact;

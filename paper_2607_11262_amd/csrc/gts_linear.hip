@@ -88,9 +88,9 @@ __device__ __forceinline__ void finish(const gts_matmul_args& a, uint32_t m, uin
 // 64 R; 32 places of the sum at a time go through registers to LDS, their loads two stages ahead of
 // the products.  The smaller tile is for small results, where more workgroups a CU hide the loads
 // (1021 x 1000 x 777 in 32 bits: 51 us in the larger, 25 in this).  In 32 bits bound by matrix issue, a
-// sixteenth of the 16-bit rate (4096 x 4096 x 4096 1022 us, 134 TFLOP/s; a library product 1033; with
+// sixteenth of the 16-bit rate (4096 x 4096 x 4096 1021 us, 135 TFLOP/s; a library product 997; with
 // loads one stage ahead, in one loop with those of the edges, 1140); in 16 bits by the way through
-// registers (4095 x 4097 x 4099 355 us, 387 TFLOP/s).
+// registers (4095 x 4097 x 4099 333 us, 413 TFLOP/s).
 constexpr uint32_t kTileK = 32;
 
 // LDS of an operand's 64 R rows (or columns) and 32 places: rows of 8 values (16 bytes) more than they
@@ -243,8 +243,8 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulParams p) {
 // fragments of a step are read while the one before is multiplied, also across stages, and the
 // one barrier of a stage stands where its last fragments have been read: there the next
 // stage has arrived, and the one behind it may be loaded over this one.  Bound by matrix issue,
-// which is busy 58 % of the time: 8192 x 8192 x 8192 in bfloat16 948 us with rows x rows (1160 TFLOP/s), 867
-// with b by columns, 865 with both; 4096 x 4096 x 4096 114 us.  Stages of 32 places, four in turn, reached
+// which is busy 59 % of the time: 8192 x 8192 x 8192 in bfloat16 955 us with rows x rows (1151 TFLOP/s), 915
+// with b by columns, 920 with both; 4096 x 4096 x 4096 123 us.  Stages of 32 places, four in turn, reached
 // 1050 TFLOP/s with rows x rows where these reached 1204.
 constexpr uint32_t kStage = 64;
 constexpr int kSteps = kStage / 16;
@@ -710,7 +710,7 @@ hipError_t launch_matmul_t(const gts_matmul_args& a, hipStream_t s) {
 
 // ---- the elementwise part of the gradient ------------------------------------------------
 // A wave takes 64 V columns of a strip of rows, and keeps its part of dbias in registers.  Two rows are
-// on their way at a time; bound by HBM (2048 x 14336 with silu and gate in bfloat16, 294 MB: 54 us, 5.4 TB/s).
+// on their way at a time; bound by HBM (2048 x 14336 with silu and gate in bfloat16, 294 MB: 55 us, 5.3 TB/s).
 struct LinearGradParams {
   gts_linear_grad_args a;
   float* db;  // [strips][n], NULL if not wanted

@@ -15,9 +15,9 @@
 // are summed there too.
 //
 // Bound by matrix and vector issue (the exponentials, conversions and maxima of a tile take about as
-// long as its products): 8 x 4096 tokens of 32 heads of 128 in bfloat16 2305 us forward (954 TFLOP/s;
-// a large product reaches 1229), 8 causal texts of 512 to 8192 tokens, 32 / 8 heads, 2069 us backward
-// (517 TFLOP/s of the five products).
+// long as its products): 8 x 4096 tokens of 32 heads of 128 in bfloat16 2423 us forward (908 TFLOP/s;
+// a large library product reached 1369 on the same card), 8 causal texts of 512 to 8192 tokens, 32 / 8 heads,
+// 2211 us backward (483 TFLOP/s of the five products).
 #include "gts_ops.h"
 #include "gts_tile.h"
 
@@ -68,7 +68,7 @@ __device__ __forceinline__ bool find_span(const int32_t* starts, uint32_t batch,
 // Any type, head, stride and alignment.  128 rows (or keys) a workgroup, 32 a wave, which
 // holds their operands in registers; 32 keys (or rows) at a time go through registers to
 // LDS.  In 32 bits the matrix rate is a sixteenth; what is left is bound by the way to LDS and its
-// barriers (one causal prompt, 32 bits: 4096 tokens, 16 / 4 heads of 64 566 us forward, 2865 backward;
+// barriers (one causal prompt, 32 bits: 4096 tokens, 16 / 4 heads of 64 541 us forward, 2872 backward;
 // 3807 with all query heads of a key-value head in one workgroup).
 constexpr uint32_t kRows = 128, kStep = 32;
 constexpr uint32_t kKeys = 64;  // keys of a workgroup of dkv_tile_kernel
@@ -243,7 +243,8 @@ __global__ __launch_bounds__(256) void prompt_kernel(PromptParams p) {
 
 // ---- the tile kernels ---------------------------------------------------------------------
 // 16-bit values whose rows are aligned to 16 bytes, heads of whole 16 bytes.  As the general
-// kernels (8 x 4096 tokens, 32 heads of 128: 6758 us there, 2305 here), with tiles of 64 rows of two matrices (keys and values, or queries and dout) that
+// kernels (8 x 4096 tokens, 32 heads of 128: 6758 us there, 2305 here when both were timed), with tiles
+// of 64 rows of two matrices (keys and values, or queries and dout) that
 // go straight to LDS while the tile before is worked on: one barrier a tile.
 constexpr uint32_t kTile = 64;
 
@@ -656,8 +657,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void prompt_tile_kernel(Pro
 // size nothing bounds.  So p is lifted by 2^10 (lse is 10 less in base 2), and ds scaled by a power of
 // two of the lane's, whose row (dq) or key (dk) the sums are: the first that is not 0 to 2^8, and less
 // when one has grown past 2^15.  The sums take both back in 32 bits.  bfloat16 has the range of
-// 32 bits.  Largest, scaling and their registers cost 3 % of the gradient (4 x 2048 tokens, 16 heads of
-// 128: 659 us without, 680 with), 11 % with heads of 256 (2 x 4096 causal, 16 / 4 heads: 2462, 2736).
+// 32 bits.  Largest, scaling and their registers cost 4 % of the gradient (4 x 2048 tokens, 16 heads of
+// 128: 706 us without, 736 with), 11 % with heads of 256 (2 x 4096 causal, 16 / 4 heads: 2498, 2779).
 template <typename T>
 constexpr float kLift = __is_same(T, _Float16) ? 10.f : 0.f;
 
@@ -1160,7 +1161,7 @@ __device__ __forceinline__ void load_to_lds4(const void* from, void* to) {
 // at the end.  dv and dk take a kernel each (`DV`), which computes the scores once more but leaves
 // registers for two waves a SIMD, one of which computes weights while the other multiplies.
 // Heads of 256 take two passes of 128 columns each, for which there are registers.  8 packed texts of
-// 512 to 8192 tokens, 32 / 8 heads of 128: dq 692, dk 804 and dv 624 us (the whole gradient took
+// 512 to 8192 tokens, 32 / 8 heads of 128: dq 729, dk 819 and dv 654 us under the profiler (the whole gradient took
 // 2604 with one kernel for both, one wave a SIMD; 2360 with two).
 template <int DP>
 constexpr int kBlocks = DP / 32 < 4 ? DP / 32 : 4;

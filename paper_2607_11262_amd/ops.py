@@ -723,7 +723,7 @@ def _rows(t):
 def layer_norm(x, weight=None, bias=None, *, eps=1e-5, center=True, out=None, mean=None, rstd=None, stream=None):
     """Rows of x [..., dim] with their mean taken off and divided by the root of
     their mean square plus eps, times weight [dim], plus bias [dim]; without `center`
-    the mean stays (RMS norm).  out=x writes over x.  mean and rstd (float32, one
+    the mean stays (RMS norm).  out=x writes over x (another overlap of the two mixes rows).  mean and rstd (float32, one
     a row) receive what layer_norm_backward takes.  Differentiable once in x, weight and
     bias by reverse mode (out, mean and rstd are then refused)."""
     _no_tangent_of("a tensor of the norm", x, weight, bias)
@@ -848,8 +848,8 @@ def linear(x, weight, bias=None, *, activation=None, gate=None, residual=None, o
     [N, K], bias [N]; gate and residual have the result's shape [..., N].  `activation` is
     None, "relu", "gelu" (by the normal distribution), "gelu_tanh" or "silu"; with gate
     the result is that of a gated layer.  All of it is computed in 32 bits and rounded
-    once.  out may be gate or residual; preact (of the result's shape and type)
-    receives x weight^T + bias for linear_backward.  Differentiable once in x, weight,
+    once.  out may be gate or residual, and shares no memory with x, weight or bias; preact (of
+    the result's shape and type) receives x weight^T + bias for linear_backward, and shares none with any.  Differentiable once in x, weight,
     bias, gate and residual by reverse mode (out and preact are then refused)."""
     act = _activation(activation)
     _no_tangent_of("a tensor of the product", x, weight, bias, gate, residual)
