@@ -299,3 +299,31 @@ def test_products_in_place(M, N, K, dtype):
         results.append((dz, dgate, dbias))
     for a, b, name in zip(*results, ("dz", "dgate", "dbias")):
         assert torch.equal(a, b), name
+
+
+# ---- streams -------------------------------------------------------------------------------------------
+
+def test_a_call_on_another_stream_behind_late_inputs():
+    """Inputs whose work on the current stream is late, a wait behind them, a call on a side stream, the
+    inputs dropped at once: the caller's order holds."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(300, 256, generator=g, device="cuda").to(BF)
+    w = torch.randn(512, 256, generator=g, device="cuda").to(BF)
+    q = torch.randn(300, 4, 64, generator=g, device="cuda").to(BF)
+    lse = torch.empty(300, 4, device="cuda")
+    o = ops.prompt_attention(q, q, q, lse=lse)
+    want = [ops.layer_norm(x), ops.linear(x, w), o, *ops.prompt_attention_backward(q, q, q, q, o, lse)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(5):
+        torch.cuda._sleep(200_000)
+        cx, cw, cq, co, cl = (t.clone() for t in (x, w, q, o, lse))
+        side.wait_stream(torch.cuda.current_stream())
+        got = [ops.layer_norm(cx, stream=side), ops.linear(cx, cw, stream=side), ops.prompt_attention(cq, cq, cq, stream=side),
+               *ops.prompt_attention_backward(cq, cq, cq, cq, co, cl, stream=side)]
+        del cx, cw, cq, co, cl
+        trash = [torch.full((n,), 9.0, device="cuda") for n in (300 * 128, 512 * 128, 300 * 128, 1200)]
+        torch.cuda.synchronize()
+        del trash
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
