@@ -619,10 +619,10 @@ float cost_of(const TileCost& c, uint32_t m, uint32_t n, uint32_t k, uint32_t sp
 // kLargeTiles: a is stored by columns, of which a tile has 128 at least.
 enum Kind { kGeneral, kTiles, kLargeTiles, kGeneral32 };
 Cut cut_of(uint32_t m, uint32_t n, uint32_t k, Kind kind) {
-  Cut best{0, 1};
-  float least = INFINITY;
   const uint32_t from = kind == kGeneral ? 4 : kind == kGeneral32 ? 6 : 0;
   const uint32_t to = kind == kGeneral ? 6 : kind == kGeneral32 ? 8 : kind == kTiles ? 4 : 3;
+  Cut best{from, 1};
+  float least = INFINITY;
   for (uint32_t t = from; t < to; ++t)
     for (const uint32_t splits : {1u, 2u, 3u, 4u, 6u, 8u, 12u, 16u, 24u, 32u}) {
       if (splits > 1 && splits * 128 > k) break;
